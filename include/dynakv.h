@@ -371,6 +371,95 @@ void dynakv_destroy(dynakv_ctx* ctx);
 int dynakv_attend_rows_noalloc(const float* q, const void* K, const void* V, int32_t n_units, int64_t n,
                                int32_t gqa_group, int32_t d, int32_t kv_dtype, float* out, void* cuda_stream);
 
+/* ---- Plain rows beside the clustered index (the paper has no counterpart) ------------------------------------------
+ *
+ * What a serving program does with keys, values and queries before they are in the index or while they must stay
+ * outside it: the norm and rotary embedding that make the q, k that dynakv_append and dynakv_decode_step take; a paged
+ * cache for prompts that are still being prefilled, for sequences too short to be clustered, for layers left dense, and
+ * for drafted tokens (an append cannot be taken back, so a draft waits here until it is accepted); attention over such
+ * a cache for one new token or for a tree of drafted ones; and reading the rows back as the arrays dynakv_build_index
+ * takes.
+ *
+ * These calls need no context and allocate nothing.  They enqueue work on cuda_stream (a cudaStream_t, NULL = default
+ * stream) of the CURRENT device, where all pointers must live, and return at once; they can be captured into a CUDA
+ * graph.  Host-detectable problems return a negative code and enqueue nothing.  What only the device can see -- a page
+ * id, slot, length or row range outside its array -- never faults: the access is skipped and DYNAKV_ST_BOUNDS is OR-ed
+ * into *status (a device word, may be NULL; the calls never clear it).  Arrays written must not overlap arrays read. */
+
+/* A paged cache.  k, v: [n_pages][n_kv_heads][32][head_dim] in kv_dtype, 16-byte aligned; with DYNAKV_FP8 the elements
+ * are e4m3 bytes and k_exp, v_exp ([n_pages][n_kv_heads][32], 16-byte aligned, else NULL) hold one scale exponent per
+ * row: element = e4m3 value * 2^exp (exp in [-120, 120]).  Slot s is row s % 32 of page s / 32, for every KV head.
+ * head_dim 64 or 128 with every kv_dtype; n_pages * n_kv_heads * 32 < 2^31. */
+typedef struct dynakv_row_cache {
+    void* k;
+    void* v;
+    int8_t* k_exp;
+    int8_t* v_exp;
+    int64_t n_pages;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t kv_dtype;
+} dynakv_row_cache;
+
+/* A [n][heads][head_dim] array, DYNAKV_F32 or DYNAKV_BF16: element e of head h of token t is at
+ * data[t * token_stride + h * head_stride + e].  Strides are in elements (a slice of a joint projection is fine);
+ * data is aligned to its element. */
+typedef struct dynakv_head_rows {
+    const void* data;
+    int64_t token_stride;
+    int64_t head_stride;
+    int32_t dtype;
+} dynakv_head_rows;
+
+/* Norm and rotary embedding of a model's heads.  Every head x of q (and of k) becomes
+ *     y = x * rsqrt(mean(x^2) + eps) * weight           (weight NULL: y = x)
+ * and its first rotary_dim elements are then rotated in pairs by angle = position * inv_freq[i], i < rotary_dim / 2:
+ *     (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin),
+ * a = i, b = i + rotary_dim / 2, or with interleaved != 0 a = 2 i, b = 2 i + 1.  The product and its reduction by whole
+ * turns are taken in 64 bits, everything else in fp32, with one rounding to the type of the result.
+ * rotary_dim is a multiple of 16, 0 .. head_dim.  q_weight, k_weight [head_dim] and inv_freq [rotary_dim / 2] are DEVICE
+ * fp32 arrays. */
+typedef struct dynakv_rotary {
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;          /* 64 or 128 */
+    int32_t rotary_dim;
+    int32_t interleaved;
+    float eps;                 /* >= 0 */
+    const float* q_weight;
+    const float* k_weight;
+    const float* inv_freq;
+} dynakv_rotary;
+
+/* q_out [n][n_heads][d] and k_out [n][n_kv_heads][d], contiguous, of q_dtype and k_dtype (DYNAKV_F32 or DYNAKV_BF16, each
+ * independent of the inputs' type) from q, k (of one dtype) and positions [n] (int32).  With one token per sequence,
+ * q_out in fp32 is the q of dynakv_decode_step and k_out the k of dynakv_append.  n >= 0. */
+int dynakv_norm_rope(const dynakv_rotary* rotary, const dynakv_head_rows* q, const dynakv_head_rows* k,
+                     const int32_t* positions, int64_t n, void* q_out, int32_t q_dtype, void* k_out, int32_t k_dtype,
+                     void* cuda_stream);
+
+/* The same pass with the keys, and the values v beside them, going into slots of a cache instead of an array: row t of
+ * every KV head goes to slot slots[t] as dynakv_rows_write stores it, rounded once from the fp32 result. */
+int dynakv_norm_rope_store(const dynakv_rotary* rotary, const dynakv_head_rows* q, const dynakv_head_rows* k,
+                           const dynakv_head_rows* v, const int32_t* positions, int64_t n, void* q_out, int32_t q_dtype,
+                           const dynakv_row_cache* cache, const int32_t* slots, uint32_t* status, void* cuda_stream);
+
+/* Rows k, v ([n][n_kv_heads][d], of one dtype, any cache type) into slots of the cache, rounded to its type; FP8 rows by
+ * the rule of DYNAKV_FP8 (smallest 2^e with max|x| / 2^e <= 448, e clamped to [-120, 120], 0 for a zero row, round to
+ * nearest even; NaN stays NaN and does not count for the maximum, an infinite element makes e 120 and reads back as an infinity).  A
+ * negative slot skips its token; a slot beyond the cache skips it and sets DYNAKV_ST_BOUNDS.  The slots >= 0 of one call
+ * must differ: of a slot named twice the rows are unspecified. */
+int dynakv_rows_write(const dynakv_row_cache* cache, const dynakv_head_rows* k, const dynakv_head_rows* v,
+                      const int32_t* slots, int64_t n, uint32_t* status, void* cuda_stream);
+
+/* Rows [first, first + n) of n_seqs sequences in order: K_out, V_out [n_seqs][n_kv_heads][n][d], contiguous, 16-byte
+ * aligned, fp32 for a DYNAKV_F32 cache, else bf16 (exact).  Row r of sequence b is in page page_table[b][r / 32]
+ * (int32 [n_seqs][pages_per_seq]); rows at or past lengths[b] are zeros.  With n_seqs sequences of one layer the result
+ * is the K, V of dynakv_build_index for U = n_seqs * n_kv_heads units.  n_seqs <= 65535. */
+int dynakv_rows_read(const dynakv_row_cache* cache, const int32_t* page_table, int32_t pages_per_seq,
+                     const int32_t* lengths, int32_t n_seqs, int64_t first, int64_t n, void* K_out, void* V_out,
+                     uint32_t* status, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,93 @@
+// Rows of single heads as the calls on plain rows see them: eight consecutive elements per lane, head_dim / 8 lanes per
+// row, loaded from strided fp32 / bf16 arrays and stored as fp32, bf16 or e4m3 with the row's power-of-two scale.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "fp8_rows.cuh"
+
+namespace dkv {
+
+// Eight consecutive elements of a strided array.  vec: base and strides keep every row 16-byte aligned; else the
+// elements are loaded one by one.
+__device__ __forceinline__ void load8(const float* p, bool vec, float (&x)[8]) {
+    if (vec) {
+        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = p[i];
+    }
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, bool vec, float (&x)[8]) {
+    if (vec) {
+        const uint4 a = *reinterpret_cast<const uint4*>(p);
+        const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = __bfloat162float(p[i]);
+    }
+}
+
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const unsigned*>(&v);
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
+// fp8_row_exp for any largest magnitude, an infinite one included (which gives 120): from the bits of amax, whose NaNs
+// the maximum has dropped.  amax = 1.m * 2^(field - 127); 448 = 1.75 * 2^8.  Subnormals land below the clamp.
+__device__ __forceinline__ int row_exp_any(float amax) {
+    if (!(amax > 0.f)) return 0;
+    const unsigned b = __float_as_uint(amax);
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return max(-120, min(120, e));
+}
+
+// The eight elements of this lane into a cache row (`row`: its index in the whole pool).  All lanes of the row's group
+// call it together; the maximum of an FP8 row is exchanged inside the group of HD / 8 lanes.
+template <int HD>
+__device__ __forceinline__ void store_cache8(const dynakv_row_cache& c, bool is_v, long long row, bool live, int l, const float (&x)[8]) {
+    constexpr int LG = HD / 8;
+    void* pool = is_v ? c.v : c.k;
+    const size_t at = (size_t)row * HD + l * 8;
+    if (c.kv_dtype == DYNAKV_F32) {
+        if (live) store8(reinterpret_cast<float*>(pool) + at, x);
+    } else if (c.kv_dtype == DYNAKV_BF16) {
+        if (live) store8(reinterpret_cast<__nv_bfloat16*>(pool) + at, x);
+    } else {
+        float m = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = fmaxf(m, fabsf(x[i]));
+        m = group_max(m, LG);
+        const int e = row_exp_any(m);
+        const float inv = pow2f(-e);
+        uint2 b;
+        b.x = fp8_pack2(x[0], x[1], inv) | ((unsigned)fp8_pack2(x[2], x[3], inv) << 16);
+        b.y = fp8_pack2(x[4], x[5], inv) | ((unsigned)fp8_pack2(x[6], x[7], inv) << 16);
+        if (live) {
+            *reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(pool) + at) = b;
+            if (l == 0) (is_v ? c.v_exp : c.k_exp)[row] = (int8_t)e;
+        }
+    }
+}
+
+// Host side: what every call on a cache checks.
+static inline bool row_cache_ok(const dynakv_row_cache* c) {
+    if (!c || !c->k || !c->v || c->n_pages < 1 || c->n_kv_heads < 1 || (c->head_dim != 64 && c->head_dim != 128)) return false;
+    if (c->kv_dtype != DYNAKV_F32 && c->kv_dtype != DYNAKV_BF16 && c->kv_dtype != DYNAKV_FP8) return false;
+    if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return false;
+    if (c->kv_dtype == DYNAKV_FP8 && (!c->k_exp || !c->v_exp || (((uintptr_t)c->k_exp | (uintptr_t)c->v_exp) & 15))) return false;
+    return c->n_pages < (1ll << 31) && c->n_pages * c->n_kv_heads < (1ll << 26);      // rows of 32-row pages fit 31 bits
+}
+
+}  // namespace dkv

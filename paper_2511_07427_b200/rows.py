@@ -1,0 +1,247 @@
+"""Plain rows beside the clustered index: norm and rotary embedding of heads, a paged row cache, tree attention over it.
+
+Argument marshalling only, like the rest of the binding: every method is one C call (two launches for ``attend_tree``) on
+the stream that is current on the tensors' device.  Nothing synchronises, results and scratch come from torch's caching
+allocator (so calls on several streams, and calls captured into several CUDA graphs, never share scratch).  The calls
+compute no gradients and refuse inputs that would need one.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+from .binding import BF16, F32, FP8, DynaKVError, load_library
+
+PAGE = 32          # rows per cache page
+MAX_TREE = 256     # drafted tokens per sequence and call
+
+
+class _RowCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("n_pages", C.c_int64),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("kv_dtype", C.c_int32)]
+
+
+class _HeadRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("dtype", C.c_int32)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("rotary_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+                ("inv_freq", C.c_void_p)]
+
+
+_vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
+SIGNATURES = {
+    "dynakv_norm_rope": (C.c_int, [_vp, _vp, _vp, _vp, _i64, _vp, _i32, _vp, _i32, _vp]),
+    "dynakv_norm_rope_store": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _i64, _vp, _i32, _vp, _vp, _vp, _vp]),
+    "dynakv_rows_write": (C.c_int, [_vp, _vp, _vp, _vp, _i64, _vp, _vp]),
+    "dynakv_rows_read": (C.c_int, [_vp, _vp, _i32, _vp, _i32, _i64, _i64, _vp, _vp, _vp, _vp]),
+}
+_bound = None
+
+
+def _library():
+    global _bound
+    if _bound is None:
+        L = load_library()
+        for name, (res, args) in SIGNATURES.items():
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = res, args
+        _bound = L
+    return _bound
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _float_type(dtype, what: str) -> int:
+    torch = _torch()
+    if dtype == torch.bfloat16:
+        return BF16
+    if dtype == torch.float32:
+        return F32
+    raise DynaKVError(f"{what} is {dtype}: expected torch.float32 or torch.bfloat16")
+
+
+def _index(t, shape, device, what: str):
+    """A contiguous int32 tensor of `shape` on `device`."""
+    torch = _torch()
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise DynaKVError(f"expected {what} as a contiguous int32 tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _heads(t, n: int, heads: int, d: int, device, dtype, what: str) -> _HeadRows:
+    """A [n, heads, d] tensor whose last dimension is contiguous; the other strides are free."""
+    if tuple(t.shape) != (n, heads, d) or t.device != device or t.dtype != dtype or (t.stride(2) != 1 and d > 1):
+        raise DynaKVError(f"expected {what} as a {dtype} tensor of shape {(n, heads, d)} on {device} with a contiguous last dimension, "
+                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {tuple(t.stride())}")
+    return _HeadRows(t.data_ptr(), t.stride(0), t.stride(1), _float_type(dtype, what))
+
+
+def _no_gradient(*tensors) -> None:
+    if _torch().is_grad_enabled() and any(t.requires_grad for t in tensors):
+        raise DynaKVError("this call computes no gradients: detach its inputs or run it under torch.no_grad()")
+
+
+def _call(device, name: str, *args) -> None:
+    """One C call on the device's current stream (its last argument), with the device made current when it is not."""
+    torch = _torch()
+    fn = getattr(_library(), name)
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if rc != 0:
+        raise DynaKVError(f"{name} returned {rc}")
+
+
+def _on_cuda(t, what: str):
+    if not t.is_cuda:
+        raise DynaKVError(f"{what} is on {t.device}: expected a CUDA tensor (there is no CPU fallback)")
+    return t.device
+
+
+class HeadRotary:
+    """Norm and rotary embedding of a model's heads (``dynakv_norm_rope``).
+
+    ``inv_freq`` [rotary_dim / 2] fp32: the angle of pair i at position p is p * inv_freq[i], taken in 64 bits;
+    ``q_weight``, ``k_weight`` [head_dim] fp32: RMS norm of every head before the rotation (None: no norm).  Pairs are
+    (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with ``interleaved``; elements past rotary_dim are only normed."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 interleaved: bool = False):
+        torch = _torch()
+        self.n_heads, self.n_kv_heads, self.head_dim = int(n_heads), int(n_kv_heads), int(head_dim)
+        if self.n_heads < 1 or self.n_kv_heads < 1 or self.head_dim not in (64, 128):
+            raise DynaKVError(f"expected at least one query and KV head of 64 or 128 elements, got {n_heads}, {n_kv_heads}, {head_dim}")
+        if not (eps >= 0.0 and math.isfinite(eps)):
+            raise DynaKVError(f"eps is {eps}: expected a number >= 0")
+        rotary_dim = 2 * inv_freq.numel()
+        if rotary_dim > self.head_dim or rotary_dim % 16 != 0:
+            raise DynaKVError(f"inv_freq has {inv_freq.numel()} elements: rotary_dim = {rotary_dim} has to be a multiple of 16 up to head_dim")
+        self.device = _on_cuda(inv_freq, "inv_freq")
+        for name, w, numel in (("inv_freq", inv_freq, rotary_dim // 2), ("q_weight", q_weight, self.head_dim), ("k_weight", k_weight, self.head_dim)):
+            if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (numel,) or not w.is_contiguous() or w.device != self.device):
+                raise DynaKVError(f"expected {name} as a contiguous float32 tensor of {numel} elements on {self.device}, got {w.dtype} {tuple(w.shape)} on {w.device}")
+        self._tensors = (inv_freq, q_weight, k_weight)
+        self._c = _Rotary(self.n_heads, self.n_kv_heads, self.head_dim, rotary_dim, 1 if interleaved else 0, eps,
+                          q_weight.data_ptr() if q_weight is not None else None,
+                          k_weight.data_ptr() if k_weight is not None else None,
+                          inv_freq.data_ptr() if rotary_dim else None)
+        self._ref = C.byref(self._c)
+
+    def _q_k(self, q, k):
+        n = q.shape[0]
+        _no_gradient(q, k)
+        return n, _heads(q, n, self.n_heads, self.head_dim, self.device, q.dtype, "q"), \
+            _heads(k, n, self.n_kv_heads, self.head_dim, self.device, q.dtype, "k")
+
+    def apply(self, q, k, positions, q_dtype=None, k_dtype=None):
+        """q [n, heads, d], k [n, KV heads, d] (fp32 or bf16, any token and head strides), positions [n] int32 ->
+        (q, k) normed and rotated, contiguous, of ``q_dtype`` and ``k_dtype`` (default: the input's).  With one token per
+        sequence an fp32 q is what ``DynaKV.decode_step`` takes and k what ``DynaKV.append`` takes, as [U, G, d] and
+        [U, d] views."""
+        torch = _torch()
+        n, qr, kr = self._q_k(q, k)
+        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=q_dtype or q.dtype, device=self.device)
+        k_out = torch.empty((n, self.n_kv_heads, self.head_dim), dtype=k_dtype or q.dtype, device=self.device)
+        _call(self.device, "dynakv_norm_rope", self._ref, C.byref(qr), C.byref(kr), _index(positions, (n,), self.device, "positions"), n,
+              q_out.data_ptr(), _float_type(q_out.dtype, "q_dtype"), k_out.data_ptr(), _float_type(k_out.dtype, "k_dtype"))
+        return q_out, k_out
+
+    def store(self, q, k, v, positions, cache: "RowCache", slots, q_dtype=None):
+        """As ``apply``, with the keys and the values v [n, KV heads, d] going into ``slots`` [n] int32 of ``cache``
+        (``RowCache.write``'s rules) in the same launch.  Returns q."""
+        torch = _torch()
+        n, qr, kr = self._q_k(q, k)
+        _no_gradient(v)
+        vr = _heads(v, n, self.n_kv_heads, self.head_dim, self.device, q.dtype, "v")
+        if cache.device != self.device or cache.head_dim != self.head_dim or cache.n_kv_heads != self.n_kv_heads:
+            raise DynaKVError(f"the cache holds {cache.n_kv_heads} heads of {cache.head_dim} on {cache.device}, the embedding has "
+                              f"{self.n_kv_heads} of {self.head_dim} on {self.device}")
+        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=q_dtype or q.dtype, device=self.device)
+        _call(self.device, "dynakv_norm_rope_store", self._ref, C.byref(qr), C.byref(kr), C.byref(vr),
+              _index(positions, (n,), self.device, "positions"), n, q_out.data_ptr(), _float_type(q_out.dtype, "q_dtype"), cache._ref,
+              _index(slots, (n,), self.device, "slots"), cache._status.data_ptr())
+        return q_out
+
+
+class RowCache:
+    """A paged cache of K/V rows in fp32, bf16 or FP8 (``dynakv_row_cache``) around tensors the caller owns.
+
+    k, v: [pages, KV heads, 32, head_dim], contiguous; float32, bfloat16, or for FP8 float8_e4m3fn (or uint8) with
+    ``k_exp``, ``v_exp`` [pages, KV heads, 32] int8, the rows' power-of-two scales.  A slot is 32 * page + row.  What only
+    the device can see (a page id, slot or length out of range) is skipped and sets a bit that ``get_status`` reads."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        torch = _torch()
+        self.device = _on_cuda(k, "k")
+        if k.dim() != 4 or k.shape[2] != PAGE or k.shape[3] not in (64, 128) or k.numel() == 0:
+            raise DynaKVError(f"expected k of shape [pages, KV heads, {PAGE}, 64 or 128], got {tuple(k.shape)}")
+        types = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: FP8, torch.uint8: FP8}
+        if k.dtype not in types:
+            raise DynaKVError(f"k is {k.dtype}: expected float32, bfloat16 or float8_e4m3fn")
+        if v.dtype != k.dtype or v.shape != k.shape or v.device != k.device or not (k.is_contiguous() and v.is_contiguous()):
+            raise DynaKVError("expected k and v contiguous, of one type and shape on one device")
+        self.kv_dtype = types[k.dtype]
+        self.n_pages, self.n_kv_heads, _, self.head_dim = (int(x) for x in k.shape)
+        for name, e in (("k_exp", k_exp), ("v_exp", v_exp)):
+            if (e is None) != (self.kv_dtype != FP8):
+                raise DynaKVError(f"{name} goes with FP8 rows, and only with them")
+            if e is not None and (e.dtype != torch.int8 or tuple(e.shape) != tuple(k.shape[:3]) or not e.is_contiguous() or e.device != self.device):
+                raise DynaKVError(f"expected {name} as a contiguous int8 tensor of shape {tuple(k.shape[:3])} on {self.device}")
+        if self.n_pages * self.n_kv_heads >= 1 << 26:
+            raise DynaKVError(f"{self.n_pages} pages x {self.n_kv_heads} heads: a cache holds fewer than 2^26 of them")
+        if any(t is not None and t.data_ptr() % 16 for t in (k, v, k_exp, v_exp)):
+            raise DynaKVError("the cache's tensors have to be 16-byte aligned")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._c = _RowCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if k_exp is not None else None,
+                            v_exp.data_ptr() if v_exp is not None else None, self.n_pages, self.n_kv_heads, self.head_dim, self.kv_dtype)
+        self._ref = C.byref(self._c)
+
+    @classmethod
+    def allocate(cls, n_pages: int, n_kv_heads: int, head_dim: int, kv_dtype: int = BF16, device="cuda") -> "RowCache":
+        """A cache with tensors of its own, contents unspecified."""
+        torch = _torch()
+        if kv_dtype not in (F32, BF16, FP8):
+            raise DynaKVError(f"kv_dtype is {kv_dtype}: expected F32, BF16 or FP8")
+        shape = (n_pages, n_kv_heads, PAGE, head_dim)
+        dtype = {F32: torch.float32, BF16: torch.bfloat16, FP8: torch.float8_e4m3fn}[kv_dtype]
+        pools = [torch.empty(shape, dtype=dtype, device=device) for _ in range(2)]
+        exps = [torch.empty(shape[:3], dtype=torch.int8, device=device) for _ in range(2)] if kv_dtype == FP8 else []
+        return cls(*pools, *exps)
+
+    def get_status(self) -> int:
+        """The status bits set since the cache was made (``ST_BOUNDS``, ``ST_INTERNAL``).  Synchronises."""
+        return int(self._status.item())
+
+    def write(self, k, v, slots) -> None:
+        """Rows k, v [n, KV heads, d] (fp32 or bf16, any token and head strides) into ``slots`` [n] int32, rounded to the
+        cache's type.  A negative slot skips its token; slots >= 0 must differ."""
+        n = k.shape[0]
+        _no_gradient(k, v)
+        kr = _heads(k, n, self.n_kv_heads, self.head_dim, self.device, k.dtype, "k")
+        vr = _heads(v, n, self.n_kv_heads, self.head_dim, self.device, k.dtype, "v")
+        _call(self.device, "dynakv_rows_write", self._ref, C.byref(kr), C.byref(vr), _index(slots, (n,), self.device, "slots"), n,
+              self._status.data_ptr())
+
+    def read(self, page_table, lengths, n: int, first: int = 0):
+        """Rows [first, first + n) of every sequence in order, (K, V) of shape [sequences, KV heads, n, d], fp32 for an
+        fp32 cache, else bf16; zeros at and past ``lengths`` [sequences] int32.  ``page_table`` [sequences, pages per
+        sequence] int32.  As [U, n, d] views these are the K, V of ``DynaKV.build_index``."""
+        torch = _torch()
+        if page_table.dim() != 2 or n < 0 or first < 0:
+            raise DynaKVError(f"expected page_table of two dimensions, n >= 0 and first >= 0, got {tuple(page_table.shape)}, {n}, {first}")
+        b, per = page_table.shape
+        dtype = torch.float32 if self.kv_dtype == F32 else torch.bfloat16
+        K = torch.empty((b, self.n_kv_heads, n, self.head_dim), dtype=dtype, device=self.device)
+        V = torch.empty_like(K)
+        _call(self.device, "dynakv_rows_read", self._ref, _index(page_table, (b, per), self.device, "page_table"), per,
+              _index(lengths, (b,), self.device, "lengths"), b, first, n, K.data_ptr(), V.data_ptr(), self._status.data_ptr())
+        return K, V
