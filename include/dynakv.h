@@ -460,6 +460,32 @@ int dynakv_rows_read(const dynakv_row_cache* cache, const int32_t* page_table, i
                      const int32_t* lengths, int32_t n_seqs, int64_t first, int64_t n, void* K_out, void* V_out,
                      uint32_t* status, void* cuda_stream);
 
+/* Attention of newly drafted tokens over a paged cache: one token per sequence (plain decoding), a chain, or a tree.
+ *
+ * The tokens of all sequences are packed: sequence b has the T_b = q_start[b + 1] - q_start[b] tokens q_start[b] ..
+ * q_start[b + 1] - 1 of q, T_b <= max_tree (T_b = 0 skips the sequence).  Its kv_len[b] rows lie in page_table as for
+ * dynakv_rows_read; the LAST T_b of them are the drafted tokens' own (stored before this call), the others the
+ * context.  Token i of the tree sees every row of the context, and of the tree row j when bit j % 64 of
+ * tree_mask[q_start[b] + i][j / 64] is set (usually its ancestors and itself); tree_mask NULL: rows j <= i (a chain).
+ *     out[i][hq] = sum_j p_j v_j / sum_j p_j,  lse[i][hq] = ln sum_j p_j,  p_j = exp(scale * q[i][hq] . k_j)
+ * over the rows it sees, KV head hq / (n_heads / n_kv_heads); a token that sees no row gets zeros and -infinity.
+ * Rows it does not see do not count whatever they hold, NaN and infinities included.
+ *
+ * q, out: [n_tokens][n_heads][head_dim], contiguous and 16-byte aligned, fp32 for a DYNAKV_F32 cache, else bf16;
+ * lse: [n_tokens][n_heads] fp32, may be NULL.  Tokens at and behind q_start[n_seqs] are left as they were.  n_heads is 1 to 8 times n_kv_heads;
+ * max_tree 1 .. 256; tree_mask [n_tokens][mask_words], mask_words 1 .. 4 (rows past the last word are not seen).
+ * Logits, weights' sums and outputs are accumulated in fp32; FP8: V rows whose scale is below 2^-60 are summed with less
+ * relative precision.  No length is needed on the host, so one captured graph serves a growing cache.
+ * workspace: dynakv_attend_tree_workspace() bytes of device memory, 16-byte aligned, contents of no interest before
+ * and after; calls that may overlap (streams, graphs) need one each. */
+int dynakv_attend_tree(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
+                       int32_t n_seqs, int32_t max_tree, const int32_t* page_table, int32_t pages_per_seq,
+                       const int32_t* kv_len, const uint64_t* tree_mask, int32_t mask_words, float scale, void* out, float* lse,
+                       void* workspace, int64_t workspace_bytes, uint32_t* status, void* cuda_stream);
+
+/* Bytes of workspace for calls with this cache, n_heads and max_tree on the current device, or a negative code. */
+int64_t dynakv_attend_tree_workspace(const dynakv_row_cache* cache, int32_t n_heads, int32_t max_tree);
+
 #ifdef __cplusplus
 }
 #endif

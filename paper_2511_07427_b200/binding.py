@@ -24,6 +24,7 @@ EXPORTED_SYMBOLS = [
     "dynakv_attend_rows_noalloc", "dynakv_export_kv", "dynakv_import_state", "dynakv_decode_loop_host", "dynakv_selftest_wait_expiry", "dynakv_time_gather_attention",
     "dynakv_build_index_placed", "dynakv_get_work_list", "dynakv_work_list_capacity", "dynakv_get_tier_stats", "dynakv_checked_build",
     "dynakv_norm_rope", "dynakv_norm_rope_store", "dynakv_rows_write", "dynakv_rows_read",
+    "dynakv_attend_tree", "dynakv_attend_tree_workspace",
 ]
 ERR_TOO_LARGE = -5
 NOALLOC_SCRATCH_BYTES = 4 * 1024 * 1024

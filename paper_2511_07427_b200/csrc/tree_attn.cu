@@ -1,0 +1,965 @@
+// dynakv_attend_tree: attention of one new token, or of a tree of drafted tokens, over the rows of a paged cache.
+//
+//   out[i] = sum_j p_ij v_j / sum_j p_ij,   p_ij = exp(q_i . k_j * scale) where token i sees row j, else 0
+//
+// All G query heads of a KV head and all tokens of the tree share every row that is read, so a CTA works on a tile of
+// query rows (token, head of the group) at once: with R rows per KV head a row of K and V (512 bytes in bf16, d = 128) meets
+// 4 d R flops, and HBM bounds the call until R is in the tens.  tree_plan.cuh says how the pages are shared out.
+//
+// Kernel shape.  One producer warp streams whole 32-row pages, K and V, into a shared-memory ring with tiled TMA loads
+// (128-byte swizzle, so that the fragment loads below meet no bank conflicts; FP8 rows' exponents follow as two 32-byte
+// bulk copies).  The consumer warps are RG row groups x KG page groups: a row group holds 16 query rows, a page group takes
+// every KG-th page of the CTA's range with a softmax state of its own, merged through shared memory at a segment's end.
+// Few rows: three page groups hide the latency of a page's chain of dependent steps; 64 rows: four row groups share a
+// page, which divides its shared-memory traffic.  A ring stage is always consumed by the same page group (a parity
+// wait cannot tell a phase from the one after the next).
+//
+// Three consumers.  bf16 rows: mma.sync m16n8k16, fragments by ldmatrix; the weights are split into bf16 hi + lo (two MMAs),
+// because bf16 weights alone would add an error as large as the output's own rounding.  FP8 rows: the bytes become f16
+// operands (exact), q is divided by a power of two per row so that it fits f16, the K row's scale multiplies the logit, and
+// the V row's scale is folded into the softmax (running maximum over logit + exponent) as in the gather-attention kernel;
+// f16 weights round to 2^-12.  fp32 rows: fp32 FMAs, one lane per key for the logits, one lane per 4 columns for the sums.
+//
+// Masked rows never reach a sum.  Logits of rows that a token does not see are replaced by -inf.  Rows of V past the
+// sequence's length (whatever an earlier sequence left there) are zeroed in shared memory, and so are drafted rows that hold
+// a NaN or an infinity, because 0 * NaN would leak them into the tokens that do not see them; tokens that do see them get
+// their share added in fp32 at the end of the segment.
+#include <cuda.h>
+#include <atomic>
+#include <float.h>
+#include <type_traits>
+
+#include "bulk_copy.cuh"
+#include "head_rows.cuh"
+#include "mma_ops.cuh"
+#include "tree_plan.cuh"
+
+namespace dkv {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float VE_LOW = -60.f;            // FP8: V rows with a smaller scale take part in the reference as if they had this one
+constexpr float LAZY = 8.f;                // the softmax's reference moves when the maximum has grown by 2^LAZY
+
+__device__ __forceinline__ void tma_page(unsigned dst, const CUtensorMap* map, int row, unsigned bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(0), "r"(bar) : "memory");
+}
+__device__ __forceinline__ float lds_f32(unsigned addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ float quad_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    v += __shfl_xor_sync(0xffffffffu, v, 1);
+    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+}
+
+template <int HD, int DT, int RG>
+struct TreeCfg {
+    static constexpr int esize = DT == DYNAKV_F32 ? 4 : DT == DYNAKV_BF16 ? 2 : 1;
+    static constexpr int row_bytes = HD * esize;
+    static constexpr int panel_w = row_bytes < 128 ? row_bytes : 128;        // bytes of a row in one swizzle panel
+    static constexpr int panels = row_bytes / panel_w;
+    static constexpr int page_bytes = PAGE * row_bytes;
+    static constexpr int stage_bytes = 2 * page_bytes;
+    // 96 KB of ring per CTA (FP8, d = 128: less, the exponents and the merge need the rest), at most 12 stages
+    static constexpr int stages = DT == DYNAKV_FP8 && HD == 128 ? (RG == 1 ? 9 : 10) : 98304 / stage_bytes < 12 ? 98304 / stage_bytes : 12;
+    static constexpr int KG = RG == 1 ? 3 : RG == 2 ? (stages % 2 == 0 ? 2 : 1) : 1;
+    static constexpr int RT = 16 * RG;
+    static constexpr int consumers = RG * KG;
+    static constexpr int threads = 32 * (consumers + 1);
+    static constexpr int per_sm = DT == DYNAKV_F32 ? 1 : 2;
+    static constexpr int exp_bytes = DT == DYNAKV_FP8 ? stages * 64 : 0;
+    static constexpr int q_bytes = DT == DYNAKV_F32 ? RG * 16 * HD * 4 : 0;
+    static constexpr int p_bytes = DT == DYNAKV_F32 ? consumers * 16 * 32 * 4 : 0;
+    static constexpr int dump_bytes = 16 * HD * 4 + 128;                     // one warp's sums, then (m, l) of its 16 rows
+    static constexpr int merge_bytes = KG > 1 ? RG * dump_bytes : 0;
+    static constexpr int fixed_bytes = 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + 36 * 8;
+    static constexpr int smem = stages * stage_bytes + exp_bytes + q_bytes + p_bytes + merge_bytes + fixed_bytes;
+    static_assert(stages % KG == 0, "each ring stage belongs to one page group");
+    static_assert(per_sm * (smem + 1024) <= 233472, "shared memory of an SM");
+};
+
+// What a consumer warp needs to know of the page it is handed.
+struct PageIn {
+    unsigned k, v;                 // shared-memory addresses
+    const signed char* exps;       // FP8: scale exponents of the 32 K rows, then of the 32 V rows
+    int key0;                      // first row's place in the sequence
+    bool mask;                     // rows of the page may be invisible
+};
+
+// Element e of a row of the pool, as a number.
+template <int DT>
+__device__ __forceinline__ float cache_elem(const unsigned char* pool, const signed char* exps, long long row, int hd, int e) {
+    if constexpr (DT == DYNAKV_F32) return reinterpret_cast<const float*>(pool)[row * hd + e];
+    else if constexpr (DT == DYNAKV_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(pool)[row * hd + e]);
+    else return fp8_unpack2((unsigned short)pool[row * hd + e], pow2f(exps[row])).x;
+}
+
+// Byte offset of 16-byte chunk c of row r inside a page of the ring, as the TMA swizzle placed it.
+template <typename C>
+__device__ __forceinline__ unsigned chunk_at(int r, int c) {
+    if constexpr (C::panel_w == 128) return (c >> 3) * (PAGE * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+    else return r * 64 + (((c & 3) ^ ((r >> 1) & 3)) << 4);
+}
+
+// ---------------------------------------------------------------------------------- mma.sync consumers (bf16, FP8)
+//
+// Lane (g = lane / 4, c = lane % 4) owns rows g and g + 8 of the warp's 16 and the columns of its fragments.
+template <int HD, int DT, int RG>
+struct MmaRows {
+    using C = TreeCfg<HD, DT, RG>;
+    static constexpr bool F8 = DT == DYNAKV_FP8;
+    static constexpr int KS = HD / 16, NT = HD / 8;
+    static constexpr bool PERM = F8 && HD == 128;       // key order inside a tile that keeps FP8 loads free of conflicts
+    unsigned qf[KS][4];
+    float qs[2];                                        // logit factor (log2 units) of the two rows
+    float acc[NT][4], m[2], l[2];
+    int t[2];                                           // token of the two rows, -1: no such row
+
+    static __device__ __forceinline__ int key_of(int n) { return PERM ? (n & 1) * 4 + (n >> 1) : n; }       // column n of an 8-key tile
+    // element of the output that acc[nt][i] (i = 0, 1) of lane column c holds
+    static __device__ __forceinline__ int elem(int nt, int i, int c) {
+        if constexpr (!F8) return nt * 8 + 2 * c + i;
+        else if constexpr (HD == 128) return 16 * (c + 4 * i) + nt;
+        else return 8 * (2 * c + i) + nt;
+    }
+
+    __device__ __forceinline__ void start(const TreeArgs& a, const Segment& g, int rg, int lane) {
+        const int c = lane & 3;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int r = g.tile * C::RT + rg * 16 + (lane >> 2) + 8 * i;
+            t[i] = r < g.T * a.G ? r / a.G : -1;
+            const unsigned* q = reinterpret_cast<const unsigned*>(
+                reinterpret_cast<const __nv_bfloat16*>(a.q) + ((size_t)(g.q0 + max(t[i], 0)) * a.Hq + g.h * a.G + (t[i] < 0 ? 0 : r - t[i] * a.G)) * HD);
+            float mx = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++) {
+                if constexpr (!F8) {
+                    qf[ks][i] = t[i] >= 0 ? q[ks * 8 + c] : 0u;
+                    qf[ks][i + 2] = t[i] >= 0 ? q[ks * 8 + c + 4] : 0u;
+                } else {             // four neighbouring elements: the lane's bytes of a K chunk are its fragments of four steps
+                    const int e = ((ks >> 2) * 4 + c) * 16 + (ks & 3) * 4;
+                    const uint2 w = t[i] >= 0 ? *reinterpret_cast<const uint2*>(q + e / 2) : make_uint2(0u, 0u);
+                    qf[ks][i] = w.x; qf[ks][i + 2] = w.y;
+#pragma unroll
+                    for (int x = 0; x < 2; x++) {
+                        const unsigned u = x ? w.y : w.x;
+                        mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(u << 16)), fabsf(__uint_as_float(u & 0xffff0000u))));
+                    }
+                }
+            }
+            qs[i] = a.scale * LOG2E;
+            if constexpr (F8) {      // q / 2^e with the largest element in [2^14, 2^15): exact in f16 down to 2^-29 of it
+                mx = quad_max(mx);
+                const int e = mx > 0.f ? max(-100, min(112, (int)(__float_as_uint(mx) >> 23) - 127 - 14)) : 0;
+                const float down = pow2f(-e);
+#pragma unroll
+                for (int ks = 0; ks < KS; ks++)
+#pragma unroll
+                    for (int x = 0; x < 4; x += 2) {
+                        const unsigned u = qf[ks][i + x];
+                        const __half2 h = __floats2half2_rn(__uint_as_float(u << 16) * down, __uint_as_float(u & 0xffff0000u) * down);
+                        qf[ks][i + x] = *reinterpret_cast<const unsigned*>(&h);
+                    }
+                qs[i] *= pow2f(e);
+            }
+            m[i] = -INFINITY; l[i] = 0.f;
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) acc[nt][x] = 0.f;
+    }
+
+    __device__ __forceinline__ void page(const TreeArgs& a, const Segment& g, const PageIn& p, int lane) {
+        const int c = lane & 3, n = lane >> 2;
+        float s[4][4];
+#pragma unroll
+        for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) s[kt][x] = 0.f;
+        if constexpr (!F8) {
+            const int mt = lane >> 3, r8 = lane & 7;
+#pragma unroll
+            for (int k2 = 0; k2 < KS / 2; k2++)
+#pragma unroll
+                for (int kt = 0; kt < 4; kt++) {
+                    unsigned b[4];
+                    ldmatrix_x4(p.k + chunk_at<C>(kt * 8 + r8, k2 * 4 + mt), b);
+                    mma_bf16(s[kt], qf[2 * k2][0], qf[2 * k2][1], qf[2 * k2][2], qf[2 * k2][3], b[0], b[1]);
+                    mma_bf16(s[kt], qf[2 * k2 + 1][0], qf[2 * k2 + 1][1], qf[2 * k2 + 1][2], qf[2 * k2 + 1][3], b[2], b[3]);
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < HD / 64; j++)
+#pragma unroll
+                for (int kt = 0; kt < 4; kt++) {
+                    const uint4 w = lds16(p.k + chunk_at<C>(kt * 8 + key_of(n), c + 4 * j));
+                    const unsigned ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int x = 0; x < 4; x++) {
+                        unsigned b0, b1;
+                        e4m3x4_to_f16x2(ww[x], b0, b1);
+                        mma_f16(s[kt], qf[j * 4 + x][0], qf[j * 4 + x][1], qf[j * 4 + x][2], qf[j * 4 + x][3], b0, b1);
+                    }
+                }
+        }
+        // logits in log2 units, FP8 with the K row's scale; the running maximum is over logit + exponent of the V row
+        unsigned win[2] = {~0u, ~0u};
+        if (p.mask) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) win[i] = t[i] >= 0 ? tree_window(a, g, t[i], p.key0) : 0u;
+        }
+        float ve[4][2];
+        float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const int key = kt * 8 + key_of(2 * c + e);
+                float f = 1.f;
+                ve[kt][e] = 0.f;
+                if constexpr (F8) { f = pow2f(p.exps[key]); ve[kt][e] = (float)p.exps[32 + key]; }
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    float& x = s[kt][2 * i + e];
+                    x *= F8 ? qs[i] * f : qs[i];
+                    if (p.mask && !((win[i] >> key) & 1u)) x = -INFINITY;
+                    mx[i] = fmaxf(mx[i], F8 ? x + fmaxf(ve[kt][e], VE_LOW) : x);
+                }
+            }
+        float ref[2];
+        bool move = false;
+#pragma unroll
+        for (int i = 0; i < 2; i++) { mx[i] = quad_max(mx[i]); move |= mx[i] > m[i] + LAZY; }
+        if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const float to = mx[i] > m[i] + LAZY ? mx[i] : m[i];
+                const float f = to == -INFINITY ? 1.f : ex2(m[i] - to);
+                m[i] = to; l[i] *= f;
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) { acc[nt][2 * i] *= f; acc[nt][2 * i + 1] *= f; }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; i++) ref[i] = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+        for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const float vr = fmaxf(ve[kt][e], VE_LOW);
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    float& x = s[kt][2 * i + e];
+                    x = ex2((F8 ? x + vr : x) - ref[i]);
+                    l[i] += F8 ? x * pow2f(-(int)vr) : x;
+                    if (F8 && ve[kt][e] < VE_LOW) x *= ex2(ve[kt][e] - VE_LOW);
+                }
+            }
+        // weights as A fragments: two 8-key tiles of the logits are the 16 keys of a step
+        if constexpr (!F8) {
+            const int mt = lane >> 3, r8 = lane & 7;
+#pragma unroll
+            for (int kk = 0; kk < 2; kk++) {
+                unsigned hi[4], lo[4];
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    split2(s[2 * kk + x][0], s[2 * kk + x][1], hi[2 * x], lo[2 * x]);
+                    split2(s[2 * kk + x][2], s[2 * kk + x][3], hi[2 * x + 1], lo[2 * x + 1]);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; nt += 2) {
+                    unsigned b[4];
+                    ldmatrix_x4_trans(p.v + chunk_at<C>(kk * 16 + (mt & 1) * 8 + r8, nt + (mt >> 1)), b);
+                    mma_bf16(acc[nt], hi[0], hi[1], hi[2], hi[3], b[0], b[1]);
+                    mma_bf16(acc[nt + 1], hi[0], hi[1], hi[2], hi[3], b[2], b[3]);
+                    mma_bf16(acc[nt], lo[0], lo[1], lo[2], lo[3], b[0], b[1]);
+                    mma_bf16(acc[nt + 1], lo[0], lo[1], lo[2], lo[3], b[2], b[3]);
+                }
+            }
+        } else {
+            constexpr int VB = HD / 8;               // bytes of a V row a lane loads: columns n of all tiles
+            const int chunk = HD == 128 ? (n & 1) * 4 + (n >> 1) : 0;
+#pragma unroll
+            for (int kk = 0; kk < 2; kk++) {
+                unsigned pa[4];
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    const __half2 h0 = __floats2half2_rn(s[2 * kk + x][0], s[2 * kk + x][1]), h1 = __floats2half2_rn(s[2 * kk + x][2], s[2 * kk + x][3]);
+                    pa[2 * x] = *reinterpret_cast<const unsigned*>(&h0);
+                    pa[2 * x + 1] = *reinterpret_cast<const unsigned*>(&h1);
+                }
+                unsigned w[4][VB / 4];
+#pragma unroll
+                for (int y = 0; y < 4; y++) {
+                    const int key = kk * 16 + (y >> 1) * 8 + key_of(2 * c + (y & 1));
+                    if constexpr (HD == 128) {
+                        const uint4 v = lds16(p.v + chunk_at<C>(key, chunk));
+                        w[y][0] = v.x; w[y][1] = v.y; w[y][2] = v.z; w[y][3] = v.w;
+                    } else {
+                        unsigned x0, x1;
+                        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];\n" : "=r"(x0), "=r"(x1) : "r"(p.v + chunk_at<C>(key, n >> 1) + (n & 1) * 8));
+                        w[y][0] = x0; w[y][1] = x1;
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < VB / 4; x++)
+#pragma unroll
+                    for (int half = 0; half < 2; half++) {
+                        const unsigned sel = half ? 0x7362u : 0x5140u;        // bytes (2, 6, 3, 7) or (0, 4, 1, 5) of two keys
+                        unsigned b0, b1, d0, d1;
+                        e4m3x4_to_f16x2(__byte_perm(w[0][x], w[1][x], sel), b0, d0);
+                        e4m3x4_to_f16x2(__byte_perm(w[2][x], w[3][x], sel), b1, d1);
+                        mma_f16(acc[4 * x + 2 * half], pa[0], pa[1], pa[2], pa[3], b0, b1);
+                        mma_f16(acc[4 * x + 2 * half + 1], pa[0], pa[1], pa[2], pa[3], d0, d1);
+                    }
+            }
+        }
+    }
+
+    __device__ __forceinline__ void finish() {
+#pragma unroll
+        for (int i = 0; i < 2; i++) l[i] = quad_sum(l[i]);
+    }
+    // This warp's state into shared memory, and another's into this one's.
+    __device__ __forceinline__ void dump(float* to, int lane) const {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) to[(nt * 4 + x) * 32 + lane] = acc[nt][x];
+        if ((lane & 3) == 0) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) reinterpret_cast<float2*>(to + NT * 128)[(lane >> 2) + 8 * i] = make_float2(m[i], l[i]);
+        }
+    }
+    __device__ __forceinline__ void merge(const float* from, int lane) {
+        float f0[2], f1[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const float2 o = reinterpret_cast<const float2*>(from + NT * 128)[(lane >> 2) + 8 * i];
+            const float to = fmaxf(m[i], o.x), ref = to == -INFINITY ? 0.f : to;
+            f0[i] = ex2(m[i] - ref); f1[i] = ex2(o.x - ref);
+            l[i] = l[i] * f0[i] + o.y * f1[i];
+            m[i] = to;
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) acc[nt][x] = acc[nt][x] * f0[x >> 1] + from[(nt * 4 + x) * 32 + lane] * f1[x >> 1];
+    }
+    // The share of a drafted row that was left out of the MMAs: key row `row` of the pool, token j of the tree.
+    __device__ __forceinline__ void add_row(const TreeArgs& a, const Segment& g, int rg, long long row, int j, int lane) {
+        const int c = lane & 3;
+        float d[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int r = g.tile * C::RT + rg * 16 + (lane >> 2) + 8 * i;
+            if (t[i] >= 0) {
+                const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q) + ((size_t)(g.q0 + t[i]) * a.Hq + g.h * a.G + r - t[i] * a.G) * HD;
+                for (int e = c; e < HD; e += 4) d[i] = fmaf(__bfloat162float(q[e]), cache_elem<DT>(a.kpool, a.kexp, row, HD, e), d[i]);
+            }
+            d[i] = quad_sum(d[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+            if (t[i] >= 0 && tree_sees(a, g, t[i], j)) {
+                const float w = ex2(d[i] * (a.scale * LOG2E) - (m[i] == -INFINITY ? 0.f : m[i]));
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int x = 0; x < 2; x++) acc[nt][2 * i + x] = fmaf(w, cache_elem<DT>(a.vpool, a.vexp, row, HD, elem(nt, x, c)), acc[nt][2 * i + x]);
+            }
+    }
+    __device__ __forceinline__ void write(const TreeArgs& a, const Segment& g, int rg, int lane, bool whole, size_t slot) const {
+        const int c = lane & 3;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            if (t[i] < 0) continue;
+            const int rl = rg * 16 + (lane >> 2) + 8 * i, r = g.tile * C::RT + rl;
+            const size_t at = (size_t)(g.q0 + t[i]) * a.Hq + g.h * a.G + r - t[i] * a.G;
+            if (whole) {
+                const float f = l[i] == 0.f ? 0.f : 1.f / l[i];
+                __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(a.out) + at * HD;
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                    if constexpr (!F8) *reinterpret_cast<unsigned*>(o + elem(nt, 0, c)) = pack_bf16(acc[nt][2 * i] * f, acc[nt][2 * i + 1] * f);
+                    else if ((nt & 1) == 0) {
+#pragma unroll
+                        for (int x = 0; x < 2; x++)
+                            *reinterpret_cast<unsigned*>(o + elem(nt, x, c)) = pack_bf16(acc[nt][2 * i + x] * f, acc[nt + 1][2 * i + x] * f);
+                    }
+                }
+                if (a.lse && c == 0) a.lse[at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * LN2;
+            } else {
+                float* o = a.acc + (slot * C::RT + rl) * HD;
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                    if constexpr (!F8) *reinterpret_cast<float2*>(o + elem(nt, 0, c)) = make_float2(acc[nt][2 * i], acc[nt][2 * i + 1]);
+                    else if ((nt & 3) == 0) {
+#pragma unroll
+                        for (int x = 0; x < 2; x++)
+                            *reinterpret_cast<float4*>(o + elem(nt, x, c)) = make_float4(acc[nt][2 * i + x], acc[nt + 1][2 * i + x], acc[nt + 2][2 * i + x], acc[nt + 3][2 * i + x]);
+                    }
+                }
+                if (c == 0) a.ml[slot * C::RT + rl] = make_float2(m[i], l[i]);
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------- fp32 consumers
+//
+// Lane = key for the logits (q is read from shared memory, the same word for all lanes), lane = HD / 32 columns for the
+// sums (the weights go through shared memory).  Every lane keeps the 16 rows' running maxima; the sums l stay split
+// over the lanes until the end.
+template <int HD, int RG>
+struct F32Rows {
+    using C = TreeCfg<HD, DYNAKV_F32, RG>;
+    static constexpr int DPL = HD / 32;
+    float acc[16][DPL], m[16], l[16];
+    unsigned q_s, p_s;             // shared memory: this row group's q [16][HD], this warp's weights [16][32]
+    int rows;                      // rows of the warp that exist
+
+    __device__ __forceinline__ void start(const TreeArgs& a, const Segment& g, int rg, int lane) {
+        rows = max(0, min(16, g.T * a.G - (g.tile * C::RT + rg * 16)));
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DPL; d++) acc[r][d] = 0.f;
+        }
+        (void)lane;
+    }
+    // q of the group's rows, every page group its own share of the copy (the caller synchronises around it)
+    static __device__ __forceinline__ void load_q(const TreeArgs& a, const Segment& g, int rg, float* q_s, int lane) {
+        for (int r = 0; r < 16; r++) {
+            const int x = g.tile * C::RT + rg * 16 + r, t = x / a.G;
+            const float* q = reinterpret_cast<const float*>(a.q) + ((size_t)(g.q0 + t) * a.Hq + g.h * a.G + x - t * a.G) * HD;
+            for (int e = lane; e < HD; e += 32) q_s[r * HD + e] = t < g.T ? q[e] * (a.scale * LOG2E) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void page(const TreeArgs& a, const Segment& g, const PageIn& p, int lane, int rg) {
+        float s[16];
+#pragma unroll
+        for (int r = 0; r < 16; r++) s[r] = 0.f;
+#pragma unroll 4
+        for (int ch = 0; ch < HD / 4; ch++) {
+            const uint4 ku = lds16(p.k + chunk_at<C>(lane, ch));
+            const float k0 = __uint_as_float(ku.x), k1 = __uint_as_float(ku.y), k2 = __uint_as_float(ku.z), k3 = __uint_as_float(ku.w);
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                if (r >= 4 && rows <= 4) continue;
+                const uint4 qu = lds16(q_s + (r * HD + ch * 4) * 4);
+                s[r] = fmaf(__uint_as_float(qu.x), k0, s[r]);
+                s[r] = fmaf(__uint_as_float(qu.y), k1, s[r]);
+                s[r] = fmaf(__uint_as_float(qu.z), k2, s[r]);
+                s[r] = fmaf(__uint_as_float(qu.w), k3, s[r]);
+            }
+        }
+        unsigned win = ~0u;                        // lane r < 16: the window of row r
+        if (p.mask) {
+            const int x = g.tile * C::RT + rg * 16 + (lane & 15), t = x / a.G;
+            win = t < g.T ? tree_window(a, g, t, p.key0) : 0u;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            if (r >= 4 && rows <= 4) continue;
+            if (p.mask && !((__shfl_sync(0xffffffffu, win, r) >> lane) & 1u)) s[r] = -INFINITY;
+            float mx = s[r];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            if (mx > m[r] + LAZY) {                // the same in all lanes
+                const float f = ex2(m[r] - mx);
+                m[r] = mx; l[r] *= f;
+#pragma unroll
+                for (int d = 0; d < DPL; d++) acc[r][d] *= f;
+            }
+            const float w = exp2f(s[r] - (m[r] == -INFINITY ? 0.f : m[r]));
+            l[r] += w;
+            asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(p_s + (r * 32 + lane) * 4), "f"(w) : "memory");
+        }
+        __syncwarp();
+#pragma unroll 2
+        for (int k4 = 0; k4 < 8; k4++) {
+            float v[4][DPL];
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                const int key = k4 * 4 + y;
+                if constexpr (DPL == 4) {
+                    const uint4 u = lds16(p.v + chunk_at<C>(key, lane));
+                    v[y][0] = __uint_as_float(u.x); v[y][1] = __uint_as_float(u.y); v[y][2] = __uint_as_float(u.z); v[y][3] = __uint_as_float(u.w);
+                } else {
+                    const unsigned at = p.v + chunk_at<C>(key, lane >> 1) + (lane & 1) * 8;
+                    v[y][0] = lds_f32(at); v[y][1] = lds_f32(at + 4);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                if (r >= 4 && rows <= 4) continue;
+                const uint4 u = lds16(p_s + (r * 32 + k4 * 4) * 4);
+                const float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+#pragma unroll
+                for (int y = 0; y < 4; y++)
+#pragma unroll
+                    for (int d = 0; d < DPL; d++) acc[r][d] = fmaf(w[y], v[y][d], acc[r][d]);
+            }
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ void finish() {
+#pragma unroll
+        for (int r = 0; r < 16; r++) l[r] = warp_sum(l[r]);
+    }
+    __device__ __forceinline__ void dump(float* to, int lane) const {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+#pragma unroll
+            for (int d = 0; d < DPL; d++) to[(r * DPL + d) * 32 + lane] = acc[r][d];
+            if (lane == r) reinterpret_cast<float2*>(to + 16 * HD)[r] = make_float2(m[r], l[r]);
+        }
+    }
+    __device__ __forceinline__ void merge(const float* from, int lane) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            const float2 o = reinterpret_cast<const float2*>(from + 16 * HD)[r];
+            const float to = fmaxf(m[r], o.x), ref = to == -INFINITY ? 0.f : to;
+            const float f0 = exp2f(m[r] - ref), f1 = exp2f(o.x - ref);
+            l[r] = l[r] * f0 + o.y * f1;
+            m[r] = to;
+#pragma unroll
+            for (int d = 0; d < DPL; d++) acc[r][d] = acc[r][d] * f0 + from[(r * DPL + d) * 32 + lane] * f1;
+        }
+    }
+    __device__ __forceinline__ void add_row(const TreeArgs& a, const Segment& g, int rg, long long row, int j, int lane) {
+        const float* k = reinterpret_cast<const float*>(a.kpool) + row * HD;
+        const float* v = reinterpret_cast<const float*>(a.vpool) + row * HD;
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            float d = 0.f;
+            for (int e = lane; e < HD; e += 32) d = fmaf(lds_f32(q_s + (r * HD + e) * 4), k[e], d);
+            d = warp_sum(d);
+            const int x = g.tile * C::RT + rg * 16 + r, t = x / a.G;
+            if (r < rows && tree_sees(a, g, t, j)) {
+                const float w = exp2f(d - (m[r] == -INFINITY ? 0.f : m[r]));
+#pragma unroll
+                for (int e = 0; e < DPL; e++) acc[r][e] = fmaf(w, v[lane * DPL + e], acc[r][e]);
+            }
+        }
+    }
+    __device__ __forceinline__ void write(const TreeArgs& a, const Segment& g, int rg, int lane, bool whole, size_t slot) const {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            if (r >= rows) continue;
+            const int rl = rg * 16 + r, x = g.tile * C::RT + rl, t = x / a.G;
+            const size_t at = (size_t)(g.q0 + t) * a.Hq + g.h * a.G + x - t * a.G;
+            const float f = !whole ? 1.f : l[r] == 0.f ? 0.f : 1.f / l[r];
+            float* o = whole ? reinterpret_cast<float*>(a.out) + at * HD : a.acc + (slot * C::RT + rl) * HD;
+#pragma unroll
+            for (int d = 0; d < DPL; d++) o[lane * DPL + d] = acc[r][d] * f;
+            if (lane == 0) {
+                if (!whole) a.ml[slot * C::RT + rl] = make_float2(m[r], l[r]);
+                else if (a.lse) a.lse[at] = l[r] == 0.f ? -INFINITY : (m[r] + log2f(l[r])) * LN2;
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------- the kernel
+
+// Rows of a V page that must not reach the MMAs: those at or past the sequence's end are zeroed, and so are drafted rows
+// that hold a NaN or an infinity, which are noted in `odd` (bit j: token j of the tree).  One warp.
+template <typename C, int DT>
+__device__ __forceinline__ void mend_page(unsigned v, const Segment& g, int key0, unsigned* odd, int lane) {
+    const int prefix = g.n - g.T;
+    unsigned wild = 0u;                                    // rows of the page with a value that is no number
+    constexpr int chunks = C::page_bytes / 16;
+    for (int x = lane; x < chunks; x += 32) {
+        const unsigned at = v + x * 16;
+        const int row = (x * 16 % (PAGE * C::panel_w)) / C::panel_w, pos = key0 + row;
+        if (pos < prefix) continue;
+        if (pos >= g.n) {
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(at), "r"(0u) : "memory");
+        } else {
+            const uint4 u = lds16(at);
+            const unsigned w[4] = {u.x, u.y, u.z, u.w};
+            bool bad = false;
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                if constexpr (DT == DYNAKV_F32) bad |= (w[y] & 0x7f800000u) == 0x7f800000u;
+                else if constexpr (DT == DYNAKV_BF16) bad |= (w[y] & 0x7f80u) == 0x7f80u || (w[y] & 0x7f800000u) == 0x7f800000u;
+                else {
+#pragma unroll
+                    for (int z = 0; z < 4; z++) bad |= ((w[y] >> (8 * z)) & 0x7fu) == 0x7fu;
+                }
+            }
+            if (bad) wild |= 1u << row;
+        }
+    }
+    wild = __reduce_or_sync(0xffffffffu, wild);
+    if (wild) {
+        for (int x = lane; x < chunks; x += 32) {
+            const int row = (x * 16 % (PAGE * C::panel_w)) / C::panel_w;
+            if ((wild >> row) & 1u) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};\n" ::"r"(v + x * 16), "r"(0u) : "memory");
+        }
+        const int j = key0 + lane - prefix;
+        if (((wild >> lane) & 1u) && j >= 0 && j < TREE_MAX) atomicOr(&odd[j >> 5], 1u << (j & 31));
+    }
+    fence_proxy_async();               // the copies that refill the stage come after these stores
+    __syncwarp();
+}
+
+template <int HD, int DT, int RG>
+__global__ void __launch_bounds__((TreeCfg<HD, DT, RG>::threads), (TreeCfg<HD, DT, RG>::per_sm))
+k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TreeArgs a) {
+    using C = TreeCfg<HD, DT, RG>;
+    constexpr int S = C::stages, KG = C::KG;
+    extern __shared__ __align__(1024) unsigned char tree_smem[];
+    unsigned char* at = tree_smem + S * C::stage_bytes;
+    signed char* exps = reinterpret_cast<signed char*>(at); at += C::exp_bytes;
+    float* q_s = reinterpret_cast<float*>(at); at += C::q_bytes;
+    float* p_s = reinterpret_cast<float*>(at); at += C::p_bytes;
+    float* dump = reinterpret_cast<float*>(at); at += C::merge_bytes;
+    long long* sh = reinterpret_cast<long long*>(at); at += 36 * 8;
+    unsigned long long* bars = reinterpret_cast<unsigned long long*>(at); at += 2 * S * 8;
+    int* s_abort = reinterpret_cast<int*>(at); at += 16;
+    unsigned* odd = reinterpret_cast<unsigned*>(at); at += 3 * 8 * 4;
+    volatile int* meta = reinterpret_cast<volatile int*>(at);
+    const unsigned ring = smem_u32(tree_smem);
+    auto full = [&](int s) { return smem_u32(&bars[s]); };
+    auto empty = [&](int s) { return smem_u32(&bars[S + s]); };
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    if (tid == 0) {
+        for (int s = 0; s < S; s++) { mbar_init(full(s), 1); mbar_init(empty(s), RG); }
+        *s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (tid < 24) odd[tid] = 0u;
+    const Range range = tree_range<C::RT>(a, KG, sh);      // holds block barriers
+    pdl_trigger();
+    SegmentWalk<C::RT> walk(a, range);
+    Segment g;
+
+    if (warp == C::consumers) {
+        // =============================== producer ===============================
+        int it = 0;
+        bool ok = true;
+        while (ok && walk.next(a, g)) {
+            for (int pc = g.p0; ok && pc < g.p1; pc += 32) {
+                const int cnt = min(32, g.p1 - pc);
+                int id = -1;
+                if (lane < cnt && g.n > 0) {
+                    id = a.page_table[(size_t)g.b * a.pages_per_seq + pc + lane];
+                    if (id < 0 || id >= a.n_pages) { id = -1; tree_status(a, DYNAKV_ST_BOUNDS); }
+                }
+                for (int j = 0; j < cnt && ok; j++, it++) {
+                    const int page = __shfl_sync(0xffffffffu, id, j);
+                    const int st = it % S;
+                    if (lane == 0) {
+                        ok = mbar_wait(empty(st), ((it / S) & 1) ^ 1);
+                        if (ok) {
+                            meta[st] = page >= 0;
+                            if (page >= 0) {
+                                const int row = (page * a.Hk + g.h) * PAGE;
+                                mbar_arrive_expect_tx(full(st), C::stage_bytes + (DT == DYNAKV_FP8 ? 64 : 0));
+                                tma_page(ring + st * C::stage_bytes, &map_k, row, full(st));
+                                tma_page(ring + st * C::stage_bytes + C::page_bytes, &map_v, row, full(st));
+                                if constexpr (DT == DYNAKV_FP8) {
+                                    bulk_g2s(smem_u32(exps + st * 64), a.kexp + row, 32, full(st));
+                                    bulk_g2s(smem_u32(exps + st * 64 + 32), a.vexp + row, 32, full(st));
+                                }
+                            } else {
+                                mbar_arrive(full(st));
+                            }
+                        }
+                    }
+                    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+                }
+            }
+        }
+        if (!ok && lane == 0) {
+            // a stage was not given back in time: report it and let the copies under way land before the block ends
+            *s_abort = 1;
+            tree_status(a, DYNAKV_ST_INTERNAL);
+            for (int s = 0; s < S; s++) {
+                const int last = it - 1 - ((it - 1 - s) % S + S) % S;          // last item that went to stage s
+                if (last >= 0) mbar_wait(full(s), (last / S) & 1);
+            }
+        }
+    } else {
+        // =============================== consumers ===============================
+        const int rg = warp % RG, kg = warp / RG;
+        constexpr bool F32 = DT == DYNAKV_F32;
+        typename std::conditional<F32, F32Rows<HD, RG>, MmaRows<HD, F32 ? DYNAKV_BF16 : DT, RG>>::type rows;
+        auto all_sync = [&]() { asm volatile("bar.sync 5, %0;\n" ::"n"(C::consumers * 32) : "memory"); };
+        auto group_sync = [&]() { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + kg), "n"(RG * 32) : "memory"); };
+        if constexpr (F32) { rows.q_s = smem_u32(q_s + rg * 16 * HD); rows.p_s = smem_u32(p_s + warp * 16 * 32); }
+        int it = 0, seg = 0;
+        bool dead = false, cut_end = false;
+        Segment cut;
+        while (walk.next(a, g)) {
+            const int prefix = g.n - g.T;
+            unsigned* odd_now = odd + (seg % 3) * 8;
+            if constexpr (F32) {
+                all_sync();                            // nobody still reads the last segment's q
+                if (kg == 0) F32Rows<HD, RG>::load_q(a, g, rg, q_s + rg * 16 * HD, lane);
+                all_sync();
+            }
+            rows.start(a, g, rg, lane);
+            for (int pg = g.p0; pg < g.p1; pg++, it++) {
+                if (KG > 1 && it % KG != kg) continue;
+                const int st = it % S;
+                if (!dead && (*reinterpret_cast<volatile int*>(s_abort) || !mbar_wait(full(st), (it / S) & 1))) {
+                    dead = true;
+                    *reinterpret_cast<volatile int*>(s_abort) = 1;
+                    tree_status(a, DYNAKV_ST_INTERNAL);
+                }
+                dead = __any_sync(0xffffffffu, dead);
+                PageIn p;
+                p.k = ring + st * C::stage_bytes; p.v = p.k + C::page_bytes; p.exps = exps + st * 64;
+                p.key0 = pg * PAGE;
+                const bool edge = p.key0 + PAGE > prefix;
+                p.mask = p.key0 + PAGE > prefix;       // holds drafted rows or the end of the sequence
+                // a page that the table does not name was not copied: the stage holds an older one
+                const bool there = !dead && meta[st] != 0;
+                if (p.mask) {                          // the same in all warps of the group, dead or not
+                    if (rg == 0 && there) mend_page<C, DT>(p.v, g, p.key0, odd_now, lane);
+                    if (RG > 1) group_sync();
+                }
+                if (there) {
+                    if constexpr (F32) rows.page(a, g, p, lane, rg);
+                    else rows.page(a, g, p, lane);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(empty(st));
+            }
+            rows.finish();
+            if (tid < 8) odd[((seg + 1) % 3) * 8 + tid] = 0u;      // last read before the previous segment's barrier
+            if (KG == 1) all_sync();
+#pragma unroll
+            for (int src = KG - 1; src >= 1; src--) {
+                float* box = dump + rg * (C::dump_bytes / 4);
+                if (kg == src) rows.dump(box, lane);
+                all_sync();
+                if (kg == 0) rows.merge(box, lane);
+                if (src > 1 || KG > 1) all_sync();
+            }
+            if (kg == 0) {
+                for (int w = 0; w < TREE_MAX / 32; w++) {
+                    unsigned bits = odd_now[w];
+                    while (bits) {
+                        const int j = w * 32 + __ffs(bits) - 1;
+                        bits &= bits - 1;
+                        const int pos = prefix + j, page = a.page_table[(size_t)g.b * a.pages_per_seq + pos / PAGE];
+                        rows.add_row(a, g, rg, ((long long)page * a.Hk + g.h) * PAGE + pos % PAGE, j, lane);
+                    }
+                }
+                rows.write(a, g, rg, lane, g.first && g.last, (size_t)blockIdx.x * 2 + (g.first ? 1 : 0));
+            }
+            if (g.last && !g.first) { cut = g; cut_end = true; }
+            seg++;
+        }
+        if (tid == 0) {
+            if (cut_end) describe_cut_unit(a, cut, range);
+            a.desc[(size_t)blockIdx.x * 8 + DESC_VALID] = cut_end ? 1 : 0;
+        }
+    }
+}
+
+// Merges the records of the units that were cut: block (x = CTA of the first launch in which the unit ends, y = 8 of its rows),
+// a warp per row.
+template <int HD, int RT, typename OUT>
+__global__ void __launch_bounds__(256) k_tree_merge(const TreeArgs a) {
+    pdl_wait();
+    const int* d = a.desc + (size_t)blockIdx.x * 8;
+    if (!d[DESC_VALID]) return;
+    constexpr int EPL = HD / 32;
+    const int lane = threadIdx.x & 31, rl = blockIdx.y * 8 + (threadIdx.x >> 5);
+    const int r = d[DESC_RT] * RT + rl, t = r / a.G;
+    if (t >= d[DESC_T]) return;
+    const int c0 = d[DESC_FIRST], n = blockIdx.x - c0 + 1;          // records: slot 1 of CTA c0, slot 0 of the others
+    auto slot = [&](int i) { return ((size_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * RT + rl; };
+    float m = -INFINITY;
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, a.ml[slot(i)].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float acc[EPL], l = 0.f;
+#pragma unroll
+    for (int e = 0; e < EPL; e++) acc[e] = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        float f = 0.f, fl = 0.f;
+        if (i0 + lane < n) { const float2 x = a.ml[slot(i0 + lane)]; f = exp2f(x.x - ref); fl = f * x.y; }
+        l += warp_sum(fl);
+        const int cnt = min(32, n - i0);
+#pragma unroll 4
+        for (int i = 0; i < cnt; i++) {
+            const float w = __shfl_sync(0xffffffffu, f, i);
+            const float* p = a.acc + slot(i0 + i) * HD + lane * EPL;
+            float v[EPL];
+            if constexpr (EPL == 4) { const float4 x = *reinterpret_cast<const float4*>(p); v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; }
+            else { const float2 x = *reinterpret_cast<const float2*>(p); v[0] = x.x; v[1] = x.y; }
+#pragma unroll
+            for (int e = 0; e < EPL; e++) acc[e] = fmaf(w, v[e], acc[e]);
+        }
+    }
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    const size_t at = (size_t)(d[DESC_Q0] + t) * a.Hq + d[DESC_H] * a.G + r - t * a.G;
+    OUT* o = reinterpret_cast<OUT*>(a.out) + at * HD + lane * EPL;
+    if constexpr (sizeof(OUT) == 4) {
+#pragma unroll
+        for (int e = 0; e < EPL; e++) o[e] = acc[e] * f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPL; e += 2) reinterpret_cast<unsigned*>(o)[e / 2] = pack_bf16(acc[e] * f, acc[e + 1] * f);
+    }
+    if (a.lse && lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+}
+
+// ---------------------------------------------------------------------------------- host side
+
+typedef CUresult (*tree_encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// Looked up through the runtime: the library carries no link-time dependency on the driver library.
+static tree_encode_fn tree_encode() {
+    static std::atomic<tree_encode_fn> fn{nullptr};
+    tree_encode_fn f = fn.load(std::memory_order_acquire);
+    if (!f) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult qr;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qr) == cudaSuccess && qr == cudaDriverEntryPointSuccess)
+            fn.store(f = reinterpret_cast<tree_encode_fn>(p), std::memory_order_release);
+        else
+            cudaGetLastError();
+    }
+    return f;
+}
+
+// Pool [rows][HD] as [panel][row][128 bytes]: a box is one page, laid out panel by panel.
+static bool tree_page_map(CUtensorMap* map, const dynakv_row_cache* c, void* pool) {
+    const tree_encode_fn enc = tree_encode();
+    if (!enc) return false;
+    const int es = c->kv_dtype == DYNAKV_F32 ? 4 : c->kv_dtype == DYNAKV_BF16 ? 2 : 1;
+    const int row = c->head_dim * es, w = row < 128 ? row : 128;
+    const cuuint64_t dims[3] = {(cuuint64_t)(w / es), (cuuint64_t)(c->n_pages * c->n_kv_heads * PAGE), (cuuint64_t)(row / w)};
+    const cuuint64_t strides[2] = {(cuuint64_t)row, (cuuint64_t)w};
+    const cuuint32_t box[3] = {(cuuint32_t)(w / es), PAGE, (cuuint32_t)(row / w)}, estr[3] = {1, 1, 1};
+    const CUtensorMapDataType dt = es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    return enc(map, dt, 3, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               w == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static int sm_count(int* rc) {
+    constexpr int MAX_DEV = 64;
+    static std::atomic<int> sms[MAX_DEV];
+    int dev = -1;
+    *rc = DYNAKV_ERR_CUDA;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEV) { cudaGetLastError(); return 0; }
+    int n = sms[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) { cudaGetLastError(); return 0; }
+        sms[dev].store(n, std::memory_order_relaxed);
+    }
+    *rc = DYNAKV_OK;
+    return n;
+}
+
+template <int HD, int DT, int RG>
+static int tree_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
+    using C = TreeCfg<HD, DT, RG>;
+    const int grid = sms * C::per_sm;
+    if (cudaFuncSetAttribute(k_tree_attn<HD, DT, RG>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem) != cudaSuccess) return DYNAKV_ERR_CUDA;
+    k_tree_attn<HD, DT, RG><<<grid, C::threads, C::smem, st>>>(mk, mv, a);
+    if (cudaGetLastError() != cudaSuccess) return DYNAKV_ERR_CUDA;
+    using OUT = typename std::conditional<DT == DYNAKV_F32, float, __nv_bfloat16>::type;
+    return launch_pdl(k_tree_merge<HD, C::RT, OUT>, dim3(grid, C::RT / 8), dim3(256), 0, st, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
+}
+
+template <int HD, int DT>
+static int tree_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
+    return rg == 1 ? tree_launch<HD, DT, 1>(mk, mv, a, sms, st) : rg == 2 ? tree_launch<HD, DT, 2>(mk, mv, a, sms, st) : tree_launch<HD, DT, 4>(mk, mv, a, sms, st);
+}
+
+// 16 rows of a tile per row group; the groups needed for all rows of a sequence in one tile, up to four
+static int row_groups(int max_rows) { return max_rows <= 16 ? 1 : max_rows <= 32 ? 2 : 4; }
+
+struct TreeSpace { size_t acc, ml, desc, bytes; };
+static TreeSpace tree_space(int ctas, int rt, int hd) {
+    TreeSpace s;
+    s.acc = 0;
+    s.ml = (size_t)ctas * 2 * rt * hd * 4;
+    s.desc = s.ml + (size_t)ctas * 2 * rt * 8;
+    s.bytes = s.desc + (size_t)ctas * 8 * 4;
+    return s;
+}
+
+static bool tree_shape_ok(const dynakv_row_cache* c, int n_heads, int max_tree) {
+    return row_cache_ok(c) && n_heads >= 1 && n_heads % c->n_kv_heads == 0 && n_heads / c->n_kv_heads <= MAX_G && max_tree >= 1 && max_tree <= TREE_MAX;
+}
+
+}  // namespace dkv
+
+using namespace dkv;
+
+extern "C" int64_t dynakv_attend_tree_workspace(const dynakv_row_cache* cache, int32_t n_heads, int32_t max_tree) {
+    if (!tree_shape_ok(cache, n_heads, max_tree)) return DYNAKV_ERR_ARG;
+    int rc;
+    const int sms = sm_count(&rc);
+    if (rc != DYNAKV_OK) return rc;
+    const int rg = row_groups(max_tree * (n_heads / cache->n_kv_heads));
+    return (int64_t)tree_space(sms * (cache->kv_dtype == DYNAKV_F32 ? 1 : 2), 16 * rg, cache->head_dim).bytes;
+}
+
+extern "C" int dynakv_attend_tree(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
+                                  int32_t n_seqs, int32_t max_tree, const int32_t* page_table, int32_t pages_per_seq, const int32_t* kv_len,
+                                  const uint64_t* tree_mask, int32_t mask_words, float scale, void* out, float* lse, void* workspace,
+                                  int64_t workspace_bytes, uint32_t* status, void* cuda_stream) {
+    if (!tree_shape_ok(cache, n_heads, max_tree) || n_tokens < 0 || n_tokens >= (1ll << 31) || n_seqs < 0 || pages_per_seq < 0 ||
+        pages_per_seq >= (1 << 26) || !(fabsf(scale) <= FLT_MAX) || (tree_mask && (mask_words < 1 || mask_words > TREE_MAX / 64))) return DYNAKV_ERR_ARG;
+    if (n_tokens == 0 || n_seqs == 0) return DYNAKV_OK;
+    if (!q || !q_start || (!page_table && pages_per_seq > 0) || !kv_len || !out || !workspace) return DYNAKV_ERR_ARG;
+    if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)workspace) & 15) return DYNAKV_ERR_ARG;
+    int rc;
+    const int sms = sm_count(&rc);
+    if (rc != DYNAKV_OK) return rc;
+    const int G = n_heads / cache->n_kv_heads, rg = row_groups(max_tree * G), f32 = cache->kv_dtype == DYNAKV_F32;
+    const TreeSpace sp = tree_space(sms * (f32 ? 1 : 2), 16 * rg, cache->head_dim);
+    if (workspace_bytes < (int64_t)sp.bytes) return DYNAKV_ERR_ARG;
+    TreeArgs a;
+    a.q = q; a.q_start = q_start; a.page_table = page_table; a.kv_len = kv_len;
+    a.mask = reinterpret_cast<const unsigned long long*>(tree_mask);
+    a.out = out; a.lse = lse;
+    char* ws = reinterpret_cast<char*>(workspace);
+    a.acc = reinterpret_cast<float*>(ws + sp.acc);
+    a.ml = reinterpret_cast<float2*>(ws + sp.ml);
+    a.desc = reinterpret_cast<int*>(ws + sp.desc);
+    a.status = status;
+    a.kpool = reinterpret_cast<const unsigned char*>(cache->k); a.vpool = reinterpret_cast<const unsigned char*>(cache->v);
+    a.kexp = reinterpret_cast<const signed char*>(cache->k_exp); a.vexp = reinterpret_cast<const signed char*>(cache->v_exp);
+    a.n_tokens = n_tokens; a.n_pages = cache->n_pages;
+    a.n_seqs = n_seqs; a.max_tree = max_tree; a.pages_per_seq = pages_per_seq; a.mask_words = tree_mask ? mask_words : 0;
+    a.G = G; a.Hq = n_heads; a.Hk = cache->n_kv_heads;
+    a.scale = scale;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    // an error left behind by an earlier, unrelated call on this thread must not be reported as this call's
+    cudaGetLastError();
+    CUtensorMap mk, mv;
+    if (!tree_page_map(&mk, cache, cache->k) || !tree_page_map(&mv, cache, cache->v)) return DYNAKV_ERR_CUDA;
+    if (cache->head_dim == 128) {
+        if (f32) return tree_launch_rows<128, DYNAKV_F32>(rg, mk, mv, a, sms, st);
+        if (cache->kv_dtype == DYNAKV_BF16) return tree_launch_rows<128, DYNAKV_BF16>(rg, mk, mv, a, sms, st);
+        return tree_launch_rows<128, DYNAKV_FP8>(rg, mk, mv, a, sms, st);
+    }
+    if (f32) return tree_launch_rows<64, DYNAKV_F32>(rg, mk, mv, a, sms, st);
+    if (cache->kv_dtype == DYNAKV_BF16) return tree_launch_rows<64, DYNAKV_BF16>(rg, mk, mv, a, sms, st);
+    return tree_launch_rows<64, DYNAKV_FP8>(rg, mk, mv, a, sms, st);
+}

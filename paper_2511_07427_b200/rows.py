@@ -38,6 +38,8 @@ SIGNATURES = {
     "dynakv_rows_write": (C.c_int, [_vp, _vp, _vp, _vp, _i64, _vp, _vp]),
     "dynakv_rows_read": (C.c_int, [_vp, _vp, _i32, _vp, _i32, _i64, _i64, _vp, _vp, _vp, _vp]),
 }
+SIGNATURES["dynakv_attend_tree"] = (C.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, C.c_float, _vp, _vp, _vp, _i64, _vp, _vp])
+SIGNATURES["dynakv_attend_tree_workspace"] = (_i64, [_vp, _i32, _i32])
 _bound = None
 
 
@@ -204,6 +206,7 @@ class RowCache:
         self._c = _RowCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if k_exp is not None else None,
                             v_exp.data_ptr() if v_exp is not None else None, self.n_pages, self.n_kv_heads, self.head_dim, self.kv_dtype)
         self._ref = C.byref(self._c)
+        self._workspace = {}           # bytes attend_tree needs, by (heads, max_tree)
 
     @classmethod
     def allocate(cls, n_pages: int, n_kv_heads: int, head_dim: int, kv_dtype: int = BF16, device="cuda") -> "RowCache":
@@ -245,3 +248,58 @@ class RowCache:
         _call(self.device, "dynakv_rows_read", self._ref, _index(page_table, (b, per), self.device, "page_table"), per,
               _index(lengths, (b,), self.device, "lengths"), b, first, n, K.data_ptr(), V.data_ptr(), self._status.data_ptr())
         return K, V
+
+    def attend_tree(self, q, page_table, kv_len, q_start, max_tree: int, tree_mask=None, scale=None, out=None):
+        """Attention of drafted tokens over the cache (``dynakv_attend_tree``): (out, lse).
+
+        q [tokens, heads, d] (fp32 for an fp32 cache, else bf16), the tokens of all sequences one after the other:
+        sequence b has tokens q_start[b] .. q_start[b + 1] - 1 (``q_start`` [sequences + 1] int32), at most ``max_tree`` of
+        them; the last as many of its ``kv_len`` [sequences] int32 rows in ``page_table`` [sequences, pages] int32 are their own, the others the
+        context, which every token sees.  ``tree_mask`` [tokens, words] int64: bit j of a token's words says that it
+        sees row j of its tree (None: a chain, j <= i).  ``scale`` defaults to 1 / sqrt(d).  lse [tokens, heads]
+        fp32 is the natural logarithm of the weights' sum, for merging with attention over other rows.  A token
+        that sees nothing gets zeros and -inf; tokens behind the last sequence are left as they are in ``out``."""
+        torch = _torch()
+        dtype = torch.float32 if self.kv_dtype == F32 else torch.bfloat16
+        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype != dtype or not q.is_contiguous() or q.device != self.device or q.data_ptr() % 16:
+            raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {dtype} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
+                              f"got {q.dtype} {tuple(q.shape)} on {q.device}")
+        _no_gradient(q)
+        n, heads, d = q.shape
+        if heads == 0 or heads % self.n_kv_heads != 0 or heads // self.n_kv_heads > 8:
+            raise DynaKVError(f"{heads} query heads over {self.n_kv_heads} KV heads: expected 1 to 8 per KV head")
+        if not 1 <= max_tree <= MAX_TREE:
+            raise DynaKVError(f"max_tree is {max_tree}: expected 1 to {MAX_TREE}")
+        if page_table.dim() != 2:
+            raise DynaKVError(f"expected page_table of two dimensions, got {tuple(page_table.shape)}")
+        b, per = page_table.shape
+        mask, words = None, 0
+        if tree_mask is not None:
+            words = tree_mask.shape[-1]
+            if tree_mask.dtype != torch.int64 or tuple(tree_mask.shape) != (n, words) or not 1 <= words <= MAX_TREE // 64 or \
+                    not tree_mask.is_contiguous() or tree_mask.device != self.device:
+                raise DynaKVError(f"expected tree_mask as a contiguous int64 tensor [{n}, 1 to {MAX_TREE // 64}] on {self.device}, "
+                                  f"got {tree_mask.dtype} {tuple(tree_mask.shape)} on {tree_mask.device}")
+            mask = tree_mask.data_ptr()
+        if scale is None:
+            scale = d ** -0.5
+        if not math.isfinite(scale):
+            raise DynaKVError(f"scale is {scale}: expected a finite number")
+        if out is None:
+            out = torch.empty_like(q)
+        elif out.dtype != dtype or out.shape != q.shape or not out.is_contiguous() or out.device != self.device or out.data_ptr() % 16:
+            raise DynaKVError(f"expected out as a contiguous, 16-byte aligned {dtype} tensor {tuple(q.shape)} on {self.device}")
+        table, lens, start = _index(page_table, (b, per), self.device, "page_table"), _index(kv_len, (b,), self.device, "kv_len"), \
+            _index(q_start, (b + 1,), self.device, "q_start")
+        lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
+        size = self._workspace.get((heads, max_tree))
+        if size is None:
+            with torch.cuda.device(self.device):
+                size = _library().dynakv_attend_tree_workspace(self._ref, heads, max_tree)
+            if size < 0:
+                raise DynaKVError(f"dynakv_attend_tree_workspace returned {size}")
+            self._workspace[heads, max_tree] = size
+        space = torch.empty(size, dtype=torch.uint8, device=self.device)
+        _call(self.device, "dynakv_attend_tree", self._ref, q.data_ptr(), heads, n, start, b, max_tree, table, per, lens, mask, words, scale,
+              out.data_ptr(), lse.data_ptr(), space.data_ptr(), size, self._status.data_ptr())
+        return out, lse
