@@ -9,6 +9,59 @@
 
 namespace dkv {
 
+// Eight elements as they lie in memory, and as floats.
+template <typename T> struct Raw8 { uint4 w[sizeof(T) / 2]; };
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_raw8(const T* p, bool vec) {
+    Raw8<T> r;
+    if (vec) {
+        r.w[0] = *reinterpret_cast<const uint4*>(p);
+        if constexpr (sizeof(T) == 4) r.w[1] = *reinterpret_cast<const uint4*>(p + 4);
+    } else if constexpr (sizeof(T) == 4) {
+        const unsigned* u = reinterpret_cast<const unsigned*>(p);
+        r.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+        r.w[1] = make_uint4(u[4], u[5], u[6], u[7]);
+    } else {
+        const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
+        r.w[0] = make_uint4(u[0] | (unsigned)u[1] << 16, u[2] | (unsigned)u[3] << 16, u[4] | (unsigned)u[5] << 16, u[6] | (unsigned)u[7] << 16);
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> zero_raw8() {
+    Raw8<T> r;
+    r.w[0] = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (sizeof(T) == 4) r.w[1] = r.w[0];
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&x)[8]) {
+    const unsigned w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+    if constexpr (sizeof(T) == 4) {
+        const unsigned v[4] = {r.w[1].x, r.w[1].y, r.w[1].z, r.w[1].w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) { x[i] = __uint_as_float(w[i]); x[4 + i] = __uint_as_float(v[i]); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+}
+
+// Two fp32 products and sums in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+        " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
 // Eight consecutive elements of a strided array.  vec: base and strides keep every row 16-byte aligned; else the
 // elements are loaded one by one.
 __device__ __forceinline__ void load8(const float* p, bool vec, float (&x)[8]) {

@@ -19,167 +19,189 @@ constexpr int ROW_THREADS = 128;
 
 // ---------------------------------------------------------------------------------- norm + rotary embedding
 //
-// Block (x = token, y = chunk of its rows): the token's sines and cosines are taken once per block, each thread keeps the
-// eight pairs of its own elements in registers and walks over the heads, q heads first, then k heads, then (store) v
-// heads.  A decode step has few tokens, so a token is cut into chunks of one pass over the block; a prompt's tokens are
-// taken whole, which shares the sines by all heads.
+// Block (x = token, y = chunk of its rows): a group of lanes walks over the token's rows, q heads first, then k heads, then
+// (store) v heads, the next row on its way while this one is normed, turned and stored.  The call is bound by the
+// instructions per row as much as by HBM (a first version that normed, turned and weighted in separate steps issued 310
+// per warp and pass and moved 2.4 TB/s), so the constants of a lane's eight elements are folded once per kind of
+// row and block: with a = weight * cos, b = weight of the partner * (+-) sin,
+//     out = f * (x * a + x_partner * b),   f = rsqrt(mean(x^2) + eps)  (1 without a norm),
+// in packed fp32 pairs; rows of v are the kind with a = 1, b = 0, f = 1.
 //
 // The angle in half turns, position * (inv_freq / pi), is one 64-bit product, and its whole turns are removed in 64 bits
 // before the rest is rounded to fp32: at position 2^20 the fp32 product alone would be off by 0.06 rad.
-template <int HD, typename T>
+template <int HD, typename T, bool STORE, bool INTER>
 __global__ void __launch_bounds__(ROW_THREADS) k_norm_rope(HeadRowsDev q, HeadRowsDev k, HeadRowsDev v, int vec, dynakv_rotary ro,
                                                            const int* __restrict__ positions, void* q_out, int q_f32,
                                                            void* k_out, int k_f32, dynakv_row_cache cache,
                                                            const int* __restrict__ slots, int passes, unsigned* status) {
     constexpr int LG = HD / 8, RPP = ROW_THREADS / LG;     // lanes per row, rows per pass
-    __shared__ float2 sc[HD / 2];
+    __shared__ __align__(16) float cos_s[HD / 2], sin_s[HD / 2];
     const long long t = blockIdx.x;
-    const int l = threadIdx.x % LG, grp = threadIdx.x / LG;
-    const bool store = slots != nullptr;
-    const int n_q = ro.n_heads, n_k = ro.n_kv_heads, n_rows = n_q + n_k + (store ? n_k : 0);
-    const int first = blockIdx.y * passes * RPP;
-    const int slot = store ? slots[t] : 0;
+    const int l = threadIdx.x % LG;
+    const int n_q = ro.n_heads, n_k = ro.n_kv_heads, n_rows = n_q + n_k + (STORE ? n_k : 0);
+    int r = blockIdx.y * passes * RPP + threadIdx.x / LG;
+    const T* qp = reinterpret_cast<const T*>(q.p) + t * q.ts + l * 8;
+    const T* kp = reinterpret_cast<const T*>(k.p) + t * k.ts + l * 8;
+    const T* vp = STORE ? reinterpret_cast<const T*>(v.p) + t * v.ts + l * 8 : nullptr;
+    auto load_row = [&](int r) {
+        if (r >= n_rows) return zero_raw8<T>();
+        return load_raw8(r < n_q ? qp + r * q.hs : !STORE || r < n_q + n_k ? kp + (r - n_q) * k.hs : vp + (r - n_q - n_k) * v.hs, vec);
+    };
+    Raw8<T> next = load_row(r);
+    const int slot = STORE ? slots[t] : 0;
     const bool slot_ok = slot >= 0 && slot < cache.n_pages * PAGE;
-    if (store && slot >= 0 && !slot_ok && status && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(status, DYNAKV_ST_BOUNDS);
-
-    if ((int)threadIdx.x < ro.rotary_dim / 2) {
+    if (STORE && slot >= 0 && !slot_ok && status && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(status, DYNAKV_ST_BOUNDS);
+    const int half = ro.rotary_dim / 2;
+    if ((int)threadIdx.x < half) {
         const double turns = (double)positions[t] * ((double)ro.inv_freq[threadIdx.x] * 0.31830988618379067154);   // half turns
-        const float r = (float)(turns - 2.0 * rint(turns * 0.5));
-        float s, c;
-        sincospif(r, &s, &c);
-        sc[threadIdx.x] = make_float2(c, s);
+        const float f = (float)(turns - 2.0 * rint(turns * 0.5));
+        sincospif(f, &sin_s[threadIdx.x], &cos_s[threadIdx.x]);
     }
     __syncthreads();
-    // the rotation of this lane's eight elements: x' = x * cs + partner * sn, the sign of the pair's half in sn
-    float cs[8], sn[8];
     const bool turned = l * 8 < ro.rotary_dim;             // rotary_dim is a multiple of 16: a lane is wholly in or out
-    const int half = ro.rotary_dim / 2;
-    int partner = l;
-    if (turned) {
-        if (ro.interleaved) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) { const float2 a = sc[l * 4 + i / 2]; cs[i] = a.x; sn[i] = (i & 1) ? a.y : -a.y; }
-        } else {
-            const bool upper = l * 8 >= half;
-            partner = upper ? l - half / 8 : l + half / 8;
-#pragma unroll
-            for (int i = 0; i < 8; i++) { const float2 a = sc[l * 8 + i - (upper ? half : 0)]; cs[i] = a.x; sn[i] = upper ? a.y : -a.y; }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) { cs[i] = 1.f; sn[i] = 0.f; }
-    }
-    float wq[8], wk[8];
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        wq[i] = ro.q_weight ? ro.q_weight[l * 8 + i] : 1.f;
-        wk[i] = ro.k_weight ? ro.k_weight[l * 8 + i] : 1.f;
-    }
+    const bool upper = !INTER && l * 8 >= half;
+    // half-split pairs: the lane with the partners of this lane's elements, half being a multiple of 8
+    const int step = INTER || !turned ? 0 : upper ? -(half / 8) : half / 8;
+    const int partner = (threadIdx.x & 31) + step;
 
-    auto row_ptr = [&](int r) -> const T* {
-        const HeadRowsDev& a = r < n_q ? q : r < n_q + n_k ? k : v;
-        const int h = r < n_q ? r : r < n_q + n_k ? r - n_q : r - n_q - n_k;
-        return reinterpret_cast<const T*>(a.p) + t * a.ts + h * a.hs + l * 8;
-    };
-    // the next row is on its way while this one is normed, turned and stored; every lane takes part in the shuffles
-    float nx[8];
-    {
-        const int r = first + grp;
-        if (r < n_rows) load8(row_ptr(r), vec, nx);
-        else {
+    float2 a[4], b[4];                                     // the constants of a kind of row
+    int kind = -1;                                         // 0: q, 1: k, 2: v
+    bool norm = false;
+    auto fold = [&]() {
+        const float* w = kind == 0 ? ro.q_weight : kind == 1 ? ro.k_weight : nullptr;
+        norm = w != nullptr;
+        float own[8], other[8];
+        if (norm) {
+            const bool wide = ((uintptr_t)w & 15) == 0;
+            load8(w + l * 8, wide, own);
+            load8(w + (l + step) * 8, wide, other);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; i++) nx[i] = 0.f;
+            for (int i = 0; i < 8; i++) own[i] = other[i] = 1.f;
         }
-    }
-    for (int p = 0; p < passes; p++) {
-        const int r = first + p * RPP + grp;
+        float c[8], s[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) { c[i] = 1.f; s[i] = 0.f; }
+        if (turned && kind < 2) {
+            if constexpr (INTER) {
+                const float4 cv = *reinterpret_cast<const float4*>(cos_s + l * 4), sv = *reinterpret_cast<const float4*>(sin_s + l * 4);
+                c[0] = c[1] = cv.x; c[2] = c[3] = cv.y; c[4] = c[5] = cv.z; c[6] = c[7] = cv.w;
+                s[0] = -sv.x; s[1] = sv.x; s[2] = -sv.y; s[3] = sv.y; s[4] = -sv.z; s[5] = sv.z; s[6] = -sv.w; s[7] = sv.w;
+            } else {
+                const int j = l * 8 - (upper ? half : 0);
+                load8(cos_s + j, true, c);
+                load8(sin_s + j, true, s);
+                if (!upper) {
+#pragma unroll
+                    for (int i = 0; i < 8; i++) s[i] = -s[i];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            a[i] = make_float2(own[2 * i] * c[2 * i], own[2 * i + 1] * c[2 * i + 1]);
+            b[i] = INTER ? make_float2(own[2 * i + 1] * s[2 * i], own[2 * i] * s[2 * i + 1]) : make_float2(other[2 * i] * s[2 * i], other[2 * i + 1] * s[2 * i + 1]);
+        }
+    };
+
+    for (int p = 0; p < passes; p++, r += RPP) {
         float x[8];
+        unpack8(next, x);
+        if (p + 1 < passes) next = load_row(r + RPP);
+        const bool live = r < n_rows;
+        const int now = r < n_q ? 0 : !STORE || r < n_q + n_k ? 1 : 2;
+        if (now != kind) { kind = now; fold(); }
+        float2 sq = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = nx[i];
-        if (p + 1 < passes && r + RPP < n_rows) load8(row_ptr(r + RPP), vec, nx);
-        const bool live = r < n_rows, is_q = r < n_q, is_v = r >= n_q + n_k;
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; i++) ss = fmaf(x[i], x[i], ss);
+        for (int i = 0; i < 4; i++) { const float2 y = make_float2(x[2 * i], x[2 * i + 1]); sq = fma2(y, y, sq); }
+        float ss = sq.x + sq.y;
 #pragma unroll
         for (int o = LG / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const bool norm = !is_v && (is_q ? ro.q_weight != nullptr : ro.k_weight != nullptr);
-        const float f = norm ? 1.f / sqrtf(ss * (1.f / HD) + ro.eps) : 1.f;
-        if (norm) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = x[i] * f * (is_q ? wq[i] : wk[i]);
-        }
-        float y[8];
-        if (ro.interleaved) {
+        const float f = norm ? rsqrtf(ss * (1.f / HD) + ro.eps) : 1.f;
+        float y[8];                                        // the partners
+        if constexpr (INTER) {
 #pragma unroll
             for (int i = 0; i < 8; i++) y[i] = x[i ^ 1];
         } else {
-            const int src = (threadIdx.x & 31) - l + partner;
 #pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = __shfl_sync(0xffffffffu, x[i], src);
-        }
-        if (turned && !is_v) {
+            for (int i = 0; i < 8; i++) y[i] = __shfl_sync(0xffffffffu, x[i], partner);
+            if (!turned || kind == 2) {                    // not its own partner: an infinity there would make 0 * inf
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = fmaf(x[i], cs[i], y[i] * sn[i]);
+                for (int i = 0; i < 8; i++) y[i] = 0.f;
+            }
         }
-        if (is_q) {
+        if (INTER && (!turned || kind == 2)) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) y[i] = 0.f;
+        }
+        const float2 ff = make_float2(f, f);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float2 o = mul2(make_float2(y[2 * i], y[2 * i + 1]), b[i]);
+            o = mul2(fma2(make_float2(x[2 * i], x[2 * i + 1]), a[i], o), ff);
+            x[2 * i] = o.x; x[2 * i + 1] = o.y;
+        }
+        if (kind == 0) {
             if (live) {
                 const size_t at = ((size_t)t * n_q + r) * HD + l * 8;
                 if (q_f32) store8(reinterpret_cast<float*>(q_out) + at, x);
                 else store8(reinterpret_cast<__nv_bfloat16*>(q_out) + at, x);
             }
-        } else if (!store) {
+        } else if (!STORE) {
             if (live) {
                 const size_t at = ((size_t)t * n_k + r - n_q) * HD + l * 8;
                 if (k_f32) store8(reinterpret_cast<float*>(k_out) + at, x);
                 else store8(reinterpret_cast<__nv_bfloat16*>(k_out) + at, x);
             }
         }
-        if (store) {         // all lanes of the warp come here: an FP8 row's maximum is exchanged by shuffles
-            const int h = is_v ? r - n_q - n_k : r - n_q;
+        if (STORE && __any_sync(0xffffffffu, kind != 0)) {     // the whole warp: an FP8 row's maximum is exchanged by shuffles
+            const int h = kind == 2 ? r - n_q - n_k : r - n_q;
             const long long row = ((long long)(slot >> 5) * n_k + h) * PAGE + (slot & 31);
-            store_cache8<HD>(cache, is_v, row, live && !is_q && slot_ok, l, x);
+            store_cache8<HD>(cache, kind == 2, row, live && kind != 0 && slot_ok, l, x);
         }
     }
 }
 
 // ---------------------------------------------------------------------------------- rows into the cache
 //
-// One flat list of rows, (token, k or v, head); a group of lanes takes WR of them, all loads before the first store.
+// A token's 2 * n_kv_heads rows (k heads, then v heads) side by side in a block's groups of lanes, as many tokens as fit
+// (or, with many heads, part of a token: blockIdx.y); each group takes the same row of `per` <= WR tokens, all loads before
+// the first store.  Which row that is takes one division per thread.
 constexpr int WR = 4;
 template <int HD, typename T>
 __global__ void __launch_bounds__(ROW_THREADS) k_rows_write(HeadRowsDev k, HeadRowsDev v, int vec, dynakv_row_cache cache,
-                                                            const int* __restrict__ slots, long long n_rows, int per, unsigned* status) {
+                                                            const int* __restrict__ slots, long long n, int per, unsigned* status) {
     constexpr int LG = HD / 8, RPP = ROW_THREADS / LG;
     const int l = threadIdx.x % LG, grp = threadIdx.x / LG;
-    const int nk = cache.n_kv_heads;
-    float x[WR][8];
-    long long row[WR];
-    bool live[WR], is_v[WR];
-    const long long r0 = (long long)blockIdx.x * (RPP * per) + grp;
+    const int nk = cache.n_kv_heads, tp = 2 * nk <= RPP ? RPP / (2 * nk) : 1;      // tokens side by side
+    const int dt = tp > 1 ? grp / (2 * nk) : 0;
+    const int h2 = blockIdx.y * RPP + grp - dt * 2 * nk;
+    const bool there = dt < tp && h2 < 2 * nk, is_v = h2 >= nk;
+    const int h = is_v ? h2 - nk : h2;
+    const HeadRowsDev& from = is_v ? v : k;
+    const T* p = reinterpret_cast<const T*>(from.p) + h * from.hs + l * 8;
+    const long long t0 = (long long)blockIdx.x * (tp * per) + dt;
+    Raw8<T> raw[WR];
+    int slot[WR];
 #pragma unroll
     for (int i = 0; i < WR; i++) {
-        const long long r = r0 + i * RPP;
-        live[i] = i < per && r < n_rows;
-        is_v[i] = false;
-        row[i] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; j++) x[i][j] = 0.f;
-        if (live[i]) {
-            const long long t = r / (2 * nk);
-            const int h2 = (int)(r - t * (2 * nk));
-            is_v[i] = h2 >= nk;
-            const int h = is_v[i] ? h2 - nk : h2;
-            const int slot = slots[t];
-            const HeadRowsDev& a = is_v[i] ? v : k;
-            load8(reinterpret_cast<const T*>(a.p) + t * a.ts + h * a.hs + l * 8, vec, x[i]);
-            live[i] = slot >= 0 && slot < cache.n_pages * PAGE;
-            if (slot >= 0 && !live[i] && status && l == 0 && h2 == 0) atomicOr(status, DYNAKV_ST_BOUNDS);
-            row[i] = ((long long)(slot >> 5) * nk + h) * PAGE + (slot & 31);
+        const long long t = t0 + i * tp;
+        raw[i] = zero_raw8<T>();
+        slot[i] = -1;
+        if (i < per && there && t < n) {
+            raw[i] = load_raw8(p + t * from.ts, vec);
+            slot[i] = slots[t];
         }
     }
 #pragma unroll
-    for (int i = 0; i < WR; i++) if (i < per) store_cache8<HD>(cache, is_v[i], row[i], live[i], l, x[i]);
+    for (int i = 0; i < WR; i++) {
+        if (i >= per) break;
+        const bool live = slot[i] >= 0 && slot[i] < cache.n_pages * PAGE;
+        if (slot[i] >= 0 && !live && status && l == 0 && h2 == 0) atomicOr(status, DYNAKV_ST_BOUNDS);
+        float x[8];
+        unpack8(raw[i], x);
+        store_cache8<HD>(cache, is_v, ((long long)(slot[i] >> 5) * nk + h) * PAGE + (slot[i] & 31), live, l, x);
+    }
 }
 
 // ---------------------------------------------------------------------------------- rows out of the cache
@@ -283,24 +305,32 @@ static int norm_rope(const dynakv_rotary* ro, const dynakv_head_rows* q, const d
     if (!float_type(q->dtype) || !head_rows_ok(q, q->dtype) || !head_rows_ok(k, q->dtype) || (v && !head_rows_ok(v, q->dtype)) || !positions ||
         !q_out || ((uintptr_t)q_out & 15) || (k_out && ((uintptr_t)k_out & 15))) return DYNAKV_ERR_ARG;
     const int rpp = ROW_THREADS / (ro->head_dim / 8);
-    const int rows = ro->n_heads + ro->n_kv_heads * (cache ? 2 : 1);
-    const int chunks = (rows + rpp - 1) / rpp;
-    // a whole token per block once that gives every SM (148) its 16 resident blocks; below that one pass per block, so
-    // that a decode step spreads over the SMs (16 tokens x 32 rows: 64 blocks of one pass against 16 blocks of four)
-    const int passes = n >= 148 * 16 ? chunks : 1;
+    const int rows = ro->n_heads + ro->n_kv_heads * (cache ? 2 : 1), chunks = (rows + rpp - 1) / rpp;
+    // a whole token per block once there are two blocks for every SM (148), which shares the sines and the folded constants by all
+    // of its rows; fewer tokens (a decode step) spread over the SMs, one pass per block
+    const int passes = n >= 148 * 2 ? chunks : 1;
     const dim3 grid((unsigned)n, (unsigned)((chunks + passes - 1) / passes));
     const int vec = head_rows_vec(q) && head_rows_vec(k) && (!v || head_rows_vec(v));
     const HeadRowsDev dq = head_rows_dev(q), dk = head_rows_dev(k), dv = v ? head_rows_dev(v) : HeadRowsDev{nullptr, 0, 0};
     const dynakv_row_cache c = cache ? *cache : dynakv_row_cache{};
     const int qf = q_dtype == DYNAKV_F32, kf = k_dtype == DYNAKV_F32;
     forget_errors();
+#define DKV_ROPE(HD, T, STORE, INTER) \
+    k_norm_rope<HD, T, STORE, INTER><<<grid, ROW_THREADS, 0, st>>>(dq, dk, dv, vec, *ro, positions, q_out, qf, k_out, kf, c, slots, passes, status)
+#define DKV_ROPE_KIND(HD, T) \
+    do { \
+        if (cache) { if (ro->interleaved) DKV_ROPE(HD, T, true, true); else DKV_ROPE(HD, T, true, false); } \
+        else { if (ro->interleaved) DKV_ROPE(HD, T, false, true); else DKV_ROPE(HD, T, false, false); } \
+    } while (0)
     if (ro->head_dim == 128) {
-        if (q->dtype == DYNAKV_F32) k_norm_rope<128, float><<<grid, ROW_THREADS, 0, st>>>(dq, dk, dv, vec, *ro, positions, q_out, qf, k_out, kf, c, slots, passes, status);
-        else k_norm_rope<128, __nv_bfloat16><<<grid, ROW_THREADS, 0, st>>>(dq, dk, dv, vec, *ro, positions, q_out, qf, k_out, kf, c, slots, passes, status);
+        if (q->dtype == DYNAKV_F32) DKV_ROPE_KIND(128, float);
+        else DKV_ROPE_KIND(128, __nv_bfloat16);
     } else {
-        if (q->dtype == DYNAKV_F32) k_norm_rope<64, float><<<grid, ROW_THREADS, 0, st>>>(dq, dk, dv, vec, *ro, positions, q_out, qf, k_out, kf, c, slots, passes, status);
-        else k_norm_rope<64, __nv_bfloat16><<<grid, ROW_THREADS, 0, st>>>(dq, dk, dv, vec, *ro, positions, q_out, qf, k_out, kf, c, slots, passes, status);
+        if (q->dtype == DYNAKV_F32) DKV_ROPE_KIND(64, float);
+        else DKV_ROPE_KIND(64, __nv_bfloat16);
     }
+#undef DKV_ROPE_KIND
+#undef DKV_ROPE
     return launched();
 }
 
@@ -326,23 +356,22 @@ extern "C" int dynakv_rows_write(const dynakv_row_cache* cache, const dynakv_hea
     if (!row_cache_ok(cache) || !k || !v || n < 0 || n >= (1ll << 31)) return DYNAKV_ERR_ARG;
     if (n == 0) return DYNAKV_OK;
     if (!float_type(k->dtype) || !head_rows_ok(k, k->dtype) || !head_rows_ok(v, k->dtype) || !slots) return DYNAKV_ERR_ARG;
-    const long long rows = n * 2 * cache->n_kv_heads;
-    const int rpp = ROW_THREADS / (cache->head_dim / 8);
-    // few rows: one per group of lanes, over as many blocks as there are; many: four, for the loads in flight
-    const int per = rows >= 148ll * 8 * rpp * WR ? WR : 1;
-    const long long blocks = (rows + rpp * per - 1) / (rpp * per);
-    if (blocks >= (1ll << 31)) return DYNAKV_ERR_TOO_LARGE;
+    const int rpp = ROW_THREADS / (cache->head_dim / 8), rows = 2 * cache->n_kv_heads;
+    const int tp = rows <= rpp ? rpp / rows : 1, chunks = (rows + rpp - 1) / rpp;
+    if (chunks > 65535) return DYNAKV_ERR_TOO_LARGE;
+    // few tokens: one per group of lanes, over as many blocks as that gives; many: four, for the loads in flight
+    const int per = n * chunks >= 148ll * 8 * tp * WR ? WR : 1;
+    const dim3 g((unsigned)((n + tp * per - 1) / (tp * per)), (unsigned)chunks);
     const int vec = head_rows_vec(k) && head_rows_vec(v);
     const HeadRowsDev dk = head_rows_dev(k), dv = head_rows_dev(v);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const unsigned g = (unsigned)blocks;
     forget_errors();
     if (cache->head_dim == 128) {
-        if (k->dtype == DYNAKV_F32) k_rows_write<128, float><<<g, ROW_THREADS, 0, st>>>(dk, dv, vec, *cache, slots, rows, per, status);
-        else k_rows_write<128, __nv_bfloat16><<<g, ROW_THREADS, 0, st>>>(dk, dv, vec, *cache, slots, rows, per, status);
+        if (k->dtype == DYNAKV_F32) k_rows_write<128, float><<<g, ROW_THREADS, 0, st>>>(dk, dv, vec, *cache, slots, n, per, status);
+        else k_rows_write<128, __nv_bfloat16><<<g, ROW_THREADS, 0, st>>>(dk, dv, vec, *cache, slots, n, per, status);
     } else {
-        if (k->dtype == DYNAKV_F32) k_rows_write<64, float><<<g, ROW_THREADS, 0, st>>>(dk, dv, vec, *cache, slots, rows, per, status);
-        else k_rows_write<64, __nv_bfloat16><<<g, ROW_THREADS, 0, st>>>(dk, dv, vec, *cache, slots, rows, per, status);
+        if (k->dtype == DYNAKV_F32) k_rows_write<64, float><<<g, ROW_THREADS, 0, st>>>(dk, dv, vec, *cache, slots, n, per, status);
+        else k_rows_write<64, __nv_bfloat16><<<g, ROW_THREADS, 0, st>>>(dk, dv, vec, *cache, slots, n, per, status);
     }
     return launched();
 }

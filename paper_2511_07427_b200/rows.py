@@ -8,6 +8,7 @@ compute no gradients and refuse inputs that would need one.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 
 from .binding import BF16, F32, FP8, DynaKVError, load_library
@@ -60,44 +61,67 @@ def _torch():
 
 
 def _float_type(dtype, what: str) -> int:
-    torch = _torch()
-    if dtype == torch.bfloat16:
+    if dtype is _bf16():
         return BF16
-    if dtype == torch.float32:
+    if dtype is _f32():
         return F32
     raise DynaKVError(f"{what} is {dtype}: expected torch.float32 or torch.bfloat16")
 
 
-def _index(t, shape, device, what: str):
-    """A contiguous int32 tensor of `shape` on `device`."""
-    torch = _torch()
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
-        raise DynaKVError(f"expected {what} as a contiguous int32 tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+@functools.lru_cache(None)
+def _bf16():
+    return _torch().bfloat16
+
+
+@functools.lru_cache(None)
+def _f32():
+    return _torch().float32
+
+
+@functools.lru_cache(None)
+def _i32_type():
+    return _torch().int32
+
+
+def _index(t, shape: tuple, device: int, what: str) -> int:
+    """A contiguous int32 tensor of `shape` on CUDA device `device`; its address."""
+    if t.dtype is not _i32_type() or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise DynaKVError(f"expected {what} as a contiguous int32 tensor of shape {shape} on cuda:{device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _heads(t, n: int, heads: int, d: int, device, dtype, what: str) -> _HeadRows:
+def _heads(t, shape: tuple, device: int, dtype, what: str) -> _HeadRows:
     """A [n, heads, d] tensor whose last dimension is contiguous; the other strides are free."""
-    if tuple(t.shape) != (n, heads, d) or t.device != device or t.dtype != dtype or (t.stride(2) != 1 and d > 1):
-        raise DynaKVError(f"expected {what} as a {dtype} tensor of shape {(n, heads, d)} on {device} with a contiguous last dimension, "
-                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {tuple(t.stride())}")
-    return _HeadRows(t.data_ptr(), t.stride(0), t.stride(1), _float_type(dtype, what))
+    stride = t.stride()
+    if t.shape != shape or t.get_device() != device or t.dtype is not dtype or stride[2] != 1:
+        raise DynaKVError(f"expected {what} as a {dtype} tensor of shape {shape} on cuda:{device} with a contiguous last dimension, "
+                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {stride}")
+    if t.requires_grad and _torch().is_grad_enabled():
+        _no_gradient()
+    return _HeadRows(t.data_ptr(), stride[0], stride[1], _float_type(dtype, what))
 
 
-def _no_gradient(*tensors) -> None:
-    if _torch().is_grad_enabled() and any(t.requires_grad for t in tensors):
-        raise DynaKVError("this call computes no gradients: detach its inputs or run it under torch.no_grad()")
+def _no_gradient() -> None:
+    raise DynaKVError("this call computes no gradients: detach its inputs or run it under torch.no_grad()")
 
 
-def _call(device, name: str, *args) -> None:
-    """One C call on the device's current stream (its last argument), with the device made current when it is not."""
+@functools.lru_cache(None)
+def _stream_of():
+    """device index -> address of its current stream: torch's raw accessor, which makes no Stream object (1.5 us a call less)."""
     torch = _torch()
-    fn = getattr(_library(), name)
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw if raw is not None else lambda device: torch.cuda.current_stream(device).cuda_stream
+
+
+def _call(device: int, name: str, *args) -> None:
+    """One C call on the device's current stream (its last argument), with the device made current when it is not."""
+    cuda = _torch().cuda
+    fn = getattr(_bound or _library(), name)
+    if cuda.current_device() == device:
+        rc = fn(*args, _stream_of()(device))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        with cuda.device(device):
+            rc = fn(*args, _stream_of()(device))
     if rc != 0:
         raise DynaKVError(f"{name} returned {rc}")
 
@@ -127,6 +151,7 @@ class HeadRotary:
         if rotary_dim > self.head_dim or rotary_dim % 16 != 0:
             raise DynaKVError(f"inv_freq has {inv_freq.numel()} elements: rotary_dim = {rotary_dim} has to be a multiple of 16 up to head_dim")
         self.device = _on_cuda(inv_freq, "inv_freq")
+        self._index = inv_freq.get_device()
         for name, w, numel in (("inv_freq", inv_freq, rotary_dim // 2), ("q_weight", q_weight, self.head_dim), ("k_weight", k_weight, self.head_dim)):
             if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (numel,) or not w.is_contiguous() or w.device != self.device):
                 raise DynaKVError(f"expected {name} as a contiguous float32 tensor of {numel} elements on {self.device}, got {w.dtype} {tuple(w.shape)} on {w.device}")
@@ -138,10 +163,11 @@ class HeadRotary:
         self._ref = C.byref(self._c)
 
     def _q_k(self, q, k):
-        n = q.shape[0]
-        _no_gradient(q, k)
-        return n, _heads(q, n, self.n_heads, self.head_dim, self.device, q.dtype, "q"), \
-            _heads(k, n, self.n_kv_heads, self.head_dim, self.device, q.dtype, "k")
+        if q.dim() != 3:
+            raise DynaKVError(f"expected q of three dimensions, got {tuple(q.shape)}")
+        n, dtype = q.shape[0], q.dtype
+        return n, dtype, _heads(q, (n, self.n_heads, self.head_dim), self._index, dtype, "q"), \
+            _heads(k, (n, self.n_kv_heads, self.head_dim), self._index, dtype, "k")
 
     def apply(self, q, k, positions, q_dtype=None, k_dtype=None):
         """q [n, heads, d], k [n, KV heads, d] (fp32 or bf16, any token and head strides), positions [n] int32 ->
@@ -149,27 +175,28 @@ class HeadRotary:
         sequence an fp32 q is what ``DynaKV.decode_step`` takes and k what ``DynaKV.append`` takes, as [U, G, d] and
         [U, d] views."""
         torch = _torch()
-        n, qr, kr = self._q_k(q, k)
-        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=q_dtype or q.dtype, device=self.device)
-        k_out = torch.empty((n, self.n_kv_heads, self.head_dim), dtype=k_dtype or q.dtype, device=self.device)
-        _call(self.device, "dynakv_norm_rope", self._ref, C.byref(qr), C.byref(kr), _index(positions, (n,), self.device, "positions"), n,
-              q_out.data_ptr(), _float_type(q_out.dtype, "q_dtype"), k_out.data_ptr(), _float_type(k_out.dtype, "k_dtype"))
+        n, dtype, qr, kr = self._q_k(q, k)
+        q_dtype, k_dtype = q_dtype or dtype, k_dtype or dtype
+        qt, kt, place = _float_type(q_dtype, "q_dtype"), _float_type(k_dtype, "k_dtype"), _index(positions, (n,), self._index, "positions")
+        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=q_dtype, device=self.device)
+        k_out = torch.empty((n, self.n_kv_heads, self.head_dim), dtype=k_dtype, device=self.device)
+        _call(self._index, "dynakv_norm_rope", self._ref, C.byref(qr), C.byref(kr), place, n, q_out.data_ptr(), qt, k_out.data_ptr(), kt)
         return q_out, k_out
 
     def store(self, q, k, v, positions, cache: "RowCache", slots, q_dtype=None):
         """As ``apply``, with the keys and the values v [n, KV heads, d] going into ``slots`` [n] int32 of ``cache``
         (``RowCache.write``'s rules) in the same launch.  Returns q."""
         torch = _torch()
-        n, qr, kr = self._q_k(q, k)
-        _no_gradient(v)
-        vr = _heads(v, n, self.n_kv_heads, self.head_dim, self.device, q.dtype, "v")
-        if cache.device != self.device or cache.head_dim != self.head_dim or cache.n_kv_heads != self.n_kv_heads:
+        n, dtype, qr, kr = self._q_k(q, k)
+        vr = _heads(v, (n, self.n_kv_heads, self.head_dim), self._index, dtype, "v")
+        if cache._index != self._index or cache.head_dim != self.head_dim or cache.n_kv_heads != self.n_kv_heads:
             raise DynaKVError(f"the cache holds {cache.n_kv_heads} heads of {cache.head_dim} on {cache.device}, the embedding has "
                               f"{self.n_kv_heads} of {self.head_dim} on {self.device}")
-        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=q_dtype or q.dtype, device=self.device)
-        _call(self.device, "dynakv_norm_rope_store", self._ref, C.byref(qr), C.byref(kr), C.byref(vr),
-              _index(positions, (n,), self.device, "positions"), n, q_out.data_ptr(), _float_type(q_out.dtype, "q_dtype"), cache._ref,
-              _index(slots, (n,), self.device, "slots"), cache._status.data_ptr())
+        q_dtype = q_dtype or dtype
+        qt, place, slot = _float_type(q_dtype, "q_dtype"), _index(positions, (n,), self._index, "positions"), _index(slots, (n,), self._index, "slots")
+        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=q_dtype, device=self.device)
+        _call(self._index, "dynakv_norm_rope_store", self._ref, C.byref(qr), C.byref(kr), C.byref(vr), place, n, q_out.data_ptr(), qt,
+              cache._ref, slot, cache._status_at)
         return q_out
 
 
@@ -183,6 +210,7 @@ class RowCache:
     def __init__(self, k, v, k_exp=None, v_exp=None):
         torch = _torch()
         self.device = _on_cuda(k, "k")
+        self._index = k.get_device()
         if k.dim() != 4 or k.shape[2] != PAGE or k.shape[3] not in (64, 128) or k.numel() == 0:
             raise DynaKVError(f"expected k of shape [pages, KV heads, {PAGE}, 64 or 128], got {tuple(k.shape)}")
         types = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: FP8, torch.uint8: FP8}
@@ -203,6 +231,7 @@ class RowCache:
             raise DynaKVError("the cache's tensors have to be 16-byte aligned")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._status_at = self._status.data_ptr()
         self._c = _RowCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if k_exp is not None else None,
                             v_exp.data_ptr() if v_exp is not None else None, self.n_pages, self.n_kv_heads, self.head_dim, self.kv_dtype)
         self._ref = C.byref(self._c)
@@ -227,12 +256,12 @@ class RowCache:
     def write(self, k, v, slots) -> None:
         """Rows k, v [n, KV heads, d] (fp32 or bf16, any token and head strides) into ``slots`` [n] int32, rounded to the
         cache's type.  A negative slot skips its token; slots >= 0 must differ."""
-        n = k.shape[0]
-        _no_gradient(k, v)
-        kr = _heads(k, n, self.n_kv_heads, self.head_dim, self.device, k.dtype, "k")
-        vr = _heads(v, n, self.n_kv_heads, self.head_dim, self.device, k.dtype, "v")
-        _call(self.device, "dynakv_rows_write", self._ref, C.byref(kr), C.byref(vr), _index(slots, (n,), self.device, "slots"), n,
-              self._status.data_ptr())
+        if k.dim() != 3:
+            raise DynaKVError(f"expected k of three dimensions, got {tuple(k.shape)}")
+        n, dtype = k.shape[0], k.dtype
+        shape = (n, self.n_kv_heads, self.head_dim)
+        kr, vr = _heads(k, shape, self._index, dtype, "k"), _heads(v, shape, self._index, dtype, "v")
+        _call(self._index, "dynakv_rows_write", self._ref, C.byref(kr), C.byref(vr), _index(slots, (n,), self._index, "slots"), n, self._status_at)
 
     def read(self, page_table, lengths, n: int, first: int = 0):
         """Rows [first, first + n) of every sequence in order, (K, V) of shape [sequences, KV heads, n, d], fp32 for an
@@ -242,11 +271,10 @@ class RowCache:
         if page_table.dim() != 2 or n < 0 or first < 0:
             raise DynaKVError(f"expected page_table of two dimensions, n >= 0 and first >= 0, got {tuple(page_table.shape)}, {n}, {first}")
         b, per = page_table.shape
-        dtype = torch.float32 if self.kv_dtype == F32 else torch.bfloat16
-        K = torch.empty((b, self.n_kv_heads, n, self.head_dim), dtype=dtype, device=self.device)
-        V = torch.empty_like(K)
-        _call(self.device, "dynakv_rows_read", self._ref, _index(page_table, (b, per), self.device, "page_table"), per,
-              _index(lengths, (b,), self.device, "lengths"), b, first, n, K.data_ptr(), V.data_ptr(), self._status.data_ptr())
+        table, lens = _index(page_table, (b, per), self._index, "page_table"), _index(lengths, (b,), self._index, "lengths")
+        shape, dtype = (b, self.n_kv_heads, n, self.head_dim), torch.float32 if self.kv_dtype == F32 else torch.bfloat16
+        K, V = torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device)
+        _call(self._index, "dynakv_rows_read", self._ref, table, per, lens, b, first, n, K.data_ptr(), V.data_ptr(), self._status_at)
         return K, V
 
     def attend_tree(self, q, page_table, kv_len, q_start, max_tree: int, tree_mask=None, scale=None, out=None):
@@ -261,10 +289,11 @@ class RowCache:
         that sees nothing gets zeros and -inf; tokens behind the last sequence are left as they are in ``out``."""
         torch = _torch()
         dtype = torch.float32 if self.kv_dtype == F32 else torch.bfloat16
-        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype != dtype or not q.is_contiguous() or q.device != self.device or q.data_ptr() % 16:
+        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != self._index or q.data_ptr() % 16:
             raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {dtype} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
                               f"got {q.dtype} {tuple(q.shape)} on {q.device}")
-        _no_gradient(q)
+        if q.requires_grad and torch.is_grad_enabled():
+            _no_gradient()
         n, heads, d = q.shape
         if heads == 0 or heads % self.n_kv_heads != 0 or heads // self.n_kv_heads > 8:
             raise DynaKVError(f"{heads} query heads over {self.n_kv_heads} KV heads: expected 1 to 8 per KV head")
@@ -276,8 +305,8 @@ class RowCache:
         mask, words = None, 0
         if tree_mask is not None:
             words = tree_mask.shape[-1]
-            if tree_mask.dtype != torch.int64 or tuple(tree_mask.shape) != (n, words) or not 1 <= words <= MAX_TREE // 64 or \
-                    not tree_mask.is_contiguous() or tree_mask.device != self.device:
+            if tree_mask.dtype is not torch.int64 or tree_mask.shape != (n, words) or not 1 <= words <= MAX_TREE // 64 or \
+                    not tree_mask.is_contiguous() or tree_mask.get_device() != self._index:
                 raise DynaKVError(f"expected tree_mask as a contiguous int64 tensor [{n}, 1 to {MAX_TREE // 64}] on {self.device}, "
                                   f"got {tree_mask.dtype} {tuple(tree_mask.shape)} on {tree_mask.device}")
             mask = tree_mask.data_ptr()
@@ -287,10 +316,10 @@ class RowCache:
             raise DynaKVError(f"scale is {scale}: expected a finite number")
         if out is None:
             out = torch.empty_like(q)
-        elif out.dtype != dtype or out.shape != q.shape or not out.is_contiguous() or out.device != self.device or out.data_ptr() % 16:
+        elif out.dtype is not dtype or out.shape != q.shape or not out.is_contiguous() or out.get_device() != self._index or out.data_ptr() % 16:
             raise DynaKVError(f"expected out as a contiguous, 16-byte aligned {dtype} tensor {tuple(q.shape)} on {self.device}")
-        table, lens, start = _index(page_table, (b, per), self.device, "page_table"), _index(kv_len, (b,), self.device, "kv_len"), \
-            _index(q_start, (b + 1,), self.device, "q_start")
+        table, lens, start = _index(page_table, (b, per), self._index, "page_table"), _index(kv_len, (b,), self._index, "kv_len"), \
+            _index(q_start, (b + 1,), self._index, "q_start")
         lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
         size = self._workspace.get((heads, max_tree))
         if size is None:
@@ -300,6 +329,6 @@ class RowCache:
                 raise DynaKVError(f"dynakv_attend_tree_workspace returned {size}")
             self._workspace[heads, max_tree] = size
         space = torch.empty(size, dtype=torch.uint8, device=self.device)
-        _call(self.device, "dynakv_attend_tree", self._ref, q.data_ptr(), heads, n, start, b, max_tree, table, per, lens, mask, words, scale,
-              out.data_ptr(), lse.data_ptr(), space.data_ptr(), size, self._status.data_ptr())
+        _call(self._index, "dynakv_attend_tree", self._ref, q.data_ptr(), heads, n, start, b, max_tree, table, per, lens, mask, words, scale,
+              out.data_ptr(), lse.data_ptr(), space.data_ptr(), size, self._status_at)
         return out, lse
