@@ -29,80 +29,9 @@
 #include <cuda_fp16.h>
 
 #include "common.cuh"
+#include "tc_ops.cuh"
 
 namespace dkv {
-
-// ------------------------------------------------------------------ small PTX wrappers
-
-__device__ __forceinline__ unsigned tc_smem_u32(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void tc_mbar_init(unsigned bar, unsigned count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void tc_mbar_arrive(unsigned bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tc_mbar_expect_tx(unsigned bar, unsigned bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
-}
-// One poll; the thread is suspended in hardware until the phase completes or about `hint_ns` have passed, so
-// a waiting role does not compete for issue slots with the warps that drain the accumulators.
-__device__ __forceinline__ bool tc_mbar_try_wait(unsigned bar, unsigned parity) {
-    unsigned ok;
-    const unsigned hint_ns = 20000u;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok) : "r"(bar), "r"(parity), "r"(hint_ns) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ unsigned long long tc_global_ns() {
-    unsigned long long v;
-    asm volatile("mov.u64 %0, %%globaltimer;\n" : "=l"(v));
-    return v;
-}
-// Bounded wait: 2^22 polls or about 0.5 s.
-__device__ __forceinline__ bool tc_mbar_wait(unsigned bar, unsigned parity) {
-    unsigned long long t0 = 0;
-    for (int i = 0; i < (1 << 22); i++) {
-        if (tc_mbar_try_wait(bar, parity)) return true;
-        if ((i & 63) == 63) {
-            const unsigned long long now = tc_global_ns();
-            if (t0 == 0) t0 = now;
-            else if (now - t0 > 500000000ull) return false;
-        }
-    }
-    return false;
-}
-// 2-D tiled TMA load (inner coordinate x in elements, outer coordinate y in rows); every CTA loads for itself.
-__device__ __forceinline__ void tc_tma_load_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
-// D[tmem] (+)= A[smem desc] * B[smem desc]; accumulate = 0 overwrites D.
-__device__ __forceinline__ void tc_mma_f16(unsigned d_tmem, unsigned long long a_desc, unsigned long long b_desc,
-                                           unsigned idesc, unsigned accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
-}
-// mbarrier arrive once every MMA issued so far by this thread has completed.
-__device__ __forceinline__ void tc_commit(unsigned bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
-}
-// 32 consecutive fp32 columns of this thread's TMEM lane.
-__device__ __forceinline__ void tc_ld32(unsigned taddr, unsigned (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tc_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
 
 // ------------------------------------------------------------------ tiles, descriptors
 
@@ -129,13 +58,6 @@ constexpr int BAR_AF = 0, BAR_AE = 2, BAR_BF = 4, BAR_BE = 4 + TC_NB, BAR_CF = 4
               BAR_COUNT = BAR_CE + TC_NACC;
 static_assert((BAR_COUNT + 2) * 8 <= 256, "barrier block");
 
-// Shared-memory matrix descriptor of a K-major panel with 128-byte rows under the 128-byte swizzle:
-// start address / 16, leading offset unused (1), 1024 B between 8-row groups, descriptor version 1,
-// layout type 2 (128-byte swizzle).
-__device__ __forceinline__ unsigned long long tc_panel_desc(unsigned smem_addr) {
-    return (unsigned long long)((smem_addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((unsigned long long)(1024 >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
-}
 // Instruction descriptor of kind::f16: fp32 accumulate, fp16 A and B, both K-major, M = 128, N = 256.
 constexpr unsigned TC_IDESC = (1u << 4) | ((unsigned)(TC_BN >> 3) << 17) | ((unsigned)(TC_BM >> 4) << 24);
 

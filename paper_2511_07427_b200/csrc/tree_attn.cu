@@ -25,13 +25,13 @@
 // a NaN or an infinity, because 0 * NaN would leak them into the tokens that do not see them; tokens that do see them get
 // their share added in fp32 at the end of the segment.
 #include <cuda.h>
-#include <atomic>
 #include <float.h>
 #include <type_traits>
 
 #include "bulk_copy.cuh"
 #include "head_rows.cuh"
 #include "mma_ops.cuh"
+#include "tree_host.cuh"
 #include "tree_plan.cuh"
 
 namespace dkv {
@@ -825,52 +825,18 @@ __global__ void __launch_bounds__(256) k_tree_merge(const TreeArgs a) {
 
 // ---------------------------------------------------------------------------------- host side
 
-typedef CUresult (*tree_encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-// Looked up through the runtime: the library carries no link-time dependency on the driver library.
-static tree_encode_fn tree_encode() {
-    static std::atomic<tree_encode_fn> fn{nullptr};
-    tree_encode_fn f = fn.load(std::memory_order_acquire);
-    if (!f) {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult qr;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qr) == cudaSuccess && qr == cudaDriverEntryPointSuccess)
-            fn.store(f = reinterpret_cast<tree_encode_fn>(p), std::memory_order_release);
-        else
-            cudaGetLastError();
-    }
-    return f;
+template <int HD, int RT>
+static cudaError_t merge_launch(bool f32, const TreeArgs& a, dim3 grid, cudaStream_t st) {
+    return f32 ? launch_pdl(k_tree_merge<HD, RT, float>, grid, dim3(256), 0, st, a) : launch_pdl(k_tree_merge<HD, RT, __nv_bfloat16>, grid, dim3(256), 0, st, a);
 }
-
-// Pool [rows][HD] as [panel][row][128 bytes]: a box is one page, laid out panel by panel.
-static bool tree_page_map(CUtensorMap* map, const dynakv_row_cache* c, void* pool) {
-    const tree_encode_fn enc = tree_encode();
-    if (!enc) return false;
-    const int es = c->kv_dtype == DYNAKV_F32 ? 4 : c->kv_dtype == DYNAKV_BF16 ? 2 : 1;
-    const int row = c->head_dim * es, w = row < 128 ? row : 128;
-    const cuuint64_t dims[3] = {(cuuint64_t)(w / es), (cuuint64_t)(c->n_pages * c->n_kv_heads * PAGE), (cuuint64_t)(row / w)};
-    const cuuint64_t strides[2] = {(cuuint64_t)row, (cuuint64_t)w};
-    const cuuint32_t box[3] = {(cuuint32_t)(w / es), PAGE, (cuuint32_t)(row / w)}, estr[3] = {1, 1, 1};
-    const CUtensorMapDataType dt = es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
-    return enc(map, dt, 3, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               w == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+template <int HD>
+static cudaError_t merge_launch_rows(int rt, bool f32, const TreeArgs& a, dim3 grid, cudaStream_t st) {
+    return rt == 16 ? merge_launch<HD, 16>(f32, a, grid, st) : rt == 32 ? merge_launch<HD, 32>(f32, a, grid, st)
+         : rt == 64 ? merge_launch<HD, 64>(f32, a, grid, st) : merge_launch<HD, 128>(f32, a, grid, st);
 }
-
-static int sm_count(int* rc) {
-    constexpr int MAX_DEV = 64;
-    static std::atomic<int> sms[MAX_DEV];
-    int dev = -1;
-    *rc = DYNAKV_ERR_CUDA;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEV) { cudaGetLastError(); return 0; }
-    int n = sms[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) { cudaGetLastError(); return 0; }
-        sms[dev].store(n, std::memory_order_relaxed);
-    }
-    *rc = DYNAKV_OK;
-    return n;
+int tree_merge_launch(int hd, int rt, bool f32, const TreeArgs& a, int ctas, cudaStream_t st) {
+    const dim3 grid(ctas, rt / 8);
+    return (hd == 128 ? merge_launch_rows<128>(rt, f32, a, grid, st) : merge_launch_rows<64>(rt, f32, a, grid, st)) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
 
 template <int HD, int DT, int RG>
@@ -880,8 +846,7 @@ static int tree_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeA
     if (cudaFuncSetAttribute(k_tree_attn<HD, DT, RG>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem) != cudaSuccess) return DYNAKV_ERR_CUDA;
     k_tree_attn<HD, DT, RG><<<grid, C::threads, C::smem, st>>>(mk, mv, a);
     if (cudaGetLastError() != cudaSuccess) return DYNAKV_ERR_CUDA;
-    using OUT = typename std::conditional<DT == DYNAKV_F32, float, __nv_bfloat16>::type;
-    return launch_pdl(k_tree_merge<HD, C::RT, OUT>, dim3(grid, C::RT / 8), dim3(256), 0, st, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
+    return tree_merge_launch(HD, C::RT, DT == DYNAKV_F32, a, grid, st);
 }
 
 template <int HD, int DT>
@@ -902,6 +867,18 @@ static TreeSpace tree_space(int ctas, int rt, int hd) {
     return s;
 }
 
+// Which kernel, and how many CTAs with how many rows per tile.
+#ifndef DKV_TREE_TC_MIN
+#define DKV_TREE_TC_MIN 33
+#endif
+struct TreeKind { bool tc; int rg, rows, ctas; };
+static TreeKind tree_kind(const dynakv_row_cache* c, int n_heads, int max_tree, int sms) {
+    const int most = max_tree * (n_heads / c->n_kv_heads);
+    if (c->kv_dtype == DYNAKV_BF16 && most >= DKV_TREE_TC_MIN) return {true, 0, TREE_TC_ROWS, sms};
+    const int rg = row_groups(most);
+    return {false, rg, 16 * rg, sms * (c->kv_dtype == DYNAKV_F32 ? 1 : 2)};
+}
+
 static bool tree_shape_ok(const dynakv_row_cache* c, int n_heads, int max_tree) {
     return row_cache_ok(c) && n_heads >= 1 && n_heads % c->n_kv_heads == 0 && n_heads / c->n_kv_heads <= MAX_G && max_tree >= 1 && max_tree <= TREE_MAX;
 }
@@ -915,8 +892,8 @@ extern "C" int64_t dynakv_attend_tree_workspace(const dynakv_row_cache* cache, i
     int rc;
     const int sms = sm_count(&rc);
     if (rc != DYNAKV_OK) return rc;
-    const int rg = row_groups(max_tree * (n_heads / cache->n_kv_heads));
-    return (int64_t)tree_space(sms * (cache->kv_dtype == DYNAKV_F32 ? 1 : 2), 16 * rg, cache->head_dim).bytes;
+    const TreeKind k = tree_kind(cache, n_heads, max_tree, sms);
+    return (int64_t)tree_space(k.ctas, k.rows, cache->head_dim).bytes;
 }
 
 extern "C" int dynakv_attend_tree(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
@@ -931,8 +908,8 @@ extern "C" int dynakv_attend_tree(const dynakv_row_cache* cache, const void* q, 
     int rc;
     const int sms = sm_count(&rc);
     if (rc != DYNAKV_OK) return rc;
-    const int G = n_heads / cache->n_kv_heads, rg = row_groups(max_tree * G), f32 = cache->kv_dtype == DYNAKV_F32;
-    const TreeSpace sp = tree_space(sms * (f32 ? 1 : 2), 16 * rg, cache->head_dim);
+    const TreeKind kind = tree_kind(cache, n_heads, max_tree, sms);
+    const TreeSpace sp = tree_space(kind.ctas, kind.rows, cache->head_dim);
     if (workspace_bytes < (int64_t)sp.bytes) return DYNAKV_ERR_ARG;
     TreeArgs a;
     a.q = q; a.q_start = q_start; a.page_table = page_table; a.kv_len = kv_len;
@@ -947,19 +924,21 @@ extern "C" int dynakv_attend_tree(const dynakv_row_cache* cache, const void* q, 
     a.kexp = reinterpret_cast<const signed char*>(cache->k_exp); a.vexp = reinterpret_cast<const signed char*>(cache->v_exp);
     a.n_tokens = n_tokens; a.n_pages = cache->n_pages;
     a.n_seqs = n_seqs; a.max_tree = max_tree; a.pages_per_seq = pages_per_seq; a.mask_words = tree_mask ? mask_words : 0;
-    a.G = G; a.Hq = n_heads; a.Hk = cache->n_kv_heads;
+    a.G = n_heads / cache->n_kv_heads; a.Hq = n_heads; a.Hk = cache->n_kv_heads;
     a.scale = scale;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     // an error left behind by an earlier, unrelated call on this thread must not be reported as this call's
     cudaGetLastError();
+    if (kind.tc) return tree_tc_launch(cache, a, sms, st);
     CUtensorMap mk, mv;
-    if (!tree_page_map(&mk, cache, cache->k) || !tree_page_map(&mv, cache, cache->v)) return DYNAKV_ERR_CUDA;
+    if (!tree_page_map(&mk, cache, cache->k, true) || !tree_page_map(&mv, cache, cache->v, true)) return DYNAKV_ERR_CUDA;
+    const int rg = kind.rg;
     if (cache->head_dim == 128) {
-        if (f32) return tree_launch_rows<128, DYNAKV_F32>(rg, mk, mv, a, sms, st);
+        if (cache->kv_dtype == DYNAKV_F32) return tree_launch_rows<128, DYNAKV_F32>(rg, mk, mv, a, sms, st);
         if (cache->kv_dtype == DYNAKV_BF16) return tree_launch_rows<128, DYNAKV_BF16>(rg, mk, mv, a, sms, st);
         return tree_launch_rows<128, DYNAKV_FP8>(rg, mk, mv, a, sms, st);
     }
-    if (f32) return tree_launch_rows<64, DYNAKV_F32>(rg, mk, mv, a, sms, st);
+    if (cache->kv_dtype == DYNAKV_F32) return tree_launch_rows<64, DYNAKV_F32>(rg, mk, mv, a, sms, st);
     if (cache->kv_dtype == DYNAKV_BF16) return tree_launch_rows<64, DYNAKV_BF16>(rg, mk, mv, a, sms, st);
     return tree_launch_rows<64, DYNAKV_FP8>(rg, mk, mv, a, sms, st);
 }
