@@ -4,6 +4,9 @@
 
 #include <cuda.h>
 
+#ifndef DKV_HINT
+#define DKV_HINT 0u
+#endif
 namespace dkv {
 
 __device__ __forceinline__ unsigned tc_smem_u32(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
@@ -20,7 +23,7 @@ __device__ __forceinline__ void tc_mbar_expect_tx(unsigned bar, unsigned bytes) 
 // a waiting role does not compete for issue slots with the warps that drain the accumulators.
 __device__ __forceinline__ bool tc_mbar_try_wait(unsigned bar, unsigned parity) {
     unsigned ok;
-    const unsigned hint_ns = 20000u;
+    const unsigned hint_ns = DKV_HINT;
     asm volatile(
         "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
         : "=r"(ok) : "r"(bar), "r"(parity), "r"(hint_ns) : "memory");

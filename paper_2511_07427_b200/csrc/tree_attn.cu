@@ -725,7 +725,6 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 PageIn p;
                 p.k = ring + st * C::stage_bytes; p.v = p.k + C::page_bytes; p.exps = exps + st * 64;
                 p.key0 = pg * PAGE;
-                const bool edge = p.key0 + PAGE > prefix;
                 p.mask = p.key0 + PAGE > prefix;       // holds drafted rows or the end of the sequence
                 // a page that the table does not name was not copied: the stage holds an older one
                 const bool there = !dead && meta[st] != 0;
@@ -832,7 +831,7 @@ static cudaError_t merge_launch(bool f32, const TreeArgs& a, dim3 grid, cudaStre
 template <int HD>
 static cudaError_t merge_launch_rows(int rt, bool f32, const TreeArgs& a, dim3 grid, cudaStream_t st) {
     return rt == 16 ? merge_launch<HD, 16>(f32, a, grid, st) : rt == 32 ? merge_launch<HD, 32>(f32, a, grid, st)
-         : rt == 64 ? merge_launch<HD, 64>(f32, a, grid, st) : merge_launch<HD, 128>(f32, a, grid, st);
+         : rt == 64 ? merge_launch<HD, 64>(f32, a, grid, st) : rt == 128 ? merge_launch<HD, 128>(f32, a, grid, st) : merge_launch<HD, 256>(f32, a, grid, st);
 }
 int tree_merge_launch(int hd, int rt, bool f32, const TreeArgs& a, int ctas, cudaStream_t st) {
     const dim3 grid(ctas, rt / 8);
@@ -874,7 +873,7 @@ static TreeSpace tree_space(int ctas, int rt, int hd) {
 struct TreeKind { bool tc; int rg, rows, ctas; };
 static TreeKind tree_kind(const dynakv_row_cache* c, int n_heads, int max_tree, int sms) {
     const int most = max_tree * (n_heads / c->n_kv_heads);
-    if (c->kv_dtype == DYNAKV_BF16 && most >= DKV_TREE_TC_MIN) return {true, 0, TREE_TC_ROWS, sms};
+    if (c->kv_dtype == DYNAKV_BF16 && most >= DKV_TREE_TC_MIN) return {true, 0, most <= 128 ? 128 : 256, sms};
     const int rg = row_groups(most);
     return {false, rg, 16 * rg, sms * (c->kv_dtype == DYNAKV_F32 ? 1 : 2)};
 }
@@ -929,7 +928,7 @@ extern "C" int dynakv_attend_tree(const dynakv_row_cache* cache, const void* q, 
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     // an error left behind by an earlier, unrelated call on this thread must not be reported as this call's
     cudaGetLastError();
-    if (kind.tc) return tree_tc_launch(cache, a, sms, st);
+    if (kind.tc) return tree_tc_launch(cache, kind.rows, a, sms, st);
     CUtensorMap mk, mv;
     if (!tree_page_map(&mk, cache, cache->k, true) || !tree_page_map(&mv, cache, cache->v, true)) return DYNAKV_ERR_CUDA;
     const int rg = kind.rg;

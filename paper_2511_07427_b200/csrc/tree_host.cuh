@@ -59,9 +59,8 @@ static int sm_count(int* rc) {
     return n;
 }
 
-// tcgen05 kernel (tree_tc.cu): bf16 rows, tiles of TREE_TC_ROWS query rows, one CTA per SM.
-constexpr int TREE_TC_ROWS = 128;
-int tree_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, int sms, cudaStream_t st);
+// tcgen05 kernel (tree_tc.cu): bf16 rows, tiles of 128 or 256 query rows, one CTA per SM.
+int tree_tc_launch(const dynakv_row_cache* cache, int rows, const TreeArgs& a, int sms, cudaStream_t st);
 // Merge of cut units (tree_attn.cu).
 int tree_merge_launch(int hd, int rt, bool f32, const TreeArgs& a, int ctas, cudaStream_t st);
 
