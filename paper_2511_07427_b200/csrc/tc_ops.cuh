@@ -4,9 +4,6 @@
 
 #include <cuda.h>
 
-#ifndef DKV_HINT
-#define DKV_HINT 0u
-#endif
 namespace dkv {
 
 __device__ __forceinline__ unsigned tc_smem_u32(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
@@ -23,7 +20,7 @@ __device__ __forceinline__ void tc_mbar_expect_tx(unsigned bar, unsigned bytes) 
 // a waiting role does not compete for issue slots with the warps that drain the accumulators.
 __device__ __forceinline__ bool tc_mbar_try_wait(unsigned bar, unsigned parity) {
     unsigned ok;
-    const unsigned hint_ns = DKV_HINT;
+    const unsigned hint_ns = 20000u;
     asm volatile(
         "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
         : "=r"(ok) : "r"(bar), "r"(parity), "r"(hint_ns) : "memory");
@@ -94,6 +91,10 @@ __device__ __forceinline__ void tc_st32(unsigned taddr, const unsigned (&r)[32])
           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
           "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
           "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tc_st8(unsigned taddr, const unsigned (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};\n"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 

@@ -78,7 +78,7 @@ struct TreeCfg {
     static constexpr int p_bytes = DT == DYNAKV_F32 ? consumers * 16 * 32 * 4 : 0;
     static constexpr int dump_bytes = 16 * HD * 4 + 128;                     // one warp's sums, then (m, l) of its 16 rows
     static constexpr int merge_bytes = KG > 1 ? RG * dump_bytes : 0;
-    static constexpr int fixed_bytes = 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + 36 * 8;
+    static constexpr int fixed_bytes = 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + 48 * 8;
     static constexpr int smem = stages * stage_bytes + exp_bytes + q_bytes + p_bytes + merge_bytes + fixed_bytes;
     static_assert(stages % KG == 0, "each ring stage belongs to one page group");
     static_assert(per_sm * (smem + 1024) <= 233472, "shared memory of an SM");
@@ -617,7 +617,7 @@ __device__ __forceinline__ void mend_page(unsigned v, const Segment& g, int key0
 
 template <int HD, int DT, int RG>
 __global__ void __launch_bounds__((TreeCfg<HD, DT, RG>::threads), (TreeCfg<HD, DT, RG>::per_sm))
-k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const TreeArgs a) {
+k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeArgs a) {
     using C = TreeCfg<HD, DT, RG>;
     constexpr int S = C::stages, KG = C::KG;
     extern __shared__ __align__(1024) unsigned char tree_smem[];
@@ -626,7 +626,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     float* q_s = reinterpret_cast<float*>(at); at += C::q_bytes;
     float* p_s = reinterpret_cast<float*>(at); at += C::p_bytes;
     float* dump = reinterpret_cast<float*>(at); at += C::merge_bytes;
-    long long* sh = reinterpret_cast<long long*>(at); at += 36 * 8;
+    long long* sh = reinterpret_cast<long long*>(at); at += 48 * 8;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(at); at += 2 * S * 8;
     int* s_abort = reinterpret_cast<int*>(at); at += 16;
     unsigned* odd = reinterpret_cast<unsigned*>(at); at += 3 * 8 * 4;
@@ -642,9 +642,11 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     if (tid < 24) odd[tid] = 0u;
-    const Range range = tree_range<C::RT>(a, KG, sh);      // holds block barriers
+    pdl_wait();                                            // from here on the results of earlier kernels are read
+    const Range range = tree_range<C::RT>(a, KG, sh);
+    __syncthreads();
     pdl_trigger();
-    SegmentWalk<C::RT> walk(a, range);
+    SegmentWalk<C::RT> walk(range, sh);
     Segment g;
 
     if (warp == C::consumers) {
@@ -703,7 +705,6 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         if constexpr (F32) { rows.q_s = smem_u32(q_s + rg * 16 * HD); rows.p_s = smem_u32(p_s + warp * 16 * 32); }
         int it = 0, seg = 0;
         bool dead = false, cut_end = false;
-        Segment cut;
         while (walk.next(a, g)) {
             const int prefix = g.n - g.T;
             unsigned* odd_now = odd + (seg % 3) * 8;
@@ -762,13 +763,10 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 }
                 rows.write(a, g, rg, lane, g.first && g.last, (size_t)blockIdx.x * 2 + (g.first ? 1 : 0));
             }
-            if (g.last && !g.first) { cut = g; cut_end = true; }
+            if (g.last && !g.first) { cut_end = true; if (tid == 0) describe_cut_unit(a, g, walk.r); }
             seg++;
         }
-        if (tid == 0) {
-            if (cut_end) describe_cut_unit(a, cut, range);
-            a.desc[(size_t)blockIdx.x * 8 + DESC_VALID] = cut_end ? 1 : 0;
-        }
+        if (tid == 0) a.desc[(size_t)blockIdx.x * 8 + DESC_VALID] = cut_end ? 1 : 0;
     }
 }
 
@@ -822,6 +820,43 @@ __global__ void __launch_bounds__(256) k_tree_merge(const TreeArgs a) {
     if (a.lse && lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
 }
 
+// The same for the tcgen05 kernel's records, four columns of all rows side by side: a thread per row and 16 columns,
+// block (x = CTA, y = 16 columns), so that the lanes' loads join.
+template <int HD, int RT>
+__global__ void __launch_bounds__(RT) k_tree_merge_cols(const TreeArgs a) {
+    pdl_wait();
+    const int* d = a.desc + (size_t)blockIdx.x * 8;
+    if (!d[DESC_VALID]) return;
+    const int rl = threadIdx.x, r = d[DESC_RT] * RT + rl, t = r / a.G, c0 = d[DESC_FIRST], n = blockIdx.x - c0 + 1;
+    if (t >= d[DESC_T]) return;
+    auto slot = [&](int i) { return (size_t)(c0 + i) * 2 + (i == 0 ? 1 : 0); };
+    const float4* acc = reinterpret_cast<const float4*>(a.acc) + (size_t)blockIdx.y * 4 * RT + rl;
+    float m = -INFINITY, l = 0.f;
+    float4 o[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = 0; i < n; i++) {
+        const float2 x = a.ml[slot(i) * RT + rl];
+        float4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = acc[(slot(i) * (HD / 4) + e) * RT];
+        const float to = fmaxf(m, x.x), ref = to == -INFINITY ? 0.f : to, f0 = exp2f(m - ref), f1 = exp2f(x.x - ref);
+        m = to;
+        l = l * f0 + x.y * f1;
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            o[e] = make_float4(o[e].x * f0 + v[e].x * f1, o[e].y * f0 + v[e].y * f1, o[e].z * f0 + v[e].z * f1, o[e].w * f0 + v[e].w * f1);
+    }
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    const size_t at = (size_t)(d[DESC_Q0] + t) * a.Hq + d[DESC_H] * a.G + r - t * a.G;
+    uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at * HD + blockIdx.y * 16);
+#pragma unroll
+    for (int e = 0; e < 4; e += 2)
+        out[e / 2] = make_uint4(pack_bf16(o[e].x * f, o[e].y * f), pack_bf16(o[e].z * f, o[e].w * f), pack_bf16(o[e + 1].x * f, o[e + 1].y * f), pack_bf16(o[e + 1].z * f, o[e + 1].w * f));
+    if (a.lse && blockIdx.y == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+}
+
 // ---------------------------------------------------------------------------------- host side
 
 template <int HD, int RT>
@@ -830,8 +865,11 @@ static cudaError_t merge_launch(bool f32, const TreeArgs& a, dim3 grid, cudaStre
 }
 template <int HD>
 static cudaError_t merge_launch_rows(int rt, bool f32, const TreeArgs& a, dim3 grid, cudaStream_t st) {
-    return rt == 16 ? merge_launch<HD, 16>(f32, a, grid, st) : rt == 32 ? merge_launch<HD, 32>(f32, a, grid, st)
-         : rt == 64 ? merge_launch<HD, 64>(f32, a, grid, st) : rt == 128 ? merge_launch<HD, 128>(f32, a, grid, st) : merge_launch<HD, 256>(f32, a, grid, st);
+    if (rt >= 128) {           // the tcgen05 kernel's tiles
+        const dim3 cols(grid.x, HD / 16);
+        return rt == 128 ? launch_pdl(k_tree_merge_cols<HD, 128>, cols, dim3(128), 0, st, a) : launch_pdl(k_tree_merge_cols<HD, 256>, cols, dim3(256), 0, st, a);
+    }
+    return rt == 16 ? merge_launch<HD, 16>(f32, a, grid, st) : rt == 32 ? merge_launch<HD, 32>(f32, a, grid, st) : merge_launch<HD, 64>(f32, a, grid, st);
 }
 int tree_merge_launch(int hd, int rt, bool f32, const TreeArgs& a, int ctas, cudaStream_t st) {
     const dim3 grid(ctas, rt / 8);
@@ -843,8 +881,7 @@ static int tree_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeA
     using C = TreeCfg<HD, DT, RG>;
     const int grid = sms * C::per_sm;
     if (cudaFuncSetAttribute(k_tree_attn<HD, DT, RG>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem) != cudaSuccess) return DYNAKV_ERR_CUDA;
-    k_tree_attn<HD, DT, RG><<<grid, C::threads, C::smem, st>>>(mk, mv, a);
-    if (cudaGetLastError() != cudaSuccess) return DYNAKV_ERR_CUDA;
+    if (launch_pdl(k_tree_attn<HD, DT, RG>, dim3(grid), dim3(C::threads), C::smem, st, mk, mv, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
     return tree_merge_launch(HD, C::RT, DT == DYNAKV_F32, a, grid, st);
 }
 

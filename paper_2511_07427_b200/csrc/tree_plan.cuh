@@ -24,7 +24,7 @@ struct TreeArgs {
     const unsigned long long* mask;        // [n_tokens][mask_words], NULL: a chain
     void* out;                             // [n_tokens][Hq][d]
     float* lse;                            // [n_tokens][Hq], may be NULL
-    float* acc;                            // records: [CTA][2][RT][d]
+    float* acc;                            // records: [CTA][2][RT][d], from the tcgen05 kernel [CTA][2][d / 4][RT][4]
     float2* ml;                            //          [CTA][2][RT] (m, l)
     int* desc;                             // [CTA][8] the cut unit that ends in the CTA
     unsigned* status;
@@ -47,8 +47,16 @@ struct SeqInfo {
     long long work;                        // pages of all the sequence's units
 };
 template <int RT>
-__device__ __forceinline__ SeqInfo seq_info(const TreeArgs& a, int b, bool report) {
+__device__ __forceinline__ SeqInfo seq_work(const TreeArgs& a, int q0, int T, int n) {
     SeqInfo s;
+    s.q0 = q0; s.T = T; s.n = n;
+    s.pages = max(1, (n + PAGE - 1) / PAGE);
+    s.tiles = (T * a.G + RT - 1) / RT;
+    s.work = (long long)s.pages * s.tiles * a.Hk;
+    return s;
+}
+template <int RT>
+__device__ __forceinline__ SeqInfo seq_info(const TreeArgs& a, int b, bool report) {
     const int q0 = a.q_start[b], q1 = a.q_start[b + 1], n = a.kv_len[b];
     long long T = (long long)q1 - q0;
     const long long rows = (long long)a.pages_per_seq * PAGE;
@@ -58,12 +66,7 @@ __device__ __forceinline__ SeqInfo seq_info(const TreeArgs& a, int b, bool repor
         T = max(0ll, min(T, min((long long)a.max_tree, a.n_tokens - q0)));
     }
     if (report && (bad_q || bad_n)) tree_status(a, DYNAKV_ST_BOUNDS);
-    s.q0 = q0; s.T = (int)T;
-    s.n = (int)max(0ll, min((long long)n, rows));
-    s.pages = max(1, (s.n + PAGE - 1) / PAGE);
-    s.tiles = (s.T * a.G + RT - 1) / RT;
-    s.work = (long long)s.pages * s.tiles * a.Hk;
-    return s;
+    return seq_work<RT>(a, q0, (int)T, (int)max(0ll, min((long long)n, rows)));
 }
 
 struct Segment {
@@ -79,14 +82,47 @@ struct Range {
     int b, C;
 };
 
-// Block-wide: every thread of the block (a multiple of 32, at most 1024) calls it.  sh: 36 long longs.
+// a * b / c for non-negative values, in 32 bits when they fit: the 64-bit division costs some hundred cycles.
+__device__ __forceinline__ long long mul_div(long long a, long long b, long long c) {
+    const long long p = a * b;
+    return p < (1ll << 32) && c < (1ll << 32) ? (long long)((unsigned)p / (unsigned)c) : p / c;
+}
+
+// Which range of the list the CTA has.  Every thread of the block (a multiple of 32, at most 1024) calls it; sh: 48 long longs.
+// Up to 32 sequences: a lane takes one each, which needs one trip to memory and no block barrier, and what the walk will
+// look up is left in sh (the caller synchronises the block); more: the block scans them, and the walk loads them again.
 template <int RT>
 __device__ __forceinline__ Range tree_range(const TreeArgs& a, int min_pages, long long* sh) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, nw = nt >> 5;
-    auto scan = [&](long long v, long long& total) {       // inclusive
-        long long x = v;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, nw = nt >> 5, c = blockIdx.x;
+    auto warp_scan = [&](long long x) {                    // inclusive
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+        return x;
+    };
+    Range r;
+    r.W = 0;
+    auto share = [&]() {
+        r.C = (int)max(1ll, min((long long)gridDim.x, r.W / min_pages));
+        r.x = c < r.C ? mul_div(c, r.W, r.C) : r.W;
+        r.end = c < r.C ? mul_div(c + 1, r.W, r.C) : r.W;
+    };
+    if (a.n_seqs <= 32) {
+        SeqInfo mine;
+        mine.work = 0;
+        if (lane < a.n_seqs) {
+            mine = seq_info<RT>(a, lane, c == 0 && warp == 0);
+            if (warp == 0) { int* to = reinterpret_cast<int*>(sh); to[lane] = mine.q0; to[32 + lane] = mine.T; to[64 + lane] = mine.n; }
+        }
+        const long long incl = warp_scan(mine.work);
+        r.W = __shfl_sync(0xffffffffu, incl, 31);
+        share();
+        const unsigned has = __ballot_sync(0xffffffffu, incl - mine.work <= r.x && r.x < incl);
+        r.b = has ? __ffs(has) - 1 : 0;
+        r.base = __shfl_sync(0xffffffffu, incl - mine.work, r.b);
+        return r;
+    }
+    auto scan = [&](long long v, long long& total) {       // inclusive, over the block
+        const long long x = warp_scan(v);
         __syncthreads();
         if (lane == 31) sh[warp] = x;
         __syncthreads();
@@ -95,20 +131,15 @@ __device__ __forceinline__ Range tree_range(const TreeArgs& a, int min_pages, lo
         for (int w = 0; w < nw; w++) { if (w < warp) before += sh[w]; total += sh[w]; }
         return x + before;
     };
-    Range r;
-    r.W = 0;
     const bool one = a.n_seqs <= nt;
     long long v = 0, incl = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += nt) {
-        v = b0 + tid < a.n_seqs ? seq_info<RT>(a, b0 + tid, blockIdx.x == 0).work : 0;
+        v = b0 + tid < a.n_seqs ? seq_info<RT>(a, b0 + tid, c == 0).work : 0;
         long long total;
         incl = scan(v, total);
         r.W += total;
     }
-    r.C = (int)max(1ll, min((long long)gridDim.x, r.W / min_pages));
-    const int c = blockIdx.x;
-    r.x = c < r.C ? c * r.W / r.C : r.W;
-    r.end = c < r.C ? (c + 1) * r.W / r.C : r.W;
+    share();
     if (tid == 0) { sh[34] = 0; sh[35] = 0; }
     __syncthreads();
     if (r.x < r.end) {                     // uniform in the block
@@ -130,21 +161,26 @@ __device__ __forceinline__ Range tree_range(const TreeArgs& a, int min_pages, lo
     return r;
 }
 
+// The CTA's segments in order.
 template <int RT>
 struct SegmentWalk {
     Range r;
-    SeqInfo s;
-    __device__ __forceinline__ SegmentWalk(const TreeArgs& a, const Range& range) : r(range) {
-        if (r.x < r.end) s = seq_info<RT>(a, r.b, false);
+    const long long* sh;
+    __device__ __forceinline__ SegmentWalk(const Range& range, const long long* shared) : r(range), sh(shared) {}
+    __device__ __forceinline__ SeqInfo look(const TreeArgs& a) const {
+        if (a.n_seqs > 32) return seq_info<RT>(a, r.b, false);
+        const int* from = reinterpret_cast<const int*>(sh);
+        return seq_work<RT>(a, from[r.b], from[32 + r.b], from[64 + r.b]);
     }
     __device__ __forceinline__ bool next(const TreeArgs& a, Segment& g) {
         if (r.x >= r.end) return false;
-        while (r.x - r.base >= s.work) { r.base += s.work; r.b++; s = seq_info<RT>(a, r.b, false); }
+        SeqInfo s = look(a);
+        while (r.x - r.base >= s.work) { r.base += s.work; r.b++; s = look(a); }
         const long long off = r.x - r.base;
         const long long unit = off < (1ll << 31) ? (long long)((unsigned)off / (unsigned)s.pages) : off / s.pages;
         g.p0 = (int)(off - unit * s.pages);
         g.p1 = (int)min((long long)s.pages, g.p0 + (r.end - r.x));
-        g.b = r.b; g.h = (int)(unit / s.tiles); g.tile = (int)(unit - (long long)g.h * s.tiles);
+        g.b = r.b; g.h = (int)((unsigned)unit / (unsigned)s.tiles); g.tile = (int)(unit - (long long)g.h * s.tiles);     // heads times tiles fit 32 bits
         g.q0 = s.q0; g.T = s.T; g.n = s.n;
         g.first = g.p0 == 0; g.last = g.p1 == s.pages;
         g.unit_start = r.base + unit * s.pages;
@@ -152,6 +188,12 @@ struct SegmentWalk {
         return true;
     }
 };
+
+// next() as a call of its own: the walk's state stays in (local) memory between segments instead of in registers of the loops
+// over pages.  Measured both ways: the tcgen05 kernel, whose softmax fills its 168 registers, gains (113 -> 111 us and 121 -> 118 us on
+// trees of 16 and of 64), the mma.sync kernel loses (90 -> 95 us on one token over 4 x 32768 rows).
+template <int RT>
+__device__ __noinline__ bool next_segment(SegmentWalk<RT>& walk, const TreeArgs& a, Segment& g) { return walk.next(a, g); }
 
 // The CTA whose range holds flat index x.
 __device__ __forceinline__ int range_owner(long long x, long long W, int C) { return (int)(((x + 1) * C - 1) / W); }

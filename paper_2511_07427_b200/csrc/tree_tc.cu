@@ -24,6 +24,7 @@
 #include <cuda.h>
 #include <float.h>
 
+#include "bulk_copy.cuh"
 #include "head_rows.cuh"
 #include "mma_ops.cuh"
 #include "tc_ops.cuh"
@@ -44,7 +45,7 @@ struct TcTree {
     static constexpr int tile_bytes = panels * panel_bytes;
     static constexpr int q_tiles = PAIR ? 2 : 1;
     static constexpr int stages = PAIR ? 2 : 3;                // of K and V each: with Q 192 KB or 224 KB at d = 128
-    static constexpr int fixed = 2 * 128 * 8 + 36 * 8 + 32 * 8 + 2 * 8 * 4 + 8 * 4 + 16;
+    static constexpr int fixed = 2 * 128 * 8 + 48 * 8 + 32 * 8 + 2 * 8 * 4 + 8 * 4 + 16;
     static constexpr int smem = (q_tiles + 2 * stages) * tile_bytes + fixed;
     static_assert(smem + 1024 <= 233472, "shared memory of an SM");
     // kind::f16, fp32 accumulate, bf16 operands, M = 128
@@ -68,19 +69,25 @@ __device__ __forceinline__ float tt_max3(float a, float b, float c) {
 __device__ __forceinline__ void sts16(unsigned addr, uint4 v) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+// True in one lane of a converged warp, the same one every time.
+__device__ __forceinline__ bool elect_one() {
+    unsigned r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void tt_proxy_fence() { asm volatile("fence.proxy.async;\n" ::: "memory"); }
 // Pages of half h of stage j of a segment of `pages` pages.
 __device__ __forceinline__ int half_pages(int pages, int j, int h) { return max(0, min(TT_HALF, pages - j * TT_PAGES - h * TT_HALF)); }
 
 template <int HD, bool PAIR>
 __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                                                           const TreeArgs a) {
+                                                           const __grid_constant__ TreeArgs a) {
     using C = TcTree<HD, PAIR>;
     constexpr int NS = C::stages;
     extern __shared__ __align__(1024) unsigned char tt_smem[];
     unsigned char* at = tt_smem + (C::q_tiles + 2 * NS) * C::tile_bytes;
     float2* ml_s = reinterpret_cast<float2*>(at); at += 2 * 128 * 8;               // [stream][row] (m, l)
-    long long* sh = reinterpret_cast<long long*>(at); at += 36 * 8;
+    long long* sh = reinterpret_cast<long long*>(at); at += 48 * 8;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(at); at += 32 * 8;
     unsigned* odd = reinterpret_cast<unsigned*>(at); at += 2 * 8 * 4;              // [segment parity][8]
     volatile int* meta = reinterpret_cast<volatile int*>(at); at += 8 * 4;         // [stage number mod 8] bit per page: it was loaded
@@ -107,11 +114,13 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
     tc_fence_before();
-    const Range range = tree_range<C::rows>(a, TT_PAGES, sh);                      // holds block barriers
+    pdl_wait();                                                // from here on the results of earlier kernels are read
+    const Range range = tree_range<C::rows>(a, TT_PAGES, sh);
+    __syncthreads();
     tc_fence_after();
     pdl_trigger();
     const unsigned tmem = *s_tmem;
-    SegmentWalk<C::rows> walk(a, range);
+    SegmentWalk<C::rows> walk(range, sh);
     Segment g;
     auto give_up = [&]() { *s_abort = 1; };
 
@@ -122,7 +131,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
         const int full = is_v ? C::VFULL : C::KFULL, empty = is_v ? C::VEMPTY : C::KEMPTY;
         int n = 0;                                             // stage number in the CTA
         bool ok = true;
-        while (ok && walk.next(a, g)) {
+        while (ok && next_segment(walk, a, g)) {
             for (int pc = g.p0; ok && pc < g.p1; pc += 32) {
                 const int cnt = min(32, g.p1 - pc);
                 int id = -1;
@@ -138,7 +147,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
                     for (int x = 0; x < TT_PAGES; x++) page[x] = __shfl_sync(0xffffffffu, id, j + x);      // -1 past the segment's end
                     const int bits = (there >> j) & 15;
                     if (lane == 0) {
-                        ok = !*s_abort && (use == 0 || tc_mbar_wait(bar(empty + st), (unsigned)(use - 1) & 1u));
+                        ok = !*s_abort && (use == 0 || mbar_wait(bar(empty + st), (unsigned)(use - 1) & 1u));
                         if (ok) {
                             if (!is_v) meta[n & 7] = bits;
                             if (bits) tc_mbar_expect_tx(bar(full + st), __popc(bits) * PAGE * HD * 2);
@@ -160,33 +169,35 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
         if (!ok && lane == 0) {
             give_up();
             // stage n - 1 was not issued; let the copies of the ones before it land before the block ends
-            for (int x = max(0, n - 1 - NS); x < n - 1; x++) tc_mbar_wait(bar(full + x % NS), (unsigned)(x / NS) & 1u);
+            for (int x = max(0, n - 1 - NS); x < n - 1; x++) mbar_wait(bar(full + x % NS), (unsigned)(x / NS) & 1u);
         }
     } else if (warp == 1 || warp == 2) {
         // =============================== MMAs of one stream ===============================
+        // The whole warp walks and waits, one elected lane issues: addresses and descriptors then stay in uniform registers, where
+        // the instructions want them.
         const int s = warp - 1;
-        if (lane == 0) {
-            int n = 0, u = 0, segs = 0;                        // stages so far, halves so far, segments in which the stream had a half
-            bool ok = true;
-            // operand descriptors of the first step; the address field counts 16 bytes
-            const unsigned long long dq = tc_panel_desc(sQ + (PAIR ? s * C::tile_bytes : 0)), dk = tc_panel_desc(sK(0)), dv = tc_rows_desc(sV(0), C::panel_bytes);
-            const unsigned tO = tmem + 256 + s * 128;
-            auto wait = [&](int b, int phase) { ok = ok && !*s_abort && tc_mbar_wait(bar(b), (unsigned)phase & 1u); };
-            while (ok && walk.next(a, g)) {
-                const int pages = g.p1 - g.p0, stages = (pages + TT_PAGES - 1) / TT_PAGES;
-                const int halves = PAIR ? (pages + TT_HALF - 1) / TT_HALF : stages - (s == 1 && half_pages(pages, stages - 1, 1) == 0 ? 1 : 0);
-                const int u0 = u;
-                // logits of half i of the segment
-                auto logits = [&](int i) {
-                    const int j = PAIR ? i >> 1 : i, h = PAIR ? i & 1 : s, st = (n + j) % NS, use = (n + j) / NS, v = u0 + i;
-                    if (i == 0) wait(C::QFULL + s, segs);
-                    if (!PAIR || h == 0) wait(C::KFULL + st, use);
-                    if (v >= 2) wait(C::ODONE + 2 * s + (v & 1), (v >> 1) - 1);        // the buffer's last weights have been used
-                    if (!ok) return;
-                    tc_fence_after();
-                    const unsigned idesc = C::idesc | ((unsigned)(half_pages(pages, j, h) * PAGE >> 3) << 17);
-                    const unsigned long long k0 = dk + ((st * C::tile_bytes + h * TT_HALF * PAGE * 128) >> 4);
-                    const unsigned tS = tmem + s * 128 + (v & 1) * 64;
+        int n = 0, u = 0, segs = 0;                            // stages so far, halves so far, segments in which the stream had a half
+        bool ok = true;
+        // operand descriptors of the first step; the address field counts 16 bytes
+        const unsigned long long dq = tc_panel_desc(sQ + (PAIR ? s * C::tile_bytes : 0)), dk = tc_panel_desc(sK(0)), dv = tc_rows_desc(sV(0), C::panel_bytes);
+        const unsigned tO = tmem + 256 + s * 128;
+        auto wait = [&](int b, int phase) { ok = ok && mbar_wait(bar(b), (unsigned)phase & 1u); ok = __all_sync(0xffffffffu, ok); };
+        while (ok && next_segment(walk, a, g)) {
+            const int pages = g.p1 - g.p0, stages = (pages + TT_PAGES - 1) / TT_PAGES;
+            const int halves = PAIR ? (pages + TT_HALF - 1) / TT_HALF : stages - (s == 1 && half_pages(pages, stages - 1, 1) == 0 ? 1 : 0);
+            const int u0 = u;
+            // logits of half i of the segment
+            auto logits = [&](int i) {
+                const int j = PAIR ? i >> 1 : i, h = PAIR ? i & 1 : s, st = (n + j) % NS, use = (n + j) / NS, v = u0 + i;
+                if (i == 0) wait(C::QFULL + s, segs);
+                if (!PAIR || h == 0) wait(C::KFULL + st, use);
+                if (v >= 2) wait(C::ODONE + 2 * s + (v & 1), (v >> 1) - 1);            // the buffer's last weights have been used
+                if (!ok) return;
+                tc_fence_after();
+                const unsigned idesc = C::idesc | ((unsigned)(half_pages(pages, j, h) * PAGE >> 3) << 17);
+                const unsigned long long k0 = dk + ((st * C::tile_bytes + h * TT_HALF * PAGE * 128) >> 4);
+                const unsigned tS = tmem + s * 128 + (v & 1) * 64;
+                if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < HD / 16; k++) {
                         const unsigned off = ((k >> 2) * C::panel_bytes + (k & 3) * 32) >> 4;
@@ -194,18 +205,21 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
                     }
                     tc_commit(bar(C::SFULL + 2 * s + (v & 1)));
                     if (!PAIR || h == 1 || i == halves - 1) tc_commit(bar(C::KEMPTY + st));
-                };
-                if (halves > 0) logits(0);
-                for (int i = 0; i < halves && ok; i++, u++) {
-                    if (i + 1 < halves) logits(i + 1);
-                    const int j = PAIR ? i >> 1 : i, h = PAIR ? i & 1 : s, st = (n + j) % NS, use = (n + j) / NS;
-                    if (!PAIR || h == 0) wait(C::VFULL + st, use);
-                    wait(C::PFULL + 2 * s + (u & 1), u >> 1);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const unsigned tP = tmem + s * 128 + (u & 1) * 64;
-                    const unsigned long long v0 = dv + ((st * C::tile_bytes + h * TT_HALF * PAGE * 128) >> 4);
-                    const int steps = half_pages(pages, j, h) * 2;
+                }
+                __syncwarp();
+            };
+            if (halves > 0) logits(0);
+            for (int i = 0; i < halves && ok; i++, u++) {
+                if (i + 1 < halves) logits(i + 1);
+                const int j = PAIR ? i >> 1 : i, h = PAIR ? i & 1 : s, st = (n + j) % NS, use = (n + j) / NS;
+                if (!PAIR || h == 0) wait(C::VFULL + st, use);
+                wait(C::PFULL + 2 * s + (u & 1), u >> 1);
+                if (!ok) break;
+                tc_fence_after();
+                const unsigned tP = tmem + s * 128 + (u & 1) * 64;
+                const unsigned long long v0 = dv + ((st * C::tile_bytes + h * TT_HALF * PAGE * 128) >> 4);
+                const int steps = half_pages(pages, j, h) * 2;
+                if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < TT_HALF * 2; k++) {
                         if (k >= steps) break;
@@ -216,20 +230,24 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
                     tc_commit(bar(C::ODONE + 2 * s + (u & 1)));
                     if (!PAIR || h == 1 || i == halves - 1) tc_commit(bar(C::VEMPTY + st));
                 }
-                if (!PAIR && halves < stages && ok) {          // the last stage has no half for this stream: give it back
-                    const int st = (n + stages - 1) % NS, use = (n + stages - 1) / NS;
-                    wait(C::KFULL + st, use);
-                    wait(C::VFULL + st, use);
-                    if (ok) { tc_mbar_arrive(bar(C::KEMPTY + st)); tc_mbar_arrive(bar(C::VEMPTY + st)); }
-                }
-                if (halves > 0) segs++;
-                n += stages;
+                __syncwarp();
             }
-            if (!ok) {
+            if (!PAIR && halves < stages && ok) {              // the last stage has no half for this stream: give it back
+                const int st = (n + stages - 1) % NS, use = (n + stages - 1) / NS;
+                wait(C::KFULL + st, use);
+                wait(C::VFULL + st, use);
+                if (ok && lane == 0) { tc_mbar_arrive(bar(C::KEMPTY + st)); tc_mbar_arrive(bar(C::VEMPTY + st)); }
+            }
+            if (halves > 0) segs++;
+            n += stages;
+        }
+        if (!ok) {
+            if (elect_one()) {
                 give_up();
                 tc_commit(bar(C::DRAIN + s));                  // whatever was issued ends before the tensor memory is freed
-                tc_mbar_wait(bar(C::DRAIN + s), 0u);
             }
+            __syncwarp();
+            mbar_wait(bar(C::DRAIN + s), 0u);
         }
     } else {
         // =============================== softmax of one stream ===============================
@@ -241,12 +259,11 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
         auto both_sync = [&]() { asm volatile("bar.sync 3, 256;\n" ::: "memory"); };
         int n = 0, u = 0, seg = 0;
         bool dead = false, cut_end = false;
-        Segment cut;
         auto wait = [&](int b, int phase) {
-            if (!dead && (*s_abort || !tc_mbar_wait(bar(b), (unsigned)phase & 1u))) { dead = true; give_up(); }
+            if (!dead && !mbar_wait(bar(b), (unsigned)phase & 1u)) { dead = true; give_up(); }
             dead = __any_sync(0xffffffffu, dead);
         };
-        while (walk.next(a, g)) {
+        while (next_segment(walk, a, g)) {
             const int pages = g.p1 - g.p0, stages = (pages + TT_PAGES - 1) / TT_PAGES, prefix = g.n - g.T;
             const int halves = PAIR ? (pages + TT_HALF - 1) / TT_HALF : stages - (s == 1 && half_pages(pages, stages - 1, 1) == 0 ? 1 : 0);
             unsigned* odd_now = odd + (seg & 1) * 8;
@@ -258,12 +275,14 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
                 const int c0 = PAIR ? 0 : s * CH;
                 const unsigned to = sQ + (PAIR ? s * C::tile_bytes : 0) + row * 128;
                 const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + q_row * HD) + c0;
+                uint4 v[CH];                                   // all loads before the first store
+#pragma unroll
+                for (int c = 0; c < CH; c++) v[c] = t >= 0 && a.scale != 0.f ? src[c] : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
                 for (int c = 0; c < CH; c++) {
-                    uint4 v = t >= 0 && a.scale != 0.f ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-                    if (flip) { v.x ^= 0x80008000u; v.y ^= 0x80008000u; v.z ^= 0x80008000u; v.w ^= 0x80008000u; }
+                    if (flip) { v[c].x ^= 0x80008000u; v[c].y ^= 0x80008000u; v[c].z ^= 0x80008000u; v[c].w ^= 0x80008000u; }
                     const int ch = c0 + c;
-                    sts16(to + (ch >> 3) * C::panel_bytes + (((ch & 7) ^ (row & 7)) << 4), v);
+                    sts16(to + (ch >> 3) * C::panel_bytes + (((ch & 7) ^ (row & 7)) << 4), v[c]);
                 }
                 tt_proxy_fence();
                 __syncwarp();
@@ -397,7 +416,7 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
             const float top = fmaxf(o0.x, o1.x), ref = top == -INFINITY ? 0.f : top;
             const float f0 = ex2(o0.x - ref), f1 = ex2(o1.x - ref), lt = o0.y * f0 + o1.y * f1;
             const bool whole = g.first && g.last;
-            const size_t slot = ((size_t)blockIdx.x * 2 + (g.first ? 1 : 0)) * C::rows + rl;
+            const size_t slot = (size_t)blockIdx.x * 2 + (g.first ? 1 : 0);
             if (!dead && !idle) {
                 const float norm = !whole ? 1.f : lt == 0.f ? 0.f : 1.f / lt;
                 unsigned any_odd = 0u;
@@ -446,27 +465,25 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
                                 to[e] = make_uint4(pack_bf16(o[8 * e] * norm, o[8 * e + 1] * norm), pack_bf16(o[8 * e + 2] * norm, o[8 * e + 3] * norm),
                                                    pack_bf16(o[8 * e + 4] * norm, o[8 * e + 5] * norm), pack_bf16(o[8 * e + 6] * norm, o[8 * e + 7] * norm));
                         } else {
-                            float4* to = reinterpret_cast<float4*>(a.acc + slot * HD + col);
+                            // four columns of all rows side by side: the lanes' stores join
+                            float4* to = reinterpret_cast<float4*>(a.acc) + (slot * (HD / 4) + col / 4) * C::rows + rl;
 #pragma unroll
-                            for (int e = 0; e < 8; e++) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                            for (int e = 0; e < 8; e++) to[e * C::rows] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                         }
                     }
                 }
                 if (t >= 0 && (PAIR || s == 0)) {
-                    if (!whole) a.ml[slot] = make_float2(top, lt);
+                    if (!whole) a.ml[slot * C::rows + rl] = make_float2(top, lt);
                     else if (a.lse) a.lse[q_row] = lt == 0.f ? -INFINITY : (top + log2f(lt)) * TT_LN2;
                 }
             }
             tc_fence_before();
             both_sync();                                       // Q, O and the records are free again
             tc_fence_after();
-            if (g.last && !g.first) { cut = g; cut_end = true; }
+            if (g.last && !g.first) { cut_end = true; if (wt == 0) describe_cut_unit(a, g, walk.r); }
             seg++;
         }
-        if (wt == 0) {
-            if (cut_end) describe_cut_unit(a, cut, range);
-            a.desc[(size_t)blockIdx.x * 8 + DESC_VALID] = cut_end ? 1 : 0;
-        }
+        if (wt == 0) a.desc[(size_t)blockIdx.x * 8 + DESC_VALID] = cut_end ? 1 : 0;
     }
     // ---- everyone meets here, on every path; then the allocating warp frees the tensor memory
     __syncwarp();
@@ -483,8 +500,7 @@ static int tree_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, i
     CUtensorMap mk, mv;
     if (!tree_page_map(&mk, cache, cache->k, false) || !tree_page_map(&mv, cache, cache->v, false)) return DYNAKV_ERR_CUDA;
     if (cudaFuncSetAttribute(k_tree_tc<HD, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem) != cudaSuccess) return DYNAKV_ERR_CUDA;
-    k_tree_tc<HD, PAIR><<<sms, TT_THREADS, C::smem, st>>>(mk, mv, a);
-    if (cudaGetLastError() != cudaSuccess) return DYNAKV_ERR_CUDA;
+    if (launch_pdl(k_tree_tc<HD, PAIR>, dim3(sms), dim3(TT_THREADS), C::smem, st, mk, mv, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
     return tree_merge_launch(HD, C::rows, false, a, sms, st);
 }
 
