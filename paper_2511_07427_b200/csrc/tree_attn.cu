@@ -66,18 +66,23 @@ struct TreeCfg {
     static constexpr int panels = row_bytes / panel_w;
     static constexpr int page_bytes = PAGE * row_bytes;
     static constexpr int stage_bytes = 2 * page_bytes;
-    // 96 KB of ring per CTA (FP8, d = 128: less, the exponents and the merge need the rest), at most 12 stages
-    static constexpr int stages = DT == DYNAKV_FP8 && HD == 128 ? (RG == 1 ? 9 : 10) : 98304 / stage_bytes < 12 ? 98304 / stage_bytes : 12;
-    static constexpr int KG = RG == 1 ? 3 : RG == 2 ? (stages % 2 == 0 ? 2 : 1) : 1;
     static constexpr int RT = 16 * RG;
+    static constexpr int dump_bytes = 16 * HD * 4 + 128;                     // one warp's sums, then (m, l) of its 16 rows
+#ifndef DKV_TREE_KG1
+#define DKV_TREE_KG1 3
+#endif
+    static constexpr int KG = RG == 1 ? DKV_TREE_KG1 : RG == 2 && DT != DYNAKV_F32 ? 2 : 1;
+    static constexpr int merge_bytes = (KG - 1) * RG * dump_bytes;
+    // the ring takes what the merge leaves of 112 KB per CTA (fp32: of 200 KB), in a multiple of the page groups, at most 12 stages
+    static constexpr int ring_bytes = (DT == DYNAKV_F32 ? 150 : 112) * 1024 - merge_bytes;
+    static constexpr int most = ring_bytes / (stage_bytes + 80) < 12 ? ring_bytes / (stage_bytes + 80) : 12;
+    static constexpr int stages = most / KG * KG;
     static constexpr int consumers = RG * KG;
     static constexpr int threads = 32 * (consumers + 1);
     static constexpr int per_sm = DT == DYNAKV_F32 ? 1 : 2;
     static constexpr int exp_bytes = DT == DYNAKV_FP8 ? stages * 64 : 0;
     static constexpr int q_bytes = DT == DYNAKV_F32 ? RG * 16 * HD * 4 : 0;
     static constexpr int p_bytes = DT == DYNAKV_F32 ? consumers * 16 * 32 * 4 : 0;
-    static constexpr int dump_bytes = 16 * HD * 4 + 128;                     // one warp's sums, then (m, l) of its 16 rows
-    static constexpr int merge_bytes = KG > 1 ? RG * dump_bytes : 0;
     static constexpr int fixed_bytes = 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + 48 * 8;
     static constexpr int smem = stages * stage_bytes + exp_bytes + q_bytes + p_bytes + merge_bytes + fixed_bytes;
     static_assert(stages % KG == 0, "each ring stage belongs to one page group");
@@ -742,15 +747,13 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             }
             rows.finish();
             if (tid < 8) odd[((seg + 1) % 3) * 8 + tid] = 0u;      // last read before the previous segment's barrier
-            if (KG == 1) all_sync();
+            if (kg > 0) rows.dump(dump + ((kg - 1) * RG + rg) * (C::dump_bytes / 4), lane);
+            all_sync();
+            if (kg == 0) {
 #pragma unroll
-            for (int src = KG - 1; src >= 1; src--) {
-                float* box = dump + rg * (C::dump_bytes / 4);
-                if (kg == src) rows.dump(box, lane);
-                all_sync();
-                if (kg == 0) rows.merge(box, lane);
-                if (src > 1 || KG > 1) all_sync();
+                for (int src = 1; src < KG; src++) rows.merge(dump + ((src - 1) * RG + rg) * (C::dump_bytes / 4), lane);
             }
+            if (KG > 1) all_sync();                    // the boxes may be filled again
             if (kg == 0) {
                 for (int w = 0; w < TREE_MAX / 32; w++) {
                     unsigned bits = odd_now[w];
@@ -770,18 +773,23 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     }
 }
 
-// Merges the records of the units that were cut: block (x = CTA of the first launch in which the unit ends, y = 8 of its rows),
-// a warp per row.
+// Merges the records of the units that were cut: block (x = CTA of the first launch in which the unit ends, y = 8 of its rows).
+// A unit of few rows may have dozens of records (one sequence of 8192 rows: 37), so the block's 8 warps share its rows out, up
+// to all eight of them taking every eighth record of one row.
 template <int HD, int RT, typename OUT>
 __global__ void __launch_bounds__(256) k_tree_merge(const TreeArgs a) {
+    constexpr int EPL = HD / 32;
+    __shared__ float part[8][HD];
     pdl_wait();
     const int* d = a.desc + (size_t)blockIdx.x * 8;
     if (!d[DESC_VALID]) return;
-    constexpr int EPL = HD / 32;
-    const int lane = threadIdx.x & 31, rl = blockIdx.y * 8 + (threadIdx.x >> 5);
-    const int r = d[DESC_RT] * RT + rl, t = r / a.G;
-    if (t >= d[DESC_T]) return;
-    const int c0 = d[DESC_FIRST], n = blockIdx.x - c0 + 1;          // records: slot 1 of CTA c0, slot 0 of the others
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int first = d[DESC_RT] * RT + blockIdx.y * 8, here = min(8, d[DESC_T] * a.G - first);
+    if (here <= 0) return;
+    const int share = here > 4 ? 1 : here > 2 ? 2 : here > 1 ? 4 : 8;        // warps per row
+    const int rb = warp / share, mine = warp % share, r = first + rb, rl = blockIdx.y * 8 + rb, t = r / a.G;
+    const bool live = rb < here;
+    const int c0 = d[DESC_FIRST], n = live ? blockIdx.x - c0 + 1 : 0;        // records: slot 1 of CTA c0, slot 0 of the others
     auto slot = [&](int i) { return ((size_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * RT + rl; };
     float m = -INFINITY;
     for (int i = lane; i < n; i += 32) m = fmaxf(m, a.ml[slot(i)].x);
@@ -796,8 +804,8 @@ __global__ void __launch_bounds__(256) k_tree_merge(const TreeArgs a) {
         if (i0 + lane < n) { const float2 x = a.ml[slot(i0 + lane)]; f = exp2f(x.x - ref); fl = f * x.y; }
         l += warp_sum(fl);
         const int cnt = min(32, n - i0);
-#pragma unroll 4
-        for (int i = 0; i < cnt; i++) {
+#pragma unroll 8
+        for (int i = mine; i < cnt; i += share) {
             const float w = __shfl_sync(0xffffffffu, f, i);
             const float* p = a.acc + slot(i0 + i) * HD + lane * EPL;
             float v[EPL];
@@ -807,6 +815,16 @@ __global__ void __launch_bounds__(256) k_tree_merge(const TreeArgs a) {
             for (int e = 0; e < EPL; e++) acc[e] = fmaf(w, v[e], acc[e]);
         }
     }
+    if (share > 1) {                               // the same in the whole block
+#pragma unroll
+        for (int e = 0; e < EPL; e++) part[warp][lane * EPL + e] = acc[e];
+        __syncthreads();
+        if (mine != 0) return;
+        for (int w = 1; w < share; w++)
+#pragma unroll
+            for (int e = 0; e < EPL; e++) acc[e] += part[warp + w][lane * EPL + e];
+    }
+    if (!live) return;
     const float f = l == 0.f ? 0.f : 1.f / l;
     const size_t at = (size_t)(d[DESC_Q0] + t) * a.Hq + d[DESC_H] * a.G + r - t * a.G;
     OUT* o = reinterpret_cast<OUT*>(a.out) + at * HD + lane * EPL;
