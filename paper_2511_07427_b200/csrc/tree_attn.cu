@@ -114,6 +114,18 @@ __device__ __forceinline__ unsigned chunk_at(int r, int c) {
 
 // ---------------------------------------------------------------------------------- mma.sync consumers (bf16, FP8)
 //
+// The MMAs are plain functions of their registers to the compiler (no volatile), and a group's operands are loaded before its
+// first product: independent chains then overlap, which is what few warps per scheduler need (two; 254 registers each).
+template <bool F16>
+__device__ __forceinline__ void tree_mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
+    if constexpr (F16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
 // Lane (g = lane / 4, c = lane % 4) owns rows g and g + 8 of the warp's 16 and the columns of its fragments.
 template <int HD, int DT, int RG>
 struct MmaRows {
@@ -192,28 +204,31 @@ struct MmaRows {
         if constexpr (!F8) {
             const int mt = lane >> 3, r8 = lane & 7;
 #pragma unroll
-            for (int k2 = 0; k2 < KS / 2; k2++)
+            for (int k2 = 0; k2 < KS / 2; k2++) {
+                unsigned b[4][4];
 #pragma unroll
-                for (int kt = 0; kt < 4; kt++) {
-                    unsigned b[4];
-                    ldmatrix_x4(p.k + chunk_at<C>(kt * 8 + r8, k2 * 4 + mt), b);
-                    mma_bf16(s[kt], qf[2 * k2][0], qf[2 * k2][1], qf[2 * k2][2], qf[2 * k2][3], b[0], b[1]);
-                    mma_bf16(s[kt], qf[2 * k2 + 1][0], qf[2 * k2 + 1][1], qf[2 * k2 + 1][2], qf[2 * k2 + 1][3], b[2], b[3]);
-                }
+                for (int kt = 0; kt < 4; kt++) ldmatrix_x4(p.k + chunk_at<C>(kt * 8 + r8, k2 * 4 + mt), b[kt]);
+#pragma unroll
+                for (int kt = 0; kt < 4; kt++) tree_mma<false>(s[kt], qf[2 * k2], b[kt][0], b[kt][1]);
+#pragma unroll
+                for (int kt = 0; kt < 4; kt++) tree_mma<false>(s[kt], qf[2 * k2 + 1], b[kt][2], b[kt][3]);
+            }
         } else {
 #pragma unroll
-            for (int j = 0; j < HD / 64; j++)
+            for (int j = 0; j < HD / 64; j++) {
+                uint4 w[4];
 #pragma unroll
-                for (int kt = 0; kt < 4; kt++) {
-                    const uint4 w = lds16(p.k + chunk_at<C>(kt * 8 + key_of(n), c + 4 * j));
-                    const unsigned ww[4] = {w.x, w.y, w.z, w.w};
+                for (int kt = 0; kt < 4; kt++) w[kt] = lds16(p.k + chunk_at<C>(kt * 8 + key_of(n), c + 4 * j));
 #pragma unroll
-                    for (int x = 0; x < 4; x++) {
+                for (int x = 0; x < 4; x++)
+#pragma unroll
+                    for (int kt = 0; kt < 4; kt++) {
+                        const unsigned ww[4] = {w[kt].x, w[kt].y, w[kt].z, w[kt].w};
                         unsigned b0, b1;
                         e4m3x4_to_f16x2(ww[x], b0, b1);
-                        mma_f16(s[kt], qf[j * 4 + x][0], qf[j * 4 + x][1], qf[j * 4 + x][2], qf[j * 4 + x][3], b0, b1);
+                        tree_mma<true>(s[kt], qf[j * 4 + x], b0, b1);
                     }
-                }
+            }
         }
         // logits in log2 units, FP8 with the K row's scale; the running maximum is over logit + exponent of the V row
         unsigned win[2] = {~0u, ~0u};
@@ -280,13 +295,14 @@ struct MmaRows {
                     split2(s[2 * kk + x][2], s[2 * kk + x][3], hi[2 * x + 1], lo[2 * x + 1]);
                 }
 #pragma unroll
-                for (int nt = 0; nt < NT; nt += 2) {
-                    unsigned b[4];
-                    ldmatrix_x4_trans(p.v + chunk_at<C>(kk * 16 + (mt & 1) * 8 + r8, nt + (mt >> 1)), b);
-                    mma_bf16(acc[nt], hi[0], hi[1], hi[2], hi[3], b[0], b[1]);
-                    mma_bf16(acc[nt + 1], hi[0], hi[1], hi[2], hi[3], b[2], b[3]);
-                    mma_bf16(acc[nt], lo[0], lo[1], lo[2], lo[3], b[0], b[1]);
-                    mma_bf16(acc[nt + 1], lo[0], lo[1], lo[2], lo[3], b[2], b[3]);
+                for (int nt = 0; nt < NT; nt += 4) {
+                    unsigned b[2][4];
+#pragma unroll
+                    for (int x = 0; x < 2; x++) ldmatrix_x4_trans(p.v + chunk_at<C>(kk * 16 + (mt & 1) * 8 + r8, nt + 2 * x + (mt >> 1)), b[x]);
+#pragma unroll
+                    for (int x = 0; x < 4; x++) tree_mma<false>(acc[nt + x], hi, b[x >> 1][2 * (x & 1)], b[x >> 1][2 * (x & 1) + 1]);
+#pragma unroll
+                    for (int x = 0; x < 4; x++) tree_mma<false>(acc[nt + x], lo, b[x >> 1][2 * (x & 1)], b[x >> 1][2 * (x & 1) + 1]);
                 }
             }
         } else {
@@ -322,8 +338,8 @@ struct MmaRows {
                         unsigned b0, b1, d0, d1;
                         e4m3x4_to_f16x2(__byte_perm(w[0][x], w[1][x], sel), b0, d0);
                         e4m3x4_to_f16x2(__byte_perm(w[2][x], w[3][x], sel), b1, d1);
-                        mma_f16(acc[4 * x + 2 * half], pa[0], pa[1], pa[2], pa[3], b0, b1);
-                        mma_f16(acc[4 * x + 2 * half + 1], pa[0], pa[1], pa[2], pa[3], d0, d1);
+                        tree_mma<true>(acc[4 * x + 2 * half], pa, b0, b1);
+                        tree_mma<true>(acc[4 * x + 2 * half + 1], pa, d0, d1);
                     }
             }
         }
