@@ -66,22 +66,21 @@ struct TreeCfg {
     static constexpr int panels = row_bytes / panel_w;
     static constexpr int page_bytes = PAGE * row_bytes;
     static constexpr int stage_bytes = 2 * page_bytes;
-    static constexpr int RT = 16 * RG;
-    static constexpr int dump_bytes = 16 * HD * 4 + 128;                     // one warp's sums, then (m, l) of its 16 rows
-#ifndef DKV_TREE_KG1
-#define DKV_TREE_KG1 3
-#endif
-    static constexpr int KG = RG == 1 ? DKV_TREE_KG1 : RG == 2 && DT != DYNAKV_F32 ? 2 : 1;
-    static constexpr int merge_bytes = (KG - 1) * RG * dump_bytes;
+    static constexpr int groups = RG == 0 ? 1 : RG;                          // row groups; RG = 0: one, of 8 rows
+    static constexpr int rows = RG == 0 ? 8 : 16;                            // rows of a group
+    static constexpr int RT = groups * rows;
+    static constexpr int dump_bytes = rows * HD * 4 + rows * 8;              // one warp's sums, then (m, l) of its rows
+    static constexpr int KG = RG <= 1 ? 3 : RG == 2 && DT != DYNAKV_F32 ? 2 : 1;
+    static constexpr int consumers = groups * KG;
+    static constexpr int merge_bytes = (KG - 1) * groups * dump_bytes;
     // the ring takes what the merge leaves of 112 KB per CTA (fp32: of 200 KB), in a multiple of the page groups, at most 12 stages
     static constexpr int ring_bytes = (DT == DYNAKV_F32 ? 150 : 112) * 1024 - merge_bytes;
-    static constexpr int most = ring_bytes / (stage_bytes + 80) < 12 ? ring_bytes / (stage_bytes + 80) : 12;
+    static constexpr int most = (ring_bytes - consumers * 512) / (stage_bytes + 80) < 12 ? (ring_bytes - consumers * 512) / (stage_bytes + 80) : 12;
     static constexpr int stages = most / KG * KG;
-    static constexpr int consumers = RG * KG;
     static constexpr int threads = 32 * (consumers + 1);
     static constexpr int per_sm = DT == DYNAKV_F32 ? 1 : 2;
-    static constexpr int exp_bytes = DT == DYNAKV_FP8 ? stages * 64 : 0;
-    static constexpr int q_bytes = DT == DYNAKV_F32 ? RG * 16 * HD * 4 : 0;
+    static constexpr int exp_bytes = DT == DYNAKV_FP8 ? stages * 64 + consumers * 32 * 16 : 0;   // and a table of scales per warp
+    static constexpr int q_bytes = DT == DYNAKV_F32 ? groups * 16 * HD * 4 : 0;
     static constexpr int p_bytes = DT == DYNAKV_F32 ? consumers * 16 * 32 * 4 : 0;
     static constexpr int fixed_bytes = 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + 48 * 8;
     static constexpr int smem = stages * stage_bytes + exp_bytes + q_bytes + p_bytes + merge_bytes + fixed_bytes;
@@ -93,6 +92,7 @@ struct TreeCfg {
 struct PageIn {
     unsigned k, v;                 // shared-memory addresses
     const signed char* exps;       // FP8: scale exponents of the 32 K rows, then of the 32 V rows
+    float4* scales;                // FP8: this warp's table of what they come to (shared memory)
     int key0;                      // first row's place in the sequence
     bool mask;                     // rows of the page may be invisible
 };
@@ -126,17 +126,20 @@ __device__ __forceinline__ void tree_mma(float (&c)[4], const unsigned (&a)[4], 
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Lane (g = lane / 4, c = lane % 4) owns rows g and g + 8 of the warp's 16 and the columns of its fragments.
+// Lane (g = lane / 4, c = lane % 4) owns rows g and g + 8 of the warp's 16 and the columns of its fragments.  With at most 8
+// rows (RG = 0: plain decoding of a group of up to 8 heads) rows 8 to 15 of the weights' tile hold the lo parts of rows 0 to 7, so
+// that one MMA does for both, and only one row per lane goes through the softmax.
 template <int HD, int DT, int RG>
 struct MmaRows {
     using C = TreeCfg<HD, DT, RG>;
     static constexpr bool F8 = DT == DYNAKV_FP8;
-    static constexpr int KS = HD / 16, NT = HD / 8;
+    static constexpr bool HALF = RG == 0;
+    static constexpr int KS = HD / 16, NT = HD / 8, NR = HALF ? 1 : 2;       // rows per lane
     static constexpr bool PERM = F8 && HD == 128;       // key order inside a tile that keeps FP8 loads free of conflicts
     unsigned qf[KS][4];
-    float qs[2];                                        // logit factor (log2 units) of the two rows
-    float acc[NT][4], m[2], l[2];
-    int t[2];                                           // token of the two rows, -1: no such row
+    float qs[NR];                                       // logit factor (log2 units) of the rows
+    float acc[NT][4], m[NR], l[NR];
+    int t[NR];                                          // token of the rows, -1: no such row
 
     static __device__ __forceinline__ int key_of(int n) { return PERM ? (n & 1) * 4 + (n >> 1) : n; }       // column n of an 8-key tile
     // element of the output that acc[nt][i] (i = 0, 1) of lane column c holds
@@ -149,7 +152,7 @@ struct MmaRows {
     __device__ __forceinline__ void start(const TreeArgs& a, const Segment& g, int rg, int lane) {
         const int c = lane & 3;
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < NR; i++) {
             const int r = g.tile * C::RT + rg * 16 + (lane >> 2) + 8 * i;
             t[i] = r < g.T * a.G ? r / a.G : -1;
             const unsigned* q = reinterpret_cast<const unsigned*>(
@@ -188,6 +191,10 @@ struct MmaRows {
             }
             m[i] = -INFINITY; l[i] = 0.f;
         }
+        if constexpr (HALF) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++) qf[ks][1] = qf[ks][3] = 0u;
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -196,6 +203,15 @@ struct MmaRows {
 
     __device__ __forceinline__ void page(const TreeArgs& a, const Segment& g, const PageIn& p, int lane) {
         const int c = lane & 3, n = lane >> 2;
+        // FP8: one lane per row turns its exponents into factors, and all lanes read what they need behind the products: the logit's
+        // factor, the exponent that takes part in the softmax, its factor back, and what a V row below 2^VE_LOW is still to be scaled by
+        bool low = false;
+        if constexpr (F8) {
+            const float ve = (float)p.exps[32 + lane], vr = fmaxf(ve, VE_LOW);
+            p.scales[lane] = make_float4(pow2f(p.exps[lane]), vr, pow2f(-(int)vr), ex2(fminf(ve - VE_LOW, 0.f)));
+            low = __any_sync(0xffffffffu, ve < VE_LOW);
+            __syncwarp();
+        }
         float s[4][4];
 #pragma unroll
         for (int kt = 0; kt < 4; kt++)
@@ -231,58 +247,67 @@ struct MmaRows {
             }
         }
         // logits in log2 units, FP8 with the K row's scale; the running maximum is over logit + exponent of the V row
-        unsigned win[2] = {~0u, ~0u};
-        if (p.mask) {
+        unsigned win[NR];
 #pragma unroll
-            for (int i = 0; i < 2; i++) win[i] = t[i] >= 0 ? tree_window(a, g, t[i], p.key0) : 0u;
-        }
-        float ve[4][2];
-        float mx[2] = {-INFINITY, -INFINITY};
+        for (int i = 0; i < NR; i++) win[i] = !p.mask ? ~0u : t[i] >= 0 ? tree_window(a, g, t[i], p.key0) : 0u;
+        float4 sc[4][2];
+        float mx[NR];
+#pragma unroll
+        for (int i = 0; i < NR; i++) mx[i] = -INFINITY;
 #pragma unroll
         for (int kt = 0; kt < 4; kt++)
 #pragma unroll
             for (int e = 0; e < 2; e++) {
                 const int key = kt * 8 + key_of(2 * c + e);
-                float f = 1.f;
-                ve[kt][e] = 0.f;
-                if constexpr (F8) { f = pow2f(p.exps[key]); ve[kt][e] = (float)p.exps[32 + key]; }
+                if constexpr (F8) sc[kt][e] = p.scales[key];
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
+                for (int i = 0; i < NR; i++) {
                     float& x = s[kt][2 * i + e];
-                    x *= F8 ? qs[i] * f : qs[i];
+                    x *= F8 ? qs[i] * sc[kt][e].x : qs[i];
                     if (p.mask && !((win[i] >> key) & 1u)) x = -INFINITY;
-                    mx[i] = fmaxf(mx[i], F8 ? x + fmaxf(ve[kt][e], VE_LOW) : x);
+                    if constexpr (F8) x += sc[kt][e].y;
+                    mx[i] = fmaxf(mx[i], x);
                 }
             }
-        float ref[2];
+        float ref[NR];
         bool move = false;
 #pragma unroll
-        for (int i = 0; i < 2; i++) { mx[i] = quad_max(mx[i]); move |= mx[i] > m[i] + LAZY; }
+        for (int i = 0; i < NR; i++) { mx[i] = quad_max(mx[i]); move |= mx[i] > m[i] + LAZY; }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
+            for (int i = 0; i < NR; i++) {
                 const float to = mx[i] > m[i] + LAZY ? mx[i] : m[i];
                 const float f = to == -INFINITY ? 1.f : ex2(m[i] - to);
                 m[i] = to; l[i] *= f;
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) { acc[nt][2 * i] *= f; acc[nt][2 * i + 1] *= f; }
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int x = 0; x < (HALF ? 4 : 2); x++) acc[nt][2 * i + x] *= f;
             }
         }
 #pragma unroll
-        for (int i = 0; i < 2; i++) ref[i] = m[i] == -INFINITY ? 0.f : m[i];
+        for (int i = 0; i < NR; i++) ref[i] = m[i] == -INFINITY ? 0.f : m[i];
 #pragma unroll
         for (int kt = 0; kt < 4; kt++)
 #pragma unroll
-            for (int e = 0; e < 2; e++) {
-                const float vr = fmaxf(ve[kt][e], VE_LOW);
+            for (int e = 0; e < 2; e++)
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
+                for (int i = 0; i < NR; i++) {
                     float& x = s[kt][2 * i + e];
-                    x = ex2((F8 ? x + vr : x) - ref[i]);
-                    l[i] += F8 ? x * pow2f(-(int)vr) : x;
-                    if (F8 && ve[kt][e] < VE_LOW) x *= ex2(ve[kt][e] - VE_LOW);
+                    x = ex2(x - ref[i]);
+                    if constexpr (F8) l[i] = fmaf(x, sc[kt][e].z, l[i]);
+                    else l[i] += x;
                 }
+        if constexpr (F8) {
+            if (low) {
+#pragma unroll
+                for (int kt = 0; kt < 4; kt++)
+#pragma unroll
+                    for (int e = 0; e < 2; e++)
+#pragma unroll
+                        for (int i = 0; i < NR; i++) s[kt][2 * i + e] *= sc[kt][e].w;
             }
+        }
         // weights as A fragments: two 8-key tiles of the logits are the 16 keys of a step
         if constexpr (!F8) {
             const int mt = lane >> 3, r8 = lane & 7;
@@ -291,8 +316,11 @@ struct MmaRows {
                 unsigned hi[4], lo[4];
 #pragma unroll
                 for (int x = 0; x < 2; x++) {
-                    split2(s[2 * kk + x][0], s[2 * kk + x][1], hi[2 * x], lo[2 * x]);
-                    split2(s[2 * kk + x][2], s[2 * kk + x][3], hi[2 * x + 1], lo[2 * x + 1]);
+                    if constexpr (HALF) split2(s[2 * kk + x][0], s[2 * kk + x][1], hi[2 * x], hi[2 * x + 1]);
+                    else {
+                        split2(s[2 * kk + x][0], s[2 * kk + x][1], hi[2 * x], lo[2 * x]);
+                        split2(s[2 * kk + x][2], s[2 * kk + x][3], hi[2 * x + 1], lo[2 * x + 1]);
+                    }
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; nt += 4) {
@@ -302,7 +330,7 @@ struct MmaRows {
 #pragma unroll
                     for (int x = 0; x < 4; x++) tree_mma<false>(acc[nt + x], hi, b[x >> 1][2 * (x & 1)], b[x >> 1][2 * (x & 1) + 1]);
 #pragma unroll
-                    for (int x = 0; x < 4; x++) tree_mma<false>(acc[nt + x], lo, b[x >> 1][2 * (x & 1)], b[x >> 1][2 * (x & 1) + 1]);
+                    for (int x = 0; x < (HALF ? 0 : 4); x++) tree_mma<false>(acc[nt + x], lo, b[x >> 1][2 * (x & 1)], b[x >> 1][2 * (x & 1) + 1]);
                 }
             }
         } else {
@@ -313,9 +341,12 @@ struct MmaRows {
                 unsigned pa[4];
 #pragma unroll
                 for (int x = 0; x < 2; x++) {
-                    const __half2 h0 = __floats2half2_rn(s[2 * kk + x][0], s[2 * kk + x][1]), h1 = __floats2half2_rn(s[2 * kk + x][2], s[2 * kk + x][3]);
-                    pa[2 * x] = *reinterpret_cast<const unsigned*>(&h0);
-                    pa[2 * x + 1] = *reinterpret_cast<const unsigned*>(&h1);
+                    if constexpr (HALF) split2h(s[2 * kk + x][0], s[2 * kk + x][1], pa[2 * x], pa[2 * x + 1]);
+                    else {
+                        const __half2 h0 = __floats2half2_rn(s[2 * kk + x][0], s[2 * kk + x][1]), h1 = __floats2half2_rn(s[2 * kk + x][2], s[2 * kk + x][3]);
+                        pa[2 * x] = *reinterpret_cast<const unsigned*>(&h0);
+                        pa[2 * x + 1] = *reinterpret_cast<const unsigned*>(&h1);
+                    }
                 }
                 unsigned w[4][VB / 4];
 #pragma unroll
@@ -347,24 +378,28 @@ struct MmaRows {
 
     __device__ __forceinline__ void finish() {
 #pragma unroll
-        for (int i = 0; i < 2; i++) l[i] = quad_sum(l[i]);
+        for (int i = 0; i < NR; i++) l[i] = quad_sum(l[i]);
+        if constexpr (HALF) {                      // the lo parts join the hi parts
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) { acc[nt][0] += acc[nt][2]; acc[nt][1] += acc[nt][3]; }
+        }
     }
     // This warp's state into shared memory, and another's into this one's.
     __device__ __forceinline__ void dump(float* to, int lane) const {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-            for (int x = 0; x < 4; x++) to[(nt * 4 + x) * 32 + lane] = acc[nt][x];
+            for (int x = 0; x < 2 * NR; x++) to[(nt * 2 * NR + x) * 32 + lane] = acc[nt][x];
         if ((lane & 3) == 0) {
 #pragma unroll
-            for (int i = 0; i < 2; i++) reinterpret_cast<float2*>(to + NT * 128)[(lane >> 2) + 8 * i] = make_float2(m[i], l[i]);
+            for (int i = 0; i < NR; i++) reinterpret_cast<float2*>(to + NT * 64 * NR)[(lane >> 2) + 8 * i] = make_float2(m[i], l[i]);
         }
     }
     __device__ __forceinline__ void merge(const float* from, int lane) {
-        float f0[2], f1[2];
+        float f0[NR], f1[NR];
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const float2 o = reinterpret_cast<const float2*>(from + NT * 128)[(lane >> 2) + 8 * i];
+        for (int i = 0; i < NR; i++) {
+            const float2 o = reinterpret_cast<const float2*>(from + NT * 64 * NR)[(lane >> 2) + 8 * i];
             const float to = fmaxf(m[i], o.x), ref = to == -INFINITY ? 0.f : to;
             f0[i] = ex2(m[i] - ref); f1[i] = ex2(o.x - ref);
             l[i] = l[i] * f0[i] + o.y * f1[i];
@@ -373,14 +408,15 @@ struct MmaRows {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-            for (int x = 0; x < 4; x++) acc[nt][x] = acc[nt][x] * f0[x >> 1] + from[(nt * 4 + x) * 32 + lane] * f1[x >> 1];
+            for (int x = 0; x < 2 * NR; x++) acc[nt][x] = acc[nt][x] * f0[x >> 1] + from[(nt * 2 * NR + x) * 32 + lane] * f1[x >> 1];
     }
     // The share of a drafted row that was left out of the MMAs: key row `row` of the pool, token j of the tree.
     __device__ __forceinline__ void add_row(const TreeArgs& a, const Segment& g, int rg, long long row, int j, int lane) {
         const int c = lane & 3;
-        float d[2] = {0.f, 0.f};
+        float d[NR];
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < NR; i++) {
+            d[i] = 0.f;
             const int r = g.tile * C::RT + rg * 16 + (lane >> 2) + 8 * i;
             if (t[i] >= 0) {
                 const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q) + ((size_t)(g.q0 + t[i]) * a.Hq + g.h * a.G + r - t[i] * a.G) * HD;
@@ -389,7 +425,7 @@ struct MmaRows {
             d[i] = quad_sum(d[i]);
         }
 #pragma unroll
-        for (int i = 0; i < 2; i++)
+        for (int i = 0; i < NR; i++)
             if (t[i] >= 0 && tree_sees(a, g, t[i], j)) {
                 const float w = ex2(d[i] * (a.scale * LOG2E) - (m[i] == -INFINITY ? 0.f : m[i]));
 #pragma unroll
@@ -401,7 +437,7 @@ struct MmaRows {
     __device__ __forceinline__ void write(const TreeArgs& a, const Segment& g, int rg, int lane, bool whole, size_t slot) const {
         const int c = lane & 3;
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < NR; i++) {
             if (t[i] < 0) continue;
             const int rl = rg * 16 + (lane >> 2) + 8 * i, r = g.tile * C::RT + rl;
             const size_t at = (size_t)(g.q0 + t[i]) * a.Hq + g.h * a.G + r - t[i] * a.G;
@@ -658,7 +694,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     if (tid == 0) {
-        for (int s = 0; s < S; s++) { mbar_init(full(s), 1); mbar_init(empty(s), RG); }
+        for (int s = 0; s < S; s++) { mbar_init(full(s), 1); mbar_init(empty(s), C::groups); }
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
@@ -718,11 +754,11 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         }
     } else {
         // =============================== consumers ===============================
-        const int rg = warp % RG, kg = warp / RG;
+        const int rg = warp % C::groups, kg = warp / C::groups;
         constexpr bool F32 = DT == DYNAKV_F32;
-        typename std::conditional<F32, F32Rows<HD, RG>, MmaRows<HD, F32 ? DYNAKV_BF16 : DT, RG>>::type rows;
+        typename std::conditional<F32, F32Rows<HD, C::groups>, MmaRows<HD, F32 ? DYNAKV_BF16 : DT, RG>>::type rows;
         auto all_sync = [&]() { asm volatile("bar.sync 5, %0;\n" ::"n"(C::consumers * 32) : "memory"); };
-        auto group_sync = [&]() { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + kg), "n"(RG * 32) : "memory"); };
+        auto group_sync = [&]() { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + kg), "n"(C::groups * 32) : "memory"); };
         if constexpr (F32) { rows.q_s = smem_u32(q_s + rg * 16 * HD); rows.p_s = smem_u32(p_s + warp * 16 * 32); }
         int it = 0, seg = 0;
         bool dead = false, cut_end = false;
@@ -731,7 +767,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             unsigned* odd_now = odd + (seg % 3) * 8;
             if constexpr (F32) {
                 all_sync();                            // nobody still reads the last segment's q
-                if (kg == 0) F32Rows<HD, RG>::load_q(a, g, rg, q_s + rg * 16 * HD, lane);
+                if (kg == 0) F32Rows<HD, C::groups>::load_q(a, g, rg, q_s + rg * 16 * HD, lane);
                 all_sync();
             }
             rows.start(a, g, rg, lane);
@@ -746,13 +782,14 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 dead = __any_sync(0xffffffffu, dead);
                 PageIn p;
                 p.k = ring + st * C::stage_bytes; p.v = p.k + C::page_bytes; p.exps = exps + st * 64;
+                p.scales = reinterpret_cast<float4*>(exps + S * 64) + warp * 32;
                 p.key0 = pg * PAGE;
                 p.mask = p.key0 + PAGE > prefix;       // holds drafted rows or the end of the sequence
                 // a page that the table does not name was not copied: the stage holds an older one
                 const bool there = !dead && meta[st] != 0;
                 if (p.mask) {                          // the same in all warps of the group, dead or not
                     if (rg == 0 && there) mend_page<C, DT>(p.v, g, p.key0, odd_now, lane);
-                    if (RG > 1) group_sync();
+                    if (C::groups > 1) group_sync();
                 }
                 if (there) {
                     if constexpr (F32) rows.page(a, g, p, lane, rg);
@@ -763,11 +800,11 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             }
             rows.finish();
             if (tid < 8) odd[((seg + 1) % 3) * 8 + tid] = 0u;      // last read before the previous segment's barrier
-            if (kg > 0) rows.dump(dump + ((kg - 1) * RG + rg) * (C::dump_bytes / 4), lane);
+            if (kg > 0) rows.dump(dump + ((kg - 1) * C::groups + rg) * (C::dump_bytes / 4), lane);
             all_sync();
             if (kg == 0) {
 #pragma unroll
-                for (int src = 1; src < KG; src++) rows.merge(dump + ((src - 1) * RG + rg) * (C::dump_bytes / 4), lane);
+                for (int src = 1; src < KG; src++) rows.merge(dump + ((src - 1) * C::groups + rg) * (C::dump_bytes / 4), lane);
             }
             if (KG > 1) all_sync();                    // the boxes may be filled again
             if (kg == 0) {
@@ -903,7 +940,7 @@ static cudaError_t merge_launch_rows(int rt, bool f32, const TreeArgs& a, dim3 g
         const dim3 cols(grid.x, HD / 16);
         return rt == 128 ? launch_pdl(k_tree_merge_cols<HD, 128>, cols, dim3(128), 0, st, a) : launch_pdl(k_tree_merge_cols<HD, 256>, cols, dim3(256), 0, st, a);
     }
-    return rt == 16 ? merge_launch<HD, 16>(f32, a, grid, st) : rt == 32 ? merge_launch<HD, 32>(f32, a, grid, st) : merge_launch<HD, 64>(f32, a, grid, st);
+    return rt == 8 ? merge_launch<HD, 8>(f32, a, grid, st) : rt == 16 ? merge_launch<HD, 16>(f32, a, grid, st) : rt == 32 ? merge_launch<HD, 32>(f32, a, grid, st) : merge_launch<HD, 64>(f32, a, grid, st);
 }
 int tree_merge_launch(int hd, int rt, bool f32, const TreeArgs& a, int ctas, cudaStream_t st) {
     const dim3 grid(ctas, rt / 8);
@@ -921,11 +958,12 @@ static int tree_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeA
 
 template <int HD, int DT>
 static int tree_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
+    if constexpr (DT != DYNAKV_F32) { if (rg == 0) return tree_launch<HD, DT, 0>(mk, mv, a, sms, st); }
     return rg == 1 ? tree_launch<HD, DT, 1>(mk, mv, a, sms, st) : rg == 2 ? tree_launch<HD, DT, 2>(mk, mv, a, sms, st) : tree_launch<HD, DT, 4>(mk, mv, a, sms, st);
 }
 
-// 16 rows of a tile per row group; the groups needed for all rows of a sequence in one tile, up to four
-static int row_groups(int max_rows) { return max_rows <= 16 ? 1 : max_rows <= 32 ? 2 : 4; }
+// 16 rows of a tile per row group; the groups needed for all rows of a sequence in one tile, up to four (0: one of 8 rows)
+static int row_groups(int max_rows, bool f32) { return max_rows <= 8 && !f32 ? 0 : max_rows <= 16 ? 1 : max_rows <= 32 ? 2 : 4; }
 
 struct TreeSpace { size_t acc, ml, desc, bytes; };
 static TreeSpace tree_space(int ctas, int rt, int hd) {
@@ -945,8 +983,8 @@ struct TreeKind { bool tc; int rg, rows, ctas; };
 static TreeKind tree_kind(const dynakv_row_cache* c, int n_heads, int max_tree, int sms) {
     const int most = max_tree * (n_heads / c->n_kv_heads);
     if (c->kv_dtype == DYNAKV_BF16 && most >= DKV_TREE_TC_MIN) return {true, 0, most <= 128 ? 128 : 256, sms};
-    const int rg = row_groups(most);
-    return {false, rg, 16 * rg, sms * (c->kv_dtype == DYNAKV_F32 ? 1 : 2)};
+    const int rg = row_groups(most, c->kv_dtype == DYNAKV_F32);
+    return {false, rg, rg == 0 ? 8 : 16 * rg, sms * (c->kv_dtype == DYNAKV_F32 ? 1 : 2)};
 }
 
 static bool tree_shape_ok(const dynakv_row_cache* c, int n_heads, int max_tree) {
