@@ -760,7 +760,9 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         auto all_sync = [&]() { asm volatile("bar.sync 5, %0;\n" ::"n"(C::consumers * 32) : "memory"); };
         auto group_sync = [&]() { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + kg), "n"(C::groups * 32) : "memory"); };
         if constexpr (F32) { rows.q_s = smem_u32(q_s + rg * 16 * HD); rows.p_s = smem_u32(p_s + warp * 16 * 32); }
-        int it = 0, seg = 0;
+        // This group's items are every KG-th of the CTA: `ahead` items pass before its next one, which lies in stage `st` in phase `ph`.
+        int ahead = kg, st = kg, seg = 0;
+        unsigned ph = 0;
         bool dead = false, cut_end = false;
         while (walk.next(a, g)) {
             const int prefix = g.n - g.T;
@@ -771,15 +773,15 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 all_sync();
             }
             rows.start(a, g, rg, lane);
-            for (int pg = g.p0; pg < g.p1; pg++, it++) {
-                if (KG > 1 && it % KG != kg) continue;
-                const int st = it % S;
-                if (!dead && (*reinterpret_cast<volatile int*>(s_abort) || !mbar_wait(full(st), (it / S) & 1))) {
-                    dead = true;
-                    *reinterpret_cast<volatile int*>(s_abort) = 1;
-                    tree_status(a, DYNAKV_ST_INTERNAL);
+            int pg = g.p0 + ahead;
+            for (; pg < g.p1; pg += KG) {
+                if (!dead && !__all_sync(0xffffffffu, mbar_try_wait(full(st), ph))) {
+                    if (!__all_sync(0xffffffffu, !*reinterpret_cast<volatile int*>(s_abort) && mbar_wait(full(st), ph))) {
+                        dead = true;
+                        *reinterpret_cast<volatile int*>(s_abort) = 1;
+                        tree_status(a, DYNAKV_ST_INTERNAL);
+                    }
                 }
-                dead = __any_sync(0xffffffffu, dead);
                 PageIn p;
                 p.k = ring + st * C::stage_bytes; p.v = p.k + C::page_bytes; p.exps = exps + st * 64;
                 p.scales = reinterpret_cast<float4*>(exps + S * 64) + warp * 32;
@@ -797,7 +799,10 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(empty(st));
+                st += KG;
+                if (st >= S) { st = kg; ph ^= 1; }
             }
+            ahead = pg - g.p1;
             rows.finish();
             if (tid < 8) odd[((seg + 1) % 3) * 8 + tid] = 0u;      // last read before the previous segment's barrier
             if (kg > 0) rows.dump(dump + ((kg - 1) * C::groups + rg) * (C::dump_bytes / 4), lane);
