@@ -956,7 +956,8 @@ template <int HD, int DT, int RG>
 static int tree_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
     using C = TreeCfg<HD, DT, RG>;
     const int grid = sms * C::per_sm;
-    if (cudaFuncSetAttribute(k_tree_attn<HD, DT, RG>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem) != cudaSuccess) return DYNAKV_ERR_CUDA;
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(k_tree_attn<HD, DT, RG>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
     if (launch_pdl(k_tree_attn<HD, DT, RG>, dim3(grid), dim3(C::threads), C::smem, st, mk, mv, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
     return tree_merge_launch(HD, C::RT, DT == DYNAKV_F32, a, grid, st);
 }

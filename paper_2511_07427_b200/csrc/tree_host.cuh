@@ -59,6 +59,17 @@ static int sm_count(int* rc) {
     return n;
 }
 
+// More than 48 KB of dynamic shared memory, asked for once per device; `done`: the kernel's own word, a bit per device.
+template <typename K>
+static bool allow_smem(K kernel, int bytes, std::atomic<unsigned long long>& done) {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    if ((done.load(std::memory_order_acquire) >> dev) & 1ull) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done.fetch_or(1ull << dev, std::memory_order_release);
+    return true;
+}
+
 // tcgen05 kernel (tree_tc.cu): bf16 rows, tiles of 128 or 256 query rows, one CTA per SM.
 int tree_tc_launch(const dynakv_row_cache* cache, int rows, const TreeArgs& a, int sms, cudaStream_t st);
 // Merge of cut units (tree_attn.cu).

@@ -499,7 +499,8 @@ static int tree_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, i
     using C = TcTree<HD, PAIR>;
     CUtensorMap mk, mv;
     if (!tree_page_map(&mk, cache, cache->k, false) || !tree_page_map(&mv, cache, cache->v, false)) return DYNAKV_ERR_CUDA;
-    if (cudaFuncSetAttribute(k_tree_tc<HD, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem) != cudaSuccess) return DYNAKV_ERR_CUDA;
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(k_tree_tc<HD, PAIR>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
     if (launch_pdl(k_tree_tc<HD, PAIR>, dim3(sms), dim3(TT_THREADS), C::smem, st, mk, mv, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
     return tree_merge_launch(HD, C::rows, false, a, sms, st);
 }

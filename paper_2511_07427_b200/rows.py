@@ -8,7 +8,6 @@ compute no gradients and refuse inputs that would need one.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import math
 
 from .binding import BF16, F32, FP8, DynaKVError, load_library
@@ -41,18 +40,40 @@ SIGNATURES = {
 }
 SIGNATURES["dynakv_attend_tree"] = (C.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, C.c_float, _vp, _vp, _vp, _i64, _vp, _vp])
 SIGNATURES["dynakv_attend_tree_workspace"] = (_i64, [_vp, _i32, _i32])
-_bound = None
 
 
-def _library():
-    global _bound
-    if _bound is None:
+class _Env:
+    """What every call looks up, found once: the library's functions, torch's types, and torch's raw accessors of the current
+    device and stream, which make no Python objects (some 2 us of a call that takes ten)."""
+
+    def __init__(self):
+        import torch
         L = load_library()
         for name, (res, args) in SIGNATURES.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
-        _bound = L
-    return _bound
+            setattr(self, name, fn)
+        self.library, self.torch = L, torch
+        self.empty, self.i32, self.f32, self.bf16, self.i64 = torch.empty, torch.int32, torch.float32, torch.bfloat16, torch.int64
+        self.types = {torch.float32: F32, torch.bfloat16: BF16}
+        self.grad = torch.is_grad_enabled
+        stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.stream = stream if stream is not None else lambda device: torch.cuda.current_stream(device).cuda_stream
+        self.device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+_env_made = None
+
+
+def _env() -> _Env:
+    global _env_made
+    if _env_made is None:
+        _env_made = _Env()
+    return _env_made
+
+
+def _library():
+    return _env().library
 
 
 def _torch():
@@ -61,69 +82,43 @@ def _torch():
 
 
 def _float_type(dtype, what: str) -> int:
-    if dtype is _bf16():
-        return BF16
-    if dtype is _f32():
-        return F32
-    raise DynaKVError(f"{what} is {dtype}: expected torch.float32 or torch.bfloat16")
+    code = _env().types.get(dtype)
+    if code is None:
+        raise DynaKVError(f"{what} is {dtype}: expected torch.float32 or torch.bfloat16")
+    return code
 
 
-@functools.lru_cache(None)
-def _bf16():
-    return _torch().bfloat16
-
-
-@functools.lru_cache(None)
-def _f32():
-    return _torch().float32
-
-
-@functools.lru_cache(None)
-def _i32_type():
-    return _torch().int32
-
-
-def _index(t, shape: tuple, device: int, what: str) -> int:
+def _index(E, t, shape: tuple, device: int, what: str) -> int:
     """A contiguous int32 tensor of `shape` on CUDA device `device`; its address."""
-    if t.dtype is not _i32_type() or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+    if t.dtype is not E.i32 or t.shape != shape or t.get_device() != device or not t.is_contiguous():
         raise DynaKVError(f"expected {what} as a contiguous int32 tensor of shape {shape} on cuda:{device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _heads(t, shape: tuple, device: int, dtype, what: str) -> _HeadRows:
+def _heads(E, t, shape: tuple, device: int, dtype, code: int, what: str) -> _HeadRows:
     """A [n, heads, d] tensor whose last dimension is contiguous; the other strides are free."""
     stride = t.stride()
-    if t.shape != shape or t.get_device() != device or t.dtype is not dtype or stride[2] != 1:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or stride[2] != 1:
         raise DynaKVError(f"expected {what} as a {dtype} tensor of shape {shape} on cuda:{device} with a contiguous last dimension, "
                           f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {stride}")
-    if t.requires_grad and _torch().is_grad_enabled():
+    if t.requires_grad and E.grad():
         _no_gradient()
-    return _HeadRows(t.data_ptr(), stride[0], stride[1], _float_type(dtype, what))
+    return _HeadRows(t.data_ptr(), stride[0], stride[1], code)
 
 
 def _no_gradient() -> None:
     raise DynaKVError("this call computes no gradients: detach its inputs or run it under torch.no_grad()")
 
 
-@functools.lru_cache(None)
-def _stream_of():
-    """device index -> address of its current stream: torch's raw accessor, which makes no Stream object (1.5 us a call less)."""
-    torch = _torch()
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw if raw is not None else lambda device: torch.cuda.current_stream(device).cuda_stream
-
-
-def _call(device: int, name: str, *args) -> None:
+def _call(E, device: int, fn, *args) -> None:
     """One C call on the device's current stream (its last argument), with the device made current when it is not."""
-    cuda = _torch().cuda
-    fn = getattr(_bound or _library(), name)
-    if cuda.current_device() == device:
-        rc = fn(*args, _stream_of()(device))
+    if E.device() == device:
+        rc = fn(*args, E.stream(device))
     else:
-        with cuda.device(device):
-            rc = fn(*args, _stream_of()(device))
+        with E.torch.cuda.device(device):
+            rc = fn(*args, E.stream(device))
     if rc != 0:
-        raise DynaKVError(f"{name} returned {rc}")
+        raise DynaKVError(f"{fn.__name__} returned {rc}")
 
 
 def _on_cuda(t, what: str):
@@ -151,7 +146,7 @@ class HeadRotary:
         if rotary_dim > self.head_dim or rotary_dim % 16 != 0:
             raise DynaKVError(f"inv_freq has {inv_freq.numel()} elements: rotary_dim = {rotary_dim} has to be a multiple of 16 up to head_dim")
         self.device = _on_cuda(inv_freq, "inv_freq")
-        self._index = inv_freq.get_device()
+        self._device = inv_freq.get_device()
         for name, w, numel in (("inv_freq", inv_freq, rotary_dim // 2), ("q_weight", q_weight, self.head_dim), ("k_weight", k_weight, self.head_dim)):
             if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (numel,) or not w.is_contiguous() or w.device != self.device):
                 raise DynaKVError(f"expected {name} as a contiguous float32 tensor of {numel} elements on {self.device}, got {w.dtype} {tuple(w.shape)} on {w.device}")
@@ -162,40 +157,44 @@ class HeadRotary:
                           inv_freq.data_ptr() if rotary_dim else None)
         self._ref = C.byref(self._c)
 
-    def _q_k(self, q, k):
+    def _q_k(self, E, q, k):
         if q.dim() != 3:
             raise DynaKVError(f"expected q of three dimensions, got {tuple(q.shape)}")
         n, dtype = q.shape[0], q.dtype
-        return n, dtype, _heads(q, (n, self.n_heads, self.head_dim), self._index, dtype, "q"), \
-            _heads(k, (n, self.n_kv_heads, self.head_dim), self._index, dtype, "k")
+        code = _float_type(dtype, "q")
+        return n, dtype, code, _heads(E, q, (n, self.n_heads, self.head_dim), self._device, dtype, code, "q"), \
+            _heads(E, k, (n, self.n_kv_heads, self.head_dim), self._device, dtype, code, "k")
 
     def apply(self, q, k, positions, q_dtype=None, k_dtype=None):
         """q [n, heads, d], k [n, KV heads, d] (fp32 or bf16, any token and head strides), positions [n] int32 ->
         (q, k) normed and rotated, contiguous, of ``q_dtype`` and ``k_dtype`` (default: the input's).  With one token per
         sequence an fp32 q is what ``DynaKV.decode_step`` takes and k what ``DynaKV.append`` takes, as [U, G, d] and
         [U, d] views."""
-        torch = _torch()
-        n, dtype, qr, kr = self._q_k(q, k)
+        E, device = _env(), self.device
+        n, dtype, code, qr, kr = self._q_k(E, q, k)
         q_dtype, k_dtype = q_dtype or dtype, k_dtype or dtype
-        qt, kt, place = _float_type(q_dtype, "q_dtype"), _float_type(k_dtype, "k_dtype"), _index(positions, (n,), self._index, "positions")
-        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=q_dtype, device=self.device)
-        k_out = torch.empty((n, self.n_kv_heads, self.head_dim), dtype=k_dtype, device=self.device)
-        _call(self._index, "dynakv_norm_rope", self._ref, C.byref(qr), C.byref(kr), place, n, q_out.data_ptr(), qt, k_out.data_ptr(), kt)
+        qt = code if q_dtype is dtype else _float_type(q_dtype, "q_dtype")
+        kt = code if k_dtype is dtype else _float_type(k_dtype, "k_dtype")
+        place = _index(E, positions, (n,), self._device, "positions")
+        q_out = E.empty((n, self.n_heads, self.head_dim), dtype=q_dtype, device=device)
+        k_out = E.empty((n, self.n_kv_heads, self.head_dim), dtype=k_dtype, device=device)
+        _call(E, self._device, E.dynakv_norm_rope, self._ref, C.byref(qr), C.byref(kr), place, n, q_out.data_ptr(), qt, k_out.data_ptr(), kt)
         return q_out, k_out
 
     def store(self, q, k, v, positions, cache: "RowCache", slots, q_dtype=None):
         """As ``apply``, with the keys and the values v [n, KV heads, d] going into ``slots`` [n] int32 of ``cache``
         (``RowCache.write``'s rules) in the same launch.  Returns q."""
-        torch = _torch()
-        n, dtype, qr, kr = self._q_k(q, k)
-        vr = _heads(v, (n, self.n_kv_heads, self.head_dim), self._index, dtype, "v")
-        if cache._index != self._index or cache.head_dim != self.head_dim or cache.n_kv_heads != self.n_kv_heads:
+        E = _env()
+        n, dtype, code, qr, kr = self._q_k(E, q, k)
+        vr = _heads(E, v, (n, self.n_kv_heads, self.head_dim), self._device, dtype, code, "v")
+        if cache._device != self._device or cache.head_dim != self.head_dim or cache.n_kv_heads != self.n_kv_heads:
             raise DynaKVError(f"the cache holds {cache.n_kv_heads} heads of {cache.head_dim} on {cache.device}, the embedding has "
                               f"{self.n_kv_heads} of {self.head_dim} on {self.device}")
         q_dtype = q_dtype or dtype
-        qt, place, slot = _float_type(q_dtype, "q_dtype"), _index(positions, (n,), self._index, "positions"), _index(slots, (n,), self._index, "slots")
-        q_out = torch.empty((n, self.n_heads, self.head_dim), dtype=q_dtype, device=self.device)
-        _call(self._index, "dynakv_norm_rope_store", self._ref, C.byref(qr), C.byref(kr), C.byref(vr), place, n, q_out.data_ptr(), qt,
+        qt = code if q_dtype is dtype else _float_type(q_dtype, "q_dtype")
+        place, slot = _index(E, positions, (n,), self._device, "positions"), _index(E, slots, (n,), self._device, "slots")
+        q_out = E.empty((n, self.n_heads, self.head_dim), dtype=q_dtype, device=self.device)
+        _call(E, self._device, E.dynakv_norm_rope_store, self._ref, C.byref(qr), C.byref(kr), C.byref(vr), place, n, q_out.data_ptr(), qt,
               cache._ref, slot, cache._status_at)
         return q_out
 
@@ -210,7 +209,7 @@ class RowCache:
     def __init__(self, k, v, k_exp=None, v_exp=None):
         torch = _torch()
         self.device = _on_cuda(k, "k")
-        self._index = k.get_device()
+        self._device = k.get_device()
         if k.dim() != 4 or k.shape[2] != PAGE or k.shape[3] not in (64, 128) or k.numel() == 0:
             raise DynaKVError(f"expected k of shape [pages, KV heads, {PAGE}, 64 or 128], got {tuple(k.shape)}")
         types = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: FP8, torch.uint8: FP8}
@@ -235,6 +234,8 @@ class RowCache:
         self._c = _RowCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if k_exp is not None else None,
                             v_exp.data_ptr() if v_exp is not None else None, self.n_pages, self.n_kv_heads, self.head_dim, self.kv_dtype)
         self._ref = C.byref(self._c)
+        self._io = torch.float32 if self.kv_dtype == F32 else torch.bfloat16      # type of q, of the results and of rows read
+        self._byte, self._scale = torch.uint8, self.head_dim ** -0.5
         self._workspace = {}           # bytes attend_tree needs, by (heads, max_tree)
 
     @classmethod
@@ -258,23 +259,24 @@ class RowCache:
         cache's type.  A negative slot skips its token; slots >= 0 must differ."""
         if k.dim() != 3:
             raise DynaKVError(f"expected k of three dimensions, got {tuple(k.shape)}")
+        E, device = _env(), self._device
         n, dtype = k.shape[0], k.dtype
-        shape = (n, self.n_kv_heads, self.head_dim)
-        kr, vr = _heads(k, shape, self._index, dtype, "k"), _heads(v, shape, self._index, dtype, "v")
-        _call(self._index, "dynakv_rows_write", self._ref, C.byref(kr), C.byref(vr), _index(slots, (n,), self._index, "slots"), n, self._status_at)
+        shape, code = (n, self.n_kv_heads, self.head_dim), _float_type(dtype, "k")
+        kr, vr = _heads(E, k, shape, device, dtype, code, "k"), _heads(E, v, shape, device, dtype, code, "v")
+        _call(E, device, E.dynakv_rows_write, self._ref, C.byref(kr), C.byref(vr), _index(E, slots, (n,), device, "slots"), n, self._status_at)
 
     def read(self, page_table, lengths, n: int, first: int = 0):
         """Rows [first, first + n) of every sequence in order, (K, V) of shape [sequences, KV heads, n, d], fp32 for an
         fp32 cache, else bf16; zeros at and past ``lengths`` [sequences] int32.  ``page_table`` [sequences, pages per
         sequence] int32.  As [U, n, d] views these are the K, V of ``DynaKV.build_index``."""
-        torch = _torch()
+        E, device = _env(), self._device
         if page_table.dim() != 2 or n < 0 or first < 0:
             raise DynaKVError(f"expected page_table of two dimensions, n >= 0 and first >= 0, got {tuple(page_table.shape)}, {n}, {first}")
         b, per = page_table.shape
-        table, lens = _index(page_table, (b, per), self._index, "page_table"), _index(lengths, (b,), self._index, "lengths")
-        shape, dtype = (b, self.n_kv_heads, n, self.head_dim), torch.float32 if self.kv_dtype == F32 else torch.bfloat16
-        K, V = torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device)
-        _call(self._index, "dynakv_rows_read", self._ref, table, per, lens, b, first, n, K.data_ptr(), V.data_ptr(), self._status_at)
+        table, lens = _index(E, page_table, (b, per), device, "page_table"), _index(E, lengths, (b,), device, "lengths")
+        shape = (b, self.n_kv_heads, n, self.head_dim)
+        K, V = E.empty(shape, dtype=self._io, device=self.device), E.empty(shape, dtype=self._io, device=self.device)
+        _call(E, device, E.dynakv_rows_read, self._ref, table, per, lens, b, first, n, K.data_ptr(), V.data_ptr(), self._status_at)
         return K, V
 
     def attend_tree(self, q, page_table, kv_len, q_start, max_tree: int, tree_mask=None, scale=None, out=None):
@@ -287,48 +289,52 @@ class RowCache:
         sees row j of its tree (None: a chain, j <= i).  ``scale`` defaults to 1 / sqrt(d).  lse [tokens, heads]
         fp32 is the natural logarithm of the weights' sum, for merging with attention over other rows.  A token
         that sees nothing gets zeros and -inf; tokens behind the last sequence are left as they are in ``out``."""
-        torch = _torch()
-        dtype = torch.float32 if self.kv_dtype == F32 else torch.bfloat16
-        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != self._index or q.data_ptr() % 16:
+        E, device, dtype = _env(), self._device, self._io
+        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != device or q.data_ptr() % 16:
             raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {dtype} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
                               f"got {q.dtype} {tuple(q.shape)} on {q.device}")
-        if q.requires_grad and torch.is_grad_enabled():
+        if q.requires_grad and E.grad():
             _no_gradient()
         n, heads, d = q.shape
-        if heads == 0 or heads % self.n_kv_heads != 0 or heads // self.n_kv_heads > 8:
-            raise DynaKVError(f"{heads} query heads over {self.n_kv_heads} KV heads: expected 1 to 8 per KV head")
-        if not 1 <= max_tree <= MAX_TREE:
-            raise DynaKVError(f"max_tree is {max_tree}: expected 1 to {MAX_TREE}")
         if page_table.dim() != 2:
             raise DynaKVError(f"expected page_table of two dimensions, got {tuple(page_table.shape)}")
         b, per = page_table.shape
+        size = self._workspace.get((heads, max_tree))
+        if size is None:
+            size = self._workspace_bytes(E, heads, max_tree)
         mask, words = None, 0
         if tree_mask is not None:
             words = tree_mask.shape[-1]
-            if tree_mask.dtype is not torch.int64 or tree_mask.shape != (n, words) or not 1 <= words <= MAX_TREE // 64 or \
-                    not tree_mask.is_contiguous() or tree_mask.get_device() != self._index:
+            if tree_mask.dtype is not E.i64 or tree_mask.shape != (n, words) or not 1 <= words <= MAX_TREE // 64 or \
+                    not tree_mask.is_contiguous() or tree_mask.get_device() != device:
                 raise DynaKVError(f"expected tree_mask as a contiguous int64 tensor [{n}, 1 to {MAX_TREE // 64}] on {self.device}, "
                                   f"got {tree_mask.dtype} {tuple(tree_mask.shape)} on {tree_mask.device}")
             mask = tree_mask.data_ptr()
         if scale is None:
-            scale = d ** -0.5
-        if not math.isfinite(scale):
+            scale = self._scale
+        elif not math.isfinite(scale):
             raise DynaKVError(f"scale is {scale}: expected a finite number")
         if out is None:
-            out = torch.empty_like(q)
-        elif out.dtype is not dtype or out.shape != q.shape or not out.is_contiguous() or out.get_device() != self._index or out.data_ptr() % 16:
+            out = E.empty((n, heads, d), dtype=dtype, device=self.device)
+        elif out.dtype is not dtype or out.shape != q.shape or not out.is_contiguous() or out.get_device() != device or out.data_ptr() % 16:
             raise DynaKVError(f"expected out as a contiguous, 16-byte aligned {dtype} tensor {tuple(q.shape)} on {self.device}")
-        table, lens, start = _index(page_table, (b, per), self._index, "page_table"), _index(kv_len, (b,), self._index, "kv_len"), \
-            _index(q_start, (b + 1,), self._index, "q_start")
-        lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
-        size = self._workspace.get((heads, max_tree))
-        if size is None:
-            with torch.cuda.device(self.device):
-                size = _library().dynakv_attend_tree_workspace(self._ref, heads, max_tree)
-            if size < 0:
-                raise DynaKVError(f"dynakv_attend_tree_workspace returned {size}")
-            self._workspace[heads, max_tree] = size
-        space = torch.empty(size, dtype=torch.uint8, device=self.device)
-        _call(self._index, "dynakv_attend_tree", self._ref, q.data_ptr(), heads, n, start, b, max_tree, table, per, lens, mask, words, scale,
+        table, lens, start = _index(E, page_table, (b, per), device, "page_table"), _index(E, kv_len, (b,), device, "kv_len"), \
+            _index(E, q_start, (b + 1,), device, "q_start")
+        lse = E.empty((n, heads), dtype=E.f32, device=self.device)
+        space = E.empty(size, dtype=self._byte, device=self.device)
+        _call(E, device, E.dynakv_attend_tree, self._ref, q.data_ptr(), heads, n, start, b, max_tree, table, per, lens, mask, words, scale,
               out.data_ptr(), lse.data_ptr(), space.data_ptr(), size, self._status_at)
         return out, lse
+
+    def _workspace_bytes(self, E, heads: int, max_tree: int) -> int:
+        """Checks the two numbers that choose the kernel, and keeps the bytes of scratch that they come to."""
+        if heads == 0 or heads % self.n_kv_heads != 0 or heads // self.n_kv_heads > 8:
+            raise DynaKVError(f"{heads} query heads over {self.n_kv_heads} KV heads: expected 1 to 8 per KV head")
+        if not 1 <= max_tree <= MAX_TREE:
+            raise DynaKVError(f"max_tree is {max_tree}: expected 1 to {MAX_TREE}")
+        with E.torch.cuda.device(self._device):
+            size = E.dynakv_attend_tree_workspace(self._ref, heads, max_tree)
+        if size < 0:
+            raise DynaKVError(f"dynakv_attend_tree_workspace returned {size}")
+        self._workspace[heads, max_tree] = size
+        return size
