@@ -29,12 +29,13 @@ constexpr int ROW_THREADS = 128;
 //
 // The angle in half turns, position * (inv_freq / pi), is one 64-bit product, and its whole turns are removed in 64 bits
 // before the rest is rounded to fp32: at position 2^20 the fp32 product alone would be off by 0.06 rad.
+constexpr int ROPE_THREADS = 64;           // two warps: the fold below is shared by twice as many rows as with four
 template <int HD, typename T, bool STORE, bool INTER>
-__global__ void __launch_bounds__(ROW_THREADS) k_norm_rope(HeadRowsDev q, HeadRowsDev k, HeadRowsDev v, int vec, dynakv_rotary ro,
+__global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(HeadRowsDev q, HeadRowsDev k, HeadRowsDev v, int vec, dynakv_rotary ro,
                                                            const int* __restrict__ positions, void* q_out, int q_f32,
                                                            void* k_out, int k_f32, dynakv_row_cache cache,
                                                            const int* __restrict__ slots, int passes, unsigned* status) {
-    constexpr int LG = HD / 8, RPP = ROW_THREADS / LG;     // lanes per row, rows per pass
+    constexpr int LG = HD / 8, RPP = ROPE_THREADS / LG;    // lanes per row, rows per pass
     __shared__ __align__(16) float cos_s[HD / 2], sin_s[HD / 2];
     const long long t = blockIdx.x;
     const int l = threadIdx.x % LG;
@@ -52,7 +53,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_norm_rope(HeadRowsDev q, HeadRo
     const bool slot_ok = slot >= 0 && slot < cache.n_pages * PAGE;
     if (STORE && slot >= 0 && !slot_ok && status && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(status, DYNAKV_ST_BOUNDS);
     const int half = ro.rotary_dim / 2;
-    if ((int)threadIdx.x < half) {
+    if ((int)threadIdx.x < half) {                         // half <= 64
         const double turns = (double)positions[t] * ((double)ro.inv_freq[threadIdx.x] * 0.31830988618379067154);   // half turns
         const float f = (float)(turns - 2.0 * rint(turns * 0.5));
         sincospif(f, &sin_s[threadIdx.x], &cos_s[threadIdx.x]);
@@ -105,8 +106,20 @@ __global__ void __launch_bounds__(ROW_THREADS) k_norm_rope(HeadRowsDev q, HeadRo
     };
 
     for (int p = 0; p < passes; p++, r += RPP) {
-        float x[8];
+        float x[8], y[8];                                  // the row's elements and their partners
         unpack8(next, x);
+        if constexpr (INTER) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) y[i] = x[i ^ 1];
+        } else {
+            Raw8<T> other;                                 // exchanged as they lie in memory: half the shuffles for bf16
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; i++) {
+                other.w[i].x = __shfl_sync(0xffffffffu, next.w[i].x, partner); other.w[i].y = __shfl_sync(0xffffffffu, next.w[i].y, partner);
+                other.w[i].z = __shfl_sync(0xffffffffu, next.w[i].z, partner); other.w[i].w = __shfl_sync(0xffffffffu, next.w[i].w, partner);
+            }
+            unpack8(other, y);
+        }
         if (p + 1 < passes) next = load_row(r + RPP);
         const bool live = r < n_rows;
         const int now = r < n_q ? 0 : !STORE || r < n_q + n_k ? 1 : 2;
@@ -118,19 +131,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_norm_rope(HeadRowsDev q, HeadRo
 #pragma unroll
         for (int o = LG / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         const float f = norm ? rsqrtf(ss * (1.f / HD) + ro.eps) : 1.f;
-        float y[8];                                        // the partners
-        if constexpr (INTER) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = x[i ^ 1];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = __shfl_sync(0xffffffffu, x[i], partner);
-            if (!turned || kind == 2) {                    // not its own partner: an infinity there would make 0 * inf
-#pragma unroll
-                for (int i = 0; i < 8; i++) y[i] = 0.f;
-            }
-        }
-        if (INTER && (!turned || kind == 2)) {
+        if (!turned || kind == 2) {                        // no partner: an infinity there would make 0 * inf
 #pragma unroll
             for (int i = 0; i < 8; i++) y[i] = 0.f;
         }
@@ -304,7 +305,7 @@ static int norm_rope(const dynakv_rotary* ro, const dynakv_head_rows* q, const d
     if (n == 0) return DYNAKV_OK;
     if (!float_type(q->dtype) || !head_rows_ok(q, q->dtype) || !head_rows_ok(k, q->dtype) || (v && !head_rows_ok(v, q->dtype)) || !positions ||
         !q_out || ((uintptr_t)q_out & 15) || (k_out && ((uintptr_t)k_out & 15))) return DYNAKV_ERR_ARG;
-    const int rpp = ROW_THREADS / (ro->head_dim / 8);
+    const int rpp = ROPE_THREADS / (ro->head_dim / 8);
     const int rows = ro->n_heads + ro->n_kv_heads * (cache ? 2 : 1), chunks = (rows + rpp - 1) / rpp;
     // a whole token per block once there are two blocks for every SM (148), which shares the sines and the folded constants by all
     // of its rows; fewer tokens (a decode step) spread over the SMs, one pass per block
@@ -316,7 +317,7 @@ static int norm_rope(const dynakv_rotary* ro, const dynakv_head_rows* q, const d
     const int qf = q_dtype == DYNAKV_F32, kf = k_dtype == DYNAKV_F32;
     forget_errors();
 #define DKV_ROPE(HD, T, STORE, INTER) \
-    k_norm_rope<HD, T, STORE, INTER><<<grid, ROW_THREADS, 0, st>>>(dq, dk, dv, vec, *ro, positions, q_out, qf, k_out, kf, c, slots, passes, status)
+    k_norm_rope<HD, T, STORE, INTER><<<grid, ROPE_THREADS, 0, st>>>(dq, dk, dv, vec, *ro, positions, q_out, qf, k_out, kf, c, slots, passes, status)
 #define DKV_ROPE_KIND(HD, T) \
     do { \
         if (cache) { if (ro->interleaved) DKV_ROPE(HD, T, true, true); else DKV_ROPE(HD, T, true, false); } \
