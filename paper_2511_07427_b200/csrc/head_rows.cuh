@@ -106,31 +106,41 @@ __device__ __forceinline__ int row_exp_any(float amax) {
     return max(-120, min(120, e));
 }
 
-// The eight elements of this lane into a cache row (`row`: its index in the whole pool).  All lanes of the row's group
-// call it together; the maximum of an FP8 row is exchanged inside the group of HD / 8 lanes.
-template <int HD>
-__device__ __forceinline__ void store_cache8(const dynakv_row_cache& c, bool is_v, long long row, bool live, int l, const float (&x)[8]) {
-    constexpr int LG = HD / 8;
+// This lane's elements into a cache row (`row`: its index in the whole pool): NC runs of eight, run c at l * 8 + c * HD / NC
+// of the row, HD / 8 / NC lanes per row.  All lanes of the row's group call it together; the maximum of an FP8 row is
+// exchanged inside the group.
+template <int HD, int NC>
+__device__ __forceinline__ void store_cache(const dynakv_row_cache& c, bool is_v, long long row, bool live, int l, const float (&x)[NC][8]) {
+    constexpr int LG = HD / 8 / NC;
     void* pool = is_v ? c.v : c.k;
     const size_t at = (size_t)row * HD + l * 8;
     if (c.kv_dtype == DYNAKV_F32) {
-        if (live) store8(reinterpret_cast<float*>(pool) + at, x);
+        if (live) {
+#pragma unroll
+            for (int y = 0; y < NC; y++) store8(reinterpret_cast<float*>(pool) + at + y * (HD / NC), x[y]);
+        }
     } else if (c.kv_dtype == DYNAKV_BF16) {
-        if (live) store8(reinterpret_cast<__nv_bfloat16*>(pool) + at, x);
+        if (live) {
+#pragma unroll
+            for (int y = 0; y < NC; y++) store8(reinterpret_cast<__nv_bfloat16*>(pool) + at + y * (HD / NC), x[y]);
+        }
     } else {
         float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; i++) m = fmaxf(m, fabsf(x[i]));
+        for (int y = 0; y < NC; y++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) m = fmaxf(m, fabsf(x[y][i]));
         m = group_max(m, LG);
         const int e = row_exp_any(m);
         const float inv = pow2f(-e);
-        uint2 b;
-        b.x = fp8_pack2(x[0], x[1], inv) | ((unsigned)fp8_pack2(x[2], x[3], inv) << 16);
-        b.y = fp8_pack2(x[4], x[5], inv) | ((unsigned)fp8_pack2(x[6], x[7], inv) << 16);
-        if (live) {
-            *reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(pool) + at) = b;
-            if (l == 0) (is_v ? c.v_exp : c.k_exp)[row] = (int8_t)e;
+#pragma unroll
+        for (int y = 0; y < NC; y++) {
+            uint2 b;
+            b.x = fp8_pack2(x[y][0], x[y][1], inv) | ((unsigned)fp8_pack2(x[y][2], x[y][3], inv) << 16);
+            b.y = fp8_pack2(x[y][4], x[y][5], inv) | ((unsigned)fp8_pack2(x[y][6], x[y][7], inv) << 16);
+            if (live) *reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(pool) + at + y * (HD / NC)) = b;
         }
+        if (live && l == 0) (is_v ? c.v_exp : c.k_exp)[row] = (int8_t)e;
     }
 }
 
