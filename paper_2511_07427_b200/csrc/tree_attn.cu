@@ -66,22 +66,23 @@ struct TreeCfg {
     static constexpr int panels = row_bytes / panel_w;
     static constexpr int page_bytes = PAGE * row_bytes;
     static constexpr int stage_bytes = 2 * page_bytes;
-    static constexpr int groups = RG == 0 ? 1 : RG;                          // row groups; RG = 0: one, of 8 rows
-    static constexpr int rows = RG == 0 ? 8 : 16;                            // rows of a group
+    static constexpr int groups = RG == 0 ? 1 : RG;                          // row groups; RG = 0: one, of few rows
+    static constexpr int rows = RG > 0 ? 16 : DT == DYNAKV_F32 ? 4 : 8;      // rows of a group
     static constexpr int RT = groups * rows;
     static constexpr int dump_bytes = rows * HD * 4 + rows * 8;              // one warp's sums, then (m, l) of its rows
-    static constexpr int KG = RG <= 1 ? 3 : RG == 2 && DT != DYNAKV_F32 ? 2 : 1;
+    // page groups; fp32 rows have one CTA per SM and a long way through a page, so more of them
+    static constexpr int KG = DT == DYNAKV_F32 ? (RG == 0 ? 6 : RG == 1 ? 4 : RG == 2 ? 2 : 1) : RG <= 1 ? 3 : RG == 2 ? 2 : 1;
     static constexpr int consumers = groups * KG;
     static constexpr int merge_bytes = (KG - 1) * groups * dump_bytes;
-    // the ring takes what the merge leaves of 112 KB per CTA (fp32: of 200 KB), in a multiple of the page groups, at most 12 stages
-    static constexpr int ring_bytes = (DT == DYNAKV_F32 ? 150 : 112) * 1024 - merge_bytes;
+    // the ring takes what the merge leaves of 112 KB per CTA (fp32: of 224 KB, with q and the weights), in a multiple of the page groups, at most 12 stages
+    static constexpr int ring_bytes = (DT == DYNAKV_F32 ? 224 * 1024 - RT * HD * 4 - consumers * rows * 128 : 112 * 1024) - merge_bytes;
     static constexpr int most = (ring_bytes - consumers * 512) / (stage_bytes + 80) < 12 ? (ring_bytes - consumers * 512) / (stage_bytes + 80) : 12;
     static constexpr int stages = most / KG * KG;
     static constexpr int threads = 32 * (consumers + 1);
     static constexpr int per_sm = DT == DYNAKV_F32 ? 1 : 2;
     static constexpr int exp_bytes = DT == DYNAKV_FP8 ? stages * 64 + consumers * 32 * 16 : 0;   // and a table of scales per warp
-    static constexpr int q_bytes = DT == DYNAKV_F32 ? groups * 16 * HD * 4 : 0;
-    static constexpr int p_bytes = DT == DYNAKV_F32 ? consumers * 16 * 32 * 4 : 0;
+    static constexpr int q_bytes = DT == DYNAKV_F32 ? RT * HD * 4 : 0;
+    static constexpr int p_bytes = DT == DYNAKV_F32 ? consumers * rows * 32 * 4 : 0;
     static constexpr int fixed_bytes = 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + 48 * 8;
     static constexpr int smem = stages * stage_bytes + exp_bytes + q_bytes + p_bytes + merge_bytes + fixed_bytes;
     static_assert(stages % KG == 0, "each ring stage belongs to one page group");
@@ -474,45 +475,46 @@ struct MmaRows {
 // ---------------------------------------------------------------------------------- fp32 consumers
 //
 // Lane = key for the logits (q is read from shared memory, the same word for all lanes), lane = HD / 32 columns for the
-// sums (the weights go through shared memory).  Every lane keeps the 16 rows' running maxima; the sums l stay split
-// over the lanes until the end.
+// sums (the weights go through shared memory).  Every lane keeps all rows' running maxima; the sums l stay split
+// over the lanes until the end.  16 rows per warp, or 4 (plain decoding of a small group), which is a quarter of the code and of
+// the latency.
 template <int HD, int RG>
 struct F32Rows {
     using C = TreeCfg<HD, DYNAKV_F32, RG>;
-    static constexpr int DPL = HD / 32;
-    float acc[16][DPL], m[16], l[16];
-    unsigned q_s, p_s;             // shared memory: this row group's q [16][HD], this warp's weights [16][32]
+    static constexpr int DPL = HD / 32, NR = C::rows;
+    float acc[NR][DPL], m[NR], l[NR];
+    unsigned q_s, p_s;             // shared memory: this row group's q [NR][HD], this warp's weights [NR][32]
     int rows;                      // rows of the warp that exist
 
     __device__ __forceinline__ void start(const TreeArgs& a, const Segment& g, int rg, int lane) {
-        rows = max(0, min(16, g.T * a.G - (g.tile * C::RT + rg * 16)));
+        rows = max(0, min(NR, g.T * a.G - (g.tile * C::RT + rg * NR)));
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
+        for (int r = 0; r < NR; r++) {
             m[r] = -INFINITY; l[r] = 0.f;
 #pragma unroll
             for (int d = 0; d < DPL; d++) acc[r][d] = 0.f;
         }
         (void)lane;
     }
-    // q of the group's rows, every page group its own share of the copy (the caller synchronises around it)
+    // q of the group's rows, scaled; rows that do not exist as zeros.  One warp, the loads of eight steps side by side.
     static __device__ __forceinline__ void load_q(const TreeArgs& a, const Segment& g, int rg, float* q_s, int lane) {
-        for (int r = 0; r < 16; r++) {
-            const int x = g.tile * C::RT + rg * 16 + r, t = x / a.G;
-            const float* q = reinterpret_cast<const float*>(a.q) + ((size_t)(g.q0 + t) * a.Hq + g.h * a.G + x - t * a.G) * HD;
-            for (int e = lane; e < HD; e += 32) q_s[r * HD + e] = t < g.T ? q[e] * (a.scale * LOG2E) : 0.f;
+#pragma unroll 8
+        for (int x = lane; x < NR * HD; x += 32) {
+            const int r = g.tile * C::RT + rg * NR + x / HD, t = r / a.G;
+            const float* q = reinterpret_cast<const float*>(a.q) + ((size_t)(g.q0 + t) * a.Hq + g.h * a.G + r - t * a.G) * HD;
+            q_s[x] = t < g.T ? __ldg(q + x % HD) * (a.scale * LOG2E) : 0.f;
         }
     }
     __device__ __forceinline__ void page(const TreeArgs& a, const Segment& g, const PageIn& p, int lane, int rg) {
-        float s[16];
+        float s[NR];
 #pragma unroll
-        for (int r = 0; r < 16; r++) s[r] = 0.f;
+        for (int r = 0; r < NR; r++) s[r] = 0.f;
 #pragma unroll 4
         for (int ch = 0; ch < HD / 4; ch++) {
             const uint4 ku = lds16(p.k + chunk_at<C>(lane, ch));
             const float k0 = __uint_as_float(ku.x), k1 = __uint_as_float(ku.y), k2 = __uint_as_float(ku.z), k3 = __uint_as_float(ku.w);
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                if (r >= 4 && rows <= 4) continue;
+            for (int r = 0; r < NR; r++) {
                 const uint4 qu = lds16(q_s + (r * HD + ch * 4) * 4);
                 s[r] = fmaf(__uint_as_float(qu.x), k0, s[r]);
                 s[r] = fmaf(__uint_as_float(qu.y), k1, s[r]);
@@ -520,14 +522,13 @@ struct F32Rows {
                 s[r] = fmaf(__uint_as_float(qu.w), k3, s[r]);
             }
         }
-        unsigned win = ~0u;                        // lane r < 16: the window of row r
+        unsigned win = ~0u;                        // lane r < NR: the window of row r
         if (p.mask) {
-            const int x = g.tile * C::RT + rg * 16 + (lane & 15), t = x / a.G;
+            const int x = g.tile * C::RT + rg * NR + (lane & (NR - 1)), t = x / a.G;
             win = t < g.T ? tree_window(a, g, t, p.key0) : 0u;
         }
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-            if (r >= 4 && rows <= 4) continue;
+        for (int r = 0; r < NR; r++) {
             if (p.mask && !((__shfl_sync(0xffffffffu, win, r) >> lane) & 1u)) s[r] = -INFINITY;
             float mx = s[r];
 #pragma unroll
@@ -558,8 +559,7 @@ struct F32Rows {
                 }
             }
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                if (r >= 4 && rows <= 4) continue;
+            for (int r = 0; r < NR; r++) {
                 const uint4 u = lds16(p_s + (r * 32 + k4 * 4) * 4);
                 const float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
 #pragma unroll
@@ -572,20 +572,20 @@ struct F32Rows {
     }
     __device__ __forceinline__ void finish() {
 #pragma unroll
-        for (int r = 0; r < 16; r++) l[r] = warp_sum(l[r]);
+        for (int r = 0; r < NR; r++) l[r] = warp_sum(l[r]);
     }
     __device__ __forceinline__ void dump(float* to, int lane) const {
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
+        for (int r = 0; r < NR; r++) {
 #pragma unroll
             for (int d = 0; d < DPL; d++) to[(r * DPL + d) * 32 + lane] = acc[r][d];
-            if (lane == r) reinterpret_cast<float2*>(to + 16 * HD)[r] = make_float2(m[r], l[r]);
+            if (lane == r) reinterpret_cast<float2*>(to + NR * HD)[r] = make_float2(m[r], l[r]);
         }
     }
     __device__ __forceinline__ void merge(const float* from, int lane) {
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-            const float2 o = reinterpret_cast<const float2*>(from + 16 * HD)[r];
+        for (int r = 0; r < NR; r++) {
+            const float2 o = reinterpret_cast<const float2*>(from + NR * HD)[r];
             const float to = fmaxf(m[r], o.x), ref = to == -INFINITY ? 0.f : to;
             const float f0 = exp2f(m[r] - ref), f1 = exp2f(o.x - ref);
             l[r] = l[r] * f0 + o.y * f1;
@@ -598,11 +598,11 @@ struct F32Rows {
         const float* k = reinterpret_cast<const float*>(a.kpool) + row * HD;
         const float* v = reinterpret_cast<const float*>(a.vpool) + row * HD;
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
+        for (int r = 0; r < NR; r++) {
             float d = 0.f;
             for (int e = lane; e < HD; e += 32) d = fmaf(lds_f32(q_s + (r * HD + e) * 4), k[e], d);
             d = warp_sum(d);
-            const int x = g.tile * C::RT + rg * 16 + r, t = x / a.G;
+            const int x = g.tile * C::RT + rg * NR + r, t = x / a.G;
             if (r < rows && tree_sees(a, g, t, j)) {
                 const float w = exp2f(d - (m[r] == -INFINITY ? 0.f : m[r]));
 #pragma unroll
@@ -612,9 +612,9 @@ struct F32Rows {
     }
     __device__ __forceinline__ void write(const TreeArgs& a, const Segment& g, int rg, int lane, bool whole, size_t slot) const {
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
+        for (int r = 0; r < NR; r++) {
             if (r >= rows) continue;
-            const int rl = rg * 16 + r, x = g.tile * C::RT + rl, t = x / a.G;
+            const int rl = rg * NR + r, x = g.tile * C::RT + rl, t = x / a.G;
             const size_t at = (size_t)(g.q0 + t) * a.Hq + g.h * a.G + x - t * a.G;
             const float f = !whole ? 1.f : l[r] == 0.f ? 0.f : 1.f / l[r];
             float* o = whole ? reinterpret_cast<float*>(a.out) + at * HD : a.acc + (slot * C::RT + rl) * HD;
@@ -756,10 +756,10 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         // =============================== consumers ===============================
         const int rg = warp % C::groups, kg = warp / C::groups;
         constexpr bool F32 = DT == DYNAKV_F32;
-        typename std::conditional<F32, F32Rows<HD, C::groups>, MmaRows<HD, F32 ? DYNAKV_BF16 : DT, RG>>::type rows;
+        typename std::conditional<F32, F32Rows<HD, RG>, MmaRows<HD, F32 ? DYNAKV_BF16 : DT, RG>>::type rows;
         auto all_sync = [&]() { asm volatile("bar.sync 5, %0;\n" ::"n"(C::consumers * 32) : "memory"); };
         auto group_sync = [&]() { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + kg), "n"(C::groups * 32) : "memory"); };
-        if constexpr (F32) { rows.q_s = smem_u32(q_s + rg * 16 * HD); rows.p_s = smem_u32(p_s + warp * 16 * 32); }
+        if constexpr (F32) { rows.q_s = smem_u32(q_s + rg * C::rows * HD); rows.p_s = smem_u32(p_s + warp * C::rows * 32); }
         // This group's items are every KG-th of the CTA: `ahead` items pass before its next one, which lies in stage `st` in phase `ph`.
         int ahead = kg, st = kg, seg = 0;
         unsigned ph = 0;
@@ -769,7 +769,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             unsigned* odd_now = odd + (seg % 3) * 8;
             if constexpr (F32) {
                 all_sync();                            // nobody still reads the last segment's q
-                if (kg == 0) F32Rows<HD, C::groups>::load_q(a, g, rg, q_s + rg * 16 * HD, lane);
+                if (kg == 0) F32Rows<HD, RG>::load_q(a, g, rg, q_s + rg * C::rows * HD, lane);
                 all_sync();
             }
             rows.start(a, g, rg, lane);
@@ -842,7 +842,7 @@ __global__ void __launch_bounds__(256) k_tree_merge(const TreeArgs a) {
     const int* d = a.desc + (size_t)blockIdx.x * 8;
     if (!d[DESC_VALID]) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int first = d[DESC_RT] * RT + blockIdx.y * 8, here = min(8, d[DESC_T] * a.G - first);
+    const int first = d[DESC_RT] * RT + blockIdx.y * 8, here = min(RT < 8 ? RT : 8, d[DESC_T] * a.G - first);
     if (here <= 0) return;
     const int share = here > 4 ? 1 : here > 2 ? 2 : here > 1 ? 4 : 8;        // warps per row
     const int rb = warp / share, mine = warp % share, r = first + rb, rl = blockIdx.y * 8 + rb, t = r / a.G;
@@ -945,10 +945,10 @@ static cudaError_t merge_launch_rows(int rt, bool f32, const TreeArgs& a, dim3 g
         const dim3 cols(grid.x, HD / 16);
         return rt == 128 ? launch_pdl(k_tree_merge_cols<HD, 128>, cols, dim3(128), 0, st, a) : launch_pdl(k_tree_merge_cols<HD, 256>, cols, dim3(256), 0, st, a);
     }
-    return rt == 8 ? merge_launch<HD, 8>(f32, a, grid, st) : rt == 16 ? merge_launch<HD, 16>(f32, a, grid, st) : rt == 32 ? merge_launch<HD, 32>(f32, a, grid, st) : merge_launch<HD, 64>(f32, a, grid, st);
+    return rt == 4 ? merge_launch<HD, 4>(f32, a, grid, st) : rt == 8 ? merge_launch<HD, 8>(f32, a, grid, st) : rt == 16 ? merge_launch<HD, 16>(f32, a, grid, st) : rt == 32 ? merge_launch<HD, 32>(f32, a, grid, st) : merge_launch<HD, 64>(f32, a, grid, st);
 }
 int tree_merge_launch(int hd, int rt, bool f32, const TreeArgs& a, int ctas, cudaStream_t st) {
-    const dim3 grid(ctas, rt / 8);
+    const dim3 grid(ctas, (rt + 7) / 8);
     return (hd == 128 ? merge_launch_rows<128>(rt, f32, a, grid, st) : merge_launch_rows<64>(rt, f32, a, grid, st)) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
 
@@ -964,12 +964,11 @@ static int tree_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeA
 
 template <int HD, int DT>
 static int tree_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
-    if constexpr (DT != DYNAKV_F32) { if (rg == 0) return tree_launch<HD, DT, 0>(mk, mv, a, sms, st); }
-    return rg == 1 ? tree_launch<HD, DT, 1>(mk, mv, a, sms, st) : rg == 2 ? tree_launch<HD, DT, 2>(mk, mv, a, sms, st) : tree_launch<HD, DT, 4>(mk, mv, a, sms, st);
+    return rg == 0 ? tree_launch<HD, DT, 0>(mk, mv, a, sms, st) : rg == 1 ? tree_launch<HD, DT, 1>(mk, mv, a, sms, st) : rg == 2 ? tree_launch<HD, DT, 2>(mk, mv, a, sms, st) : tree_launch<HD, DT, 4>(mk, mv, a, sms, st);
 }
 
-// 16 rows of a tile per row group; the groups needed for all rows of a sequence in one tile, up to four (0: one of 8 rows)
-static int row_groups(int max_rows, bool f32) { return max_rows <= 8 && !f32 ? 0 : max_rows <= 16 ? 1 : max_rows <= 32 ? 2 : 4; }
+// 16 rows of a tile per row group; the groups needed for all rows of a sequence in one tile, up to four (0: one of few rows)
+static int row_groups(int max_rows, bool f32) { return max_rows <= (f32 ? 4 : 8) ? 0 : max_rows <= 16 ? 1 : max_rows <= 32 ? 2 : 4; }
 
 struct TreeSpace { size_t acc, ml, desc, bytes; };
 static TreeSpace tree_space(int ctas, int rt, int hd) {
@@ -990,7 +989,7 @@ static TreeKind tree_kind(const dynakv_row_cache* c, int n_heads, int max_tree, 
     const int most = max_tree * (n_heads / c->n_kv_heads);
     if (c->kv_dtype == DYNAKV_BF16 && most >= DKV_TREE_TC_MIN) return {true, 0, most <= 128 ? 128 : 256, sms};
     const int rg = row_groups(most, c->kv_dtype == DYNAKV_F32);
-    return {false, rg, rg == 0 ? 8 : 16 * rg, sms * (c->kv_dtype == DYNAKV_F32 ? 1 : 2)};
+    return {false, rg, rg > 0 ? 16 * rg : c->kv_dtype == DYNAKV_F32 ? 4 : 8, sms * (c->kv_dtype == DYNAKV_F32 ? 1 : 2)};
 }
 
 static bool tree_shape_ok(const dynakv_row_cache* c, int n_heads, int max_tree) {
