@@ -144,6 +144,14 @@ __device__ __forceinline__ void store_cache(const dynakv_row_cache& c, bool is_v
     }
 }
 
+// Element e of a row of the pool, as a number.
+template <int DT>
+__device__ __forceinline__ float cache_elem(const unsigned char* pool, const signed char* exps, long long row, int hd, int e) {
+    if constexpr (DT == DYNAKV_F32) return reinterpret_cast<const float*>(pool)[row * hd + e];
+    else if constexpr (DT == DYNAKV_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(pool)[row * hd + e]);
+    else return fp8_unpack2((unsigned short)pool[row * hd + e], pow2f(exps[row])).x;
+}
+
 // Host side: what every call on a cache checks.
 static inline bool row_cache_ok(const dynakv_row_cache* c) {
     if (!c || !c->k || !c->v || c->n_pages < 1 || c->n_kv_heads < 1 || (c->head_dim != 64 && c->head_dim != 128)) return false;

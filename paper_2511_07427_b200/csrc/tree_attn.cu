@@ -98,14 +98,6 @@ struct PageIn {
     bool mask;                     // rows of the page may be invisible
 };
 
-// Element e of a row of the pool, as a number.
-template <int DT>
-__device__ __forceinline__ float cache_elem(const unsigned char* pool, const signed char* exps, long long row, int hd, int e) {
-    if constexpr (DT == DYNAKV_F32) return reinterpret_cast<const float*>(pool)[row * hd + e];
-    else if constexpr (DT == DYNAKV_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(pool)[row * hd + e]);
-    else return fp8_unpack2((unsigned short)pool[row * hd + e], pow2f(exps[row])).x;
-}
-
 // Byte offset of 16-byte chunk c of row r inside a page of the ring, as the TMA swizzle placed it.
 template <typename C>
 __device__ __forceinline__ unsigned chunk_at(int r, int c) {
@@ -758,7 +750,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         constexpr bool F32 = DT == DYNAKV_F32;
         typename std::conditional<F32, F32Rows<HD, RG>, MmaRows<HD, F32 ? DYNAKV_BF16 : DT, RG>>::type rows;
         auto all_sync = [&]() { asm volatile("bar.sync 5, %0;\n" ::"n"(C::consumers * 32) : "memory"); };
-        auto group_sync = [&]() { asm volatile("bar.sync %0, %1;\n" ::"r"(1 + kg), "n"(C::groups * 32) : "memory"); };
+        auto group_sync = [&]() { asm volatile("bar.sync %0, %1;\n" ::"r"(6 + kg), "n"(C::groups * 32) : "memory"); };
         if constexpr (F32) { rows.q_s = smem_u32(q_s + rg * C::rows * HD); rows.p_s = smem_u32(p_s + warp * C::rows * 32); }
         // This group's items are every KG-th of the CTA: `ahead` items pass before its next one, which lies in stage `st` in phase `ph`.
         int ahead = kg, st = kg, seg = 0;
@@ -980,14 +972,20 @@ static TreeSpace tree_space(int ctas, int rt, int hd) {
     return s;
 }
 
-// Which kernel, and how many CTAs with how many rows per tile.
-#ifndef DKV_TREE_TC_MIN
-#define DKV_TREE_TC_MIN 33
+// Which kernel, and how many CTAs with how many rows per tile.  The tcgen05 kernel pays from so many query rows per KV head on
+// (4 sequences of 32768 rows, 8 KV heads; mma.sync against tcgen05 in us).  bf16: 16 rows 93 / 99, 32 rows 100 / 101, 48 rows
+// 176 / 101.  FP8, whose rows the tcgen05 kernel has to convert in shared memory: 64 rows 188 / 244, 80 rows 270 / 247, 128 rows
+// 352 / 263.
+#ifndef DKV_TREE_TC_BF16
+#define DKV_TREE_TC_BF16 33
+#endif
+#ifndef DKV_TREE_TC_FP8
+#define DKV_TREE_TC_FP8 65
 #endif
 struct TreeKind { bool tc; int rg, rows, ctas; };
 static TreeKind tree_kind(const dynakv_row_cache* c, int n_heads, int max_tree, int sms) {
     const int most = max_tree * (n_heads / c->n_kv_heads);
-    if (c->kv_dtype == DYNAKV_BF16 && most >= DKV_TREE_TC_MIN) return {true, 0, most <= 128 ? 128 : 256, sms};
+    if (c->kv_dtype != DYNAKV_F32 && most >= (c->kv_dtype == DYNAKV_FP8 ? DKV_TREE_TC_FP8 : DKV_TREE_TC_BF16)) return {true, 0, most <= 128 ? 128 : 256, sms};
     const int rg = row_groups(most, c->kv_dtype == DYNAKV_F32);
     return {false, rg, rg > 0 ? 16 * rg : c->kv_dtype == DYNAKV_F32 ? 4 : 8, sms * (c->kv_dtype == DYNAKV_F32 ? 1 : 2)};
 }

@@ -70,7 +70,7 @@ static bool allow_smem(K kernel, int bytes, std::atomic<unsigned long long>& don
     return true;
 }
 
-// tcgen05 kernel (tree_tc.cu): bf16 rows, tiles of 128 or 256 query rows, one CTA per SM.
+// tcgen05 kernel (tree_tc.cu): bf16 and FP8 rows, tiles of 128 or 256 query rows, one CTA per SM.
 int tree_tc_launch(const dynakv_row_cache* cache, int rows, const TreeArgs& a, int sms, cudaStream_t st);
 // Merge of cut units (tree_attn.cu).
 int tree_merge_launch(int hd, int rt, bool f32, const TreeArgs& a, int ctas, cudaStream_t st);

@@ -1,4 +1,4 @@
-// Tree attention on the tcgen05 tensor cores: bf16 rows, tiles of 128 or 256 query rows (token, head of the group).
+// Tree attention on the tcgen05 tensor cores: bf16 and FP8 rows, tiles of 128 or 256 query rows (token, head of the group).
 //
 // With R query rows per KV head a bf16 row of K and V (512 bytes at d = 128) meets 4 d R flops: from a few dozen rows on the
 // mma.sync kernel is bound by the legacy tensor pipe (one m16n8k16 per 8.2 cycles and scheduler), while tcgen05 keeps
@@ -15,6 +15,7 @@
 //   warp 1 / warp 2     tcgen05.mma of stream 0 / 1: S = Q K^T (M = 128, N = 64 keys), then O += P V with P from tensor
 //                       memory and V read with its rows as the contraction index, no transposed copy anywhere
 //   warps 4-7 / 8-11    softmax of stream 0 / 1: a query row per thread
+//   warps 12-15         FP8 rows only: they fetch the rows and turn them into bf16 stages (warps 0 and 3 then rest)
 // Tensor memory (512 columns): S of stream s at 128 s and 128 s + 64, O at 256 + 128 s.  The weights replace the logits in
 // place: 32 logits of a row become 16 columns of bf16 hi pairs and 16 of lo pairs (the two MMAs of the split keep fp32 weights to
 // 2^-17; bf16 weights alone would add an error as large as the output's own rounding).  The softmax's reference moves
@@ -34,11 +35,12 @@
 namespace dkv {
 
 constexpr int TT_PAGES = 4, TT_HALF = 2;                       // pages of a stage and of the half a stream works on
-constexpr int TT_THREADS = 384;
+constexpr int TT_CONVERT = 128;                                // FP8: threads that load rows and convert them
 constexpr float TT_LOG2E = 1.4426950408889634f, TT_LN2 = 0.6931471805599453f, TT_LAZY = 8.f;
 
-template <int HD, bool PAIR>
+template <int HD, bool PAIR, bool F8>
 struct TcTree {
+    static constexpr int threads = 384 + (F8 ? TT_CONVERT : 0);
     static constexpr int rows = PAIR ? 256 : 128;              // query rows of a tile
     static constexpr int panels = HD / 64;                     // 128-byte column panels of a row
     static constexpr int panel_bytes = 128 * 128;              // 128 rows of 128 bytes
@@ -79,10 +81,10 @@ __device__ __forceinline__ void tt_proxy_fence() { asm volatile("fence.proxy.asy
 // Pages of half h of stage j of a segment of `pages` pages.
 __device__ __forceinline__ int half_pages(int pages, int j, int h) { return max(0, min(TT_HALF, pages - j * TT_PAGES - h * TT_HALF)); }
 
-template <int HD, bool PAIR>
-__global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+template <int HD, bool PAIR, bool F8>
+__global__ void __launch_bounds__((TcTree<HD, PAIR, F8>::threads), 1) k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                            const __grid_constant__ TreeArgs a) {
-    using C = TcTree<HD, PAIR>;
+    using C = TcTree<HD, PAIR, F8>;
     constexpr int NS = C::stages;
     extern __shared__ __align__(1024) unsigned char tt_smem[];
     unsigned char* at = tt_smem + (C::q_tiles + 2 * NS) * C::tile_bytes;
@@ -103,7 +105,8 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
     if (tid == 0) {
         for (int i = 0; i < C::count; i++) {
             const bool empty = (i >= C::KEMPTY && i < C::VFULL) || (i >= C::VEMPTY && i < C::SFULL);
-            tc_mbar_init(bar(i), empty ? 2 : i >= C::PFULL && i < C::ODONE ? 4 : i >= C::QFULL && i < C::DRAIN ? 8 : 1);
+            const bool full = (i >= C::KFULL && i < C::KEMPTY) || (i >= C::VFULL && i < C::VEMPTY);
+            tc_mbar_init(bar(i), empty ? 2 : full && F8 ? TT_CONVERT / 32 : i >= C::PFULL && i < C::ODONE ? 4 : i >= C::QFULL && i < C::DRAIN ? 8 : 1);
         }
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -124,7 +127,9 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
     Segment g;
     auto give_up = [&]() { *s_abort = 1; };
 
-    if (warp == 0 || warp == 3) {
+    if (F8 && (warp == 0 || warp == 3)) {
+        // nothing to load by TMA: the converting warps fetch the rows themselves
+    } else if (warp == 0 || warp == 3) {
         // =============================== loads: warp 0 K, warp 3 V ===============================
         const bool is_v = warp == 3;
         const CUtensorMap* map = is_v ? &map_v : &map_k;
@@ -249,6 +254,89 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
             __syncwarp();
             mbar_wait(bar(C::DRAIN + s), 0u);
         }
+    } else if (F8 && warp >= 12) {
+        // =============================== FP8 rows to bf16 stages ===============================
+        // A thread takes the same 16 bytes of every RPP-th row of a stage.  K and V alternate: while one is converted (exactly: e4m3
+        // times a power of two is a bf16 value) and stored where the TMA would have put it, the other's loads are under way.
+        constexpr int CPR = HD / 16, RPP = TT_CONVERT / CPR, NP = TT_PAGES * PAGE / RPP;
+        const int ct = tid - 384, chunk = ct % CPR, row0 = ct / CPR;
+        int n = 0, pc = 0, id = -1;
+        bool ok = true, more = false;
+        int page[TT_PAGES], bits = 0, h = 0;                   // the stage to load next
+        auto advance = [&](bool first) {                       // all lanes together
+            if (!first) pc += TT_PAGES;
+            if (first || pc >= g.p1) { more = next_segment(walk, a, g); pc = more ? g.p0 : 0; }
+            if (!more) return;
+            if (((pc - g.p0) & 31) == 0) {
+                id = -1;
+                if (pc + lane < g.p1 && g.n > 0) {
+                    id = a.page_table[(size_t)g.b * a.pages_per_seq + pc + lane];
+                    if (id < 0 || id >= a.n_pages) { id = -1; tree_status(a, DYNAKV_ST_BOUNDS); }
+                }
+            }
+            const int j = (pc - g.p0) & 31;
+            const unsigned there = __ballot_sync(0xffffffffu, id >= 0);
+            bits = (there >> j) & 15;
+#pragma unroll
+            for (int x = 0; x < TT_PAGES; x++) page[x] = __shfl_sync(0xffffffffu, id, j + x);
+            h = g.h;
+        };
+        uint4 raw[2][NP];                                      // K, V
+        int ex[2][NP];
+        auto fetch = [&](int kv) {
+            const unsigned char* pool = kv ? a.vpool : a.kpool;
+            const signed char* exps = kv ? a.vexp : a.kexp;
+#pragma unroll
+            for (int i = 0; i < NP; i++) {
+                const int pg = page[i * RPP / PAGE];
+                const size_t r = ((size_t)(pg < 0 ? 0 : pg) * a.Hk + h) * PAGE + (i * RPP + row0) % PAGE;
+                raw[kv][i] = pg >= 0 ? __ldg(reinterpret_cast<const uint4*>(pool + r * HD) + chunk) : make_uint4(0u, 0u, 0u, 0u);
+                ex[kv][i] = pg >= 0 ? (int)__ldg(reinterpret_cast<const signed char*>(exps) + r) : 0;
+            }
+        };
+        auto convert = [&](int kv, unsigned dst) {
+#pragma unroll
+            for (int i = 0; i < NP; i++) {
+                const int row = i * RPP + row0;
+                const float sc = pow2f(ex[kv][i]);
+                const float2 sc2 = make_float2(sc, sc);
+                const unsigned w[4] = {raw[kv][i].x, raw[kv][i].y, raw[kv][i].z, raw[kv][i].w};
+                unsigned o[8];
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    unsigned lo, hi;
+                    e4m3x4_to_f16x2(w[x], lo, hi);
+                    const float2 p = mul2(__half22float2(*reinterpret_cast<const __half2*>(&lo)), sc2), q = mul2(__half22float2(*reinterpret_cast<const __half2*>(&hi)), sc2);
+                    o[2 * x] = pack_bf16(p.x, p.y);
+                    o[2 * x + 1] = pack_bf16(q.x, q.y);
+                }
+                const unsigned to = dst + (chunk >> 2) * C::panel_bytes + row * 128, ch = (2 * chunk) & 7;
+                sts16(to + ((ch ^ (row & 7)) << 4), make_uint4(o[0], o[1], o[2], o[3]));
+                sts16(to + (((ch + 1) ^ (row & 7)) << 4), make_uint4(o[4], o[5], o[6], o[7]));
+            }
+            tt_proxy_fence();
+            __syncwarp();
+        };
+        auto wait = [&](int b, int phase) { ok = ok && mbar_wait(bar(b), (unsigned)phase & 1u); ok = __all_sync(0xffffffffu, ok); };
+        advance(true);
+        if (more) fetch(0);
+        while (more && ok) {
+            const int st = n % NS, use = n / NS, bits_now = bits;
+            fetch(1);
+            if (use > 0) wait(C::KEMPTY + st, use - 1);
+            if (!ok) break;
+            if (ct == 0) meta[n & 7] = bits_now;
+            convert(0, sK(st));
+            if (lane == 0) tc_mbar_arrive(bar(C::KFULL + st));
+            advance(false);
+            if (more) fetch(0);
+            if (use > 0) wait(C::VEMPTY + st, use - 1);
+            if (!ok) break;
+            convert(1, sV(st));
+            if (lane == 0) tc_mbar_arrive(bar(C::VFULL + st));
+            n++;
+        }
+        if (!ok && lane == 0) give_up();
     } else {
         // =============================== softmax of one stream ===============================
         const int s = (warp - 4) >> 2, row = (warp & 3) * 32 + lane, wt = tid - 128;       // wt: thread of the 256
@@ -382,18 +470,21 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
 #pragma unroll
                     for (int c = 0; c < TT_HALF; c++)
                         if (c < cnt) {
-                            unsigned w[32];
 #pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
-                                float2 y = fma2(make_float2(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])), qs2, ref2);
-                                y = make_float2(ex2(y.x), ex2(y.y));
-                                sum = fma2(y, one, sum);
-                                const unsigned hi = pack_bf16(y.x, y.y);
-                                const float2 lo = fma2(make_float2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), neg, y);
-                                w[e / 2] = hi;
-                                w[16 + e / 2] = pack_bf16(lo.x, lo.y);
+                            for (int part = 0; part < 2; part++) {             // 16 keys at a time: fewer registers
+                                unsigned hi[8], lo[8];
+#pragma unroll
+                                for (int e = 0; e < 8; e++) {
+                                    float2 y = fma2(make_float2(__uint_as_float(x[c][part * 16 + 2 * e]), __uint_as_float(x[c][part * 16 + 2 * e + 1])), qs2, ref2);
+                                    y = make_float2(ex2(y.x), ex2(y.y));
+                                    sum = fma2(y, one, sum);
+                                    hi[e] = pack_bf16(y.x, y.y);
+                                    const float2 z = fma2(make_float2(__uint_as_float(hi[e] << 16), __uint_as_float(hi[e] & 0xffff0000u)), neg, y);
+                                    lo[e] = pack_bf16(z.x, z.y);
+                                }
+                                tc_st8(tS + c * 32 + part * 8, hi);
+                                tc_st8(tS + c * 32 + 16 + part * 8, lo);
                             }
-                            tc_st32(tS + c * 32, w);
                         }
                     l += sum.x + sum.y;
                     tc_st_wait();
@@ -445,15 +536,14 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
                                 bits &= bits - 1;
                                 if (!tree_sees(a, g, t, jj)) continue;
                                 const int page = a.page_table[(size_t)g.b * a.pages_per_seq + pos / PAGE];
-                                const size_t key = ((size_t)page * a.Hk + g.h) * PAGE + pos % PAGE;
-                                const __nv_bfloat16* kr = reinterpret_cast<const __nv_bfloat16*>(a.kpool) + key * HD;
-                                const __nv_bfloat16* vr = reinterpret_cast<const __nv_bfloat16*>(a.vpool) + key * HD + col;
+                                const long long key = ((long long)page * a.Hk + g.h) * PAGE + pos % PAGE;
+                                constexpr int DT = F8 ? DYNAKV_FP8 : DYNAKV_BF16;
                                 const __nv_bfloat16* qr = reinterpret_cast<const __nv_bfloat16*>(a.q) + q_row * HD;
                                 float d = 0.f;
-                                for (int e = 0; e < HD; e++) d = fmaf(__bfloat162float(qr[e]), __bfloat162float(kr[e]), d);
+                                for (int e = 0; e < HD; e++) d = fmaf(__bfloat162float(qr[e]), cache_elem<DT>(a.kpool, a.kexp, key, HD, e), d);
                                 const float p = ex2(d * (a.scale * TT_LOG2E) - ref);
 #pragma unroll
-                                for (int e = 0; e < 32; e++) o[e] = fmaf(p, __bfloat162float(vr[e]), o[e]);
+                                for (int e = 0; e < 32; e++) o[e] = fmaf(p, cache_elem<DT>(a.vpool, a.vexp, key, HD, col + e), o[e]);
                             }
                         }
                     }
@@ -494,20 +584,24 @@ __global__ void __launch_bounds__(TT_THREADS, 1) k_tree_tc(const __grid_constant
     if (tid == 0 && *s_abort) tree_status(a, DYNAKV_ST_INTERNAL);
 }
 
-template <int HD, bool PAIR>
+template <int HD, bool PAIR, bool F8>
 static int tree_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, int sms, cudaStream_t st) {
-    using C = TcTree<HD, PAIR>;
+    using C = TcTree<HD, PAIR, F8>;
     CUtensorMap mk, mv;
     if (!tree_page_map(&mk, cache, cache->k, false) || !tree_page_map(&mv, cache, cache->v, false)) return DYNAKV_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
-    if (!allow_smem(k_tree_tc<HD, PAIR>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
-    if (launch_pdl(k_tree_tc<HD, PAIR>, dim3(sms), dim3(TT_THREADS), C::smem, st, mk, mv, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
+    if (!allow_smem(k_tree_tc<HD, PAIR, F8>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
+    if (launch_pdl(k_tree_tc<HD, PAIR, F8>, dim3(sms), dim3(C::threads), C::smem, st, mk, mv, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
     return tree_merge_launch(HD, C::rows, false, a, sms, st);
+}
+template <int HD>
+static int tree_tc_launch_hd(const dynakv_row_cache* cache, int rows, const TreeArgs& a, int sms, cudaStream_t st) {
+    if (cache->kv_dtype == DYNAKV_FP8) return rows == 128 ? tree_tc_launch_as<HD, false, true>(cache, a, sms, st) : tree_tc_launch_as<HD, true, true>(cache, a, sms, st);
+    return rows == 128 ? tree_tc_launch_as<HD, false, false>(cache, a, sms, st) : tree_tc_launch_as<HD, true, false>(cache, a, sms, st);
 }
 
 int tree_tc_launch(const dynakv_row_cache* cache, int rows, const TreeArgs& a, int sms, cudaStream_t st) {
-    if (cache->head_dim == 128) return rows == 128 ? tree_tc_launch_as<128, false>(cache, a, sms, st) : tree_tc_launch_as<128, true>(cache, a, sms, st);
-    return rows == 128 ? tree_tc_launch_as<64, false>(cache, a, sms, st) : tree_tc_launch_as<64, true>(cache, a, sms, st);
+    return cache->head_dim == 128 ? tree_tc_launch_hd<128>(cache, rows, a, sms, st) : tree_tc_launch_hd<64>(cache, rows, a, sms, st);
 }
 
 }  // namespace dkv
