@@ -739,10 +739,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             // a stage was not given back in time: report it and let the copies under way land before the block ends
             *s_abort = 1;
             tree_status(a, DYNAKV_ST_INTERNAL);
-            for (int s = 0; s < S; s++) {
-                const int last = it - 1 - ((it - 1 - s) % S + S) % S;          // last item that went to stage s
-                if (last >= 0) mbar_wait(full(s), (last / S) & 1);
-            }
+            for (int x = max(0, it - 1 - S); x < it - 1; x++) mbar_wait(full(x % S), (x / S) & 1);       // item it - 1 was not issued
         }
     } else {
         // =============================== consumers ===============================

@@ -6,6 +6,9 @@ relative error of a weight, doubled because the sum of weights has it too.  Weig
 f16 (2^-11 of the weight, 2^-25 of the largest weight times scale when subnormal) or fp32; a sum over n rows adds n u; the
 output's own rounding half a step."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -280,6 +283,72 @@ def test_same_bits_every_time_and_under_a_graph():
     torch.cuda.synchronize()
     for g, r in graphs:
         assert torch.equal(r[0], want[0]) and torch.equal(r[1], want[1])
+
+
+@pytest.mark.parametrize("cache,lens,drafts,heads,hk,d", [("bf16", [2, 40], [5, 60], 2, 1, 128), ("fp8", [50, 3], [200, 3], 4, 4, 64), ("fp8", [70], [100], 4, 2, 128),
+                                                          ("f32", [7], [9], 6, 3, 64), ("bf16", [33, 90], [256, 7], 3, 1, 64)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_more_drafts_than_rows(cache, lens, drafts, heads, hk, d, tree):
+    """The rows are the tree's last ones: those that would lie before the cache's first row do not exist."""
+    p = Problem(lens, drafts, heads, hk, d, cache, tree=tree, seed=9)
+    p.check(*p.run())
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+def test_two_streams_at_once(cache):
+    a, b = (Problem([4000, 900], [3, 20], 8, 2, 128, cache, seed=s) for s in (1, 2))
+    want = [x.run() for x in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(5):
+        for st, x in zip(streams, (a, b)):
+            with torch.cuda.stream(st):
+                got.append(x.run())
+    torch.cuda.synchronize()
+    for i, (o, l) in enumerate(got):
+        assert torch.equal(o, want[i % 2][0]) and torch.equal(l, want[i % 2][1])
+
+
+@pytest.mark.parametrize("cache,heads", [(P.BF16, 2), (P.FP8, 2), (P.BF16, 8)])
+def test_a_cache_of_more_than_2_to_the_31_elements(cache, heads):
+    hk, d, pages = 1, 128, (1 << 31) // (32 * 128) + 40
+    c = P.RowCache.allocate(pages, hk, d, cache)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    n, t = 70, 8
+    table = torch.tensor([[pages - 1, 3, pages - 30]], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(n, hk, d, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    i = torch.arange(n, device="cuda")
+    c.write(k, v, (table[0].long()[i // 32] * 32 + i % 32).to(torch.int32))
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    K, V = c.read(table, lens, n)
+    if cache == P.BF16:
+        assert torch.equal(K[0, 0], k[:, 0]) and torch.equal(V[0, 0], v[:, 0])
+    else:
+        assert (K[0, 0].float() - k[:, 0].float()).abs().max().item() <= 2.0 ** -4 * k.float().abs().max().item()
+    q = torch.randn(t, heads, d, generator=g, device="cuda").to(torch.bfloat16)
+    out, _ = c.attend_tree(q, table, lens, torch.tensor([0, t], dtype=torch.int32, device="cuda"), t)
+    small = P.RowCache.allocate(3, hk, d, cache)
+    near = torch.arange(3, dtype=torch.int32, device="cuda")[None]
+    small.write(k, v, i.to(torch.int32))
+    want, _ = small.attend_tree(q, near, lens, torch.tensor([0, t], dtype=torch.int32, device="cuda"), t)
+    assert torch.equal(out, want) and c.get_status() == 0
+
+
+def test_first_call_of_a_process_under_capture():
+    code = ("import torch, sys; sys.path.insert(0, %r); import paper_2511_07427_b200 as P\n"
+            "i = dict(dtype=torch.int32, device='cuda')\n"
+            "for cache, heads in ((P.BF16, 4), (P.FP8, 8), (P.BF16, 8)):\n"
+            "    c = P.RowCache.allocate(3, 1, 128, cache)\n"
+            "    x = torch.ones(80, 1, 128, dtype=torch.bfloat16, device='cuda'); s = torch.arange(80, **i)\n"
+            "    q = torch.ones(16, heads, 128, dtype=torch.bfloat16, device='cuda'); t = torch.arange(3, **i)[None]; n = torch.tensor([80], **i); b = torch.tensor([0, 16], **i)\n"
+            "    g = torch.cuda.CUDAGraph()\n"
+            "    with torch.cuda.graph(g):\n"
+            "        c.write(x, x, s); o, l = c.attend_tree(q, t, n, b, 16); k, v = c.read(t, n, 80)\n"
+            "    g.replay(); torch.cuda.synchronize()\n"
+            "    assert bool((o == 1).all()) and bool((k == 1).all()) and c.get_status() == 0\n") % os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
 
 
 def test_bad_pages_lengths_and_token_ranges_are_skipped_and_reported():

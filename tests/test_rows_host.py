@@ -95,3 +95,26 @@ def test_binding_refuses_cpu_tensors():
         P.HeadRotary(4, 2, 128, torch.ones(64), eps=-1.0)
     with pytest.raises(P.DynaKVError, match="heads|head"):
         P.HeadRotary(0, 2, 128, torch.ones(64))
+
+
+def _attend(cache=None, q=ADDR, n_heads=4, n_tokens=3, q_start=ADDR, n_seqs=1, max_tree=3, table=ADDR, per=2, kv_len=ADDR, mask=None, words=0, scale=0.1,
+            out=ADDR, lse=None, space=ADDR, size=1 << 40):
+    return R._library().dynakv_attend_tree(C.byref(cache or _cache()), q, n_heads, n_tokens, q_start, n_seqs, max_tree, table, per, kv_len, mask, words, scale,
+                                           out, lse, space, size, None, None)
+
+
+@pytest.mark.parametrize("bad", [dict(n_heads=0), dict(n_heads=3), dict(n_heads=18), dict(max_tree=0), dict(max_tree=257), dict(n_tokens=-1), dict(n_tokens=1 << 31),
+                                 dict(n_seqs=-1), dict(per=-1), dict(per=1 << 26), dict(scale=float("nan")), dict(scale=float("inf")), dict(mask=ADDR, words=0),
+                                 dict(mask=ADDR, words=5), dict(q=None), dict(q_start=None), dict(table=None), dict(kv_len=None), dict(out=None), dict(space=None),
+                                 dict(q=ADDR + 8), dict(out=ADDR + 2), dict(space=ADDR + 4), dict(cache=_cache(head_dim=32)), dict(cache=_cache(kv_dtype=P.FP8))])
+def test_attend_tree_refuses_bad_arguments(bad):
+    assert _attend(**bad) == -1
+
+
+def test_attend_tree_without_tokens_or_sequences_needs_nothing():
+    assert _attend(n_tokens=0, q=None, out=None, space=None) == 0
+    assert _attend(n_seqs=0, q=None, out=None, space=None) == 0
+    for bad in (dict(n_heads=5), dict(max_tree=0), dict(max_tree=1000)):
+        a = dict(n_heads=4, max_tree=3)
+        a.update(bad)
+        assert R._library().dynakv_attend_tree_workspace(C.byref(_cache()), a["n_heads"], a["max_tree"]) == -1
