@@ -46,7 +46,8 @@ struct TcTree {
     static constexpr int panel_bytes = 128 * 128;              // 128 rows of 128 bytes
     static constexpr int tile_bytes = panels * panel_bytes;
     static constexpr int q_tiles = PAIR ? 2 : 1;
-    static constexpr int stages = 2;                           // of K and V each: with Q 160 or 192 KB at d = 128 (three: 4 to 8 % slower)
+    static constexpr int stages = 2;                           // of K and V each: with Q 160 or 192 KB at d = 128 (three: 3 to 8 % slower,
+                                                               // three of only one of them: no difference)
     static constexpr int fixed = 2 * 128 * 8 + 48 * 8 + 32 * 8 + 2 * 8 * 4 + 8 * 4 + 16;
     static constexpr int smem = (q_tiles + 2 * stages) * tile_bytes + fixed;
     static_assert(smem + 1024 <= 233472, "shared memory of an SM");
