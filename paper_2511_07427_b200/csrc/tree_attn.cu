@@ -7,8 +7,8 @@
 // 4 d R flops, and HBM bounds the call until R is in the tens.  tree_plan.cuh says how the pages are shared out.
 //
 // Kernel shape.  One producer warp streams whole 32-row pages, K and V, into a shared-memory ring with tiled TMA loads
-// (128-byte swizzle, so that the fragment loads below meet no bank conflicts; FP8 rows' exponents follow as two 32-byte
-// bulk copies).  The consumer warps are RG row groups x KG page groups: a row group holds 16 query rows, a page group takes
+// (128-byte swizzle, so that the fragment loads below meet no bank conflicts; FP8 rows' exponents come by cp.async, because the two
+// bulk copies of 32 bytes cost as much issue time as the pages: 4 x 32768 rows of 64, 8 KV heads, 52 -> 46 us without them).  The consumer warps are RG row groups x KG page groups: a row group holds 16 query rows, a page group takes
 // every KG-th page of the CTA's range with a softmax state of its own, merged through shared memory at a segment's end.
 // Few rows: three page groups hide the latency of a page's chain of dependent steps; 64 rows: four row groups share a
 // page, which divides its shared-memory traffic.  A ring stage is always consumed by the same page group (a parity
@@ -43,6 +43,13 @@ constexpr float LAZY = 8.f;                // the softmax's reference moves when
 __device__ __forceinline__ void tma_page(unsigned dst, const CUtensorMap* map, int row, unsigned bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n"
                  ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(0), "r"(bar) : "memory");
+}
+// Two 16-byte copies global -> shared that arrive at `bar` (one arrival) together with all earlier ones of the thread.
+__device__ __forceinline__ void copy32(unsigned dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n cp.async.cg.shared.global [%0 + 16], [%1 + 16], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_arrive(unsigned bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ float lds_f32(unsigned addr) {
     float v;
@@ -83,7 +90,7 @@ struct TreeCfg {
     static constexpr int exp_bytes = DT == DYNAKV_FP8 ? stages * 64 + consumers * 32 * 16 : 0;   // and a table of scales per warp
     static constexpr int q_bytes = DT == DYNAKV_F32 ? RT * HD * 4 : 0;
     static constexpr int p_bytes = DT == DYNAKV_F32 ? consumers * rows * 32 * 4 : 0;
-    static constexpr int fixed_bytes = 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + 48 * 8;
+    static constexpr int fixed_bytes = 32 * 4 + 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + 48 * 8;
     static constexpr int smem = stages * stage_bytes + exp_bytes + q_bytes + p_bytes + merge_bytes + fixed_bytes;
     static_assert(stages % KG == 0, "each ring stage belongs to one page group");
     static_assert(per_sm * (smem + 1024) <= 233472, "shared memory of an SM");
@@ -464,6 +471,261 @@ struct MmaRows {
     }
 };
 
+// ---------------------------------------------------------------------------------- FP8 rows of 128, few queries
+//
+// With at most 8 query rows of 128 elements (RG = 0) the products are turned round: the rows of K and of V are the 16-row operand
+// and the queries the 8-column one, S^T = K Q^T and O^T = V^T P^T, so that no MMA works on empty rows; MmaRows fills those rows
+// with the lo parts of the weights, which bf16 weights need and f16 weights do not, and bytes turned into f16 come at a price.
+// Lane (n = lane / 4, c = lane % 4) has query rows 2 c and 2 c + 1, of the logits the keys 8 y + key_of(n), of the sums the
+// columns elem() names.  The weights become the second product's operand by four 8 x 8 transpositions.  Measured on 16 sequences
+// of up to 20480 rows: 55 us, MmaRows 60; rows of 64: 47 us, MmaRows 45, and 0.5 to 1 us more for short bf16 caches, so that
+// MmaRows has those.
+struct TurnedRows {
+    static constexpr int HD = 128, KS = HD / 16, MT = HD / 16;
+    using C = TreeCfg<HD, DYNAKV_FP8, 0>;
+    unsigned qb[KS][2];
+    float qs[2];                                        // logit factor (log2 units) of the two rows
+    float acc[MT][4], m[2], l[2];                       // acc[mt][x]: query row 2 c + (x & 1)
+    int t[2];                                           // token of the two rows, -1: no such row
+
+    // key order inside 8 keys that keeps the loads free of bank conflicts
+    static __device__ __forceinline__ int key_of(int n) { return (n & 1) * 4 + (n >> 1); }
+    // element of the output that acc[mt][2 * half], acc[mt][2 * half + 1] hold: the 16 bytes of a lane are neighbours
+    static __device__ __forceinline__ int elem(int mt, int half, int n) { return 16 * key_of(n) + 2 * mt + half; }
+    static __device__ __forceinline__ float max_over_keys(float v) {               // over the 8 lanes that share c
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+        return v;
+    }
+    static __device__ __forceinline__ float sum_over_keys(float v) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+    static __device__ __forceinline__ unsigned transposed(unsigned v) {            // of an 8 x 8 matrix of 16-bit values
+        unsigned r;
+        asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(v));
+        return r;
+    }
+    static __device__ __forceinline__ const __nv_bfloat16* q_row(const TreeArgs& a, const Segment& g, int r, int token) {
+        return reinterpret_cast<const __nv_bfloat16*>(a.q) + ((size_t)(g.q0 + token) * a.Hq + g.h * a.G + r - token * a.G) * HD;
+    }
+
+    __device__ __forceinline__ void start(const TreeArgs& a, const Segment& g, int, int lane) {
+        const int c = lane & 3, r0 = g.tile * C::RT, rows = g.T * a.G;
+        // the lane loads for row n: four neighbouring elements per step, divided by a power of two per row, as in MmaRows
+        const int rq = r0 + (lane >> 2);
+        const unsigned* q = reinterpret_cast<const unsigned*>(rq < rows ? q_row(a, g, rq, rq / a.G) : nullptr);
+        float mx = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) {
+            const int e = ((ks >> 2) * 4 + c) * 16 + (ks & 3) * 4;
+            const uint2 w = q ? *reinterpret_cast<const uint2*>(q + e / 2) : make_uint2(0u, 0u);
+            qb[ks][0] = w.x; qb[ks][1] = w.y;
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+                const unsigned u = qb[ks][x];
+                mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(u << 16)), fabsf(__uint_as_float(u & 0xffff0000u))));
+            }
+        }
+        mx = quad_max(mx);
+        const int e = mx > 0.f ? max(-100, min(112, (int)(__float_as_uint(mx) >> 23) - 127 - 14)) : 0;
+        const float down = pow2f(-e), mine = a.scale * LOG2E * pow2f(e);
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++)
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+                const unsigned u = qb[ks][x];
+                const __half2 h = __floats2half2_rn(__uint_as_float(u << 16) * down, __uint_as_float(u & 0xffff0000u) * down);
+                qb[ks][x] = *reinterpret_cast<const unsigned*>(&h);
+            }
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int r = r0 + 2 * c + i;
+            t[i] = r < rows ? r / a.G : -1;
+            qs[i] = __shfl_sync(0xffffffffu, mine, (2 * c + i) * 4);
+            m[i] = -INFINITY; l[i] = 0.f;
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) acc[mt][x] = 0.f;
+    }
+
+    __device__ __forceinline__ void page(const TreeArgs& a, const Segment& g, const PageIn& p, int lane) {
+        const int c = lane & 3, n = lane >> 2;
+        // the scales of the 32 rows, one row per lane, as in MmaRows
+        const float ve = (float)p.exps[32 + lane], vr = fmaxf(ve, VE_LOW);
+        p.scales[lane] = make_float4(pow2f(p.exps[lane]), vr, pow2f(-(int)vr), ex2(fminf(ve - VE_LOW, 0.f)));
+        const bool low = __any_sync(0xffffffffu, ve < VE_LOW);
+        __syncwarp();
+        float s[2][4];               // [16 keys][(key n, row 2 c), (n, 2 c + 1), (n + 8, 2 c), (n + 8, 2 c + 1)]
+#pragma unroll
+        for (int k16 = 0; k16 < 2; k16++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) s[k16][x] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+            unsigned w[4][4];
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                const uint4 u = lds16(p.k + chunk_at<C>(y * 8 + key_of(n), c + 4 * j));
+                w[y][0] = u.x; w[y][1] = u.y; w[y][2] = u.z; w[y][3] = u.w;
+            }
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+#pragma unroll
+                for (int k16 = 0; k16 < 2; k16++) {
+                    unsigned k[4];
+                    e4m3x4_to_f16x2(w[2 * k16][x], k[0], k[2]);
+                    e4m3x4_to_f16x2(w[2 * k16 + 1][x], k[1], k[3]);
+                    tree_mma<true>(s[k16], k, qb[j * 4 + x][0], qb[j * 4 + x][1]);
+                }
+        }
+        unsigned win[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) win[i] = !p.mask ? ~0u : t[i] >= 0 ? tree_window(a, g, t[i], p.key0) : 0u;
+        float4 sc[2][2];
+        float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int k16 = 0; k16 < 2; k16++)
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+                const int key = k16 * 16 + y * 8 + key_of(n);
+                sc[k16][y] = p.scales[key];
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    float& x = s[k16][2 * y + i];
+                    x *= qs[i] * sc[k16][y].x;
+                    if (p.mask && !((win[i] >> key) & 1u)) x = -INFINITY;
+                    x += sc[k16][y].y;
+                    mx[i] = fmaxf(mx[i], x);
+                }
+            }
+        bool move = false;
+#pragma unroll
+        for (int i = 0; i < 2; i++) { mx[i] = max_over_keys(mx[i]); move |= mx[i] > m[i] + LAZY; }
+        if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const float to = mx[i] > m[i] + LAZY ? mx[i] : m[i];
+                const float f = to == -INFINITY ? 1.f : ex2(m[i] - to);
+                m[i] = to; l[i] *= f;
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++) { acc[mt][i] *= f; acc[mt][2 + i] *= f; }
+            }
+        }
+        unsigned b[2][2];            // [16 keys][half]: the weights as the second product's operand
+#pragma unroll
+        for (int k16 = 0; k16 < 2; k16++)
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+                float w[2];
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    w[i] = ex2(s[k16][2 * y + i] - (m[i] == -INFINITY ? 0.f : m[i]));
+                    l[i] = fmaf(w[i], sc[k16][y].z, l[i]);
+                    if (low) w[i] *= sc[k16][y].w;
+                }
+                const __half2 h = __floats2half2_rn(w[0], w[1]);
+                b[k16][y] = transposed(*reinterpret_cast<const unsigned*>(&h));
+            }
+#pragma unroll
+        for (int k16 = 0; k16 < 2; k16++) {
+            unsigned w[4][4];
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                const uint4 v = lds16(p.v + chunk_at<C>(k16 * 16 + (y >> 1) * 8 + key_of(2 * c + (y & 1)), key_of(n)));
+                w[y][0] = v.x; w[y][1] = v.y; w[y][2] = v.z; w[y][3] = v.w;
+            }
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    const unsigned sel = half ? 0x7362u : 0x5140u;        // bytes (2, 6, 3, 7) or (0, 4, 1, 5) of two keys
+                    unsigned v[4];
+                    e4m3x4_to_f16x2(__byte_perm(w[0][x], w[1][x], sel), v[0], v[1]);
+                    e4m3x4_to_f16x2(__byte_perm(w[2][x], w[3][x], sel), v[2], v[3]);
+                    tree_mma<true>(acc[2 * x + half], v, b[k16][0], b[k16][1]);
+                }
+        }
+    }
+
+    __device__ __forceinline__ void finish() {
+#pragma unroll
+        for (int i = 0; i < 2; i++) l[i] = sum_over_keys(l[i]);
+    }
+    __device__ __forceinline__ void dump(float* to, int lane) const {
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) to[(mt * 4 + x) * 32 + lane] = acc[mt][x];
+        if (lane < 4) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) reinterpret_cast<float2*>(to + MT * 128)[2 * lane + i] = make_float2(m[i], l[i]);
+        }
+    }
+    __device__ __forceinline__ void merge(const float* from, int lane) {
+        float f0[2], f1[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const float2 o = reinterpret_cast<const float2*>(from + MT * 128)[2 * (lane & 3) + i];
+            const float to = fmaxf(m[i], o.x), ref = to == -INFINITY ? 0.f : to;
+            f0[i] = ex2(m[i] - ref); f1[i] = ex2(o.x - ref);
+            l[i] = l[i] * f0[i] + o.y * f1[i];
+            m[i] = to;
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) acc[mt][x] = acc[mt][x] * f0[x & 1] + from[(mt * 4 + x) * 32 + lane] * f1[x & 1];
+    }
+    // The share of a drafted row that was left out of the MMAs: key row `row` of the pool, token j of the tree.
+    __device__ __forceinline__ void add_row(const TreeArgs& a, const Segment& g, int, long long row, int j, int lane) {
+        const int c = lane & 3, n = lane >> 2;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            float d = 0.f;
+            if (t[i] >= 0) {
+                const __nv_bfloat16* q = q_row(a, g, g.tile * C::RT + 2 * c + i, t[i]);
+                for (int e = n; e < HD; e += 8) d = fmaf(__bfloat162float(q[e]), cache_elem<DYNAKV_FP8>(a.kpool, a.kexp, row, HD, e), d);
+            }
+            d = sum_over_keys(d);
+            if (t[i] >= 0 && tree_sees(a, g, t[i], j)) {
+                const float w = ex2(d * (a.scale * LOG2E) - (m[i] == -INFINITY ? 0.f : m[i]));
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                    for (int half = 0; half < 2; half++)
+                        acc[mt][2 * half + i] = fmaf(w, cache_elem<DYNAKV_FP8>(a.vpool, a.vexp, row, HD, elem(mt, half, n)), acc[mt][2 * half + i]);
+            }
+        }
+    }
+    __device__ __forceinline__ void write(const TreeArgs& a, const Segment& g, int, int lane, bool whole, size_t slot) const {
+        const int c = lane & 3, n = lane >> 2;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            if (t[i] < 0) continue;
+            const int rl = 2 * c + i, r = g.tile * C::RT + rl;
+            const size_t at = (size_t)(g.q0 + t[i]) * a.Hq + g.h * a.G + (r - t[i] * a.G);
+            const float f = !whole ? 1.f : l[i] == 0.f ? 0.f : 1.f / l[i];
+            __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(a.out) + at * HD;
+            float* part = a.acc + (slot * C::RT + rl) * HD;
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                const float x = acc[mt][i] * f, y = acc[mt][2 + i] * f;
+                const int e = elem(mt, 0, n);
+                if (whole) *reinterpret_cast<unsigned*>(o + e) = pack_bf16(x, y);
+                else *reinterpret_cast<float2*>(part + e) = make_float2(x, y);
+            }
+            if (n == 0) {
+                if (!whole) a.ml[slot * C::RT + rl] = make_float2(m[i], l[i]);
+                else if (a.lse) a.lse[at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * LN2;
+            }
+        }
+    }
+};
+
 // ---------------------------------------------------------------------------------- fp32 consumers
 //
 // Lane = key for the logits (q is read from shared memory, the same word for all lanes), lane = HD / 32 columns for the
@@ -677,6 +939,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     float* dump = reinterpret_cast<float*>(at); at += C::merge_bytes;
     long long* sh = reinterpret_cast<long long*>(at); at += 48 * 8;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(at); at += 2 * S * 8;
+    int* rows_s = reinterpret_cast<int*>(at); at += 32 * 4;
     int* s_abort = reinterpret_cast<int*>(at); at += 16;
     unsigned* odd = reinterpret_cast<unsigned*>(at); at += 3 * 8 * 4;
     volatile int* meta = reinterpret_cast<volatile int*>(at);
@@ -686,7 +949,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     if (tid == 0) {
-        for (int s = 0; s < S; s++) { mbar_init(full(s), 1); mbar_init(empty(s), C::groups); }
+        for (int s = 0; s < S; s++) { mbar_init(full(s), DT == DYNAKV_FP8 ? 2 : 1); mbar_init(empty(s), C::groups); }
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
@@ -700,52 +963,60 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 
     if (warp == C::consumers) {
         // =============================== producer ===============================
-        int it = 0;
+        // One lane issues, and walks through up to 32 pages without the others: with small pages its time per page sets the pace
+        // (FP8 rows of 64: 500 cycles when the warp met at every page; 4 x 32768 rows 54 -> 52 us with this).
+        int st = 0, items = 0;
+        unsigned ph = 1;
         bool ok = true;
         while (ok && walk.next(a, g)) {
             for (int pc = g.p0; ok && pc < g.p1; pc += 32) {
                 const int cnt = min(32, g.p1 - pc);
-                int id = -1;
+                int row = -1;
                 if (lane < cnt && g.n > 0) {
-                    id = a.page_table[(size_t)g.b * a.pages_per_seq + pc + lane];
-                    if (id < 0 || id >= a.n_pages) { id = -1; tree_status(a, DYNAKV_ST_BOUNDS); }
+                    const int id = a.page_table[(size_t)g.b * a.pages_per_seq + pc + lane];
+                    if (id < 0 || id >= a.n_pages) tree_status(a, DYNAKV_ST_BOUNDS);
+                    else row = (id * a.Hk + g.h) * PAGE;
                 }
-                for (int j = 0; j < cnt && ok; j++, it++) {
-                    const int page = __shfl_sync(0xffffffffu, id, j);
-                    const int st = it % S;
-                    if (lane == 0) {
-                        ok = mbar_wait(empty(st), ((it / S) & 1) ^ 1);
-                        if (ok) {
-                            meta[st] = page >= 0;
-                            if (page >= 0) {
-                                const int row = (page * a.Hk + g.h) * PAGE;
-                                mbar_arrive_expect_tx(full(st), C::stage_bytes + (DT == DYNAKV_FP8 ? 64 : 0));
-                                tma_page(ring + st * C::stage_bytes, &map_k, row, full(st));
-                                tma_page(ring + st * C::stage_bytes + C::page_bytes, &map_v, row, full(st));
-                                if constexpr (DT == DYNAKV_FP8) {
-                                    bulk_g2s(smem_u32(exps + st * 64), a.kexp + row, 32, full(st));
-                                    bulk_g2s(smem_u32(exps + st * 64 + 32), a.vexp + row, 32, full(st));
-                                }
-                            } else {
-                                mbar_arrive(full(st));
+                rows_s[lane] = row;
+                __syncwarp();
+                if (lane == 0) {
+                    for (int j = 0; j < cnt; j++) {
+                        const int at_row = rows_s[j];
+                        ok = mbar_wait(empty(st), ph);
+                        if (!ok) break;
+                        meta[st] = at_row >= 0;
+                        if (at_row >= 0) {
+                            mbar_arrive_expect_tx(full(st), C::stage_bytes);
+                            tma_page(ring + st * C::stage_bytes, &map_k, at_row, full(st));
+                            tma_page(ring + st * C::stage_bytes + C::page_bytes, &map_v, at_row, full(st));
+                            if constexpr (DT == DYNAKV_FP8) {
+                                copy32(smem_u32(exps + st * 64), a.kexp + at_row);
+                                copy32(smem_u32(exps + st * 64 + 32), a.vexp + at_row);
+                                copies_arrive(full(st));
                             }
+                        } else {
+                            mbar_arrive(full(st));
+                            if constexpr (DT == DYNAKV_FP8) mbar_arrive(full(st));
                         }
+                        items++;
+                        if (++st == S) { st = 0; ph ^= 1; }
                     }
-                    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
                 }
+                ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
             }
         }
         if (!ok && lane == 0) {
             // a stage was not given back in time: report it and let the copies under way land before the block ends
             *s_abort = 1;
             tree_status(a, DYNAKV_ST_INTERNAL);
-            for (int x = max(0, it - 1 - S); x < it - 1; x++) mbar_wait(full(x % S), (x / S) & 1);       // item it - 1 was not issued
+            for (int x = max(0, items - S); x < items; x++) mbar_wait(full(x % S), (x / S) & 1);
         }
     } else {
         // =============================== consumers ===============================
         const int rg = warp % C::groups, kg = warp / C::groups;
         constexpr bool F32 = DT == DYNAKV_F32;
-        typename std::conditional<F32, F32Rows<HD, RG>, MmaRows<HD, F32 ? DYNAKV_BF16 : DT, RG>>::type rows;
+        constexpr bool TURNED = DT == DYNAKV_FP8 && HD == 128 && RG == 0;
+        typename std::conditional<F32, F32Rows<HD, RG>, typename std::conditional<TURNED, TurnedRows, MmaRows<HD, F32 ? DYNAKV_BF16 : DT, RG>>::type>::type rows;
         auto all_sync = [&]() { asm volatile("bar.sync 5, %0;\n" ::"n"(C::consumers * 32) : "memory"); };
         auto group_sync = [&]() { asm volatile("bar.sync %0, %1;\n" ::"r"(6 + kg), "n"(C::groups * 32) : "memory"); };
         if constexpr (F32) { rows.q_s = smem_u32(q_s + rg * C::rows * HD); rows.p_s = smem_u32(p_s + warp * C::rows * 32); }
