@@ -8,17 +8,18 @@
 //
 // Kernel shape.  One producer warp streams whole 32-row pages, K and V, into a shared-memory ring with tiled TMA loads
 // (128-byte swizzle, so that the fragment loads below meet no bank conflicts; FP8 rows' exponents come by cp.async, because the two
-// bulk copies of 32 bytes cost as much issue time as the pages: 4 x 32768 rows of 64, 8 KV heads, 52 -> 46 us without them).  The consumer warps are RG row groups x KG page groups: a row group holds 16 query rows, a page group takes
-// every KG-th page of the CTA's range with a softmax state of its own, merged through shared memory at a segment's end.
+// bulk copies of 32 bytes cost as much issue time as the pages: 4 x 32768 rows of 64, 8 KV heads, 52 -> 46 us without them).
+// The consumer warps are RG row groups x KG page groups: a row group holds 16 query rows, a page group takes every KG-th
+// page of the CTA's range with a softmax state of its own, merged through shared memory at a segment's end.
 // Few rows: three page groups hide the latency of a page's chain of dependent steps; 64 rows: four row groups share a
 // page, which divides its shared-memory traffic.  A ring stage is always consumed by the same page group (a parity
 // wait cannot tell a phase from the one after the next).
 //
-// Three consumers.  bf16 rows: mma.sync m16n8k16, fragments by ldmatrix; the weights are split into bf16 hi + lo (two MMAs),
+// The consumers.  bf16 rows: mma.sync m16n8k16, fragments by ldmatrix; the weights are split into bf16 hi + lo (two MMAs),
 // because bf16 weights alone would add an error as large as the output's own rounding.  FP8 rows: the bytes become f16
 // operands (exact), q is divided by a power of two per row so that it fits f16, the K row's scale multiplies the logit, and
 // the V row's scale is folded into the softmax (running maximum over logit + exponent) as in the gather-attention kernel;
-// f16 weights round to 2^-12.  fp32 rows: fp32 FMAs, one lane per key for the logits, one lane per 4 columns for the sums.
+// f16 weights round to 2^-12; with few query rows of 128 elements the products are turned round.  fp32 rows: fp32 FMAs, one lane per key for the logits, one lane per 4 columns for the sums.
 //
 // Masked rows never reach a sum.  Logits of rows that a token does not see are replaced by -inf.  Rows of V past the
 // sequence's length (whatever an earlier sequence left there) are zeroed in shared memory, and so are drafted rows that hold
@@ -760,22 +761,25 @@ struct F32Rows {
         }
     }
     __device__ __forceinline__ void page(const TreeArgs& a, const Segment& g, const PageIn& p, int lane, int rg) {
-        float s[NR];
+        // Four chains per logit, in pairs that share an instruction: one chain of 64 carries the sum of a few large channels through
+        // all the rest.  Output error on such keys (one sequence of 2048 rows, logits up to 40): 1.4e-6 of its size with one
+        // chain, 2e-7 to 8e-7 with four.  16 rows have registers for two steps at a time, not four.
+        float2 s4[NR][2];
 #pragma unroll
-        for (int r = 0; r < NR; r++) s[r] = 0.f;
-#pragma unroll 4
+        for (int r = 0; r < NR; r++) s4[r][0] = s4[r][1] = make_float2(0.f, 0.f);
+#pragma unroll (NR == 16 ? 2 : 4)
         for (int ch = 0; ch < HD / 4; ch++) {
-            const uint4 ku = lds16(p.k + chunk_at<C>(lane, ch));
-            const float k0 = __uint_as_float(ku.x), k1 = __uint_as_float(ku.y), k2 = __uint_as_float(ku.z), k3 = __uint_as_float(ku.w);
+            const uint4 k = lds16(p.k + chunk_at<C>(lane, ch));
 #pragma unroll
             for (int r = 0; r < NR; r++) {
-                const uint4 qu = lds16(q_s + (r * HD + ch * 4) * 4);
-                s[r] = fmaf(__uint_as_float(qu.x), k0, s[r]);
-                s[r] = fmaf(__uint_as_float(qu.y), k1, s[r]);
-                s[r] = fmaf(__uint_as_float(qu.z), k2, s[r]);
-                s[r] = fmaf(__uint_as_float(qu.w), k3, s[r]);
+                const uint4 q = lds16(q_s + (r * HD + ch * 4) * 4);
+                s4[r][0] = fma2(make_float2(__uint_as_float(q.x), __uint_as_float(q.y)), make_float2(__uint_as_float(k.x), __uint_as_float(k.y)), s4[r][0]);
+                s4[r][1] = fma2(make_float2(__uint_as_float(q.z), __uint_as_float(q.w)), make_float2(__uint_as_float(k.z), __uint_as_float(k.w)), s4[r][1]);
             }
         }
+        float s[NR];
+#pragma unroll
+        for (int r = 0; r < NR; r++) s[r] = (s4[r][0].x + s4[r][0].y) + (s4[r][1].x + s4[r][1].y);
         unsigned win = ~0u;                        // lane r < NR: the window of row r
         if (p.mask) {
             const int x = g.tile * C::RT + rg * NR + (lane & (NR - 1)), t = x / a.G;
@@ -819,7 +823,10 @@ struct F32Rows {
 #pragma unroll
                 for (int y = 0; y < 4; y++)
 #pragma unroll
-                    for (int d = 0; d < DPL; d++) acc[r][d] = fmaf(w[y], v[y][d], acc[r][d]);
+                    for (int d = 0; d < DPL; d += 2) {
+                        const float2 x = fma2(make_float2(w[y], w[y]), make_float2(v[y][d], v[y][d + 1]), make_float2(acc[r][d], acc[r][d + 1]));
+                        acc[r][d] = x.x; acc[r][d + 1] = x.y;
+                    }
             }
         }
         __syncwarp();
