@@ -39,6 +39,12 @@ namespace dkv {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float VE_LOW = -60.f;            // FP8: V rows with a smaller scale take part in the reference as if they had this one
+// l * 2^d, d <= 0, where 2^d by itself may lie below fp32's range: FP8 rows' sums of weights are kept relative to a maximum that
+// has the V rows' exponents in it, so they are as far from 1 as those exponents are from another.
+__device__ __forceinline__ float scaled_sum(float l, float d) {
+    const float h = exp2f(0.5f * d);
+    return l * h * h;
+}
 constexpr float LAZY = 8.f;                // the softmax's reference moves when the maximum has grown by 2^LAZY
 
 __device__ __forceinline__ void tma_page(unsigned dst, const CUtensorMap* map, int row, unsigned bar) {
@@ -205,11 +211,11 @@ struct MmaRows {
     __device__ __forceinline__ void page(const TreeArgs& a, const Segment& g, const PageIn& p, int lane) {
         const int c = lane & 3, n = lane >> 2;
         // FP8: one lane per row turns its exponents into factors, and all lanes read what they need behind the products: the logit's
-        // factor, the exponent that takes part in the softmax, its factor back, and what a V row below 2^VE_LOW is still to be scaled by
+        // factor, the exponent that takes part in the softmax, and what a V row below 2^VE_LOW is still to be scaled by
         bool low = false;
         if constexpr (F8) {
             const float ve = (float)p.exps[32 + lane], vr = fmaxf(ve, VE_LOW);
-            p.scales[lane] = make_float4(pow2f(p.exps[lane]), vr, pow2f(-(int)vr), ex2(fminf(ve - VE_LOW, 0.f)));
+            p.scales[lane] = make_float4(pow2f(p.exps[lane]), vr, ex2(fminf(ve - VE_LOW, 0.f)), 0.f);
             low = __any_sync(0xffffffffu, ve < VE_LOW);
             __syncwarp();
         }
@@ -279,7 +285,8 @@ struct MmaRows {
             for (int i = 0; i < NR; i++) {
                 const float to = mx[i] > m[i] + LAZY ? mx[i] : m[i];
                 const float f = to == -INFINITY ? 1.f : ex2(m[i] - to);
-                m[i] = to; l[i] *= f;
+                l[i] = !F8 ? l[i] * f : to == -INFINITY ? l[i] : scaled_sum(l[i], m[i] - to);
+                m[i] = to;
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -295,8 +302,10 @@ struct MmaRows {
 #pragma unroll
                 for (int i = 0; i < NR; i++) {
                     float& x = s[kt][2 * i + e];
-                    x = ex2(x - ref[i]);
-                    if constexpr (F8) l[i] = fmaf(x, sc[kt][e].z, l[i]);
+                    const float y = x - ref[i];
+                    x = ex2(y);
+                    // not x / 2^exponent: x is 0 where this V row's scale is far below another's, its weight is not
+                    if constexpr (F8) l[i] += ex2(y - sc[kt][e].y);
                     else l[i] += x;
                 }
         if constexpr (F8) {
@@ -306,7 +315,7 @@ struct MmaRows {
 #pragma unroll
                     for (int e = 0; e < 2; e++)
 #pragma unroll
-                        for (int i = 0; i < NR; i++) s[kt][2 * i + e] *= sc[kt][e].w;
+                        for (int i = 0; i < NR; i++) s[kt][2 * i + e] *= sc[kt][e].z;
             }
         }
         // weights as A fragments: two 8-key tiles of the logits are the 16 keys of a step
@@ -403,7 +412,7 @@ struct MmaRows {
             const float2 o = reinterpret_cast<const float2*>(from + NT * 64 * NR)[(lane >> 2) + 8 * i];
             const float to = fmaxf(m[i], o.x), ref = to == -INFINITY ? 0.f : to;
             f0[i] = ex2(m[i] - ref); f1[i] = ex2(o.x - ref);
-            l[i] = l[i] * f0[i] + o.y * f1[i];
+            l[i] = F8 ? scaled_sum(l[i], m[i] - ref) + scaled_sum(o.y, o.x - ref) : l[i] * f0[i] + o.y * f1[i];
             m[i] = to;
         }
 #pragma unroll
@@ -557,7 +566,7 @@ struct TurnedRows {
         const int c = lane & 3, n = lane >> 2;
         // the scales of the 32 rows, one row per lane, as in MmaRows
         const float ve = (float)p.exps[32 + lane], vr = fmaxf(ve, VE_LOW);
-        p.scales[lane] = make_float4(pow2f(p.exps[lane]), vr, pow2f(-(int)vr), ex2(fminf(ve - VE_LOW, 0.f)));
+        p.scales[lane] = make_float4(pow2f(p.exps[lane]), vr, ex2(fminf(ve - VE_LOW, 0.f)), 0.f);
         const bool low = __any_sync(0xffffffffu, ve < VE_LOW);
         __syncwarp();
         float s[2][4];               // [16 keys][(key n, row 2 c), (n, 2 c + 1), (n + 8, 2 c), (n + 8, 2 c + 1)]
@@ -611,7 +620,8 @@ struct TurnedRows {
             for (int i = 0; i < 2; i++) {
                 const float to = mx[i] > m[i] + LAZY ? mx[i] : m[i];
                 const float f = to == -INFINITY ? 1.f : ex2(m[i] - to);
-                m[i] = to; l[i] *= f;
+                l[i] = to == -INFINITY ? l[i] : scaled_sum(l[i], m[i] - to);
+                m[i] = to;
 #pragma unroll
                 for (int mt = 0; mt < MT; mt++) { acc[mt][i] *= f; acc[mt][2 + i] *= f; }
             }
@@ -624,9 +634,10 @@ struct TurnedRows {
                 float w[2];
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
-                    w[i] = ex2(s[k16][2 * y + i] - (m[i] == -INFINITY ? 0.f : m[i]));
-                    l[i] = fmaf(w[i], sc[k16][y].z, l[i]);
-                    if (low) w[i] *= sc[k16][y].w;
+                    const float z = s[k16][2 * y + i] - (m[i] == -INFINITY ? 0.f : m[i]);
+                    w[i] = ex2(z);
+                    l[i] += ex2(z - sc[k16][y].y);             // as in MmaRows
+                    if (low) w[i] *= sc[k16][y].z;
                 }
                 const __half2 h = __floats2half2_rn(w[0], w[1]);
                 b[k16][y] = transposed(*reinterpret_cast<const unsigned*>(&h));
@@ -673,7 +684,7 @@ struct TurnedRows {
             const float2 o = reinterpret_cast<const float2*>(from + MT * 128)[2 * (lane & 3) + i];
             const float to = fmaxf(m[i], o.x), ref = to == -INFINITY ? 0.f : to;
             f0[i] = ex2(m[i] - ref); f1[i] = ex2(o.x - ref);
-            l[i] = l[i] * f0[i] + o.y * f1[i];
+            l[i] = scaled_sum(l[i], m[i] - ref) + scaled_sum(o.y, o.x - ref);
             m[i] = to;
         }
 #pragma unroll
@@ -1126,7 +1137,7 @@ __global__ void __launch_bounds__(256) k_tree_merge(const TreeArgs a) {
     for (int e = 0; e < EPL; e++) acc[e] = 0.f;
     for (int i0 = 0; i0 < n; i0 += 32) {
         float f = 0.f, fl = 0.f;
-        if (i0 + lane < n) { const float2 x = a.ml[slot(i0 + lane)]; f = exp2f(x.x - ref); fl = f * x.y; }
+        if (i0 + lane < n) { const float2 x = a.ml[slot(i0 + lane)]; f = exp2f(x.x - ref); fl = x.x - ref < -100.f ? scaled_sum(x.y, x.x - ref) : f * x.y; }
         l += warp_sum(fl);
         const int cnt = min(32, n - i0);
 #pragma unroll 8

@@ -199,6 +199,32 @@ def test_nan_and_infinities_in_rows_not_seen(cache, d, heads, what):
         _check_rows(p, b, at, out, lse, rows)
 
 
+@pytest.mark.parametrize("cache,d", [("fp8", 128), ("fp8", 64), ("bf16", 128), ("f32", 64)])
+def test_drafted_nan_rows_with_few_query_rows(cache, d):
+    p = Problem([45, 70], [4, 3], 2, 1, d, cache, tree=True, seed=12)       # at most 8 query rows
+    for b, j, which in ((0, 1, "v"), (0, 3, "k"), (1, 2, "v")):
+        p.sees[b][:, j] = False
+        p.sees[b][j, j] = True
+        n = p.lens[b] - p.drafts[b] + j
+        pool = getattr(p.c, which)
+        row = pool[p.table[b, n // 32].item(), :, n % 32] if cache != "fp8" else pool.view(torch.uint8)[p.table[b, n // 32].item(), :, n % 32]
+        row[:, 3] = float("nan") if cache != "fp8" else 0x7f
+    p.pack()
+    out, lse = p.run()
+    for b, at, rows in ((0, 0, [0, 1, 2]), (1, 4, [0, 1, 2])):
+        _check_rows(p, b, at, out, lse, rows)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,drafts", [(7, 1), (2, 4), (4, 4), (8, 8), (8, 16)])
+def test_fp8_rows_of_very_different_scales(d, heads, drafts):
+    p = Problem([333, 64], [drafts, 1], heads, 1, d, "fp8", seed=13)
+    g = torch.Generator(device="cuda").manual_seed(14)
+    p.c.v_exp.copy_(torch.randint(-120, 100, p.c.v_exp.shape, generator=g, device="cuda"))
+    p.c.k_exp.sub_(torch.randint(0, 30, p.c.k_exp.shape, generator=g, device="cuda").to(torch.int8))
+    p.check(*p.run())
+
+
 def _check_rows(p, b, at, out, lse, rows):
     """Some tokens of sequence b (its first one is packed row `at`) against the formula over the rows they see, and only those."""
     n, t, group = p.lens[b], p.drafts[b], p.heads // p.hk
