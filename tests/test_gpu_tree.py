@@ -398,6 +398,20 @@ def test_bad_pages_lengths_and_token_ranges_are_skipped_and_reported():
         assert c.get_status() == P.ST_BOUNDS, kw
 
 
+@pytest.mark.parametrize("cache,heads,d,drafts", [("fp8", 4, 128, 1), ("fp8", 4, 64, 1), ("fp8", 4, 128, 9), ("fp8", 8, 128, 40), ("f32", 4, 64, 1), ("bf16", 8, 128, 40)])
+def test_missing_pages_in_a_long_table(cache, heads, d, drafts):
+    p = Problem([3000], [drafts], heads, 2, d, cache, seed=21)
+    good, gone = p.table.clone(), [1, 5, 6, 40, 90]
+    for i, x in zip(gone, (1 << 30, -1, -(1 << 31), p.c.k.shape[0], 1 << 30)):
+        p.table[0, i] = x
+    out, lse = p.run()
+    assert p.c.get_status() == P.ST_BOUNDS
+    q = Problem([3000 - 32 * len(gone)], [drafts], heads, 2, d, cache, seed=21)
+    q.table = good[:, [i for i in range(good.shape[1]) if i not in gone]].contiguous()
+    q.c, q.q = P.RowCache(p.c.k, p.c.v, p.c.k_exp, p.c.v_exp), p.q         # the same rows, a status of its own
+    q.check(out, lse)
+
+
 def test_refusals():
     p = Problem([50], [3], 4, 2, 128, "bf16")
     i32 = dict(dtype=torch.int32, device="cuda")
