@@ -19,7 +19,8 @@
 // because bf16 weights alone would add an error as large as the output's own rounding.  FP8 rows: the bytes become f16
 // operands (exact), q is divided by a power of two per row so that it fits f16, the K row's scale multiplies the logit, and
 // the V row's scale is folded into the softmax (running maximum over logit + exponent) as in the gather-attention kernel;
-// f16 weights round to 2^-12; with few query rows of 128 elements the products are turned round.  fp32 rows: fp32 FMAs, one lane per key for the logits, one lane per 4 columns for the sums.
+// f16 weights round to 2^-12; with few query rows of 128 elements the products are turned round.  fp32 rows: fp32 FMAs, one
+// lane per key for the logits, one lane per 4 columns for the sums.
 //
 // Masked rows never reach a sum.  Logits of rows that a token does not see are replaced by -inf.  Rows of V past the
 // sequence's length (whatever an earlier sequence left there) are zeroed in shared memory, and so are drafted rows that hold
