@@ -474,8 +474,10 @@ int dynakv_rows_read(const dynakv_row_cache* cache, const int32_t* page_table, i
  * q, out: [n_tokens][n_heads][head_dim], contiguous and 16-byte aligned, fp32 for a DYNAKV_F32 cache, else bf16;
  * lse: [n_tokens][n_heads] fp32, may be NULL.  Tokens at and behind q_start[n_seqs] are left as they were.  n_heads is 1 to 8 times n_kv_heads;
  * max_tree 1 .. 256; tree_mask [n_tokens][mask_words], mask_words 1 .. 4 (rows past the last word are not seen).
- * Logits, weights' sums and outputs are accumulated in fp32; FP8: V rows whose scale is below 2^-60 are summed with less
- * relative precision.  No length is needed on the host, so one captured graph serves a growing cache.
+ * Logits, weights' sums and outputs are accumulated in fp32.  Weights enter the products with V in fp32 (DYNAKV_F32), to 2^-17
+ * (DYNAKV_BF16, and DYNAKV_FP8 with more than 64 query rows, max_tree * n_heads / n_kv_heads, per KV head) or, DYNAKV_FP8 with up
+ * to 64 query rows, as f16: p_j * 2^exp_j is off by 2^-12 of itself down to 2^-26 of the token's largest, below that by 2^-37 of
+ * the largest, and V rows whose scale is below 2^-60 count as rows of scale 2^-60 in that.  No length is needed on the host, so one captured graph serves a growing cache.
  * workspace: dynakv_attend_tree_workspace() bytes of device memory, 16-byte aligned, contents of no interest before
  * and after; calls that may overlap (streams, graphs) need one each. */
 int dynakv_attend_tree(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,

@@ -31,7 +31,7 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], unsigned a0, unsigned a1,
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// (hi, lo) f16 split of two floats in [-1, 1], packed as f16x2 (first value in the low half).
+// (hi, lo) f16 split of two floats of at most 65504, packed as f16x2 (first value in the low half).
 __device__ __forceinline__ void split2h(float x, float y, unsigned& hi, unsigned& lo) {
     const __half2 h = __floats2half2_rn(x, y);
     const float2 hf = __half22float2(h);

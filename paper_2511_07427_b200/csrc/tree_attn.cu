@@ -19,7 +19,8 @@
 // because bf16 weights alone would add an error as large as the output's own rounding.  FP8 rows: the bytes become f16
 // operands (exact), q is divided by a power of two per row so that it fits f16, the K row's scale multiplies the logit, and
 // the V row's scale is folded into the softmax (running maximum over logit + exponent) as in the gather-attention kernel;
-// f16 weights round to 2^-12; with few query rows of 128 elements the products are turned round.  fp32 rows: fp32 FMAs, one
+// f16 weights round to 2^-12 of themselves down to 2^-26 of the largest weight times scale, below to 2^-37 of it (F16_BELOW); with
+// few query rows of 128 elements the products are turned round.  fp32 rows: fp32 FMAs, one
 // lane per key for the logits, one lane per 4 columns for the sums.
 //
 // Masked rows never reach a sum.  Logits of rows that a token does not see are replaced by -inf.  Rows of V past the
@@ -46,7 +47,12 @@ __device__ __forceinline__ float scaled_sum(float l, float d) {
     const float h = exp2f(0.5f * d);
     return l * h * h;
 }
-constexpr float LAZY = 8.f;                // the softmax's reference moves when the maximum has grown by 2^LAZY
+// The softmax's reference moves when the maximum has outgrown it by 2^LAZY, to the maximum.  FP8 rows, whose weights become f16
+// values (65504 at most, subnormal below 2^-14): to 2^F16_BELOW below the maximum, and again when that has grown by 2^F16_LAZY, so
+// that weights stay below 2^15.8 and those down to 2^-26 of the largest are normal.  With the reference at the maximum they were
+// subnormal from 2^-14 on and lost below 2^-25, which a column sees where a dominant row holds a zero: it came out as 0.  The
+// lower reference and earlier moves cost up to 2 % (4 x 32768 rows, 8 KV heads: 32 query rows 104 -> 106 us, 64 rows 187 -> 190 us).
+constexpr float LAZY = 8.f, F16_BELOW = 12.f, F16_LAZY = 3.75f;
 
 __device__ __forceinline__ void tma_page(unsigned dst, const CUtensorMap* map, int row, unsigned bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n"
@@ -143,6 +149,7 @@ struct MmaRows {
     static constexpr bool F8 = DT == DYNAKV_FP8;
     static constexpr bool HALF = RG == 0;
     static constexpr int KS = HD / 16, NT = HD / 8, NR = HALF ? 1 : 2;       // rows per lane
+    static constexpr float BELOW = F8 ? F16_BELOW : 0.f, GROW = F8 ? F16_BELOW + F16_LAZY : LAZY;
     static constexpr bool PERM = F8 && HD == 128;       // key order inside a tile that keeps FP8 loads free of conflicts
     unsigned qf[KS][4];
     float qs[NR];                                       // logit factor (log2 units) of the rows
@@ -280,11 +287,11 @@ struct MmaRows {
         float ref[NR];
         bool move = false;
 #pragma unroll
-        for (int i = 0; i < NR; i++) { mx[i] = quad_max(mx[i]); move |= mx[i] > m[i] + LAZY; }
+        for (int i = 0; i < NR; i++) { mx[i] = quad_max(mx[i]); move |= mx[i] > m[i] + GROW; }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
             for (int i = 0; i < NR; i++) {
-                const float to = mx[i] > m[i] + LAZY ? mx[i] : m[i];
+                const float to = mx[i] > m[i] + GROW ? mx[i] - BELOW : m[i];
                 const float f = to == -INFINITY ? 1.f : ex2(m[i] - to);
                 l[i] = !F8 ? l[i] * f : to == -INFINITY ? l[i] : scaled_sum(l[i], m[i] - to);
                 m[i] = to;
@@ -615,11 +622,11 @@ struct TurnedRows {
             }
         bool move = false;
 #pragma unroll
-        for (int i = 0; i < 2; i++) { mx[i] = max_over_keys(mx[i]); move |= mx[i] > m[i] + LAZY; }
+        for (int i = 0; i < 2; i++) { mx[i] = max_over_keys(mx[i]); move |= mx[i] > m[i] + (F16_BELOW + F16_LAZY); }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
             for (int i = 0; i < 2; i++) {
-                const float to = mx[i] > m[i] + LAZY ? mx[i] : m[i];
+                const float to = mx[i] > m[i] + (F16_BELOW + F16_LAZY) ? mx[i] - F16_BELOW : m[i];
                 const float f = to == -INFINITY ? 1.f : ex2(m[i] - to);
                 l[i] = to == -INFINITY ? l[i] : scaled_sum(l[i], m[i] - to);
                 m[i] = to;
