@@ -3,7 +3,7 @@
 Argument marshalling only, like the rest of the binding: every method is one C call (two launches for ``attend_tree``) on
 the stream that is current on the tensors' device.  Nothing synchronises, results and scratch come from torch's caching
 allocator (so calls on several streams, and calls captured into several CUDA graphs, never share scratch).  The calls
-compute no gradients and refuse inputs that would need one.
+compute no gradients and refuse, unless gradients are off, tensors that would need one: inputs, weights and cache rows alike.
 """
 from __future__ import annotations
 
@@ -110,6 +110,14 @@ def _no_gradient() -> None:
     raise DynaKVError("this call computes no gradients: detach its inputs or run it under torch.no_grad()")
 
 
+def _held(E, tensors) -> None:
+    """What a call checks of the tensors that its object was made around."""
+    if E.grad():
+        for t in tensors:
+            if t.requires_grad:
+                _no_gradient()
+
+
 def _call(E, device: int, fn, *args) -> None:
     """One C call on the device's current stream (its last argument), with the device made current when it is not."""
     if E.device() == device:
@@ -150,7 +158,7 @@ class HeadRotary:
         for name, w, numel in (("inv_freq", inv_freq, rotary_dim // 2), ("q_weight", q_weight, self.head_dim), ("k_weight", k_weight, self.head_dim)):
             if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (numel,) or not w.is_contiguous() or w.device != self.device):
                 raise DynaKVError(f"expected {name} as a contiguous float32 tensor of {numel} elements on {self.device}, got {w.dtype} {tuple(w.shape)} on {w.device}")
-        self._tensors = (inv_freq, q_weight, k_weight)
+        self._tensors = tuple(t for t in (inv_freq, q_weight, k_weight) if t is not None)
         self._c = _Rotary(self.n_heads, self.n_kv_heads, self.head_dim, rotary_dim, 1 if interleaved else 0, eps,
                           q_weight.data_ptr() if q_weight is not None else None,
                           k_weight.data_ptr() if k_weight is not None else None,
@@ -160,6 +168,7 @@ class HeadRotary:
     def _q_k(self, E, q, k):
         if q.dim() != 3:
             raise DynaKVError(f"expected q of three dimensions, got {tuple(q.shape)}")
+        _held(E, self._tensors)
         n, dtype = q.shape[0], q.dtype
         code = _float_type(dtype, "q")
         return n, dtype, code, _heads(E, q, (n, self.n_heads, self.head_dim), self._device, dtype, code, "q"), \
@@ -187,6 +196,7 @@ class HeadRotary:
         E = _env()
         n, dtype, code, qr, kr = self._q_k(E, q, k)
         vr = _heads(E, v, (n, self.n_kv_heads, self.head_dim), self._device, dtype, code, "v")
+        _held(E, cache._tensors)
         if cache._device != self._device or cache.head_dim != self.head_dim or cache.n_kv_heads != self.n_kv_heads:
             raise DynaKVError(f"the cache holds {cache.n_kv_heads} heads of {cache.head_dim} on {cache.device}, the embedding has "
                               f"{self.n_kv_heads} of {self.head_dim} on {self.device}")
@@ -229,6 +239,7 @@ class RowCache:
         if any(t is not None and t.data_ptr() % 16 for t in (k, v, k_exp, v_exp)):
             raise DynaKVError("the cache's tensors have to be 16-byte aligned")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._tensors = tuple(t for t in (k, v, k_exp, v_exp) if t is not None)
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._status_at = self._status.data_ptr()
         self._c = _RowCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if k_exp is not None else None,
@@ -260,6 +271,7 @@ class RowCache:
         if k.dim() != 3:
             raise DynaKVError(f"expected k of three dimensions, got {tuple(k.shape)}")
         E, device = _env(), self._device
+        _held(E, self._tensors)
         n, dtype = k.shape[0], k.dtype
         shape, code = (n, self.n_kv_heads, self.head_dim), _float_type(dtype, "k")
         kr, vr = _heads(E, k, shape, device, dtype, code, "k"), _heads(E, v, shape, device, dtype, code, "v")
@@ -270,6 +282,7 @@ class RowCache:
         fp32 cache, else bf16; zeros at and past ``lengths`` [sequences] int32.  ``page_table`` [sequences, pages per
         sequence] int32.  As [U, n, d] views these are the K, V of ``DynaKV.build_index``."""
         E, device = _env(), self._device
+        _held(E, self._tensors)
         if page_table.dim() != 2 or n < 0 or first < 0:
             raise DynaKVError(f"expected page_table of two dimensions, n >= 0 and first >= 0, got {tuple(page_table.shape)}, {n}, {first}")
         b, per = page_table.shape
@@ -293,7 +306,8 @@ class RowCache:
         if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != device or q.data_ptr() % 16:
             raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {dtype} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
                               f"got {q.dtype} {tuple(q.shape)} on {q.device}")
-        if q.requires_grad and E.grad():
+        _held(E, self._tensors)
+        if E.grad() and (q.requires_grad or out is not None and out.requires_grad):
             _no_gradient()
         n, heads, d = q.shape
         if page_table.dim() != 2:
