@@ -111,11 +111,14 @@ def _no_gradient() -> None:
 
 
 def _held(E, tensors) -> None:
-    """What a call checks of the tensors that its object was made around."""
-    if E.grad():
-        for t in tensors:
-            if t.requires_grad:
-                _no_gradient()
+    """What a call checks of the tensors that its object was made around, (tensor, address) pairs: their memory is where it was (not
+    replaced by ``.data =`` or a resize of the storage) and none of them wants a gradient."""
+    grad = E.grad()
+    for t, at in tensors:
+        if t.data_ptr() != at:
+            raise DynaKVError("a tensor of this object has got other memory since the object was made: make a new one")
+        if grad and t.requires_grad:
+            _no_gradient()
 
 
 def _call(E, device: int, fn, *args) -> None:
@@ -158,7 +161,7 @@ class HeadRotary:
         for name, w, numel in (("inv_freq", inv_freq, rotary_dim // 2), ("q_weight", q_weight, self.head_dim), ("k_weight", k_weight, self.head_dim)):
             if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (numel,) or not w.is_contiguous() or w.device != self.device):
                 raise DynaKVError(f"expected {name} as a contiguous float32 tensor of {numel} elements on {self.device}, got {w.dtype} {tuple(w.shape)} on {w.device}")
-        self._tensors = tuple(t for t in (inv_freq, q_weight, k_weight) if t is not None)
+        self._tensors = tuple((t, t.data_ptr()) for t in (inv_freq, q_weight, k_weight) if t is not None)
         self._c = _Rotary(self.n_heads, self.n_kv_heads, self.head_dim, rotary_dim, 1 if interleaved else 0, eps,
                           q_weight.data_ptr() if q_weight is not None else None,
                           k_weight.data_ptr() if k_weight is not None else None,
@@ -239,7 +242,7 @@ class RowCache:
         if any(t is not None and t.data_ptr() % 16 for t in (k, v, k_exp, v_exp)):
             raise DynaKVError("the cache's tensors have to be 16-byte aligned")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
-        self._tensors = tuple(t for t in (k, v, k_exp, v_exp) if t is not None)
+        self._tensors = tuple((t, t.data_ptr()) for t in (k, v, k_exp, v_exp) if t is not None)
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._status_at = self._status.data_ptr()
         self._c = _RowCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if k_exp is not None else None,

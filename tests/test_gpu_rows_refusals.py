@@ -55,3 +55,24 @@ def test_a_cache_whose_rows_want_a_gradient(which, dtype):
     with pytest.raises(P.DynaKVError, match="gradient"):
         c.attend_tree(q, table, lens, start, 3, out=out)
     assert c.get_status() == 0
+
+
+def test_tensors_whose_memory_was_replaced():
+    x, q, at = _things()
+    w = torch.nn.Parameter(torch.ones(128, device="cuda"), requires_grad=False)
+    ro = P.HeadRotary(4, 2, 128, torch.ones(64, device="cuda"), q_weight=w)
+    k, v = (torch.zeros(1, 2, 32, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    c = P.RowCache(k, v)
+    table, lens, start = torch.zeros(1, 1, **I32), torch.full((1,), 3, **I32), torch.tensor([0, 3], **I32)
+    before = ro.apply(q + 1, x + 1, at)[0]
+    w.mul_(2.0)                                   # the same memory: fine
+    assert torch.equal(ro.apply(q + 1, x + 1, at)[0], (before.float() * 2).bfloat16())
+    w.data = torch.ones(128, device="cuda")
+    for f in (lambda: ro.apply(q, x, at), lambda: ro.store(q, x, x, at, c, at)):
+        with pytest.raises(P.DynaKVError, match="memory"):
+            f()
+    ro = P.HeadRotary(4, 2, 128, torch.ones(64, device="cuda"), q_weight=w)
+    v.untyped_storage().resize_(0)
+    for f in (lambda: c.write(x, x, at), lambda: c.read(table, lens, 3), lambda: ro.store(q, x, x, at, c, at), lambda: c.attend_tree(q, table, lens, start, 3)):
+        with pytest.raises(P.DynaKVError, match="memory"):
+            f()
