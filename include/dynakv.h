@@ -472,7 +472,8 @@ int dynakv_rows_read(const dynakv_row_cache* cache, const int32_t* page_table, i
  * Rows it does not see do not count whatever they hold, NaN and infinities included.
  *
  * q, out: [n_tokens][n_heads][head_dim], contiguous and 16-byte aligned, fp32 for a DYNAKV_F32 cache, else bf16;
- * lse: [n_tokens][n_heads] fp32, may be NULL.  Tokens at and behind q_start[n_seqs] are left as they were.  n_heads is 1 to 8 times n_kv_heads;
+ * lse: [n_tokens][n_heads] fp32, may be NULL.  Tokens of no sequence, before q_start[0] or from q_start[n_seqs] on, are left as they were
+ * in both.  n_heads is 1 to 8 times n_kv_heads;
  * max_tree 1 .. 256; tree_mask [n_tokens][mask_words], mask_words 1 .. 4 (rows past the last word are not seen).
  * Logits, weights' sums and outputs are accumulated in fp32.  Weights enter the products with V in fp32 (DYNAKV_F32), to 2^-17
  * (DYNAKV_BF16, and DYNAKV_FP8 with more than 64 query rows, max_tree * n_heads / n_kv_heads, per KV head) or, DYNAKV_FP8 with up

@@ -110,6 +110,12 @@ def _no_gradient() -> None:
     raise DynaKVError("this call computes no gradients: detach its inputs or run it under torch.no_grad()")
 
 
+def _overlap(a, b) -> bool:
+    """Whether two contiguous tensors share memory."""
+    x, y = a.data_ptr(), b.data_ptr()
+    return x < y + b.numel() * b.element_size() and y < x + a.numel() * a.element_size()
+
+
 def _held(E, tensors) -> None:
     """What a call checks of the tensors that its object was made around, (tensor, address) pairs: their memory is where it was (not
     replaced by ``.data =`` or a resize of the storage) and none of them wants a gradient."""
@@ -295,7 +301,7 @@ class RowCache:
         _call(E, device, E.dynakv_rows_read, self._ref, table, per, lens, b, first, n, K.data_ptr(), V.data_ptr(), self._status_at)
         return K, V
 
-    def attend_tree(self, q, page_table, kv_len, q_start, max_tree: int, tree_mask=None, scale=None, out=None):
+    def attend_tree(self, q, page_table, kv_len, q_start, max_tree: int, tree_mask=None, scale=None, out=None, lse=None):
         """Attention of drafted tokens over the cache (``dynakv_attend_tree``): (out, lse).
 
         q [tokens, heads, d] (fp32 for an fp32 cache, else bf16), the tokens of all sequences one after the other:
@@ -303,14 +309,16 @@ class RowCache:
         them; the last as many of its ``kv_len`` [sequences] int32 rows in ``page_table`` [sequences, pages] int32 are their own, the others the
         context, which every token sees.  ``tree_mask`` [tokens, words] int64: bit j of a token's words says that it
         sees row j of its tree (None: a chain, j <= i).  ``scale`` defaults to 1 / sqrt(d).  lse [tokens, heads]
-        fp32 is the natural logarithm of the weights' sum, for merging with attention over other rows.  A token
-        that sees nothing gets zeros and -inf; tokens behind the last sequence are left as they are in ``out``."""
+        fp32 is the natural logarithm of the weights' sum, for merging with attention over other rows.  A token that sees
+        nothing gets zeros and -inf.  Tokens of no sequence (before q_start[0], behind the last sequence: a padded batch) are left as
+        they are in ``out`` and ``lse``, so what they hold is unspecified in one that is not passed in.  Neither may share memory with
+        the other or with anything that is read."""
         E, device, dtype = _env(), self._device, self._io
         if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != device or q.data_ptr() % 16:
             raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {dtype} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
                               f"got {q.dtype} {tuple(q.shape)} on {q.device}")
         _held(E, self._tensors)
-        if E.grad() and (q.requires_grad or out is not None and out.requires_grad):
+        if E.grad() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
             _no_gradient()
         n, heads, d = q.shape
         if page_table.dim() != 2:
@@ -335,9 +343,16 @@ class RowCache:
             out = E.empty((n, heads, d), dtype=dtype, device=self.device)
         elif out.dtype is not dtype or out.shape != q.shape or not out.is_contiguous() or out.get_device() != device or out.data_ptr() % 16:
             raise DynaKVError(f"expected out as a contiguous, 16-byte aligned {dtype} tensor {tuple(q.shape)} on {self.device}")
+        elif _overlap(out, q):
+            raise DynaKVError("out shares memory with q")
+        if lse is None:
+            lse = E.empty((n, heads), dtype=E.f32, device=self.device)
+        elif lse.dtype is not E.f32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != device:
+            raise DynaKVError(f"expected lse as a contiguous float32 tensor {(n, heads)} on {self.device}, got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
+        elif _overlap(lse, q) or _overlap(lse, out):
+            raise DynaKVError("lse shares memory with q or out")
         table, lens, start = _index(E, page_table, (b, per), device, "page_table"), _index(E, kv_len, (b,), device, "kv_len"), \
             _index(E, q_start, (b + 1,), device, "q_start")
-        lse = E.empty((n, heads), dtype=E.f32, device=self.device)
         space = E.empty(size, dtype=self._byte, device=self.device)
         _call(E, device, E.dynakv_attend_tree, self._ref, q.data_ptr(), heads, n, start, b, max_tree, table, per, lens, mask, words, scale,
               out.data_ptr(), lse.data_ptr(), space.data_ptr(), size, self._status_at)
