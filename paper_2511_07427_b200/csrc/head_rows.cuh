@@ -62,8 +62,7 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     return d;
 }
 
-// Eight consecutive elements of a strided array.  vec: base and strides keep every row 16-byte aligned; else the
-// elements are loaded one by one.
+// Eight consecutive floats.  vec: p is 16-byte aligned; else the elements are loaded one by one.
 __device__ __forceinline__ void load8(const float* p, bool vec, float (&x)[8]) {
     if (vec) {
         const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
@@ -71,17 +70,6 @@ __device__ __forceinline__ void load8(const float* p, bool vec, float (&x)[8]) {
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++) x[i] = p[i];
-    }
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, bool vec, float (&x)[8]) {
-    if (vec) {
-        const uint4 a = *reinterpret_cast<const uint4*>(p);
-        const unsigned w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; i++) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = __bfloat162float(p[i]);
     }
 }
 
