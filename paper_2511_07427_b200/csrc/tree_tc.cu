@@ -588,8 +588,8 @@ __global__ void __launch_bounds__((TcTree<HD, PAIR, F8>::threads), 1) k_tree_tc(
 template <int HD, bool PAIR, bool F8>
 static int tree_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, int sms, cudaStream_t st) {
     using C = TcTree<HD, PAIR, F8>;
-    CUtensorMap mk, mv;
-    if (!tree_page_map(&mk, cache, cache->k, false) || !tree_page_map(&mv, cache, cache->v, false)) return DYNAKV_ERR_CUDA;
+    CUtensorMap mk = {}, mv = {};              // FP8 rows are fetched by plain loads: that kernel looks at neither
+    if (!F8 && (!tree_page_map(&mk, cache, cache->k, false) || !tree_page_map(&mv, cache, cache->v, false))) return DYNAKV_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(k_tree_tc<HD, PAIR, F8>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
     if (launch_pdl(k_tree_tc<HD, PAIR, F8>, dim3(sms), dim3(C::threads), C::smem, st, mk, mv, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
