@@ -330,6 +330,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows_read(dynakv_row_cache cach
     const int h = blockIdx.y, b = blockIdx.z, nk = cache.n_kv_heads;
     const long long len = lengths[b];
     const int* table = page_table + (size_t)b * pages_per_seq;
+    if (len < 0 && status && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) atomicOr(status, DYNAKV_ST_BOUNDS);
     uint4 raw[2][NR][DT == DYNAKV_F32 ? 2 : 1];
     float scale[2][NR];
     bool there[NR];

@@ -76,3 +76,16 @@ def test_tensors_whose_memory_was_replaced():
     for f in (lambda: c.write(x, x, at), lambda: c.read(table, lens, 3), lambda: ro.store(q, x, x, at, c, at), lambda: c.attend_tree(q, table, lens, start, 3)):
         with pytest.raises(P.DynaKVError, match="memory"):
             f()
+
+
+@pytest.mark.parametrize("cache", [P.F32, P.BF16, P.FP8])
+def test_a_negative_length_is_read_as_zeros_and_reported(cache):
+    c = P.RowCache.allocate(2, 2, 64, cache)
+    x = torch.ones(64, 2, 64, device="cuda")
+    c.write(x, x, torch.arange(64, **I32))
+    table = torch.tensor([[0], [1]], **I32)
+    K, V = c.read(table, torch.tensor([0, 32], **I32), 40)
+    assert c.get_status() == 0 and float(K[0].abs().max()) == 0 and float(K[1, :, :32].min()) == 1
+    K, V = c.read(table, torch.tensor([32, -1], **I32), 40)
+    assert float(K[0, :, :32].min()) == 1 and float(K[1].abs().max()) == 0 and float(V[1].abs().max()) == 0
+    assert c.get_status() == P.ST_BOUNDS          # as attend_tree reports it
