@@ -81,8 +81,8 @@ def _torch():
     return torch
 
 
-def _float_type(dtype, what: str) -> int:
-    code = _env().types.get(dtype)
+def _float_type(E, dtype, what: str) -> int:
+    code = E.types.get(dtype)
     if code is None:
         raise DynaKVError(f"{what} is {dtype}: expected torch.float32 or torch.bfloat16")
     return code
@@ -116,15 +116,23 @@ def _overlap(a, b) -> bool:
     return x < y + b.numel() * b.element_size() and y < x + a.numel() * a.element_size()
 
 
-def _held(E, tensors) -> None:
-    """What a call checks of the tensors that its object was made around, (tensor, address) pairs: their memory is where it was (not
-    replaced by ``.data =`` or a resize of the storage) and none of them wants a gradient."""
-    grad = E.grad()
-    for t, at in tensors:
-        if t.data_ptr() != at:
-            raise DynaKVError("a tensor of this object has got other memory since the object was made: make a new one")
-        if grad and t.requires_grad:
-            _no_gradient()
+class _Held:
+    """The tensors that an object was made around, and what its calls check of them: their memory is where it was (not replaced by
+    ``.data =`` or a resize of the storage) and none of them wants a gradient."""
+    __slots__ = ("where", "leaves")
+
+    def __init__(self, *tensors):
+        tensors = [t for t in tensors if t is not None]
+        self.where = tuple((t.data_ptr, t.data_ptr()) for t in tensors)         # bound methods: half the time of looking them up
+        self.leaves = tuple(t for t in tensors if t.is_floating_point())
+
+    def check(self, E) -> None:
+        for now, then in self.where:
+            if now() != then:
+                raise DynaKVError("a tensor of this object has got other memory since the object was made: make a new one")
+        for t in self.leaves:
+            if t.requires_grad and E.grad():
+                _no_gradient()
 
 
 def _call(E, device: int, fn, *args) -> None:
@@ -167,7 +175,7 @@ class HeadRotary:
         for name, w, numel in (("inv_freq", inv_freq, rotary_dim // 2), ("q_weight", q_weight, self.head_dim), ("k_weight", k_weight, self.head_dim)):
             if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (numel,) or not w.is_contiguous() or w.device != self.device):
                 raise DynaKVError(f"expected {name} as a contiguous float32 tensor of {numel} elements on {self.device}, got {w.dtype} {tuple(w.shape)} on {w.device}")
-        self._tensors = tuple((t, t.data_ptr()) for t in (inv_freq, q_weight, k_weight) if t is not None)
+        self._held = _Held(inv_freq, q_weight, k_weight)
         self._c = _Rotary(self.n_heads, self.n_kv_heads, self.head_dim, rotary_dim, 1 if interleaved else 0, eps,
                           q_weight.data_ptr() if q_weight is not None else None,
                           k_weight.data_ptr() if k_weight is not None else None,
@@ -177,9 +185,9 @@ class HeadRotary:
     def _q_k(self, E, q, k):
         if q.dim() != 3:
             raise DynaKVError(f"expected q of three dimensions, got {tuple(q.shape)}")
-        _held(E, self._tensors)
+        self._held.check(E)
         n, dtype = q.shape[0], q.dtype
-        code = _float_type(dtype, "q")
+        code = _float_type(E, dtype, "q")
         return n, dtype, code, _heads(E, q, (n, self.n_heads, self.head_dim), self._device, dtype, code, "q"), \
             _heads(E, k, (n, self.n_kv_heads, self.head_dim), self._device, dtype, code, "k")
 
@@ -191,8 +199,8 @@ class HeadRotary:
         E, device = _env(), self.device
         n, dtype, code, qr, kr = self._q_k(E, q, k)
         q_dtype, k_dtype = q_dtype or dtype, k_dtype or dtype
-        qt = code if q_dtype is dtype else _float_type(q_dtype, "q_dtype")
-        kt = code if k_dtype is dtype else _float_type(k_dtype, "k_dtype")
+        qt = code if q_dtype is dtype else _float_type(E, q_dtype, "q_dtype")
+        kt = code if k_dtype is dtype else _float_type(E, k_dtype, "k_dtype")
         place = _index(E, positions, (n,), self._device, "positions")
         q_out = E.empty((n, self.n_heads, self.head_dim), dtype=q_dtype, device=device)
         k_out = E.empty((n, self.n_kv_heads, self.head_dim), dtype=k_dtype, device=device)
@@ -205,12 +213,12 @@ class HeadRotary:
         E = _env()
         n, dtype, code, qr, kr = self._q_k(E, q, k)
         vr = _heads(E, v, (n, self.n_kv_heads, self.head_dim), self._device, dtype, code, "v")
-        _held(E, cache._tensors)
+        cache._held.check(E)
         if cache._device != self._device or cache.head_dim != self.head_dim or cache.n_kv_heads != self.n_kv_heads:
             raise DynaKVError(f"the cache holds {cache.n_kv_heads} heads of {cache.head_dim} on {cache.device}, the embedding has "
                               f"{self.n_kv_heads} of {self.head_dim} on {self.device}")
         q_dtype = q_dtype or dtype
-        qt = code if q_dtype is dtype else _float_type(q_dtype, "q_dtype")
+        qt = code if q_dtype is dtype else _float_type(E, q_dtype, "q_dtype")
         place, slot = _index(E, positions, (n,), self._device, "positions"), _index(E, slots, (n,), self._device, "slots")
         q_out = E.empty((n, self.n_heads, self.head_dim), dtype=q_dtype, device=self.device)
         _call(E, self._device, E.dynakv_norm_rope_store, self._ref, C.byref(qr), C.byref(kr), C.byref(vr), place, n, q_out.data_ptr(), qt,
@@ -248,7 +256,7 @@ class RowCache:
         if any(t is not None and t.data_ptr() % 16 for t in (k, v, k_exp, v_exp)):
             raise DynaKVError("the cache's tensors have to be 16-byte aligned")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
-        self._tensors = tuple((t, t.data_ptr()) for t in (k, v, k_exp, v_exp) if t is not None)
+        self._held = _Held(k, v, k_exp, v_exp)
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._status_at = self._status.data_ptr()
         self._c = _RowCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if k_exp is not None else None,
@@ -280,9 +288,9 @@ class RowCache:
         if k.dim() != 3:
             raise DynaKVError(f"expected k of three dimensions, got {tuple(k.shape)}")
         E, device = _env(), self._device
-        _held(E, self._tensors)
+        self._held.check(E)
         n, dtype = k.shape[0], k.dtype
-        shape, code = (n, self.n_kv_heads, self.head_dim), _float_type(dtype, "k")
+        shape, code = (n, self.n_kv_heads, self.head_dim), _float_type(E, dtype, "k")
         kr, vr = _heads(E, k, shape, device, dtype, code, "k"), _heads(E, v, shape, device, dtype, code, "v")
         _call(E, device, E.dynakv_rows_write, self._ref, C.byref(kr), C.byref(vr), _index(E, slots, (n,), device, "slots"), n, self._status_at)
 
@@ -291,7 +299,7 @@ class RowCache:
         fp32 cache, else bf16; zeros at and past ``lengths`` [sequences] int32.  ``page_table`` [sequences, pages per
         sequence] int32.  As [U, n, d] views these are the K, V of ``DynaKV.build_index``."""
         E, device = _env(), self._device
-        _held(E, self._tensors)
+        self._held.check(E)
         if page_table.dim() != 2 or n < 0 or first < 0:
             raise DynaKVError(f"expected page_table of two dimensions, n >= 0 and first >= 0, got {tuple(page_table.shape)}, {n}, {first}")
         b, per = page_table.shape
@@ -317,7 +325,7 @@ class RowCache:
         if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != device or q.data_ptr() % 16:
             raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {dtype} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
                               f"got {q.dtype} {tuple(q.shape)} on {q.device}")
-        _held(E, self._tensors)
+        self._held.check(E)
         if E.grad() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
             _no_gradient()
         n, heads, d = q.shape
