@@ -27,8 +27,19 @@ constexpr int ROW_THREADS = 128;
 //     out = f * (x * a + x_partner * b),   f = rsqrt(mean(x^2) + eps)  (1 without a norm),
 // in packed fp32 pairs; rows of v are the kind with a = 1, b = 0, f = 1.
 //
-// The angle in half turns, position * (inv_freq / pi), is one 64-bit product, and its whole turns are removed in 64 bits
-// before the rest is rounded to fp32: at position 2^20 the fp32 product alone would be off by 0.06 rad.
+// The angle in half turns, position * (inv_freq / pi), is one 64-bit product, and its whole turns are removed in 64 bits: at
+// position 2^20 the fp32 product alone would be off by 0.06 rad.  What the rest loses when it is rounded to fp32 (up to pi 2^-25 rad, more
+// than the sine's own rounding) is put back with the first term of the addition formulas; the next one is below 2^-47.
+__device__ __forceinline__ void head_angle(int position, float inv_freq, float* sine, float* cosine) {
+    const double turns = (double)position * ((double)inv_freq * 0.31830988618379067154);   // half turns
+    const double part = turns - 2.0 * rint(turns * 0.5);
+    const float f = (float)part, left = (float)(part - (double)f) * 3.14159265f;
+    float s, c;
+    sincospif(f, &s, &c);
+    *sine = fmaf(left, c, s);
+    *cosine = fmaf(-left, s, c);
+}
+
 constexpr int ROPE_THREADS = 64;           // two warps: the fold below is shared by twice as many rows as with four
 template <int HD, typename T, bool STORE, bool INTER>
 __global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(HeadRowsDev q, HeadRowsDev k, HeadRowsDev v, int vec, dynakv_rotary ro,
@@ -54,9 +65,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(HeadRowsDev q, HeadR
     if (STORE && slot >= 0 && !slot_ok && status && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(status, DYNAKV_ST_BOUNDS);
     const int half = ro.rotary_dim / 2;
     if ((int)threadIdx.x < half) {                         // half <= 64
-        const double turns = (double)positions[t] * ((double)ro.inv_freq[threadIdx.x] * 0.31830988618379067154);   // half turns
-        const float f = (float)(turns - 2.0 * rint(turns * 0.5));
-        sincospif(f, &sin_s[threadIdx.x], &cos_s[threadIdx.x]);
+        head_angle(positions[t], ro.inv_freq[threadIdx.x], &sin_s[threadIdx.x], &cos_s[threadIdx.x]);
     }
     __syncthreads();
     const bool turned = l * 8 < ro.rotary_dim;             // rotary_dim is a multiple of 16: a lane is wholly in or out
@@ -195,9 +204,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, 13) k_norm_rope_whole(HeadRowsDe
     const bool slot_ok = slot >= 0 && slot < cache.n_pages * PAGE;
     if (STORE && slot >= 0 && !slot_ok && status && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(status, DYNAKV_ST_BOUNDS);
     if ((int)threadIdx.x < H2) {
-        const double turns = (double)positions[t] * ((double)ro.inv_freq[threadIdx.x] * 0.31830988618379067154);   // half turns
-        const float f = (float)(turns - 2.0 * rint(turns * 0.5));
-        sincospif(f, &sin_s[threadIdx.x], &cos_s[threadIdx.x]);
+        head_angle(positions[t], ro.inv_freq[threadIdx.x], &sin_s[threadIdx.x], &cos_s[threadIdx.x]);
     }
     __syncthreads();
     // lo' = lo * (w_lo cos) - hi * (w_hi sin), hi' = hi * (w_hi cos) + lo * (w_lo sin)
