@@ -375,10 +375,11 @@ int dynakv_attend_rows_noalloc(const float* q, const void* K, const void* V, int
  *
  * What a serving program does with keys, values and queries before they are in the index or while they must stay
  * outside it: the norm and rotary embedding that make the q, k that dynakv_append and dynakv_decode_step take; a paged
- * cache for prompts that are still being prefilled, for sequences too short to be clustered, for layers left dense, and
- * for drafted tokens (an append cannot be taken back, so a draft waits here until it is accepted); attention over such
- * a cache for one new token or for a tree of drafted ones; and reading the rows back as the arrays dynakv_build_index
- * takes.
+ * cache for prompts that are still being prefilled, for sequences too short to be clustered and for layers left dense;
+ * attention over such a cache for one new token or for a tree of drafted ones; and reading the rows back as the arrays
+ * dynakv_build_index takes.  A sequence that drafts tokens has all its rows here, not in an index: an append cannot be taken
+ * back, and dynakv_decode_step gives no log-sum-exp with which its attention over the index could be merged with
+ * attention over drafts.
  *
  * These calls need no context and allocate nothing.  They enqueue work on cuda_stream (a cudaStream_t, NULL = default
  * stream) of the CURRENT device, where all pointers must live, and return at once; they can be captured into a CUDA
@@ -474,7 +475,7 @@ int dynakv_rows_read(const dynakv_row_cache* cache, const int32_t* page_table, i
  * q, out: [n_tokens][n_heads][head_dim], contiguous and 16-byte aligned, fp32 for a DYNAKV_F32 cache, else bf16;
  * lse: [n_tokens][n_heads] fp32, may be NULL.  Tokens of no sequence, before q_start[0] or from q_start[n_seqs] on, are left as they were
  * in both.  n_heads is 1 to 8 times n_kv_heads;
- * max_tree 1 .. 256; tree_mask [n_tokens][mask_words], mask_words 1 .. 4 (rows past the last word are not seen).
+ * max_tree 1 .. 256 (a prompt attends in chunks of at most so many tokens, each of which reads all rows before it); tree_mask [n_tokens][mask_words], mask_words 1 .. 4 (rows past the last word are not seen).
  * Logits, weights' sums and outputs are accumulated in fp32.  Weights enter the products with V in fp32 (DYNAKV_F32), to 2^-17
  * (DYNAKV_BF16, and DYNAKV_FP8 with more than 64 query rows, max_tree * n_heads / n_kv_heads, per KV head) or, DYNAKV_FP8 with up
  * to 64 query rows, as f16: p_j * 2^exp_j is off by 2^-12 of itself down to 2^-26 of the token's largest, below that by 2^-37 of

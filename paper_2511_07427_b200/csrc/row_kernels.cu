@@ -176,7 +176,8 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(HeadRowsDev q, HeadR
 // The same for the usual case, whole heads rotated in half-split pairs (rotary_dim = head_dim): a lane takes the eight elements
 // at l * 8 and the eight at l * 8 + head_dim / 2, so that every pair lies inside it.  No exchange of partners, half the
 // lanes per row and half the per-row instructions (8192 tokens of 32 + 8 heads: 43 us with the kernel above, 34 us with
-// this one, against 26 us at the measured copy rate).  72 registers: 13 blocks per SM (96: 37 us; 64: 37 us).
+// this one, against 26 us at the measured copy rate).  72 registers, 40 to 68 bytes spilled in most variants: 13 blocks per SM
+// (96 registers: 37 us; 64: 37 us).
 template <int HD, typename T, bool STORE>
 __global__ void __launch_bounds__(ROPE_THREADS, 13) k_norm_rope_whole(HeadRowsDev q, HeadRowsDev k, HeadRowsDev v, int vec, dynakv_rotary ro,
                                                                   const int* __restrict__ positions, void* q_out, int q_f32,
@@ -428,7 +429,7 @@ static int norm_rope(const dynakv_rotary* ro, const dynakv_head_rows* q, const d
     const bool whole = !ro->interleaved && ro->rotary_dim == ro->head_dim;
     const int rpp = ROPE_THREADS / (ro->head_dim / (whole ? 16 : 8));
     const int rows = ro->n_heads + ro->n_kv_heads * (cache ? 2 : 1), chunks = (rows + rpp - 1) / rpp;
-    // a whole token per block once there are two blocks for every SM (148), which shares the sines and the folded constants by all
+    // a whole token per block once there are two blocks for every SM of a B200 (148), which shares the sines and the folded constants by all
     // of its rows; fewer tokens (a decode step) spread over the SMs, one pass per block
     const int passes = n >= 148 * 2 ? chunks : 1;
     const dim3 grid((unsigned)n, (unsigned)((chunks + passes - 1) / passes));

@@ -1266,10 +1266,15 @@ static TreeSpace tree_space(int ctas, int rt, int hd) {
     return s;
 }
 
-// Which kernel, and how many CTAs with how many rows per tile.  The tcgen05 kernel pays from so many query rows per KV head on
-// (4 sequences of 32768 rows, 8 KV heads; mma.sync against tcgen05 in us).  bf16: 16 rows 93 / 99, 32 rows 100 / 101, 48 rows
-// 176 / 101.  FP8, whose rows the tcgen05 kernel has to convert in shared memory: 64 rows 188 / 244, 80 rows 270 / 247, 128 rows
-// 352 / 263.
+// Which kernel, and how many CTAs with how many rows per tile.  The tcgen05 kernel pays from so many query rows per KV head on;
+// mma.sync / tcgen05 in us, 8 KV heads:
+//                   bf16: 16 rows   32 rows    40 rows    64 rows | FP8: 48 rows   64 rows    80 rows    128 rows
+//   4 x 32768, d = 128   93 / 100  100 / 101  176 / 104  177 / 104 |  188 / 241  191 / 241  274 / 245  356 / 258
+//   16 x 4096, d = 128   46 / 53    51 / 54    83 / 56    86 / 58  |   88 / 113   91 / 114  120 / 116  161 / 122
+//   1 x 2048, d = 128    17 / 19    18 / 20    22 / 20    23 / 20  |   24 / 23    25 / 24    26 / 24    28 / 25
+//   4 x 32768, d = 64    53 / 84    63 / 84   109 / 84   109 / 85  |  130 / 171  131 / 172  188 / 178  243 / 189
+// (FP8 rows have to be converted in shared memory there.)  Spilled on mma.sync with 32 and 64 rows of 128 elements: FP8 134 to
+// 138 bytes a thread, bf16 54, fp32 78.
 #ifndef DKV_TREE_TC_BF16
 #define DKV_TREE_TC_BF16 33
 #endif

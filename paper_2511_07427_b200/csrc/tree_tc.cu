@@ -1,8 +1,11 @@
 // Tree attention on the tcgen05 tensor cores: bf16 and FP8 rows, tiles of 128 or 256 query rows (token, head of the group).
 //
 // With R query rows per KV head a bf16 row of K and V (512 bytes at d = 128) meets 4 d R flops: from a few dozen rows on the
-// mma.sync kernel is bound by the legacy tensor pipe (one m16n8k16 per 8.2 cycles and scheduler), while tcgen05 keeps
-// the call near the HBM side up to R = 256.
+// mma.sync kernel is bound by the legacy tensor pipe (one m16n8k16 per 8.2 cycles and scheduler).  On tcgen05 the softmax's
+// instructions per logit set the pace: bf16 trees of 16 (R = 64) over 4 x 32768 rows take 105 us in a burst and 120 when run for long, of 64
+// (R = 256) over 2 x 34816 rows 115 and 132, with all pages read from L2 still 91 and 114; the bytes alone would take 79 and 43.
+// FP8 rows: 244 us at R = 80 and 259 at R = 128 over 4 x 32768 rows, whose bytes take 40, because four warps convert every
+// element and the softmax has 128 registers a thread (282 to 298 bytes spilled; bf16 rows: 168 registers, 18 to 26 bytes).
 //
 // One CTA per SM walks over its range of pages (tree_plan.cuh) in stages of four pages (128 keys) of K and of V.  Two streams
 // work on every stage, each with logits S, a running softmax and an output sum O of its own in tensor memory: with up to

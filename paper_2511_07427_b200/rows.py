@@ -317,7 +317,7 @@ class RowCache:
         them; the last as many of its ``kv_len`` [sequences] int32 rows in ``page_table`` [sequences, pages] int32 are their own, the others the
         context, which every token sees.  ``tree_mask`` [tokens, words] int64: bit j of a token's words says that it
         sees row j of its tree (None: a chain, j <= i).  ``scale`` defaults to 1 / sqrt(d).  lse [tokens, heads]
-        fp32 is the natural logarithm of the weights' sum, for merging with attention over other rows.  A token that sees
+        fp32 is the natural logarithm of the weights' sum, for merging with other calls of this kind.  A token that sees
         nothing gets zeros and -inf.  Tokens of no sequence (before q_start[0], behind the last sequence: a padded batch) are left as
         they are in ``out`` and ``lse``, so what they hold is unspecified in one that is not passed in.  Neither may share memory with
         the other or with anything that is read."""
