@@ -25,7 +25,7 @@ constexpr int ROW_THREADS = 128;
 // per warp and pass and moved 2.4 TB/s), so the constants of a lane's eight elements are folded once per kind of
 // row and block: with a = weight * cos, b = weight of the partner * (+-) sin,
 //     out = f * (x * a + x_partner * b),   f = rsqrt(mean(x^2) + eps)  (1 without a norm),
-// in packed fp32 pairs; rows of v are the kind with a = 1, b = 0, f = 1.
+// in packed fp32 pairs; rows of v stay as they are.
 //
 // The angle in half turns, position * (inv_freq / pi), is one 64-bit product, and its whole turns are removed in 64 bits: at
 // position 2^20 the fp32 product alone would be off by 0.06 rad.  What the rest loses when it is rounded to fp32 (up to pi 2^-25 rad, more
@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(HeadRowsDev q, HeadR
     int kind = -1;                                         // 0: q, 1: k, 2: v
     bool norm = false;
     auto fold = [&]() {
-        const float* w = kind == 0 ? ro.q_weight : kind == 1 ? ro.k_weight : nullptr;
+        const float* w = kind == 0 ? ro.q_weight : ro.k_weight;
         norm = w != nullptr;
         float own[8], other[8];
         if (norm) {
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(HeadRowsDev q, HeadR
         float c[8], s[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) { c[i] = 1.f; s[i] = 0.f; }
-        if (turned && kind < 2) {
+        if (turned) {
             if constexpr (INTER) {
                 const float4 cv = *reinterpret_cast<const float4*>(cos_s + l * 4), sv = *reinterpret_cast<const float4*>(sin_s + l * 4);
                 c[0] = c[1] = cv.x; c[2] = c[3] = cv.y; c[4] = c[5] = cv.z; c[6] = c[7] = cv.w;
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(HeadRowsDev q, HeadR
         if (p + 1 < passes) next = load_row(r + RPP);
         const bool live = r < n_rows;
         const int now = r < n_q ? 0 : !STORE || r < n_q + n_k ? 1 : 2;
-        if (now != kind) { kind = now; fold(); }
+        if (now != kind) { kind = now; if (kind < 2) fold(); }
         float2 sq = make_float2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < 4; i++) { const float2 y = make_float2(x[2 * i], x[2 * i + 1]); sq = fma2(y, y, sq); }
@@ -140,16 +140,18 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_norm_rope(HeadRowsDev q, HeadR
 #pragma unroll
         for (int o = LG / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         const float f = norm ? rsqrtf(ss * (1.f / HD) + ro.eps) : 1.f;
-        if (!turned || kind == 2) {                        // no partner: an infinity there would make 0 * inf
+        if (!turned) {                                     // no partner: an infinity there would make 0 * inf
 #pragma unroll
             for (int i = 0; i < 8; i++) y[i] = 0.f;
         }
         const float2 ff = make_float2(f, f);
+        if (kind < 2) {                                    // rows of v stay as they are, signs of zeros too
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            float2 o = mul2(make_float2(y[2 * i], y[2 * i + 1]), b[i]);
-            o = mul2(fma2(make_float2(x[2 * i], x[2 * i + 1]), a[i], o), ff);
-            x[2 * i] = o.x; x[2 * i + 1] = o.y;
+            for (int i = 0; i < 4; i++) {
+                float2 o = mul2(make_float2(y[2 * i], y[2 * i + 1]), b[i]);
+                o = mul2(fma2(make_float2(x[2 * i], x[2 * i + 1]), a[i], o), ff);
+                x[2 * i] = o.x; x[2 * i + 1] = o.y;
+            }
         }
         if (kind == 0) {
             if (live) {

@@ -81,3 +81,25 @@ def test_values_that_are_no_numbers_stay_in_their_rows(d, rot, inter):
     rows[6, 0] = False
     assert torch.equal(kept(wild, wild.k)[rows], kept(clean, clean.k)[rows])
     assert torch.equal(torch.nan_to_num(kept(wild, wild.v), nan=7.0), torch.nan_to_num(v.cpu(), nan=7.0))
+
+
+@pytest.mark.parametrize("cache_type", [P.F32, P.BF16, P.FP8])
+@pytest.mark.parametrize("d,rot,inter", FORMS)
+def test_values_are_stored_as_the_write_stores_them(cache_type, d, rot, inter):
+    """Zeros of either sign included."""
+    n, h, hk = 33, 3, 2
+    q, k, v = (x.clone() for x in _joint(n, h, hk, d, torch.bfloat16, "joint"))
+    v[:, :, ::3] = -0.0
+    v[5], v[6] = -0.0, 0.0
+    inv_freq = (10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / max(rot, 1))).float().cuda()
+    ro = P.HeadRotary(h, hk, d, inv_freq, interleaved=inter)
+    at = torch.arange(n, dtype=torch.int32, device="cuda")
+    a, b = (P.RowCache.allocate(2, hk, d, cache_type) for _ in range(2))
+    for c in (a, b):
+        c.v.view(torch.uint8).zero_()
+        if c.v_exp is not None:
+            c.v_exp.zero_()
+    ro.store(q, k, v, at, a, at)
+    b.write(k, v, at)
+    assert torch.equal(a.v.view(torch.uint8), b.v.view(torch.uint8))
+    assert a.v_exp is None or torch.equal(a.v_exp, b.v_exp)
