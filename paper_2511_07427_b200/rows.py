@@ -183,10 +183,11 @@ class HeadRotary:
         self._ref = C.byref(self._c)
 
     def _q_k(self, E, q, k):
-        if q.dim() != 3:
-            raise DynaKVError(f"expected q of three dimensions, got {tuple(q.shape)}")
+        shape = q.shape
+        if len(shape) != 3:
+            raise DynaKVError(f"expected q of three dimensions, got {tuple(shape)}")
         self._held.check(E)
-        n, dtype = q.shape[0], q.dtype
+        n, dtype = shape[0], q.dtype
         code = _float_type(E, dtype, "q")
         return n, dtype, code, _heads(E, q, (n, self.n_heads, self.head_dim), self._device, dtype, code, "q"), \
             _heads(E, k, (n, self.n_kv_heads, self.head_dim), self._device, dtype, code, "k")
@@ -196,7 +197,7 @@ class HeadRotary:
         (q, k) normed and rotated, contiguous, of ``q_dtype`` and ``k_dtype`` (default: the input's).  With one token per
         sequence an fp32 q is what ``DynaKV.decode_step`` takes and k what ``DynaKV.append`` takes, as [U, G, d] and
         [U, d] views."""
-        E, device = _env(), self.device
+        E, device = _env_made or _env(), self.device
         n, dtype, code, qr, kr = self._q_k(E, q, k)
         q_dtype, k_dtype = q_dtype or dtype, k_dtype or dtype
         qt = code if q_dtype is dtype else _float_type(E, q_dtype, "q_dtype")
@@ -210,7 +211,7 @@ class HeadRotary:
     def store(self, q, k, v, positions, cache: "RowCache", slots, q_dtype=None):
         """As ``apply``, with the keys and the values v [n, KV heads, d] going into ``slots`` [n] int32 of ``cache``
         (``RowCache.write``'s rules) in the same launch.  Returns q."""
-        E = _env()
+        E = _env_made or _env()
         n, dtype, code, qr, kr = self._q_k(E, q, k)
         vr = _heads(E, v, (n, self.n_kv_heads, self.head_dim), self._device, dtype, code, "v")
         cache._held.check(E)
@@ -285,11 +286,12 @@ class RowCache:
     def write(self, k, v, slots) -> None:
         """Rows k, v [n, KV heads, d] (fp32 or bf16, any token and head strides) into ``slots`` [n] int32, rounded to the
         cache's type.  A negative slot skips its token; slots >= 0 must differ."""
-        if k.dim() != 3:
-            raise DynaKVError(f"expected k of three dimensions, got {tuple(k.shape)}")
-        E, device = _env(), self._device
+        shape = k.shape
+        if len(shape) != 3:
+            raise DynaKVError(f"expected k of three dimensions, got {tuple(shape)}")
+        E, device = _env_made or _env(), self._device
         self._held.check(E)
-        n, dtype = k.shape[0], k.dtype
+        n, dtype = shape[0], k.dtype
         shape, code = (n, self.n_kv_heads, self.head_dim), _float_type(E, dtype, "k")
         kr, vr = _heads(E, k, shape, device, dtype, code, "k"), _heads(E, v, shape, device, dtype, code, "v")
         _call(E, device, E.dynakv_rows_write, self._ref, C.byref(kr), C.byref(vr), _index(E, slots, (n,), device, "slots"), n, self._status_at)
@@ -298,11 +300,12 @@ class RowCache:
         """Rows [first, first + n) of every sequence in order, (K, V) of shape [sequences, KV heads, n, d], fp32 for an
         fp32 cache, else bf16; zeros at and past ``lengths`` [sequences] int32.  ``page_table`` [sequences, pages per
         sequence] int32.  As [U, n, d] views these are the K, V of ``DynaKV.build_index``."""
-        E, device = _env(), self._device
+        E, device = _env_made or _env(), self._device
         self._held.check(E)
-        if page_table.dim() != 2 or n < 0 or first < 0:
-            raise DynaKVError(f"expected page_table of two dimensions, n >= 0 and first >= 0, got {tuple(page_table.shape)}, {n}, {first}")
-        b, per = page_table.shape
+        rows = page_table.shape
+        if len(rows) != 2 or n < 0 or first < 0:
+            raise DynaKVError(f"expected page_table of two dimensions, n >= 0 and first >= 0, got {tuple(rows)}, {n}, {first}")
+        b, per = rows
         table, lens = _index(E, page_table, (b, per), device, "page_table"), _index(E, lengths, (b,), device, "lengths")
         shape = (b, self.n_kv_heads, n, self.head_dim)
         K, V = E.empty(shape, dtype=self._io, device=self.device), E.empty(shape, dtype=self._io, device=self.device)
@@ -321,17 +324,19 @@ class RowCache:
         nothing gets zeros and -inf.  Tokens of no sequence (before q_start[0], behind the last sequence: a padded batch) are left as
         they are in ``out`` and ``lse``, so what they hold is unspecified in one that is not passed in.  Neither may share memory with
         the other or with anything that is read."""
-        E, device, dtype = _env(), self._device, self._io
-        if q.dim() != 3 or q.shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != device or q.data_ptr() % 16:
+        E, device, dtype = _env_made or _env(), self._device, self._io
+        shape = q.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != device or q.data_ptr() % 16:
             raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {dtype} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
                               f"got {q.dtype} {tuple(q.shape)} on {q.device}")
         self._held.check(E)
         if E.grad() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
             _no_gradient()
-        n, heads, d = q.shape
-        if page_table.dim() != 2:
-            raise DynaKVError(f"expected page_table of two dimensions, got {tuple(page_table.shape)}")
-        b, per = page_table.shape
+        n, heads, d = shape
+        rows = page_table.shape
+        if len(rows) != 2:
+            raise DynaKVError(f"expected page_table of two dimensions, got {tuple(rows)}")
+        b, per = rows
         size = self._workspace.get((heads, max_tree))
         if size is None:
             size = self._workspace_bytes(E, heads, max_tree)
