@@ -490,6 +490,43 @@ int dynakv_attend_tree(const dynakv_row_cache* cache, const void* q, int32_t n_h
 /* Bytes of workspace for calls with this cache, n_heads and max_tree on the current device, or a negative code. */
 int64_t dynakv_attend_tree_workspace(const dynakv_row_cache* cache, int32_t n_heads, int32_t max_tree);
 
+/* What the scores of dynakv_attend_chunk are.  With s = scale * q . k, P the place of the token's own row in its sequence and j a row:
+ *   softcap > 0:      s = softcap * tanh(s / softcap)
+ *   slopes != NULL:   s = s - slopes[head] * |P - j|          ([n_heads] fp32, on the device)
+ *   rows_from, rows_to ([n_tokens] int32, on the device, each may be NULL), window: the token sees row j if
+ *       rows_from[token] <= j (NULL: 0 <= j),  P - window < j (window 0: no such bound),  j < rows_to[token] (NULL: j <= P),
+ *     of the rows that its sequence has.  NULL, NULL, 0 is the causal mask; rows_from = first row of the token's document a document
+ *     mask; rows_to = max(P + 1, prefix length) a prefix that all of it sees. */
+typedef struct dynakv_scores {
+    float scale;
+    float softcap;                 /* >= 0, 0: none */
+    int32_t window;                /* >= 0, 0: none */
+    const float* slopes;
+    const int32_t* rows_from;
+    const int32_t* rows_to;
+} dynakv_scores;
+
+/* Attention of a chunk of new tokens per sequence over a paged cache: prompts in chunks of any length, batches of prompts and
+ * single tokens, layers with a sliding window, capped scores, a bias by distance, documents or a prefix.
+ *
+ * The arrays are those of dynakv_attend_tree: sequence b has the T_b = q_start[b + 1] - q_start[b] <= max_chunk tokens from
+ * q_start[b] on, whose own rows are the LAST T_b of its kv_len[b] (token i's is P = kv_len[b] - T_b + i), stored before this call.
+ *     out[i][hq] = sum_j p_j v_j / sum_j p_j,  lse[i][hq] = ln sum_j p_j,  p_j = exp(s_j)
+ * over the rows that the token sees; one that sees none gets zeros and -infinity.  Rows it does not see do not count whatever they
+ * hold, NaN and infinities included (values that are no numbers among the V rows that are read make the call slow).  Logits, sums and
+ * outputs are accumulated in fp32.
+ * n_heads is 1 to 8 times n_kv_heads; max_chunk 1 .. 2^24.  Tokens of no sequence are left as they were.
+ * workspace: dynakv_attend_chunk_workspace() bytes of device memory, 16-byte aligned, contents of no interest before and after;
+ * calls that may overlap need one each. */
+int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
+                        int32_t n_seqs, int32_t max_chunk, const int32_t* page_table, int32_t pages_per_seq, const int32_t* kv_len,
+                        const dynakv_scores* scores, void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                        uint32_t* status, void* cuda_stream);
+
+/* Bytes of workspace for calls of n_tokens tokens in n_seqs sequences with this cache, n_heads and max_chunk on the current device, or
+ * a negative code. */
+int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, int32_t n_heads, int64_t n_tokens, int32_t n_seqs, int32_t max_chunk);
+
 #ifdef __cplusplus
 }
 #endif

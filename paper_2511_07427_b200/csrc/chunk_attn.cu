@@ -1,0 +1,80 @@
+// dynakv_attend_chunk: which kernel a call takes, and its launch.
+#include "tree_rows.cuh"
+
+namespace dkv {
+
+template <int HD, int DT, int RG>
+static int chunk_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
+    using C = TreeCfg<HD, DT, RG, true>;
+    const int grid = sms * C::per_sm;
+    static std::atomic<unsigned long long> allowed{0};
+    if (!allow_smem(k_tree_attn<HD, DT, RG, true>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
+    if (launch_pdl(k_tree_attn<HD, DT, RG, true>, dim3(grid), dim3(C::threads), C::smem, st, mk, mv, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
+    return tree_merge_launch(HD, C::RT, DT == DYNAKV_F32, a, grid, st);
+}
+template <int HD, int DT>
+static int chunk_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
+    return rg == 0 ? chunk_launch<HD, DT, 0>(mk, mv, a, sms, st) : rg == 1 ? chunk_launch<HD, DT, 1>(mk, mv, a, sms, st) : rg == 2 ? chunk_launch<HD, DT, 2>(mk, mv, a, sms, st) : chunk_launch<HD, DT, 4>(mk, mv, a, sms, st);
+}
+
+struct ChunkKind { int rg, rows, ctas; };
+static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int max_chunk, int sms) {
+    const bool f32 = c->kv_dtype == DYNAKV_F32;
+    const int rg = row_groups((int)min(1000ll, (long long)max_chunk * (n_heads / c->n_kv_heads)), f32);
+    return {rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2)};
+}
+
+static bool chunk_shape_ok(const dynakv_row_cache* c, int n_heads, int64_t n_tokens, int n_seqs, int max_chunk) {
+    return row_cache_ok(c) && n_heads >= 1 && n_heads % c->n_kv_heads == 0 && n_heads / c->n_kv_heads <= MAX_G && max_chunk >= 1 && max_chunk <= (1 << 24) &&
+           n_tokens >= 0 && n_tokens < (1ll << 31) && n_seqs >= 0;
+}
+
+}  // namespace dkv
+
+using namespace dkv;
+
+extern "C" int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, int32_t n_heads, int64_t n_tokens, int32_t n_seqs, int32_t max_chunk) {
+    if (!chunk_shape_ok(cache, n_heads, n_tokens, n_seqs, max_chunk)) return DYNAKV_ERR_ARG;
+    int rc;
+    const int sms = sm_count(&rc);
+    if (rc != DYNAKV_OK) return rc;
+    const ChunkKind k = chunk_kind(cache, n_heads, max_chunk, sms);
+    return (int64_t)tree_space(k.ctas, k.rows, cache->head_dim).bytes;
+}
+
+extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
+                                   int32_t n_seqs, int32_t max_chunk, const int32_t* page_table, int32_t pages_per_seq, const int32_t* kv_len,
+                                   const dynakv_scores* scores, void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                                   uint32_t* status, void* cuda_stream) {
+    if (!chunk_shape_ok(cache, n_heads, n_tokens, n_seqs, max_chunk) || pages_per_seq < 0 || pages_per_seq >= (1 << 26) || !scores ||
+        !(fabsf(scores->scale) <= FLT_MAX) || !(scores->softcap >= 0.f && scores->softcap <= FLT_MAX) || scores->window < 0) return DYNAKV_ERR_ARG;
+    if (n_tokens == 0 || n_seqs == 0) return DYNAKV_OK;
+    if (!q || !q_start || (!page_table && pages_per_seq > 0) || !kv_len || !out || !workspace) return DYNAKV_ERR_ARG;
+    if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)workspace) & 15) return DYNAKV_ERR_ARG;
+    int rc;
+    const int sms = sm_count(&rc);
+    if (rc != DYNAKV_OK) return rc;
+    const ChunkKind kind = chunk_kind(cache, n_heads, max_chunk, sms);
+    const TreeSpace sp = tree_space(kind.ctas, kind.rows, cache->head_dim);
+    if (workspace_bytes < (int64_t)sp.bytes) return DYNAKV_ERR_ARG;
+    TreeArgs a = tree_args(cache, q, n_heads, n_tokens, q_start, n_seqs, max_chunk, page_table, pages_per_seq, kv_len, out, lse, workspace, sp, status);
+    a.scale = scores->scale;
+    a.cap = scores->softcap;
+    a.slopes = scores->slopes;
+    a.window = min(scores->window, 1 << 30);
+    a.rows_from = scores->rows_from; a.rows_to = scores->rows_to;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    // an error left behind by an earlier, unrelated call on this thread must not be reported as this call's
+    cudaGetLastError();
+    CUtensorMap mk, mv;
+    if (!tree_page_map(&mk, cache, cache->k, true) || !tree_page_map(&mv, cache, cache->v, true)) return DYNAKV_ERR_CUDA;
+    const int rg = kind.rg;
+    if (cache->head_dim == 128) {
+        if (cache->kv_dtype == DYNAKV_F32) return chunk_launch_rows<128, DYNAKV_F32>(rg, mk, mv, a, sms, st);
+        if (cache->kv_dtype == DYNAKV_BF16) return chunk_launch_rows<128, DYNAKV_BF16>(rg, mk, mv, a, sms, st);
+        return chunk_launch_rows<128, DYNAKV_FP8>(rg, mk, mv, a, sms, st);
+    }
+    if (cache->kv_dtype == DYNAKV_F32) return chunk_launch_rows<64, DYNAKV_F32>(rg, mk, mv, a, sms, st);
+    if (cache->kv_dtype == DYNAKV_BF16) return chunk_launch_rows<64, DYNAKV_BF16>(rg, mk, mv, a, sms, st);
+    return chunk_launch_rows<64, DYNAKV_FP8>(rg, mk, mv, a, sms, st);
+}

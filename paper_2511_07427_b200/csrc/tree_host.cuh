@@ -1,4 +1,4 @@
-// Host side of dynakv_attend_tree's kernels: tensor maps of a row cache, the device's SM count, the workspace.
+// Host side of the kernels behind dynakv_attend_tree and dynakv_attend_chunk: tensor maps of a row cache, the device's SM count, the workspace.
 #pragma once
 
 #include <cuda.h>
@@ -68,6 +68,39 @@ static bool allow_smem(K kernel, int bytes, std::atomic<unsigned long long>& don
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
     done.fetch_or(1ull << dev, std::memory_order_release);
     return true;
+}
+
+// 16 rows of a tile per row group; the groups needed for all rows of a sequence in one tile, up to four (0: one of few rows)
+static inline int row_groups(int max_rows, bool f32) { return max_rows <= (f32 ? 4 : 8) ? 0 : max_rows <= 16 ? 1 : max_rows <= 32 ? 2 : 4; }
+
+struct TreeSpace { size_t acc, ml, desc, bytes; };
+static inline TreeSpace tree_space(int ctas, int rt, int hd) {
+    TreeSpace s;
+    s.acc = 0;
+    s.ml = (size_t)ctas * 2 * rt * hd * 4;
+    s.desc = s.ml + (size_t)ctas * 2 * rt * 8;
+    s.bytes = s.desc + (size_t)ctas * 8 * 4;
+    return s;
+}
+
+
+static inline TreeArgs tree_args(const dynakv_row_cache* cache, const void* q, int n_heads, int64_t n_tokens, const int* q_start, int n_seqs, int max_tokens,
+                                 const int* page_table, int pages_per_seq, const int* kv_len, void* out, float* lse, void* workspace, const TreeSpace& sp,
+                                 unsigned* status) {
+    TreeArgs a = {};
+    a.q = q; a.q_start = q_start; a.page_table = page_table; a.kv_len = kv_len;
+    a.out = out; a.lse = lse;
+    char* ws = reinterpret_cast<char*>(workspace);
+    a.acc = reinterpret_cast<float*>(ws + sp.acc);
+    a.ml = reinterpret_cast<float2*>(ws + sp.ml);
+    a.desc = reinterpret_cast<int*>(ws + sp.desc);
+    a.status = status;
+    a.kpool = reinterpret_cast<const unsigned char*>(cache->k); a.vpool = reinterpret_cast<const unsigned char*>(cache->v);
+    a.kexp = reinterpret_cast<const signed char*>(cache->k_exp); a.vexp = reinterpret_cast<const signed char*>(cache->v_exp);
+    a.n_tokens = n_tokens; a.n_pages = cache->n_pages;
+    a.n_seqs = n_seqs; a.max_tree = max_tokens; a.pages_per_seq = pages_per_seq;
+    a.G = n_heads / cache->n_kv_heads; a.Hq = n_heads; a.Hk = cache->n_kv_heads;
+    return a;
 }
 
 // tcgen05 kernel (tree_tc.cu): bf16 and FP8 rows, tiles of 128 or 256 query rows, one CTA per SM.

@@ -35,6 +35,12 @@ struct TreeArgs {
     long long n_tokens, n_pages;
     int n_seqs, max_tree, pages_per_seq, mask_words, G, Hq, Hk;
     float scale;                           // logits are q . k * scale
+    // dynakv_attend_chunk
+    const int* rows_from;                  // [n_tokens] first row that a token sees, NULL: 0
+    const int* rows_to;                    // [n_tokens] end of the rows that it sees, NULL: its own row + 1
+    const float* slopes;                   // [Hq] lowers a logit by slope * distance, may be NULL
+    float cap;                             // > 0: logits become cap * tanh(logit / cap)
+    int window;                            // > 0: the last so many rows up to its own
 };
 enum { DESC_VALID = 0, DESC_FIRST = 1, DESC_Q0 = 2, DESC_T = 3, DESC_H = 4, DESC_RT = 5 };
 
@@ -42,20 +48,28 @@ __device__ __forceinline__ void tree_status(const TreeArgs& a, unsigned bit) {
     if (a.status) atomicOr(a.status, bit);
 }
 
+// dynakv_attend_chunk: the rows [lo, hi) that packed token `token`, whose own row is `place`, sees of a sequence of n.
+__device__ __forceinline__ void chunk_sees(const TreeArgs& a, int token, int place, int n, int& lo, int& hi) {
+    lo = a.rows_from ? a.rows_from[token] : 0;
+    if (a.window > 0) lo = max(lo, place + 1 - a.window);
+    hi = min(a.rows_to ? a.rows_to[token] : place + 1, n);
+}
+
 struct SeqInfo {
     int q0, T, n, pages, tiles;            // first packed token, drafted tokens, rows, pages (at least 1), row tiles
+    int from;                              // first page (MOD: pages that no token sees are left out)
     long long work;                        // pages of all the sequence's units
 };
 template <int RT>
-__device__ __forceinline__ SeqInfo seq_work(const TreeArgs& a, int q0, int T, int n) {
+__device__ __forceinline__ SeqInfo seq_work(const TreeArgs& a, int q0, int T, int n, int from, int pages) {
     SeqInfo s;
     s.q0 = q0; s.T = T; s.n = n;
-    s.pages = max(1, (n + PAGE - 1) / PAGE);
+    s.from = from; s.pages = pages;
     s.tiles = (T * a.G + RT - 1) / RT;
     s.work = (long long)s.pages * s.tiles * a.Hk;
     return s;
 }
-template <int RT>
+template <int RT, bool MOD>
 __device__ __forceinline__ SeqInfo seq_info(const TreeArgs& a, int b, bool report) {
     const int q0 = a.q_start[b], q1 = a.q_start[b + 1], n = a.kv_len[b];
     long long T = (long long)q1 - q0;
@@ -66,7 +80,23 @@ __device__ __forceinline__ SeqInfo seq_info(const TreeArgs& a, int b, bool repor
         T = max(0ll, min(T, min((long long)a.max_tree, a.n_tokens - q0)));
     }
     if (report && (bad_q || bad_n)) tree_status(a, DYNAKV_ST_BOUNDS);
-    return seq_work<RT>(a, q0, (int)T, (int)max(0ll, min((long long)n, rows)));
+    const int len = (int)max(0ll, min((long long)n, rows));
+    int from = 0, end = len;
+    if constexpr (MOD) {
+        const int place = len - (int)T;        // of the first token
+        if (!a.rows_from && !a.rows_to) {
+            from = a.window > 0 ? max(0, place + 1 - a.window) : 0;
+        } else {
+            from = len; end = 0;
+            for (int t = 0; t < T; t++) {
+                int lo, hi;
+                chunk_sees(a, q0 + t, place + t, len, lo, hi);
+                if (lo < hi) { from = min(from, max(lo, 0)); end = max(end, hi); }
+            }
+        }
+        from = from < end ? from / PAGE : 0;
+    }
+    return seq_work<RT>(a, q0, (int)T, len, from, max(1, (end + PAGE - 1) / PAGE - from));
 }
 
 struct Segment {
@@ -88,10 +118,10 @@ __device__ __forceinline__ long long mul_div(long long a, long long b, long long
     return p < (1ll << 32) && c < (1ll << 32) ? (long long)((unsigned)p / (unsigned)c) : p / c;
 }
 
-// Which range of the list the CTA has.  Every thread of the block (a multiple of 32, at most 1024) calls it; sh: 48 long longs.
+// Which range of the list the CTA has.  Every thread of the block (a multiple of 32, at most 1024) calls it; sh: 48 long longs (MOD: 80).
 // Up to 32 sequences: a lane takes one each, which needs one trip to memory and no block barrier, and what the walk will
 // look up is left in sh (the caller synchronises the block); more: the block scans them, and the walk loads them again.
-template <int RT>
+template <int RT, bool MOD = false>
 __device__ __forceinline__ Range tree_range(const TreeArgs& a, int min_pages, long long* sh) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, nw = nt >> 5, c = blockIdx.x;
     auto warp_scan = [&](long long x) {                    // inclusive
@@ -110,8 +140,8 @@ __device__ __forceinline__ Range tree_range(const TreeArgs& a, int min_pages, lo
         SeqInfo mine;
         mine.work = 0;
         if (lane < a.n_seqs) {
-            mine = seq_info<RT>(a, lane, c == 0 && warp == 0);
-            if (warp == 0) { int* to = reinterpret_cast<int*>(sh); to[lane] = mine.q0; to[32 + lane] = mine.T; to[64 + lane] = mine.n; }
+            mine = seq_info<RT, MOD>(a, lane, c == 0 && warp == 0);
+            if (warp == 0) { int* to = reinterpret_cast<int*>(sh); to[lane] = mine.q0; to[32 + lane] = mine.T; to[64 + lane] = mine.n; if (MOD) { to[96 + lane] = mine.from; to[128 + lane] = mine.pages; } }
         }
         const long long incl = warp_scan(mine.work);
         r.W = __shfl_sync(0xffffffffu, incl, 31);
@@ -134,7 +164,7 @@ __device__ __forceinline__ Range tree_range(const TreeArgs& a, int min_pages, lo
     const bool one = a.n_seqs <= nt;
     long long v = 0, incl = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += nt) {
-        v = b0 + tid < a.n_seqs ? seq_info<RT>(a, b0 + tid, c == 0).work : 0;
+        v = b0 + tid < a.n_seqs ? seq_info<RT, MOD>(a, b0 + tid, c == 0).work : 0;
         long long total;
         incl = scan(v, total);
         r.W += total;
@@ -147,7 +177,7 @@ __device__ __forceinline__ Range tree_range(const TreeArgs& a, int min_pages, lo
         for (int b0 = 0; b0 < a.n_seqs; b0 += nt) {
             long long total = r.W;
             if (!one) {
-                v = b0 + tid < a.n_seqs ? seq_info<RT>(a, b0 + tid, false).work : 0;
+                v = b0 + tid < a.n_seqs ? seq_info<RT, MOD>(a, b0 + tid, false).work : 0;
                 incl = scan(v, total);
             }
             const long long lo = run + incl - v, hi = run + incl;
@@ -162,15 +192,16 @@ __device__ __forceinline__ Range tree_range(const TreeArgs& a, int min_pages, lo
 }
 
 // The CTA's segments in order.
-template <int RT>
+template <int RT, bool MOD = false>
 struct SegmentWalk {
     Range r;
     const long long* sh;
     __device__ __forceinline__ SegmentWalk(const Range& range, const long long* shared) : r(range), sh(shared) {}
     __device__ __forceinline__ SeqInfo look(const TreeArgs& a) const {
-        if (a.n_seqs > 32) return seq_info<RT>(a, r.b, false);
+        if (a.n_seqs > 32) return seq_info<RT, MOD>(a, r.b, false);
         const int* from = reinterpret_cast<const int*>(sh);
-        return seq_work<RT>(a, from[r.b], from[32 + r.b], from[64 + r.b]);
+        const int n = from[64 + r.b];
+        return seq_work<RT>(a, from[r.b], from[32 + r.b], n, MOD ? from[96 + r.b] : 0, MOD ? from[128 + r.b] : max(1, (n + PAGE - 1) / PAGE));
     }
     __device__ __forceinline__ bool next(const TreeArgs& a, Segment& g) {
         if (r.x >= r.end) return false;
@@ -184,6 +215,7 @@ struct SegmentWalk {
         g.q0 = s.q0; g.T = s.T; g.n = s.n;
         g.first = g.p0 == 0; g.last = g.p1 == s.pages;
         g.unit_start = r.base + unit * s.pages;
+        if (MOD) { g.p0 += s.from; g.p1 += s.from; }
         r.x += g.p1 - g.p0;
         return true;
     }

@@ -14,6 +14,7 @@ from .binding import BF16, F32, FP8, DynaKVError, load_library
 
 PAGE = 32          # rows per cache page
 MAX_TREE = 256     # drafted tokens per sequence and call
+MAX_CHUNK = 1 << 24
 
 
 class _RowCache(C.Structure):
@@ -31,6 +32,11 @@ class _Rotary(C.Structure):
                 ("inv_freq", C.c_void_p)]
 
 
+class _Scores(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p), ("rows_from", C.c_void_p),
+                ("rows_to", C.c_void_p)]
+
+
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
 SIGNATURES = {
     "dynakv_norm_rope": (C.c_int, [_vp, _vp, _vp, _vp, _i64, _vp, _i32, _vp, _i32, _vp]),
@@ -40,6 +46,8 @@ SIGNATURES = {
 }
 SIGNATURES["dynakv_attend_tree"] = (C.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, C.c_float, _vp, _vp, _vp, _i64, _vp, _vp])
 SIGNATURES["dynakv_attend_tree_workspace"] = (_i64, [_vp, _i32, _i32])
+SIGNATURES["dynakv_attend_chunk"] = (C.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp])
+SIGNATURES["dynakv_attend_chunk_workspace"] = (_i64, [_vp, _i32, _i64, _i32, _i32])
 
 
 class _Env:
@@ -265,7 +273,7 @@ class RowCache:
         self._ref = C.byref(self._c)
         self._io = torch.float32 if self.kv_dtype == F32 else torch.bfloat16      # type of q, of the results and of rows read
         self._byte, self._scale = torch.uint8, self.head_dim ** -0.5
-        self._workspace = {}           # bytes attend_tree needs, by (heads, max_tree)
+        self._workspace = {}           # bytes attend_tree needs, by (heads, max_tree), and attend_chunk
 
     @classmethod
     def allocate(cls, n_pages: int, n_kv_heads: int, head_dim: int, kv_dtype: int = BF16, device="cuda") -> "RowCache":
@@ -324,19 +332,8 @@ class RowCache:
         nothing gets zeros and -inf.  Tokens of no sequence (before q_start[0], behind the last sequence: a padded batch) are left as
         they are in ``out`` and ``lse``, so what they hold is unspecified in one that is not passed in.  Neither may share memory with
         the other or with anything that is read."""
-        E, device, dtype = _env_made or _env(), self._device, self._io
-        shape = q.shape
-        if len(shape) != 3 or shape[2] != self.head_dim or q.dtype is not dtype or not q.is_contiguous() or q.get_device() != device or q.data_ptr() % 16:
-            raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {dtype} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
-                              f"got {q.dtype} {tuple(q.shape)} on {q.device}")
-        self._held.check(E)
-        if E.grad() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
-            _no_gradient()
-        n, heads, d = shape
-        rows = page_table.shape
-        if len(rows) != 2:
-            raise DynaKVError(f"expected page_table of two dimensions, got {tuple(rows)}")
-        b, per = rows
+        E, device = _env_made or _env(), self._device
+        n, heads, b, per = self._queries(E, q, page_table, out, lse)
         size = self._workspace.get((heads, max_tree))
         if size is None:
             size = self._workspace_bytes(E, heads, max_tree)
@@ -352,6 +349,69 @@ class RowCache:
             scale = self._scale
         elif not math.isfinite(scale):
             raise DynaKVError(f"scale is {scale}: expected a finite number")
+        out, lse = self._results(E, q, out, lse)
+        table, lens, start = _index(E, page_table, (b, per), device, "page_table"), _index(E, kv_len, (b,), device, "kv_len"), \
+            _index(E, q_start, (b + 1,), device, "q_start")
+        space = E.empty(size, dtype=self._byte, device=self.device)
+        _call(E, device, E.dynakv_attend_tree, self._ref, q.data_ptr(), heads, n, start, b, max_tree, table, per, lens, mask, words, scale,
+              out.data_ptr(), lse.data_ptr(), space.data_ptr(), size, self._status_at)
+        return out, lse
+
+    def attend_chunk(self, q, page_table, kv_len, q_start, max_chunk: int, scale=None, softcap: float = 0.0, window: int = 0, slopes=None,
+                     rows_from=None, rows_to=None, out=None, lse=None):
+        """Attention of a chunk of new tokens per sequence over the cache (``dynakv_attend_chunk``): (out, lse).
+
+        q, ``q_start``, ``kv_len``, ``page_table``, ``scale``, ``out`` and ``lse`` as in ``attend_tree``, for chunks of any length up to
+        ``max_chunk``: the last rows of a sequence are its tokens' own, token i's at P = kv_len - T + i.  It sees the rows before and
+        at P, or with ``rows_to`` [tokens] int32 those before rows_to; of these with ``rows_from`` [tokens] int32 those from
+        rows_from on, and with ``window`` the last so many up to P.  (Documents in one sequence: rows_from is the first row of the token's
+        document; a prefix that all tokens see: rows_to = max(P + 1, prefix length).)  ``softcap``: logits s become
+        softcap * tanh(s / softcap); ``slopes`` [heads] float32: then s - slope * |P - j| for row j.  A token that sees nothing gets
+        zeros and -inf."""
+        E, device = _env_made or _env(), self._device
+        n, heads, b, per = self._queries(E, q, page_table, out, lse)
+        size = self._workspace.get((heads, max_chunk, n, b))
+        if size is None:
+            size = self._chunk_workspace_bytes(E, heads, max_chunk, n, b)
+        if scale is None:
+            scale = self._scale
+        if not (math.isfinite(scale) and 0.0 <= softcap < math.inf and 0 <= window < 1 << 31):
+            raise DynaKVError(f"scale is {scale}, softcap {softcap}, window {window}: expected finite numbers, softcap and window not negative")
+        at_slopes = None
+        if slopes is not None:
+            if slopes.dtype is not E.f32 or slopes.shape != (heads,) or slopes.get_device() != device or not slopes.is_contiguous():
+                raise DynaKVError(f"expected slopes as a contiguous float32 tensor of {heads} elements on {self.device}, got {slopes.dtype} {tuple(slopes.shape)} on {slopes.device}")
+            if slopes.requires_grad and E.grad():
+                _no_gradient()
+            at_slopes = slopes.data_ptr()
+        first = _index(E, rows_from, (n,), device, "rows_from") if rows_from is not None else None
+        end = _index(E, rows_to, (n,), device, "rows_to") if rows_to is not None else None
+        out, lse = self._results(E, q, out, lse)
+        table, lens, start = _index(E, page_table, (b, per), device, "page_table"), _index(E, kv_len, (b,), device, "kv_len"), \
+            _index(E, q_start, (b + 1,), device, "q_start")
+        space = E.empty(size, dtype=self._byte, device=self.device)
+        _call(E, device, E.dynakv_attend_chunk, self._ref, q.data_ptr(), heads, n, start, b, max_chunk, table, per, lens,
+              C.byref(_Scores(scale, softcap, window, at_slopes, first, end)), out.data_ptr(), lse.data_ptr(), space.data_ptr(), size, self._status_at)
+        return out, lse
+
+    def _queries(self, E, q, page_table, out, lse):
+        """What both kinds of attention check first: (tokens, heads, sequences, pages per sequence)."""
+        shape = q.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or q.dtype is not self._io or not q.is_contiguous() or q.get_device() != self._device or q.data_ptr() % 16:
+            raise DynaKVError(f"expected q as a contiguous, 16-byte aligned {self._io} tensor [tokens, heads, {self.head_dim}] on {self.device}, "
+                              f"got {q.dtype} {tuple(q.shape)} on {q.device}")
+        self._held.check(E)
+        if E.grad() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
+            _no_gradient()
+        rows = page_table.shape
+        if len(rows) != 2:
+            raise DynaKVError(f"expected page_table of two dimensions, got {tuple(rows)}")
+        return shape[0], shape[1], rows[0], rows[1]
+
+    def _results(self, E, q, out, lse):
+        """(out, lse), checked or made."""
+        n, heads, d = q.shape
+        device, dtype = self._device, self._io
         if out is None:
             out = E.empty((n, heads, d), dtype=dtype, device=self.device)
         elif out.dtype is not dtype or out.shape != q.shape or not out.is_contiguous() or out.get_device() != device or out.data_ptr() % 16:
@@ -364,12 +424,21 @@ class RowCache:
             raise DynaKVError(f"expected lse as a contiguous float32 tensor {(n, heads)} on {self.device}, got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
         elif _overlap(lse, q) or _overlap(lse, out):
             raise DynaKVError("lse shares memory with q or out")
-        table, lens, start = _index(E, page_table, (b, per), device, "page_table"), _index(E, kv_len, (b,), device, "kv_len"), \
-            _index(E, q_start, (b + 1,), device, "q_start")
-        space = E.empty(size, dtype=self._byte, device=self.device)
-        _call(E, device, E.dynakv_attend_tree, self._ref, q.data_ptr(), heads, n, start, b, max_tree, table, per, lens, mask, words, scale,
-              out.data_ptr(), lse.data_ptr(), space.data_ptr(), size, self._status_at)
         return out, lse
+
+    def _chunk_workspace_bytes(self, E, heads: int, max_chunk: int, n: int, b: int) -> int:
+        if heads == 0 or heads % self.n_kv_heads != 0 or heads // self.n_kv_heads > 8:
+            raise DynaKVError(f"{heads} query heads over {self.n_kv_heads} KV heads: expected 1 to 8 per KV head")
+        if not 1 <= max_chunk <= MAX_CHUNK:
+            raise DynaKVError(f"max_chunk is {max_chunk}: expected 1 to {MAX_CHUNK}")
+        with E.torch.cuda.device(self._device):
+            size = E.dynakv_attend_chunk_workspace(self._ref, heads, n, b, max_chunk)
+        if size < 0:
+            raise DynaKVError(f"dynakv_attend_chunk_workspace returned {size}")
+        if len(self._workspace) >= 4096:       # lengths of prompts differ without end
+            self._workspace.clear()
+        self._workspace[heads, max_chunk, n, b] = size
+        return size
 
     def _workspace_bytes(self, E, heads: int, max_tree: int) -> int:
         """Checks the two numbers that choose the kernel, and keeps the bytes of scratch that they come to."""
