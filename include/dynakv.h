@@ -527,6 +527,66 @@ int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_
  * a negative code. */
 int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, int32_t n_heads, int64_t n_tokens, int32_t n_seqs, int32_t max_chunk);
 
+/* ---- Pages for new tokens, and drafted tokens after their attention ------------------------------------------------ */
+
+/* Free pages of a cache: the first *count of free_pages[n_pages] (both on the device), taken from and given back to the end, like
+ * a stack.  n_pages < 2^26. */
+typedef struct dynakv_page_pool {
+    int32_t* free_pages;
+    int32_t* count;
+    int64_t n_pages;
+} dynakv_page_pool;
+
+/* Rows for new_len[b] >= 0 new tokens at the end of every sequence b: kv_len[b] grows by as many, page_table[b]
+ * ([n_seqs][pages_per_seq], entries past a sequence's pages are of no interest) gets the pages that it needs, in order of
+ * sequences and of rows from the top of the pool, and q_start [n_seqs + 1], positions, slots [n_tokens] say where the packed tokens
+ * lie: token i of sequence b is q_start[b] + i, its position kv_len[b] + i as it was before, its slot that of its row.  That is what
+ * dynakv_norm_rope_store, dynakv_attend_tree and dynakv_attend_chunk take.  Places behind the last token get position 0 and slot -1,
+ * which is skipped where rows are stored.
+ * Sequences are served in order up to the first one for which pages (DYNAKV_ST_PAGE_POOL) or places (DYNAKV_ST_BOUNDS) are too few; it
+ * and those behind it stay as they are, with no tokens.  So does a sequence whose numbers are negative or whose rows would not fit its
+ * row of the table (DYNAKV_ST_BOUNDS).  The arrays must not overlap; calls on one pool or table must not run at the same time. */
+int dynakv_pages_extend(const dynakv_page_pool* pool, int32_t* page_table, int32_t pages_per_seq, int32_t* kv_len, const int32_t* new_len,
+                        int32_t n_seqs, int64_t n_tokens, int32_t* q_start, int32_t* positions, int32_t* slots, uint32_t* status,
+                        void* cuda_stream);
+
+/* The last drop[b] >= 0 rows of every sequence given up: kv_len[b] falls by as many, pages that hold no row any more return to the
+ * pool and their entries become -1.  Dropping what the last call of dynakv_pages_extend added puts the pool back as it was.  What is out of
+ * range (drop[b] > kv_len[b], a page id outside the pool) sets DYNAKV_ST_BOUNDS, more pages than the pool has places DYNAKV_ST_PAGE_POOL;
+ * sequences are treated as by dynakv_pages_extend. */
+int dynakv_pages_trim(const dynakv_page_pool* pool, int32_t* page_table, int32_t pages_per_seq, int32_t* kv_len, const int32_t* drop,
+                      int32_t n_seqs, uint32_t* status, void* cuda_stream);
+
+/* Which drafted tokens the target model accepts, and the token that follows, from random numbers that the caller draws.
+ *
+ * Sequence b's tokens q_start[b] .. q_start[b + 1] - 1 (at most max_tree <= 256) are a tree as dynakv_attend_tree attends to it: the first is the
+ * root, which is certain, the others are drafts; parent[q_start[b] + i] is the place in the tree, before i, of draft i's parent (NULL: i - 1, a
+ * chain).  logits[i] ([n_tokens][vocab], logits_stride elements from row to row, DYNAKV_F32 or DYNAKV_BF16, finite or -infinity) are
+ * the target's behind token i.  From the root on, with p = softmax(logits / temperature[b]) of the token reached, its children
+ * are tried in order: child c with token x is accepted, and reached, if uniform[c] * q(x) * sum(p) < p(x); else p becomes
+ * max(p - q, 0).  q is draft_probs[c] ([n_tokens][vocab] fp32, draft_stride elements from row to row), the distribution that x was drawn from, or
+ * with draft_probs NULL all of it on x, which leaves p without x; draft_probs goes with chains only.  When no child is accepted (or there
+ * is none) the next token is the first whose running sum of p exceeds uniform[root] * sum(p); where max(p - q, 0) is zero everywhere, p stays.
+ * With uniform drawn from [0, 1) the kept tokens are distributed as the target's own.  temperature[b] <= 0: p is all on the first of the largest logits.
+ *
+ * kept [n_seqs]: tokens of the accepted path, the root included; dropped [n_seqs]: the others; path [n_seqs][max_tree]: the places in the
+ * tree of the kept ones, upward from 0, then -1; next_token [n_seqs], -1 where no token has a weight.  A sequence without tokens gets 0, 0, -1, -1, one whose range
+ * is none of n_tokens or longer than max_tree 0, -1, -1, -1.  A token outside the vocabulary is never accepted.  n_tokens < 2^24, n_seqs <= 65535.
+ * Acceptance is decided on sums of fp32 exponentials (relative error below 1e-6), the next token on 64-bit sums.
+ * workspace: dynakv_verify_drafts_workspace() bytes, 16-byte aligned; calls that may overlap need one each. */
+int dynakv_verify_drafts(const void* logits, int64_t logits_stride, int32_t logits_dtype, int64_t n_tokens, int32_t vocab, const int32_t* tokens,
+                         const int32_t* q_start, int32_t n_seqs, int32_t max_tree, const float* uniform, const float* temperature,
+                         const int32_t* parent, const float* draft_probs, int64_t draft_stride, int32_t* kept, int32_t* dropped, int32_t* path,
+                         int32_t* next_token, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+int64_t dynakv_verify_drafts_workspace(int32_t logits_dtype, int64_t n_tokens, int32_t vocab, int32_t n_seqs, int32_t max_tree);
+
+/* Rows of the accepted path of a tree moved together: the T_b = q_start[b + 1] - q_start[b] last rows of sequence b are its tree's, and row
+ * path[b][i] of the tree goes to row i, for i < kept[b] (path [n_seqs][path_width], going upward from path[b][0] = 0).  Rows of the tree from kept[b]
+ * on stay as they are (dynakv_pages_trim gives them up).  FP8 rows move with their exponents.  What is out of range is skipped and sets DYNAKV_ST_BOUNDS. */
+int dynakv_rows_keep(const dynakv_row_cache* cache, const int32_t* page_table, int32_t pages_per_seq, const int32_t* kv_len,
+                     const int32_t* q_start, int32_t n_seqs, const int32_t* path, int32_t path_width, const int32_t* kept, uint32_t* status,
+                     void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

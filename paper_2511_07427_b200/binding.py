@@ -25,6 +25,7 @@ EXPORTED_SYMBOLS = [
     "dynakv_build_index_placed", "dynakv_get_work_list", "dynakv_work_list_capacity", "dynakv_get_tier_stats", "dynakv_checked_build",
     "dynakv_norm_rope", "dynakv_norm_rope_store", "dynakv_rows_write", "dynakv_rows_read",
     "dynakv_attend_tree", "dynakv_attend_tree_workspace", "dynakv_attend_chunk", "dynakv_attend_chunk_workspace",
+    "dynakv_pages_extend", "dynakv_pages_trim", "dynakv_verify_drafts", "dynakv_verify_drafts_workspace", "dynakv_rows_keep",
 ]
 ERR_TOO_LARGE = -5
 NOALLOC_SCRATCH_BYTES = 4 * 1024 * 1024

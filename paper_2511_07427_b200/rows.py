@@ -48,6 +48,11 @@ SIGNATURES["dynakv_attend_tree"] = (C.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _
 SIGNATURES["dynakv_attend_tree_workspace"] = (_i64, [_vp, _i32, _i32])
 SIGNATURES["dynakv_attend_chunk"] = (C.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp])
 SIGNATURES["dynakv_attend_chunk_workspace"] = (_i64, [_vp, _i32, _i64, _i32, _i32])
+SIGNATURES["dynakv_rows_keep"] = (C.c_int, [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp])
+SIGNATURES["dynakv_pages_extend"] = (C.c_int, [_vp, _vp, _i32, _vp, _vp, _i32, _i64, _vp, _vp, _vp, _vp, _vp])
+SIGNATURES["dynakv_pages_trim"] = (C.c_int, [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp])
+SIGNATURES["dynakv_verify_drafts"] = (C.c_int, [_vp, _i64, _i32, _i64, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp])
+SIGNATURES["dynakv_verify_drafts_workspace"] = (_i64, [_i32, _i64, _i32, _i32, _i32])
 
 
 class _Env:
@@ -319,6 +324,20 @@ class RowCache:
         K, V = E.empty(shape, dtype=self._io, device=self.device), E.empty(shape, dtype=self._io, device=self.device)
         _call(E, device, E.dynakv_rows_read, self._ref, table, per, lens, b, first, n, K.data_ptr(), V.data_ptr(), self._status_at)
         return K, V
+
+    def keep(self, page_table, kv_len, q_start, path, kept) -> None:
+        """Rows of accepted drafts moved together (``dynakv_rows_keep``): of every sequence's last q_start[b + 1] - q_start[b] rows, its
+        tree's, row ``path`` [sequences, width] int32 [b, i] goes to row i for i < ``kept`` [sequences] int32.  Paths go upward from 0, as
+        ``verify_drafts`` returns them."""
+        E, device = _env_made or _env(), self._device
+        self._held.check(E)
+        rows, wide = page_table.shape, path.shape
+        if len(rows) != 2 or len(wide) != 2:
+            raise DynaKVError(f"expected page_table and path of two dimensions, got {tuple(rows)}, {tuple(wide)}")
+        b, per = rows
+        _call(E, device, E.dynakv_rows_keep, self._ref, _index(E, page_table, (b, per), device, "page_table"), per, _index(E, kv_len, (b,), device, "kv_len"),
+              _index(E, q_start, (b + 1,), device, "q_start"), b, _index(E, path, (b, wide[1]), device, "path"), wide[1],
+              _index(E, kept, (b,), device, "kept"), self._status_at)
 
     def attend_tree(self, q, page_table, kv_len, q_start, max_tree: int, tree_mask=None, scale=None, out=None, lse=None):
         """Attention of drafted tokens over the cache (``dynakv_attend_tree``): (out, lse).
