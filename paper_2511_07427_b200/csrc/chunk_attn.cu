@@ -1,7 +1,12 @@
 // dynakv_attend_chunk: which kernel a call takes, and its launch.
+#include "chunk_plan.cuh"
 #include "tree_rows.cuh"
 
 namespace dkv {
+
+// tcgen05 kernel (chunk_tc.cu), and the bytes up to the end of its plan in a workspace whose first `at` are taken.
+int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st);
+size_t chunk_plan_space(int64_t n_tokens, int G, int n_seqs, int ctas, size_t at, char* base, ChunkPlan* plan);
 
 template <int HD, int DT, int RG>
 static int chunk_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
@@ -17,11 +22,19 @@ static int chunk_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& m
     return rg == 0 ? chunk_launch<HD, DT, 0>(mk, mv, a, sms, st) : rg == 1 ? chunk_launch<HD, DT, 1>(mk, mv, a, sms, st) : rg == 2 ? chunk_launch<HD, DT, 2>(mk, mv, a, sms, st) : chunk_launch<HD, DT, 4>(mk, mv, a, sms, st);
 }
 
-struct ChunkKind { int rg, rows, ctas; };
+#ifndef DKV_CHUNK_TC_BF16
+#define DKV_CHUNK_TC_BF16 33
+#endif
+#ifndef DKV_CHUNK_TC_FP8
+#define DKV_CHUNK_TC_FP8 65
+#endif
+struct ChunkKind { bool tc; int rg, rows, ctas; };
 static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int max_chunk, int sms) {
     const bool f32 = c->kv_dtype == DYNAKV_F32;
-    const int rg = row_groups((int)min(1000ll, (long long)max_chunk * (n_heads / c->n_kv_heads)), f32);
-    return {rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2)};
+    const int most = (int)min(1000ll, (long long)max_chunk * (n_heads / c->n_kv_heads));
+    if (!f32 && most >= (c->kv_dtype == DYNAKV_FP8 ? DKV_CHUNK_TC_FP8 : DKV_CHUNK_TC_BF16)) return {true, 0, CT_ROWS, sms};
+    const int rg = row_groups(most, f32);
+    return {false, rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2)};
 }
 
 static bool chunk_shape_ok(const dynakv_row_cache* c, int n_heads, int64_t n_tokens, int n_seqs, int max_chunk) {
@@ -39,7 +52,8 @@ extern "C" int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, 
     const int sms = sm_count(&rc);
     if (rc != DYNAKV_OK) return rc;
     const ChunkKind k = chunk_kind(cache, n_heads, max_chunk, sms);
-    return (int64_t)tree_space(k.ctas, k.rows, cache->head_dim).bytes;
+    const size_t records = tree_space(k.ctas, k.rows, cache->head_dim).bytes;
+    return (int64_t)(k.tc ? chunk_plan_space(n_tokens, n_heads / cache->n_kv_heads, n_seqs, sms, records, nullptr, nullptr) : records);
 }
 
 extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
@@ -56,7 +70,9 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
     if (rc != DYNAKV_OK) return rc;
     const ChunkKind kind = chunk_kind(cache, n_heads, max_chunk, sms);
     const TreeSpace sp = tree_space(kind.ctas, kind.rows, cache->head_dim);
-    if (workspace_bytes < (int64_t)sp.bytes) return DYNAKV_ERR_ARG;
+    ChunkPlan plan = {};
+    const size_t bytes = kind.tc ? chunk_plan_space(n_tokens, n_heads / cache->n_kv_heads, n_seqs, sms, sp.bytes, reinterpret_cast<char*>(workspace), &plan) : sp.bytes;
+    if (workspace_bytes < (int64_t)bytes) return DYNAKV_ERR_ARG;
     TreeArgs a = tree_args(cache, q, n_heads, n_tokens, q_start, n_seqs, max_chunk, page_table, pages_per_seq, kv_len, out, lse, workspace, sp, status);
     a.scale = scores->scale;
     a.cap = scores->softcap;
@@ -66,6 +82,7 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     // an error left behind by an earlier, unrelated call on this thread must not be reported as this call's
     cudaGetLastError();
+    if (kind.tc) return chunk_tc_launch(cache, a, plan, sms, st);
     CUtensorMap mk, mv;
     if (!tree_page_map(&mk, cache, cache->k, true) || !tree_page_map(&mv, cache, cache->v, true)) return DYNAKV_ERR_CUDA;
     const int rg = kind.rg;

@@ -32,6 +32,7 @@
 #include "head_rows.cuh"
 #include "mma_ops.cuh"
 #include "tc_ops.cuh"
+#include "tc_rows.cuh"
 #include "tree_host.cuh"
 #include "tree_plan.cuh"
 
@@ -63,25 +64,6 @@ struct TcTree {
     static_assert(count <= 32, "barrier block");
 };
 
-__device__ __forceinline__ void tt_load(unsigned dst, const CUtensorMap* map, int row, int panel, unsigned bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n"
-                 ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(panel), "r"(bar) : "memory");
-}
-__device__ __forceinline__ float tt_max3(float a, float b, float c) {
-    float r;
-    asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-__device__ __forceinline__ void sts16(unsigned addr, uint4 v) {
-    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-// True in one lane of a converged warp, the same one every time.
-__device__ __forceinline__ bool elect_one() {
-    unsigned r;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
-    return r != 0;
-}
-__device__ __forceinline__ void tt_proxy_fence() { asm volatile("fence.proxy.async;\n" ::: "memory"); }
 // Pages of half h of stage j of a segment of `pages` pages.
 __device__ __forceinline__ int half_pages(int pages, int j, int h) { return max(0, min(TT_HALF, pages - j * TT_PAGES - h * TT_HALF)); }
 
