@@ -1,10 +1,12 @@
 // How dynakv_attend_chunk on tcgen05 cuts its work.
 //
-// A tile is 256 query rows of one sequence, row = token * G + head of the group; a unit is a tile and a KV head; its work is the
-// stages of 128 rows (4 pages) between the first and the last row that one of its tokens sees.  A first launch writes down every
-// tile's stages, their prefix sums and where every CTA of the main kernel begins, because that depends on lengths and ranges that only the
-// device has.  All units' stages, in the order sequence, KV head, tile (so that CTAs side by side read the same rows), form one
-// list that the CTAs share out evenly; a unit cut by a border leaves records that a last launch merges, as in tree_plan.cuh.
+// A tile is the query rows, row = token * G + head of the group, of 2 (128 / G) consecutive tokens of one sequence: two streams of up to
+// 128 rows that begin with a token's first head, which is what lets the TMA fetch them.  A unit is a tile and a KV head; its work
+// is the stages of 128 rows (4 pages) between the first and the last row that one of its tokens sees.  A first launch writes down
+// every tile's stages, their prefix sums and where every CTA of the main kernel begins, because that depends on lengths and ranges that
+// only the device has.  All units' stages, in the order sequence, KV head, tile (so that CTAs side by side read the same
+// rows), form one list that the CTAs share out evenly, a unit's beginning counted as CT_UNIT_COST stages more; a unit cut by a border leaves
+// records that a last launch merges, as in tree_plan.cuh.
 #pragma once
 
 #include "tree_plan.cuh"
@@ -12,59 +14,65 @@
 namespace dkv {
 
 constexpr int CT_ROWS = 256, CT_KEYS = 128, CT_PAGES = CT_KEYS / PAGE;
+#ifndef DKV_CHUNK_UNIT_COST
+#define DKV_CHUNK_UNIT_COST 2
+#endif
+constexpr int CT_UNIT_COST = DKV_CHUNK_UNIT_COST;
 
-struct ChunkTile { int seq, tile, from, stages; };
-struct ChunkSeq { int q0, T, n, first; };          // first packed token, tokens, rows, first tile
-struct ChunkStart { int tile, head, off, left; };  // where a CTA begins: tile, KV head, stage of the unit; stages it has in all
+struct __align__(16) ChunkTile {
+    int seq, tile, from, stages;                   // of the sequence; first stage, stages
+    int q0, T, n, first;                           // the sequence's first packed token, tokens, rows and first tile
+};
+struct __align__(16) ChunkStart {                  // where a CTA begins: tile, KV head, stage of the unit; stages it has in all
+    int tile, head, off, left;
+    long long at;                                  // and their place in the list of all stages
+};
 struct ChunkPlan {
     ChunkTile* tiles;                              // [most tiles]
     long long* before;                             // [most tiles + 1] stages of the tiles before, for one KV head
-    ChunkSeq* seqs;                                // [n_seqs + 1]; of the last only `first` counts: the number of tiles
     ChunkStart* starts;                            // [CTAs]
-    long long* total;                              // [2] stages of one KV head, CTAs that have work
 };
+
+__device__ __host__ __forceinline__ int tile_tokens(int G) { return 2 * (128 / G); }
+__device__ __forceinline__ int seq_tiles(int T, int G) { return (T + tile_tokens(G) - 1) / tile_tokens(G); }
 
 struct ChunkSeg {
     int seq, h, tile, s0, s1;                      // stages [s0, s1) of the sequence
     int q0, T, n;
+    int tokens;                                    // of the tile
     bool first, last;                              // holds the unit's first / last stage
-    long long unit_start;                          // flat index of the unit's first stage
+    long long unit_start;                          // place of the unit's first stage in the list of all stages
 };
 
+// A CTA's segments in order.  The next tile's record is on its way while this one's is worked on.
 struct ChunkWalk {
     int e, h, off, left;
-    ChunkTile t;
-    ChunkSeq s;
-    int next_first;
-    __device__ __forceinline__ void look(const ChunkPlan& p) {
-        t = p.tiles[e];
-        s = p.seqs[t.seq];
-        next_first = p.seqs[t.seq + 1].first;
-    }
-    __device__ __forceinline__ void start(const ChunkPlan& p) {
+    long long at;
+    ChunkTile t, ahead;
+    __device__ __forceinline__ void start(const TreeArgs& a, const ChunkPlan& p) {
         const ChunkStart c = p.starts[blockIdx.x];
-        e = c.tile; h = c.head; off = c.off; left = c.left;
-        if (left > 0) look(p);
+        e = c.tile; h = c.head; off = c.off; left = c.left; at = c.at;
+        if (left > 0) ahead = p.tiles[e];
     }
     __device__ __forceinline__ bool next(const TreeArgs& a, const ChunkPlan& p, ChunkSeg& g) {
         if (left <= 0) return false;
-        if (off == t.stages) {                     // the next tile, or the sequence's next head, or the next sequence
-            off = 0;
-            e++;
-            if (e == next_first && h + 1 < a.Hk) { h++; e = s.first; }
-            else if (e == next_first) h = 0;
-            look(p);
-        }
-        const int here = min(left, t.stages - off);
+        t = ahead;
+        const int here = min(left, t.stages - off), per = tile_tokens(a.G);
         g.seq = t.seq; g.h = h; g.tile = t.tile;
         g.s0 = t.from + off; g.s1 = g.s0 + here;
-        g.q0 = s.q0; g.T = s.T; g.n = s.n;
+        g.q0 = t.q0; g.T = t.T; g.n = t.n;
+        g.tokens = min(per, t.T - t.tile * per);
         g.first = off == 0; g.last = off + here == t.stages;
-        if (!(g.first && g.last)) {
-            const long long lead = p.before[s.first], all = p.before[next_first] - lead;
-            g.unit_start = lead * a.Hk + h * all + p.before[e] - lead;
+        g.unit_start = at - off;
+        at += here; left -= here; off = 0;
+        if (left > 0) {                            // the next tile, or the sequence's next head, or the next sequence
+            e++;
+            if (e == t.first + seq_tiles(t.T, a.G)) {
+                if (h + 1 < a.Hk) { h++; e = t.first; }
+                else h = 0;
+            }
+            ahead = p.tiles[e];
         }
-        off += here; left -= here;
         return true;
     }
 };

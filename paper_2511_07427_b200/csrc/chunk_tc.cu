@@ -7,6 +7,7 @@
 // first half of the columns); the next logits overwrite them, in the tensor pipe's own order, after the products that read them.
 //   warp 0 / warp 2      TMA loads of K / of V, one 32-row panel of 128 bytes per copy, 128-byte swizzle
 //   warp 1               tcgen05.mma of both streams
+//   warp 3               TMA loads of the next unit's queries, when the last logits of this one have been multiplied
 //   warps 4-7 / 8-11     softmax of stream 0 / 1: a query row per thread
 //   warps 12-15          FP8 rows only: they fetch the rows and turn them into bf16 stages (warps 0 and 2 then rest)
 // Weights enter the products as bf16 (2^-9 of each).
@@ -29,16 +30,13 @@ constexpr float CT_LAZY = 8.f;                                 // the softmax's 
 
 // ---------------------------------------------------------------------------------- the plan
 
-constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_THREADS = 1024, PLAN_NEAR = 2048;            // prefix sums of so many tiles are kept in shared memory as well
 
-__device__ __forceinline__ ChunkSeq chunk_seq(const TreeArgs& a, int b, bool report) {
-    const SeqInfo s = seq_info<CT_ROWS, false>(a, b, report);
-    return {s.q0, s.T, s.n, s.tiles};
-}
-
-__global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, const ChunkPlan p, int ctas, int min_stages, long long most) {
+__global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, const ChunkPlan p, int ctas, long long most) {
     __shared__ long long sums[32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ long long near_s[PLAN_NEAR + 1];
+    __shared__ long long at_s[PLAN_THREADS + 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = tile_tokens(a.G);
     pdl_wait();
     pdl_trigger();
     auto scan = [&](long long x, long long& total) {           // inclusive, over the block
@@ -54,89 +52,99 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
         const long long before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
         return x + (warp ? before : 0);
     };
-    // ---- sequences, and where their tiles begin
+    // ---- sequences and their tiles
     long long tiles = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += PLAN_THREADS) {
         const int b = b0 + tid;
-        ChunkSeq s = {0, 0, 0, 0};
-        if (b < a.n_seqs) s = chunk_seq(a, b, true);
-        long long total, incl = scan(s.first, total);
-        int count = s.first;
+        SeqInfo s = {};
+        if (b < a.n_seqs) s = seq_info<CT_ROWS, false>(a, b, true);
+        int count = seq_tiles(s.T, a.G);
+        long long total, incl = scan(count, total);
         if (tiles + total > most) {                            // ranges of q that overlap: the workspace has no room for more tiles than tokens make
             if (tiles + incl > most) { count = 0; s.T = 0; tree_status(a, DYNAKV_ST_BOUNDS); }
             incl = scan(count, total);
         }
-        s.first = (int)(tiles + incl - count);
-        if (b < a.n_seqs) p.seqs[b] = s;
-        // the tiles' sequences: few sequences have many tiles, so a warp writes a sequence's
-        for (int src = 0; src < 32; src++) {
-            const int c = __shfl_sync(0xffffffffu, count, src), f = __shfl_sync(0xffffffffu, s.first, src);
-            for (int i = lane; i < c; i += 32) { p.tiles[f + i].seq = b0 + warp * 32 + src; p.tiles[f + i].tile = i; }
+        const int first = (int)(tiles + incl - count);
+        for (int src = 0; src < 32; src++) {                   // few sequences have many tiles, so a warp writes a sequence's
+            const int c = __shfl_sync(0xffffffffu, count, src), f = __shfl_sync(0xffffffffu, first, src), q0 = __shfl_sync(0xffffffffu, s.q0, src),
+                      T = __shfl_sync(0xffffffffu, s.T, src), n = __shfl_sync(0xffffffffu, s.n, src);
+            for (int i = lane; i < c; i += 32) {
+                const int from = i * per, to = min(T, from + per), place = n - T;
+                int lo = n, hi = 0;
+                if (!a.rows_from && !a.rows_to) {
+                    lo = a.window > 0 ? max(0, place + from + 1 - a.window) : 0;
+                    hi = place + to;
+                }
+                p.tiles[f + i] = {b0 + warp * 32 + src, i, lo, hi, q0, T, n, f};
+            }
         }
         tiles += total;
     }
-    if (tid == 0) p.seqs[a.n_seqs].first = (int)tiles;
     __syncthreads();
-    // ---- stages of every tile: a thread per tile, or a warp where the tokens' ranges have to be read
-    const bool ranges = a.rows_from || a.rows_to;
+    // ---- stages of every tile; where the tokens' ranges have to be read, a warp per tile finds the first and the last row
+    if (a.rows_from || a.rows_to) {
+        for (int i = warp; i < tiles; i += 32) {
+            const ChunkTile t = p.tiles[i];
+            const int from = t.tile * per, to = min(t.T, from + per);
+            int lo = t.n, hi = 0;
+            for (int x = from + lane; x < to; x += 32) {
+                int l, h;
+                chunk_sees(a, t.q0 + x, t.n - t.T + x, t.n, l, h);
+                if (l < h) { lo = min(lo, max(l, 0)); hi = max(hi, h); }
+            }
+            lo = __reduce_min_sync(0xffffffffu, lo); hi = __reduce_max_sync(0xffffffffu, hi);
+            if (lane == 0) { p.tiles[i].from = lo; p.tiles[i].stages = hi; }
+        }
+        __syncthreads();
+    }
     long long run = 0;
     for (int t0 = 0; t0 < tiles; t0 += PLAN_THREADS) {
-        const int n_here = (int)min((long long)PLAN_THREADS, tiles - t0);
-        if (ranges) {
-            for (int i = warp; i < n_here; i += 32) {
-                ChunkTile& t = p.tiles[t0 + i];
-                const ChunkSeq s = p.seqs[t.seq];
-                const int from = t.tile * CT_ROWS / a.G, to = min(s.T, ((t.tile + 1) * CT_ROWS + a.G - 1) / a.G);
-                int lo = s.n, hi = 0;
-                for (int x = from + lane; x < to; x += 32) {
-                    int l, h;
-                    chunk_sees(a, s.q0 + x, s.n - s.T + x, s.n, l, h);
-                    if (l < h) { lo = min(lo, max(l, 0)); hi = max(hi, h); }
-                }
-                lo = __reduce_min_sync(0xffffffffu, lo); hi = __reduce_max_sync(0xffffffffu, hi);
-                if (lane == 0) { t.from = lo < hi ? lo / CT_KEYS : 0; t.stages = lo < hi ? (hi + CT_KEYS - 1) / CT_KEYS - t.from : 1; }
-            }
-            __syncthreads();
-        }
+        const int i = t0 + tid;
         long long mine = 0;
-        if (tid < n_here) {
-            ChunkTile& t = p.tiles[t0 + tid];
-            if (!ranges) {
-                const ChunkSeq s = p.seqs[t.seq];
-                const int from = t.tile * CT_ROWS / a.G, to = min(s.T, ((t.tile + 1) * CT_ROWS + a.G - 1) / a.G), place = s.n - s.T;
-                const int lo = a.window > 0 ? max(0, place + from + 1 - a.window) : 0, hi = place + to;
-                t.from = lo < hi ? lo / CT_KEYS : 0;
-                t.stages = lo < hi ? (hi + CT_KEYS - 1) / CT_KEYS - t.from : 1;
-            }
-            mine = t.stages;
+        if (i < tiles) {
+            const int lo = p.tiles[i].from, hi = p.tiles[i].stages, from = lo < hi ? lo / CT_KEYS : 0;
+            mine = lo < hi ? (hi + CT_KEYS - 1) / CT_KEYS - from : 1;
+            p.tiles[i].from = from;
+            p.tiles[i].stages = (int)mine;
         }
         long long total;
         const long long incl = scan(mine, total);
-        if (tid < n_here) p.before[t0 + tid] = run + incl - mine;
+        if (i < tiles) { p.before[i] = run + incl - mine; if (i < PLAN_NEAR) near_s[i] = run + incl - mine; }
         run += total;
     }
-    if (tid == 0) p.before[tiles] = run;
+    if (tid == 0) { p.before[tiles] = run; if (tiles <= PLAN_NEAR) near_s[tiles] = run; }
     __syncthreads();
-    // ---- where every CTA begins
-    const long long W = run * a.Hk;
-    const int C = (int)max(1ll, min((long long)ctas, W / min_stages));
-    if (tid == 0) { p.total[0] = run; p.total[1] = C; }
-    for (int c = tid; c < ctas; c += PLAN_THREADS) {
-        ChunkStart st = {0, 0, 0, 0};
-        const long long x = c < C ? mul_div(c, W, C) : W, end = c < C ? mul_div(c + 1, W, C) : W;
-        if (x < end) {
-            auto find = [&](long long y, int lo, int hi) {     // last tile of [lo, hi) with before <= y
-                while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (p.before[mid] <= y) lo = mid; else hi = mid; }
+    // ---- where every CTA begins: cost x is stage x of the list in which every unit has CT_UNIT_COST stages more
+    const long long* before = tiles <= PLAN_NEAR ? near_s : p.before;
+    const long long W = (run + tiles * CT_UNIT_COST) * a.Hk;
+    const int C = (int)max(1ll, min((long long)ctas, run * a.Hk));
+    for (int c0 = 0; c0 < ctas; c0 += PLAN_THREADS) {
+        // the CTA's place, and that of the one behind it
+        ChunkStart st = {0, 0, 0, 0, run * a.Hk};
+        const int c = c0 + tid;
+        const long long x = c < C ? mul_div(c, W, C) : W;
+        if (c <= ctas && x < W) {
+            auto find = [&](long long y, int lo, int hi) {     // last tile of [lo, hi) whose cost before it is <= y
+                while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (before[mid] + (long long)mid * CT_UNIT_COST <= y) lo = mid; else hi = mid; }
                 return lo;
             };
-            const int any = find(x / a.Hk, 0, (int)tiles), b = p.tiles[any].seq, e0 = p.seqs[b].first, e1 = p.seqs[b + 1].first;
-            const long long lead = p.before[e0], all = p.before[e1] - lead, off = x - lead * a.Hk;
-            st.head = (int)(off / all);
-            st.tile = find(lead + off - st.head * all, e0, e1);
-            st.off = (int)(lead + off - st.head * all - p.before[st.tile]);
-            st.left = (int)(end - x);
+            const ChunkTile t = p.tiles[find(x / a.Hk, 0, (int)tiles)];
+            const int e0 = t.first, e1 = e0 + seq_tiles(t.T, a.G);
+            const long long lead = before[e0] + (long long)e0 * CT_UNIT_COST, all = before[e1] + (long long)e1 * CT_UNIT_COST - lead, cost = x - lead * a.Hk;
+            st.head = (int)(cost / all);
+            const long long y = lead + cost - st.head * all;
+            st.tile = find(y, e0, e1);
+            st.off = (int)max(0ll, y - before[st.tile] - (long long)(st.tile + 1) * CT_UNIT_COST);
+            st.at = before[e0] * a.Hk + st.head * (before[e1] - before[e0]) + before[st.tile] - before[e0] + st.off;
         }
-        p.starts[c] = st;
+        at_s[tid] = st.at;
+        __syncthreads();
+        if (c < ctas) {
+            // up to where the next one begins; the last of a batch of CTAs (more than 1024: none has been built) finds its end in the list's
+            st.left = (int)((tid + 1 < PLAN_THREADS ? at_s[tid + 1] : run * a.Hk) - st.at);
+            p.starts[c] = st;
+        }
+        __syncthreads();
     }
 }
 
@@ -159,11 +167,20 @@ struct TcChunk {
     static constexpr unsigned idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);
     static constexpr unsigned idesc_qk = idesc | ((unsigned)(CT_KEYS >> 3) << 17);
     static constexpr unsigned idesc_pv = idesc | (1u << 16) | ((unsigned)(HD >> 3) << 17);      // B's contraction index is its outer one
-    static constexpr int KFULL = 0, KEMPTY = stages, VFULL = 2 * stages, VEMPTY = 3 * stages, SFULL = 4 * stages, PFULL = SFULL + 2,
-                         OFULL = PFULL + 2, QFULL = OFULL + 2, DRAIN = QFULL + 2, count = DRAIN + 1;
+    static constexpr int KFULL = 0, KEMPTY = stages, VFULL = 2 * stages, VEMPTY = 3 * stages, SFULL = 4 * stages, OFULL = SFULL + 2,
+                         QFULL = OFULL + 2, QEMPTY = QFULL + 2, DRAIN = QEMPTY + 2, PHALF = DRAIN + 1, PFULL = PHALF + 2, count = PFULL + 2;
     static_assert(count <= 32, "barrier block");
 };
 
+// 32 bytes in one store where the address allows.
+__device__ __forceinline__ void store32(void* to, const unsigned (&p)[8], bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(to), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3]), "r"(p[4]), "r"(p[5]), "r"(p[6]), "r"(p[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(p[0], p[1], p[2], p[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(p[4], p[5], p[6], p[7]);
+    }
+}
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(N)); }
 
@@ -172,6 +189,24 @@ struct ChunkRow {
     int lo, hi, place;
     float slope;
 };
+// What the scores need beside the factor and the mask.
+enum { PLAIN = 0, BIASED = 1, CAPPED = 2 };
+// tanh(y) / y for |y| <= 1 as a polynomial of y^2 (interpolated at Chebyshev nodes; tanh is off by 9e-8 at most), two at a time.
+constexpr float CT_TANH_RANGE = 1.f;
+__device__ __forceinline__ float2 tanh_near2(float2 y) {
+    const float2 z = mul2(y, y);
+    auto c = [](float x) { return make_float2(x, x); };
+    float2 p = fma2(c(-0.0003548834f), z, c(0.0022876456f));
+    p = fma2(p, z, c(-0.0079249460f));
+    p = fma2(p, z, c(0.0214699805f));
+    p = fma2(p, z, c(-0.0538727380f));
+    p = fma2(p, z, c(0.1333219111f));
+    p = fma2(p, z, c(-0.3333328068f));
+    p = fma2(p, z, c(1.f));
+    return mul2(p, y);
+}
+// tanh(y) = 1 - 2 / (1 + e^2y) for any y: off by 2e-7 at most.
+__device__ __forceinline__ float tanh_far(float y) { return fmaf(-2.f, __fdividef(1.f, 1.f + ex2(2.f * CT_LOG2E * (y > 40.f ? 40.f : y))), 1.f); }
 __device__ __forceinline__ float chunk_score(const TreeArgs& a, const ChunkRow& w, float x, int key) {
     if (a.cap > 0.f) x = a.cap * CT_LOG2E * tanhf(x);
     if (a.slopes) x = fmaf(-w.slope, fabsf((float)(w.place - key)), x);
@@ -196,9 +231,9 @@ __device__ __noinline__ void chunk_again(const TreeArgs& a, const ChunkSeg& g, c
     }
 }
 
-template <int HD, bool F8, bool MODS>
-__global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                                                                           const __grid_constant__ TreeArgs a, const __grid_constant__ ChunkPlan plan) {
+template <int HD, bool F8, int MODE>
+__global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                                           const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeArgs a, const __grid_constant__ ChunkPlan plan) {
     using C = TcChunk<HD, F8>;
     constexpr int NS = C::stages;
     extern __shared__ __align__(1024) unsigned char ct_smem[];
@@ -217,7 +252,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
     if (tid == 0) {
         for (int i = 0; i < C::count; i++) {
             const bool full = (i >= C::KFULL && i < C::KEMPTY) || (i >= C::VFULL && i < C::VEMPTY);
-            tc_mbar_init(bar(i), full && F8 ? CT_CONVERT / 32 : (i >= C::PFULL && i < C::OFULL) || (i >= C::QFULL && i < C::DRAIN) ? 4 : 1);
+            tc_mbar_init(bar(i), full && F8 ? CT_CONVERT / 32 : i >= C::PHALF ? 4 : 1);
         }
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -226,6 +261,11 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(tc_smem_u32((const void*)s_tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
+    if (tid < 256 && (tid & 127) >= 128 / a.G * a.G) {         // rows that no query is loaded into
+#pragma unroll
+        for (int c = 0; c < HD / 8; c++) sts16(sQ + (tid >> 7) * C::tile_bytes + (c >> 3) * C::panel_bytes + (tid & 127) * 128 + (c & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
+        tt_proxy_fence();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -233,8 +273,8 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
     pdl_wait();                                                // from here on the results of earlier kernels are read
     pdl_trigger();
     ChunkWalk walk;
-    walk.start(plan);
-    ChunkSeg g;
+    walk.start(a, plan);
+    ChunkSeg g = {};
     auto give_up = [&]() { *s_abort = 1; };
     // pages of stage s of the walk's segment that exist and are known to the table, as bits; ids by lane (4 lanes)
     auto page_of = [&](int s) {
@@ -289,6 +329,31 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                 // stage n - 1 was not issued; let the copies of the ones before it land before the block ends
                 for (int x = max(0, n - 1 - NS); x < n - 1; x++) mbar_wait(bar(full + x % NS), (unsigned)(x / NS) & 1u);
             }
+        } else if (warp == 3) {
+            // =============================== queries ===============================
+            // A stream's rows are the heads of the group of 128 / G tokens; tokens behind the chunk's last come along and are not used.
+            const int step = 128 / a.G;
+            int segs[2] = {0, 0};
+            bool ok = true;
+            while (ok && walk.next(a, plan, g)) {
+                for (int s = 0; s < (g.tokens > step ? 2 : 1) && ok; s++, __syncwarp()) {
+                    if (lane == 0) {
+                        ok = !*s_abort && (segs[s] == 0 || mbar_wait(bar(C::QEMPTY + s), (unsigned)(segs[s] - 1) & 1u));
+                        if (ok) {
+                            tc_mbar_expect_tx(bar(C::QFULL + s), step * a.G * HD * 2);
+#pragma unroll
+                            for (int q = 0; q < C::panels; q++)
+                                tt_load3(sQ + s * C::tile_bytes + q * C::panel_bytes, &map_q, q * 64, g.h * a.G, g.q0 + g.tile * 2 * step + s * step, bar(C::QFULL + s));
+                        }
+                    }
+                    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+                    if (ok) segs[s]++;
+                }
+            }
+            if (!ok && lane == 0) {
+                give_up();
+                for (int s = 0; s < 2; s++) if (segs[s] > 0) mbar_wait(bar(C::QFULL + s), (unsigned)(segs[s] - 1) & 1u);     // copies under way land first
+            }
         } else if (warp == 1) {
             // =============================== MMAs ===============================
             // The whole warp walks and waits, one elected lane issues.
@@ -297,7 +362,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
             const unsigned long long dq[2] = {tc_panel_desc(sQ), tc_panel_desc(sQ + C::tile_bytes)}, dk = tc_panel_desc(sK(0)), dv = tc_rows_desc(sV(0), C::panel_bytes);
             auto wait = [&](int b, int phase) { ok = ok && mbar_wait(bar(b), (unsigned)phase & 1u); ok = __all_sync(0xffffffffu, ok); };
             while (ok && walk.next(a, plan, g)) {
-                const int stages = g.s1 - g.s0, active = g.T * a.G - g.tile * CT_ROWS > 128 ? 2 : 1;
+                const int stages = g.s1 - g.s0, active = g.tokens > 128 / a.G ? 2 : 1;
                 auto logits = [&](int s, int j) {              // of stage j of the segment
                     const int st = (n + j) % NS;
                     if (s == 0) wait(C::KFULL + st, (n + j) / NS);
@@ -312,6 +377,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                         }
                         tc_commit(bar(C::SFULL + s));
                         if (s == active - 1) tc_commit(bar(C::KEMPTY + st));
+                        if (j + 1 == stages) tc_commit(bar(C::QEMPTY + s));
                     }
                     __syncwarp();
                 };
@@ -320,18 +386,23 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     const int st = (n + j) % NS;
                     for (int s = 0; s < active && ok; s++) {
                         if (s == 0) wait(C::VFULL + st, (n + j) / NS);
-                        wait(C::PFULL + s, u[s]);
+                        // the weights of the first 64 rows are used while the others are made
+#pragma unroll
+                        for (int half = 0; half < 2; half++) {
+                            wait((half ? C::PFULL : C::PHALF) + s, u[s]);
+                            if (!ok) break;
+                            tc_fence_after();
+                            if (elect_one()) {
+#pragma unroll
+                                for (int k = half * (CT_KEYS / 32); k < (half + 1) * (CT_KEYS / 32); k++)
+                                    tc_mma_f16_ta(tmem + 256 + s * 128, tmem + s * 128 + k * 8, dv + ((st * C::tile_bytes + k * 2048) >> 4), C::idesc_pv, j > 0 || k > 0 ? 1u : 0u);
+                                if (half && s == active - 1) tc_commit(bar(C::VEMPTY + st));
+                                if (half && j + 1 == stages) tc_commit(bar(C::OFULL + s));
+                            }
+                            __syncwarp();
+                        }
                         if (!ok) break;
                         u[s]++;
-                        tc_fence_after();
-                        if (elect_one()) {
-#pragma unroll
-                            for (int k = 0; k < CT_KEYS / 16; k++)
-                                tc_mma_f16_ta(tmem + 256 + s * 128, tmem + s * 128 + k * 8, dv + ((st * C::tile_bytes + k * 2048) >> 4), C::idesc_pv, j > 0 || k > 0 ? 1u : 0u);
-                            if (s == active - 1) tc_commit(bar(C::VEMPTY + st));
-                            if (j + 1 == stages) tc_commit(bar(C::OFULL + s));
-                        }
-                        __syncwarp();
                         if (j + 1 < stages) logits(s, j + 1);
                     }
                 }
@@ -412,9 +483,9 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
         const int s = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
         const unsigned lane_base = (unsigned)((warp & 3) * 32) << 16;
         const unsigned tS = tmem + s * 128 + lane_base, tO = tmem + 256 + s * 128 + lane_base;
-        const bool flip = a.scale < 0.f;                       // q changes sign, so that the largest product is the largest logit
-        // scale 0: q is taken as zero, so that a masked -inf stays one
-        const float qs = a.scale == 0.f ? 1.f : fabsf(a.scale) * (MODS && a.cap > 0.f ? 1.f / a.cap : CT_LOG2E);
+        const int step = 128 / a.G, my_token = row / a.G + s * step, my_head = row % a.G;          // token of the tile
+        const float qs = a.scale * (MODE == CAPPED ? 1.f / a.cap : CT_LOG2E);                      // PLAIN: positive
+        const bool wide = ((uintptr_t)a.out & 31) == 0;
         int n = 0, u = 0, seg = 0;
         bool dead = false, cut_end = false;
         auto wait = [&](int b, int phase) {
@@ -422,31 +493,15 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
             dead = __any_sync(0xffffffffu, dead);
         };
         while (walk.next(a, plan, g)) {
-            const int stages = g.s1 - g.s0, r = g.tile * CT_ROWS + s * 128 + row, t = r < g.T * a.G ? r / a.G : -1;
-            if (s == 1 && g.T * a.G - g.tile * CT_ROWS <= 128) {           // no rows for this stream
+            const int stages = g.s1 - g.s0, t = row < step * a.G && my_token < g.tokens ? g.tile * 2 * step + my_token : -1;
+            if (s == 1 && g.tokens <= step) {                  // no rows for this stream
                 n += stages;
                 continue;
             }
-            const size_t q_row = (size_t)(g.q0 + max(t, 0)) * a.Hq + g.h * a.G + (t < 0 ? 0 : r - t * a.G);
+            const size_t q_row = (size_t)(g.q0 + max(t, 0)) * a.Hq + g.h * a.G + my_head;
             ChunkRow w = {0, g.n, g.n - g.T + max(t, 0), 0.f};
             if (t >= 0) chunk_sees(a, g.q0 + t, w.place, g.n, w.lo, w.hi);
-            if (MODS && a.slopes && t >= 0) w.slope = a.slopes[g.h * a.G + r - t * a.G] * CT_LOG2E;
-            // ---- Q: this thread's row; rows that do not exist as zeros
-            {
-                const unsigned to = sQ + s * C::tile_bytes + row * 128;
-                const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + q_row * HD);
-                uint4 v[HD / 8];                               // all loads before the first store
-#pragma unroll
-                for (int c = 0; c < HD / 8; c++) v[c] = t >= 0 && a.scale != 0.f ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-                for (int c = 0; c < HD / 8; c++) {
-                    if (flip) { v[c].x ^= 0x80008000u; v[c].y ^= 0x80008000u; v[c].z ^= 0x80008000u; v[c].w ^= 0x80008000u; }
-                    sts16(to + (c >> 3) * C::panel_bytes + (((c & 7) ^ (row & 7)) << 4), v[c]);
-                }
-                tt_proxy_fence();
-                __syncwarp();
-                if (lane == 0) tc_mbar_arrive(bar(C::QFULL + s));
-            }
+            if (MODE != PLAIN && a.slopes) w.slope = a.slopes[g.h * a.G + my_head] * CT_LOG2E;
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < stages; j++, u++) {
                 const int key0 = (g.s0 + j) * CT_KEYS, st = (n + j) % NS;
@@ -469,9 +524,36 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     for (int c = 0; c < 4; c++) tc_ld32(tS + c * 32, x[c]);
                     tc_ld_wait();
                     float f = qs;                              // what is left to do to the logits
-                    if constexpr (MODS) {
+                    if constexpr (MODE == CAPPED) {
+                        float hi = 0.f;
 #pragma unroll
-                        for (int e = 0; e < CT_KEYS; e++) x[e >> 5][e & 31] = __float_as_uint(chunk_score(a, w, __uint_as_float(x[e >> 5][e & 31]) * qs, key0 + e));
+                        for (int e = 0; e < CT_KEYS; e += 2) hi = tt_max3(hi, fabsf(__uint_as_float(x[e >> 5][e & 31])), fabsf(__uint_as_float(x[e >> 5][(e & 31) + 1])));
+                        const float2 qs2 = make_float2(qs, qs);
+                        if (__any_sync(0xffffffffu, !(hi * fabsf(qs) <= CT_TANH_RANGE))) {
+#pragma unroll
+                            for (int e = 0; e < CT_KEYS; e++) x[e >> 5][e & 31] = __float_as_uint(tanh_far(__uint_as_float(x[e >> 5][e & 31]) * qs));
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < CT_KEYS; e += 2) {
+                                const float2 y = tanh_near2(mul2(make_float2(__uint_as_float(x[e >> 5][e & 31]), __uint_as_float(x[e >> 5][(e & 31) + 1])), qs2));
+                                x[e >> 5][e & 31] = __float_as_uint(y.x); x[e >> 5][(e & 31) + 1] = __float_as_uint(y.y);
+                            }
+                        }
+                        f = a.cap * CT_LOG2E;
+                    }
+                    if (MODE == BIASED || (MODE == CAPPED && a.slopes)) {
+                        const float2 f2 = make_float2(f, f);
+                        if (__all_sync(0xffffffffu, w.place >= key0 + CT_KEYS - 1)) {              // the distance falls from row to row
+                            const float2 base = make_float2(w.slope * (float)(key0 - w.place), w.slope * (float)(key0 - w.place)), sl = make_float2(w.slope, w.slope);
+#pragma unroll
+                            for (int e = 0; e < CT_KEYS; e += 2) {
+                                const float2 y = fma2(make_float2(__uint_as_float(x[e >> 5][e & 31]), __uint_as_float(x[e >> 5][(e & 31) + 1])), f2, fma2(sl, make_float2((float)e, (float)(e + 1)), base));
+                                x[e >> 5][e & 31] = __float_as_uint(y.x); x[e >> 5][(e & 31) + 1] = __float_as_uint(y.y);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < CT_KEYS; e++) x[e >> 5][e & 31] = __float_as_uint(fmaf(__uint_as_float(x[e >> 5][e & 31]), f, -w.slope * fabsf((float)(w.place - key0 - e))));
+                        }
                         f = 1.f;
                     }
                     if (__any_sync(0xffffffffu, w.lo > key0 || w.hi < key0 + CT_KEYS) || have != (1 << CT_PAGES) - 1) {
@@ -516,13 +598,22 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                             p[e] = pack_bf16(y.x, y.y);
                         }
                         tc_st16(tS + c * 16, p);
+                        if (c == 1) {                          // half of the weights are there
+                            tc_st_wait();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) tc_mbar_arrive(bar(C::PHALF + s));
+                        }
                     }
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tc_st_wait();
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc_mbar_arrive(bar(C::PFULL + s));
+                if (lane == 0) {
+                    if (dead) tc_mbar_arrive(bar(C::PHALF + s));
+                    tc_mbar_arrive(bar(C::PFULL + s));
+                }
             }
             n += stages;
             wait(C::OFULL + s, seg);
@@ -544,18 +635,21 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     for (int e = 0; e < 32; e++) { o[e] = __uint_as_float(v[e]); wild |= !(fabsf(o[e]) <= FLT_MAX); }
                     if (wild && t >= 0) {
                         float again[32];
-                        chunk_again<HD, F8>(a, g, w, q_row, a.cap > 0.f ? a.scale / a.cap : a.scale * CT_LOG2E, m == -INFINITY ? 0.f : m, c * 32, again);
+                        chunk_again<HD, F8>(a, g, w, q_row, MODE == CAPPED ? a.scale / a.cap : a.scale * CT_LOG2E, m == -INFINITY ? 0.f : m, c * 32, again);
 #pragma unroll
                         for (int e = 0; e < 32; e++) o[e] = again[e];
                     }
                     __syncwarp();
                     if (t >= 0) {
                         if (whole) {
-                            uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + q_row * HD + c * 32);
+                            __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(a.out) + q_row * HD + c * 32;
 #pragma unroll
-                            for (int e = 0; e < 4; e++)
-                                to[e] = make_uint4(pack_bf16(o[8 * e] * norm, o[8 * e + 1] * norm), pack_bf16(o[8 * e + 2] * norm, o[8 * e + 3] * norm),
-                                                   pack_bf16(o[8 * e + 4] * norm, o[8 * e + 5] * norm), pack_bf16(o[8 * e + 6] * norm, o[8 * e + 7] * norm));
+                            for (int e = 0; e < 2; e++) {
+                                unsigned p[8];
+#pragma unroll
+                                for (int i = 0; i < 8; i++) p[i] = pack_bf16(o[16 * e + 2 * i] * norm, o[16 * e + 2 * i + 1] * norm);
+                                store32(to + 16 * e, p, wide);
+                            }
                         } else {
                             // four columns of all rows side by side: the lanes' stores join
                             float4* to = reinterpret_cast<float4*>(a.acc) + (slot * (HD / 4) + c * 8) * CT_ROWS + s * 128 + row;
@@ -574,8 +668,10 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                 cut_end = true;
                 if (tid == 128) {
                     int* d = a.desc + (size_t)blockIdx.x * 8;
-                    d[DESC_FIRST] = range_owner(g.unit_start, plan.total[0] * a.Hk, (int)plan.total[1]);
-                    d[DESC_Q0] = g.q0; d[DESC_T] = g.T; d[DESC_H] = g.h; d[DESC_RT] = g.tile;
+                    int c = blockIdx.x;
+                    while (c > 0 && plan.starts[c].at > g.unit_start) c--;
+                    d[DESC_FIRST] = c;
+                    d[DESC_Q0] = g.q0 + g.tile * 2 * step; d[DESC_T] = g.tokens; d[DESC_H] = g.h;
                 }
             }
         }
@@ -590,43 +686,93 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
     if (tid == 0 && *s_abort) tree_status(a, DYNAKV_ST_INTERNAL);
 }
 
-template <int HD, bool F8, bool MODS>
+// Merges the records of the units that were cut: block (x = CTA in which the unit ends, y = 16 columns), a thread per row.
+template <int HD>
+__global__ void __launch_bounds__(CT_ROWS) k_chunk_merge(const TreeArgs a) {
+    pdl_wait();
+    const int* d = a.desc + (size_t)blockIdx.x * 8;
+    if (!d[DESC_VALID]) return;
+    const int step = 128 / a.G, rl = threadIdx.x, row = rl & 127, t = (rl >> 7) * step + row / a.G, c0 = d[DESC_FIRST], n = blockIdx.x - c0 + 1;
+    if (row >= step * a.G || t >= d[DESC_T]) return;
+    auto slot = [&](int i) { return (size_t)(c0 + i) * 2 + (i == 0 ? 1 : 0); };
+    const float4* acc = reinterpret_cast<const float4*>(a.acc) + (size_t)blockIdx.y * 4 * CT_ROWS + rl;
+    float m = -INFINITY, l = 0.f;
+    float4 o[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = 0; i < n; i++) {
+        const float2 x = a.ml[slot(i) * CT_ROWS + rl];
+        float4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = acc[(slot(i) * (HD / 4) + e) * CT_ROWS];
+        const float to = fmaxf(m, x.x), ref = to == -INFINITY ? 0.f : to, f0 = ex2(m - ref), f1 = ex2(x.x - ref);
+        m = to;
+        l = l * f0 + x.y * f1;
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            o[e] = make_float4(o[e].x * f0 + v[e].x * f1, o[e].y * f0 + v[e].y * f1, o[e].z * f0 + v[e].z * f1, o[e].w * f0 + v[e].w * f1);
+    }
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    const size_t at = (size_t)(d[DESC_Q0] + t) * a.Hq + d[DESC_H] * a.G + row % a.G;
+    uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at * HD + blockIdx.y * 16);
+#pragma unroll
+    for (int e = 0; e < 4; e += 2)
+        out[e / 2] = make_uint4(pack_bf16(o[e].x * f, o[e].y * f), pack_bf16(o[e].z * f, o[e].w * f), pack_bf16(o[e + 1].x * f, o[e + 1].y * f), pack_bf16(o[e + 1].z * f, o[e + 1].w * f));
+    if (a.lse && blockIdx.y == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * CT_LN2;
+}
+
+// ---------------------------------------------------------------------------------- host side
+
+// q [tokens][heads][HD]: a box is 64 elements of a group's heads of a stream's tokens.
+static bool chunk_query_map(CUtensorMap* map, const TreeArgs& a, int hd) {
+    const tree_encode_fn enc = tree_encode();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)hd, (cuuint64_t)a.Hq, (cuuint64_t)a.n_tokens}, strides[2] = {(cuuint64_t)hd * 2, (cuuint64_t)a.Hq * hd * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)(128 / a.G)}, estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static long long chunk_most_tiles(int64_t n_tokens, int G, int n_seqs) { return n_tokens / tile_tokens(G) + n_seqs; }
+
+template <int HD, bool F8, int MODE>
 static int chunk_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
     using C = TcChunk<HD, F8>;
-    CUtensorMap mk = {}, mv = {};              // FP8 rows are fetched by plain loads: that kernel looks at neither
+    CUtensorMap mq, mk = {}, mv = {};          // FP8 rows are fetched by plain loads
+    if (!chunk_query_map(&mq, a, HD)) return DYNAKV_ERR_CUDA;
     if (!F8 && (!tree_page_map(&mk, cache, cache->k, false) || !tree_page_map(&mv, cache, cache->v, false))) return DYNAKV_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
-    if (!allow_smem(k_chunk_tc<HD, F8, MODS>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
+    if (!allow_smem(k_chunk_tc<HD, F8, MODE>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
     // the warpgroups' shares of the registers add up to what the launch gets, or the kernel would wait for them forever
     static const int regs = [] {
         cudaFuncAttributes f;
-        return cudaFuncGetAttributes(&f, k_chunk_tc<HD, F8, MODS>) == cudaSuccess ? f.numRegs : 0;
+        return cudaFuncGetAttributes(&f, k_chunk_tc<HD, F8, MODE>) == cudaSuccess ? f.numRegs : 0;
     }();
     if (regs * (C::threads / 128) < 2 * C::regs_softmax + C::regs_rest + (F8 ? C::regs_convert : 0)) return DYNAKV_ERR_CUDA;
-    const long long most = a.n_tokens * a.G / CT_ROWS + a.n_seqs;
-    if (launch_pdl(k_chunk_plan, dim3(1), dim3(PLAN_THREADS), 0, st, a, plan, sms, 1, most) != cudaSuccess) return DYNAKV_ERR_CUDA;
-    if (launch_pdl(k_chunk_tc<HD, F8, MODS>, dim3(sms), dim3(C::threads), C::smem, st, mk, mv, a, plan) != cudaSuccess) return DYNAKV_ERR_CUDA;
-    return tree_merge_launch(HD, CT_ROWS, false, a, sms, st);
+    if (launch_pdl(k_chunk_plan, dim3(1), dim3(PLAN_THREADS), 0, st, a, plan, sms, chunk_most_tiles(a.n_tokens, a.G, a.n_seqs)) != cudaSuccess) return DYNAKV_ERR_CUDA;
+    if (launch_pdl(k_chunk_tc<HD, F8, MODE>, dim3(sms), dim3(C::threads), C::smem, st, mq, mk, mv, a, plan) != cudaSuccess) return DYNAKV_ERR_CUDA;
+    return launch_pdl(k_chunk_merge<HD>, dim3(sms, HD / 16), dim3(CT_ROWS), 0, st, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
 template <int HD, bool F8>
-static int chunk_tc_launch_mods(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
-    return a.cap > 0.f || a.slopes ? chunk_tc_launch_as<HD, F8, true>(cache, a, plan, sms, st) : chunk_tc_launch_as<HD, F8, false>(cache, a, plan, sms, st);
+static int chunk_tc_launch_mode(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
+    // PLAIN takes the largest product for the largest logit; BIASED multiplies first
+    if (a.cap > 0.f) return chunk_tc_launch_as<HD, F8, CAPPED>(cache, a, plan, sms, st);
+    return a.slopes || !(a.scale > 0.f) ? chunk_tc_launch_as<HD, F8, BIASED>(cache, a, plan, sms, st) : chunk_tc_launch_as<HD, F8, PLAIN>(cache, a, plan, sms, st);
 }
 template <int HD>
 static int chunk_tc_launch_hd(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
-    return cache->kv_dtype == DYNAKV_FP8 ? chunk_tc_launch_mods<HD, true>(cache, a, plan, sms, st) : chunk_tc_launch_mods<HD, false>(cache, a, plan, sms, st);
+    return cache->kv_dtype == DYNAKV_FP8 ? chunk_tc_launch_mode<HD, true>(cache, a, plan, sms, st) : chunk_tc_launch_mode<HD, false>(cache, a, plan, sms, st);
 }
 
 // The plan's part of the workspace behind the records'.
 size_t chunk_plan_space(int64_t n_tokens, int G, int n_seqs, int ctas, size_t at, char* base, ChunkPlan* plan) {
-    const size_t tiles = (size_t)(n_tokens * G / CT_ROWS) + n_seqs;
+    const size_t tiles = (size_t)chunk_most_tiles(n_tokens, G, n_seqs);
     auto take = [&](size_t bytes) { const size_t x = (at + 15) / 16 * 16; at = x + bytes; return base + x; };
     ChunkPlan p;
     p.tiles = reinterpret_cast<ChunkTile*>(take(tiles * sizeof(ChunkTile)));
     p.before = reinterpret_cast<long long*>(take((tiles + 1) * 8));
-    p.seqs = reinterpret_cast<ChunkSeq*>(take(((size_t)n_seqs + 1) * sizeof(ChunkSeq)));
     p.starts = reinterpret_cast<ChunkStart*>(take((size_t)ctas * sizeof(ChunkStart)));
-    p.total = reinterpret_cast<long long*>(take(16));
     if (plan) *plan = p;
     return at;
 }
