@@ -18,9 +18,10 @@ constexpr int CT_ROWS = 256, CT_KEYS = 128, CT_PAGES = CT_KEYS / PAGE;
 #define DKV_CHUNK_UNIT_COST 2
 #endif
 constexpr int CT_UNIT_COST = DKV_CHUNK_UNIT_COST;
+constexpr int CT_WHOLE = 12;                       // stages up to which a unit is not cut
 
 struct __align__(16) ChunkTile {
-    int seq, tile, from, stages;                   // of the sequence; first stage, stages
+    int seq, tile, from, stages;                   // 2 * tile of the sequence, + 1 the last; first stage, stages
     int q0, T, n, first;                           // the sequence's first packed token, tokens, rows and first tile
 };
 struct __align__(16) ChunkStart {                  // where a CTA begins: tile, KV head, stage of the unit; stages it has in all
@@ -49,26 +50,26 @@ struct ChunkWalk {
     int e, h, off, left;
     long long at;
     ChunkTile t, ahead;
-    __device__ __forceinline__ void start(const TreeArgs& a, const ChunkPlan& p) {
+    __device__ __forceinline__ void start(const ChunkPlan& p) {
         const ChunkStart c = p.starts[blockIdx.x];
         e = c.tile; h = c.head; off = c.off; left = c.left; at = c.at;
         if (left > 0) ahead = p.tiles[e];
     }
-    __device__ __forceinline__ bool next(const TreeArgs& a, const ChunkPlan& p, ChunkSeg& g) {
+    __device__ __forceinline__ bool next(int heads, int per, const ChunkPlan& p, ChunkSeg& g) {
         if (left <= 0) return false;
         t = ahead;
-        const int here = min(left, t.stages - off), per = tile_tokens(a.G);
-        g.seq = t.seq; g.h = h; g.tile = t.tile;
+        const int here = min(left, t.stages - off);
+        g.seq = t.seq; g.h = h; g.tile = t.tile >> 1;
         g.s0 = t.from + off; g.s1 = g.s0 + here;
         g.q0 = t.q0; g.T = t.T; g.n = t.n;
-        g.tokens = min(per, t.T - t.tile * per);
+        g.tokens = min(per, t.T - g.tile * per);
         g.first = off == 0; g.last = off + here == t.stages;
         g.unit_start = at - off;
         at += here; left -= here; off = 0;
         if (left > 0) {                            // the next tile, or the sequence's next head, or the next sequence
             e++;
-            if (e == t.first + seq_tiles(t.T, a.G)) {
-                if (h + 1 < a.Hk) { h++; e = t.first; }
+            if (t.tile & 1) {
+                if (h + 1 < heads) { h++; e = t.first; }
                 else h = 0;
             }
             ahead = p.tiles[e];

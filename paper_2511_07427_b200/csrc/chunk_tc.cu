@@ -9,10 +9,12 @@
 //   warp 1               tcgen05.mma of both streams
 //   warp 3               TMA loads of the next unit's queries, when the last logits of this one have been multiplied
 //   warps 4-7 / 8-11     softmax of stream 0 / 1: a query row per thread
-//   warps 12-15          FP8 rows only: they fetch the rows and turn them into bf16 stages (warps 0 and 2 then rest)
+//   warps 12-15          FP8 rows only: they turn the rows, which warps 0 and 2 then fetch as they are, into bf16 stages
 // Weights enter the products as bf16 (2^-9 of each).
 #include <cuda.h>
 #include <float.h>
+
+#include <type_traits>
 
 #include "bulk_copy.cuh"
 #include "chunk_plan.cuh"
@@ -24,9 +26,11 @@
 
 namespace dkv {
 
-constexpr int CT_CONVERT = 128;                                // FP8: threads that load rows and convert them
+constexpr int CT_CONVERT = 128;                                // FP8: threads that turn rows into bf16
 constexpr float CT_LOG2E = 1.4426950408889634f, CT_LN2 = 0.6931471805599453f;
-constexpr float CT_LAZY = 8.f;                                 // the softmax's reference moves when the maximum has outgrown it by 2^8
+// The softmax's reference moves when the maximum has outgrown it by 2^24, so that O is rescaled next to never: weights have the range of
+// fp32, and sums of 2^24 rows' weights times V stay below its end up to |V| = 2^79.
+constexpr float CT_LAZY = 24.f;
 
 // ---------------------------------------------------------------------------------- the plan
 
@@ -65,7 +69,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
             incl = scan(count, total);
         }
         const int first = (int)(tiles + incl - count);
-        for (int src = 0; src < 32; src++) {                   // few sequences have many tiles, so a warp writes a sequence's
+        for (unsigned left = __ballot_sync(0xffffffffu, count > 0); left; left &= left - 1) {      // few sequences have many tiles, so a warp writes a sequence's
+            const int src = __ffs(left) - 1;
             const int c = __shfl_sync(0xffffffffu, count, src), f = __shfl_sync(0xffffffffu, first, src), q0 = __shfl_sync(0xffffffffu, s.q0, src),
                       T = __shfl_sync(0xffffffffu, s.T, src), n = __shfl_sync(0xffffffffu, s.n, src);
             for (int i = lane; i < c; i += 32) {
@@ -75,25 +80,30 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
                     lo = a.window > 0 ? max(0, place + from + 1 - a.window) : 0;
                     hi = place + to;
                 }
-                p.tiles[f + i] = {b0 + warp * 32 + src, i, lo, hi, q0, T, n, f};
+                p.tiles[f + i] = {b0 + warp * 32 + src, 2 * i + (i == c - 1 ? 1 : 0), lo, hi, q0, T, n, f};
             }
         }
         tiles += total;
     }
     __syncthreads();
-    // ---- stages of every tile; where the tokens' ranges have to be read, a warp per tile finds the first and the last row
+    // ---- stages of every tile; where the tokens' ranges have to be read, 8 lanes per tile find the first and the last row
     if (a.rows_from || a.rows_to) {
-        for (int i = warp; i < tiles; i += 32) {
-            const ChunkTile t = p.tiles[i];
-            const int from = t.tile * per, to = min(t.T, from + per);
-            int lo = t.n, hi = 0;
-            for (int x = from + lane; x < to; x += 32) {
-                int l, h;
-                chunk_sees(a, t.q0 + x, t.n - t.T + x, t.n, l, h);
-                if (l < h) { lo = min(lo, max(l, 0)); hi = max(hi, h); }
+        for (int i0 = warp * 4; i0 < tiles; i0 += PLAN_THREADS / 8) {
+            const int i = i0 + (lane >> 3);
+            int lo = 0x7fffffff, hi = 0;
+            if (i < tiles) {
+                const ChunkTile t = p.tiles[i];
+                const int from = (t.tile >> 1) * per, to = min(t.T, from + per);
+#pragma unroll 4
+                for (int x = from + (lane & 7); x < to; x += 8) {
+                    int l, h;
+                    chunk_sees(a, t.q0 + x, t.n - t.T + x, t.n, l, h);
+                    if (l < h) { lo = min(lo, max(l, 0)); hi = max(hi, h); }
+                }
             }
-            lo = __reduce_min_sync(0xffffffffu, lo); hi = __reduce_max_sync(0xffffffffu, hi);
-            if (lane == 0) { p.tiles[i].from = lo; p.tiles[i].stages = hi; }
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) { lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o)); hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o)); }
+            if (i < tiles && (lane & 7) == 0) { p.tiles[i].from = lo; p.tiles[i].stages = hi; }
         }
         __syncthreads();
     }
@@ -135,7 +145,17 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
             const long long y = lead + cost - st.head * all;
             st.tile = find(y, e0, e1);
             st.off = (int)max(0ll, y - before[st.tile] - (long long)(st.tile + 1) * CT_UNIT_COST);
+            // a short unit is not cut where a CTA has several: two records and their merge cost more than what it adds to one side
+            const int whole = (int)(before[st.tile + 1] - before[st.tile]);
+            if (whole <= CT_WHOLE && (whole + CT_UNIT_COST) * 3ll * C <= W) st.off = st.off * 2 >= whole ? whole : 0;
             st.at = before[e0] * a.Hk + st.head * (before[e1] - before[e0]) + before[st.tile] - before[e0] + st.off;
+            if (st.off == whole) {                             // the unit behind it
+                st.off = 0;
+                if (++st.tile == e1) {
+                    if (st.head + 1 < a.Hk) { st.head++; st.tile = e0; }
+                    else st.head = 0;
+                }
+            }
         }
         at_s[tid] = st.at;
         __syncthreads();
@@ -157,8 +177,10 @@ struct TcChunk {
     static constexpr int panel_bytes = 128 * 128;              // 128 rows of 128 bytes
     static constexpr int tile_bytes = panels * panel_bytes;
     static constexpr int stages = 2;                           // of K and V each
+    static constexpr int raw_bytes = F8 ? CT_KEYS * HD : 0;    // FP8 rows as they come, one stage of K and of V, then their exponents
+    static constexpr int exp_bytes = F8 ? CT_KEYS : 0;
     static constexpr int fixed = 32 * 8 + 8 * 4 + 16;
-    static constexpr int smem = (2 + 2 * stages) * tile_bytes + fixed;
+    static constexpr int smem = (2 + 2 * stages) * tile_bytes + 2 * (raw_bytes + exp_bytes) + fixed;
     static_assert(smem + 1024 <= 233472, "shared memory of an SM");
     // registers a thread: what the launch gives (64 K over all threads, in steps of 8) is shared out anew among the warpgroups
     static constexpr int regs_rest = F8 ? 64 : 104, regs_softmax = F8 ? 184 : 200, regs_convert = 80;
@@ -168,7 +190,7 @@ struct TcChunk {
     static constexpr unsigned idesc_qk = idesc | ((unsigned)(CT_KEYS >> 3) << 17);
     static constexpr unsigned idesc_pv = idesc | (1u << 16) | ((unsigned)(HD >> 3) << 17);      // B's contraction index is its outer one
     static constexpr int KFULL = 0, KEMPTY = stages, VFULL = 2 * stages, VEMPTY = 3 * stages, SFULL = 4 * stages, OFULL = SFULL + 2,
-                         QFULL = OFULL + 2, QEMPTY = QFULL + 2, DRAIN = QEMPTY + 2, PHALF = DRAIN + 1, PFULL = PHALF + 2, count = PFULL + 2;
+                         QFULL = OFULL + 2, QEMPTY = QFULL + 2, DRAIN = QEMPTY + 2, PFULL = DRAIN + 1, RAWEMPTY = PFULL + 2, RAWFULL = RAWEMPTY + 2, count = RAWFULL + 2;
     static_assert(count <= 32, "barrier block");
 };
 
@@ -189,19 +211,32 @@ struct ChunkRow {
     int lo, hi, place;
     float slope;
 };
+__device__ __forceinline__ int lds_s8(unsigned addr) {
+    int v;
+    asm volatile("ld.shared.s8 %0, [%1];\n" : "=r"(v) : "r"(addr));
+    return v;
+}
 // What the scores need beside the factor and the mask.
 enum { PLAIN = 0, BIASED = 1, CAPPED = 2 };
-// tanh(y) / y for |y| <= 1 as a polynomial of y^2 (interpolated at Chebyshev nodes; tanh is off by 9e-8 at most), two at a time.
-constexpr float CT_TANH_RANGE = 1.f;
+// tanh(y) / y as a polynomial of y^2 (interpolated at Chebyshev nodes; tanh is off by 9e-8 at most), two at a time: for |y| <= 0.4, which
+// is what a cap well above the logits gives, and for |y| <= 1.  The FMA pipe is what this costs: 5 and 9 instructions' worth per logit.
+constexpr float CT_TANH_SHORT = 0.4f, CT_TANH_LONG = 1.f;
+template <bool SHORT>
 __device__ __forceinline__ float2 tanh_near2(float2 y) {
     const float2 z = mul2(y, y);
     auto c = [](float x) { return make_float2(x, x); };
-    float2 p = fma2(c(-0.0003548834f), z, c(0.0022876456f));
-    p = fma2(p, z, c(-0.0079249460f));
-    p = fma2(p, z, c(0.0214699805f));
-    p = fma2(p, z, c(-0.0538727380f));
-    p = fma2(p, z, c(0.1333219111f));
-    p = fma2(p, z, c(-0.3333328068f));
+    float2 p;
+    if constexpr (SHORT) {
+        p = fma2(c(-0.0475610755f), z, c(0.1327115595f));
+        p = fma2(p, z, c(-0.3333137333f));
+    } else {
+        p = fma2(c(-0.0003548834f), z, c(0.0022876456f));
+        p = fma2(p, z, c(-0.0079249460f));
+        p = fma2(p, z, c(0.0214699805f));
+        p = fma2(p, z, c(-0.0538727380f));
+        p = fma2(p, z, c(0.1333219111f));
+        p = fma2(p, z, c(-0.3333328068f));
+    }
     p = fma2(p, z, c(1.f));
     return mul2(p, y);
 }
@@ -238,6 +273,8 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
     constexpr int NS = C::stages;
     extern __shared__ __align__(1024) unsigned char ct_smem[];
     unsigned char* at = ct_smem + (2 + 2 * NS) * C::tile_bytes;
+    const unsigned sRaw = tc_smem_u32(at); at += 2 * C::raw_bytes;                 // K, V
+    const unsigned sExp = tc_smem_u32(at); at += 2 * C::exp_bytes;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(at); at += 32 * 8;
     volatile int* meta = reinterpret_cast<volatile int*>(at); at += 8 * 4;         // [stage number mod 8] bit per page: it was loaded
     volatile unsigned* s_tmem = reinterpret_cast<volatile unsigned*>(at);
@@ -252,7 +289,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
     if (tid == 0) {
         for (int i = 0; i < C::count; i++) {
             const bool full = (i >= C::KFULL && i < C::KEMPTY) || (i >= C::VFULL && i < C::VEMPTY);
-            tc_mbar_init(bar(i), full && F8 ? CT_CONVERT / 32 : i >= C::PHALF ? 4 : 1);
+            tc_mbar_init(bar(i), (full && F8) || (i >= C::PFULL && i < C::RAWFULL) ? 4 : 1);             // 4: warps
         }
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -272,8 +309,9 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
     const unsigned tmem = *s_tmem;
     pdl_wait();                                                // from here on the results of earlier kernels are read
     pdl_trigger();
+    const int tokens = tile_tokens(a.G);
     ChunkWalk walk;
-    walk.start(a, plan);
+    walk.start(plan);
     ChunkSeg g = {};
     auto give_up = [&]() { *s_abort = 1; };
     // pages of stage s of the walk's segment that exist and are known to the table, as bits; ids by lane (4 lanes)
@@ -289,17 +327,18 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
 
     if (warp < 4) {
         regs_down<C::regs_rest>();
-        if (!F8 && (warp == 0 || warp == 2)) {
+        if (warp == 0 || warp == 2) {
             // =============================== loads: warp 0 K, warp 2 V ===============================
             const bool is_v = warp == 2;
             const CUtensorMap* map = is_v ? &map_v : &map_k;
-            const int full = is_v ? C::VFULL : C::KFULL, empty = is_v ? C::VEMPTY : C::KEMPTY;
+            constexpr int RING = F8 ? 1 : NS;
+            const int full = F8 ? C::RAWFULL + is_v : is_v ? C::VFULL : C::KFULL, empty = F8 ? C::RAWEMPTY + is_v : is_v ? C::VEMPTY : C::KEMPTY;
             int n = 0;                                         // stage number in the CTA
             bool ok = true;
-            while (ok && walk.next(a, plan, g)) {
+            while (ok && walk.next(a.Hk, tokens, plan, g)) {
                 int id = page_of(g.s0);
                 for (int s = g.s0; s < g.s1 && ok; s++, n++) {
-                    const int st = n % NS, use = n / NS, now = id;
+                    const int st = n % RING, use = n / RING, now = id;
                     if (s + 1 < g.s1) id = page_of(s + 1);
                     const int bits = (int)__ballot_sync(0xffffffffu, now >= 0);
                     int page[CT_PAGES];
@@ -309,12 +348,18 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                         ok = !*s_abort && (use == 0 || mbar_wait(bar(empty + st), (unsigned)(use - 1) & 1u));
                         if (ok) {
                             if (!is_v) meta[n & 7] = bits;
-                            if (bits) tc_mbar_expect_tx(bar(full + st), __popc(bits) * PAGE * HD * 2);
+                            if (bits) tc_mbar_expect_tx(bar(full + st), __popc(bits) * PAGE * (F8 ? HD + 1 : HD * 2));
                             else tc_mbar_arrive(bar(full + st));
-                            const unsigned dst = is_v ? sV(st) : sK(st);
+                            const unsigned dst = F8 ? sRaw + is_v * C::raw_bytes : is_v ? sV(st) : sK(st);
 #pragma unroll
                             for (int x = 0; x < CT_PAGES; x++) {
                                 if (page[x] < 0) continue;
+                                if constexpr (F8) {
+                                    const int r = (page[x] * a.Hk + g.h) * PAGE;
+                                    tt_load(dst + x * PAGE * HD, map, r, 0, bar(full));
+                                    bulk_g2s(sExp + is_v * C::exp_bytes + x * PAGE, (is_v ? a.vexp : a.kexp) + r, PAGE, bar(full));
+                                    continue;
+                                }
 #pragma unroll
                                 for (int q = 0; q < C::panels; q++)
                                     tt_load(dst + q * C::panel_bytes + x * PAGE * 128, map, (page[x] * a.Hk + g.h) * PAGE, q, bar(full + st));
@@ -327,15 +372,15 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
             if (!ok && lane == 0) {
                 give_up();
                 // stage n - 1 was not issued; let the copies of the ones before it land before the block ends
-                for (int x = max(0, n - 1 - NS); x < n - 1; x++) mbar_wait(bar(full + x % NS), (unsigned)(x / NS) & 1u);
+                for (int x = max(0, n - 1 - RING); x < n - 1; x++) mbar_wait(bar(full + x % RING), (unsigned)(x / RING) & 1u);
             }
         } else if (warp == 3) {
             // =============================== queries ===============================
             // A stream's rows are the heads of the group of 128 / G tokens; tokens behind the chunk's last come along and are not used.
-            const int step = 128 / a.G;
+            const int step = tokens / 2;
             int segs[2] = {0, 0};
             bool ok = true;
-            while (ok && walk.next(a, plan, g)) {
+            while (ok && walk.next(a.Hk, tokens, plan, g)) {
                 for (int s = 0; s < (g.tokens > step ? 2 : 1) && ok; s++, __syncwarp()) {
                     if (lane == 0) {
                         ok = !*s_abort && (segs[s] == 0 || mbar_wait(bar(C::QEMPTY + s), (unsigned)(segs[s] - 1) & 1u));
@@ -361,8 +406,8 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
             bool ok = true;
             const unsigned long long dq[2] = {tc_panel_desc(sQ), tc_panel_desc(sQ + C::tile_bytes)}, dk = tc_panel_desc(sK(0)), dv = tc_rows_desc(sV(0), C::panel_bytes);
             auto wait = [&](int b, int phase) { ok = ok && mbar_wait(bar(b), (unsigned)phase & 1u); ok = __all_sync(0xffffffffu, ok); };
-            while (ok && walk.next(a, plan, g)) {
-                const int stages = g.s1 - g.s0, active = g.tokens > 128 / a.G ? 2 : 1;
+            while (ok && walk.next(a.Hk, tokens, plan, g)) {
+                const int stages = g.s1 - g.s0, active = g.tokens > tokens / 2 ? 2 : 1;
                 auto logits = [&](int s, int j) {              // of stage j of the segment
                     const int st = (n + j) % NS;
                     if (s == 0) wait(C::KFULL + st, (n + j) / NS);
@@ -386,23 +431,18 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     const int st = (n + j) % NS;
                     for (int s = 0; s < active && ok; s++) {
                         if (s == 0) wait(C::VFULL + st, (n + j) / NS);
-                        // the weights of the first 64 rows are used while the others are made
-#pragma unroll
-                        for (int half = 0; half < 2; half++) {
-                            wait((half ? C::PFULL : C::PHALF) + s, u[s]);
-                            if (!ok) break;
-                            tc_fence_after();
-                            if (elect_one()) {
-#pragma unroll
-                                for (int k = half * (CT_KEYS / 32); k < (half + 1) * (CT_KEYS / 32); k++)
-                                    tc_mma_f16_ta(tmem + 256 + s * 128, tmem + s * 128 + k * 8, dv + ((st * C::tile_bytes + k * 2048) >> 4), C::idesc_pv, j > 0 || k > 0 ? 1u : 0u);
-                                if (half && s == active - 1) tc_commit(bar(C::VEMPTY + st));
-                                if (half && j + 1 == stages) tc_commit(bar(C::OFULL + s));
-                            }
-                            __syncwarp();
-                        }
+                        wait(C::PFULL + s, u[s]);
                         if (!ok) break;
                         u[s]++;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < CT_KEYS / 16; k++)
+                                tc_mma_f16_ta(tmem + 256 + s * 128, tmem + s * 128 + k * 8, dv + ((st * C::tile_bytes + k * 2048) >> 4), C::idesc_pv, j > 0 || k > 0 ? 1u : 0u);
+                            if (s == active - 1) tc_commit(bar(C::VEMPTY + st));
+                            if (j + 1 == stages) tc_commit(bar(C::OFULL + s));
+                        }
+                        __syncwarp();
                         if (j + 1 < stages) logits(s, j + 1);
                     }
                 }
@@ -419,44 +459,30 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
         }
     } else if (F8 && warp >= 12) {
         // =============================== FP8 rows to bf16 stages ===============================
-        // A thread takes the same 16 bytes of every RPP-th row of a stage.  K and V alternate: while one is converted (exactly: e4m3
-        // times a power of two is a bf16 value) and stored where the TMA would have put it, the other's loads are under way.
+        // A thread takes the same 16 bytes of every RPP-th row of a stage, as the TMA has put them, and stores them where it would put
+        // bf16 rows (exactly: e4m3 times a power of two is a bf16 value).
         regs_down<C::regs_convert>();
         constexpr int CPR = HD / 16, RPP = CT_CONVERT / CPR, NP = CT_KEYS / RPP;
         const int ct = tid - 384, chunk = ct % CPR, row0 = ct / CPR;
         int n = 0;
         bool ok = true;
         auto wait = [&](int b, int phase) { ok = ok && mbar_wait(bar(b), (unsigned)phase & 1u); ok = __all_sync(0xffffffffu, ok); };
-        while (ok && walk.next(a, plan, g)) {
+        while (ok && walk.next(a.Hk, tokens, plan, g)) {
             for (int s = g.s0; s < g.s1 && ok; s++, n++) {
-                const int st = n % NS, use = n / NS, id = page_of(s);
-                const int bits = (int)__ballot_sync(0xffffffffu, id >= 0);
-                int page[CT_PAGES];
-#pragma unroll
-                for (int x = 0; x < CT_PAGES; x++) page[x] = __shfl_sync(0xffffffffu, id, x);
+                const int st = n % NS, use = n / NS;
 #pragma unroll 1
                 for (int kv = 0; kv < 2; kv++) {
-                    const unsigned char* pool = kv ? a.vpool : a.kpool;
-                    const signed char* exps = kv ? a.vexp : a.kexp;
-                    uint4 raw[NP];
-                    int ex[NP];
-#pragma unroll
-                    for (int i = 0; i < NP; i++) {
-                        const int pg = page[i * RPP / PAGE];
-                        const size_t r = ((size_t)(pg < 0 ? 0 : pg) * a.Hk + g.h) * PAGE + (i * RPP + row0) % PAGE;
-                        raw[i] = pg >= 0 ? __ldg(reinterpret_cast<const uint4*>(pool + r * HD) + chunk) : make_uint4(0u, 0u, 0u, 0u);
-                        ex[i] = pg >= 0 ? (int)__ldg(exps + r) : 0;
-                    }
+                    wait(C::RAWFULL + kv, n);
                     if (use > 0) wait((kv ? C::VEMPTY : C::KEMPTY) + st, use - 1);
                     if (!ok) break;
-                    if (ct == 0 && kv == 0) meta[n & 7] = bits;
-                    const unsigned dst = kv ? sV(st) : sK(st);
+                    const unsigned dst = kv ? sV(st) : sK(st), from = sRaw + kv * C::raw_bytes, exps = sExp + kv * C::exp_bytes;
 #pragma unroll
                     for (int i = 0; i < NP; i++) {
                         const int row = i * RPP + row0;
-                        const float sc = pow2f(ex[i]);
+                        const uint4 raw = lds16(from + row * HD + ((HD == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3)) << 4));
+                        const float sc = pow2f(lds_s8(exps + row));
                         const float2 sc2 = make_float2(sc, sc);
-                        const unsigned w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                        const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
                         unsigned o[8];
 #pragma unroll
                         for (int x = 0; x < 4; x++) {
@@ -472,7 +498,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     }
                     tt_proxy_fence();
                     __syncwarp();
-                    if (lane == 0) tc_mbar_arrive(bar((kv ? C::VFULL : C::KFULL) + st));
+                    if (lane == 0) { tc_mbar_arrive(bar(C::RAWEMPTY + kv)); tc_mbar_arrive(bar((kv ? C::VFULL : C::KFULL) + st)); }
                 }
             }
         }
@@ -483,7 +509,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
         const int s = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
         const unsigned lane_base = (unsigned)((warp & 3) * 32) << 16;
         const unsigned tS = tmem + s * 128 + lane_base, tO = tmem + 256 + s * 128 + lane_base;
-        const int step = 128 / a.G, my_token = row / a.G + s * step, my_head = row % a.G;          // token of the tile
+        const int step = tokens / 2, my_token = row / a.G + s * step, my_head = row % a.G;          // token of the tile
         const float qs = a.scale * (MODE == CAPPED ? 1.f / a.cap : CT_LOG2E);                      // PLAIN: positive
         const bool wide = ((uintptr_t)a.out & 31) == 0;
         int n = 0, u = 0, seg = 0;
@@ -492,7 +518,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
             if (!dead && !mbar_wait(bar(b), (unsigned)phase & 1u)) { dead = true; give_up(); }
             dead = __any_sync(0xffffffffu, dead);
         };
-        while (walk.next(a, plan, g)) {
+        while (walk.next(a.Hk, tokens, plan, g)) {
             const int stages = g.s1 - g.s0, t = row < step * a.G && my_token < g.tokens ? g.tile * 2 * step + my_token : -1;
             if (s == 1 && g.tokens <= step) {                  // no rows for this stream
                 n += stages;
@@ -529,15 +555,19 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
 #pragma unroll
                         for (int e = 0; e < CT_KEYS; e += 2) hi = tt_max3(hi, fabsf(__uint_as_float(x[e >> 5][e & 31])), fabsf(__uint_as_float(x[e >> 5][(e & 31) + 1])));
                         const float2 qs2 = make_float2(qs, qs);
-                        if (__any_sync(0xffffffffu, !(hi * fabsf(qs) <= CT_TANH_RANGE))) {
-#pragma unroll
-                            for (int e = 0; e < CT_KEYS; e++) x[e >> 5][e & 31] = __float_as_uint(tanh_far(__uint_as_float(x[e >> 5][e & 31]) * qs));
-                        } else {
+                        hi *= fabsf(qs);
+                        auto near = [&](auto is_short) {
 #pragma unroll
                             for (int e = 0; e < CT_KEYS; e += 2) {
-                                const float2 y = tanh_near2(mul2(make_float2(__uint_as_float(x[e >> 5][e & 31]), __uint_as_float(x[e >> 5][(e & 31) + 1])), qs2));
+                                const float2 y = tanh_near2<decltype(is_short)::value>(mul2(make_float2(__uint_as_float(x[e >> 5][e & 31]), __uint_as_float(x[e >> 5][(e & 31) + 1])), qs2));
                                 x[e >> 5][e & 31] = __float_as_uint(y.x); x[e >> 5][(e & 31) + 1] = __float_as_uint(y.y);
                             }
+                        };
+                        if (__all_sync(0xffffffffu, hi <= CT_TANH_SHORT)) near(std::true_type());
+                        else if (__all_sync(0xffffffffu, hi <= CT_TANH_LONG)) near(std::false_type());
+                        else {
+#pragma unroll
+                            for (int e = 0; e < CT_KEYS; e++) x[e >> 5][e & 31] = __float_as_uint(tanh_far(__uint_as_float(x[e >> 5][e & 31]) * qs));
                         }
                         f = a.cap * CT_LOG2E;
                     }
@@ -556,12 +586,23 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                         }
                         f = 1.f;
                     }
+                    // Which pages of the stage nobody in the warp sees, and which not everybody: the former are left out.
+                    unsigned none = 0u;
                     if (__any_sync(0xffffffffu, w.lo > key0 || w.hi < key0 + CT_KEYS) || have != (1 << CT_PAGES) - 1) {
 #pragma unroll
                         for (int c = 0; c < 4; c++) {
                             const int from = w.lo - key0 - c * 32, to = ((have >> c) & 1) ? w.hi - key0 - c * 32 : 0;
+                            if (__all_sync(0xffffffffu, from >= 32 || to <= 0 || from >= to)) {
+                                none |= 1u << c;
 #pragma unroll
-                            for (int e = 0; e < 32; e++) if (e < from || e >= to) x[c][e] = 0xff800000u;
+                                for (int e = 0; e < 32; e++) x[c][e] = 0xff800000u;
+                            }
+                            else if (__any_sync(0xffffffffu, from > 0 || to < 32)) {
+                                const int y = min(to, 32), z = max(from, 0);
+                                const unsigned win = z >= y ? 0u : (y == 32 ? ~0u : (1u << y) - 1u) & ~((1u << z) - 1u);
+#pragma unroll
+                                for (int e = 0; e < 32; e++) if (!((win >> e) & 1u)) x[c][e] = 0xff800000u;
+                            }
                         }
                     }
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -571,8 +612,9 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     const bool move = mx > m + CT_LAZY;
                     if (__any_sync(0xffffffffu, move)) {
                         const float to = move ? mx : m, down = to == -INFINITY ? 1.f : ex2(m - to);
+                        const bool carry = move && l > 0.f;    // without weights so far O is zero
                         m = to; l *= down;
-                        if (j > 0) {
+                        if (__any_sync(0xffffffffu, carry)) {
 #pragma unroll 1
                             for (int c = 0; c < HD / 16; c++) {
                                 unsigned o[16];
@@ -587,8 +629,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     const float ref = m == -INFINITY ? 0.f : m;
                     const float2 f2 = make_float2(f, f), ref2 = make_float2(-ref, -ref);
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-                    for (int c = 0; c < CT_KEYS / 32; c++) {
+                    auto weights = [&](int c) {
                         unsigned p[16];
 #pragma unroll
                         for (int e = 0; e < 16; e++) {
@@ -598,11 +639,16 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                             p[e] = pack_bf16(y.x, y.y);
                         }
                         tc_st16(tS + c * 16, p);
-                        if (c == 1) {                          // half of the weights are there
-                            tc_st_wait();
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) tc_mbar_arrive(bar(C::PHALF + s));
+                    };
+                    if (none == 0u) {                          // one run of instructions without a branch
+#pragma unroll
+                        for (int c = 0; c < 4; c++) weights(c);
+                    } else {
+                        const unsigned zero[16] = {};
+#pragma unroll
+                        for (int c = 0; c < 4; c++) {
+                            if ((none >> c) & 1u) tc_st16(tS + c * 16, zero);
+                            else weights(c);
                         }
                     }
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
@@ -610,10 +656,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) {
-                    if (dead) tc_mbar_arrive(bar(C::PHALF + s));
-                    tc_mbar_arrive(bar(C::PFULL + s));
-                }
+                if (lane == 0) tc_mbar_arrive(bar(C::PFULL + s));
             }
             n += stages;
             wait(C::OFULL + s, seg);
@@ -739,9 +782,8 @@ static long long chunk_most_tiles(int64_t n_tokens, int G, int n_seqs) { return 
 template <int HD, bool F8, int MODE>
 static int chunk_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
     using C = TcChunk<HD, F8>;
-    CUtensorMap mq, mk = {}, mv = {};          // FP8 rows are fetched by plain loads
-    if (!chunk_query_map(&mq, a, HD)) return DYNAKV_ERR_CUDA;
-    if (!F8 && (!tree_page_map(&mk, cache, cache->k, false) || !tree_page_map(&mv, cache, cache->v, false))) return DYNAKV_ERR_CUDA;
+    CUtensorMap mq, mk, mv;
+    if (!chunk_query_map(&mq, a, HD) || !tree_page_map(&mk, cache, cache->k, false) || !tree_page_map(&mv, cache, cache->v, false)) return DYNAKV_ERR_CUDA;
     static std::atomic<unsigned long long> allowed{0};
     if (!allow_smem(k_chunk_tc<HD, F8, MODE>, C::smem, allowed)) return DYNAKV_ERR_CUDA;
     // the warpgroups' shares of the registers add up to what the launch gets, or the kernel would wait for them forever
