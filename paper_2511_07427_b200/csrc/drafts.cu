@@ -21,7 +21,7 @@ namespace dkv {
 
 namespace cg = cooperative_groups;
 
-constexpr int RS_THREADS = 256;
+constexpr int RS_THREADS = 256, RS_VECS = 8, RS_BYTES = RS_THREADS * RS_VECS * 16;     // a block's piece of a row
 constexpr int VF_THREADS = 512, VF_WARPS = VF_THREADS / 32, VF_CLUSTER = 8;
 
 struct VerifyArgs {
@@ -46,6 +46,8 @@ __device__ __forceinline__ bool verify_range(const VerifyArgs& a, int b, int& q0
 struct Best { float top; int at; };
 __device__ __forceinline__ Best better(Best a, Best b) { return b.top > a.top || (b.top == a.top && b.at < a.at) ? b : a; }
 
+// A piece is loaded whole, every thread's 128 bytes on their way before anything is looked at: then the largest, then the sum
+// relative to it.  (A running maximum with two loads under way took 31 us for 98 MB, this takes RS_TIME.)
 template <typename T>
 __global__ void __launch_bounds__(RS_THREADS) k_row_stats(const VerifyArgs a) {
     constexpr int N = 16 / sizeof(T);      // elements of a load
@@ -53,72 +55,73 @@ __global__ void __launch_bounds__(RS_THREADS) k_row_stats(const VerifyArgs a) {
     __shared__ float heat_s;
     __shared__ Best best_s[RS_THREADS / 32];
     __shared__ float sum_s[RS_THREADS / 32];
-    if (tid == 0) heat_s = -1.f;
     pdl_wait();
+    const T* p = reinterpret_cast<const T*>(a.logits) + (long long)row * a.stride;
+    // elements before the first 16-byte boundary, whole vectors, and what is left
+    const int head = min(a.vocab, (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T))), vecs = (a.vocab - head) / N, tail = a.vocab - head - vecs * N;
+    const int v0 = piece * (RS_THREADS * RS_VECS) + tid;
+    const uint4* pv = reinterpret_cast<const uint4*>(p + head);
+    const unsigned low = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;                   // -infinity
+    uint4 w[RS_VECS];
+#pragma unroll
+    for (int i = 0; i < RS_VECS; i++) w[i] = v0 + i * RS_THREADS < vecs ? __ldg(pv + v0 + i * RS_THREADS) : make_uint4(low, low, low, low);
+    // the first piece's threads have the elements around the vectors
+    float x_odd = -INFINITY;
+    int at_odd = 0x7fffffff;
+    if (piece == 0 && tid < head + tail) { at_odd = tid < head ? tid : vecs * N + tid; x_odd = to_f(p[at_odd]); }
+    if (tid == 0) heat_s = -1.f;
     __syncthreads();
     for (int b = tid; b < a.n_seqs; b += RS_THREADS)       // at most one sequence has the row
         if (a.q_start[b] <= row && row < a.q_start[b + 1]) heat_s = fmaxf(a.heat[b], 0.f);
+    auto elem = [&](int i, int e) {
+        const unsigned u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        if constexpr (sizeof(T) == 4) return __uint_as_float(u[e]);
+        else return __uint_as_float(e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
+    };
+    float m = x_odd;
+#pragma unroll
+    for (int i = 0; i < RS_VECS; i++)
+#pragma unroll
+        for (int e = 0; e < N; e++) m = fmaxf(m, elem(i, e));
+    Best best = {m, 0x7fffffff};
+    float top = m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (m == top) {                        // few threads look for the place of the warp's largest
+        if (x_odd == m) best.at = at_odd;
+#pragma unroll
+        for (int i = RS_VECS - 1; i >= 0; i--)
+#pragma unroll
+            for (int e = N - 1; e >= 0; e--) if (elem(i, e) == m && v0 + i * RS_THREADS < vecs) best.at = min(best.at, head + (v0 + i * RS_THREADS) * N + e);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) best = better(best, Best{__shfl_xor_sync(0xffffffffu, best.top, o), __shfl_xor_sync(0xffffffffu, best.at, o)});
+    if (lane == 0) best_s[warp] = best;
     __syncthreads();
     pdl_trigger();
     const float heat = heat_s;
     if (heat < 0.f) return;                                // a row of no sequence
-    const float f = heat > 0.f ? 1.4426950408889634f / heat : 0.f;
-    const T* p = reinterpret_cast<const T*>(a.logits) + (long long)row * a.stride;
-    // elements before the first 16-byte boundary, whole vectors, and what is left
-    const int head = min(a.vocab, (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T))), vecs = (a.vocab - head) / N;
-    const int v0 = (int)((long long)vecs * piece / a.pieces), v1 = (int)((long long)vecs * (piece + 1) / a.pieces);
-    const uint4* pv = reinterpret_cast<const uint4*>(p + head);
-    Best best = {-INFINITY, 0x7fffffff};
-    float m = -INFINITY, sum = 0.f;                        // sum of exp relative to m
-    auto one = [&](float x, int at) {
-        best = better(best, Best{x, at});
-        if (f > 0.f && x > -INFINITY) {
-            if (x > m) { sum = m == -INFINITY ? 0.f : sum * ex2((m - x) * f); m = x; }
-            sum += ex2((x - m) * f);
-        }
-    };
-#pragma unroll 2
-    for (int v = v0 + tid; v < v1; v += RS_THREADS) {
-        const uint4 w = __ldcs(pv + v);
-        const unsigned u[4] = {w.x, w.y, w.z, w.w};
-        float x[N];
+    best = best_s[0];
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(u[i]);
-            else { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-        }
-        float top = x[0];
+    for (int k = 1; k < RS_THREADS / 32; k++) best = better(best, best_s[k]);
+    float sum = 0.f;
+    if (heat > 0.f && best.top > -INFINITY) {
+        const float f = 1.4426950408889634f / heat, shift = best.top;
+        float part[2] = {0.f, 0.f};
+        if (x_odd > -INFINITY) part[0] = ex2((x_odd - shift) * f);
 #pragma unroll
-        for (int i = 1; i < N; i++) top = fmaxf(top, x[i]);
-        if (top > best.top) {                              // rare after the first few: later equals lose
-            best.top = top;
+        for (int i = 0; i < RS_VECS; i++)
 #pragma unroll
-            for (int i = N - 1; i >= 0; i--) if (x[i] == top) best.at = head + v * N + i;
-        }
-        if (f > 0.f && best.top > -INFINITY) {
-            if (best.top > m) { sum = m == -INFINITY ? 0.f : sum * ex2((m - best.top) * f); m = best.top; }
-#pragma unroll
-            for (int i = 0; i < N; i++) sum += ex2((x[i] - m) * f);        // not x f - m f, which is off by the rounding of m f
-        }
+            for (int e = 0; e < N; e++) part[e & 1] += ex2((elem(i, e) - shift) * f);      // not x f - m f, which is off by the rounding of m f
+        sum = warp_sum(part[0] + part[1]);
     }
-    if (piece == 0 && tid < head) one(to_f(p[tid]), tid);
-    if (piece == a.pieces - 1 && tid < a.vocab - head - vecs * N) one(to_f(p[head + vecs * N + tid]), head + vecs * N + tid);
-    Best all = best;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) all = better(all, Best{__shfl_xor_sync(0xffffffffu, all.top, o), __shfl_xor_sync(0xffffffffu, all.at, o)});
-    if (lane == 0) best_s[warp] = all;
-    __syncthreads();
-    all = best_s[0];
-#pragma unroll
-    for (int w = 1; w < RS_THREADS / 32; w++) all = better(all, best_s[w]);
-    sum = warp_sum(m == -INFINITY ? 0.f : sum * ex2((m - all.top) * f));
     if (lane == 0) sum_s[warp] = sum;
     __syncthreads();
     if (tid == 0) {
         float total = 0.f;
 #pragma unroll
-        for (int w = 0; w < RS_THREADS / 32; w++) total += sum_s[w];
-        a.stats[(size_t)row * a.pieces + piece] = make_float4(all.top, __int_as_float(all.at), total, 0.f);
+        for (int k = 0; k < RS_THREADS / 32; k++) total += sum_s[k];
+        a.stats[(size_t)row * a.pieces + piece] = make_float4(best.top, __int_as_float(best.at), total, 0.f);
     }
 }
 
@@ -128,15 +131,33 @@ __device__ __forceinline__ double warp_sum64(double v) {
     return v;
 }
 
+// 2^x in 64 bits for x <= 0: 2^x = 2^n * 2^(j / 32) * 2^r with |r| <= 1 / 64, the middle factor from a table and the last from its
+// series up to r^6 (what is left out is below 2^-57).  Results below 2^-1000 are 0.
+__device__ __forceinline__ double exp2_64(double x, const double* table) {
+    if (!(x > -1000.0)) return 0.0;
+    const double shift = 6755399441055744.0 / 32.0;        // 1.5 * 2^52 in units of 1 / 32: the sum's last bits are round(32 x)
+    const double t = x + shift, r = x - (t - shift);
+    const int k = __double2loint(t);
+    const double y = r * 0.69314718055994530942;
+    double p = fma(y, 1.0 / 720.0, 1.0 / 120.0);
+    p = fma(p, y, 1.0 / 24.0);
+    p = fma(p, y, 1.0 / 6.0);
+    p = fma(p, y, 0.5);
+    p = fma(p, y, 1.0);
+    const double z = table[k & 31];
+    p = fma(p * y, z, z);
+    return __hiloint2double(__double2hiint(p) + ((k >> 5) << 20), __double2loint(p));
+}
+
 struct VerifyShared {
     double weight[TREE_MAX], sum[TREE_MAX];        // of a draft: its token's weight behind its parent; [a row]: sum of the row's weights
     float top[TREE_MAX];                           // [a row] largest logit
     int best[TREE_MAX];                            //         first place of it
     int token[TREE_MAX], up[TREE_MAX], first[TREE_MAX];
-    double part[VF_WARPS];
+    unsigned char again[TREE_MAX];                 // an older sibling has the same token
+    double table[32];                              // 2^(j / 32)
     double slices[VF_CLUSTER * VF_WARPS];
     int last, refused, found;
-    double z;
 };
 
 // 512 threads per CTA, one slice of the vocabulary per warp.
@@ -159,6 +180,8 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
     }
     const float heat = a.heat[b];
     const bool draws = heat > 0.f;
+    const double scale = 1.4426950408889634074 / (double)heat;             // weights are 2^((logit - largest) * scale)
+    if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0);
     // ---- every row's largest logit and sum, a warp per row
     for (int i = warp; i < n; i += VF_WARPS) {
         const float4* st = a.stats + (size_t)(q0 + i) * a.pieces;
@@ -168,7 +191,7 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         for (int o = 16; o > 0; o >>= 1) best = better(best, Best{__shfl_xor_sync(0xffffffffu, best.top, o), __shfl_xor_sync(0xffffffffu, best.at, o)});
         double sum = 0.0;
         for (int k = lane; k < a.pieces; k += 32)
-            if (draws && st[k].x > -INFINITY) sum += (double)st[k].z * exp(((double)st[k].x - (double)best.top) / (double)heat);
+            if (draws && st[k].x > -INFINITY) sum += (double)st[k].z * exp2(((double)st[k].x - (double)best.top) * scale);
         sum = warp_sum64(sum);
         if (lane == 0) { sh.top[i] = best.top; sh.best[i] = best.at; sh.sum[i] = sum; }
     }
@@ -181,9 +204,15 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
     __syncthreads();
     auto weight = [&](int row, int x) {                    // of token x behind row `row`, relative to the row's largest
         if (x < 0 || x >= a.vocab || sh.top[row] == -INFINITY) return 0.0;
-        return exp(((double)to_f(logits[(long long)(q0 + row) * a.stride + x]) - (double)sh.top[row]) / (double)heat);
+        return exp2_64(((double)to_f(logits[(long long)(q0 + row) * a.stride + x]) - (double)sh.top[row]) * scale, sh.table);
     };
-    for (int i = tid; i < n; i += VF_THREADS) sh.weight[i] = draws && sh.up[i] >= 0 ? weight(sh.up[i], sh.token[i]) : 0.0;
+    for (int i = tid; i < n; i += VF_THREADS) {
+        const int up = sh.up[i];
+        sh.weight[i] = draws && up >= 0 ? weight(up, sh.token[i]) : 0.0;
+        bool again = false;
+        if (a.parent && up >= 0) for (int s = up + 1; s < i; s++) again |= sh.up[s] == up && sh.token[s] == sh.token[i];
+        sh.again[i] = again;
+    }
     __syncthreads();
     // ---- every draft's test, against what its older siblings leave
     for (int i = tid; i < n; i += VF_THREADS) {
@@ -194,15 +223,8 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         else if (a.draft) pass = x >= 0 && x < a.vocab && (double)a.uniform[q0 + i] * (double)a.draft[(long long)(q0 + i) * a.draft_stride + x] * sh.sum[up] < sh.weight[i];
         else {
             double left = sh.sum[up];
-            bool again = false;
-            for (int s = up + 1; s < i; s++) {
-                if (sh.up[s] != up) continue;
-                if (sh.token[s] == x) { again = true; break; }
-                bool counted = false;                      // a token that two older siblings share is taken off once
-                for (int r = up + 1; r < s && !counted; r++) counted = sh.up[r] == up && sh.token[r] == sh.token[s];
-                if (!counted) left -= sh.weight[s];
-            }
-            pass = !again && (double)a.uniform[q0 + i] * left < sh.weight[i];
+            if (a.parent) for (int s = up + 1; s < i; s++) if (sh.up[s] == up && !sh.again[s]) left -= sh.weight[s];
+            pass = !sh.again[i] && (double)a.uniform[q0 + i] * left < sh.weight[i];
         }
         if (pass) atomicMin(&sh.first[up], i);
     }
@@ -236,27 +258,48 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
     const bool taken = a.draft && refused > 0;
     const T* row = logits + (long long)(q0 + last) * a.stride;
     const float* q = taken ? a.draft + (long long)(q0 + sh.first[0]) * a.draft_stride : nullptr;
-    const double top = (double)sh.top[last], temper = (double)heat;
-    const int slice = cta * VF_WARPS + warp, slices = ctas * VF_WARPS;
-    const int e0 = (int)((long long)a.vocab * slice / slices), e1 = (int)((long long)a.vocab * (slice + 1) / slices);
+    const double top = (double)sh.top[last];
+    const int slice = cta * VF_WARPS + warp, slices = ctas * VF_WARPS, e0 = (int)((long long)a.vocab * slice / slices), e1 = (int)((long long)a.vocab * (slice + 1) / slices);
     double norm = 0.0;                                     // 1 / sum of weights; 0: nothing is taken off
-    auto value = [&](int i) {
-        double w = exp(((double)to_f(row[i]) - top) / temper);
-        if (norm > 0.0) return fmax(w * norm - (double)q[i], 0.0);
+    auto value = [&](int i, float l, float minus) {
+        double w = exp2_64(((double)l - top) * scale, sh.table);
+        if (norm > 0.0) return fmax(fma(w, norm, -(double)minus), 0.0);
         if (!a.draft) for (int r = 0; r < refused; r++) if (sh.token[sh.first[r]] == i) w = 0.0;
         return w;
     };
-    // sums of all slices, the same in all CTAs; returns their total
+    // Sums of all slices, the same in all CTAs: every lane has those of `mine` consecutive ones, `before` those ahead of them; returns the total.
+    constexpr int MOST = VF_CLUSTER * VF_WARPS / 32;
+    const int mine = (slices + 31) / 32;
+    double held[MOST], before = 0.0;
     auto sum_all = [&]() {
-        double s = 0.0;
-        for (int i = e0 + lane; i < e1; i += 32) s += value(i);
-        s = warp_sum64(s);
+        double s[2] = {0.0, 0.0};
+        constexpr int U = 8;                               // loads of so many steps side by side
+        for (int base = e0 + lane; base < e1; base += 32 * U) {
+            float l[U], minus[U];
+#pragma unroll
+            for (int k = 0; k < U; k++) {
+                const bool in = base + k * 32 < e1;
+                l[k] = in ? to_f(row[base + k * 32]) : -INFINITY;
+                minus[k] = in && norm > 0.0 ? q[base + k * 32] : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < U; k++) s[k & 1] += value(base + k * 32, l[k], minus[k]);
+        }
+        const double all = warp_sum64(s[0] + s[1]);
         cluster.sync();                                    // nobody reads the last sums any more
-        if (lane == 0) for (int c = 0; c < ctas; c++) cluster.map_shared_rank(sh.slices, c)[slice] = s;
+        if (lane < ctas) cluster.map_shared_rank(sh.slices, lane)[slice] = all;
         cluster.sync();
-        double total = 0.0;
-        for (int i = 0; i < slices; i++) total += sh.slices[i];
-        return total;
+        double incl = 0.0;
+#pragma unroll
+        for (int k = 0; k < MOST; k++) {
+            held[k] = k < mine && lane * mine + k < slices ? sh.slices[lane * mine + k] : 0.0;
+            incl += held[k];
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += y; }
+        before = __shfl_up_sync(0xffffffffu, incl, 1);
+        if (lane == 0) before = 0.0;
+        return __shfl_sync(0xffffffffu, incl, 31);
     };
     double total = sum_all();
     if (taken && total > 0.0) {
@@ -269,28 +312,31 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         if (cta == 0 && tid == 0) a.next[b] = -1;
     } else {
         const double goal = (double)a.uniform[q0] * total;
-        double before = 0.0;
-        int pick = slices;                                 // slice that holds it; if rounding lets none: the last with a weight
-        for (int i = 0; i < slices; i++) {
-            if (sh.slices[i] > 0.0 && before + sh.slices[i] > goal) { pick = i; break; }
-            before += sh.slices[i];
+        int pick = -1, some = -1;                          // this lane's slice that holds it; its last with a weight
+        double ahead = before, start = 0.0;
+#pragma unroll
+        for (int k = 0; k < MOST; k++) {
+            if (held[k] > 0.0) {
+                some = lane * mine + k;
+                if (pick < 0 && ahead + held[k] > goal) { pick = some; start = ahead; }
+            }
+            ahead += held[k];
         }
-        if (pick == slices) {
-            before = -INFINITY;
-            for (int i = 0; i < slices; i++) if (sh.slices[i] > 0.0) pick = i;
-        }
+        const unsigned hits = __ballot_sync(0xffffffffu, pick >= 0), any = __ballot_sync(0xffffffffu, some >= 0);
+        if (hits) { const int src = __ffs(hits) - 1; pick = __shfl_sync(0xffffffffu, pick, src); start = __shfl_sync(0xffffffffu, start, src); }
+        else { pick = __shfl_sync(0xffffffffu, some, 31 - __clz(any)); start = -INFINITY; }        // rounding leaves none: the last with a weight
         if (pick == slice) {
             int found = -1, fallback = -1;
-            double run = before;
+            double run = start;
             for (int base = e0; base < e1 && found < 0; base += 32) {
                 const int i = base + lane;
-                const double v = i < e1 ? value(i) : 0.0;
+                const double v = i < e1 ? value(i, to_f(row[i]), norm > 0.0 ? q[i] : 0.f) : 0.0;
                 double x = v;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-                const unsigned hit = __ballot_sync(0xffffffffu, v > 0.0 && run + x > goal), some = __ballot_sync(0xffffffffu, v > 0.0);
+                const unsigned hit = __ballot_sync(0xffffffffu, v > 0.0 && run + x > goal), weighs = __ballot_sync(0xffffffffu, v > 0.0);
                 if (hit) found = base + __ffs(hit) - 1;
-                if (some) fallback = base + 31 - __clz(some);
+                if (weighs) fallback = base + 31 - __clz(weighs);
                 run += __shfl_sync(0xffffffffu, x, 31);
             }
             if (lane == 0) a.next[b] = found >= 0 ? found : fallback;
@@ -362,16 +408,14 @@ __global__ void __launch_bounds__(KEEP_THREADS) k_rows_keep(const KeepArgs a, in
     if (trouble && a.status) atomicOr(a.status, DYNAKV_ST_BOUNDS);
 }
 
-// Pieces of a row: enough blocks for all SMs, and at least 8 KB each.
-static int verify_pieces(int64_t n_tokens, int vocab, int es, int sms) {
-    const long long want = (8ll * sms + n_tokens - 1) / (n_tokens > 0 ? n_tokens : 1), most = ((long long)vocab * es + 8191) / 8192;
-    return (int)max(1ll, min(min(want, most), 256ll));
-}
+static int verify_pieces(int vocab, int es) { return (int)(((long long)vocab * es + RS_BYTES - 1) / RS_BYTES); }
 
 template <typename T>
-static int verify_launch(const VerifyArgs& a, cudaStream_t st) {
+static int verify_launch(const VerifyArgs& a, int sms, cudaStream_t st) {
     if (a.n_tokens > 0 && launch_pdl(k_row_stats<T>, dim3(a.n_tokens, a.pieces), dim3(RS_THREADS), 0, st, a) != cudaSuccess) return DYNAKV_ERR_CUDA;
-    const int ctas = a.vocab > 8192 ? VF_CLUSTER : 1;
+    // CTAs of a sequence: as many as keep all of them on the device at once, down to 4 K elements each
+    int ctas = 1;
+    while (ctas < VF_CLUSTER && 2ll * ctas * a.n_seqs <= sms && a.vocab > 4096 * ctas) ctas *= 2;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     cfg.gridDim = dim3(ctas, a.n_seqs); cfg.blockDim = dim3(VF_THREADS); cfg.stream = st;
@@ -388,16 +432,13 @@ static int verify_launch(const VerifyArgs& a, cudaStream_t st) {
 using namespace dkv;
 
 static bool verify_shape_ok(int32_t dtype, int64_t n_tokens, int32_t vocab, int32_t n_seqs, int32_t max_tree) {
-    return (dtype == DYNAKV_F32 || dtype == DYNAKV_BF16) && n_tokens >= 0 && n_tokens < (1ll << 24) && vocab >= 1 && vocab < (1 << 30) && n_seqs >= 0 &&
+    return (dtype == DYNAKV_F32 || dtype == DYNAKV_BF16) && n_tokens >= 0 && n_tokens < (1ll << 24) && vocab >= 1 && vocab <= (1 << 28) && n_seqs >= 0 &&
            n_seqs <= 65535 && max_tree >= 1 && max_tree <= TREE_MAX;
 }
 
 extern "C" int64_t dynakv_verify_drafts_workspace(int32_t logits_dtype, int64_t n_tokens, int32_t vocab, int32_t n_seqs, int32_t max_tree) {
     if (!verify_shape_ok(logits_dtype, n_tokens, vocab, n_seqs, max_tree)) return DYNAKV_ERR_ARG;
-    int rc;
-    const int sms = sm_count(&rc);
-    if (rc != DYNAKV_OK) return rc;
-    return (int64_t)max(1ll, (long long)n_tokens) * verify_pieces(n_tokens, vocab, logits_dtype == DYNAKV_F32 ? 4 : 2, sms) * 16;
+    return (int64_t)max(1ll, (long long)n_tokens) * verify_pieces(vocab, logits_dtype == DYNAKV_F32 ? 4 : 2) * 16;
 }
 
 extern "C" int dynakv_verify_drafts(const void* logits, int64_t logits_stride, int32_t logits_dtype, int64_t n_tokens, int32_t vocab, const int32_t* tokens,
@@ -417,12 +458,12 @@ extern "C" int dynakv_verify_drafts(const void* logits, int64_t logits_stride, i
     a.draft = draft_probs; a.draft_stride = draft_stride; a.kept = kept; a.dropped = dropped; a.path = path; a.next = next_token;
     a.stats = reinterpret_cast<float4*>(workspace);
     a.n_tokens = (int)n_tokens; a.n_seqs = n_seqs; a.vocab = vocab; a.most = max_tree;
-    a.pieces = verify_pieces(n_tokens, vocab, es, sms);
+    a.pieces = verify_pieces(vocab, es);
     if (workspace_bytes < max(1ll, (long long)n_tokens) * a.pieces * 16) return DYNAKV_ERR_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     // an error left behind by an earlier, unrelated call on this thread must not be reported as this call's
     cudaGetLastError();
-    return logits_dtype == DYNAKV_F32 ? verify_launch<float>(a, st) : verify_launch<__nv_bfloat16>(a, st);
+    return logits_dtype == DYNAKV_F32 ? verify_launch<float>(a, sms, st) : verify_launch<__nv_bfloat16>(a, sms, st);
 }
 
 extern "C" int dynakv_rows_keep(const dynakv_row_cache* cache, const int32_t* page_table, int32_t pages_per_seq, const int32_t* kv_len,

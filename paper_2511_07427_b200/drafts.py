@@ -119,8 +119,8 @@ def verify_drafts(logits, tokens, q_start, max_tree: int, uniform, temperature, 
     b = q_start.shape[0] - 1 if q_start.dim() == 1 else -1
     if b < 0:
         raise DynaKVError(f"expected q_start of sequences + 1 elements, got {tuple(q_start.shape)}")
-    if not 1 <= max_tree <= MAX_TREE or not 1 <= vocab < 1 << 30 or n >= 1 << 24 or b > 65535:
-        raise DynaKVError(f"max_tree is {max_tree}, {n} tokens of a vocabulary of {vocab}, {b} sequences: expected 1 to {MAX_TREE}, fewer than 2^24, 1 to 2^30 - 1, at most 65535")
+    if not 1 <= max_tree <= MAX_TREE or not 1 <= vocab <= 1 << 28 or n >= 1 << 24 or b > 65535:
+        raise DynaKVError(f"max_tree is {max_tree}, {n} tokens of a vocabulary of {vocab}, {b} sequences: expected 1 to {MAX_TREE}, fewer than 2^24, 1 to 2^28, at most 65535")
     at = _matrix(E, logits, (n, vocab), device, (E.f32, E.bf16), "logits")
     if parent is not None and draft_probs is not None:
         raise DynaKVError("draft_probs goes with chains (parent=None): drafts of a tree are taken as looked up")
