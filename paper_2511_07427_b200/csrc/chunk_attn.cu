@@ -4,10 +4,6 @@
 
 namespace dkv {
 
-// tcgen05 kernel (chunk_tc.cu), and the bytes up to the end of its plan in a workspace whose first `at` are taken.
-int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st);
-size_t chunk_plan_space(int64_t n_tokens, int G, int n_seqs, int ctas, size_t at, char* base, ChunkPlan* plan);
-
 template <int HD, int DT, int RG>
 static int chunk_launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
     using C = TreeCfg<HD, DT, RG, true>;
@@ -28,13 +24,19 @@ static int chunk_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& m
 #ifndef DKV_CHUNK_TC_FP8
 #define DKV_CHUNK_TC_FP8 65
 #endif
-struct ChunkKind { bool tc; int rg, rows, ctas; };
+#ifndef DKV_CHUNK_F32
+#define DKV_CHUNK_F32 65
+#endif
+struct ChunkKind { bool planned; int rg, rows, ctas, per; };             // per: tokens of a planned tile
 static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int max_chunk, int sms) {
     const bool f32 = c->kv_dtype == DYNAKV_F32;
     const int most = (int)min(1000ll, (long long)max_chunk * (n_heads / c->n_kv_heads));
-    if (!f32 && most >= (c->kv_dtype == DYNAKV_FP8 ? DKV_CHUNK_TC_FP8 : DKV_CHUNK_TC_BF16)) return {true, 0, CT_ROWS, sms};
+    if (most >= (f32 ? DKV_CHUNK_F32 : c->kv_dtype == DYNAKV_FP8 ? DKV_CHUNK_TC_FP8 : DKV_CHUNK_TC_BF16)) {
+        const int G = n_heads / c->n_kv_heads;
+        return {true, 0, f32 ? CF_ROWS : CT_ROWS, sms, f32 ? CF_ROWS / G : tile_tokens(G)};
+    }
     const int rg = row_groups(most, f32);
-    return {false, rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2)};
+    return {false, rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2), 0};
 }
 
 static bool chunk_shape_ok(const dynakv_row_cache* c, int n_heads, int64_t n_tokens, int n_seqs, int max_chunk) {
@@ -53,7 +55,7 @@ extern "C" int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, 
     if (rc != DYNAKV_OK) return rc;
     const ChunkKind k = chunk_kind(cache, n_heads, max_chunk, sms);
     const size_t records = tree_space(k.ctas, k.rows, cache->head_dim).bytes;
-    return (int64_t)(k.tc ? chunk_plan_space(n_tokens, n_heads / cache->n_kv_heads, n_seqs, sms, records, nullptr, nullptr) : records);
+    return (int64_t)(k.planned ? chunk_plan_space(n_tokens, k.per, n_seqs, sms, records, nullptr, nullptr) : records);
 }
 
 extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
@@ -71,7 +73,7 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
     const ChunkKind kind = chunk_kind(cache, n_heads, max_chunk, sms);
     const TreeSpace sp = tree_space(kind.ctas, kind.rows, cache->head_dim);
     ChunkPlan plan = {};
-    const size_t bytes = kind.tc ? chunk_plan_space(n_tokens, n_heads / cache->n_kv_heads, n_seqs, sms, sp.bytes, reinterpret_cast<char*>(workspace), &plan) : sp.bytes;
+    const size_t bytes = kind.planned ? chunk_plan_space(n_tokens, kind.per, n_seqs, sms, sp.bytes, reinterpret_cast<char*>(workspace), &plan) : sp.bytes;
     if (workspace_bytes < (int64_t)bytes) return DYNAKV_ERR_ARG;
     TreeArgs a = tree_args(cache, q, n_heads, n_tokens, q_start, n_seqs, max_chunk, page_table, pages_per_seq, kv_len, out, lse, workspace, sp, status);
     a.scale = scores->scale;
@@ -82,7 +84,7 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     // an error left behind by an earlier, unrelated call on this thread must not be reported as this call's
     cudaGetLastError();
-    if (kind.tc) return chunk_tc_launch(cache, a, plan, sms, st);
+    if (kind.planned) return cache->kv_dtype == DYNAKV_F32 ? chunk_f32_launch(cache, a, plan, sms, st) : chunk_tc_launch(cache, a, plan, sms, st);
     CUtensorMap mk, mv;
     if (!tree_page_map(&mk, cache, cache->k, true) || !tree_page_map(&mv, cache, cache->v, true)) return DYNAKV_ERR_CUDA;
     const int rg = kind.rg;

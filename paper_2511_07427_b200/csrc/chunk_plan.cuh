@@ -1,8 +1,8 @@
-// How dynakv_attend_chunk on tcgen05 cuts its work.
+// How dynakv_attend_chunk cuts the work of its kernels for many query rows.
 //
-// A tile is the query rows, row = token * G + head of the group, of 2 (128 / G) consecutive tokens of one sequence: two streams of up to
-// 128 rows that begin with a token's first head, which is what lets the TMA fetch them.  A unit is a tile and a KV head; its work
-// is the stages of 128 rows (4 pages) between the first and the last row that one of its tokens sees.  A first launch writes down
+// A tile is the query rows, row = token * G + head of the group, of so many consecutive tokens of one sequence: of 128 / G, or on tcgen05 of
+// two streams of as many, which begin with a token's first head, so that the TMA can fetch them.  A unit is a tile and a KV head; its work
+// is the stages of 64 or 128 rows between the first and the last row that one of its tokens sees.  A first launch writes down
 // every tile's stages, their prefix sums and where every CTA of the main kernel begins, because that depends on lengths and ranges that
 // only the device has.  All units' stages, in the order sequence, KV head, tile (so that CTAs side by side read the same
 // rows), form one list that the CTAs share out evenly, a unit's beginning counted as CT_UNIT_COST stages more; a unit cut by a border leaves
@@ -13,7 +13,8 @@
 
 namespace dkv {
 
-constexpr int CT_ROWS = 256, CT_KEYS = 128, CT_PAGES = CT_KEYS / PAGE;
+constexpr int CT_ROWS = 256, CT_KEYS = 128, CT_PAGES = CT_KEYS / PAGE;       // rows of a tile and of a stage: tcgen05
+constexpr int CF_ROWS = 128, CF_KEYS = 64;                                    // fp32 rows
 #ifndef DKV_CHUNK_UNIT_COST
 #define DKV_CHUNK_UNIT_COST 2
 #endif
@@ -35,7 +36,6 @@ struct ChunkPlan {
 };
 
 __device__ __host__ __forceinline__ int tile_tokens(int G) { return 2 * (128 / G); }
-__device__ __forceinline__ int seq_tiles(int T, int G) { return (T + tile_tokens(G) - 1) / tile_tokens(G); }
 
 struct ChunkSeg {
     int seq, h, tile, s0, s1;                      // stages [s0, s1) of the sequence
@@ -77,5 +77,13 @@ struct ChunkWalk {
         return true;
     }
 };
+
+// Host side.  per: tokens of a tile, keys: rows of a stage.
+int chunk_plan_launch(const TreeArgs& a, const ChunkPlan& plan, int sms, int per, int keys, cudaStream_t st);
+// The bytes up to the end of the plan in a workspace whose first `at` are taken.
+size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, size_t at, char* base, ChunkPlan* plan);
+// The kernels: chunk_tc.cu (bf16 and FP8 rows, tcgen05), chunk_f32.cu.
+int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st);
+int chunk_f32_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st);
 
 }  // namespace dkv

@@ -32,142 +32,6 @@ constexpr float CT_LOG2E = 1.4426950408889634f, CT_LN2 = 0.6931471805599453f;
 // fp32, and sums of 2^24 rows' weights times V stay below its end up to |V| = 2^79.
 constexpr float CT_LAZY = 24.f;
 
-// ---------------------------------------------------------------------------------- the plan
-
-constexpr int PLAN_THREADS = 1024, PLAN_NEAR = 2048;            // prefix sums of so many tiles are kept in shared memory as well
-
-__global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, const ChunkPlan p, int ctas, long long most) {
-    __shared__ long long sums[32];
-    __shared__ long long near_s[PLAN_NEAR + 1];
-    __shared__ long long at_s[PLAN_THREADS + 1];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = tile_tokens(a.G);
-    pdl_wait();
-    pdl_trigger();
-    auto scan = [&](long long x, long long& total) {           // inclusive, over the block
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-        __syncthreads();
-        if (lane == 31) sums[warp] = x;
-        __syncthreads();
-        long long w = sums[lane];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += y; }
-        total = __shfl_sync(0xffffffffu, w, 31);
-        const long long before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
-        return x + (warp ? before : 0);
-    };
-    // ---- sequences and their tiles
-    long long tiles = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += PLAN_THREADS) {
-        const int b = b0 + tid;
-        SeqInfo s = {};
-        if (b < a.n_seqs) s = seq_info<CT_ROWS, false>(a, b, true);
-        int count = seq_tiles(s.T, a.G);
-        long long total, incl = scan(count, total);
-        if (tiles + total > most) {                            // ranges of q that overlap: the workspace has no room for more tiles than tokens make
-            if (tiles + incl > most) { count = 0; s.T = 0; tree_status(a, DYNAKV_ST_BOUNDS); }
-            incl = scan(count, total);
-        }
-        const int first = (int)(tiles + incl - count);
-        for (unsigned left = __ballot_sync(0xffffffffu, count > 0); left; left &= left - 1) {      // few sequences have many tiles, so a warp writes a sequence's
-            const int src = __ffs(left) - 1;
-            const int c = __shfl_sync(0xffffffffu, count, src), f = __shfl_sync(0xffffffffu, first, src), q0 = __shfl_sync(0xffffffffu, s.q0, src),
-                      T = __shfl_sync(0xffffffffu, s.T, src), n = __shfl_sync(0xffffffffu, s.n, src);
-            for (int i = lane; i < c; i += 32) {
-                const int from = i * per, to = min(T, from + per), place = n - T;
-                int lo = n, hi = 0;
-                if (!a.rows_from && !a.rows_to) {
-                    lo = a.window > 0 ? max(0, place + from + 1 - a.window) : 0;
-                    hi = place + to;
-                }
-                p.tiles[f + i] = {b0 + warp * 32 + src, 2 * i + (i == c - 1 ? 1 : 0), lo, hi, q0, T, n, f};
-            }
-        }
-        tiles += total;
-    }
-    __syncthreads();
-    // ---- stages of every tile; where the tokens' ranges have to be read, 8 lanes per tile find the first and the last row
-    if (a.rows_from || a.rows_to) {
-        for (int i0 = warp * 4; i0 < tiles; i0 += PLAN_THREADS / 8) {
-            const int i = i0 + (lane >> 3);
-            int lo = 0x7fffffff, hi = 0;
-            if (i < tiles) {
-                const ChunkTile t = p.tiles[i];
-                const int from = (t.tile >> 1) * per, to = min(t.T, from + per);
-#pragma unroll 4
-                for (int x = from + (lane & 7); x < to; x += 8) {
-                    int l, h;
-                    chunk_sees(a, t.q0 + x, t.n - t.T + x, t.n, l, h);
-                    if (l < h) { lo = min(lo, max(l, 0)); hi = max(hi, h); }
-                }
-            }
-#pragma unroll
-            for (int o = 1; o < 8; o <<= 1) { lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o)); hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o)); }
-            if (i < tiles && (lane & 7) == 0) { p.tiles[i].from = lo; p.tiles[i].stages = hi; }
-        }
-        __syncthreads();
-    }
-    long long run = 0;
-    for (int t0 = 0; t0 < tiles; t0 += PLAN_THREADS) {
-        const int i = t0 + tid;
-        long long mine = 0;
-        if (i < tiles) {
-            const int lo = p.tiles[i].from, hi = p.tiles[i].stages, from = lo < hi ? lo / CT_KEYS : 0;
-            mine = lo < hi ? (hi + CT_KEYS - 1) / CT_KEYS - from : 1;
-            p.tiles[i].from = from;
-            p.tiles[i].stages = (int)mine;
-        }
-        long long total;
-        const long long incl = scan(mine, total);
-        if (i < tiles) { p.before[i] = run + incl - mine; if (i < PLAN_NEAR) near_s[i] = run + incl - mine; }
-        run += total;
-    }
-    if (tid == 0) { p.before[tiles] = run; if (tiles <= PLAN_NEAR) near_s[tiles] = run; }
-    __syncthreads();
-    // ---- where every CTA begins: cost x is stage x of the list in which every unit has CT_UNIT_COST stages more
-    const long long* before = tiles <= PLAN_NEAR ? near_s : p.before;
-    const long long W = (run + tiles * CT_UNIT_COST) * a.Hk;
-    const int C = (int)max(1ll, min((long long)ctas, run * a.Hk));
-    for (int c0 = 0; c0 < ctas; c0 += PLAN_THREADS) {
-        // the CTA's place, and that of the one behind it
-        ChunkStart st = {0, 0, 0, 0, run * a.Hk};
-        const int c = c0 + tid;
-        const long long x = c < C ? mul_div(c, W, C) : W;
-        if (c <= ctas && x < W) {
-            auto find = [&](long long y, int lo, int hi) {     // last tile of [lo, hi) whose cost before it is <= y
-                while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (before[mid] + (long long)mid * CT_UNIT_COST <= y) lo = mid; else hi = mid; }
-                return lo;
-            };
-            const ChunkTile t = p.tiles[find(x / a.Hk, 0, (int)tiles)];
-            const int e0 = t.first, e1 = e0 + seq_tiles(t.T, a.G);
-            const long long lead = before[e0] + (long long)e0 * CT_UNIT_COST, all = before[e1] + (long long)e1 * CT_UNIT_COST - lead, cost = x - lead * a.Hk;
-            st.head = (int)(cost / all);
-            const long long y = lead + cost - st.head * all;
-            st.tile = find(y, e0, e1);
-            st.off = (int)max(0ll, y - before[st.tile] - (long long)(st.tile + 1) * CT_UNIT_COST);
-            // a short unit is not cut where a CTA has several: two records and their merge cost more than what it adds to one side
-            const int whole = (int)(before[st.tile + 1] - before[st.tile]);
-            if (whole <= CT_WHOLE && (whole + CT_UNIT_COST) * 3ll * C <= W) st.off = st.off * 2 >= whole ? whole : 0;
-            st.at = before[e0] * a.Hk + st.head * (before[e1] - before[e0]) + before[st.tile] - before[e0] + st.off;
-            if (st.off == whole) {                             // the unit behind it
-                st.off = 0;
-                if (++st.tile == e1) {
-                    if (st.head + 1 < a.Hk) { st.head++; st.tile = e0; }
-                    else st.head = 0;
-                }
-            }
-        }
-        at_s[tid] = st.at;
-        __syncthreads();
-        if (c < ctas) {
-            // up to where the next one begins; the last of a batch of CTAs (more than 1024: none has been built) finds its end in the list's
-            st.left = (int)((tid + 1 < PLAN_THREADS ? at_s[tid + 1] : run * a.Hk) - st.at);
-            p.starts[c] = st;
-        }
-        __syncthreads();
-    }
-}
-
 // ---------------------------------------------------------------------------------- the kernel
 
 template <int HD, bool F8>
@@ -203,8 +67,6 @@ __device__ __forceinline__ void store32(void* to, const unsigned (&p)[8], bool w
         reinterpret_cast<uint4*>(to)[1] = make_uint4(p[4], p[5], p[6], p[7]);
     }
 }
-template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(N)); }
 
 // A query row: what it sees, and how its logits become scores (log2 units).
 struct ChunkRow {
@@ -777,8 +639,6 @@ static bool chunk_query_map(CUtensorMap* map, const TreeArgs& a, int hd) {
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static long long chunk_most_tiles(int64_t n_tokens, int G, int n_seqs) { return n_tokens / tile_tokens(G) + n_seqs; }
-
 template <int HD, bool F8, int MODE>
 static int chunk_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
     using C = TcChunk<HD, F8>;
@@ -792,7 +652,8 @@ static int chunk_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, 
         return cudaFuncGetAttributes(&f, k_chunk_tc<HD, F8, MODE>) == cudaSuccess ? f.numRegs : 0;
     }();
     if (regs * (C::threads / 128) < 2 * C::regs_softmax + C::regs_rest + (F8 ? C::regs_convert : 0)) return DYNAKV_ERR_CUDA;
-    if (launch_pdl(k_chunk_plan, dim3(1), dim3(PLAN_THREADS), 0, st, a, plan, sms, chunk_most_tiles(a.n_tokens, a.G, a.n_seqs)) != cudaSuccess) return DYNAKV_ERR_CUDA;
+    const int rc = chunk_plan_launch(a, plan, sms, tile_tokens(a.G), CT_KEYS, st);
+    if (rc != DYNAKV_OK) return rc;
     if (launch_pdl(k_chunk_tc<HD, F8, MODE>, dim3(sms), dim3(C::threads), C::smem, st, mq, mk, mv, a, plan) != cudaSuccess) return DYNAKV_ERR_CUDA;
     return launch_pdl(k_chunk_merge<HD>, dim3(sms, HD / 16), dim3(CT_ROWS), 0, st, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
@@ -805,18 +666,6 @@ static int chunk_tc_launch_mode(const dynakv_row_cache* cache, const TreeArgs& a
 template <int HD>
 static int chunk_tc_launch_hd(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
     return cache->kv_dtype == DYNAKV_FP8 ? chunk_tc_launch_mode<HD, true>(cache, a, plan, sms, st) : chunk_tc_launch_mode<HD, false>(cache, a, plan, sms, st);
-}
-
-// The plan's part of the workspace behind the records'.
-size_t chunk_plan_space(int64_t n_tokens, int G, int n_seqs, int ctas, size_t at, char* base, ChunkPlan* plan) {
-    const size_t tiles = (size_t)chunk_most_tiles(n_tokens, G, n_seqs);
-    auto take = [&](size_t bytes) { const size_t x = (at + 15) / 16 * 16; at = x + bytes; return base + x; };
-    ChunkPlan p;
-    p.tiles = reinterpret_cast<ChunkTile*>(take(tiles * sizeof(ChunkTile)));
-    p.before = reinterpret_cast<long long*>(take((tiles + 1) * 8));
-    p.starts = reinterpret_cast<ChunkStart*>(take((size_t)ctas * sizeof(ChunkStart)));
-    if (plan) *plan = p;
-    return at;
 }
 
 int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {

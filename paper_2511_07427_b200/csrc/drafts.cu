@@ -15,6 +15,7 @@
 #include "bulk_copy.cuh"
 #include "head_rows.cuh"
 #include "mma_ops.cuh"
+#include "tc_rows.cuh"
 #include "tree_host.cuh"
 
 namespace dkv {
@@ -49,12 +50,12 @@ __device__ __forceinline__ Best better(Best a, Best b) { return b.top > a.top ||
 // A piece is loaded whole, every thread's 128 bytes on their way before anything is looked at: then the largest, then the sum
 // relative to it.  (A running maximum with two loads under way took 31 us for 98 MB, this takes RS_TIME.)
 template <typename T>
-__global__ void __launch_bounds__(RS_THREADS) k_row_stats(const VerifyArgs a) {
+__global__ void __launch_bounds__(RS_THREADS, 4) k_row_stats(const VerifyArgs a) {
     constexpr int N = 16 / sizeof(T);      // elements of a load
     const int row = blockIdx.x, piece = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __shared__ float heat_s;
-    __shared__ Best best_s[RS_THREADS / 32];
-    __shared__ float sum_s[RS_THREADS / 32];
+    __shared__ float top_s[RS_THREADS / 32], sum_s[RS_THREADS / 32];
+    __shared__ int at_s;
     pdl_wait();
     const T* p = reinterpret_cast<const T*>(a.logits) + (long long)row * a.stride;
     // elements before the first 16-byte boundary, whole vectors, and what is left
@@ -69,7 +70,7 @@ __global__ void __launch_bounds__(RS_THREADS) k_row_stats(const VerifyArgs a) {
     float x_odd = -INFINITY;
     int at_odd = 0x7fffffff;
     if (piece == 0 && tid < head + tail) { at_odd = tid < head ? tid : vecs * N + tid; x_odd = to_f(p[at_odd]); }
-    if (tid == 0) heat_s = -1.f;
+    if (tid == 0) { heat_s = -1.f; at_s = 0x7fffffff; }
     __syncthreads();
     for (int b = tid; b < a.n_seqs; b += RS_THREADS)       // at most one sequence has the row
         if (a.q_start[b] <= row && row < a.q_start[b + 1]) heat_s = fmaxf(a.heat[b], 0.f);
@@ -83,37 +84,38 @@ __global__ void __launch_bounds__(RS_THREADS) k_row_stats(const VerifyArgs a) {
     for (int i = 0; i < RS_VECS; i++)
 #pragma unroll
         for (int e = 0; e < N; e++) m = fmaxf(m, elem(i, e));
-    Best best = {m, 0x7fffffff};
     float top = m;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (m == top) {                        // few threads look for the place of the warp's largest
-        if (x_odd == m) best.at = at_odd;
-#pragma unroll
-        for (int i = RS_VECS - 1; i >= 0; i--)
-#pragma unroll
-            for (int e = N - 1; e >= 0; e--) if (elem(i, e) == m && v0 + i * RS_THREADS < vecs) best.at = min(best.at, head + (v0 + i * RS_THREADS) * N + e);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = better(best, Best{__shfl_xor_sync(0xffffffffu, best.top, o), __shfl_xor_sync(0xffffffffu, best.at, o)});
-    if (lane == 0) best_s[warp] = best;
+    if (lane == 0) top_s[warp] = top;
     __syncthreads();
     pdl_trigger();
     const float heat = heat_s;
     if (heat < 0.f) return;                                // a row of no sequence
-    best = best_s[0];
+    top = top_s[0];
 #pragma unroll
-    for (int k = 1; k < RS_THREADS / 32; k++) best = better(best, best_s[k]);
-    float sum = 0.f;
-    if (heat > 0.f && best.top > -INFINITY) {
-        const float f = 1.4426950408889634f / heat, shift = best.top;
-        float part[2] = {0.f, 0.f};
-        if (x_odd > -INFINITY) part[0] = ex2((x_odd - shift) * f);
+    for (int k = 1; k < RS_THREADS / 32; k++) top = fmaxf(top, top_s[k]);
+    if (m == top) {                                        // the few threads that have the largest look for its place
+        int at = x_odd == m ? at_odd : 0x7fffffff;
 #pragma unroll
         for (int i = 0; i < RS_VECS; i++)
 #pragma unroll
-            for (int e = 0; e < N; e++) part[e & 1] += ex2((elem(i, e) - shift) * f);      // not x f - m f, which is off by the rounding of m f
-        sum = warp_sum(part[0] + part[1]);
+            for (int e = 0; e < N; e++) if (elem(i, e) == m && v0 + i * RS_THREADS < vecs) at = min(at, head + (v0 + i * RS_THREADS) * N + e);
+        atomicMin(&at_s, at);
+    }
+    float sum = 0.f;
+    if (heat > 0.f && top > -INFINITY) {
+        const float f = 1.4426950408889634f / heat;
+        const float2 f2 = make_float2(f, f), less = make_float2(-top, -top);
+        float2 part = make_float2(x_odd > -INFINITY ? ex2((x_odd - top) * f) : 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < RS_VECS; i++)
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const float2 y = mul2(add2(make_float2(elem(i, e), elem(i, e + 1)), less), f2);        // not x f - m f, which is off by the rounding of m f
+                part = add2(part, make_float2(ex2(y.x), ex2(y.y)));
+            }
+        sum = warp_sum(part.x + part.y);
     }
     if (lane == 0) sum_s[warp] = sum;
     __syncthreads();
@@ -121,7 +123,7 @@ __global__ void __launch_bounds__(RS_THREADS) k_row_stats(const VerifyArgs a) {
         float total = 0.f;
 #pragma unroll
         for (int k = 0; k < RS_THREADS / 32; k++) total += sum_s[k];
-        a.stats[(size_t)row * a.pieces + piece] = make_float4(best.top, __int_as_float(best.at), total, 0.f);
+        a.stats[(size_t)row * a.pieces + piece] = make_float4(top, __int_as_float(at_s), total, 0.f);
     }
 }
 
@@ -131,23 +133,54 @@ __device__ __forceinline__ double warp_sum64(double v) {
     return v;
 }
 
-// 2^x in 64 bits for x <= 0: 2^x = 2^n * 2^(j / 32) * 2^r with |r| <= 1 / 64, the middle factor from a table and the last from its
-// series up to r^6 (what is left out is below 2^-57).  Results below 2^-1000 are 0.
-__device__ __forceinline__ double exp2_64(double x, const double* table) {
-    if (!(x > -1000.0)) return 0.0;
-    const double shift = 6755399441055744.0 / 32.0;        // 1.5 * 2^52 in units of 1 / 32: the sum's last bits are round(32 x)
-    const double t = x + shift, r = x - (t - shift);
-    const int k = __double2loint(t);
-    const double y = r * 0.69314718055994530942;
-    double p = fma(y, 1.0 / 720.0, 1.0 / 120.0);
-    p = fma(p, y, 1.0 / 24.0);
-    p = fma(p, y, 1.0 / 6.0);
-    p = fma(p, y, 0.5);
-    p = fma(p, y, 1.0);
-    const double z = table[k & 31];
-    p = fma(p * y, z, z);
-    return __hiloint2double(__double2hiint(p) + ((k >> 5) << 20), __double2loint(p));
+// Bytes [p, p + n) into L2, as far as whole 16-byte pieces go.
+__device__ __forceinline__ void prefetch_l2(const void* p, size_t n) {
+    const uintptr_t from = ((uintptr_t)p + 15) & ~(uintptr_t)15, end = ((uintptr_t)p + n) & ~(uintptr_t)15;
+    for (uintptr_t at = from; at < end; at += 65536)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(at), "r"((unsigned)(end - at < 65536 ? end - at : 65536)) : "memory");
 }
+
+constexpr int EXP_TABLE = 16;
+__device__ const double two_to[EXP_TABLE] = {      // 2^(j / 16)
+    1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927,
+    1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543, 1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
+// N values of 2^((l - top) * scale) in 64 bits, l <= top: the exponent is n + j / 16 + r with |r| <= 1 / 32, the factor of j comes from a table
+// (in shared memory once per pair of lanes, so that no two meet in a bank) and that of r from its series up to r^5 (what is left out is
+// below 2^-42 of the value, far below what could misplace a draw).  Values below 2^-1000 are 0.  Step by step for all N, because a 64-bit operation's result is a long time in coming: one value after the other,
+// the 8 M of a large call took 140 us.
+template <int N>
+__device__ __forceinline__ void exp2_64(const float (&l)[N], double top, double scale, float lowest, const double* table, double (&w)[N]) {
+    const double shift = 6755399441055744.0 / EXP_TABLE;   // 1.5 * 2^52 in units of 1 / 16: the sum's last bits are round(16 x)
+    int k[N];
+    double r[N], p[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) w[i] = (double)l[i] - top;
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma(w[i], scale, shift);
+#pragma unroll
+    for (int i = 0; i < N; i++) { k[i] = __double2loint(p[i]); p[i] -= shift; }
+#pragma unroll
+    for (int i = 0; i < N; i++) { r[i] = fma(w[i], scale, -p[i]); w[i] = table[(k[i] & (EXP_TABLE - 1)) * 16]; }
+    // (ln 2)^k / k!
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma(r[i], 0.0013333558146428441, 0.0096181291076284769);
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma(p[i], r[i], 0.055504108664821576);
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma(p[i], r[i], 0.24022650695910069);
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma(p[i], r[i], 0.69314718055994529);
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] *= r[i];
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma(p[i], w[i], w[i]);
+#pragma unroll
+    for (int i = 0; i < N; i++) w[i] = l[i] > lowest ? __hiloint2double(__double2hiint(p[i]) + ((k[i] >> 4) << 20), __double2loint(p[i])) : 0.0;
+}
+// The logit below which a weight is 0.
+__device__ __forceinline__ float lowest_logit(double top, double scale) { return (float)(top - 1000.0 / scale); }
+
+constexpr int LEFT_STEPS = 8;                      // loads of so many steps side by side
 
 struct VerifyShared {
     double weight[TREE_MAX], sum[TREE_MAX];        // of a draft: its token's weight behind its parent; [a row]: sum of the row's weights
@@ -155,10 +188,69 @@ struct VerifyShared {
     int best[TREE_MAX];                            //         first place of it
     int token[TREE_MAX], up[TREE_MAX], first[TREE_MAX];
     unsigned char again[TREE_MAX];                 // an older sibling has the same token
-    double table[32];                              // 2^(j / 32)
-    double slices[VF_CLUSTER * VF_WARPS];
+    double table[EXP_TABLE * 16];
+    double slices[VF_CLUSTER * VF_WARPS], part[VF_WARPS];
+    double held[32 * LEFT_STEPS];                  // weights of the run in which the drawn token lies
     int last, refused, found;
 };
+
+// What is left of a row's distribution: its weights, or (norm > 0) weight * norm - q, without the tokens of `refused` children.
+template <typename T>
+struct RowLeft {
+    const T* row;
+    const float* q;
+    double top, scale, norm;
+    int refused;
+};
+// The sum over elements [from, end), by one warp; `held`: the weights of up to 32 LEFT_STEPS of them are kept there.  One function,
+// not inlined: the code is run once or twice, and fetching it is what it would cost.
+template <typename T>
+__device__ __noinline__ double left_sum(const RowLeft<T> a, const VerifyShared& sh, int from, int end, double* held) {
+    const int lane = threadIdx.x & 31;
+    const bool less = a.norm > 0.0;
+    const float lowest = lowest_logit(a.top, a.scale);
+    double s[2] = {0.0, 0.0};
+    T l[LEFT_STEPS];
+    float q[LEFT_STEPS] = {};
+    // The next elements, while these are worked on.  Every lane loads, those behind the end the last one again: loads under conditions of their
+    // own wait for one another.
+    auto fetch = [&](int base) {
+#pragma unroll
+        for (int k = 0; k < LEFT_STEPS; k++) l[k] = a.row[min(base + k * 32, end - 1)];
+        if (less) {
+#pragma unroll
+            for (int k = 0; k < LEFT_STEPS; k++) q[k] = a.q[min(base + k * 32, end - 1)];
+        }
+    };
+    if (from < end) fetch(from + lane);
+    for (int base = from + lane; base - lane < end; base += 32 * LEFT_STEPS) {
+        double w[LEFT_STEPS];
+        float now[LEFT_STEPS], minus[LEFT_STEPS];
+#pragma unroll
+        for (int k = 0; k < LEFT_STEPS; k++) { now[k] = base + k * 32 < end ? to_f(l[k]) : -INFINITY; minus[k] = q[k]; }
+        for (int r = 0; r < a.refused; r++) {              // a refused token weighs nothing
+            const int off = sh.token[sh.first[r]] - base;
+            if ((unsigned)(off + lane) >= 32u * LEFT_STEPS) continue;          // the same in the whole warp
+#pragma unroll
+            for (int k = 0; k < LEFT_STEPS; k++) if (off == k * 32) now[k] = -INFINITY;
+        }
+        if (base - lane + 32 * LEFT_STEPS < end) fetch(base + 32 * LEFT_STEPS);
+        exp2_64(now, a.top, a.scale, lowest, sh.table + (lane & 15), w);
+        if (less) {
+#pragma unroll
+            for (int k = 0; k < LEFT_STEPS; k++) w[k] = fma(w[k], a.norm, -(double)minus[k]);
+#pragma unroll
+            for (int k = 0; k < LEFT_STEPS; k++) w[k] = w[k] > 0.0 ? w[k] : 0.0;
+        }
+        if (held) {
+#pragma unroll
+            for (int k = 0; k < LEFT_STEPS; k++) held[k * 32 + lane] = w[k];
+        }
+#pragma unroll
+        for (int k = 0; k < LEFT_STEPS; k += 2) { s[0] += w[k]; s[1] += w[k + 1]; }
+    }
+    return warp_sum64(s[0] + s[1]);
+}
 
 // 512 threads per CTA, one slice of the vocabulary per warp.
 template <typename T>
@@ -181,7 +273,14 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
     const float heat = a.heat[b];
     const bool draws = heat > 0.f;
     const double scale = 1.4426950408889634074 / (double)heat;             // weights are 2^((logit - largest) * scale)
-    if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0);
+    if (tid < EXP_TABLE * 16) sh.table[tid] = two_to[tid / 16];
+    __syncthreads();
+    auto weight_of = [&](float l, float top) {
+        const float x[1] = {l};
+        double w[1];
+        exp2_64(x, (double)top, scale, lowest_logit((double)top, scale), sh.table + (lane & 15), w);
+        return w[0];
+    };
     // ---- every row's largest logit and sum, a warp per row
     for (int i = warp; i < n; i += VF_WARPS) {
         const float4* st = a.stats + (size_t)(q0 + i) * a.pieces;
@@ -191,7 +290,7 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         for (int o = 16; o > 0; o >>= 1) best = better(best, Best{__shfl_xor_sync(0xffffffffu, best.top, o), __shfl_xor_sync(0xffffffffu, best.at, o)});
         double sum = 0.0;
         for (int k = lane; k < a.pieces; k += 32)
-            if (draws && st[k].x > -INFINITY) sum += (double)st[k].z * exp2(((double)st[k].x - (double)best.top) * scale);
+            if (draws && st[k].x > -INFINITY) sum += (double)st[k].z * weight_of(st[k].x, best.top);
         sum = warp_sum64(sum);
         if (lane == 0) { sh.top[i] = best.top; sh.best[i] = best.at; sh.sum[i] = sum; }
     }
@@ -204,7 +303,7 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
     __syncthreads();
     auto weight = [&](int row, int x) {                    // of token x behind row `row`, relative to the row's largest
         if (x < 0 || x >= a.vocab || sh.top[row] == -INFINITY) return 0.0;
-        return exp2_64(((double)to_f(logits[(long long)(q0 + row) * a.stride + x]) - (double)sh.top[row]) * scale, sh.table);
+        return weight_of(to_f(logits[(long long)(q0 + row) * a.stride + x]), sh.top[row]);
     };
     for (int i = tid; i < n; i += VF_THREADS) {
         const int up = sh.up[i];
@@ -256,36 +355,19 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
     __syncthreads();
     const int refused = sh.refused;
     const bool taken = a.draft && refused > 0;
-    const T* row = logits + (long long)(q0 + last) * a.stride;
-    const float* q = taken ? a.draft + (long long)(q0 + sh.first[0]) * a.draft_stride : nullptr;
-    const double top = (double)sh.top[last];
     const int slice = cta * VF_WARPS + warp, slices = ctas * VF_WARPS, e0 = (int)((long long)a.vocab * slice / slices), e1 = (int)((long long)a.vocab * (slice + 1) / slices);
-    double norm = 0.0;                                     // 1 / sum of weights; 0: nothing is taken off
-    auto value = [&](int i, float l, float minus) {
-        double w = exp2_64(((double)l - top) * scale, sh.table);
-        if (norm > 0.0) return fmax(fma(w, norm, -(double)minus), 0.0);
-        if (!a.draft) for (int r = 0; r < refused; r++) if (sh.token[sh.first[r]] == i) w = 0.0;
-        return w;
-    };
+    RowLeft<T> left = {logits + (long long)(q0 + last) * a.stride, taken ? a.draft + (long long)(q0 + sh.first[0]) * a.draft_stride : nullptr,
+                       (double)sh.top[last], scale, 0.0, a.draft ? 0 : refused};
+    if (lane == 0) {                                       // both rows on their way: the sums have too few loads under way to wait for HBM
+        prefetch_l2(left.row + e0, (size_t)(e1 - e0) * sizeof(T));
+        if (taken) prefetch_l2(left.q + e0, (size_t)(e1 - e0) * 4);
+    }
     // Sums of all slices, the same in all CTAs: every lane has those of `mine` consecutive ones, `before` those ahead of them; returns the total.
     constexpr int MOST = VF_CLUSTER * VF_WARPS / 32;
     const int mine = (slices + 31) / 32;
     double held[MOST], before = 0.0;
     auto sum_all = [&]() {
-        double s[2] = {0.0, 0.0};
-        constexpr int U = 8;                               // loads of so many steps side by side
-        for (int base = e0 + lane; base < e1; base += 32 * U) {
-            float l[U], minus[U];
-#pragma unroll
-            for (int k = 0; k < U; k++) {
-                const bool in = base + k * 32 < e1;
-                l[k] = in ? to_f(row[base + k * 32]) : -INFINITY;
-                minus[k] = in && norm > 0.0 ? q[base + k * 32] : 0.f;
-            }
-#pragma unroll
-            for (int k = 0; k < U; k++) s[k & 1] += value(base + k * 32, l[k], minus[k]);
-        }
-        const double all = warp_sum64(s[0] + s[1]);
+        const double all = left_sum(left, sh, e0, e1, nullptr);
         cluster.sync();                                    // nobody reads the last sums any more
         if (lane < ctas) cluster.map_shared_rank(sh.slices, lane)[slice] = all;
         cluster.sync();
@@ -301,11 +383,12 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         if (lane == 0) before = 0.0;
         return __shfl_sync(0xffffffffu, incl, 31);
     };
-    double total = sum_all();
-    if (taken && total > 0.0) {
-        norm = 1.0 / total;
+    double total;
+    for (int round = 0;; round++) {
         total = sum_all();
-        if (!(total > 0.0)) { norm = 0.0; total = sum_all(); }     // nothing left: the draft's distribution covers the target's
+        if (round == 0 && taken && total > 0.0) left.norm = 1.0 / total;               // now what the refused draft leaves
+        else if (round == 1 && !(total > 0.0)) left.norm = 0.0;                        // nothing: its distribution covers the target's
+        else break;
     }
     // ---- the first element whose running sum exceeds u * total
     if (!(total > 0.0)) {
@@ -325,21 +408,40 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         const unsigned hits = __ballot_sync(0xffffffffu, pick >= 0), any = __ballot_sync(0xffffffffu, some >= 0);
         if (hits) { const int src = __ffs(hits) - 1; pick = __shfl_sync(0xffffffffu, pick, src); start = __shfl_sync(0xffffffffu, start, src); }
         else { pick = __shfl_sync(0xffffffffu, some, 31 - __clz(any)); start = -INFINITY; }        // rounding leaves none: the last with a weight
-        if (pick == slice) {
-            int found = -1, fallback = -1;
-            double run = start;
-            for (int base = e0; base < e1 && found < 0; base += 32) {
-                const int i = base + lane;
-                const double v = i < e1 ? value(i, to_f(row[i]), norm > 0.0 ? q[i] : 0.f) : 0.0;
-                double x = v;
+        if (pick / VF_WARPS == cta) {                      // the same in the whole CTA: its warps share the slice out
+            const int p0 = (int)((long long)a.vocab * pick / slices), p1 = (int)((long long)a.vocab * (pick + 1) / slices);
+            const int f0 = p0 + (int)((long long)(p1 - p0) * warp / VF_WARPS), f1 = p0 + (int)((long long)(p1 - p0) * (warp + 1) / VF_WARPS);
+            const double part = left_sum(left, sh, f0, f1, nullptr);
+            if (lane == 0) sh.part[warp] = part;
+            __syncthreads();
+            double incl = lane < VF_WARPS ? sh.part[lane] : 0.0;
+            const bool weighs = incl > 0.0;
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-                const unsigned hit = __ballot_sync(0xffffffffu, v > 0.0 && run + x > goal), weighs = __ballot_sync(0xffffffffu, v > 0.0);
-                if (hit) found = base + __ffs(hit) - 1;
-                if (weighs) fallback = base + 31 - __clz(weighs);
-                run += __shfl_sync(0xffffffffu, x, 31);
+            for (int o = 1; o < VF_WARPS; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += y; }
+            const unsigned over = __ballot_sync(0xffffffffu, weighs && start + incl > goal), has = __ballot_sync(0xffffffffu, weighs);
+            const int sub = over ? __ffs(over) - 1 : 31 - __clz(has);
+            const double ahead_of = __shfl_sync(0xffffffffu, incl, max(sub - 1, 0));
+            if (warp == sub) {
+                double run = sub > 0 ? start + ahead_of : start;
+                int found = -1, last_one = -1;
+                for (int base = f0; base < f1 && found < 0; base += 32 * LEFT_STEPS) {
+                    left_sum(left, sh, base, min(f1, base + 32 * LEFT_STEPS), sh.held);
+                    __syncwarp();
+#pragma unroll 1
+                    for (int k = 0; k < LEFT_STEPS && found < 0; k++) {
+                        const double v = sh.held[k * 32 + lane];
+                        double x = v;
+#pragma unroll
+                        for (int o = 1; o < 32; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+                        const unsigned hit = __ballot_sync(0xffffffffu, v > 0.0 && run + x > goal), some_here = __ballot_sync(0xffffffffu, v > 0.0);
+                        if (hit) found = base + k * 32 + __ffs(hit) - 1;
+                        if (some_here) last_one = base + k * 32 + 31 - __clz(some_here);
+                        run += __shfl_sync(0xffffffffu, x, 31);
+                    }
+                    __syncwarp();
+                }
+                if (lane == 0) a.next[b] = found >= 0 ? found : last_one;
             }
-            if (lane == 0) a.next[b] = found >= 0 ? found : fallback;
         }
     }
     cluster.sync();                                        // no CTA leaves while others write to its shared memory

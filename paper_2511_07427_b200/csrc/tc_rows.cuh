@@ -29,6 +29,9 @@ __device__ __forceinline__ bool elect_one() {
     return r != 0;
 }
 __device__ __forceinline__ void tt_proxy_fence() { asm volatile("fence.proxy.async;\n" ::: "memory"); }
+// Registers a thread of the warpgroup is to have from here on, out of what the launch gave the block.
+template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(N)); }
 // Two fp32 sums in one instruction.
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     float2 d;
