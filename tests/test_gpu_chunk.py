@@ -1,0 +1,461 @@
+"""Attention of chunks over a paged cache against a 64-bit reference.
+
+Tolerances, with u = 2^-24.  A logit of d products summed in fp32 is off by at most (d + 4) u sum |q_e k_e| scale; a cap adds 2^-22 of
+itself, a bias 6 u of its size a stage (128 rows) further on; the exponential of a difference adds 4 u of the logits' size, and 2^-21 for the
+approximate instruction and the merges: eps, the relative error of a weight, doubled because the sum of weights has it too.
+Weights enter the products as fp32 (fp32 rows), as bf16 (2^-8 of the weight; so many query rows per KV head that the tcgen05 kernel takes
+them), as bf16 hi + lo (2^-16) or as f16 (2^-11); a sum over n rows adds n u; the output's own rounding half a step."""
+import math
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_07427_b200 as P
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+KV = {"f32": P.F32, "bf16": P.BF16, "fp8": P.FP8}
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+class Chunk:
+    """Sequences of given lengths on shuffled pages and the last of their tokens; NaN wherever nothing was written."""
+
+    def __init__(self, lens, new, heads, hk, d, cache, seed=0, lead=0, tail=0, extra=0, size=1.0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.lens, self.new, self.heads, self.hk, self.d, self.cache = lens, new, heads, hk, d, cache
+        per = [(n + 31) // 32 for n in lens]
+        total = sum(per) + 2
+        self.c = P.RowCache.allocate(total, hk, d, KV[cache])
+        for t in (self.c.k, self.c.v, self.c.k_exp, self.c.v_exp):
+            if t is not None:
+                t.view(torch.uint8).fill_(0xff)
+        order = torch.randperm(total, generator=g, device="cuda").to(torch.int32)
+        self.table = torch.full((len(lens), max(per + [0]) + extra), 1 << 30, dtype=torch.int32, device="cuda")
+        io = torch.float32 if cache == "f32" else torch.bfloat16
+        at = 0
+        for b, n in enumerate(lens):
+            self.table[b, :per[b]] = order[at:at + per[b]]
+            at += per[b]
+            if n:
+                k, v = (torch.randn(n, hk, d, generator=g, device="cuda").to(io) for _ in range(2))
+                i = torch.arange(n, device="cuda")
+                self.c.write(k, v, (self.table[b].long()[i // 32] * 32 + i % 32).to(torch.int32))
+        n = lead + sum(new) + tail
+        self.q = (size * torch.randn(n, heads, d, generator=g, device="cuda")).to(io)
+        self.q_start = torch.tensor(lead + np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+        self.kv_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        self.most = max(new + [1])
+        self.lead, self.n = lead, n
+        self.low = torch.zeros(n, dtype=torch.int64, device="cuda")
+        self.high = torch.zeros(n, dtype=torch.int64, device="cuda")
+        self.place = torch.zeros(n, dtype=torch.int64, device="cuda")
+        at = lead
+        for length, t in zip(lens, new):
+            self.place[at:at + t] = torch.arange(length - t, length, device="cuda")
+            at += t
+        self.high[:] = self.place + 1
+        self.from_to = {}
+        self.slopes = None
+
+    def see(self, low=None, high=None):
+        """Ranges of rows: functions of (sequence, own rows, length)."""
+        for name, f, mine in (("rows_from", low, self.low), ("rows_to", high, self.high)):
+            if f is not None:
+                at = self.lead
+                for b, (n, t) in enumerate(zip(self.lens, self.new)):
+                    mine[at:at + t] = f(b, self.place[at:at + t], n)
+                    at += t
+                self.from_to[name] = mine.to(torch.int32)
+        return self
+
+    def run(self, **kw):
+        return self.c.attend_chunk(self.q, self.table, self.kv_len, self.q_start, self.most, slopes=self.slopes, **self.from_to, **kw)
+
+    def rows(self, b, h):
+        n = self.lens[b]
+        pages = self.table[b].long()[:(n + 31) // 32]
+        known = (pages >= 0) & (pages < self.c.n_pages)
+        pages = torch.where(known, pages, 0)
+        got = []
+        for pool, exp in ((self.c.k, self.c.k_exp), (self.c.v, self.c.v_exp)):
+            x = pool.view(torch.uint8)[pages, h].contiguous().view(pool.dtype).float().double().reshape(-1, self.d)[:n]
+            if exp is not None:
+                x = x * torch.exp2(exp[pages, h].double()).reshape(-1)[:n, None]
+            got.append(x)
+        return *got, known.repeat_interleave(32)[:n]
+
+    def check(self, out, lse, scale=None, softcap=0.0, window=0):
+        scale = scale if scale is not None else self.d ** -0.5
+        group, half = self.heads // self.hk, torch.finfo(out.dtype).eps / 2
+        many = self.most * group
+        grain = {"f32": 0.0, "bf16": 2.0 ** -8 if many > 32 else 2.0 ** -16, "fp8": 2.0 ** -8 if many > 64 else 2.0 ** -11}[self.cache]
+        at = self.lead
+        for b, (n, t) in enumerate(zip(self.lens, self.new)):
+            place = self.place[at:at + t]
+            low = torch.maximum(self.low[at:at + t], place + 1 - window) if window else self.low[at:at + t]
+            row = torch.arange(n, device="cuda")
+            for h in range(self.hk if t else 0):
+                k, v, known = self.rows(b, h)
+                see = (row >= low[:, None]) & (row < self.high[at:at + t, None]) & known
+                for hq in range(h * group, (h + 1) * group):
+                    q = self.q[at:at + t, hq].double()
+                    s = (q @ k.T) * scale
+                    err = (self.d + 4) * U * (q.abs() @ k.abs().T) * abs(scale)
+                    if softcap:
+                        s = softcap * torch.tanh(s / softcap)
+                        err = err + 2.0 ** -22 * softcap
+                    if self.slopes is not None:
+                        away = self.slopes[hq].double() * (place[:, None] - row).abs()
+                        s = s - away
+                        err = err + 6 * U * (away.abs() + self.slopes[hq].double().abs() * 128)
+                    s = torch.where(see, s, -math.inf)
+                    want_lse = torch.logsumexp(s, -1) if n else torch.full((t,), -math.inf, dtype=torch.float64, device="cuda")
+                    w = torch.where(see, torch.exp(s - torch.where(torch.isfinite(want_lse), want_lse, 0.0)[:, None]), 0.0)
+                    vv = torch.where(known[:, None], v, 0.0)
+                    vv = torch.where(torch.isfinite(vv), vv, 0.0)              # rows that hold no numbers: the caller checks who sees them
+                    want, weight = w @ vv, w @ vv.abs()
+                    seen_err = torch.where(see, err + 4 * U * s.abs().nan_to_num(posinf=0.0, neginf=0.0), 0.0)
+                    eps = 2 * (seen_err.amax(-1) if n else torch.zeros(t, dtype=torch.float64, device="cuda")) + 2.0 ** -20
+                    none = ~see.any(-1)
+                    assert not out[at:at + t, hq][none].any() and bool((lse[at:at + t, hq][none] == -math.inf).all())
+                    got = out[at:at + t, hq].double()
+                    bound = (eps + grain + n * U)[:, None] * weight + half * want.abs() + 1e-30
+                    bad = (got - want).abs() > bound
+                    assert not bad.any(), (b, hq, float(((got - want).abs() / bound).max()), int(bad.sum()))
+                    ok = ~none
+                    assert bool(((lse[at:at + t, hq].double() - want_lse).abs()[ok] <= (eps + n * U + 2 * U * want_lse.abs())[ok]).all()), (b, hq)
+            at += t
+        assert self.c.get_status() == 0
+
+
+GROUPS = [(4, 4), (4, 2), (6, 2), (8, 2), (5, 1), (6, 1), (7, 1), (16, 2)]
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,hk", GROUPS)
+def test_causal_chunks_of_every_group(cache, d, heads, hk):
+    p = Chunk([333, 70, 129, 64], [150, 70, 1, 0], heads, hk, d, cache)
+    p.check(*p.run())
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("lens,new", [([1], [1]), ([0], [1]), ([0, 5], [3, 5]), ([31, 32, 33], [31, 32, 33]), ([127, 128, 129], [127, 128, 129]), ([4], [9]),
+                                      ([1000], [1]), ([3000, 1], [2, 1]), ([257, 255, 256], [257, 255, 256])])
+def test_short_and_odd_lengths(cache, lens, new):
+    p = Chunk(lens, new, 8, 2, 128, cache, seed=3, extra=1)
+    # more tokens than rows: those before the first row see nothing
+    p.check(*p.run())
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [1, 5, 300])
+@pytest.mark.parametrize("window", [1, 2, 31, 128, 1000, 2 ** 31 - 1])
+def test_windows(cache, new, window):
+    p = Chunk([700, 40 + new, 301], [new, new, min(new, 7)], 12, 4, 64, cache, seed=window % 97)
+    p.check(*p.run(window=window), window=window)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [2, 200])
+@pytest.mark.parametrize("cap,size", [(50.0, 1.0), (30.0, 8.0), (1.0, 1.0), (0.25, 4.0), (1e4, 1.0)])
+def test_capped_scores(cache, new, cap, size):
+    p = Chunk([513, 200], [new, 100 if new > 2 else 1], 8, 2, 128, cache, seed=5, size=size)
+    p.check(*p.run(softcap=cap), softcap=cap)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [3, 260])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_biases_by_distance(cache, new, cap):
+    p = Chunk([600, 300], [new, 3], 6, 2, 128, cache, seed=6)
+    p.slopes = torch.tensor([0.5, 0.0, 2.0 ** -8, 1.0, -0.002, 3.0], device="cuda")
+    p.see(high=lambda b, place, n: torch.minimum(place + 40, torch.full_like(place, n)))        # rows on both sides
+    p.check(*p.run(softcap=cap), softcap=cap)
+
+
+def documents(length, seed):
+    """Borders of documents, some of one row, and each row's first and last + 1."""
+    rng = np.random.default_rng(seed)
+    borders = np.unique(np.concatenate([[0, length], rng.integers(0, length + 1, 9), [min(5, length), min(6, length)]]))
+    owner = np.searchsorted(borders, np.arange(length), side="right") - 1
+    return torch.tensor(borders[owner], device="cuda"), torch.tensor(borders[owner + 1], device="cuda")
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("d,heads,hk", [(128, 7, 1), (64, 8, 8)])
+@pytest.mark.parametrize("both", [False, True])
+def test_documents(cache, d, heads, hk, both):
+    lens, new = [900, 411], [900, 200]
+    p = Chunk(lens, new, heads, hk, d, cache, seed=7)
+    docs = [documents(n, i) for i, n in enumerate(lens)]
+    p.see(low=lambda b, place, n: docs[b][0][place], high=(lambda b, place, n: docs[b][1][place]) if both else None)
+    p.check(*p.run())
+    p.check(*p.run(window=50), window=50)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [1, 40, 500])
+def test_prefixes_that_all_tokens_see(cache, new):
+    p = Chunk([500, 150 + new], [new, min(new, 90)], 8, 2, 64, cache, seed=8)
+    p.see(high=lambda b, place, n: (place + 1).clamp(min=n // 2))
+    p.check(*p.run())
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [6, 300])
+def test_ranges_that_leave_nothing_and_reach_beyond(cache, new):
+    p = Chunk([310, 305], [new, 5], 8, 2, 128, cache, seed=9)
+    # empty, upside down, one row, all rows, beyond both ends
+    kinds = [(0, 0), (200, 100), (17, 18), (0, 310), (-5, 10 ** 9), (309, 10 ** 6), (500, 600), (-100, -50)]
+    pick = lambda i: lambda b, place, n: torch.tensor([kinds[int(x) % len(kinds)][i] for x in place], device="cuda")
+    p.see(low=pick(0), high=pick(1))
+    out, lse = p.run()
+    p.high.clamp_(max=10 ** 6)
+    p.check(out, lse)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [1, 200])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.0])
+def test_scales(cache, new, scale):
+    p = Chunk([300], [new], 8, 2, 64, cache, seed=10, size=0.5)
+    p.check(*p.run(scale=scale), scale=scale)
+    p.check(*p.run(scale=scale, softcap=5.0), scale=scale, softcap=5.0)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+def test_long_rows_are_shared_out_and_merged(cache):
+    for lens, new in (([9000, 40], [70, 40]), ([5000], [1]), ([6000, 6000, 17], [130, 4, 17])):
+        p = Chunk(lens, new, 8, 2, 128, cache, seed=11)
+        p.check(*p.run())
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("most", [1, 40])
+def test_many_sequences(cache, most):
+    rng = np.random.default_rng(1)
+    lens = [int(x) for x in rng.integers(0, 90, 1100)]
+    new = [int(min(n, rng.integers(0, most + 1))) for n in lens]
+    p = Chunk(lens, new, 2, 1, 64, cache, seed=12)
+    out, lse = p.run()
+    # a sample of them against the reference
+    p2 = np.flatnonzero(np.array(new))[::97]
+    starts = p.q_start.tolist()
+    for b in p2:
+        sub = Chunk([lens[b]], [new[b]], 2, 1, 64, cache)
+        sub.c, sub.table, sub.q = p.c, p.table[b:b + 1], p.q[starts[b]:starts[b + 1]]
+        sub.most = p.most
+        sub.check(out[starts[b]:starts[b + 1]], lse[starts[b]:starts[b + 1]])
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [3, 140])
+def test_tokens_of_no_sequence_are_left(cache, new):
+    p = Chunk([200, 180], [new, new], 4, 1, 128, cache, seed=13, lead=5, tail=11)
+    out, lse = torch.full_like(p.q, 7.0), torch.full((p.n, 4), 9.0, device="cuda")
+    got = p.run(out=out, lse=lse)
+    assert got[0] is out and got[1] is lse
+    for x, v in ((out, 7.0), (lse, 9.0)):
+        assert bool((x[:5] == v).all()) and bool((x[-11:] == v).all())
+    p.check(out, lse)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [4, 160])
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+def test_rows_that_hold_no_numbers_reach_only_who_sees_them(cache, new, what):
+    if cache == "fp8" and what == math.inf:
+        what = -math.inf
+    p = Chunk([400], [new], 8, 2, 128, cache, seed=14)
+    io = torch.float32 if cache == "f32" else torch.bfloat16
+    place = 400 - new // 2                                        # half of the tokens see it
+    k, v = torch.randn(1, 2, 128, device="cuda").to(io), torch.randn(1, 2, 128, device="cuda").to(io)
+    v[0, 1, 77] = what
+    p.c.write(k, v, (p.table[0].long()[place // 32] * 32 + place % 32).to(torch.int32).view(1))
+    out, lse = p.run()
+    sees = p.place >= place
+    mine = out[:, 4:]                                             # the second KV head's
+    assert torch.isfinite(lse).all() and torch.isfinite(out[:, :4]).all() and torch.isfinite(mine[~sees]).all()
+    if cache == "fp8" and what == -math.inf:
+        # e4m3 has no infinity: the row holds 448 * 2^120 (5.9e38, beyond fp32), which weights of 1 / 400 and less bring back into range
+        assert bool((mine[sees][:, :, 77].abs() > 1e30).all())
+    else:
+        assert not torch.isfinite(mine[sees][:, :, 77]).any()
+    if not (cache == "fp8"):                                      # there an infinite element scales the others of its row to nothing
+        rest = torch.ones(128, dtype=torch.bool, device="cuda")
+        rest[77] = False
+        assert torch.isfinite(mine[sees][:, :, rest]).all()
+        fixed = out.clone()
+        fixed[:, 4:, 77] = 0
+        p.c.v[p.table[0, place // 32].long(), 1, place % 32, 77] = 0.0
+        clean, _ = p.run()
+        clean[:, 4:, 77] = 0
+        assert torch.allclose(fixed.float(), clean.float(), rtol=2.0 ** -6, atol=2.0 ** -7)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [2, 100])
+def test_unseen_keys_that_hold_no_numbers(cache, new):
+    p = Chunk([256], [new], 8, 2, 64, cache, seed=15)
+    p.see(low=lambda b, place, n: torch.full_like(place, 20))
+    page = int(p.table[0, 0])
+    want = p.run()
+    for pool in (p.c.k, p.c.v):
+        pool.view(torch.uint8)[page, :, :20] = 0xff
+    got = p.run()
+    for x, y in zip(want, got):
+        assert torch.isfinite(y).all()
+        assert torch.allclose(x.float(), y.float(), rtol=2.0 ** -6, atol=2.0 ** -8)       # sums taken again row by row, without rounded weights
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [2, 150])
+def test_same_bits_every_time_and_under_a_graph(cache, new):
+    p = Chunk([2000, 700], [new, new], 8, 2, 128, cache, seed=16)
+    first = p.run(softcap=30.0, window=900)
+    again = p.run(softcap=30.0, window=900)
+    assert all(torch.equal(x, y) for x, y in zip(first, again))
+    stream = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        p.run(softcap=30.0, window=900)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            out, lse = p.run(softcap=30.0, window=900)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    # other lengths under the same graph
+    p.kv_len.copy_(torch.tensor([1500, new], dtype=torch.int32))
+    graph.replay()
+    torch.cuda.synchronize()
+    q = Chunk([1500, new], [new, new], 8, 2, 128, cache)
+    q.c, q.table, q.q = p.c, p.table, p.q
+    q.check(out, lse, softcap=30.0, window=900)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+def test_two_streams_and_two_graphs_at_once(cache):
+    p = [Chunk([3000, 500], [n, 77], 8, 2, 64, cache, seed=17 + n) for n in (90, 130)]
+    want = [x.run() for x in p]
+    streams, graphs, got = [torch.cuda.Stream() for _ in p], [torch.cuda.CUDAGraph() for _ in p], [None, None]
+    torch.cuda.synchronize()
+    for i, x in enumerate(p):
+        with torch.cuda.stream(streams[i]):
+            with torch.cuda.graph(graphs[i], stream=streams[i]):
+                got[i] = x.run()
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+                p[i].run()
+    torch.cuda.synchronize()
+    for x, y in zip(want, got):
+        assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+
+
+@pytest.mark.parametrize("heads,new", [(1, 3), (4, 60)])
+def test_a_cache_of_more_than_2_to_the_31_elements(heads, new):
+    pages, hk, d = 70000, 8, 128
+    c = P.RowCache.allocate(pages, hk, d, P.BF16)
+    p = Chunk([200], [new], heads * hk, hk, d, "bf16", seed=18)
+    high = torch.arange(pages - 7, pages, device="cuda")
+    for mine, big in ((p.c.k, c.k), (p.c.v, c.v)):
+        big[high] = mine[p.table[0].long()]
+    p.c, p.table = c, high.to(torch.int32).view(1, 7)
+    p.check(*p.run())
+
+
+def test_missing_pages_and_lengths_out_of_range():
+    for cache in ("f32", "bf16", "fp8"):
+        for new in (2, 150):
+            p = Chunk([500, 300], [new, new], 8, 2, 128, cache, seed=19)
+            good = p.table.clone()
+            p.table[0, 1], p.table[0, 7], p.table[1, 0] = -1, p.c.n_pages, 1 << 30
+            out, lse = p.run()
+            assert p.c.get_status() == P.ST_BOUNDS
+            p.c._status.zero_()
+            p.check(out, lse)                                     # the rows of those pages count as not seen
+            # a sequence whose range or length is none has no part in the others
+            p.table.copy_(good)
+            for lens, starts in (([-1, 300], [0, new, 2 * new]), ([10 ** 9, 300], [0, new, 2 * new]), ([500, 300], [-4, new, 2 * new]), ([500, 300], [new + 50, new, 2 * new])):
+                p.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+                p.q_start.copy_(torch.tensor(starts, dtype=torch.int32))
+                o, z = p.run()
+                assert p.c.get_status() == P.ST_BOUNDS
+                p.c._status.zero_()
+                q = Chunk([300], [new], 8, 2, 128, cache)
+                q.c, q.table, q.q, q.most = p.c, p.table[1:], p.q[new:], p.most
+                q.check(o[new:], z[new:])
+
+
+def test_overlapping_token_ranges_stay_inside_the_workspace():
+    p = Chunk([300] * 6, [100] * 6, 8, 2, 128, "bf16", seed=20)
+    p.q_start.copy_(torch.tensor([0, 600, 0, 600, 0, 600, 0], dtype=torch.int32))
+    p.most = 600
+    p.run()
+    assert p.c.get_status() & P.ST_BOUNDS
+
+
+def test_agrees_with_tree_attention():
+    for cache in ("f32", "bf16", "fp8"):
+        p = Chunk([700, 300, 90], [40, 3, 25], 8, 2, 128, cache, seed=21)
+        a, b = p.run(), p.c.attend_tree(p.q, p.table, p.kv_len, p.q_start, p.most)
+        assert torch.allclose(a[0].float(), b[0].float(), rtol=2.0 ** -6, atol=2.0 ** -7)
+        assert torch.allclose(a[1], b[1], rtol=1e-5, atol=1e-5)
+
+
+def test_first_call_of_a_process_under_capture():
+    code = """
+import torch, paper_2511_07427_b200 as P
+for dtype, new in ((P.BF16, 60), (P.FP8, 80), (P.F32, 80), (P.BF16, 1)):
+    c = P.RowCache.allocate(8, 2, 128, dtype)
+    io = torch.float32 if dtype == P.F32 else torch.bfloat16
+    k = torch.randn(128, 2, 128, device="cuda").to(io)
+    slots = torch.arange(128, dtype=torch.int32, device="cuda")
+    c.write(k, k, slots)
+    q = torch.randn(new, 4, 128, device="cuda").to(io)
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(1, 4)
+    n = torch.tensor([128], dtype=torch.int32, device="cuda")
+    s = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        out, lse = c.attend_chunk(q, table, n, s, new, softcap=9.0)
+    g.replay()
+    torch.cuda.synchronize()
+    want, _ = c.attend_chunk(q, table, n, s, new, softcap=9.0)
+    assert torch.equal(out, want) and bool(torch.isfinite(out).all()) and bool(out.any())
+print("fine")
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stdout + r.stderr
+
+
+def test_refusals():
+    p = Chunk([100], [4], 8, 2, 128, "bf16")
+    q, table, lens, start = p.q, p.table, p.kv_len, p.q_start
+    ok = dict(q=q, page_table=table, kv_len=lens, q_start=start, max_chunk=4)
+    slopes, rows = torch.ones(8, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    for bad in (dict(q=q.float()), dict(q=q[:, :, :64]), dict(q=q.transpose(0, 1)), dict(q=q.cpu()), dict(q=q[:, :7].contiguous()), dict(q=q[:, :0].contiguous()),
+                dict(page_table=table[0]), dict(page_table=table.long()), dict(kv_len=lens.long()), dict(kv_len=lens.cpu()), dict(q_start=start[:1]),
+                dict(max_chunk=0), dict(max_chunk=(1 << 24) + 1), dict(scale=math.nan), dict(scale=math.inf), dict(softcap=-1.0), dict(softcap=math.inf),
+                dict(softcap=math.nan), dict(window=-1), dict(window=1 << 31), dict(slopes=slopes[:7]), dict(slopes=slopes.double()), dict(slopes=slopes.cpu()),
+                dict(slopes=torch.ones(16, device="cuda")[::2]), dict(rows_from=rows[:3]), dict(rows_to=rows.long()), dict(rows_from=rows.cpu()),
+                dict(out=q.float()), dict(out=q), dict(out=torch.empty_like(q)[:2]), dict(lse=torch.empty(4, 8, dtype=torch.bfloat16, device="cuda")),
+                dict(lse=torch.empty(4, 7, device="cuda"))):
+        with pytest.raises(P.DynaKVError):
+            p.c.attend_chunk(**{**ok, **bad})
+    with pytest.raises(P.DynaKVError, match="gradient"):
+        p.c.attend_chunk(**{**ok, "q": q.clone().requires_grad_()})
+    with pytest.raises(P.DynaKVError, match="gradient"):
+        p.c.attend_chunk(**ok, slopes=slopes.clone().requires_grad_())
+    with torch.no_grad():
+        p.c.attend_chunk(**{**ok, "q": q.clone().requires_grad_()})
+    assert p.c.attend_chunk(q[:0], table[:0], lens[:0], start[:1], 4)[0].shape == (0, 8, 128)
