@@ -27,42 +27,59 @@ static int chunk_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& m
 #ifndef DKV_CHUNK_F32
 #define DKV_CHUNK_F32 65
 #endif
-struct ChunkKind { bool planned; int rg, rows, ctas, per; };             // per: tokens of a planned tile
-static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int max_chunk, int sms) {
+// From three tiles per sequence on FP8 rows are turned into bf16 first (chunk_tc.cu), unless that takes more than CHUNK_WIDE bytes.
+constexpr size_t CHUNK_WIDE = (size_t)2 << 30;
+struct ChunkKind { bool planned; int rg, rows, ctas, per; bool wide; };             // per: tokens of a planned tile
+static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int n_seqs, int max_chunk, int pages_per_seq, int sms) {
     const bool f32 = c->kv_dtype == DYNAKV_F32;
     const int most = (int)min(1000ll, (long long)max_chunk * (n_heads / c->n_kv_heads));
     if (most >= (f32 ? DKV_CHUNK_F32 : c->kv_dtype == DYNAKV_FP8 ? DKV_CHUNK_TC_FP8 : DKV_CHUNK_TC_BF16)) {
         const int G = n_heads / c->n_kv_heads;
-        return {true, 0, f32 ? CF_ROWS : CT_ROWS, sms, f32 ? CF_ROWS / G : tile_tokens(G)};
+        return {true, 0, f32 ? CF_ROWS : CT_ROWS, sms, f32 ? CF_ROWS / G : tile_tokens(G),
+                c->kv_dtype == DYNAKV_FP8 && max_chunk > 2 * tile_tokens(G) && n_seqs <= 65535 && c->n_kv_heads <= 65535 && chunk_wide_bytes(c, n_seqs, pages_per_seq) <= CHUNK_WIDE};
     }
     const int rg = row_groups(most, f32);
-    return {false, rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2), 0};
+    return {false, rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2), 0, false};
 }
 
-static bool chunk_shape_ok(const dynakv_row_cache* c, int n_heads, int64_t n_tokens, int n_seqs, int max_chunk) {
+// Workspace: records, the plan, rows as bf16.
+struct ChunkSpace { TreeSpace records; size_t wide, bytes; };
+static ChunkSpace chunk_space(const dynakv_row_cache* c, const ChunkKind& k, int64_t n_tokens, int n_seqs, int pages_per_seq, char* base, ChunkPlan* plan) {
+    ChunkSpace s;
+    s.records = tree_space(k.ctas, k.rows, c->head_dim);
+    s.wide = 0;
+    s.bytes = s.records.bytes;
+    if (k.planned) s.bytes = chunk_plan_space(n_tokens, k.per, n_seqs, k.ctas, s.bytes, base, plan);
+    if (k.wide) {
+        s.wide = (s.bytes + 127) / 128 * 128;
+        s.bytes = s.wide + chunk_wide_bytes(c, n_seqs, pages_per_seq) + 128;       // the workspace itself is aligned to 16 bytes
+    }
+    return s;
+}
+
+static bool chunk_shape_ok(const dynakv_row_cache* c, int n_heads, int64_t n_tokens, int n_seqs, int max_chunk, int pages_per_seq) {
     return row_cache_ok(c) && n_heads >= 1 && n_heads % c->n_kv_heads == 0 && n_heads / c->n_kv_heads <= MAX_G && max_chunk >= 1 && max_chunk <= (1 << 24) &&
-           n_tokens >= 0 && n_tokens < (1ll << 31) && n_seqs >= 0;
+           n_tokens >= 0 && n_tokens < (1ll << 31) && n_seqs >= 0 && pages_per_seq >= 0 && pages_per_seq < (1 << 26);
 }
 
 }  // namespace dkv
 
 using namespace dkv;
 
-extern "C" int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, int32_t n_heads, int64_t n_tokens, int32_t n_seqs, int32_t max_chunk) {
-    if (!chunk_shape_ok(cache, n_heads, n_tokens, n_seqs, max_chunk)) return DYNAKV_ERR_ARG;
+extern "C" int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, int32_t n_heads, int64_t n_tokens, int32_t n_seqs, int32_t max_chunk,
+                                                 int32_t pages_per_seq) {
+    if (!chunk_shape_ok(cache, n_heads, n_tokens, n_seqs, max_chunk, pages_per_seq)) return DYNAKV_ERR_ARG;
     int rc;
     const int sms = sm_count(&rc);
     if (rc != DYNAKV_OK) return rc;
-    const ChunkKind k = chunk_kind(cache, n_heads, max_chunk, sms);
-    const size_t records = tree_space(k.ctas, k.rows, cache->head_dim).bytes;
-    return (int64_t)(k.planned ? chunk_plan_space(n_tokens, k.per, n_seqs, sms, records, nullptr, nullptr) : records);
+    return (int64_t)chunk_space(cache, chunk_kind(cache, n_heads, n_seqs, max_chunk, pages_per_seq, sms), n_tokens, n_seqs, pages_per_seq, nullptr, nullptr).bytes;
 }
 
 extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
                                    int32_t n_seqs, int32_t max_chunk, const int32_t* page_table, int32_t pages_per_seq, const int32_t* kv_len,
                                    const dynakv_scores* scores, void* out, float* lse, void* workspace, int64_t workspace_bytes,
                                    uint32_t* status, void* cuda_stream) {
-    if (!chunk_shape_ok(cache, n_heads, n_tokens, n_seqs, max_chunk) || pages_per_seq < 0 || pages_per_seq >= (1 << 26) || !scores ||
+    if (!chunk_shape_ok(cache, n_heads, n_tokens, n_seqs, max_chunk, pages_per_seq) || !scores ||
         !(fabsf(scores->scale) <= FLT_MAX) || !(scores->softcap >= 0.f && scores->softcap <= FLT_MAX) || scores->window < 0) return DYNAKV_ERR_ARG;
     if (n_tokens == 0 || n_seqs == 0) return DYNAKV_OK;
     if (!q || !q_start || (!page_table && pages_per_seq > 0) || !kv_len || !out || !workspace) return DYNAKV_ERR_ARG;
@@ -70,12 +87,11 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
     int rc;
     const int sms = sm_count(&rc);
     if (rc != DYNAKV_OK) return rc;
-    const ChunkKind kind = chunk_kind(cache, n_heads, max_chunk, sms);
-    const TreeSpace sp = tree_space(kind.ctas, kind.rows, cache->head_dim);
+    const ChunkKind kind = chunk_kind(cache, n_heads, n_seqs, max_chunk, pages_per_seq, sms);
     ChunkPlan plan = {};
-    const size_t bytes = kind.planned ? chunk_plan_space(n_tokens, kind.per, n_seqs, sms, sp.bytes, reinterpret_cast<char*>(workspace), &plan) : sp.bytes;
-    if (workspace_bytes < (int64_t)bytes) return DYNAKV_ERR_ARG;
-    TreeArgs a = tree_args(cache, q, n_heads, n_tokens, q_start, n_seqs, max_chunk, page_table, pages_per_seq, kv_len, out, lse, workspace, sp, status);
+    const ChunkSpace sp = chunk_space(cache, kind, n_tokens, n_seqs, pages_per_seq, reinterpret_cast<char*>(workspace), &plan);
+    if (workspace_bytes < (int64_t)sp.bytes) return DYNAKV_ERR_ARG;
+    TreeArgs a = tree_args(cache, q, n_heads, n_tokens, q_start, n_seqs, max_chunk, page_table, pages_per_seq, kv_len, out, lse, workspace, sp.records, status);
     a.scale = scores->scale;
     a.cap = scores->softcap;
     a.slopes = scores->slopes;
@@ -84,7 +100,11 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     // an error left behind by an earlier, unrelated call on this thread must not be reported as this call's
     cudaGetLastError();
-    if (kind.planned) return cache->kv_dtype == DYNAKV_F32 ? chunk_f32_launch(cache, a, plan, sms, st) : chunk_tc_launch(cache, a, plan, sms, st);
+    if (kind.planned && cache->kv_dtype == DYNAKV_F32) return chunk_f32_launch(cache, a, plan, sms, st);
+    if (kind.planned) {
+        void* wide = reinterpret_cast<void*>(((uintptr_t)workspace + sp.wide + 127) / 128 * 128);
+        return chunk_tc_launch(cache, a, plan, kind.wide ? wide : nullptr, sms, st);
+    }
     CUtensorMap mk, mv;
     if (!tree_page_map(&mk, cache, cache->k, true) || !tree_page_map(&mv, cache, cache->v, true)) return DYNAKV_ERR_CUDA;
     const int rg = kind.rg;

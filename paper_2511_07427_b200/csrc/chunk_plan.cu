@@ -39,6 +39,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
             incl = scan(count, total);
         }
         const int first = (int)(tiles + incl - count);
+        if (b < a.n_seqs) p.first[b] = first;
         for (unsigned left = __ballot_sync(0xffffffffu, count > 0); left; left &= left - 1) {      // few sequences have many tiles, so a warp writes a sequence's
             const int src = __ffs(left) - 1;
             const int c = __shfl_sync(0xffffffffu, count, src), f = __shfl_sync(0xffffffffu, first, src), q0 = __shfl_sync(0xffffffffu, s.q0, src),
@@ -55,6 +56,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
         }
         tiles += total;
     }
+    if (tid == 0) p.first[a.n_seqs] = (int)tiles;
     __syncthreads();
     // ---- stages of every tile; where the tokens' ranges have to be read, 8 lanes per tile find the first and the last row
     if (a.rows_from || a.rows_to) {
@@ -152,6 +154,7 @@ size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, size_t 
     p.tiles = reinterpret_cast<ChunkTile*>(take(tiles * sizeof(ChunkTile)));
     p.before = reinterpret_cast<long long*>(take((tiles + 1) * 8));
     p.starts = reinterpret_cast<ChunkStart*>(take((size_t)ctas * sizeof(ChunkStart)));
+    p.first = reinterpret_cast<int*>(take(((size_t)n_seqs + 1) * 4));
     if (plan) *plan = p;
     return at;
 }

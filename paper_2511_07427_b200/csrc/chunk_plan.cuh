@@ -33,6 +33,7 @@ struct ChunkPlan {
     ChunkTile* tiles;                              // [most tiles]
     long long* before;                             // [most tiles + 1] stages of the tiles before, for one KV head
     ChunkStart* starts;                            // [CTAs]
+    int* first;                                    // [n_seqs + 1] first tile of every sequence
 };
 
 __device__ __host__ __forceinline__ int tile_tokens(int G) { return 2 * (128 / G); }
@@ -83,7 +84,11 @@ int chunk_plan_launch(const TreeArgs& a, const ChunkPlan& plan, int sms, int per
 // The bytes up to the end of the plan in a workspace whose first `at` are taken.
 size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, size_t at, char* base, ChunkPlan* plan);
 // The kernels: chunk_tc.cu (bf16 and FP8 rows, tcgen05), chunk_f32.cu.
-int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st);
+// wide: where FP8 rows are turned into bf16 first (chunk_wide_bytes() bytes, 128-byte aligned), NULL: they are not.
+int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, void* wide, int sms, cudaStream_t st);
+static inline size_t chunk_wide_bytes(const dynakv_row_cache* c, int n_seqs, int pages_per_seq) {
+    return (size_t)n_seqs * pages_per_seq * c->n_kv_heads * PAGE * c->head_dim * 2 * 2;
+}
 int chunk_f32_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st);
 
 }  // namespace dkv

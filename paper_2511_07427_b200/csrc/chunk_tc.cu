@@ -78,6 +78,20 @@ __device__ __forceinline__ int lds_s8(unsigned addr) {
     asm volatile("ld.shared.s8 %0, [%1];\n" : "=r"(v) : "r"(addr));
     return v;
 }
+// 16 e4m3 values times 2^e as bf16 pairs (exact).
+__device__ __forceinline__ void widen16(uint4 raw, int e, unsigned (&o)[8]) {
+    const float sc = pow2f(e);
+    const float2 sc2 = make_float2(sc, sc);
+    const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int x = 0; x < 4; x++) {
+        unsigned lo, hi;
+        e4m3x4_to_f16x2(w[x], lo, hi);
+        const float2 y = mul2(__half22float2(*reinterpret_cast<const __half2*>(&lo)), sc2), z = mul2(__half22float2(*reinterpret_cast<const __half2*>(&hi)), sc2);
+        o[2 * x] = pack_bf16(y.x, y.y);
+        o[2 * x + 1] = pack_bf16(z.x, z.y);
+    }
+}
 // What the scores need beside the factor and the mask.
 enum { PLAIN = 0, BIASED = 1, CAPPED = 2 };
 // tanh(y) / y as a polynomial of y^2 (interpolated at Chebyshev nodes; tanh is off by 9e-8 at most), two at a time: for |y| <= 0.4, which
@@ -118,8 +132,8 @@ __device__ __noinline__ void chunk_again(const TreeArgs& a, const ChunkSeg& g, c
     const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q) + q_row * HD;
     for (int e = 0; e < 32; e++) o[e] = 0.f;
     for (int pos = max(w.lo, g.s0 * CT_KEYS); pos < min(w.hi, g.s1 * CT_KEYS); pos++) {
-        const int page = a.page_table[(size_t)g.seq * a.pages_per_seq + pos / PAGE];
-        if (page < 0 || page >= a.n_pages) continue;
+        const int page = chunk_page(a, g.seq, pos / PAGE);
+        if (page < 0) continue;
         const long long key = ((long long)page * a.Hk + g.h) * PAGE + pos % PAGE;
         float d = 0.f;
         for (int e = 0; e < HD; e++) d = fmaf(__bfloat162float(q[e]), cache_elem<DT>(a.kpool, a.kexp, key, HD, e), d);
@@ -181,8 +195,8 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
         int id = -1;
         const int pg = s * CT_PAGES + lane;
         if (lane < CT_PAGES && pg * PAGE < g.n) {
-            id = a.page_table[(size_t)g.seq * a.pages_per_seq + pg];
-            if (id < 0 || id >= a.n_pages) { id = -1; tree_status(a, DYNAKV_ST_BOUNDS); }
+            id = chunk_page(a, g.seq, pg);
+            if (id < 0) tree_status(a, DYNAKV_ST_BOUNDS);
         }
         return id;
     };
@@ -216,15 +230,14 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
 #pragma unroll
                             for (int x = 0; x < CT_PAGES; x++) {
                                 if (page[x] < 0) continue;
+                                const int r = (page[x] * a.Hk + g.h) * PAGE;
                                 if constexpr (F8) {
-                                    const int r = (page[x] * a.Hk + g.h) * PAGE;
                                     tt_load(dst + x * PAGE * HD, map, r, 0, bar(full));
                                     bulk_g2s(sExp + is_v * C::exp_bytes + x * PAGE, (is_v ? a.vexp : a.kexp) + r, PAGE, bar(full));
-                                    continue;
-                                }
+                                } else {
 #pragma unroll
-                                for (int q = 0; q < C::panels; q++)
-                                    tt_load(dst + q * C::panel_bytes + x * PAGE * 128, map, (page[x] * a.Hk + g.h) * PAGE, q, bar(full + st));
+                                    for (int q = 0; q < C::panels; q++) tt_load(dst + q * C::panel_bytes + x * PAGE * 128, map, r, q, bar(full + st));
+                                }
                             }
                         }
                     }
@@ -342,18 +355,8 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     for (int i = 0; i < NP; i++) {
                         const int row = i * RPP + row0;
                         const uint4 raw = lds16(from + row * HD + ((HD == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3)) << 4));
-                        const float sc = pow2f(lds_s8(exps + row));
-                        const float2 sc2 = make_float2(sc, sc);
-                        const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
                         unsigned o[8];
-#pragma unroll
-                        for (int x = 0; x < 4; x++) {
-                            unsigned lo, hi;
-                            e4m3x4_to_f16x2(w[x], lo, hi);
-                            const float2 y = mul2(__half22float2(*reinterpret_cast<const __half2*>(&lo)), sc2), z = mul2(__half22float2(*reinterpret_cast<const __half2*>(&hi)), sc2);
-                            o[2 * x] = pack_bf16(y.x, y.y);
-                            o[2 * x + 1] = pack_bf16(z.x, z.y);
-                        }
+                        widen16(raw, lds_s8(exps + row), o);
                         const unsigned to = dst + (chunk >> 2) * C::panel_bytes + row * 128, ch = (2 * chunk) & 7;
                         sts16(to + ((ch ^ (row & 7)) << 4), make_uint4(o[0], o[1], o[2], o[3]));
                         sts16(to + (((ch + 1) ^ (row & 7)) << 4), make_uint4(o[4], o[5], o[6], o[7]));
@@ -411,13 +414,27 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
 #pragma unroll
                     for (int c = 0; c < 4; c++) tc_ld32(tS + c * 32, x[c]);
                     tc_ld_wait();
+                    // Which rows of the stage this query sees, and (none) which pages nobody in the warp does: those are left out
+                    const bool edge = __any_sync(0xffffffffu, w.lo > key0 || w.hi < key0 + CT_KEYS) || have != (1 << CT_PAGES) - 1;
+                    unsigned win[4] = {~0u, ~0u, ~0u, ~0u}, none = 0u;
+                    if (edge) {
+#pragma unroll
+                        for (int c = 0; c < 4; c++) {
+                            const int z = max(w.lo - key0 - c * 32, 0), y = ((have >> c) & 1) ? min(w.hi - key0 - c * 32, 32) : 0;
+                            win[c] = z >= y ? 0u : (y == 32 ? ~0u : (1u << y) - 1u) & ~((1u << z) - 1u);
+                        }
+                    }
                     float f = qs;                              // what is left to do to the logits
                     if constexpr (MODE == CAPPED) {
+                        if (edge) {                            // what is not seen has no say in which of the tanh is taken: it may be anything
+#pragma unroll
+                            for (int e = 0; e < CT_KEYS; e++) if (!((win[e >> 5] >> (e & 31)) & 1u)) x[e >> 5][e & 31] = 0u;
+                        }
                         float hi = 0.f;
 #pragma unroll
                         for (int e = 0; e < CT_KEYS; e += 2) hi = tt_max3(hi, fabsf(__uint_as_float(x[e >> 5][e & 31])), fabsf(__uint_as_float(x[e >> 5][(e & 31) + 1])));
                         const float2 qs2 = make_float2(qs, qs);
-                        hi *= fabsf(qs);
+                        hi = t < 0 ? 0.f : hi * fabsf(qs);
                         auto near = [&](auto is_short) {
 #pragma unroll
                             for (int e = 0; e < CT_KEYS; e += 2) {
@@ -448,23 +465,13 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                         }
                         f = 1.f;
                     }
-                    // Which pages of the stage nobody in the warp sees, and which not everybody: the former are left out.
-                    unsigned none = 0u;
-                    if (__any_sync(0xffffffffu, w.lo > key0 || w.hi < key0 + CT_KEYS) || have != (1 << CT_PAGES) - 1) {
+                    if (edge) {
 #pragma unroll
                         for (int c = 0; c < 4; c++) {
-                            const int from = w.lo - key0 - c * 32, to = ((have >> c) & 1) ? w.hi - key0 - c * 32 : 0;
-                            if (__all_sync(0xffffffffu, from >= 32 || to <= 0 || from >= to)) {
-                                none |= 1u << c;
+                            if (__all_sync(0xffffffffu, win[c] == ~0u)) continue;
+                            if (__all_sync(0xffffffffu, win[c] == 0u)) none |= 1u << c;
 #pragma unroll
-                                for (int e = 0; e < 32; e++) x[c][e] = 0xff800000u;
-                            }
-                            else if (__any_sync(0xffffffffu, from > 0 || to < 32)) {
-                                const int y = min(to, 32), z = max(from, 0);
-                                const unsigned win = z >= y ? 0u : (y == 32 ? ~0u : (1u << y) - 1u) & ~((1u << z) - 1u);
-#pragma unroll
-                                for (int e = 0; e < 32; e++) if (!((win >> e) & 1u)) x[c][e] = 0xff800000u;
-                            }
+                            for (int e = 0; e < 32; e++) if (!((win[c] >> e) & 1u)) x[c][e] = 0xff800000u;
                         }
                     }
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -627,6 +634,46 @@ __global__ void __launch_bounds__(CT_ROWS) k_chunk_merge(const TreeArgs a) {
     if (a.lse && blockIdx.y == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * CT_LN2;
 }
 
+// ---------------------------------------------------------------------------------- FP8 rows as bf16
+//
+// Every tile of a sequence reads the same rows, and what turns a stage into bf16 inside the kernel competes with its softmax for the same
+// pipes: 4096 tokens over 16384 rows, 8 KV heads, take 1330 us that way, 826 as bf16 rows.  So from three tiles per sequence on (two would break
+// even) the stages that any tile needs are turned once, into the workspace, in the order of the page table.  Block (x = stage, y = KV head, z = sequence).
+constexpr int CW_THREADS = 256;
+
+template <int HD>
+__global__ void __launch_bounds__(CW_THREADS) k_chunk_widen(const TreeArgs a, const ChunkPlan p, uint4* k_out, uint4* v_out) {
+    constexpr int CPR = HD / 16, RPP = CW_THREADS / CPR, NP = CT_KEYS / RPP;               // 16-byte chunks of a row, rows and passes
+    const int stage = blockIdx.x, h = blockIdx.y, seq = blockIdx.z, tid = threadIdx.x, chunk = tid % CPR, row0 = tid / CPR;
+    pdl_wait();
+    pdl_trigger();
+    bool need = false;
+    for (int i = p.first[seq] + tid; i < p.first[seq + 1]; i += CW_THREADS) { const ChunkTile& t = p.tiles[i]; need |= t.from <= stage && stage < t.from + t.stages && stage * CT_KEYS < t.n; }
+    if (!__syncthreads_or(need)) return;
+    uint4 raw[2][NP];
+    int ex[2][NP];
+    size_t to[NP];
+    bool there[NP];
+#pragma unroll
+    for (int i = 0; i < NP; i++) {
+        const int row = i * RPP + row0, column = stage * CT_PAGES + row / PAGE, page = column < a.pages_per_seq ? chunk_page(a, seq, column) : -1;
+        there[i] = page >= 0;
+        const size_t r = ((size_t)(there[i] ? page : 0) * a.Hk + h) * PAGE + row % PAGE;
+        to[i] = (((size_t)seq * a.pages_per_seq + column) * a.Hk + h) * PAGE + row % PAGE;
+        raw[0][i] = __ldg(reinterpret_cast<const uint4*>(a.kpool + r * HD) + chunk); ex[0][i] = __ldg(a.kexp + r);
+        raw[1][i] = __ldg(reinterpret_cast<const uint4*>(a.vpool + r * HD) + chunk); ex[1][i] = __ldg(a.vexp + r);
+    }
+#pragma unroll
+    for (int kv = 0; kv < 2; kv++)
+#pragma unroll
+        for (int i = 0; i < NP; i++) {
+            unsigned o[8];
+            widen16(raw[kv][i], ex[kv][i], o);
+            uint4* out = (kv ? v_out : k_out) + to[i] * (HD / 8) + 2 * chunk;
+            if (there[i]) { out[0] = make_uint4(o[0], o[1], o[2], o[3]); out[1] = make_uint4(o[4], o[5], o[6], o[7]); }
+        }
+}
+
 // ---------------------------------------------------------------------------------- host side
 
 // q [tokens][heads][HD]: a box is 64 elements of a group's heads of a stream's tokens.
@@ -652,8 +699,6 @@ static int chunk_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, 
         return cudaFuncGetAttributes(&f, k_chunk_tc<HD, F8, MODE>) == cudaSuccess ? f.numRegs : 0;
     }();
     if (regs * (C::threads / 128) < 2 * C::regs_softmax + C::regs_rest + (F8 ? C::regs_convert : 0)) return DYNAKV_ERR_CUDA;
-    const int rc = chunk_plan_launch(a, plan, sms, tile_tokens(a.G), CT_KEYS, st);
-    if (rc != DYNAKV_OK) return rc;
     if (launch_pdl(k_chunk_tc<HD, F8, MODE>, dim3(sms), dim3(C::threads), C::smem, st, mq, mk, mv, a, plan) != cudaSuccess) return DYNAKV_ERR_CUDA;
     return launch_pdl(k_chunk_merge<HD>, dim3(sms, HD / 16), dim3(CT_ROWS), 0, st, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
@@ -668,8 +713,23 @@ static int chunk_tc_launch_hd(const dynakv_row_cache* cache, const TreeArgs& a, 
     return cache->kv_dtype == DYNAKV_FP8 ? chunk_tc_launch_mode<HD, true>(cache, a, plan, sms, st) : chunk_tc_launch_mode<HD, false>(cache, a, plan, sms, st);
 }
 
-int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
-    return cache->head_dim == 128 ? chunk_tc_launch_hd<128>(cache, a, plan, sms, st) : chunk_tc_launch_hd<64>(cache, a, plan, sms, st);
+int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, void* wide, int sms, cudaStream_t st) {
+    const int rc = chunk_plan_launch(a, plan, sms, tile_tokens(a.G), CT_KEYS, st);
+    if (rc != DYNAKV_OK) return rc;
+    if (!wide) return cache->head_dim == 128 ? chunk_tc_launch_hd<128>(cache, a, plan, sms, st) : chunk_tc_launch_hd<64>(cache, a, plan, sms, st);
+    // FP8 rows turned into bf16 once, then the kernel of bf16 rows
+    dynakv_row_cache c = *cache;
+    c.n_pages = (int64_t)a.n_seqs * a.pages_per_seq;
+    c.k = wide; c.v = reinterpret_cast<char*>(wide) + chunk_wide_bytes(cache, a.n_seqs, a.pages_per_seq) / 2;
+    c.k_exp = c.v_exp = nullptr; c.kv_dtype = DYNAKV_BF16;
+    const dim3 grid((a.pages_per_seq + CT_PAGES - 1) / CT_PAGES, a.Hk, a.n_seqs);
+    const cudaError_t e = cache->head_dim == 128 ? launch_pdl(k_chunk_widen<128>, grid, dim3(CW_THREADS), 0, st, a, plan, reinterpret_cast<uint4*>(c.k), reinterpret_cast<uint4*>(c.v))
+                                                 : launch_pdl(k_chunk_widen<64>, grid, dim3(CW_THREADS), 0, st, a, plan, reinterpret_cast<uint4*>(c.k), reinterpret_cast<uint4*>(c.v));
+    if (e != cudaSuccess) return DYNAKV_ERR_CUDA;
+    TreeArgs w = a;
+    w.kpool = reinterpret_cast<const unsigned char*>(c.k); w.vpool = reinterpret_cast<const unsigned char*>(c.v);
+    w.kexp = w.vexp = nullptr; w.widened = 1;
+    return c.head_dim == 128 ? chunk_tc_launch_hd<128>(&c, w, plan, sms, st) : chunk_tc_launch_hd<64>(&c, w, plan, sms, st);
 }
 
 }  // namespace dkv

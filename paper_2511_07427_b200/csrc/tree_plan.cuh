@@ -41,6 +41,7 @@ struct TreeArgs {
     const float* slopes;                   // [Hq] lowers a logit by slope * distance, may be NULL
     float cap;                             // > 0: logits become cap * tanh(logit / cap)
     int window;                            // > 0: the last so many rows up to its own
+    int widened;                           // 1: kpool, vpool are the pages of page_table in order, as bf16
 };
 enum { DESC_VALID = 0, DESC_FIRST = 1, DESC_Q0 = 2, DESC_T = 3, DESC_H = 4, DESC_RT = 5 };
 
@@ -53,6 +54,12 @@ __device__ __forceinline__ void chunk_sees(const TreeArgs& a, int token, int pla
     lo = a.rows_from ? a.rows_from[token] : 0;
     if (a.window > 0) lo = max(lo, place + 1 - a.window);
     hi = min(a.rows_to ? a.rows_to[token] : place + 1, n);
+}
+
+// The page of a sequence's column: its place in the pool, -1 where the table names none.
+__device__ __forceinline__ int chunk_page(const TreeArgs& a, int seq, int column) {
+    const int id = a.page_table[(size_t)seq * a.pages_per_seq + column];
+    return id < 0 || id >= a.n_pages ? -1 : a.widened ? seq * a.pages_per_seq + column : id;
 }
 
 struct SeqInfo {

@@ -47,7 +47,7 @@ SIGNATURES = {
 SIGNATURES["dynakv_attend_tree"] = (C.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, C.c_float, _vp, _vp, _vp, _i64, _vp, _vp])
 SIGNATURES["dynakv_attend_tree_workspace"] = (_i64, [_vp, _i32, _i32])
 SIGNATURES["dynakv_attend_chunk"] = (C.c_int, [_vp, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp])
-SIGNATURES["dynakv_attend_chunk_workspace"] = (_i64, [_vp, _i32, _i64, _i32, _i32])
+SIGNATURES["dynakv_attend_chunk_workspace"] = (_i64, [_vp, _i32, _i64, _i32, _i32, _i32])
 SIGNATURES["dynakv_rows_keep"] = (C.c_int, [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp])
 SIGNATURES["dynakv_pages_extend"] = (C.c_int, [_vp, _vp, _i32, _vp, _vp, _i32, _i64, _vp, _vp, _vp, _vp, _vp])
 SIGNATURES["dynakv_pages_trim"] = (C.c_int, [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp])
@@ -389,9 +389,9 @@ class RowCache:
         zeros and -inf."""
         E, device = _env_made or _env(), self._device
         n, heads, b, per = self._queries(E, q, page_table, out, lse)
-        size = self._workspace.get((heads, max_chunk, n, b))
+        size = self._workspace.get((heads, max_chunk, n, b, per))
         if size is None:
-            size = self._chunk_workspace_bytes(E, heads, max_chunk, n, b)
+            size = self._chunk_workspace_bytes(E, heads, max_chunk, n, b, per)
         if scale is None:
             scale = self._scale
         if not (math.isfinite(scale) and 0.0 <= softcap < math.inf and 0 <= window < 1 << 31):
@@ -445,18 +445,18 @@ class RowCache:
             raise DynaKVError("lse shares memory with q or out")
         return out, lse
 
-    def _chunk_workspace_bytes(self, E, heads: int, max_chunk: int, n: int, b: int) -> int:
+    def _chunk_workspace_bytes(self, E, heads: int, max_chunk: int, n: int, b: int, per: int) -> int:
         if heads == 0 or heads % self.n_kv_heads != 0 or heads // self.n_kv_heads > 8:
             raise DynaKVError(f"{heads} query heads over {self.n_kv_heads} KV heads: expected 1 to 8 per KV head")
         if not 1 <= max_chunk <= MAX_CHUNK:
             raise DynaKVError(f"max_chunk is {max_chunk}: expected 1 to {MAX_CHUNK}")
         with E.torch.cuda.device(self._device):
-            size = E.dynakv_attend_chunk_workspace(self._ref, heads, n, b, max_chunk)
+            size = E.dynakv_attend_chunk_workspace(self._ref, heads, n, b, max_chunk, per)
         if size < 0:
             raise DynaKVError(f"dynakv_attend_chunk_workspace returned {size}")
         if len(self._workspace) >= 4096:       # lengths of prompts differ without end
             self._workspace.clear()
-        self._workspace[heads, max_chunk, n, b] = size
+        self._workspace[heads, max_chunk, n, b, per] = size
         return size
 
     def _workspace_bytes(self, E, heads: int, max_tree: int) -> int:

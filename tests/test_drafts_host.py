@@ -37,10 +37,10 @@ def test_attend_chunk_refuses_bad_arguments(bad):
 def test_attend_chunk_without_tokens_or_sequences_needs_nothing():
     assert _chunk(n_tokens=0, q=None, out=None, space=None) == 0
     assert _chunk(n_seqs=0, q=None, out=None, space=None) == 0
-    for bad in (dict(n_heads=5), dict(max_chunk=0), dict(n_tokens=-1), dict(n_seqs=-1)):
-        a = dict(n_heads=4, n_tokens=3, n_seqs=1, max_chunk=3)
+    for bad in (dict(n_heads=5), dict(max_chunk=0), dict(n_tokens=-1), dict(n_seqs=-1), dict(per=-1)):
+        a = dict(n_heads=4, n_tokens=3, n_seqs=1, max_chunk=3, per=2)
         a.update(bad)
-        assert R._library().dynakv_attend_chunk_workspace(C.byref(_cache()), a["n_heads"], a["n_tokens"], a["n_seqs"], a["max_chunk"]) == -1
+        assert R._library().dynakv_attend_chunk_workspace(C.byref(_cache()), a["n_heads"], a["n_tokens"], a["n_seqs"], a["max_chunk"], a["per"]) == -1
 
 
 def _pool(**kw):
