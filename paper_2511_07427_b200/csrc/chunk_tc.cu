@@ -94,27 +94,42 @@ __device__ __forceinline__ void widen16(uint4 raw, int e, unsigned (&o)[8]) {
 }
 // What the scores need beside the factor and the mask.
 enum { PLAIN = 0, BIASED = 1, CAPPED = 2 };
-// tanh(y) / y as a polynomial of y^2 (interpolated at Chebyshev nodes; tanh is off by 9e-8 at most), two at a time: for |y| <= 0.4, which
-// is what a cap well above the logits gives, and for |y| <= 1.  The FMA pipe is what this costs: 5 and 9 instructions' worth per logit.
+// tanh(y) / y as a polynomial of y^2 (interpolated at Chebyshev nodes; tanh is off by 1e-7 at most): for |y| <= 0.4, which is what a cap well above
+// the logits gives, and for |y| <= 1.  The FMA pipe is what this costs, 5 and 9 instructions' worth per logit.  N pairs step by step: one after
+// the other they would wait for their own results.
 constexpr float CT_TANH_SHORT = 0.4f, CT_TANH_LONG = 1.f;
-template <bool SHORT>
-__device__ __forceinline__ float2 tanh_near2(float2 y) {
-    const float2 z = mul2(y, y);
-    auto c = [](float x) { return make_float2(x, x); };
-    float2 p;
-    if constexpr (SHORT) {
-        p = fma2(c(-0.0475610755f), z, c(0.1327115595f));
-        p = fma2(p, z, c(-0.3333137333f));
-    } else {
-        p = fma2(c(-0.0003548834f), z, c(0.0022876456f));
-        p = fma2(p, z, c(-0.0079249460f));
-        p = fma2(p, z, c(0.0214699805f));
-        p = fma2(p, z, c(-0.0538727380f));
-        p = fma2(p, z, c(0.1333219111f));
-        p = fma2(p, z, c(-0.3333328068f));
-    }
-    p = fma2(p, z, c(1.f));
-    return mul2(p, y);
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+struct TanhShort { float k0, k1, k2, k3; };                    // x (k0 + k1 x^2 + k2 x^4 + k3 x^6) = f tanh(x s)
+__device__ __forceinline__ TanhShort tanh_short(float s, float f) {
+    const float z = s * s, k = s * f;
+    return {k, -0.3333137333f * z * k, 0.1327115595f * (z * z) * k, -0.0475610755f * (z * z) * (z * k)};
+}
+template <int N>
+__device__ __forceinline__ void tanh_short2(float2 (&x)[N], const TanhShort& k) {
+    float2 z[N], p[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) z[i] = mul2(x[i], x[i]);
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma2(both(k.k3), z[i], both(k.k2));
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma2(p[i], z[i], both(k.k1));
+#pragma unroll
+    for (int i = 0; i < N; i++) p[i] = fma2(p[i], z[i], both(k.k0));
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = mul2(p[i], x[i]);
+}
+template <int N>
+__device__ __forceinline__ void tanh_long2(float2 (&x)[N], float s) {
+    constexpr float c[8] = {1.f, -0.3333328068f, 0.1333219111f, -0.0538727380f, 0.0214699805f, -0.0079249460f, 0.0022876456f, -0.0003548834f};
+    float2 z[N], p[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) { x[i] = mul2(x[i], both(s)); z[i] = mul2(x[i], x[i]); p[i] = both(c[7]); }
+#pragma unroll
+    for (int k = 6; k >= 0; k--)
+#pragma unroll
+        for (int i = 0; i < N; i++) p[i] = fma2(p[i], z[i], both(c[k]));
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = mul2(p[i], x[i]);
 }
 // tanh(y) = 1 - 2 / (1 + e^2y) for any y: off by 2e-7 at most.
 __device__ __forceinline__ float tanh_far(float y) { return fmaf(-2.f, __fdividef(1.f, 1.f + ex2(2.f * CT_LOG2E * (y > 40.f ? 40.f : y))), 1.f); }
@@ -376,6 +391,8 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
         const unsigned tS = tmem + s * 128 + lane_base, tO = tmem + 256 + s * 128 + lane_base;
         const int step = tokens / 2, my_token = row / a.G + s * step, my_head = row % a.G;          // token of the tile
         const float qs = a.scale * (MODE == CAPPED ? 1.f / a.cap : CT_LOG2E);                      // PLAIN: positive
+        const float top = a.cap * CT_LOG2E, short_range = fabsf(qs) > 1e-6f ? CT_TANH_SHORT / fabsf(qs) : 0.f;     // below that the powers leave fp32's range
+        const TanhShort k_short = tanh_short(qs, top);
         const bool wide = ((uintptr_t)a.out & 31) == 0;
         int n = 0, u = 0, seg = 0;
         bool dead = false, cut_end = false;
@@ -433,31 +450,48 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                         float hi = 0.f;
 #pragma unroll
                         for (int e = 0; e < CT_KEYS; e += 2) hi = tt_max3(hi, fabsf(__uint_as_float(x[e >> 5][e & 31])), fabsf(__uint_as_float(x[e >> 5][(e & 31) + 1])));
-                        const float2 qs2 = make_float2(qs, qs);
-                        hi = t < 0 ? 0.f : hi * fabsf(qs);
-                        auto near = [&](auto is_short) {
+                        hi = t < 0 ? 0.f : hi;                 // nor have rows that do not exist
+                        auto groups = [&](auto work) {
+                            constexpr int N = 8;
 #pragma unroll
-                            for (int e = 0; e < CT_KEYS; e += 2) {
-                                const float2 y = tanh_near2<decltype(is_short)::value>(mul2(make_float2(__uint_as_float(x[e >> 5][e & 31]), __uint_as_float(x[e >> 5][(e & 31) + 1])), qs2));
-                                x[e >> 5][e & 31] = __float_as_uint(y.x); x[e >> 5][(e & 31) + 1] = __float_as_uint(y.y);
+                            for (int b = 0; b < CT_KEYS; b += 2 * N) {
+                                float2 y[N];
+#pragma unroll
+                                for (int e = 0; e < N; e++) y[e] = make_float2(__uint_as_float(x[(b + 2 * e) >> 5][(b + 2 * e) & 31]), __uint_as_float(x[(b + 2 * e) >> 5][(b + 2 * e + 1) & 31]));
+                                work(y);
+#pragma unroll
+                                for (int e = 0; e < N; e++) { x[(b + 2 * e) >> 5][(b + 2 * e) & 31] = __float_as_uint(y[e].x); x[(b + 2 * e) >> 5][(b + 2 * e + 1) & 31] = __float_as_uint(y[e].y); }
                             }
                         };
-                        if (__all_sync(0xffffffffu, hi <= CT_TANH_SHORT)) near(std::true_type());
-                        else if (__all_sync(0xffffffffu, hi <= CT_TANH_LONG)) near(std::false_type());
+                        f = 1.f;
+                        if (__all_sync(0xffffffffu, hi <= short_range)) groups([&](float2 (&y)[8]) { tanh_short2(y, k_short); });
                         else {
+                            f = top;
+                            if (__all_sync(0xffffffffu, hi * fabsf(qs) <= CT_TANH_LONG)) groups([&](float2 (&y)[8]) { tanh_long2(y, qs); });
+                            else {
 #pragma unroll
-                            for (int e = 0; e < CT_KEYS; e++) x[e >> 5][e & 31] = __float_as_uint(tanh_far(__uint_as_float(x[e >> 5][e & 31]) * qs));
+                                for (int e = 0; e < CT_KEYS; e++) x[e >> 5][e & 31] = __float_as_uint(tanh_far(__uint_as_float(x[e >> 5][e & 31]) * qs));
+                            }
                         }
-                        f = a.cap * CT_LOG2E;
                     }
                     if (MODE == BIASED || (MODE == CAPPED && a.slopes)) {
-                        const float2 f2 = make_float2(f, f);
+                        const float2 f2 = both(f);
                         if (__all_sync(0xffffffffu, w.place >= key0 + CT_KEYS - 1)) {              // the distance falls from row to row
-                            const float2 base = make_float2(w.slope * (float)(key0 - w.place), w.slope * (float)(key0 - w.place)), sl = make_float2(w.slope, w.slope);
+                            // a base for every 8 rows, and what the rows inside them add
+                            float2 more[4];
 #pragma unroll
-                            for (int e = 0; e < CT_KEYS; e += 2) {
-                                const float2 y = fma2(make_float2(__uint_as_float(x[e >> 5][e & 31]), __uint_as_float(x[e >> 5][(e & 31) + 1])), f2, fma2(sl, make_float2((float)e, (float)(e + 1)), base));
-                                x[e >> 5][e & 31] = __float_as_uint(y.x); x[e >> 5][(e & 31) + 1] = __float_as_uint(y.y);
+                            for (int e = 0; e < 4; e++) more[e] = make_float2(w.slope * (float)(2 * e), w.slope * (float)(2 * e + 1));
+#pragma unroll
+                            for (int b = 0; b < CT_KEYS; b += 8) {
+                                const float base = w.slope * (float)(key0 + b - w.place);
+                                const float2 base2 = both(base);
+#pragma unroll
+                                for (int e = 0; e < 4; e++) {
+                                    unsigned& lo = x[b >> 5][(b & 31) + 2 * e];
+                                    unsigned& hi = x[b >> 5][(b & 31) + 2 * e + 1];
+                                    const float2 y = fma2(make_float2(__uint_as_float(lo), __uint_as_float(hi)), f2, add2(base2, more[e]));
+                                    lo = __float_as_uint(y.x); hi = __float_as_uint(y.y);
+                                }
                             }
                         } else {
 #pragma unroll
@@ -496,7 +530,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                         }
                     }
                     const float ref = m == -INFINITY ? 0.f : m;
-                    const float2 f2 = make_float2(f, f), ref2 = make_float2(-ref, -ref);
+                    const float2 f2 = both(f), ref2 = make_float2(-ref, -ref);
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     auto weights = [&](int c) {
                         unsigned p[16];
