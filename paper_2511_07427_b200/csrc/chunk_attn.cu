@@ -18,14 +18,16 @@ static int chunk_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& m
     return rg == 0 ? chunk_launch<HD, DT, 0>(mk, mv, a, sms, st) : rg == 1 ? chunk_launch<HD, DT, 1>(mk, mv, a, sms, st) : rg == 2 ? chunk_launch<HD, DT, 2>(mk, mv, a, sms, st) : chunk_launch<HD, DT, 4>(mk, mv, a, sms, st);
 }
 
-#ifndef DKV_CHUNK_TC_BF16
-#define DKV_CHUNK_TC_BF16 33
-#endif
-#ifndef DKV_CHUNK_TC_FP8
-#define DKV_CHUNK_TC_FP8 65
-#endif
-#ifndef DKV_CHUNK_F32
-#define DKV_CHUNK_F32 65
+// From so many query rows per KV head on the kernels for many rows pay (rows of 128 elements, of 64).  In us, 8 KV heads, the kernel for few
+// rows / tcgen05 (bf16, FP8) or the 128-row tiles (fp32):
+//                             bf16: 32 rows  40 rows   64 rows   128 rows | FP8: 32 rows  40 rows   64 rows  128 rows | fp32: 32 rows   64 rows   128 rows
+//   4 x 16384 (fp32: 4096), d = 128  66 / 70  104 / 70  105 / 71  183 / 72 |    69 / 87  112 / 87  113 / 88  197 / 89 |     151 / 191  230 / 192  401 / 195
+//   16 x 2048, d = 128               38 / 46   54 / 46   57 / 46   91 / 48 |    38 / 51   55 / 52   59 / 52   99 / 54 |     249 / 334  402 / 334  756 / 339
+//   1 x 1024, d = 128                20 / 22   20 / 22   21 / 22   20 / 23 |    20 / 23   21 / 24   23 / 24   22 / 24 |      37 / 49    41 / 50    62 / 52
+//   4 x 16384 (fp32: 4096), d = 64   40 / 61   64 / 61   65 / 61  112 / 62 |    43 / 71   70 / 71   72 / 71  126 / 72 |      76 / 112  112 / 112  190 / 114
+//   16 x 2048, d = 64                24 / 38   33 / 38   35 / 38   57 / 39 |    26 / 43   37 / 43   40 / 43   64 / 44 |     126 / 192  200 / 192  360 / 195
+#ifndef DKV_CHUNK_FEW
+#define DKV_CHUNK_FEW (c->head_dim == 128 ? 32 : 64)
 #endif
 // From three tiles per sequence on FP8 rows are turned into bf16 first (chunk_tc.cu), unless that takes more than CHUNK_WIDE bytes.
 constexpr size_t CHUNK_WIDE = (size_t)2 << 30;
@@ -33,7 +35,7 @@ struct ChunkKind { bool planned; int rg, rows, ctas, per; bool wide; };         
 static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int n_seqs, int max_chunk, int pages_per_seq, int sms) {
     const bool f32 = c->kv_dtype == DYNAKV_F32;
     const int most = (int)min(1000ll, (long long)max_chunk * (n_heads / c->n_kv_heads));
-    if (most >= (f32 ? DKV_CHUNK_F32 : c->kv_dtype == DYNAKV_FP8 ? DKV_CHUNK_TC_FP8 : DKV_CHUNK_TC_BF16)) {
+    if (most > DKV_CHUNK_FEW) {
         const int G = n_heads / c->n_kv_heads;
         return {true, 0, f32 ? CF_ROWS : CT_ROWS, sms, f32 ? CF_ROWS / G : tile_tokens(G),
                 c->kv_dtype == DYNAKV_FP8 && max_chunk > 2 * tile_tokens(G) && n_seqs <= 65535 && c->n_kv_heads <= 65535 && chunk_wide_bytes(c, n_seqs, pages_per_seq) <= CHUNK_WIDE};

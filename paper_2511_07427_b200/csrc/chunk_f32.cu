@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __
 #pragma unroll
                 for (int j = 0; j < 4; j++) s[i][j] = make_float2(0.f, 0.f);
             if (!dead) {
-#pragma unroll 2
+#pragma unroll 4
                 for (int c = 0; c < HD / 4; c++) {
                     uint4 k[4];
 #pragma unroll
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __
                 __syncwarp();
             }
             if (!dead) {
-#pragma unroll 2
+#pragma unroll 4
                 for (int k2 = 0; k2 < CF_KEYS / 2; k2++) {
                     uint4 v[2][C::cols];
 #pragma unroll

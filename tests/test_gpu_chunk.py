@@ -92,8 +92,8 @@ class Chunk:
     def check(self, out, lse, scale=None, softcap=0.0, window=0):
         scale = scale if scale is not None else self.d ** -0.5
         group, half = self.heads // self.hk, torch.finfo(out.dtype).eps / 2
-        many = self.most * group
-        grain = {"f32": 0.0, "bf16": 2.0 ** -8 if many > 32 else 2.0 ** -16, "fp8": 2.0 ** -8 if many > 64 else 2.0 ** -11}[self.cache]
+        many = self.most * group > (32 if self.d == 128 else 64)             # the tcgen05 kernel's, with weights in bf16
+        grain = {"f32": 0.0, "bf16": 2.0 ** -8 if many else 2.0 ** -16, "fp8": 2.0 ** -8 if many else 2.0 ** -11}[self.cache]
         at = self.lead
         for b, (n, t) in enumerate(zip(self.lens, self.new)):
             place = self.place[at:at + t]
