@@ -475,7 +475,7 @@ int dynakv_rows_read(const dynakv_row_cache* cache, const int32_t* page_table, i
  * q, out: [n_tokens][n_heads][head_dim], contiguous and 16-byte aligned, fp32 for a DYNAKV_F32 cache, else bf16;
  * lse: [n_tokens][n_heads] fp32, may be NULL.  Tokens of no sequence, before q_start[0] or from q_start[n_seqs] on, are left as they were
  * in both.  n_heads is 1 to 8 times n_kv_heads;
- * max_tree 1 .. 256 (a prompt attends in chunks of at most so many tokens, each of which reads all rows before it); tree_mask [n_tokens][mask_words], mask_words 1 .. 4 (rows past the last word are not seen).
+ * max_tree 1 .. 256 (prompts: dynakv_attend_chunk); tree_mask [n_tokens][mask_words], mask_words 1 .. 4 (rows past the last word are not seen).
  * Logits, weights' sums and outputs are accumulated in fp32.  Weights enter the products with V in fp32 (DYNAKV_F32), to 2^-17
  * (DYNAKV_BF16, and DYNAKV_FP8 with more than 64 query rows, max_tree * n_heads / n_kv_heads, per KV head) or, DYNAKV_FP8 with up
  * to 64 query rows, as f16: p_j * 2^exp_j is off by 2^-12 of itself down to 2^-26 of the token's largest, below that by 2^-37 of
@@ -514,7 +514,8 @@ typedef struct dynakv_scores {
  *     out[i][hq] = sum_j p_j v_j / sum_j p_j,  lse[i][hq] = ln sum_j p_j,  p_j = exp(s_j)
  * over the rows that the token sees; one that sees none gets zeros and -infinity.  Rows it does not see do not count whatever they
  * hold, NaN and infinities included (values that are no numbers among the V rows that are read make the call slow).  Logits, sums and
- * outputs are accumulated in fp32.
+ * outputs are accumulated in fp32.  Weights enter the products with V in fp32 (DYNAKV_F32); with more than 32 query rows per KV head (max_chunk *
+ * n_heads / n_kv_heads; head_dim 64: 64) as bf16, each off by 2^-8 of itself at most; with fewer as for dynakv_attend_tree.
  * n_heads is 1 to 8 times n_kv_heads; max_chunk 1 .. 2^24.  Tokens of no sequence are left as they were.
  * workspace: dynakv_attend_chunk_workspace() bytes of device memory, 16-byte aligned, contents of no interest before and after;
  * calls that may overlap need one each. */

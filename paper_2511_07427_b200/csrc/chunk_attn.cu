@@ -15,7 +15,8 @@ static int chunk_launch(const CUtensorMap& mk, const CUtensorMap& mv, const Tree
 }
 template <int HD, int DT>
 static int chunk_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& a, int sms, cudaStream_t st) {
-    return rg == 0 ? chunk_launch<HD, DT, 0>(mk, mv, a, sms, st) : rg == 1 ? chunk_launch<HD, DT, 1>(mk, mv, a, sms, st) : rg == 2 ? chunk_launch<HD, DT, 2>(mk, mv, a, sms, st) : chunk_launch<HD, DT, 4>(mk, mv, a, sms, st);
+    if constexpr (HD == 64) { if (rg == 4) return chunk_launch<HD, DT, 4>(mk, mv, a, sms, st); }     // rows of 128: 32 at most come here
+    return rg == 0 ? chunk_launch<HD, DT, 0>(mk, mv, a, sms, st) : rg == 1 ? chunk_launch<HD, DT, 1>(mk, mv, a, sms, st) : chunk_launch<HD, DT, 2>(mk, mv, a, sms, st);
 }
 
 // From so many query rows per KV head on the kernels for many rows pay (rows of 128 elements, of 64).  In us, 8 KV heads, the kernel for few
@@ -26,16 +27,14 @@ static int chunk_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& m
 //   1 x 1024, d = 128                20 / 22   20 / 22   21 / 22   20 / 23 |    20 / 23   21 / 24   23 / 24   22 / 24 |      37 / 49    41 / 50    62 / 52
 //   4 x 16384 (fp32: 4096), d = 64   40 / 61   64 / 61   65 / 61  112 / 62 |    43 / 71   70 / 71   72 / 71  126 / 72 |      76 / 112  112 / 112  190 / 114
 //   16 x 2048, d = 64                24 / 38   33 / 38   35 / 38   57 / 39 |    26 / 43   37 / 43   40 / 43   64 / 44 |     126 / 192  200 / 192  360 / 195
-#ifndef DKV_CHUNK_FEW
-#define DKV_CHUNK_FEW (c->head_dim == 128 ? 32 : 64)
-#endif
+static int chunk_few(const dynakv_row_cache* c) { return c->head_dim == 128 ? 32 : 64; }
 // From three tiles per sequence on FP8 rows are turned into bf16 first (chunk_tc.cu), unless that takes more than CHUNK_WIDE bytes.
 constexpr size_t CHUNK_WIDE = (size_t)2 << 30;
 struct ChunkKind { bool planned; int rg, rows, ctas, per; bool wide; };             // per: tokens of a planned tile
 static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int n_seqs, int max_chunk, int pages_per_seq, int sms) {
     const bool f32 = c->kv_dtype == DYNAKV_F32;
     const int most = (int)min(1000ll, (long long)max_chunk * (n_heads / c->n_kv_heads));
-    if (most > DKV_CHUNK_FEW) {
+    if (most > chunk_few(c)) {
         const int G = n_heads / c->n_kv_heads;
         return {true, 0, f32 ? CF_ROWS : CT_ROWS, sms, f32 ? CF_ROWS / G : tile_tokens(G),
                 c->kv_dtype == DYNAKV_FP8 && max_chunk > 2 * tile_tokens(G) && n_seqs <= 65535 && c->n_kv_heads <= 65535 && chunk_wide_bytes(c, n_seqs, pages_per_seq) <= CHUNK_WIDE};

