@@ -499,7 +499,7 @@ int64_t dynakv_attend_tree_workspace(const dynakv_row_cache* cache, int32_t n_he
  *     mask; rows_to = max(P + 1, prefix length) a prefix that all of it sees. */
 typedef struct dynakv_scores {
     float scale;
-    float softcap;                 /* >= 0, 0: none */
+    float softcap;                 /* 2^-100 .. 2^100, scale / softcap finite; 0: none */
     int32_t window;                /* >= 0, 0: none */
     const float* slopes;
     const int32_t* rows_from;
@@ -574,7 +574,7 @@ int dynakv_pages_trim(const dynakv_page_pool* pool, int32_t* page_table, int32_t
  *
  * kept [n_seqs]: tokens of the accepted path, the root included; dropped [n_seqs]: the others; path [n_seqs][max_tree]: the places in the
  * tree of the kept ones, upward from 0, then -1; next_token [n_seqs], -1 where no token has a weight.  A sequence without tokens gets 0, 0, -1, -1, one whose range
- * is none of n_tokens or longer than max_tree 0, -1, -1, -1.  A token outside the vocabulary is never accepted.  n_tokens < 2^24, n_seqs <= 65535.
+ * is none of n_tokens or longer than max_tree 0, -1, -1, -1.  A token outside the vocabulary is never accepted.  n_tokens < 2^24, n_seqs <= 65535, vocab <= 2^26.
  * Acceptance is decided on sums of fp32 exponentials (relative error below 1e-6), the next token on 64-bit sums.
  * workspace: dynakv_verify_drafts_workspace() bytes, 16-byte aligned; calls that may overlap need one each. */
 int dynakv_verify_drafts(const void* logits, int64_t logits_stride, int32_t logits_dtype, int64_t n_tokens, int32_t vocab, const int32_t* tokens,

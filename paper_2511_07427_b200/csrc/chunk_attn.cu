@@ -81,7 +81,9 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
                                    const dynakv_scores* scores, void* out, float* lse, void* workspace, int64_t workspace_bytes,
                                    uint32_t* status, void* cuda_stream) {
     if (!chunk_shape_ok(cache, n_heads, n_tokens, n_seqs, max_chunk, pages_per_seq) || !scores ||
-        !(fabsf(scores->scale) <= FLT_MAX) || !(scores->softcap >= 0.f && scores->softcap <= FLT_MAX) || scores->window < 0) return DYNAKV_ERR_ARG;
+        !(fabsf(scores->scale) <= FLT_MAX) || scores->window < 0) return DYNAKV_ERR_ARG;
+    const float cap = scores->softcap;
+    if (cap != 0.f && !(cap >= 0x1p-100f && cap <= 0x1p100f && fabsf(scores->scale / cap) <= FLT_MAX)) return DYNAKV_ERR_ARG;
     if (n_tokens == 0 || n_seqs == 0) return DYNAKV_OK;
     if (!q || !q_start || (!page_table && pages_per_seq > 0) || !kv_len || !out || !workspace) return DYNAKV_ERR_ARG;
     if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)workspace) & 15) return DYNAKV_ERR_ARG;

@@ -537,7 +537,7 @@ static int verify_launch(const VerifyArgs& a, int sms, cudaStream_t st) {
 using namespace dkv;
 
 static bool verify_shape_ok(int32_t dtype, int64_t n_tokens, int32_t vocab, int32_t n_seqs, int32_t max_tree) {
-    return (dtype == DYNAKV_F32 || dtype == DYNAKV_BF16) && n_tokens >= 0 && n_tokens < (1ll << 24) && vocab >= 1 && vocab <= (1 << 28) && n_seqs >= 0 &&
+    return (dtype == DYNAKV_F32 || dtype == DYNAKV_BF16) && n_tokens >= 0 && n_tokens < (1ll << 24) && vocab >= 1 && vocab <= (1 << 26) && n_seqs >= 0 &&
            n_seqs <= 65535 && max_tree >= 1 && max_tree <= TREE_MAX;
 }
 

@@ -63,7 +63,7 @@ class PagePool:
         b, per, table, lens, add = self._tables(E, page_table, kv_len, new_len, "new_len")
         if not 0 <= n_tokens < 1 << 31:
             raise DynaKVError(f"n_tokens is {n_tokens}: expected 0 to 2^31 - 1")
-        q_start, positions, slots = (E.empty(n, dtype=E.i32, device=self.device) for n in (b + 1, n_tokens, n_tokens))
+        q_start, positions, slots = E.empty(b + 1, dtype=E.i32, device=self.device), E.empty(n_tokens, dtype=E.i32, device=self.device), E.empty(n_tokens, dtype=E.i32, device=self.device)
         _call(E, self._device, E.dynakv_pages_extend, self._ref, table, per, lens, add, b, n_tokens, q_start.data_ptr(), positions.data_ptr(), slots.data_ptr(),
               self._status_at)
         return q_start, positions, slots
@@ -119,8 +119,8 @@ def verify_drafts(logits, tokens, q_start, max_tree: int, uniform, temperature, 
     b = q_start.shape[0] - 1 if q_start.dim() == 1 else -1
     if b < 0:
         raise DynaKVError(f"expected q_start of sequences + 1 elements, got {tuple(q_start.shape)}")
-    if not 1 <= max_tree <= MAX_TREE or not 1 <= vocab <= 1 << 28 or n >= 1 << 24 or b > 65535:
-        raise DynaKVError(f"max_tree is {max_tree}, {n} tokens of a vocabulary of {vocab}, {b} sequences: expected 1 to {MAX_TREE}, fewer than 2^24, 1 to 2^28, at most 65535")
+    if not 1 <= max_tree <= MAX_TREE or not 1 <= vocab <= 1 << 26 or n >= 1 << 24 or b > 65535:
+        raise DynaKVError(f"max_tree is {max_tree}, {n} tokens of a vocabulary of {vocab}, {b} sequences: expected 1 to {MAX_TREE}, fewer than 2^24, 1 to 2^26, at most 65535")
     at = _matrix(E, logits, (n, vocab), device, (E.f32, E.bf16), "logits")
     if parent is not None and draft_probs is not None:
         raise DynaKVError("draft_probs goes with chains (parent=None): drafts of a tree are taken as looked up")
@@ -139,9 +139,9 @@ def verify_drafts(logits, tokens, q_start, max_tree: int, uniform, temperature, 
     words, start = _index(E, tokens, (n,), device, "tokens"), _index(E, q_start, (b + 1,), device, "q_start")
     above = _index(E, parent, (n,), device, "parent") if parent is not None else None
     chance, heat = _floats(E, uniform, (n,), device, "uniform"), _floats(E, temperature, (b,), device, "temperature")
-    kept, dropped, following = (E.empty(b, dtype=E.i32, device=where) for _ in range(3))
-    path, space = E.empty((b, max_tree), dtype=E.i32, device=where), E.empty(size, dtype=E.torch.uint8, device=where)
+    results, space = E.empty(b * (3 + max_tree), dtype=E.i32, device=where), E.empty(size, dtype=E.byte, device=where)      # an allocation costs more than a view
+    to = results.data_ptr()
     _call(E, device, E.dynakv_verify_drafts, at, logits.stride(0), code, n, vocab, words, start, b, max_tree, chance, heat, above,
-          draft, draft_probs.stride(0) if draft is not None else 0, kept.data_ptr(), dropped.data_ptr(), path.data_ptr(), following.data_ptr(),
-          space.data_ptr(), size)
-    return kept, dropped, path, following
+          draft, draft_probs.stride(0) if draft is not None else 0, to, to + 4 * b, to + 12 * b, to + 8 * b, space.data_ptr(), size)
+    kept, dropped, following, path = results.split_with_sizes((b, b, b, b * max_tree))
+    return kept, dropped, path.view(b, max_tree), following

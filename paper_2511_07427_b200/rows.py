@@ -67,7 +67,7 @@ class _Env:
             fn.restype, fn.argtypes = res, args
             setattr(self, name, fn)
         self.library, self.torch = L, torch
-        self.empty, self.i32, self.f32, self.bf16, self.i64 = torch.empty, torch.int32, torch.float32, torch.bfloat16, torch.int64
+        self.empty, self.i32, self.f32, self.bf16, self.i64, self.byte = torch.empty, torch.int32, torch.float32, torch.bfloat16, torch.int64, torch.uint8
         self.types = {torch.float32: F32, torch.bfloat16: BF16}
         self.grad = torch.is_grad_enabled
         stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -394,8 +394,9 @@ class RowCache:
             size = self._chunk_workspace_bytes(E, heads, max_chunk, n, b, per)
         if scale is None:
             scale = self._scale
-        if not (math.isfinite(scale) and 0.0 <= softcap < math.inf and 0 <= window < 1 << 31):
-            raise DynaKVError(f"scale is {scale}, softcap {softcap}, window {window}: expected finite numbers, softcap and window not negative")
+        if not (math.isfinite(scale) and (softcap == 0.0 or 2.0 ** -100 <= softcap <= 2.0 ** 100 and abs(scale / softcap) < 2.0 ** 127) and 0 <= window < 1 << 31):
+            raise DynaKVError(f"scale is {scale}, softcap {softcap}, window {window}: expected finite numbers, softcap 0 or 2^-100 to 2^100, scale / softcap below 2^127, "
+                              "window not negative")
         at_slopes = None
         if slopes is not None:
             if slopes.dtype is not E.f32 or slopes.shape != (heads,) or slopes.get_device() != device or not slopes.is_contiguous():

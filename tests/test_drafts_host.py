@@ -27,7 +27,7 @@ def _chunk(cache=None, q=ADDR, n_heads=4, n_tokens=3, q_start=ADDR, n_seqs=1, ma
 
 @pytest.mark.parametrize("bad", [dict(n_heads=0), dict(n_heads=3), dict(n_heads=18), dict(max_chunk=0), dict(max_chunk=(1 << 24) + 1), dict(n_tokens=-1), dict(n_tokens=1 << 31),
                                  dict(n_seqs=-1), dict(per=-1), dict(per=1 << 26), dict(scale=float("nan")), dict(scale=float("inf")), dict(softcap=-1.0),
-                                 dict(softcap=float("inf")), dict(softcap=float("nan")), dict(window=-1), dict(no_scores=True), dict(q=None), dict(q_start=None),
+                                 dict(softcap=float("inf")), dict(softcap=float("nan")), dict(softcap=1e-40), dict(softcap=1e38), dict(softcap=1e-10, scale=1e30), dict(window=-1), dict(no_scores=True), dict(q=None), dict(q_start=None),
                                  dict(table=None), dict(kv_len=None), dict(out=None), dict(space=None), dict(q=ADDR + 8), dict(out=ADDR + 2), dict(space=ADDR + 4),
                                  dict(cache=_cache(head_dim=32)), dict(cache=_cache(kv_dtype=P.FP8)), dict(cache=_cache(k=None))])
 def test_attend_chunk_refuses_bad_arguments(bad):
@@ -76,7 +76,7 @@ def _verify(**kw):
     return R._library().dynakv_verify_drafts(*a.values(), None)
 
 
-@pytest.mark.parametrize("bad", [dict(dtype=P.FP8), dict(dtype=7), dict(n=-1), dict(n=1 << 24), dict(vocab=0), dict(vocab=(1 << 28) + 1), dict(n_seqs=-1), dict(n_seqs=65536),
+@pytest.mark.parametrize("bad", [dict(dtype=P.FP8), dict(dtype=7), dict(n=-1), dict(n=1 << 24), dict(vocab=0), dict(vocab=(1 << 26) + 1), dict(n_seqs=-1), dict(n_seqs=65536),
                                  dict(most=0), dict(most=257), dict(parent=ADDR, draft=ADDR), dict(q_start=None), dict(heat=None), dict(kept=None), dict(dropped=None),
                                  dict(path=None), dict(following=None), dict(space=None), dict(space=ADDR + 8), dict(logits=None), dict(tokens=None), dict(uniform=None),
                                  dict(logits=ADDR + 2), dict(draft=ADDR + 2), dict(stride=-1), dict(draft=ADDR, draft_stride=-1)])

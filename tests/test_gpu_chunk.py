@@ -163,7 +163,7 @@ def test_windows(cache, new, window):
 
 @pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
 @pytest.mark.parametrize("new", [2, 200])
-@pytest.mark.parametrize("cap,size", [(50.0, 1.0), (30.0, 8.0), (1.0, 1.0), (0.25, 4.0), (1e4, 1.0)])
+@pytest.mark.parametrize("cap,size", [(50.0, 1.0), (30.0, 8.0), (1.0, 1.0), (0.25, 4.0), (1e4, 1.0), (2.0 ** 60, 1.0), (2.0 ** -60, 1.0)])
 def test_capped_scores(cache, new, cap, size):
     p = Chunk([513, 200], [new, 100 if new > 2 else 1], 8, 2, 128, cache, seed=5, size=size)
     p.check(*p.run(softcap=cap), softcap=cap)
@@ -446,7 +446,7 @@ def test_refusals():
     for bad in (dict(q=q.float()), dict(q=q[:, :, :64]), dict(q=q.transpose(0, 1)), dict(q=q.cpu()), dict(q=q[:, :7].contiguous()), dict(q=q[:, :0].contiguous()),
                 dict(page_table=table[0]), dict(page_table=table.long()), dict(kv_len=lens.long()), dict(kv_len=lens.cpu()), dict(q_start=start[:1]),
                 dict(max_chunk=0), dict(max_chunk=(1 << 24) + 1), dict(scale=math.nan), dict(scale=math.inf), dict(softcap=-1.0), dict(softcap=math.inf),
-                dict(softcap=math.nan), dict(window=-1), dict(window=1 << 31), dict(slopes=slopes[:7]), dict(slopes=slopes.double()), dict(slopes=slopes.cpu()),
+                dict(softcap=math.nan), dict(softcap=1e-40), dict(softcap=1e38), dict(softcap=1e-10, scale=1e30), dict(window=-1), dict(window=1 << 31), dict(slopes=slopes[:7]), dict(slopes=slopes.double()), dict(slopes=slopes.cpu()),
                 dict(slopes=torch.ones(16, device="cuda")[::2]), dict(rows_from=rows[:3]), dict(rows_to=rows.long()), dict(rows_from=rows.cpu()),
                 dict(out=q.float()), dict(out=q), dict(out=torch.empty_like(q)[:2]), dict(lse=torch.empty(4, 8, dtype=torch.bfloat16, device="cuda")),
                 dict(lse=torch.empty(4, 7, device="cuda"))):
