@@ -555,7 +555,7 @@ int dynakv_pages_extend(const dynakv_page_pool* pool, int32_t* page_table, int32
 
 /* The last drop[b] >= 0 rows of every sequence given up: kv_len[b] falls by as many, pages that hold no row any more return to the
  * pool and their entries become -1.  Dropping what the last call of dynakv_pages_extend added puts the pool back as it was.  What is out of
- * range (drop[b] > kv_len[b], a page id outside the pool) sets DYNAKV_ST_BOUNDS, more pages than the pool has places DYNAKV_ST_PAGE_POOL;
+ * range (drop[b] > kv_len[b], a page id outside the pool, which goes there as it is) sets DYNAKV_ST_BOUNDS, more pages than the pool has places DYNAKV_ST_PAGE_POOL;
  * sequences are treated as by dynakv_pages_extend. */
 int dynakv_pages_trim(const dynakv_page_pool* pool, int32_t* page_table, int32_t pages_per_seq, int32_t* kv_len, const int32_t* drop,
                       int32_t n_seqs, uint32_t* status, void* cuda_stream);
@@ -570,7 +570,8 @@ int dynakv_pages_trim(const dynakv_page_pool* pool, int32_t* page_table, int32_t
  * max(p - q, 0).  q is draft_probs[c] ([n_tokens][vocab] fp32, draft_stride elements from row to row), the distribution that x was drawn from, or
  * with draft_probs NULL all of it on x, which leaves p without x; draft_probs goes with chains only.  When no child is accepted (or there
  * is none) the next token is the first whose running sum of p exceeds uniform[root] * sum(p); where max(p - q, 0) is zero everywhere, p stays.
- * With uniform drawn from [0, 1) the kept tokens are distributed as the target's own.  temperature[b] <= 0: p is all on the first of the largest logits.
+ * With uniform drawn from [0, 1) the kept tokens are distributed as the target's own.  temperature[b] <= 0: p is all on the first of the largest logits.  Others
+ * are taken as within 2^-100 and 2^100.
  *
  * kept [n_seqs]: tokens of the accepted path, the root included; dropped [n_seqs]: the others; path [n_seqs][max_tree]: the places in the
  * tree of the kept ones, upward from 0, then -1; next_token [n_seqs], -1 where no token has a weight.  A sequence without tokens gets 0, 0, -1, -1, one whose range

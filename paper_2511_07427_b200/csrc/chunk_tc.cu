@@ -399,8 +399,11 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
         const unsigned tS = tmem + s * 128 + lane_base, tO = tmem + 256 + s * 128 + lane_base;
         const int step = tokens / 2, my_token = row / a.G + s * step, my_head = row % a.G;          // token of the tile
         const float qs = a.scale * (MODE == CAPPED ? 1.f / a.cap : CT_LOG2E);                      // PLAIN: positive
-        const float top = a.cap * CT_LOG2E, short_range = fabsf(qs) > 1e-6f ? CT_TANH_SHORT / fabsf(qs) : 0.f;     // below that the powers leave fp32's range
+        const float top = a.cap * CT_LOG2E;
         const TanhShort k_short = tanh_short(qs, top);
+        // where the powers leave fp32's range: not taken
+        const bool powers = fabsf(qs) > 1e-6f && fabsf(k_short.k0) + fabsf(k_short.k1) + fabsf(k_short.k2) + fabsf(k_short.k3) <= FLT_MAX;
+        const float short_range = powers ? CT_TANH_SHORT / fabsf(qs) : -1.f;
         const bool wide = ((uintptr_t)a.out & 31) == 0;
         int n = 0, u = 0, seg = 0;
         bool dead = false, cut_end = false;
@@ -746,9 +749,9 @@ static int chunk_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, 
 }
 template <int HD, bool F8>
 static int chunk_tc_launch_mode(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
-    // PLAIN takes the largest product for the largest logit; BIASED multiplies first
+    // PLAIN takes the largest product for the largest logit, and -infinity times the factor for what is not seen; BIASED multiplies first
     if (a.cap > 0.f) return chunk_tc_launch_as<HD, F8, CAPPED>(cache, a, plan, sms, st);
-    return a.slopes || !(a.scale > 0.f) ? chunk_tc_launch_as<HD, F8, BIASED>(cache, a, plan, sms, st) : chunk_tc_launch_as<HD, F8, PLAIN>(cache, a, plan, sms, st);
+    return a.slopes || !(a.scale >= FLT_MIN) ? chunk_tc_launch_as<HD, F8, BIASED>(cache, a, plan, sms, st) : chunk_tc_launch_as<HD, F8, PLAIN>(cache, a, plan, sms, st);
 }
 template <int HD>
 static int chunk_tc_launch_hd(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {

@@ -47,6 +47,9 @@ __device__ __forceinline__ bool verify_range(const VerifyArgs& a, int b, int& q0
     return ok;
 }
 
+// A sequence's temperature, 0: the first largest logit.  Beyond 2^-100 and 2^100 the distribution stays the same, while quotients would leave fp32's range.
+__device__ __forceinline__ float heat_of(const VerifyArgs& a, int b) { const float h = a.heat[b]; return h > 0.f ? fminf(fmaxf(h, 0x1p-100f), 0x1p100f) : 0.f; }
+
 struct Best { float top; int at; };
 __device__ __forceinline__ Best better(Best a, Best b) { return b.top > a.top || (b.top == a.top && b.at < a.at) ? b : a; }
 
@@ -76,7 +79,7 @@ __global__ void __launch_bounds__(RS_THREADS, 12) k_row_stats(const VerifyArgs a
     if (tid == 0) { heat_s = -1.f; at_s = 0x7fffffff; }
     __syncthreads();
     for (int b = tid; b < a.n_seqs; b += RS_THREADS)       // at most one sequence has the row
-        if (a.q_start[b] <= row && row < a.q_start[b + 1]) heat_s = fmaxf(a.heat[b], 0.f);
+        if (a.q_start[b] <= row && row < a.q_start[b + 1]) heat_s = heat_of(a, b);
     auto elem = [&](int i, int e) {
         const unsigned u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
         if constexpr (sizeof(T) == 4) return __uint_as_float(u[e]);
@@ -178,10 +181,10 @@ __device__ __forceinline__ void exp2_64(const float (&l)[N], double top, double 
 #pragma unroll
     for (int i = 0; i < N; i++) p[i] = fma(p[i], w[i], w[i]);
 #pragma unroll
-    for (int i = 0; i < N; i++) w[i] = l[i] > lowest ? __hiloint2double(__double2hiint(p[i]) + ((k[i] >> 4) << 20), __double2loint(p[i])) : 0.0;
+    for (int i = 0; i < N; i++) w[i] = l[i] >= lowest ? __hiloint2double(__double2hiint(p[i]) + ((k[i] >> 4) << 20), __double2loint(p[i])) : 0.0;
 }
-// The logit below which a weight is 0.
-__device__ __forceinline__ float lowest_logit(double top, double scale) { return (float)(top - 1000.0 / scale); }
+// The logit below which a weight is 0: rounded up, to the largest one at most, so that no weight is below 2^-1000, the largest never left out, and -infinity always.
+__device__ __forceinline__ float lowest_logit(double top, double scale) { return __double2float_ru(top - 1000.0 / scale); }
 
 constexpr int LEFT_STEPS = 8;                      // loads of so many steps side by side
 
@@ -273,7 +276,7 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         }
         return;
     }
-    const float heat = a.heat[b];
+    const float heat = heat_of(a, b);
     const bool draws = heat > 0.f;
     const double scale = 1.4426950408889634074 / (double)heat;             // weights are 2^((logit - largest) * scale)
     if (tid < EXP_TABLE * 16) sh.table[tid] = two_to[tid / 16];

@@ -49,11 +49,12 @@ __device__ __forceinline__ void tree_status(const TreeArgs& a, unsigned bit) {
     if (a.status) atomicOr(a.status, bit);
 }
 
-// dynakv_attend_chunk: the rows [lo, hi) that packed token `token`, whose own row is `place`, sees of a sequence of n.
+// dynakv_attend_chunk: the rows [lo, hi) that packed token `token`, whose own row is `place`, sees of a sequence of n.  Neither is
+// negative, so that differences with other rows stay in range whatever rows_from and rows_to hold.
 __device__ __forceinline__ void chunk_sees(const TreeArgs& a, int token, int place, int n, int& lo, int& hi) {
-    lo = a.rows_from ? a.rows_from[token] : 0;
+    lo = a.rows_from ? max(a.rows_from[token], 0) : 0;
     if (a.window > 0) lo = max(lo, place + 1 - a.window);
-    hi = min(a.rows_to ? a.rows_to[token] : place + 1, n);
+    hi = max(0, min(a.rows_to ? a.rows_to[token] : place + 1, n));
 }
 
 // The page of a sequence's column: its place in the pool, -1 where the table names none.

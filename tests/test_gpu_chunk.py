@@ -221,6 +221,29 @@ def test_ranges_that_leave_nothing_and_reach_beyond(cache, new):
 
 
 @pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [6, 300])
+@pytest.mark.parametrize("window", [0, 40])
+def test_ranges_at_the_ends_of_their_type(cache, new, window):
+    p = Chunk([310, 305], [new, 5], 8, 2, 128, cache, seed=19)
+    least, most = -2 ** 31, 2 ** 31 - 1
+    kinds = [(least, least), (0, least), (least, most), (most, most), (most, least), (200, most), (least, 150)]
+    pick = lambda i: lambda b, place, n: torch.tensor([kinds[int(x) % len(kinds)][i] for x in place], device="cuda")
+    p.see(low=pick(0), high=pick(1))
+    p.check(*p.run(window=window), window=window)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", [2, 200])
+@pytest.mark.parametrize("cap", [2.0 ** -100, 2.0 ** 100])
+def test_the_largest_and_smallest_caps(cache, new, cap):
+    p = Chunk([300, 130], [new, 100 if new > 2 else 1], 8, 2, 128, cache, seed=20)
+    p.q[::3] = 0                                                  # logits of 0: in whole warps' rows, and beside others
+    p.check(*p.run(softcap=cap), softcap=cap)
+    p.q.zero_()
+    p.check(*p.run(softcap=cap), softcap=cap)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "fp8"])
 @pytest.mark.parametrize("new", [1, 200])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1.0])
 def test_scales(cache, new, scale):

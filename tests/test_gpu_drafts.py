@@ -333,6 +333,30 @@ def test_masked_logits_and_the_ends_of_the_draw():
     assert got[0].tolist() == [1, 1, 1, 1] and all(x == -1 or x >= 4900 or x == 4321 for x in got[3].tolist())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("drawn", [False, True])
+def test_temperatures_near_zero_and_without_end(dtype, drawn):
+    vocab, n = 5000, 6
+    a = drafts([4, 2], vocab, dtype, "chain", drawn, 21)
+    a["logits"].clamp_(max=19.0)
+    best = torch.tensor([7, 4999, 0, 2500, 1234, 4095], device="cuda")
+    a["logits"][torch.arange(n, device="cuda"), best] = 20.0
+    a["logits"][:, 3000:4000] = -math.inf
+    a["tokens"][1:3] = best[:2].to(torch.int32)                   # the first two drafts are the largest, the third and the other sequence's are not
+    a["tokens"][3] = a["tokens"][5] = 1
+    a["uniform"] = torch.tensor([0.25, 0.5, 0.75, 0.3, 0.6, 0.9], device="cuda")
+    for heat in (1e-6, 1e-9, 1e-12, 1e-30, 2.0 ** -126, 1e-44):
+        got = P.verify_drafts(**a, temperature=torch.full((2,), heat, device="cuda"))
+        assert got[0].tolist() == [3, 1] and got[3].tolist() == [0, 1234], heat
+    # all that is not masked weighs the same: the draw counts through the 4000 tokens
+    a["draft_probs"] = None
+    a["tokens"][1] = a["tokens"][5] = 3500                        # masked: refused
+    a["uniform"][0], a["uniform"][4] = (3100 + 0.5) / 4000, (1000 + 0.5) / 4000
+    for heat in (2.0 ** 90, 2.0 ** 120, math.inf):
+        got = P.verify_drafts(**a, temperature=torch.full((2,), heat, device="cuda"))
+        assert got[0].tolist() == [1, 1] and got[3].tolist() == [4100, 1000], heat
+
+
 def test_a_draft_that_covers_the_target():
     # equal logits, so that the target's probabilities are quarters exactly (those of ln 0.25 in fp32 are off by 2e-8, and 2e-8 would be left)
     p = torch.tensor([[0.25, 0.25, 0.25, 0.25, 0.0]] * 2, device="cuda")
