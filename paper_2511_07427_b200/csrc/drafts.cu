@@ -9,11 +9,14 @@
 //   k_verify, a cluster of CTAs per sequence: every draft's test from those and one logit, at once for all drafts; the walk in shared
 //     memory; then the drawing from the last kept token's row, which is by inverse sums in 64 bits: among 10^5 tokens fp32 sums
 //     misplace the draw with a chance of about 10^-3, and the same numbers have to give the same token however the sums are split.
-// Measured, calls one after the other: 64 sequences of 6 tokens over 128256, drafts drawn, 72 us: 22 for the rows, 8 until the walk is done, 15
-// each for the target's sum and for what is left of it (64-bit operations and the loads that feed them, 128 CTAs), 3 for the place of the draw.
-// 16 trees of 32 over 50257: 31 us.  One sequence of 5 over 32000: 14 us on the device, a chain of dependent loads; 22 us of host time.
+// Measured, calls one after the other: 64 sequences of 6 tokens over 128256, drafts drawn, 52 us: 22 for the rows, 6 until the walk is done, 16
+// for the sums (36 instructions an element, 11 of them in 64 bits; 128 CTAs; in two passes, the target's sum first, 31), 6 for the place of
+// the draw.  16 trees of 32 over 50257: 26 us.  One sequence of 5 over 32000: 12 us on the device, a chain of dependent loads; 19 us of host time.
+// 512 sequences of one token over 128256: 169 us, of which 36 without the draw (one CTA of 512 threads per SM 176).
 #include <cooperative_groups.h>
 #include <float.h>
+
+#include <utility>
 
 #include "bulk_copy.cuh"
 #include "head_rows.cuh"
@@ -26,7 +29,7 @@ namespace dkv {
 namespace cg = cooperative_groups;
 
 constexpr int RS_THREADS = 128, RS_VECS = 4, RS_BYTES = RS_THREADS * RS_VECS * 16;     // a block's piece of a row
-constexpr int VF_THREADS = 512, VF_WARPS = VF_THREADS / 32, VF_CLUSTER = 8;
+constexpr int VF_THREADS = 512, VF_WARPS = VF_THREADS / 32, VF_CLUSTER = 8;            // at most
 
 struct VerifyArgs {
     const void* logits; long long stride;  // row stride, elements
@@ -63,6 +66,7 @@ __global__ void __launch_bounds__(RS_THREADS, 12) k_row_stats(const VerifyArgs a
     __shared__ float top_s[RS_THREADS / 32], sum_s[RS_THREADS / 32];
     __shared__ int at_s;
     pdl_wait();
+    pdl_trigger();
     const T* p = reinterpret_cast<const T*>(a.logits) + (long long)row * a.stride;
     // elements before the first 16-byte boundary, whole vectors, and what is left
     const int head = min(a.vocab, (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T))), vecs = (a.vocab - head) / N, tail = a.vocab - head - vecs * N;
@@ -76,10 +80,23 @@ __global__ void __launch_bounds__(RS_THREADS, 12) k_row_stats(const VerifyArgs a
     float x_odd = -INFINITY;
     int at_odd = 0x7fffffff;
     if (piece == 0 && tid < head + tail) { at_odd = tid < head ? tid : vecs * N + tid; x_odd = to_f(p[at_odd]); }
-    if (tid == 0) { heat_s = -1.f; at_s = 0x7fffffff; }
-    __syncthreads();
-    for (int b = tid; b < a.n_seqs; b += RS_THREADS)       // at most one sequence has the row
-        if (a.q_start[b] <= row && row < a.q_start[b + 1]) heat_s = heat_of(a, b);
+    if (tid == 0) at_s = 0x7fffffff;
+    if (warp == 0) {
+        // the last sequence that begins at or before the row: 32 of them are looked at a time
+        int lo = 0;
+        for (int n = a.n_seqs; n > 1;) {
+            const int step = (n + 31) / 32, at = lane * step;
+            const unsigned before = __ballot_sync(0xffffffffu, at < n && a.q_start[lo + min(at, n - 1)] <= row);
+            const int skip = max(0, __popc(before) - 1) * step;
+            lo += skip; n = min(step, n - skip);
+        }
+        auto has = [&](int b) { return a.q_start[b] <= row && row < a.q_start[b + 1]; };
+        int mine = has(lo) ? lo : -1;
+        if (mine < 0)                                      // a row of no sequence, or ranges out of order, of which some may be sound
+            for (int b = lane; b < a.n_seqs; b += 32) if (has(b)) mine = b;
+        mine = __reduce_max_sync(0xffffffffu, mine);
+        if (lane == 0) heat_s = mine >= 0 ? heat_of(a, mine) : -1.f;
+    }
     auto elem = [&](int i, int e) {
         const unsigned u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
         if constexpr (sizeof(T) == 4) return __uint_as_float(u[e]);
@@ -95,7 +112,6 @@ __global__ void __launch_bounds__(RS_THREADS, 12) k_row_stats(const VerifyArgs a
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (lane == 0) top_s[warp] = top;
     __syncthreads();
-    pdl_trigger();
     const float heat = heat_s;
     if (heat < 0.f) return;                                // a row of no sequence
     top = top_s[0];
@@ -146,17 +162,20 @@ __device__ __forceinline__ void prefetch_l2(const void* p, size_t n) {
         asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(at), "r"((unsigned)(end - at < 65536 ? end - at : 65536)) : "memory");
 }
 
-constexpr int EXP_TABLE = 16;
-__device__ const double two_to[EXP_TABLE] = {      // 2^(j / 16)
-    1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927,
-    1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543, 1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
-// N values of 2^((l - top) * scale) in 64 bits, l <= top: the exponent is n + j / 16 + r with |r| <= 1 / 32, the factor of j comes from a table
-// (in shared memory once per pair of lanes, so that no two meet in a bank) and that of r from its series up to r^5 (what is left out is
+constexpr int EXP_TABLE = 256;
+__device__ const double two_to[32] = {             // 2^(j / 16), 2^(j / 256)
+    1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484, 1.2968395546510096,
+    1.3542555469368927, 1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543, 1.681792830507429, 1.7562521603732995,
+    1.8340080864093424, 1.9152065613971474, 1.0, 1.0027112750502025, 1.0054299011128027, 1.0081558981184175, 1.0108892860517005,
+    1.0136300849514894, 1.016378314910953, 1.019133996077738, 1.0218971486541166, 1.0246677928971357, 1.0274459491187637, 1.030231637686041,
+    1.0330248790212284, 1.0358256936019572, 1.0386341019613787, 1.041450124688316};
+// N values of 2^((l - top) * scale) in 64 bits, l <= top: the exponent is n + j / 256 + r with |r| <= 1 / 512, the factor of j comes from a table
+// (in shared memory once per pair of lanes, so that no two meet in a bank) and that of r from its series up to r^3 (what is left out is
 // below 2^-42 of the value, far below what could misplace a draw).  Values below 2^-1000 are 0.  Step by step for all N, because a 64-bit operation's result is a long time in coming: one value after the other,
 // the 8 M of a large call took 140 us.
 template <int N>
 __device__ __forceinline__ void exp2_64(const float (&l)[N], double top, double scale, float lowest, const double* table, double (&w)[N]) {
-    const double shift = 6755399441055744.0 / EXP_TABLE;   // 1.5 * 2^52 in units of 1 / 16: the sum's last bits are round(16 x)
+    const double shift = 6755399441055744.0 / EXP_TABLE;   // 1.5 * 2^52 in units of 1 / 256: the sum's last bits are round(256 x)
     int k[N];
     double r[N], p[N];
 #pragma unroll
@@ -169,11 +188,7 @@ __device__ __forceinline__ void exp2_64(const float (&l)[N], double top, double 
     for (int i = 0; i < N; i++) { r[i] = fma(w[i], scale, -p[i]); w[i] = table[(k[i] & (EXP_TABLE - 1)) * 16]; }
     // (ln 2)^k / k!
 #pragma unroll
-    for (int i = 0; i < N; i++) p[i] = fma(r[i], 0.0013333558146428441, 0.0096181291076284769);
-#pragma unroll
-    for (int i = 0; i < N; i++) p[i] = fma(p[i], r[i], 0.055504108664821576);
-#pragma unroll
-    for (int i = 0; i < N; i++) p[i] = fma(p[i], r[i], 0.24022650695910069);
+    for (int i = 0; i < N; i++) p[i] = fma(r[i], 0.055504108664821576, 0.24022650695910069);
 #pragma unroll
     for (int i = 0; i < N; i++) p[i] = fma(p[i], r[i], 0.69314718055994529);
 #pragma unroll
@@ -181,12 +196,12 @@ __device__ __forceinline__ void exp2_64(const float (&l)[N], double top, double 
 #pragma unroll
     for (int i = 0; i < N; i++) p[i] = fma(p[i], w[i], w[i]);
 #pragma unroll
-    for (int i = 0; i < N; i++) w[i] = l[i] >= lowest ? __hiloint2double(__double2hiint(p[i]) + ((k[i] >> 4) << 20), __double2loint(p[i])) : 0.0;
+    for (int i = 0; i < N; i++) w[i] = l[i] >= lowest ? __hiloint2double(__double2hiint(p[i]) + ((k[i] >> 8) << 20), __double2loint(p[i])) : 0.0;
 }
 // The logit below which a weight is 0: rounded up, to the largest one at most, so that no weight is below 2^-1000, the largest never left out, and -infinity always.
-__device__ __forceinline__ float lowest_logit(double top, double scale) { return __double2float_ru(top - 1000.0 / scale); }
+__device__ __forceinline__ float lowest_logit(double top, double scale_inv) { return __double2float_ru(top - 1000.0 * scale_inv); }
 
-constexpr int LEFT_STEPS = 8;                      // loads of so many steps side by side
+constexpr int LEFT_EACH = 8, LEFT_RUN = 32 * LEFT_EACH;     // elements of a lane and of a warp at a time
 
 struct VerifyShared {
     double weight[TREE_MAX], sum[TREE_MAX];        // of a draft: its token's weight behind its parent; [a row]: sum of the row's weights
@@ -195,144 +210,209 @@ struct VerifyShared {
     int token[TREE_MAX], up[TREE_MAX], first[TREE_MAX];
     unsigned char again[TREE_MAX];                 // an older sibling has the same token
     double table[EXP_TABLE * 16];
-    double slices[VF_CLUSTER * VF_WARPS], part[VF_WARPS];
-    double held[32 * LEFT_STEPS];                  // weights of the run in which the drawn token lies
+    double slices[3][VF_CLUSTER * VF_WARPS], part[VF_WARPS];
+    double held[LEFT_RUN];                  // weights of the run in which the drawn token lies
     int last, refused, found;
 };
 
-// What is left of a row's distribution: its weights, or (norm > 0) weight * norm - q, without the tokens of `refused` children.
+// What is left of a row's distribution: its weights without the tokens of `refused` children, or (a refused draft that was drawn from q)
+// max(weight / S - q, 0), S the sum of the weights.  Which elements of the latter are not 0 is decided with S as fp32 sums give it (near = 1 / S): the
+// others' sums P and Q can then be taken in the pass that finds S in 64 bits, and P / S - Q is off by what such elements as lie within 1e-6 of 0 add,
+// where each adds next to nothing.
+enum { LEFT_ALL = 0, LEFT_LESS = 1, LEFT_SUMS = 2 };       // weights; max(weight norm - q, 0); all three sums
 template <typename T>
 struct RowLeft {
     const T* row;
     const float* q;
-    double top, scale, norm;
-    int refused;
+    double top, scale, scale_inv, near, norm;
+    int refused, what;
 };
-// The sum over elements [from, end), by one warp; `held`: the weights of up to 32 LEFT_STEPS of them are kept there.  One function,
-// not inlined: the code is run once or twice, and fetching it is what it would cost.
+struct LeftSums { double all, p, q; };
+// The largest element <= x at which the row has a 16-byte boundary (it may lie before the row).
 template <typename T>
-__device__ __noinline__ double left_sum(const RowLeft<T> a, const VerifyShared& sh, int from, int end, double* held) {
+__device__ __forceinline__ int left_aligned(const T* row, int x) { return x - (int)(((uintptr_t)(row + x) & 15) / sizeof(T)); }
+// The sum over elements [from, end), by one warp, each lane LEFT_EACH elements side by side, from 16-byte boundaries on; `held`: the weights of one
+// run are kept there, in their order from the boundary on.  One function, not inlined: the code is run once or twice, and fetching it is what it would cost.
+template <typename T>
+__device__ __noinline__ LeftSums left_sum(const RowLeft<T> a, const VerifyShared& sh, int vocab, int from, int end, double* held) {
+    constexpr int WORDS = LEFT_EACH * sizeof(T) / 16;
     const int lane = threadIdx.x & 31;
-    const bool less = a.norm > 0.0;
-    const float lowest = lowest_logit(a.top, a.scale);
-    double s[2] = {0.0, 0.0};
-    T l[LEFT_STEPS];
-    float q[LEFT_STEPS] = {};
-    // The next elements, while these are worked on.  Every lane loads, those behind the end the last one again: loads under conditions of their
-    // own wait for one another.
-    auto fetch = [&](int base) {
+    const bool less = a.what != LEFT_ALL, less16 = less && (((uintptr_t)(a.q + left_aligned(a.row, from)) & 15) == 0);
+    const float lowest = lowest_logit(a.top, a.scale_inv);
+    double s[2] = {0.0, 0.0}, p[2] = {0.0, 0.0}, m[2] = {0.0, 0.0};
+    uint4 l[WORDS];
+    float q[LEFT_EACH] = {};
+    // The next elements, while these are worked on.  Whole vectors but at the row's ends.
+    auto fetch = [&](int at) {
+        if (at >= 0 && at + LEFT_EACH <= vocab) {
 #pragma unroll
-        for (int k = 0; k < LEFT_STEPS; k++) l[k] = a.row[min(base + k * 32, end - 1)];
-        if (less) {
+            for (int k = 0; k < WORDS; k++) l[k] = __ldg(reinterpret_cast<const uint4*>(a.row + at) + k);
+            if (less16) {
 #pragma unroll
-            for (int k = 0; k < LEFT_STEPS; k++) q[k] = a.q[min(base + k * 32, end - 1)];
+                for (int k = 0; k < LEFT_EACH; k += 4) {
+                    const float4 v = __ldg(reinterpret_cast<const float4*>(a.q + at + k));
+                    q[k] = v.x; q[k + 1] = v.y; q[k + 2] = v.z; q[k + 3] = v.w;
+                }
+            } else if (less) {
+#pragma unroll
+                for (int k = 0; k < LEFT_EACH; k++) q[k] = __ldg(a.q + at + k);
+            }
+            return;
         }
+        unsigned u[4 * WORDS];
+#pragma unroll
+        for (int k = 0; k < 4 * WORDS; k++) u[k] = 0u;
+#pragma unroll
+        for (int k = 0; k < LEFT_EACH; k++) {
+            if ((unsigned)(at + k) >= (unsigned)vocab) continue;
+            if constexpr (sizeof(T) == 4) u[k] = __float_as_uint(a.row[at + k]);
+            else u[k >> 1] |= (unsigned)__bfloat16_as_ushort(a.row[at + k]) << (16 * (k & 1));
+            if (less) q[k] = a.q[at + k];
+        }
+#pragma unroll
+        for (int k = 0; k < WORDS; k++) l[k] = make_uint4(u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
     };
-    if (from < end) fetch(from + lane);
-    for (int base = from + lane; base - lane < end; base += 32 * LEFT_STEPS) {
-        double w[LEFT_STEPS];
-        float now[LEFT_STEPS], minus[LEFT_STEPS];
+    int at = left_aligned(a.row, from) + lane * LEFT_EACH;         // this lane's elements
+    if (from < end) fetch(at);
+    for (; at - lane * LEFT_EACH < end; at += LEFT_RUN) {
+        double w[LEFT_EACH];
+        float now[LEFT_EACH], minus[LEFT_EACH];
 #pragma unroll
-        for (int k = 0; k < LEFT_STEPS; k++) { now[k] = base + k * 32 < end ? to_f(l[k]) : -INFINITY; minus[k] = q[k]; }
-        for (int r = 0; r < a.refused; r++) {              // a refused token weighs nothing
-            const int off = sh.token[sh.first[r]] - base;
-            if ((unsigned)(off + lane) >= 32u * LEFT_STEPS) continue;          // the same in the whole warp
-#pragma unroll
-            for (int k = 0; k < LEFT_STEPS; k++) if (off == k * 32) now[k] = -INFINITY;
+        for (int k = 0; k < LEFT_EACH; k++) {
+            const uint4 v = l[k * sizeof(T) / 16];
+            const unsigned u[4] = {v.x, v.y, v.z, v.w};
+            if constexpr (sizeof(T) == 4) now[k] = __uint_as_float(u[k & 3]);
+            else now[k] = __uint_as_float(k & 1 ? u[k >> 1] & 0xffff0000u : u[k >> 1] << 16);
+            minus[k] = q[k];
         }
-        if (base - lane + 32 * LEFT_STEPS < end) fetch(base + 32 * LEFT_STEPS);
+        if (__any_sync(0xffffffffu, at < from || at + LEFT_EACH > end)) {
+#pragma unroll
+            for (int k = 0; k < LEFT_EACH; k++) if (at + k < from || at + k >= end) { now[k] = -INFINITY; minus[k] = 0.f; }
+        }
+        for (int r = 0; r < a.refused; r++) {              // a refused token weighs nothing
+            const int off = sh.token[sh.first[r]] - at;
+            if (!__any_sync(0xffffffffu, (unsigned)off < (unsigned)LEFT_EACH)) continue;
+#pragma unroll
+            for (int k = 0; k < LEFT_EACH; k++) if (off == k) now[k] = -INFINITY;
+        }
+        if (at - lane * LEFT_EACH + LEFT_RUN < end) fetch(at + LEFT_RUN);
         exp2_64(now, a.top, a.scale, lowest, sh.table + (lane & 15), w);
-        if (less) {
+        if (a.what == LEFT_SUMS) {
 #pragma unroll
-            for (int k = 0; k < LEFT_STEPS; k++) w[k] = fma(w[k], a.norm, -(double)minus[k]);
+            for (int k = 0; k < LEFT_EACH; k++) {
+                const double x = (double)minus[k];
+                const bool more = w[k] * a.near > x;
+                p[k & 1] += more ? w[k] : 0.0;
+                m[k & 1] += more ? x : 0.0;
+            }
+        } else if (less) {
 #pragma unroll
-            for (int k = 0; k < LEFT_STEPS; k++) w[k] = w[k] > 0.0 ? w[k] : 0.0;
+            for (int k = 0; k < LEFT_EACH; k++) {
+                const double x = (double)minus[k];
+                w[k] = w[k] * a.near > x ? fmax(fma(w[k], a.norm, -x), 1e-300) : 0.0;
+            }
         }
         if (held) {
 #pragma unroll
-            for (int k = 0; k < LEFT_STEPS; k++) held[k * 32 + lane] = w[k];
+            for (int k = 0; k < LEFT_EACH; k++) held[lane * LEFT_EACH + k] = w[k];
         }
 #pragma unroll
-        for (int k = 0; k < LEFT_STEPS; k += 2) { s[0] += w[k]; s[1] += w[k + 1]; }
+        for (int k = 0; k < LEFT_EACH; k += 2) { s[0] += w[k]; s[1] += w[k + 1]; }
     }
-    return warp_sum64(s[0] + s[1]);
+    LeftSums sums = {warp_sum64(s[0] + s[1]), 0.0, 0.0};
+    if (a.what == LEFT_SUMS) { sums.p = warp_sum64(p[0] + p[1]); sums.q = warp_sum64(m[0] + m[1]); }
+    return sums;
 }
 
-// 512 threads per CTA, one slice of the vocabulary per warp.
-template <typename T>
-__global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
+// One slice of the vocabulary per warp.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_verify(const VerifyArgs a) {
+    constexpr int WARPS = THREADS / 32, EACH = (TREE_MAX + THREADS - 1) / THREADS;
     __shared__ VerifyShared sh;
     const cg::cluster_group cluster = cg::this_cluster();
     const int ctas = gridDim.x, cta = blockIdx.x, b = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    for (int i = tid; i < EXP_TABLE * 16; i += THREADS) sh.table[i] = two_to[i >> 8] * two_to[16 + ((i >> 4) & 15)];
     pdl_wait();
     int q0, n;
     const bool ok = verify_range(a, b, q0, n);
     const T* logits = reinterpret_cast<const T*>(a.logits);
     if (n == 0) {                                          // the same in the whole cluster
         if (cta == 0) {
-            for (int i = tid; i < a.most; i += VF_THREADS) a.path[(size_t)b * a.most + i] = -1;
+            for (int i = tid; i < a.most; i += THREADS) a.path[(size_t)b * a.most + i] = -1;
             if (tid == 0) { a.kept[b] = 0; a.dropped[b] = ok ? 0 : -1; a.next[b] = -1; }
         }
         return;
     }
+    cg::cluster_group::arrival_token begun = cluster.barrier_arrive();
     const float heat = heat_of(a, b);
     const bool draws = heat > 0.f;
-    const double scale = 1.4426950408889634074 / (double)heat;             // weights are 2^((logit - largest) * scale)
-    if (tid < EXP_TABLE * 16) sh.table[tid] = two_to[tid / 16];
+    const double scale = 1.4426950408889634074 / (double)heat, scale_inv = 0.69314718055994530942 * (double)heat;         // weights are 2^((logit - largest) * scale)
+    // what the tests will need is on its way before anything is waited for
+    int token[EACH], up[EACH];
+    float chance[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+        const int i = tid + e * THREADS;
+        token[e] = i < n ? a.tokens[q0 + i] : -1;
+        up[e] = i < n && i > 0 ? a.parent ? a.parent[q0 + i] : i - 1 : -1;
+        chance[e] = i < n ? a.uniform[q0 + i] : 0.f;
+    }
     __syncthreads();
     auto weight_of = [&](float l, float top) {
         const float x[1] = {l};
         double w[1];
-        exp2_64(x, (double)top, scale, lowest_logit((double)top, scale), sh.table + (lane & 15), w);
+        exp2_64(x, (double)top, scale, lowest_logit((double)top, scale_inv), sh.table + (lane & 15), w);
         return w[0];
     };
     // ---- every row's largest logit and sum, a warp per row
-    for (int i = warp; i < n; i += VF_WARPS) {
+    for (int i = warp; i < n; i += WARPS) {
         const float4* st = a.stats + (size_t)(q0 + i) * a.pieces;
-        Best best = {-INFINITY, 0x7fffffff};
-        for (int k = lane; k < a.pieces; k += 32) best = better(best, Best{st[k].x, __float_as_int(st[k].y)});
+        const float4 mine = lane < a.pieces ? st[lane] : make_float4(-INFINITY, __int_as_float(0x7fffffff), 0.f, 0.f);
+        Best best = {mine.x, __float_as_int(mine.y)};
+        for (int k = lane + 32; k < a.pieces; k += 32) best = better(best, Best{st[k].x, __float_as_int(st[k].y)});
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) best = better(best, Best{__shfl_xor_sync(0xffffffffu, best.top, o), __shfl_xor_sync(0xffffffffu, best.at, o)});
-        double sum = 0.0;
-        for (int k = lane; k < a.pieces; k += 32)
+        double sum = draws && mine.x > -INFINITY ? (double)mine.z * weight_of(mine.x, best.top) : 0.0;
+        for (int k = lane + 32; k < a.pieces; k += 32)
             if (draws && st[k].x > -INFINITY) sum += (double)st[k].z * weight_of(st[k].x, best.top);
         sum = warp_sum64(sum);
         if (lane == 0) { sh.top[i] = best.top; sh.best[i] = best.at; sh.sum[i] = sum; }
     }
-    for (int i = tid; i < n; i += VF_THREADS) {
-        sh.token[i] = a.tokens[q0 + i];
-        const int up = i == 0 ? -1 : a.parent ? a.parent[q0 + i] : i - 1;
-        sh.up[i] = up >= 0 && up < i ? up : -1;            // a draft without a parent before it is never reached
-        sh.first[i] = n;
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+        const int i = tid + e * THREADS;
+        if (up[e] < 0 || up[e] >= i) up[e] = -1;           // a draft without a parent before it is never reached
+        if (i < n) { sh.token[i] = token[e]; sh.up[i] = up[e]; sh.first[i] = n; }
     }
     __syncthreads();
-    auto weight = [&](int row, int x) {                    // of token x behind row `row`, relative to the row's largest
-        if (x < 0 || x >= a.vocab || sh.top[row] == -INFINITY) return 0.0;
-        return weight_of(to_f(logits[(long long)(q0 + row) * a.stride + x]), sh.top[row]);
-    };
-    for (int i = tid; i < n; i += VF_THREADS) {
-        const int up = sh.up[i];
-        sh.weight[i] = draws && up >= 0 ? weight(up, sh.token[i]) : 0.0;
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+        const int i = tid + e * THREADS, x = token[e];
+        if (i >= n) continue;
+        // of token x behind row up, relative to the row's largest
+        sh.weight[i] = draws && up[e] >= 0 && x >= 0 && x < a.vocab && sh.top[up[e]] > -INFINITY ? weight_of(to_f(logits[(long long)(q0 + up[e]) * a.stride + x]), sh.top[up[e]]) : 0.0;
         bool again = false;
-        if (a.parent && up >= 0) for (int s = up + 1; s < i; s++) again |= sh.up[s] == up && sh.token[s] == sh.token[i];
+        if (a.parent && up[e] >= 0) for (int s = up[e] + 1; s < i; s++) again |= sh.up[s] == up[e] && sh.token[s] == x;
         sh.again[i] = again;
     }
     __syncthreads();
     // ---- every draft's test, against what its older siblings leave
-    for (int i = tid; i < n; i += VF_THREADS) {
-        const int up = sh.up[i], x = sh.token[i];
-        if (up < 0) continue;
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+        const int i = tid + e * THREADS, x = token[e], above = up[e];
+        if (above < 0) continue;
         bool pass;
-        if (!draws) pass = sh.best[up] == x && sh.top[up] > -INFINITY;
-        else if (a.draft) pass = x >= 0 && x < a.vocab && (double)a.uniform[q0 + i] * (double)a.draft[(long long)(q0 + i) * a.draft_stride + x] * sh.sum[up] < sh.weight[i];
+        if (!draws) pass = sh.best[above] == x && sh.top[above] > -INFINITY;
+        else if (a.draft) pass = x >= 0 && x < a.vocab && (double)chance[e] * (double)a.draft[(long long)(q0 + i) * a.draft_stride + x] * sh.sum[above] < sh.weight[i];
         else {
-            double left = sh.sum[up];
-            if (a.parent) for (int s = up + 1; s < i; s++) if (sh.up[s] == up && !sh.again[s]) left -= sh.weight[s];
-            pass = !sh.again[i] && (double)a.uniform[q0 + i] * left < sh.weight[i];
+            double left = sh.sum[above];
+            if (a.parent) for (int s = above + 1; s < i; s++) if (sh.up[s] == above && !sh.again[s]) left -= sh.weight[s];
+            pass = !sh.again[i] && (double)chance[e] * left < sh.weight[i];
         }
-        if (pass) atomicMin(&sh.first[up], i);
+        if (pass) atomicMin(&sh.first[above], i);
     }
+    if (tid == 0) sh.refused = 0;
     __syncthreads();
     // ---- the walk
     if (tid == 0) {
@@ -348,39 +428,47 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
     }
     __syncthreads();
     const int last = sh.last;
-    if (cta == 0) for (int i = sh.found + tid; i < a.most; i += VF_THREADS) a.path[(size_t)b * a.most + i] = -1;
+    if (cta == 0) for (int i = sh.found + tid; i < a.most; i += THREADS) a.path[(size_t)b * a.most + i] = -1;
     if (!draws || sh.top[last] == -INFINITY) {             // the same in the whole cluster
         if (cta == 0 && tid == 0) a.next[b] = sh.top[last] == -INFINITY ? -1 : sh.best[last];
+        cluster.barrier_wait(std::move(begun));
         return;
     }
     // ---- the token behind the last kept one.  Its refused children: their tokens are out, or (drawn) the one child's distribution is taken off
-    __syncthreads();
-    if (tid == 0) sh.refused = 0;
-    __syncthreads();
-    for (int i = last + 1 + tid; i < n; i += VF_THREADS) if (sh.up[i] == last) sh.first[atomicAdd(&sh.refused, 1)] = i;       // the links are not needed any more
+#pragma unroll
+    for (int e = 0; e < EACH; e++) if (up[e] == last) sh.first[atomicAdd(&sh.refused, 1)] = tid + e * THREADS;         // the links are not needed any more
     __syncthreads();
     const int refused = sh.refused;
     const bool taken = a.draft && refused > 0;
-    const int slice = cta * VF_WARPS + warp, slices = ctas * VF_WARPS, e0 = (int)((long long)a.vocab * slice / slices), e1 = (int)((long long)a.vocab * (slice + 1) / slices);
+    const int slice = cta * WARPS + warp, slices = ctas * WARPS, shift = __ffs(slices) - 1;         // a power of two
+    auto begin = [&](int x) { return (int)((long long)a.vocab * x >> shift); };
+    const int e0 = begin(slice), e1 = begin(slice + 1);
     RowLeft<T> left = {logits + (long long)(q0 + last) * a.stride, taken ? a.draft + (long long)(q0 + sh.first[0]) * a.draft_stride : nullptr,
-                       (double)sh.top[last], scale, 0.0, a.draft ? 0 : refused};
+                       (double)sh.top[last], scale, scale_inv, taken ? 1.0 / sh.sum[last] : 0.0, 0.0, a.draft ? 0 : refused, taken ? LEFT_SUMS : LEFT_ALL};
     if (lane == 0) {                                       // both rows on their way: the sums have too few loads under way to wait for HBM
         prefetch_l2(left.row + e0, (size_t)(e1 - e0) * sizeof(T));
         if (taken) prefetch_l2(left.q + e0, (size_t)(e1 - e0) * 4);
     }
-    // Sums of all slices, the same in all CTAs: every lane has those of `mine` consecutive ones, `before` those ahead of them; returns the total.
+    {
+        const LeftSums mine = left_sum(left, sh, a.vocab, e0, e1, nullptr);
+        cluster.barrier_wait(std::move(begun));            // all CTAs have begun
+        if (lane < ctas) {
+            VerifyShared* to = cluster.map_shared_rank(&sh, lane);
+            to->slices[0][slice] = mine.all;
+            if (taken) { to->slices[1][slice] = mine.p; to->slices[2][slice] = mine.q; }
+        }
+        cluster.sync();
+    }
+    // Sums of all slices, the same in all CTAs: every lane has those of `mine` consecutive ones, `before` those ahead of them
     constexpr int MOST = VF_CLUSTER * VF_WARPS / 32;
     const int mine = (slices + 31) / 32;
     double held[MOST], before = 0.0;
     auto sum_all = [&]() {
-        const double all = left_sum(left, sh, e0, e1, nullptr);
-        cluster.sync();                                    // nobody reads the last sums any more
-        if (lane < ctas) cluster.map_shared_rank(sh.slices, lane)[slice] = all;
-        cluster.sync();
         double incl = 0.0;
 #pragma unroll
         for (int k = 0; k < MOST; k++) {
-            held[k] = k < mine && lane * mine + k < slices ? sh.slices[lane * mine + k] : 0.0;
+            const int at = lane * mine + k;
+            held[k] = k >= mine || at >= slices ? 0.0 : left.what == LEFT_LESS ? fmax(fma(sh.slices[1][at], left.norm, -sh.slices[2][at]), 0.0) : sh.slices[0][at];
             incl += held[k];
         }
 #pragma unroll
@@ -389,12 +477,13 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         if (lane == 0) before = 0.0;
         return __shfl_sync(0xffffffffu, incl, 31);
     };
-    double total;
-    for (int round = 0;; round++) {
-        total = sum_all();
-        if (round == 0 && taken && total > 0.0) left.norm = 1.0 / total;               // now what the refused draft leaves
-        else if (round == 1 && !(total > 0.0)) left.norm = 0.0;                        // nothing: its distribution covers the target's
-        else break;
+    left.what = LEFT_ALL;
+    double total = sum_all();
+    if (taken && total > 0.0) {
+        left.norm = 1.0 / total; left.what = LEFT_LESS;
+        const double less = sum_all();
+        if (less > 0.0) total = less;
+        else { left.what = LEFT_ALL; sum_all(); }          // nothing: its distribution covers the target's
     }
     // ---- the first element whose running sum exceeds u * total
     if (!(total > 0.0)) {
@@ -414,36 +503,48 @@ __global__ void __launch_bounds__(VF_THREADS) k_verify(const VerifyArgs a) {
         const unsigned hits = __ballot_sync(0xffffffffu, pick >= 0), any = __ballot_sync(0xffffffffu, some >= 0);
         if (hits) { const int src = __ffs(hits) - 1; pick = __shfl_sync(0xffffffffu, pick, src); start = __shfl_sync(0xffffffffu, start, src); }
         else { pick = __shfl_sync(0xffffffffu, some, 31 - __clz(any)); start = -INFINITY; }        // rounding leaves none: the last with a weight
-        if (pick / VF_WARPS == cta) {                      // the same in the whole CTA: its warps share the slice out
-            const int p0 = (int)((long long)a.vocab * pick / slices), p1 = (int)((long long)a.vocab * (pick + 1) / slices);
-            const int f0 = p0 + (int)((long long)(p1 - p0) * warp / VF_WARPS), f1 = p0 + (int)((long long)(p1 - p0) * (warp + 1) / VF_WARPS);
-            const double part = left_sum(left, sh, f0, f1, nullptr);
-            if (lane == 0) sh.part[warp] = part;
-            __syncthreads();
-            double incl = lane < VF_WARPS ? sh.part[lane] : 0.0;
+        if (pick / WARPS == cta) {                      // the same in the whole CTA: its warps share the slice out
+            const int p0 = begin(pick), p1 = begin(pick + 1);
+            const bool share = p1 - p0 > 2 * LEFT_RUN;         // or the first warp has it alone
+            const int f0 = share ? p0 + (int)((long long)(p1 - p0) * warp / WARPS) : p0, f1 = share ? p0 + (int)((long long)(p1 - p0) * (warp + 1) / WARPS) : p1;
+            if (share) {
+                const double part = left_sum(left, sh, a.vocab, f0, f1, nullptr).all;
+                if (lane == 0) sh.part[warp] = part;
+                __syncthreads();
+            }
+            double incl = share && lane < WARPS ? sh.part[lane] : 0.0;
             const bool weighs = incl > 0.0;
 #pragma unroll
-            for (int o = 1; o < VF_WARPS; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += y; }
+            for (int o = 1; o < WARPS; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += y; }
             const unsigned over = __ballot_sync(0xffffffffu, weighs && start + incl > goal), has = __ballot_sync(0xffffffffu, weighs);
-            const int sub = over ? __ffs(over) - 1 : 31 - __clz(has);
+            const int sub = !share ? 0 : over ? __ffs(over) - 1 : 31 - __clz(has);
             const double ahead_of = __shfl_sync(0xffffffffu, incl, max(sub - 1, 0));
             if (warp == sub) {
                 double run = sub > 0 ? start + ahead_of : start;
                 int found = -1, last_one = -1;
-                for (int base = f0; base < f1 && found < 0; base += 32 * LEFT_STEPS) {
-                    left_sum(left, sh, base, min(f1, base + 32 * LEFT_STEPS), sh.held);
+                for (int base = left_aligned(left.row, f0); base < f1 && found < 0; base += LEFT_RUN) {
+                    left_sum(left, sh, a.vocab, max(base, f0), min(f1, base + LEFT_RUN), sh.held);
                     __syncwarp();
-#pragma unroll 1
-                    for (int k = 0; k < LEFT_STEPS && found < 0; k++) {
-                        const double v = sh.held[k * 32 + lane];
-                        double x = v;
+                    // a lane's elements one after the other, behind those of the lanes before it
+                    double v[LEFT_EACH], x = 0.0;
 #pragma unroll
-                        for (int o = 1; o < 32; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-                        const unsigned hit = __ballot_sync(0xffffffffu, v > 0.0 && run + x > goal), some_here = __ballot_sync(0xffffffffu, v > 0.0);
-                        if (hit) found = base + k * 32 + __ffs(hit) - 1;
-                        if (some_here) last_one = base + k * 32 + 31 - __clz(some_here);
-                        run += __shfl_sync(0xffffffffu, x, 31);
+                    for (int k = 0; k < LEFT_EACH; k++) { v[k] = sh.held[lane * LEFT_EACH + k]; x += v[k]; }
+                    double upto = x;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += y; }
+                    double ahead_here = __shfl_up_sync(0xffffffffu, upto, 1);
+                    if (lane == 0) ahead_here = 0.0;
+                    int hit = -1, some_here = -1;
+                    double sum = run + ahead_here;
+#pragma unroll
+                    for (int k = 0; k < LEFT_EACH; k++) {
+                        sum += v[k];
+                        if (v[k] > 0.0) { some_here = k; if (hit < 0 && sum > goal) hit = k; }
                     }
+                    const unsigned hits_here = __ballot_sync(0xffffffffu, hit >= 0), any_here = __ballot_sync(0xffffffffu, some_here >= 0);
+                    if (hits_here) { const int src = __ffs(hits_here) - 1; found = base + src * LEFT_EACH + __shfl_sync(0xffffffffu, hit, src); }
+                    if (any_here) { const int src = 31 - __clz(any_here); last_one = base + src * LEFT_EACH + __shfl_sync(0xffffffffu, some_here, src); }
+                    run += __shfl_sync(0xffffffffu, upto, 31);
                     __syncwarp();
                 }
                 if (lane == 0) a.next[b] = found >= 0 ? found : last_one;
@@ -524,15 +625,18 @@ static int verify_launch(const VerifyArgs& a, int sms, cudaStream_t st) {
     // CTAs of a sequence: as many as keep all of them on the device at once, down to 4 K elements each
     int ctas = 1;
     while (ctas < VF_CLUSTER && 2ll * ctas * a.n_seqs <= sms && a.vocab > 4096 * ctas) ctas *= 2;
+    // more sequences than SMs: two smaller CTAs per SM, of which one sums while the other waits
+    const bool few = a.n_seqs <= sms;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
-    cfg.gridDim = dim3(ctas, a.n_seqs); cfg.blockDim = dim3(VF_THREADS); cfg.stream = st;
+    cfg.gridDim = dim3(ctas, a.n_seqs); cfg.blockDim = dim3(few ? VF_THREADS : VF_THREADS / 2); cfg.stream = st;
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, k_verify<T>, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
+    const cudaError_t e = few ? cudaLaunchKernelEx(&cfg, k_verify<T, VF_THREADS>, a) : cudaLaunchKernelEx(&cfg, k_verify<T, VF_THREADS / 2>, a);
+    return e == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
 
 }  // namespace dkv

@@ -292,6 +292,15 @@ def test_batches(batch, shape, drawn):
     compare(a, torch.tensor(rng.choice([0.0, 0.5, 1.0], batch + 1), dtype=torch.float32, device="cuda"))
 
 
+@pytest.mark.parametrize("batch,vocab", [(200, 9001), (1100, 37), (64, 20011)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape,drawn", [("chain", True), ("tree", False)])
+def test_more_sequences_than_processors_and_long_slices(batch, vocab, dtype, shape, drawn):
+    rng = np.random.default_rng(batch)
+    a = drafts([int(x) for x in rng.integers(0, 4, batch)], vocab, dtype, shape, drawn, batch)
+    compare(a, torch.tensor(rng.choice([0.0, 0.7, 1.0], batch), dtype=torch.float32, device="cuda"))
+
+
 def test_wide_and_deep_trees():
     for width in (1, 255):                                        # a chain of 256; 255 drafts behind the root
         a = drafts([256], 500, torch.float32, "tree", False, 3, spread=1.0)
