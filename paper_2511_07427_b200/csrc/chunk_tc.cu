@@ -17,7 +17,9 @@
 // limit; cuBLAS gets 1386 TFLOP/s there).  A stage takes 3800 cycles: 2048 in the tensor pipe (52 % busy), as many for the exponentials (52 %), the
 // rest what a stream waits for the other's products and for barriers.  Tried and not kept: weights handed over in halves (830 -> 888 us), a part of the
 // exponentials as polynomials on the FMA pipe (a quarter 832, a third 862 against 827: the power that this takes), waits that poll
-// (876), logits read twice instead of kept (caps: 694 -> 912).  A unit costs 4.8 us more than its stages, two stages' worth (CT_UNIT_COST).
+// (876), logits read twice instead of kept (caps: 694 -> 912), two threads per query row (815 -> 932, caps 1265 -> 1879: 96 registers do not hold half a
+// row), weights taken before the stage's maximum is known and thrown away if it moves (818 -> 847; caps on long rows 1265 -> 1150, but documents 166 -> 183
+// and windows 268 -> 288).  A unit costs 4.8 us more than its stages, two stages' worth (CT_UNIT_COST).
 // FP8 rows turned into bf16 in the kernel: 1330 us; with their conversion left out 990.
 #include <cuda.h>
 #include <float.h>

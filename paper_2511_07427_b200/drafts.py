@@ -63,9 +63,10 @@ class PagePool:
         b, per, table, lens, add = self._tables(E, page_table, kv_len, new_len, "new_len")
         if not 0 <= n_tokens < 1 << 31:
             raise DynaKVError(f"n_tokens is {n_tokens}: expected 0 to 2^31 - 1")
-        q_start, positions, slots = E.empty(b + 1, dtype=E.i32, device=self.device), E.empty(n_tokens, dtype=E.i32, device=self.device), E.empty(n_tokens, dtype=E.i32, device=self.device)
-        _call(E, self._device, E.dynakv_pages_extend, self._ref, table, per, lens, add, b, n_tokens, q_start.data_ptr(), positions.data_ptr(), slots.data_ptr(),
-              self._status_at)
+        results = E.empty(2 * n_tokens + b + 1, dtype=E.i32, device=self.device)         # an allocation costs more than a view
+        to = results.data_ptr()
+        _call(E, self._device, E.dynakv_pages_extend, self._ref, table, per, lens, add, b, n_tokens, to + 8 * n_tokens, to, to + 4 * n_tokens, self._status_at)
+        positions, slots, q_start = results.split_with_sizes((n_tokens, n_tokens, b + 1))
         return q_start, positions, slots
 
     def trim(self, page_table, kv_len, drop) -> None:
