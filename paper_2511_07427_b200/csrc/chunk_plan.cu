@@ -102,38 +102,47 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
     const int C = (int)max(1ll, min((long long)ctas, run * a.Hk));
     for (int c0 = 0; c0 < ctas; c0 += PLAN_THREADS) {
         // the CTA's place, and that of the one behind it
-        ChunkStart st = {0, 0, 0, 0, run * a.Hk};
+        ChunkStart st = {{0, 0, 0, 0}, {0, 0, 0, 0}, run * a.Hk};
+        ChunkPlace& to = st.first;
+        int rest = 0, e0 = 0, e1 = 0;                          // stages of the unit from the place on; the sequence's tiles
         const int c = c0 + tid;
         const long long x = c < C ? mul_div(c, W, C) : W;
+        auto behind = [&]() {                                  // the unit behind
+            to.off = 0;
+            if (++to.tile == e1) {
+                if (to.head + 1 < a.Hk) { to.head++; to.tile = e0; }
+                else to.head = 0;
+            }
+        };
         if (c <= ctas && x < W) {
             auto find = [&](long long y, int lo, int hi) {     // last tile of [lo, hi) whose cost before it is <= y
                 while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (before[mid] + (long long)mid * CT_UNIT_COST <= y) lo = mid; else hi = mid; }
                 return lo;
             };
             const ChunkTile t = p.tiles[find(x / a.Hk, 0, (int)tiles)];
-            const int e0 = t.first, e1 = e0 + (t.T + per - 1) / per;
+            e0 = t.first; e1 = e0 + (t.T + per - 1) / per;
             const long long lead = before[e0] + (long long)e0 * CT_UNIT_COST, all = before[e1] + (long long)e1 * CT_UNIT_COST - lead, cost = x - lead * a.Hk;
-            st.head = (int)(cost / all);
-            const long long y = lead + cost - st.head * all;
-            st.tile = find(y, e0, e1);
-            st.off = (int)max(0ll, y - before[st.tile] - (long long)(st.tile + 1) * CT_UNIT_COST);
+            to.head = (int)(cost / all);
+            const long long y = lead + cost - to.head * all;
+            to.tile = find(y, e0, e1);
+            to.off = (int)max(0ll, y - before[to.tile] - (long long)(to.tile + 1) * CT_UNIT_COST);
             // a short unit is not cut where a CTA has several: two records and their merge cost more than what it adds to one side
-            const int whole = (int)(before[st.tile + 1] - before[st.tile]);
-            if (whole <= CT_WHOLE && (whole + CT_UNIT_COST) * 3ll * C <= W) st.off = st.off * 2 >= whole ? whole : 0;
-            st.at = before[e0] * a.Hk + st.head * (before[e1] - before[e0]) + before[st.tile] - before[e0] + st.off;
-            if (st.off == whole) {                             // the unit behind it
-                st.off = 0;
-                if (++st.tile == e1) {
-                    if (st.head + 1 < a.Hk) { st.head++; st.tile = e0; }
-                    else st.head = 0;
-                }
-            }
+            const int whole = (int)(before[to.tile + 1] - before[to.tile]);
+            if (whole <= CT_WHOLE && (whole + CT_UNIT_COST) * 3ll * C <= W) to.off = to.off * 2 >= whole ? whole : 0;
+            st.at = before[e0] * a.Hk + to.head * (before[e1] - before[e0]) + before[to.tile] - before[e0] + to.off;
+            if (to.off == whole) behind();
+            else rest = whole - to.off;
         }
         at_s[tid] = st.at;
         __syncthreads();
         if (c < ctas) {
             // up to where the next one begins; the last of a batch of CTAs (more than 1024: none has been built) finds its end in the list's
-            st.left = (int)((tid + 1 < PLAN_THREADS ? at_s[tid + 1] : run * a.Hk) - st.at);
+            to.left = (int)((tid + 1 < PLAN_THREADS ? at_s[tid + 1] : run * a.Hk) - st.at);
+            if (to.off > 0 && to.left > rest) {                // the end of a unit, and more: it comes last
+                st.late = {to.tile, to.head, to.off, rest};
+                to.left -= rest;
+                behind();
+            }
             p.starts[c] = st;
         }
         __syncthreads();
