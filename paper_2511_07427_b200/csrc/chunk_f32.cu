@@ -14,6 +14,7 @@
 #include <float.h>
 
 #include "bulk_copy.cuh"
+#include "chunk_again.cuh"
 #include "chunk_plan.cuh"
 #include "head_rows.cuh"
 #include "mma_ops.cuh"
@@ -41,6 +42,20 @@ __device__ __forceinline__ int cf_chunk(int r, int c) { return (c >> 3) * (PAGE 
 __device__ __forceinline__ float2 lo2(uint4 v) { return make_float2(__uint_as_float(v.x), __uint_as_float(v.y)); }
 __device__ __forceinline__ float2 hi2(uint4 v) { return make_float2(__uint_as_float(v.z), __uint_as_float(v.w)); }
 
+// The CTA's segments once more, by the warps that have query rows (chunk_again.cuh).
+template <int HD>
+__device__ __noinline__ void chunk_f32_again(const TreeArgs& a, const ChunkPlan& plan, int warp, int* shared) {
+    const int tokens = CF_ROWS / a.G;
+    ChunkWalk walk;
+    walk.start(plan);
+    for (ChunkSeg g; walk.next(a.Hk, tokens, plan, g);) {
+        const AgainSeg part = {g.seq, g.h, g.s0 * CF_KEYS, min(g.n, g.s1 * CF_KEYS), g.q0, g.T, g.n, g.tokens * a.G, g.first && g.last, (size_t)blockIdx.x * 2 + (g.first ? 1 : 0)};
+        chunk_segment_again<HD, DYNAKV_F32, CF_ROWS, false, CF_WARPS>(a, part, warp, shared,
+            [&](int r) { return (long long)(g.q0 + g.tile * tokens + r / a.G) * a.Hq + g.h * a.G + r % a.G; },
+            [] { asm volatile("bar.sync 1, %0;\n" ::"n"(CF_WARPS * 32) : "memory"); });
+    }
+}
+
 template <int HD>
 __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                          const __grid_constant__ TreeArgs a, const __grid_constant__ ChunkPlan plan) {
@@ -51,11 +66,12 @@ __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(row_s + CF_ROWS);
     volatile int* meta = reinterpret_cast<volatile int*>(bars + 4);                                      // [stage number mod 4] bit per page: it was loaded
     volatile int* s_abort = meta + 4;
+    volatile int* s_odd = s_abort + 1;                                                                   // rows are to be taken again
     const unsigned KFULL = smem_u32(bars), KEMPTY = KFULL + 8, VFULL = KFULL + 16, VEMPTY = KFULL + 24;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
         mbar_init(KFULL, 1); mbar_init(KEMPTY, CF_WARPS); mbar_init(VFULL, 1); mbar_init(VEMPTY, CF_WARPS);
-        *s_abort = 0;
+        *s_abort = 0; *s_odd = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     __syncthreads();
@@ -279,44 +295,9 @@ __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __
 #pragma unroll
             for (int b = 1; b < 16; b <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], b);
 #pragma unroll
-            for (int d = 0; d < 2 * C::cols; d++) wild |= !(fabsf(o[i][d].x) <= FLT_MAX) || !(fabsf(o[i][d].y) <= FLT_MAX);
+            for (int d = 0; d < 2 * C::cols; d++) wild |= !(is_number(o[i][d].x) && is_number(o[i][d].y)) && is_number(l[i]);
         }
-        if (!dead && __any_sync(0xffffffffu, wild)) {
-            // a row of V with a value that is no number has reached sums of queries that do not see it (or that do): all taken again, row by row
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-#pragma unroll
-                for (int d = 0; d < 2 * C::cols; d++) o[i][d] = make_float2(0.f, 0.f);
-            for (int pos = g.s0 * CF_KEYS; pos < min(g.n, g.s1 * CF_KEYS); pos++) {
-                const int page = a.page_table[(size_t)g.seq * a.pages_per_seq + pos / PAGE];
-                if (page < 0 || page >= a.n_pages) continue;
-                const size_t key = (((size_t)page * a.Hk + g.h) * PAGE + pos % PAGE) * HD;
-                const float* kr = reinterpret_cast<const float*>(a.kpool) + key;
-                const float* vr = reinterpret_cast<const float*>(a.vpool) + key;
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const int4 w = row_s[row0 + i];
-                    float d = 0.f;
-                    for (int e = tx; e < HD; e += 16) {
-                        float q;
-                        asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(q) : "r"(sQ + (row0 + i) * C::row_bytes + e * 4));
-                        d = fmaf(q, kr[e], d);
-                    }
-#pragma unroll
-                    for (int b = 1; b < 16; b <<= 1) d += __shfl_xor_sync(0xffffffffu, d, b);
-                    if (a.cap > 0.f) d = a.cap * CF_LOG2E * tanhf(d);
-                    if (a.slopes) d = fmaf(-__int_as_float(w.w), fabsf((float)(w.z - pos)), d);
-                    if (pos < w.x || pos >= w.y) continue;     // uniform in the 16 lanes of the row; nothing below meets other lanes
-                    const float p = exp2f(d - (m[i] == -INFINITY ? 0.f : m[i]));
-#pragma unroll
-                    for (int c = 0; c < C::cols; c++) {
-                        const float* ve = vr + 64 * c + 4 * tx;
-                        o[i][2 * c] = make_float2(fmaf(p, ve[0], o[i][2 * c].x), fmaf(p, ve[1], o[i][2 * c].y));
-                        o[i][2 * c + 1] = make_float2(fmaf(p, ve[2], o[i][2 * c + 1].x), fmaf(p, ve[3], o[i][2 * c + 1].y));
-                    }
-                }
-            }
-        }
+        if (wild) *s_odd = 1;
         if (!dead) {
 #pragma unroll
             for (int i = 0; i < 8; i++) {
@@ -345,6 +326,9 @@ __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __
         }
     }
     if (tid == 0) a.desc[(size_t)blockIdx.x * 8 + DESC_VALID] = cut_end ? 1 : 0;
+    // ---- all is done: rows whose sums are no numbers are taken again
+    asm volatile("bar.sync 1, %0;\n" ::"n"(CF_WARPS * 32) : "memory");
+    if (*s_odd && !*s_abort) chunk_f32_again<HD>(a, plan, warp, reinterpret_cast<int*>(cf_smem));
 }
 
 // Merges the records of the units that were cut: block (x = CTA in which the unit ends, y = 8 rows), a warp per row.

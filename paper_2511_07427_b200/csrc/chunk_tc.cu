@@ -27,6 +27,7 @@
 #include <type_traits>
 
 #include "bulk_copy.cuh"
+#include "chunk_again.cuh"
 #include "chunk_plan.cuh"
 #include "head_rows.cuh"
 #include "mma_ops.cuh"
@@ -143,27 +144,20 @@ __device__ __forceinline__ void tanh_long2(float2 (&x)[N], float s) {
 }
 // tanh(y) = 1 - 2 / (1 + e^2y) for any y: off by 2e-7 at most.
 __device__ __forceinline__ float tanh_far(float y) { return fmaf(-2.f, __fdividef(1.f, 1.f + ex2(2.f * CT_LOG2E * (y > 40.f ? 40.f : y))), 1.f); }
-__device__ __forceinline__ float chunk_score(const TreeArgs& a, const ChunkRow& w, float x, int key) {
-    if (a.cap > 0.f) x = a.cap * CT_LOG2E * tanhf(x);
-    if (a.slopes) x = fmaf(-w.slope, fabsf((float)(w.place - key)), x);
-    return x;
-}
 
-// Columns [col, col + 32) of a row's sums taken again, row by row with the rows that it sees: a row of V with a value that is no number
-// has reached them (0 * NaN where the row is not seen).
+// The CTA's segments once more, by the eight softmax warps (chunk_again.cuh).
 template <int HD, bool F8>
-__device__ __noinline__ void chunk_again(const TreeArgs& a, const ChunkSeg& g, const ChunkRow& w, size_t q_row, float factor, float ref, int col, float* o) {
-    constexpr int DT = F8 ? DYNAKV_FP8 : DYNAKV_BF16;
-    const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q) + q_row * HD;
-    for (int e = 0; e < 32; e++) o[e] = 0.f;
-    for (int pos = max(w.lo, g.s0 * CT_KEYS); pos < min(w.hi, g.s1 * CT_KEYS); pos++) {
-        const int page = chunk_page(a, g.seq, pos / PAGE);
-        if (page < 0) continue;
-        const long long key = ((long long)page * a.Hk + g.h) * PAGE + pos % PAGE;
-        float d = 0.f;
-        for (int e = 0; e < HD; e++) d = fmaf(__bfloat162float(q[e]), cache_elem<DT>(a.kpool, a.kexp, key, HD, e), d);
-        const float x = ex2(chunk_score(a, w, d * factor, pos) - ref);
-        for (int e = 0; e < 32; e++) o[e] = fmaf(x, cache_elem<DT>(a.vpool, a.vexp, key, HD, col + e), o[e]);
+__device__ __noinline__ void chunk_tc_again(const TreeArgs& a, const ChunkPlan& plan, int warp, int* shared) {
+    const int step = 128 / a.G;
+    ChunkWalk walk;
+    walk.start(plan);
+    for (ChunkSeg g; walk.next(a.Hk, 2 * step, plan, g);) {
+        const AgainSeg part = {g.seq, g.h, g.s0 * CT_KEYS, min(g.n, g.s1 * CT_KEYS), g.q0, g.T, g.n, CT_ROWS, g.first && g.last, (size_t)blockIdx.x * 2 + (g.first ? 1 : 0)};
+        chunk_segment_again<HD, F8 ? DYNAKV_FP8 : DYNAKV_BF16, CT_ROWS, true, 8>(a, part, warp, shared,
+            [&](int r) {
+                const int mine = (r & 127) / a.G + (r >> 7) * step;
+                return (r & 127) >= step * a.G || mine >= g.tokens ? -1ll : (long long)(g.q0 + g.tile * 2 * step + mine) * a.Hq + g.h * a.G + (r & 127) % a.G;
+            }, [] { asm volatile("bar.sync 1, 256;\n" ::: "memory"); });
     }
 }
 
@@ -180,6 +174,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
     volatile int* meta = reinterpret_cast<volatile int*>(at); at += 8 * 4;         // [stage number mod 8] bit per page: it was loaded
     volatile unsigned* s_tmem = reinterpret_cast<volatile unsigned*>(at);
     volatile int* s_abort = reinterpret_cast<volatile int*>(at + 4);
+    volatile int* s_odd = s_abort + 1;                                             // rows are to be taken again
     const unsigned sQ = tc_smem_u32(ct_smem);
     auto sK = [&](int st) { return sQ + (2 + st) * C::tile_bytes; };
     auto sV = [&](int st) { return sQ + (2 + NS + st) * C::tile_bytes; };
@@ -192,7 +187,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
             const bool full = (i >= C::KFULL && i < C::KEMPTY) || (i >= C::VFULL && i < C::VEMPTY);
             tc_mbar_init(bar(i), (full && F8) || (i >= C::PFULL && i < C::RAWFULL) ? 4 : 1);             // 4: warps
         }
-        *s_abort = 0;
+        *s_abort = 0; *s_odd = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     if (warp == 1) {
@@ -583,22 +578,15 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
             const size_t slot = (size_t)blockIdx.x * 2 + (g.first ? 1 : 0);
             if (!dead) {
                 const float norm = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+                bool wild = false;
 #pragma unroll 1
                 for (int c = 0; c < HD / 32; c++) {
                     float o[32];
                     unsigned v[32];
                     tc_ld32(tO + c * 32, v);
                     tc_ld_wait();
-                    bool wild = false;
 #pragma unroll
-                    for (int e = 0; e < 32; e++) { o[e] = __uint_as_float(v[e]); wild |= !(fabsf(o[e]) <= FLT_MAX); }
-                    if (wild && t >= 0) {
-                        float again[32];
-                        chunk_again<HD, F8>(a, g, w, q_row, MODE == CAPPED ? a.scale / a.cap : a.scale * CT_LOG2E, m == -INFINITY ? 0.f : m, c * 32, again);
-#pragma unroll
-                        for (int e = 0; e < 32; e++) o[e] = again[e];
-                    }
-                    __syncwarp();
+                    for (int e = 0; e < 32; e++) { o[e] = __uint_as_float(v[e]); wild |= !is_number(o[e]); }
                     if (t >= 0) {
                         if (whole) {
                             __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(a.out) + q_row * HD + c * 32;
@@ -620,6 +608,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                 if (t >= 0) {
                     if (!whole) a.ml[slot * CT_ROWS + s * 128 + row] = make_float2(m, l);
                     else if (a.lse) a.lse[q_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * CT_LN2;
+                    if (wild && is_number(l)) *s_odd = 1;
                 }
             }
             tc_fence_before();                                 // O has been read: the next segment's products may overwrite it
@@ -635,6 +624,9 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
             }
         }
         if (tid == 128) a.desc[(size_t)blockIdx.x * 8 + DESC_VALID] = cut_end ? 1 : 0;
+        // ---- all is done: rows whose sums are no numbers are taken again
+        asm volatile("bar.sync 1, 256;\n" ::: "memory");
+        if (*s_odd && !*s_abort) chunk_tc_again<HD, F8>(a, plan, warp - 4, reinterpret_cast<int*>(ct_smem));
     }
     // ---- everyone meets here, on every path; then the allocating warp frees the tensor memory
     __syncwarp();

@@ -36,6 +36,7 @@
 #include <type_traits>
 
 #include "bulk_copy.cuh"
+#include "chunk_again.cuh"
 #include "head_rows.cuh"
 #include "mma_ops.cuh"
 #include "tree_host.cuh"
@@ -44,6 +45,7 @@
 namespace dkv {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int PLAN_RANGE = 80;
 constexpr float VE_LOW = -60.f;            // FP8: V rows with a smaller scale take part in the reference as if they had this one
 // l * 2^d, d <= 0, where 2^d by itself may lie below fp32's range: FP8 rows' sums of weights are kept relative to a maximum that
 // has the V rows' exponents in it, so they are as far from 1 as those exponents are from another.
@@ -108,7 +110,7 @@ struct TreeCfg {
     static constexpr int exp_bytes = DT == DYNAKV_FP8 ? stages * 64 + consumers * 32 * 16 : 0;   // and a table of scales per warp
     static constexpr int q_bytes = DT == DYNAKV_F32 ? RT * HD * 4 : 0;
     static constexpr int p_bytes = DT == DYNAKV_F32 ? consumers * rows * 32 * 4 : 0;
-    static constexpr int plan_words = MOD ? 80 : 48;                         // what tree_range leaves for the walk
+    static constexpr int plan_words = MOD ? PLAN_RANGE + sizeof(Range) / 8 : 48;       // what tree_range leaves for the walk, and (MOD) the range itself
     static constexpr int fixed_bytes = 32 * 4 + 2 * stages * 8 + stages * 4 + 3 * 8 * 4 + 16 + plan_words * 8;
     static constexpr int smem = stages * stage_bytes + exp_bytes + q_bytes + p_bytes + merge_bytes + fixed_bytes;
     static_assert(stages % KG == 0, "each ring stage belongs to one page group");
@@ -177,11 +179,6 @@ template <bool MOD>
 __device__ __forceinline__ unsigned page_window(const TreeArgs& a, const Segment& g, const PageIn& p, int t, const RowScore<MOD>& s) {
     if constexpr (MOD) return s.window(p.key0);
     else return !p.mask ? ~0u : t >= 0 ? tree_window(a, g, t, p.key0) : 0u;
-}
-template <bool MOD>
-__device__ __forceinline__ bool row_sees(const TreeArgs& a, const Segment& g, int t, int j, const RowScore<MOD>& s) {
-    if constexpr (MOD) return s.lo <= j && j < s.hi;
-    else return tree_sees(a, g, t, j);
 }
 
 // ---------------------------------------------------------------------------------- mma.sync consumers (bf16, FP8)
@@ -490,22 +487,16 @@ struct MmaRows {
 #pragma unroll
             for (int x = 0; x < 2 * NR; x++) acc[nt][x] = acc[nt][x] * f0[x >> 1] + from[(nt * 2 * NR + x) * 32 + lane] * f1[x >> 1];
     }
-    // Whether a sum that is no number was met in this warp, and the sums taken back (MOD).
+    // Whether a sum of this lane's rows is no number while the sum of the row's weights is one (MOD).
     __device__ __forceinline__ bool wild() const {
         bool bad = false;
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-            for (int x = 0; x < 2 * NR; x++) bad |= !(fabsf(acc[nt][x]) <= FLT_MAX);
-        return __any_sync(0xffffffffu, bad);
+            for (int x = 0; x < 2 * NR; x++) bad |= !is_number(acc[nt][x]) && is_number(l[x >> 1]);
+        return bad;
     }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-            for (int x = 0; x < 4; x++) acc[nt][x] = 0.f;
-    }
-    // The share of a row that was left out of the MMAs: key row `row` of the pool, token j of the tree (MOD: row j of the sequence).
+    // The share of a row that was left out of the MMAs: key row `row` of the pool, token j of the tree.
     __device__ __forceinline__ void add_row(const TreeArgs& a, const Segment& g, int rg, long long row, int j, int lane) {
         const int c = lane & 3;
         float d[NR];
@@ -521,10 +512,8 @@ struct MmaRows {
         }
 #pragma unroll
         for (int i = 0; i < NR; i++)
-            if (t[i] >= 0 && row_sees<MOD>(a, g, t[i], j, score[i])) {
-                float x = d[i] * logit_factor<MOD>(a);
-                if constexpr (MOD) x = score[i].logit(a, x, j);
-                const float w = ex2(x - (m[i] == -INFINITY ? 0.f : m[i]));
+            if (t[i] >= 0 && tree_sees(a, g, t[i], j)) {
+                const float w = ex2(d[i] * (a.scale * LOG2E) - (m[i] == -INFINITY ? 0.f : m[i]));
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -789,14 +778,8 @@ struct TurnedRows {
 #pragma unroll
         for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-            for (int x = 0; x < 4; x++) bad |= !(fabsf(acc[mt][x]) <= FLT_MAX);
-        return __any_sync(0xffffffffu, bad);
-    }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-            for (int x = 0; x < 4; x++) acc[mt][x] = 0.f;
+            for (int x = 0; x < 4; x++) bad |= !is_number(acc[mt][x]) && is_number(l[x & 1]);
+        return bad;
     }
     // As in MmaRows.
     __device__ __forceinline__ void add_row(const TreeArgs& a, const Segment& g, int, long long row, int j, int lane) {
@@ -809,10 +792,8 @@ struct TurnedRows {
                 for (int e = n; e < HD; e += 8) d = fmaf(__bfloat162float(q[e]), cache_elem<DYNAKV_FP8>(a.kpool, a.kexp, row, HD, e), d);
             }
             d = sum_over_keys(d);
-            if (t[i] >= 0 && row_sees<MOD>(a, g, t[i], j, score[i])) {
-                float x = d * logit_factor<MOD>(a);
-                if constexpr (MOD) x = score[i].logit(a, x, j);
-                const float w = ex2(x - (m[i] == -INFINITY ? 0.f : m[i]));
+            if (t[i] >= 0 && tree_sees(a, g, t[i], j)) {
+                const float w = ex2(d * (a.scale * LOG2E) - (m[i] == -INFINITY ? 0.f : m[i]));
 #pragma unroll
                 for (int mt = 0; mt < MT; mt++)
 #pragma unroll
@@ -934,7 +915,8 @@ struct F32Rows {
             asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(p_s + (r * 32 + lane) * 4), "f"(w) : "memory");
         }
         __syncwarp();
-#pragma unroll 2
+        // (MOD, rows of 128: two steps at a time find no registers, 32 query rows over 4 x 4096: 190 us, one at a time 145)
+#pragma unroll (MOD && HD == 128 && NR == 16 ? 1 : 2)
         for (int k4 = 0; k4 < 8; k4++) {
             float v[4][DPL];
 #pragma unroll
@@ -992,14 +974,8 @@ struct F32Rows {
 #pragma unroll
         for (int r = 0; r < NR; r++)
 #pragma unroll
-            for (int d = 0; d < DPL; d++) bad |= !(fabsf(acc[r][d]) <= FLT_MAX);
-        return __any_sync(0xffffffffu, bad);
-    }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int r = 0; r < NR; r++)
-#pragma unroll
-            for (int d = 0; d < DPL; d++) acc[r][d] = 0.f;
+            for (int d = 0; d < DPL; d++) bad |= !is_number(acc[r][d]) && is_number(l[r]);
+        return bad;
     }
     __device__ __forceinline__ void add_row(const TreeArgs& a, const Segment& g, int rg, long long row, int j, int lane) {
         const float* k = reinterpret_cast<const float*>(a.kpool) + row * HD;
@@ -1010,9 +986,7 @@ struct F32Rows {
             for (int e = lane; e < HD; e += 32) d = fmaf(lds_f32(q_s + (r * HD + e) * 4), k[e], d);
             d = warp_sum(d);
             const int x = g.tile * C::RT + rg * NR + r, t = x / a.G;
-            const RowScore<MOD> mine = score.from_lane(r);
-            if (r < rows && row_sees<MOD>(a, g, t, j, mine)) {
-                if constexpr (MOD) d = mine.logit(a, d, j);
+            if (r < rows && tree_sees(a, g, t, j)) {
                 const float w = exp2f(d - (m[r] == -INFINITY ? 0.f : m[r]));
 #pragma unroll
                 for (int e = 0; e < DPL; e++) acc[r][e] = fmaf(w, v[lane * DPL + e], acc[r][e]);
@@ -1081,6 +1055,23 @@ __device__ __forceinline__ void mend_page(unsigned v, const Segment& g, int key0
     __syncwarp();
 }
 
+// The CTA's segments once more, by the consuming warps (chunk_again.cuh).
+template <int HD, int DT, int RG>
+__device__ __forceinline__ void tree_rows_again(const TreeArgs& a, const long long* sh, int warp, int* shared) {
+    using C = TreeCfg<HD, DT, RG, true>;
+    SegmentWalk<C::RT, true> walk(*reinterpret_cast<const Range*>(sh + PLAN_RANGE), sh);
+    for (Segment g; walk.next(a, g);) {
+        const AgainSeg part = {g.b, g.h, g.p0 * PAGE, min(g.n, g.p1 * PAGE), g.q0, g.T, g.n, min(C::RT, g.T * a.G - g.tile * C::RT), g.first && g.last, (size_t)blockIdx.x * 2 + (g.first ? 1 : 0)};
+        chunk_segment_again<HD, DT, C::RT, false, C::consumers>(a, part, warp, shared,
+            [&](int r) { const int x = g.tile * C::RT + r; return (long long)(g.q0 + x / a.G) * a.Hq + g.h * a.G + x % a.G; },
+            [] { asm volatile("bar.sync 5, %0;\n" ::"n"(C::consumers * 32) : "memory"); });
+    }
+}
+// As a call of its own, so that what it needs does not weigh on the kernel's registers.  Not for fp32 rows: with a call in it that kernel becomes slower (rows of 64,
+// 4 x 4096, 16, 32 and 64 query rows: 58, 75 and 110 us without, 63, 85 and 127 with one).
+template <int HD, int DT, int RG>
+__device__ __noinline__ void tree_rows_again_call(const TreeArgs& a, const long long* sh, int warp, int* shared) { tree_rows_again<HD, DT, RG>(a, sh, warp, shared); }
+
 template <int HD, int DT, int RG, bool MOD>
 __global__ void __launch_bounds__((TreeCfg<HD, DT, RG, MOD>::threads), (TreeCfg<HD, DT, RG, MOD>::per_sm))
 k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeArgs a) {
@@ -1111,6 +1102,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     if (tid < 24) odd[tid] = 0u;
     pdl_wait();                                            // from here on the results of earlier kernels are read
     const Range range = tree_range<C::RT, MOD>(a, KG, sh);
+    if (MOD && tid == 0) *reinterpret_cast<Range*>(sh + PLAN_RANGE) = range;
     __syncthreads();
     pdl_trigger();
     SegmentWalk<C::RT, MOD> walk(range, sh);
@@ -1219,7 +1211,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             }
             ahead = pg - g.p1;
             rows.finish();
-            if (tid < 8) odd[((seg + 1) % 3) * 8 + tid] = 0u;      // last read before the previous segment's barrier
+            if (!MOD && tid < 8) odd[((seg + 1) % 3) * 8 + tid] = 0u;      // last read before the previous segment's barrier
             if (kg > 0) rows.dump(dump + ((kg - 1) * C::groups + rg) * (C::dump_bytes / 4), lane);
             all_sync();
             if (kg == 0) {
@@ -1229,15 +1221,7 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             if (KG > 1) all_sync();                    // the boxes may be filled again
             if (kg == 0) {
                 if constexpr (MOD) {
-                    // 0 * NaN: a row of V with a value that is no number has reached sums of tokens that do not see it (or that do).  The
-                    // segment's sums are taken again, row by row, with the rows that each token sees
-                    if (rows.wild()) {
-                        rows.clear();
-                        for (int pos = g.p0 * PAGE; pos < min(g.n, g.p1 * PAGE); pos++) {
-                            const int page = a.page_table[(size_t)g.b * a.pages_per_seq + pos / PAGE];
-                            if (page >= 0 && page < a.n_pages) rows.add_row(a, g, rg, ((long long)page * a.Hk + g.h) * PAGE + pos % PAGE, pos, lane);
-                        }
-                    }
+                    if (rows.wild()) odd[0] = 1u;      // seen to when all is done
                 }
                 for (int w = 0; w < (MOD ? 0 : TREE_MAX / 32); w++) {
                     unsigned bits = odd_now[w];
@@ -1254,6 +1238,14 @@ k_tree_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             seg++;
         }
         if (tid == 0) a.desc[(size_t)blockIdx.x * 8 + DESC_VALID] = cut_end ? 1 : 0;
+        if constexpr (MOD) {
+            // all is done: rows whose sums are no numbers are taken again
+            all_sync();
+            if (odd[0] && !*reinterpret_cast<volatile int*>(s_abort)) {
+                if constexpr (F32) tree_rows_again<HD, DT, RG>(a, sh, warp, reinterpret_cast<int*>(tree_smem));
+                else tree_rows_again_call<HD, DT, RG>(a, sh, warp, reinterpret_cast<int*>(tree_smem));
+            }
+        }
     }
 }
 
