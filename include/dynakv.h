@@ -513,8 +513,8 @@ typedef struct dynakv_scores {
  * q_start[b] on, whose own rows are the LAST T_b of its kv_len[b] (token i's is P = kv_len[b] - T_b + i), stored before this call.
  *     out[i][hq] = sum_j p_j v_j / sum_j p_j,  lse[i][hq] = ln sum_j p_j,  p_j = exp(s_j)
  * over the rows that the token sees; one that sees none gets zeros and -infinity.  Rows it does not see do not count whatever they
- * hold, NaN and infinities included (values that are no numbers among the V rows that are read make the call slow).  Logits, sums and
- * outputs are accumulated in fp32.  Weights enter the products with V in fp32 (DYNAKV_F32); with more than 32 query rows per KV head (max_chunk *
+ * hold, NaN and infinities included (values among the V rows that are read that are no numbers, or beyond 2^76 or so, make the call
+ * slow).  Logits, sums and outputs are accumulated in fp32.  Weights enter the products with V in fp32 (DYNAKV_F32); with more than 32 query rows per KV head (max_chunk *
  * n_heads / n_kv_heads; head_dim 64: 64) as bf16, each off by 2^-8 of itself at most; with fewer as for dynakv_attend_tree.
  * n_heads is 1 to 8 times n_kv_heads; max_chunk 1 .. 2^24.  Tokens of no sequence are left as they were.
  * workspace: dynakv_attend_chunk_workspace() bytes of device memory, 16-byte aligned, contents of no interest before and after;

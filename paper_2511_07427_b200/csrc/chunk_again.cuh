@@ -1,7 +1,7 @@
 // Query rows of dynakv_attend_chunk that are taken again by themselves.
 //
 // The kernels multiply a tile's weights with all rows of V of a stage, so that 0 * NaN reaches the sums of query rows that do not see
-// the row of V in which the NaN lies.  (0 * infinity does too, and sums may leave fp32 although the result fits it.)  While they walk over their
+// the row of V in which the NaN lies.  (0 * infinity does too, and sums of large values may leave fp32 although the result fits it.)  While they walk over their
 // segments they only note that it happened.  A CTA that has a note goes over its segments once more when all of them are done and no copy, product or
 // wait is left: rows whose values are no numbers, in out or in a record, are taken again, a warp per row, from the rows that the query sees
 // alone.  (Done between two units it kept the warps that load and multiply waiting beyond the limit of their waits, from some tens of thousands
@@ -18,7 +18,9 @@
 namespace dkv {
 
 __device__ __forceinline__ bool is_number(float x) { return fabsf(x) <= FLT_MAX; }
-constexpr float AGAIN_FAR = 0x1p100f;              // sums of a record up to here: those of all records of a unit stay in fp32's range
+// A record's sums are as good as none from here on, because those of all records of a unit together might leave fp32's range.
+constexpr float AGAIN_FAR = 0x1p100f;
+__device__ __forceinline__ bool far_out(float x) { return !(fabsf(x) <= AGAIN_FAR); }
 
 // This lane's HD / 32 consecutive elements of a row of the pool, FP8 without the row's scale.
 template <int HD, int DT>
@@ -61,7 +63,7 @@ __device__ __forceinline__ unsigned odd_values(const TreeArgs& a, const AgainSeg
     for (int e = 0; e < E; e++) {
         const size_t at = (size_t)place * HD + lane * E + e;
         const float x = !g.whole ? record_part<HD, RT, COLS>(a, g.slot, row, lane)[e] : DT == DYNAKV_F32 ? reinterpret_cast<const float*>(a.out)[at] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.out)[at]);
-        if (!is_number(x)) bits |= 1u << e;
+        if (g.whole ? !is_number(x) : far_out(x)) bits |= 1u << e;
     }
     return bits;
 }
@@ -156,7 +158,7 @@ __device__ __forceinline__ void chunk_row_again(const TreeArgs& a, const AgainSe
         float by = 0.f;
         bool far = false;
 #pragma unroll
-        for (int e = 0; e < E; e++) far |= is_number(o[e]) && fabsf(o[e] * was.y) > AGAIN_FAR;
+        for (int e = 0; e < E; e++) far |= is_number(o[e]) && far_out(o[e] * was.y);
         if (__any_sync(0xffffffffu, far) && was.y > 0.f) by = (float)(ilogbf(was.y) + 11);
         const float sum = was.y * exp2f(-by);
         float* to = record_part<HD, RT, COLS>(a, g.slot, row, lane);

@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __
 #pragma unroll
             for (int b = 1; b < 16; b <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], b);
 #pragma unroll
-            for (int d = 0; d < 2 * C::cols; d++) wild |= !(is_number(o[i][d].x) && is_number(o[i][d].y)) && is_number(l[i]);
+            for (int d = 0; d < 2 * C::cols; d++) wild |= (far_out(o[i][d].x) || far_out(o[i][d].y)) && is_number(l[i]);
         }
         if (wild) *s_odd = 1;
         if (!dead) {

@@ -586,7 +586,7 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
                     tc_ld32(tO + c * 32, v);
                     tc_ld_wait();
 #pragma unroll
-                    for (int e = 0; e < 32; e++) { o[e] = __uint_as_float(v[e]); wild |= !is_number(o[e]); }
+                    for (int e = 0; e < 32; e++) { o[e] = __uint_as_float(v[e]); wild |= far_out(o[e]); }
                     if (t >= 0) {
                         if (whole) {
                             __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(a.out) + q_row * HD + c * 32;

@@ -487,13 +487,13 @@ struct MmaRows {
 #pragma unroll
             for (int x = 0; x < 2 * NR; x++) acc[nt][x] = acc[nt][x] * f0[x >> 1] + from[(nt * 2 * NR + x) * 32 + lane] * f1[x >> 1];
     }
-    // Whether a sum of this lane's rows is no number while the sum of the row's weights is one (MOD).
+    // Whether a sum of this lane's rows is no number, or near the end of fp32, while the sum of the row's weights is one (MOD).
     __device__ __forceinline__ bool wild() const {
         bool bad = false;
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-            for (int x = 0; x < 2 * NR; x++) bad |= !is_number(acc[nt][x]) && is_number(l[x >> 1]);
+            for (int x = 0; x < 2 * NR; x++) bad |= far_out(acc[nt][x]) && is_number(l[x >> 1]);
         return bad;
     }
     // The share of a row that was left out of the MMAs: key row `row` of the pool, token j of the tree.
@@ -778,7 +778,7 @@ struct TurnedRows {
 #pragma unroll
         for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-            for (int x = 0; x < 4; x++) bad |= !is_number(acc[mt][x]) && is_number(l[x & 1]);
+            for (int x = 0; x < 4; x++) bad |= far_out(acc[mt][x]) && is_number(l[x & 1]);
         return bad;
     }
     // As in MmaRows.
@@ -974,7 +974,7 @@ struct F32Rows {
 #pragma unroll
         for (int r = 0; r < NR; r++)
 #pragma unroll
-            for (int d = 0; d < DPL; d++) bad |= !is_number(acc[r][d]) && is_number(l[r]);
+            for (int d = 0; d < DPL; d++) bad |= far_out(acc[r][d]) && is_number(l[r]);
         return bad;
     }
     __device__ __forceinline__ void add_row(const TreeArgs& a, const Segment& g, int rg, long long row, int j, int lane) {

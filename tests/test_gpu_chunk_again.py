@@ -187,3 +187,19 @@ def test_a_long_prompt_is_slow_but_comes_to_an_end():
     assert bool((away <= 2.0 ** -6 * clean.float().abs() + 2.0 ** -6).all())
     for u in undo:
         u()
+
+
+@pytest.mark.parametrize("cache", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,new", [([5000, 300], [1, 1]), ([5000, 300], [3, 3]), ([3000, 300], [8, 2]), ([5000, 300], [200, 100]), ([900, 40, 9000], [900, 40, 30])])
+def test_values_near_the_end_of_fp32(cache, d, lens, new):
+    """V of one sign around 2^120: the sum of the weighted rows leaves fp32, the weighted mean does not."""
+    p = Strict(lens, new, 8, 2, d, cache, seed=9)
+    if cache == "fp8":
+        p.c.v.view(torch.uint8).bitwise_and_(0x7f)
+        p.c.v_exp += 118                                          # about 2^-8 for these rows
+    else:
+        p.c.v.abs_().mul_(2.0 ** 120)
+    p.check(*p.run())
+    p.check(*p.run(window=500), window=500)
+    p.check(*p.run(softcap=3.0), softcap=3.0)
