@@ -37,7 +37,7 @@ static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int n_seqs, 
     if (most > chunk_few(c)) {
         const int G = n_heads / c->n_kv_heads;
         return {true, 0, f32 ? CF_ROWS : CT_ROWS, sms, f32 ? CF_ROWS / G : tile_tokens(G),
-                c->kv_dtype == DYNAKV_FP8 && max_chunk > 2 * tile_tokens(G) && n_seqs <= 65535 && c->n_kv_heads <= 65535 && chunk_wide_bytes(c, n_seqs, pages_per_seq) <= CHUNK_WIDE};
+                c->kv_dtype == DYNAKV_FP8 && max_chunk > 2 * tile_tokens(G) && pages_per_seq > 0 && n_seqs <= 65535 && c->n_kv_heads <= 65535 && chunk_wide_bytes(c, n_seqs, pages_per_seq) <= CHUNK_WIDE};
     }
     const int rg = row_groups(most, f32);
     return {false, rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2), 0, false};
