@@ -516,7 +516,7 @@ typedef struct dynakv_scores {
  * hold, NaN and infinities included (values among the V rows that are read that are no numbers, or beyond 2^76 or so, make the call
  * slow).  Logits, sums and outputs are accumulated in fp32.  Weights enter the products with V in fp32 (DYNAKV_F32); with more than 32 query rows per KV head (max_chunk *
  * n_heads / n_kv_heads; head_dim 64: 64) as bf16, each off by 2^-8 of itself at most; with fewer as for dynakv_attend_tree.
- * n_heads is 1 to 8 times n_kv_heads; max_chunk 1 .. 2^24.  Tokens of no sequence are left as they were.
+ * n_heads is 1 to 8 times n_kv_heads; max_chunk 1 .. 2^24; pages_per_seq at most 2^25.  Tokens of no sequence are left as they were.
  * workspace: dynakv_attend_chunk_workspace() bytes of device memory, 16-byte aligned, contents of no interest before and after;
  * calls that may overlap need one each. */
 int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,

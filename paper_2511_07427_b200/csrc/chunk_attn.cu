@@ -58,9 +58,12 @@ static ChunkSpace chunk_space(const dynakv_row_cache* c, const ChunkKind& k, int
     return s;
 }
 
+// Rows of a sequence and windows up to 2^30, so that sums of two of them, and of a stage more, stay in 32 bits.
+constexpr int CHUNK_COLUMNS = (1 << 30) / PAGE;
+
 static bool chunk_shape_ok(const dynakv_row_cache* c, int n_heads, int64_t n_tokens, int n_seqs, int max_chunk, int pages_per_seq) {
     return row_cache_ok(c) && n_heads >= 1 && n_heads % c->n_kv_heads == 0 && n_heads / c->n_kv_heads <= MAX_G && max_chunk >= 1 && max_chunk <= (1 << 24) &&
-           n_tokens >= 0 && n_tokens < (1ll << 31) && n_seqs >= 0 && pages_per_seq >= 0 && pages_per_seq < (1 << 26);
+           n_tokens >= 0 && n_tokens < (1ll << 31) && n_seqs >= 0 && pages_per_seq >= 0 && pages_per_seq <= CHUNK_COLUMNS;
 }
 
 }  // namespace dkv
