@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __
     // =============================== 16 query rows per warp ===============================
     regs_up<C::regs_sums>();
     const int tx = lane & 15, row0 = warp * 16 + (lane >> 4) * 8;               // this thread's 8 rows; keys tx + 16 j; columns 4 tx and 64 + 4 tx
-    const float factor = a.cap > 0.f ? a.scale / a.cap : a.scale * CF_LOG2E;
+    const float2 factors = chunk_factor(a);
+    const float factor = factors.x;
     int n = 0;
     bool dead = false, cut_end = false;
     auto wait = [&](unsigned b, int phase) {
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(F32Chunk<HD>::threads, 1) k_chunk_f32(const __
 #pragma unroll
                 for (int i = 0; i < 8; i++)
 #pragma unroll
-                    for (int j = 0; j < 4; j++) x[i][j] = a.cap * CF_LOG2E * tanhf(x[i][j]);
+                    for (int j = 0; j < 4; j++) x[i][j] = a.cap * CF_LOG2E * tanhf(x[i][j] * factors.y);
             }
             if (a.slopes) {
 #pragma unroll

@@ -57,6 +57,14 @@ __device__ __forceinline__ void chunk_sees(const TreeArgs& a, int token, int pla
     hi = max(0, min(a.rows_to ? a.rows_to[token] : place + 1, n));
 }
 
+// The factor of the logits in two, one for fp32 queries before their products with keys and one for the products: with a cap it may be anything from 2^-127 to
+// 2^127, and ordinary queries times that leave fp32.  The second is 1 but for such.
+__device__ __forceinline__ float2 chunk_factor(const TreeArgs& a) {
+    if (!(a.cap > 0.f)) return make_float2(a.scale * 1.4426950408889634f, 1.f);
+    const float f = a.scale / a.cap, first = copysignf(fminf(fmaxf(fabsf(f), 0x1p-40f), 0x1p40f), f);
+    return make_float2(first, f / first);
+}
+
 // The page of a sequence's column: its place in the pool, -1 where the table names none.
 __device__ __forceinline__ int chunk_page(const TreeArgs& a, int seq, int column) {
     const int id = a.page_table[(size_t)seq * a.pages_per_seq + column];

@@ -862,7 +862,7 @@ struct F32Rows {
         for (int x = lane; x < NR * HD; x += 32) {
             const int r = g.tile * C::RT + rg * NR + x / HD, t = r / a.G;
             const float* q = reinterpret_cast<const float*>(a.q) + ((size_t)(g.q0 + t) * a.Hq + g.h * a.G + r - t * a.G) * HD;
-            q_s[x] = t < g.T ? __ldg(q + x % HD) * logit_factor<MOD>(a) : 0.f;
+            q_s[x] = t < g.T ? __ldg(q + x % HD) * (MOD ? chunk_factor(a).x : a.scale * LOG2E) : 0.f;
         }
     }
     __device__ __forceinline__ void page(const TreeArgs& a, const Segment& g, const PageIn& p, int lane, int rg) {
@@ -891,8 +891,9 @@ struct F32Rows {
             win = page_window<MOD>(a, g, p, 0, score);
             mask = __any_sync(0xffffffffu, win != ~0u);
             if (a.cap > 0.f || a.slopes) {
+                const float rest = chunk_factor(a).y;
 #pragma unroll
-                for (int r = 0; r < NR; r++) s[r] = score.from_lane(r).logit(a, s[r], p.key0 + lane);
+                for (int r = 0; r < NR; r++) s[r] = score.from_lane(r).logit(a, s[r] * rest, p.key0 + lane);
             }
         } else if (p.mask) {
             const int x = g.tile * C::RT + rg * NR + (lane & (NR - 1)), t = x / a.G;
