@@ -576,7 +576,7 @@ int dynakv_pages_trim(const dynakv_page_pool* pool, int32_t* page_table, int32_t
  * kept [n_seqs]: tokens of the accepted path, the root included; dropped [n_seqs]: the others; path [n_seqs][max_tree]: the places in the
  * tree of the kept ones, upward from 0, then -1; next_token [n_seqs], -1 where no token has a weight.  A sequence without tokens gets 0, 0, -1, -1, one whose range
  * is none of n_tokens or longer than max_tree 0, -1, -1, -1.  A token outside the vocabulary is never accepted.  n_tokens < 2^24, n_seqs <= 65535, vocab <= 2^26.
- * Acceptance is decided on sums of fp32 exponentials (relative error below 1e-6), the next token on 64-bit sums.
+ * Everything is decided as sums in 64 bits decide it (acceptance on sums of fp32 exponentials where their error leaves no doubt).
  * workspace: dynakv_verify_drafts_workspace() bytes, 16-byte aligned; calls that may overlap need one each. */
 int dynakv_verify_drafts(const void* logits, int64_t logits_stride, int32_t logits_dtype, int64_t n_tokens, int32_t vocab, const int32_t* tokens,
                          const int32_t* q_start, int32_t n_seqs, int32_t max_tree, const float* uniform, const float* temperature,

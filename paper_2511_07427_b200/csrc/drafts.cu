@@ -6,8 +6,8 @@
 // the token that is drawn at the end, all up to a factor that is carried along.  A draft that was not drawn has q = 1 at x, so that what is
 // left is p without x.
 //   k_row_stats: the one pass over the logits, HBM bound: (largest, first place of it, sum of exp) of every row, in pieces.
-//   k_verify, a cluster of CTAs per sequence: every draft's test from those and one logit, at once for all drafts; the walk in shared
-//     memory; then the drawing from the last kept token's row, which is by inverse sums in 64 bits: among 10^5 tokens fp32 sums
+//   k_verify, a cluster of CTAs per sequence: every draft's test from those and one logit, at once for all drafts (and from sums in 64 bits where
+//     they leave it open); the walk in shared memory; then the drawing from the last kept token's row, which is by inverse sums in 64 bits: among 10^5 tokens fp32 sums
 //     misplace the draw with a chance of about 10^-3, and the same numbers have to give the same token however the sums are split.
 // Measured, calls one after the other: 64 sequences of 6 tokens over 128256, drafts drawn, 52 us: 22 for the rows, 6 until the walk is done, 16
 // for the sums (36 instructions an element, 11 of them in 64 bits; 128 CTAs; in two passes, the target's sum first, 31), 6 for the place of
@@ -201,6 +201,10 @@ __device__ __forceinline__ void exp2_64(const float (&l)[N], double top, double 
 // The logit below which a weight is 0: rounded up, to the largest one at most, so that no weight is below 2^-1000, the largest never left out, and -infinity always.
 __device__ __forceinline__ float lowest_logit(double top, double scale_inv) { return __double2float_ru(top - 1000.0 * scale_inv); }
 
+// What a row's sum of fp32 exponentials may be off by, relative to it: logits minus the largest times 1 / temperature carry three roundings and the factor's own,
+// 4 2^-24 of an exponent of at most 26 where the weight of up to 2^26 tokens lies (times ln 2: 72 2^-24), ex2 2^-22 and some 50 additions 2^-24 each.
+constexpr double SUM_OFF = 0x1p-16;
+
 constexpr int LEFT_EACH = 8, LEFT_RUN = 32 * LEFT_EACH;     // elements of a lane and of a warp at a time
 
 struct VerifyShared {
@@ -209,6 +213,8 @@ struct VerifyShared {
     int best[TREE_MAX];                            //         first place of it
     int token[TREE_MAX], up[TREE_MAX], first[TREE_MAX];
     unsigned char again[TREE_MAX];                 // an older sibling has the same token
+    unsigned char out[TREE_MAX];                   // drafts whose tokens are refused
+    unsigned unsure[TREE_MAX / 32];                // bit per draft: its test needs the sum in 64 bits
     double table[EXP_TABLE * 16];
     double slices[3][VF_CLUSTER * VF_WARPS], part[VF_WARPS];
     double held[LEFT_RUN];                  // weights of the run in which the drawn token lies
@@ -290,7 +296,7 @@ __device__ __noinline__ LeftSums left_sum(const RowLeft<T> a, const VerifyShared
             for (int k = 0; k < LEFT_EACH; k++) if (at + k < from || at + k >= end) { now[k] = -INFINITY; minus[k] = 0.f; }
         }
         for (int r = 0; r < a.refused; r++) {              // a refused token weighs nothing
-            const int off = sh.token[sh.first[r]] - at;
+            const int off = sh.token[sh.out[r]] - at;
             if (!__any_sync(0xffffffffu, (unsigned)off < (unsigned)LEFT_EACH)) continue;
 #pragma unroll
             for (int k = 0; k < LEFT_EACH; k++) if (off == k) now[k] = -INFINITY;
@@ -385,6 +391,7 @@ __global__ void __launch_bounds__(THREADS) k_verify(const VerifyArgs a) {
         if (up[e] < 0 || up[e] >= i) up[e] = -1;           // a draft without a parent before it is never reached
         if (i < n) { sh.token[i] = token[e]; sh.up[i] = up[e]; sh.first[i] = n; }
     }
+    if (tid < TREE_MAX / 32) sh.unsure[tid] = 0u;
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < EACH; e++) {
@@ -402,18 +409,42 @@ __global__ void __launch_bounds__(THREADS) k_verify(const VerifyArgs a) {
     for (int e = 0; e < EACH; e++) {
         const int i = tid + e * THREADS, x = token[e], above = up[e];
         if (above < 0) continue;
-        bool pass;
+        bool pass = false;
         if (!draws) pass = sh.best[above] == x && sh.top[above] > -INFINITY;
-        else if (a.draft) pass = x >= 0 && x < a.vocab && (double)chance[e] * (double)a.draft[(long long)(q0 + i) * a.draft_stride + x] * sh.sum[above] < sh.weight[i];
-        else {
-            double left = sh.sum[above];
-            if (a.parent) for (int s = above + 1; s < i; s++) if (sh.up[s] == above && !sh.again[s]) left -= sh.weight[s];
-            pass = !sh.again[i] && (double)chance[e] * left < sh.weight[i];
+        else if (sh.weight[i] > 0.0 && !sh.again[i]) {
+            double left = sh.sum[above], part = (double)chance[e];
+            const double off = left * SUM_OFF;
+            if (a.draft) part *= (double)a.draft[(long long)(q0 + i) * a.draft_stride + x];
+            else if (a.parent) for (int s = above + 1; s < i; s++) if (sh.up[s] == above && !sh.again[s]) left -= sh.weight[s];
+            pass = part * (left + off) < sh.weight[i];
+            if (!pass && part * (left - off) < sh.weight[i]) atomicOr(&sh.unsure[i >> 5], 1u << (i & 31));
         }
         if (pass) atomicMin(&sh.first[above], i);
     }
     if (tid == 0) sh.refused = 0;
     __syncthreads();
+    // ---- tests that lie within the error of the sums (next to never; or where older siblings have nearly all of the weight): the row once more in 64 bits, without
+    // the older siblings' tokens, by every CTA for itself
+    for (int k = 0; k < n; k += 32) for (unsigned open = sh.unsure[k >> 5]; open; open &= open - 1) {          // the same in the whole cluster
+        const int i = k + __ffs(open) - 1, above = sh.up[i];
+        if (tid == 0) {
+            int count = 0;
+            if (!a.draft) for (int s = above + 1; s < i; s++) if (sh.up[s] == above && !sh.again[s]) sh.out[count++] = (unsigned char)s;
+            sh.found = count;
+        }
+        __syncthreads();
+        const RowLeft<T> row = {logits + (long long)(q0 + above) * a.stride, nullptr, (double)sh.top[above], scale, scale_inv, 0.0, 0.0, sh.found, LEFT_ALL};
+        const double mine = left_sum(row, sh, a.vocab, (int)((long long)a.vocab * warp / WARPS), (int)((long long)a.vocab * (warp + 1) / WARPS), nullptr).all;
+        if (lane == 0) sh.part[warp] = mine;
+        __syncthreads();
+        if (tid == 0) {
+            double left = 0.0, part = (double)a.uniform[q0 + i];
+            for (int k = 0; k < WARPS; k++) left += sh.part[k];
+            if (a.draft) part *= (double)a.draft[(long long)(q0 + i) * a.draft_stride + sh.token[i]];
+            if (part * left < sh.weight[i]) sh.first[above] = min(sh.first[above], i);
+        }
+        __syncthreads();
+    }
     // ---- the walk
     if (tid == 0) {
         int at = 0, kept = 1;
@@ -436,14 +467,14 @@ __global__ void __launch_bounds__(THREADS) k_verify(const VerifyArgs a) {
     }
     // ---- the token behind the last kept one.  Its refused children: their tokens are out, or (drawn) the one child's distribution is taken off
 #pragma unroll
-    for (int e = 0; e < EACH; e++) if (up[e] == last) sh.first[atomicAdd(&sh.refused, 1)] = tid + e * THREADS;         // the links are not needed any more
+    for (int e = 0; e < EACH; e++) if (up[e] == last) sh.out[atomicAdd(&sh.refused, 1)] = (unsigned char)(tid + e * THREADS);
     __syncthreads();
     const int refused = sh.refused;
     const bool taken = a.draft && refused > 0;
     const int slice = cta * WARPS + warp, slices = ctas * WARPS, shift = __ffs(slices) - 1;         // a power of two
     auto begin = [&](int x) { return (int)((long long)a.vocab * x >> shift); };
     const int e0 = begin(slice), e1 = begin(slice + 1);
-    RowLeft<T> left = {logits + (long long)(q0 + last) * a.stride, taken ? a.draft + (long long)(q0 + sh.first[0]) * a.draft_stride : nullptr,
+    RowLeft<T> left = {logits + (long long)(q0 + last) * a.stride, taken ? a.draft + (long long)(q0 + sh.out[0]) * a.draft_stride : nullptr,
                        (double)sh.top[last], scale, scale_inv, taken ? 1.0 / sh.sum[last] : 0.0, 0.0, a.draft ? 0 : refused, taken ? LEFT_SUMS : LEFT_ALL};
     if (lane == 0) {                                       // both rows on their way: the sums have too few loads under way to wait for HBM
         prefetch_l2(left.row + e0, (size_t)(e1 - e0) * sizeof(T));
