@@ -224,7 +224,9 @@ struct VerifyShared {
 // What is left of a row's distribution: its weights without the tokens of `refused` children, or (a refused draft that was drawn from q)
 // max(weight / S - q, 0), S the sum of the weights.  Which elements of the latter are not 0 is decided with S as fp32 sums give it (near = 1 / S): the
 // others' sums P and Q can then be taken in the pass that finds S in 64 bits, and P / S - Q is off by what such elements as lie within 1e-6 of 0 add,
-// where each adds next to nothing.
+// where each adds next to nothing.  Where what is left is itself little (LEFT_LITTLE: a draft drawn from nearly the target's distribution, which is refused as seldom) that is
+// not nothing, and the elements are gone over once more with S in 64 bits.
+constexpr double LEFT_LITTLE = 0x1p-10;
 enum { LEFT_ALL = 0, LEFT_LESS = 1, LEFT_SUMS = 2 };       // weights; max(weight norm - q, 0); all three sums
 template <typename T>
 struct RowLeft {
@@ -494,12 +496,13 @@ __global__ void __launch_bounds__(THREADS) k_verify(const VerifyArgs a) {
     constexpr int MOST = VF_CLUSTER * VF_WARPS / 32;
     const int mine = (slices + 31) / 32;
     double held[MOST], before = 0.0;
-    auto sum_all = [&]() {
+    // kind LEFT_ALL: the weights, LEFT_LESS: P / S - Q, LEFT_SUMS: what the slices hold in place of P
+    auto sum_all = [&](int kind) {
         double incl = 0.0;
 #pragma unroll
         for (int k = 0; k < MOST; k++) {
             const int at = lane * mine + k;
-            held[k] = k >= mine || at >= slices ? 0.0 : left.what == LEFT_LESS ? fmax(fma(sh.slices[1][at], left.norm, -sh.slices[2][at]), 0.0) : sh.slices[0][at];
+            held[k] = k >= mine || at >= slices ? 0.0 : kind == LEFT_LESS ? fmax(fma(sh.slices[1][at], left.norm, -sh.slices[2][at]), 0.0) : sh.slices[kind == LEFT_ALL ? 0 : 1][at];
             incl += held[k];
         }
 #pragma unroll
@@ -509,12 +512,20 @@ __global__ void __launch_bounds__(THREADS) k_verify(const VerifyArgs a) {
         return __shfl_sync(0xffffffffu, incl, 31);
     };
     left.what = LEFT_ALL;
-    double total = sum_all();
+    double total = sum_all(LEFT_ALL);
     if (taken && total > 0.0) {
         left.norm = 1.0 / total; left.what = LEFT_LESS;
-        const double less = sum_all();
+        double less = sum_all(LEFT_LESS);
+        if (less < LEFT_LITTLE) {                          // the same in the whole cluster
+            left.near = left.norm;
+            const double exact = left_sum(left, sh, a.vocab, e0, e1, nullptr).all;
+            cluster.sync();                                // the sums have been read
+            if (lane < ctas) cluster.map_shared_rank(&sh, lane)->slices[1][slice] = exact;
+            cluster.sync();
+            less = sum_all(LEFT_SUMS);
+        }
         if (less > 0.0) total = less;
-        else { left.what = LEFT_ALL; sum_all(); }          // nothing: its distribution covers the target's
+        else { left.what = LEFT_ALL; sum_all(LEFT_ALL); }  // nothing: its distribution covers the target's
     }
     // ---- the first element whose running sum exceeds u * total
     if (!(total > 0.0)) {

@@ -79,3 +79,27 @@ def test_many_open_tests_in_one_tree():
         a = dict(logits=logits, tokens=tokens, q_start=ints([0, n]), max_tree=n, parent=ints([-1] + [0] * 255), draft_probs=None, uniform=torch.tensor(u, device="cuda"))
         kept, _, path, _ = compare(a, torch.ones(1, device="cuda"))
         assert int(kept) == (1 if above else 2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,moved", [(50257, 1e-5), (4001, 1e-5), (4001, 1e-3), (128256, 1e-4)])
+def test_a_draft_that_was_drawn_from_nearly_the_target(dtype, vocab, moved):
+    """q is the target's own softmax in fp32 but for a little weight moved onto the draft: what a refused draft leaves is that little and the roundings of q."""
+    batch = 48
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    logits = (2.0 * torch.randn(2 * batch, vocab, generator=g, device="cuda")).to(dtype)
+    q = torch.softmax(logits.float(), -1)[::2].repeat_interleave(2, 0)
+    x = torch.randint(vocab, (batch,), generator=g, device="cuda")
+    rows = torch.arange(batch, device="cuda")
+    from_ = q[1::2].argmax(-1)
+    from_ = torch.where(from_ == x, (from_ + 1) % vocab, from_)
+    q[1 + 2 * rows, from_] -= moved
+    q[1 + 2 * rows, x] += moved
+    tokens = torch.stack([torch.zeros_like(x), x], 1).view(-1).to(torch.int32)
+    u = torch.rand(2 * batch, generator=g, device="cuda")
+    u[1::2] = LAST
+    a = dict(logits=logits, tokens=tokens, q_start=ints(2 * np.arange(batch + 1)), max_tree=2, parent=None, draft_probs=q.contiguous(), uniform=u)
+    for seed in range(4):
+        u[0::2] = torch.rand(batch, generator=g, device="cuda")
+        kept, _, _, _ = compare(a, torch.ones(batch, device="cuda"))
+        assert int((kept == 1).sum()) > batch // 2
