@@ -525,8 +525,9 @@ int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_
                         uint32_t* status, void* cuda_stream);
 
 /* Bytes of workspace for calls of n_tokens tokens in n_seqs sequences of pages_per_seq pages with this cache, n_heads and max_chunk on the current
- * device, or a negative code.  Records of some 40 MB, and for long chunks over FP8 rows (more than 2 tiles of 256 query rows) all rows that the page table
- * can name as bf16, up to 2 GB; where that is not enough, rows are turned into bf16 as they are read, which is slower. */
+ * device, or a negative code.  Records of some 40 MB, and for long chunks over FP8 rows (more than 2 tiles of 256 query rows) room for rows as bf16: as many
+ * pages as the page table can name or the cache has, 2 GB at most.  Batches that have more rows than that (one page in several sequences, long caches)
+ * have them turned into bf16 as they are read, which is slower. */
 int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, int32_t n_heads, int64_t n_tokens, int32_t n_seqs, int32_t max_chunk,
                                       int32_t pages_per_seq);
 

@@ -28,32 +28,35 @@ static int chunk_launch_rows(int rg, const CUtensorMap& mk, const CUtensorMap& m
 //   4 x 16384 (fp32: 4096), d = 64   40 / 61   64 / 61   65 / 61  112 / 62 |    43 / 71   70 / 71   72 / 71  126 / 72 |      76 / 112  112 / 112  190 / 114
 //   16 x 2048, d = 64                24 / 38   33 / 38   35 / 38   57 / 39 |    26 / 43   37 / 43   40 / 43   64 / 44 |     126 / 192  200 / 192  360 / 195
 static int chunk_few(const dynakv_row_cache* c) { return c->head_dim == 128 ? 32 : 64; }
-// From three tiles per sequence on FP8 rows are turned into bf16 first (chunk_tc.cu), unless that takes more than CHUNK_WIDE bytes.
+// From three tiles per sequence on FP8 rows are turned into bf16 first (chunk_tc.cu).  There is room for as many pages as the table can name or the cache has, in
+// CHUNK_WIDE bytes at most; the plan counts how many the sequences have, and where those are more (the same page in many sequences; long caches) the rows are turned
+// into bf16 as they are read.
 constexpr size_t CHUNK_WIDE = (size_t)2 << 30;
-struct ChunkKind { bool planned; int rg, rows, ctas, per; bool wide; };             // per: tokens of a planned tile
+struct ChunkKind { bool planned; int rg, rows, ctas, per; long long wide; };        // per: tokens of a planned tile; wide: pages turned into bf16 at most, 0: none
 static ChunkKind chunk_kind(const dynakv_row_cache* c, int n_heads, int n_seqs, int max_chunk, int pages_per_seq, int sms) {
     const bool f32 = c->kv_dtype == DYNAKV_F32;
     const int most = (int)min(1000ll, (long long)max_chunk * (n_heads / c->n_kv_heads));
     if (most > chunk_few(c)) {
         const int G = n_heads / c->n_kv_heads;
-        return {true, 0, f32 ? CF_ROWS : CT_ROWS, sms, f32 ? CF_ROWS / G : tile_tokens(G),
-                c->kv_dtype == DYNAKV_FP8 && max_chunk > 2 * tile_tokens(G) && pages_per_seq > 0 && n_seqs <= 65535 && c->n_kv_heads <= 65535 && chunk_wide_bytes(c, n_seqs, pages_per_seq) <= CHUNK_WIDE};
+        const long long table = (long long)n_seqs * pages_per_seq;
+        const bool wide = c->kv_dtype == DYNAKV_FP8 && max_chunk > 2 * tile_tokens(G) && n_seqs <= 65535 && c->n_kv_heads <= 65535;
+        return {true, 0, f32 ? CF_ROWS : CT_ROWS, sms, f32 ? CF_ROWS / G : tile_tokens(G), wide ? min(min(table, (long long)c->n_pages), (long long)(CHUNK_WIDE / chunk_wide_page(c))) : 0};
     }
     const int rg = row_groups(most, f32);
-    return {false, rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2), 0, false};
+    return {false, rg, rg > 0 ? 16 * rg : f32 ? 4 : 8, sms * (f32 ? 1 : 2), 0, 0};
 }
 
 // Workspace: records, the plan, rows as bf16.
 struct ChunkSpace { TreeSpace records; size_t wide, bytes; };
-static ChunkSpace chunk_space(const dynakv_row_cache* c, const ChunkKind& k, int64_t n_tokens, int n_seqs, int pages_per_seq, char* base, ChunkPlan* plan) {
+static ChunkSpace chunk_space(const dynakv_row_cache* c, const ChunkKind& k, int64_t n_tokens, int n_seqs, char* base, ChunkPlan* plan) {
     ChunkSpace s;
     s.records = tree_space(k.ctas, k.rows, c->head_dim);
     s.wide = 0;
     s.bytes = s.records.bytes;
-    if (k.planned) s.bytes = chunk_plan_space(n_tokens, k.per, n_seqs, k.ctas, s.bytes, base, plan);
-    if (k.wide) {
+    if (k.planned) s.bytes = chunk_plan_space(n_tokens, k.per, n_seqs, k.ctas, k.wide, s.bytes, base, plan);
+    if (k.wide > 0) {
         s.wide = (s.bytes + 127) / 128 * 128;
-        s.bytes = s.wide + chunk_wide_bytes(c, n_seqs, pages_per_seq) + 128;       // the workspace itself is aligned to 16 bytes
+        s.bytes = s.wide + k.wide * chunk_wide_page(c) + 128;       // the workspace itself is aligned to 16 bytes
     }
     return s;
 }
@@ -76,7 +79,7 @@ extern "C" int64_t dynakv_attend_chunk_workspace(const dynakv_row_cache* cache, 
     int rc;
     const int sms = sm_count(&rc);
     if (rc != DYNAKV_OK) return rc;
-    return (int64_t)chunk_space(cache, chunk_kind(cache, n_heads, n_seqs, max_chunk, pages_per_seq, sms), n_tokens, n_seqs, pages_per_seq, nullptr, nullptr).bytes;
+    return (int64_t)chunk_space(cache, chunk_kind(cache, n_heads, n_seqs, max_chunk, pages_per_seq, sms), n_tokens, n_seqs, nullptr, nullptr).bytes;
 }
 
 extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q, int32_t n_heads, int64_t n_tokens, const int32_t* q_start,
@@ -95,7 +98,7 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
     if (rc != DYNAKV_OK) return rc;
     const ChunkKind kind = chunk_kind(cache, n_heads, n_seqs, max_chunk, pages_per_seq, sms);
     ChunkPlan plan = {};
-    const ChunkSpace sp = chunk_space(cache, kind, n_tokens, n_seqs, pages_per_seq, reinterpret_cast<char*>(workspace), &plan);
+    const ChunkSpace sp = chunk_space(cache, kind, n_tokens, n_seqs, reinterpret_cast<char*>(workspace), &plan);
     if (workspace_bytes < (int64_t)sp.bytes) return DYNAKV_ERR_ARG;
     TreeArgs a = tree_args(cache, q, n_heads, n_tokens, q_start, n_seqs, max_chunk, page_table, pages_per_seq, kv_len, out, lse, workspace, sp.records, status);
     a.scale = scores->scale;
@@ -109,7 +112,7 @@ extern "C" int dynakv_attend_chunk(const dynakv_row_cache* cache, const void* q,
     if (kind.planned && cache->kv_dtype == DYNAKV_F32) return chunk_f32_launch(cache, a, plan, sms, st);
     if (kind.planned) {
         void* wide = reinterpret_cast<void*>(((uintptr_t)workspace + sp.wide + 127) / 128 * 128);
-        return chunk_tc_launch(cache, a, plan, kind.wide ? wide : nullptr, sms, st);
+        return chunk_tc_launch(cache, a, plan, kind.wide > 0 ? wide : nullptr, kind.wide >= (long long)n_seqs * pages_per_seq, sms, st);
     }
     CUtensorMap mk, mv;
     if (!tree_page_map(&mk, cache, cache->k, true) || !tree_page_map(&mv, cache, cache->v, true)) return DYNAKV_ERR_CUDA;

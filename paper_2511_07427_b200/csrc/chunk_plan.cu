@@ -26,8 +26,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
         const long long before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
         return x + (warp ? before : 0);
     };
-    // ---- sequences and their tiles
-    long long tiles = 0;
+    // ---- sequences and their tiles; where pages lie that are turned into bf16: from the first that a token may see to the last
+    long long tiles = 0, wide = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += PLAN_THREADS) {
         const int b = b0 + tid;
         SeqInfo s = {};
@@ -40,6 +40,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
         }
         const int first = (int)(tiles + incl - count);
         if (b < a.n_seqs) p.first[b] = first;
+        if (p.wide_base) {
+            const int from = a.rows_from || a.rows_to || a.window == 0 ? 0 : max(0, s.n - s.T + 1 - a.window) / CT_KEYS * CT_PAGES, pages = count > 0 ? (s.n + PAGE - 1) / PAGE - from : 0;
+            long long all;
+            const long long upto = scan(pages, all);
+            if (b < a.n_seqs) p.wide_base[b] = (int)min(wide + upto - pages, p.wide_pages) - from;         // (looked at only when all fit)
+            wide += all;
+        }
         for (unsigned left = __ballot_sync(0xffffffffu, count > 0); left; left &= left - 1) {      // few sequences have many tiles, so a warp writes a sequence's
             const int src = __ffs(left) - 1;
             const int c = __shfl_sync(0xffffffffu, count, src), f = __shfl_sync(0xffffffffu, first, src), q0 = __shfl_sync(0xffffffffu, s.q0, src),
@@ -56,7 +63,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
         }
         tiles += total;
     }
-    if (tid == 0) p.first[a.n_seqs] = (int)tiles;
+    if (tid == 0) { p.first[a.n_seqs] = (int)tiles; if (p.wide_base) *p.wide_fits = wide <= p.wide_pages ? 1 : 0; }
     __syncthreads();
     // ---- stages of every tile; where the tokens' ranges have to be read, 8 lanes per tile find the first and the last row
     if (a.rows_from || a.rows_to) {
@@ -156,7 +163,7 @@ int chunk_plan_launch(const TreeArgs& a, const ChunkPlan& plan, int sms, int per
 }
 
 // The plan's part of the workspace behind the records'.
-size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, size_t at, char* base, ChunkPlan* plan) {
+size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, long long wide_pages, size_t at, char* base, ChunkPlan* plan) {
     const size_t tiles = (size_t)chunk_most_tiles(n_tokens, per, n_seqs);
     auto take = [&](size_t bytes) { const size_t x = (at + 15) / 16 * 16; at = x + bytes; return base + x; };
     ChunkPlan p;
@@ -164,6 +171,9 @@ size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, size_t 
     p.before = reinterpret_cast<long long*>(take((tiles + 1) * 8));
     p.starts = reinterpret_cast<ChunkStart*>(take((size_t)ctas * sizeof(ChunkStart)));
     p.first = reinterpret_cast<int*>(take(((size_t)n_seqs + 1) * 4));
+    p.wide_base = wide_pages > 0 ? reinterpret_cast<int*>(take((size_t)n_seqs * 4)) : nullptr;
+    p.wide_fits = wide_pages > 0 ? reinterpret_cast<int*>(take(4)) : nullptr;
+    p.wide_pages = wide_pages;
     if (plan) *plan = p;
     return at;
 }

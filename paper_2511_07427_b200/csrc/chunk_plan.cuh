@@ -35,6 +35,10 @@ struct ChunkPlan {
     long long* before;                             // [most tiles + 1] stages of the tiles before, for one KV head
     ChunkStart* starts;                            // [CTAs]
     int* first;                                    // [n_seqs + 1] first tile of every sequence
+    // long chunks over FP8 rows (else NULL): where a sequence's pages lie when they are turned into bf16, and whether all find room
+    int* wide_base;                                // [n_seqs] column 0's page
+    int* wide_fits;                                // [1]
+    long long wide_pages;                          // pages there is room for
 };
 
 __device__ __host__ __forceinline__ int tile_tokens(int G) { return 2 * (128 / G); }
@@ -89,13 +93,13 @@ struct ChunkWalk {
 // Host side.  per: tokens of a tile, keys: rows of a stage.
 int chunk_plan_launch(const TreeArgs& a, const ChunkPlan& plan, int sms, int per, int keys, cudaStream_t st);
 // The bytes up to the end of the plan in a workspace whose first `at` are taken.
-size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, size_t at, char* base, ChunkPlan* plan);
+// wide_pages > 0: FP8 rows are turned into bf16.
+size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, long long wide_pages, size_t at, char* base, ChunkPlan* plan);
 // The kernels: chunk_tc.cu (bf16 and FP8 rows, tcgen05), chunk_f32.cu.
-// wide: where FP8 rows are turned into bf16 first (chunk_wide_bytes() bytes, 128-byte aligned), NULL: they are not.
-int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, void* wide, int sms, cudaStream_t st);
-static inline size_t chunk_wide_bytes(const dynakv_row_cache* c, int n_seqs, int pages_per_seq) {
-    return (size_t)n_seqs * pages_per_seq * c->n_kv_heads * PAGE * c->head_dim * 2 * 2;
-}
+// wide: where FP8 rows are turned into bf16 first (plan.wide_pages pages, 128-byte aligned), NULL: they are not.  always: there is room for whatever the table names.
+int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, void* wide, bool always, int sms, cudaStream_t st);
+// Bytes of a page's K and V as bf16.
+static inline size_t chunk_wide_page(const dynakv_row_cache* c) { return (size_t)c->n_kv_heads * PAGE * c->head_dim * 2 * 2; }
 int chunk_f32_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st);
 
 }  // namespace dkv

@@ -182,6 +182,10 @@ __global__ void __launch_bounds__((TcChunk<HD, F8>::threads), 1) k_chunk_tc(cons
     auto bar = [&](int i) { return bar0 + i * 8; };
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
+    if (a.wide_fits) {                                         // both kernels are launched, and one of them has nothing to do
+        pdl_wait();
+        if (*a.wide_fits != (F8 ? 0 : 1)) return;
+    }
     if (tid == 0) {
         for (int i = 0; i < C::count; i++) {
             const bool full = (i >= C::KFULL && i < C::KEMPTY) || (i >= C::VFULL && i < C::VEMPTY);
@@ -677,40 +681,45 @@ __global__ void __launch_bounds__(CT_ROWS) k_chunk_merge(const TreeArgs a) {
 //
 // Every tile of a sequence reads the same rows, and what turns a stage into bf16 inside the kernel competes with its softmax for the same
 // pipes: 4096 tokens over 16384 rows, 8 KV heads, take 1330 us that way, 826 as bf16 rows.  So from three tiles per sequence on (two would break
-// even) the stages that any tile needs are turned once, into the workspace, in the order of the page table.  Block (x = stage, y = KV head, z = sequence).
-constexpr int CW_THREADS = 256;
+// even) the stages that any tile needs are turned once, into the workspace, sequence by sequence.  Block (x: every gridDim.x-th stage, y = KV head, z = sequence).
+constexpr int CW_THREADS = 256, CW_BLOCKS = 8192;
 
 template <int HD>
 __global__ void __launch_bounds__(CW_THREADS) k_chunk_widen(const TreeArgs a, const ChunkPlan p, uint4* k_out, uint4* v_out) {
     constexpr int CPR = HD / 16, RPP = CW_THREADS / CPR, NP = CT_KEYS / RPP;               // 16-byte chunks of a row, rows and passes
-    const int stage = blockIdx.x, h = blockIdx.y, seq = blockIdx.z, tid = threadIdx.x, chunk = tid % CPR, row0 = tid / CPR;
+    const int h = blockIdx.y, seq = blockIdx.z, tid = threadIdx.x, chunk = tid % CPR, row0 = tid / CPR;
     pdl_wait();
     pdl_trigger();
-    bool need = false;
-    for (int i = p.first[seq] + tid; i < p.first[seq + 1]; i += CW_THREADS) { const ChunkTile& t = p.tiles[i]; need |= t.from <= stage && stage < t.from + t.stages && stage * CT_KEYS < t.n; }
-    if (!__syncthreads_or(need)) return;
-    uint4 raw[2][NP];
-    int ex[2][NP];
-    size_t to[NP];
-    bool there[NP];
-#pragma unroll
-    for (int i = 0; i < NP; i++) {
-        const int row = i * RPP + row0, column = stage * CT_PAGES + row / PAGE, page = column < a.pages_per_seq ? chunk_page(a, seq, column) : -1;
-        there[i] = page >= 0;
-        const size_t r = ((size_t)(there[i] ? page : 0) * a.Hk + h) * PAGE + row % PAGE;
-        to[i] = (((size_t)seq * a.pages_per_seq + column) * a.Hk + h) * PAGE + row % PAGE;
-        raw[0][i] = __ldg(reinterpret_cast<const uint4*>(a.kpool + r * HD) + chunk); ex[0][i] = __ldg(a.kexp + r);
-        raw[1][i] = __ldg(reinterpret_cast<const uint4*>(a.vpool + r * HD) + chunk); ex[1][i] = __ldg(a.vexp + r);
-    }
-#pragma unroll
-    for (int kv = 0; kv < 2; kv++)
+    const int t0 = p.first[seq], t1 = p.first[seq + 1], n = t0 < t1 ? p.tiles[t0].n : 0;
+    if (!*p.wide_fits) return;
+    const int base = p.wide_base[seq];
+    for (int stage = blockIdx.x; stage * CT_KEYS < n; stage += gridDim.x) {
+        bool need = false;
+        for (int i = t0 + tid; i < t1; i += CW_THREADS) { const ChunkTile& t = p.tiles[i]; need |= t.from <= stage && stage < t.from + t.stages; }
+        if (!__syncthreads_or(need)) continue;
+        uint4 raw[2][NP];
+        int ex[2][NP];
+        size_t to[NP];
+        bool there[NP];
 #pragma unroll
         for (int i = 0; i < NP; i++) {
-            unsigned o[8];
-            widen16(raw[kv][i], ex[kv][i], o);
-            uint4* out = (kv ? v_out : k_out) + to[i] * (HD / 8) + 2 * chunk;
-            if (there[i]) { out[0] = make_uint4(o[0], o[1], o[2], o[3]); out[1] = make_uint4(o[4], o[5], o[6], o[7]); }
+            const int row = i * RPP + row0, column = stage * CT_PAGES + row / PAGE, page = column * PAGE < n ? chunk_page(a, seq, column) : -1;
+            there[i] = page >= 0;
+            const size_t r = ((size_t)(there[i] ? page : 0) * a.Hk + h) * PAGE + row % PAGE;
+            to[i] = ((size_t)(base + column) * a.Hk + h) * PAGE + row % PAGE;
+            raw[0][i] = __ldg(reinterpret_cast<const uint4*>(a.kpool + r * HD) + chunk); ex[0][i] = __ldg(a.kexp + r);
+            raw[1][i] = __ldg(reinterpret_cast<const uint4*>(a.vpool + r * HD) + chunk); ex[1][i] = __ldg(a.vexp + r);
         }
+#pragma unroll
+        for (int kv = 0; kv < 2; kv++)
+#pragma unroll
+            for (int i = 0; i < NP; i++) {
+                unsigned o[8];
+                widen16(raw[kv][i], ex[kv][i], o);
+                uint4* out = (kv ? v_out : k_out) + to[i] * (HD / 8) + 2 * chunk;
+                if (there[i]) { out[0] = make_uint4(o[0], o[1], o[2], o[3]); out[1] = make_uint4(o[4], o[5], o[6], o[7]); }
+            }
+    }
 }
 
 // ---------------------------------------------------------------------------------- host side
@@ -738,8 +747,7 @@ static int chunk_tc_launch_as(const dynakv_row_cache* cache, const TreeArgs& a, 
         return cudaFuncGetAttributes(&f, k_chunk_tc<HD, F8, MODE>) == cudaSuccess ? f.numRegs : 0;
     }();
     if (regs * (C::threads / 128) < 2 * C::regs_softmax + C::regs_rest + (F8 ? C::regs_convert : 0)) return DYNAKV_ERR_CUDA;
-    if (launch_pdl(k_chunk_tc<HD, F8, MODE>, dim3(sms), dim3(C::threads), C::smem, st, mq, mk, mv, a, plan) != cudaSuccess) return DYNAKV_ERR_CUDA;
-    return launch_pdl(k_chunk_merge<HD>, dim3(sms, HD / 16), dim3(CT_ROWS), 0, st, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
+    return launch_pdl(k_chunk_tc<HD, F8, MODE>, dim3(sms), dim3(C::threads), C::smem, st, mq, mk, mv, a, plan) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
 template <int HD, bool F8>
 static int chunk_tc_launch_mode(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
@@ -748,27 +756,33 @@ static int chunk_tc_launch_mode(const dynakv_row_cache* cache, const TreeArgs& a
     return a.slopes || !(a.scale >= FLT_MIN) ? chunk_tc_launch_as<HD, F8, BIASED>(cache, a, plan, sms, st) : chunk_tc_launch_as<HD, F8, PLAIN>(cache, a, plan, sms, st);
 }
 template <int HD>
-static int chunk_tc_launch_hd(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, int sms, cudaStream_t st) {
-    return cache->kv_dtype == DYNAKV_FP8 ? chunk_tc_launch_mode<HD, true>(cache, a, plan, sms, st) : chunk_tc_launch_mode<HD, false>(cache, a, plan, sms, st);
+static int chunk_tc_launch_hd(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, void* wide, bool always, int sms, cudaStream_t st) {
+    int rc = DYNAKV_OK;
+    TreeArgs own = a;
+    if (wide) {
+        // FP8 rows turned into bf16 once, then the kernel of bf16 rows; where they may not all find room, that of FP8 rows behind it, of which one has the call
+        dynakv_row_cache c = *cache;
+        c.n_pages = plan.wide_pages;
+        c.k = wide; c.v = reinterpret_cast<char*>(wide) + plan.wide_pages * chunk_wide_page(cache) / 2;
+        c.k_exp = c.v_exp = nullptr; c.kv_dtype = DYNAKV_BF16;
+        const int stages = (a.pages_per_seq + CT_PAGES - 1) / CT_PAGES;
+        const dim3 grid(max(1, min(stages, CW_BLOCKS / a.Hk / a.n_seqs)), a.Hk, a.n_seqs);
+        if (launch_pdl(k_chunk_widen<HD>, grid, dim3(CW_THREADS), 0, st, a, plan, reinterpret_cast<uint4*>(c.k), reinterpret_cast<uint4*>(c.v)) != cudaSuccess) return DYNAKV_ERR_CUDA;
+        TreeArgs w = a;
+        w.kpool = reinterpret_cast<const unsigned char*>(c.k); w.vpool = reinterpret_cast<const unsigned char*>(c.v);
+        w.kexp = w.vexp = nullptr; w.wide_base = plan.wide_base;
+        if (!always) own.wide_fits = w.wide_fits = plan.wide_fits;
+        rc = chunk_tc_launch_mode<HD, false>(&c, w, plan, sms, st);
+    }
+    if (rc == DYNAKV_OK && !(wide && always)) rc = cache->kv_dtype == DYNAKV_FP8 ? chunk_tc_launch_mode<HD, true>(cache, own, plan, sms, st) : chunk_tc_launch_mode<HD, false>(cache, own, plan, sms, st);
+    if (rc != DYNAKV_OK) return rc;
+    return launch_pdl(k_chunk_merge<HD>, dim3(sms, HD / 16), dim3(CT_ROWS), 0, st, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
 
-int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, void* wide, int sms, cudaStream_t st) {
+int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, void* wide, bool always, int sms, cudaStream_t st) {
     const int rc = chunk_plan_launch(a, plan, sms, tile_tokens(a.G), CT_KEYS, st);
     if (rc != DYNAKV_OK) return rc;
-    if (!wide) return cache->head_dim == 128 ? chunk_tc_launch_hd<128>(cache, a, plan, sms, st) : chunk_tc_launch_hd<64>(cache, a, plan, sms, st);
-    // FP8 rows turned into bf16 once, then the kernel of bf16 rows
-    dynakv_row_cache c = *cache;
-    c.n_pages = (int64_t)a.n_seqs * a.pages_per_seq;
-    c.k = wide; c.v = reinterpret_cast<char*>(wide) + chunk_wide_bytes(cache, a.n_seqs, a.pages_per_seq) / 2;
-    c.k_exp = c.v_exp = nullptr; c.kv_dtype = DYNAKV_BF16;
-    const dim3 grid((a.pages_per_seq + CT_PAGES - 1) / CT_PAGES, a.Hk, a.n_seqs);
-    const cudaError_t e = cache->head_dim == 128 ? launch_pdl(k_chunk_widen<128>, grid, dim3(CW_THREADS), 0, st, a, plan, reinterpret_cast<uint4*>(c.k), reinterpret_cast<uint4*>(c.v))
-                                                 : launch_pdl(k_chunk_widen<64>, grid, dim3(CW_THREADS), 0, st, a, plan, reinterpret_cast<uint4*>(c.k), reinterpret_cast<uint4*>(c.v));
-    if (e != cudaSuccess) return DYNAKV_ERR_CUDA;
-    TreeArgs w = a;
-    w.kpool = reinterpret_cast<const unsigned char*>(c.k); w.vpool = reinterpret_cast<const unsigned char*>(c.v);
-    w.kexp = w.vexp = nullptr; w.widened = 1;
-    return c.head_dim == 128 ? chunk_tc_launch_hd<128>(&c, w, plan, sms, st) : chunk_tc_launch_hd<64>(&c, w, plan, sms, st);
+    return cache->head_dim == 128 ? chunk_tc_launch_hd<128>(cache, a, plan, wide, always, sms, st) : chunk_tc_launch_hd<64>(cache, a, plan, wide, always, sms, st);
 }
 
 }  // namespace dkv

@@ -41,7 +41,8 @@ struct TreeArgs {
     const float* slopes;                   // [Hq] lowers a logit by slope * distance, may be NULL
     float cap;                             // > 0: logits become cap * tanh(logit / cap)
     int window;                            // > 0: the last so many rows up to its own
-    int widened;                           // 1: kpool, vpool are the pages of page_table in order, as bf16
+    const int* wide_base;                  // not NULL: kpool, vpool are pages turned into bf16, column c of sequence b the page wide_base[b] + c
+    const int* wide_fits;                  // not NULL: 1, and the kernel for bf16 rows has the call, or 0, and the one for FP8 rows has it
 };
 enum { DESC_VALID = 0, DESC_FIRST = 1, DESC_Q0 = 2, DESC_T = 3, DESC_H = 4, DESC_RT = 5 };
 
@@ -68,7 +69,7 @@ __device__ __forceinline__ float2 chunk_factor(const TreeArgs& a) {
 // The page of a sequence's column: its place in the pool, -1 where the table names none.
 __device__ __forceinline__ int chunk_page(const TreeArgs& a, int seq, int column) {
     const int id = a.page_table[(size_t)seq * a.pages_per_seq + column];
-    return id < 0 || id >= a.n_pages ? -1 : a.widened ? seq * a.pages_per_seq + column : id;
+    return id < 0 || id >= a.n_pages ? -1 : a.wide_base ? a.wide_base[seq] + column : id;
 }
 
 struct SeqInfo {
