@@ -545,7 +545,8 @@ typedef struct dynakv_page_pool {
  * ([n_seqs][pages_per_seq], entries past a sequence's pages are of no interest) gets the pages that it needs, in order of
  * sequences and of rows from the top of the pool, and q_start [n_seqs + 1], positions, slots [n_tokens] say where the packed tokens
  * lie: token i of sequence b is q_start[b] + i, its position kv_len[b] + i as it was before, its slot that of its row.  That is what
- * dynakv_norm_rope_store, dynakv_attend_tree and dynakv_attend_chunk take.  Places behind the last token get position 0 and slot -1,
+ * dynakv_norm_rope_store, dynakv_attend_tree and dynakv_attend_chunk take (drafts of a tree are rotated by the position of their depth
+ * instead: kv_len[b] as it was before plus the number of their ancestors in the tree).  Places behind the last token get position 0 and slot -1,
  * which is skipped where rows are stored.
  * Sequences are served in order up to the first one for which pages (DYNAKV_ST_PAGE_POOL) or places (DYNAKV_ST_BOUNDS) are too few; it
  * and those behind it stay as they are, with no tokens.  So does a sequence whose numbers are negative or whose rows would not fit its
@@ -563,7 +564,7 @@ int dynakv_pages_trim(const dynakv_page_pool* pool, int32_t* page_table, int32_t
 
 /* Which drafted tokens the target model accepts, and the token that follows, from random numbers that the caller draws.
  *
- * Sequence b's tokens q_start[b] .. q_start[b + 1] - 1 (at most max_tree <= 256) are a tree as dynakv_attend_tree attends to it: the first is the
+ * Sequence b's tokens q_start[b] .. q_start[b + 1] - 1 (at most max_tree <= 256, no token in two sequences) are a tree as dynakv_attend_tree attends to it: the first is the
  * root, which is certain, the others are drafts; parent[q_start[b] + i] is the place in the tree, before i, of draft i's parent (NULL: i - 1, a
  * chain).  logits[i] ([n_tokens][vocab], logits_stride elements from row to row, DYNAKV_F32 or DYNAKV_BF16, finite or -infinity) are
  * the target's behind token i.  From the root on, with p = softmax(logits / temperature[b]) of the token reached, its children

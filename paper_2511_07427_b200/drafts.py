@@ -57,7 +57,8 @@ class PagePool:
     def extend(self, page_table, kv_len, new_len, n_tokens: int):
         """Rows for ``new_len`` [sequences] int32 new tokens behind every sequence: ``page_table`` [sequences, pages] and ``kv_len``
         [sequences] int32 are brought up to date, and (q_start [sequences + 1], positions [n_tokens], slots [n_tokens]), all int32, are
-        what ``HeadRotary.store``, ``RowCache.write`` and the attention calls take.  ``n_tokens``: places in the packed batch; those that are left over get
+        what ``HeadRotary.store``, ``RowCache.write`` and the attention calls take; drafts of a tree are rotated by their depth in it, ``positions`` minus
+        their place in the tree plus their depth.  ``n_tokens``: places in the packed batch; those that are left over get
         position 0 and slot -1.  Sequences are served in order until pages or places run out."""
         E = _rows._env_made or _rows._env()
         b, per, table, lens, add = self._tables(E, page_table, kv_len, new_len, "new_len")

@@ -386,7 +386,8 @@ class RowCache:
         rows_from on, and with ``window`` the last so many up to P.  (Documents in one sequence: rows_from is the first row of the token's
         document; a prefix that all tokens see: rows_to = max(P + 1, prefix length).)  ``softcap``: logits s become
         softcap * tanh(s / softcap); ``slopes`` [heads] float32: then s - slope * |P - j| for row j.  A token that sees nothing gets
-        zeros and -inf."""
+        zeros and -inf.  Over bf16 and FP8 rows, with more than 32 query rows per KV head (``max_chunk`` * heads / KV heads; rows of 64: 64), results
+        are a little coarser than ``attend_tree``'s: weights enter the products with V as bf16, each off by 2^-8 of itself at most."""
         E, device = _env_made or _env(), self._device
         n, heads, b, per = self._queries(E, q, page_table, out, lse)
         size = self._workspace.get((heads, max_chunk, n, b, per))
