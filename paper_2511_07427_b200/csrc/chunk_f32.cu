@@ -373,7 +373,7 @@ static int chunk_f32_launch_hd(const dynakv_row_cache* cache, const TreeArgs& a,
         return cudaFuncGetAttributes(&f, k_chunk_f32<HD>) == cudaSuccess ? f.numRegs : 0;
     }();
     if (3 * regs < 2 * C::regs_sums + C::regs_loads) return DYNAKV_ERR_CUDA;
-    const int rc = chunk_plan_launch(a, plan, sms, CF_ROWS / a.G, CF_KEYS, st);
+    const int rc = chunk_plan_launch(a, plan, sms, {CF_ROWS / a.G, CF_KEYS, CF_UNIT_COST, CF_WHOLE}, st);
     if (rc != DYNAKV_OK) return rc;
     if (launch_pdl(k_chunk_f32<HD>, dim3(sms), dim3(C::threads), C::smem, st, mk, mv, a, plan) != cudaSuccess) return DYNAKV_ERR_CUDA;
     return launch_pdl(k_chunk_merge_f32<HD>, dim3(sms, CF_ROWS / 8), dim3(256), 0, st, a) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;

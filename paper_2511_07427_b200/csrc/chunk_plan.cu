@@ -6,11 +6,11 @@ namespace dkv {
 
 constexpr int PLAN_THREADS = 1024, PLAN_NEAR = 2048;            // prefix sums of so many tiles are kept in shared memory as well
 
-__global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, const ChunkPlan p, int ctas, long long most, int per, int keys) {
+__global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, const ChunkPlan p, int ctas, long long most, const ChunkCut cut) {
     __shared__ long long sums[32];
     __shared__ long long near_s[PLAN_NEAR + 1];
     __shared__ long long at_s[PLAN_THREADS + 1];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = cut.per, keys = cut.keys, unit = cut.unit;
     pdl_wait();
     pdl_trigger();
     auto scan = [&](long long x, long long& total) {           // inclusive, over the block
@@ -103,9 +103,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
     }
     if (tid == 0) { p.before[tiles] = run; if (tiles <= PLAN_NEAR) near_s[tiles] = run; }
     __syncthreads();
-    // ---- where every CTA begins: cost x is stage x of the list in which every unit has CT_UNIT_COST stages more
+    // ---- where every CTA begins: cost x is stage x of the list in which every unit has unit stages more
     const long long* before = tiles <= PLAN_NEAR ? near_s : p.before;
-    const long long W = (run + tiles * CT_UNIT_COST) * a.Hk;
+    const long long W = (run + tiles * unit) * a.Hk;
     const int C = (int)max(1ll, min((long long)ctas, run * a.Hk));
     for (int c0 = 0; c0 < ctas; c0 += PLAN_THREADS) {
         // the CTA's place, and that of the one behind it
@@ -123,19 +123,19 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
         };
         if (c <= ctas && x < W) {
             auto find = [&](long long y, int lo, int hi) {     // last tile of [lo, hi) whose cost before it is <= y
-                while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (before[mid] + (long long)mid * CT_UNIT_COST <= y) lo = mid; else hi = mid; }
+                while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (before[mid] + (long long)mid * unit <= y) lo = mid; else hi = mid; }
                 return lo;
             };
             const ChunkTile t = p.tiles[find(x / a.Hk, 0, (int)tiles)];
             e0 = t.first; e1 = e0 + (t.T + per - 1) / per;
-            const long long lead = before[e0] + (long long)e0 * CT_UNIT_COST, all = before[e1] + (long long)e1 * CT_UNIT_COST - lead, cost = x - lead * a.Hk;
+            const long long lead = before[e0] + (long long)e0 * unit, all = before[e1] + (long long)e1 * unit - lead, cost = x - lead * a.Hk;
             to.head = (int)(cost / all);
             const long long y = lead + cost - to.head * all;
             to.tile = find(y, e0, e1);
-            to.off = (int)max(0ll, y - before[to.tile] - (long long)(to.tile + 1) * CT_UNIT_COST);
+            to.off = (int)max(0ll, y - before[to.tile] - (long long)(to.tile + 1) * unit);
             // a short unit is not cut where a CTA has several: two records and their merge cost more than what it adds to one side
             const int whole = (int)(before[to.tile + 1] - before[to.tile]);
-            if (whole <= CT_WHOLE && (whole + CT_UNIT_COST) * 3ll * C <= W) to.off = to.off * 2 >= whole ? whole : 0;
+            if (whole <= cut.whole && (whole + unit) * 3ll * C <= W) to.off = to.off * 2 >= whole ? whole : 0;
             st.at = before[e0] * a.Hk + to.head * (before[e1] - before[e0]) + before[to.tile] - before[e0] + to.off;
             if (to.off == whole) behind();
             else rest = whole - to.off;
@@ -158,8 +158,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_chunk_plan(const TreeArgs a, c
 
 static long long chunk_most_tiles(int64_t n_tokens, int per, int n_seqs) { return n_tokens / per + n_seqs; }
 
-int chunk_plan_launch(const TreeArgs& a, const ChunkPlan& plan, int sms, int per, int keys, cudaStream_t st) {
-    return launch_pdl(k_chunk_plan, dim3(1), dim3(PLAN_THREADS), 0, st, a, plan, sms, chunk_most_tiles(a.n_tokens, per, a.n_seqs), per, keys) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
+int chunk_plan_launch(const TreeArgs& a, const ChunkPlan& plan, int sms, const ChunkCut& cut, cudaStream_t st) {
+    return launch_pdl(k_chunk_plan, dim3(1), dim3(PLAN_THREADS), 0, st, a, plan, sms, chunk_most_tiles(a.n_tokens, cut.per, a.n_seqs), cut) == cudaSuccess ? DYNAKV_OK : DYNAKV_ERR_CUDA;
 }
 
 // The plan's part of the workspace behind the records'.

@@ -5,7 +5,7 @@
 // is the stages of 64 or 128 rows between the first and the last row that one of its tokens sees.  A first launch writes down
 // every tile's stages, their prefix sums and where every CTA of the main kernel begins, because that depends on lengths and ranges that
 // only the device has.  All units' stages, in the order sequence, KV head, tile (so that CTAs side by side read the same
-// rows), form one list that the CTAs share out evenly, a unit's beginning counted as CT_UNIT_COST stages more; a unit cut by a border leaves
+// rows), form one list that the CTAs share out evenly, a unit's beginning counted as ChunkCut::unit stages more; a unit cut by a border leaves
 // records that a last launch merges, as in tree_plan.cuh.
 #pragma once
 
@@ -15,11 +15,13 @@ namespace dkv {
 
 constexpr int CT_ROWS = 256, CT_KEYS = 128, CT_PAGES = CT_KEYS / PAGE;       // rows of a tile and of a stage: tcgen05
 constexpr int CF_ROWS = 128, CF_KEYS = 64;                                    // fp32 rows
-#ifndef DKV_CHUNK_UNIT_COST
-#define DKV_CHUNK_UNIT_COST 2
-#endif
-constexpr int CT_UNIT_COST = DKV_CHUNK_UNIT_COST;
-constexpr int CT_WHOLE = 12;                       // stages up to which a unit is not cut
+// How a kernel's work is cut: tokens of a tile, rows of a stage, what a unit costs beside its stages (in stages), stages up to which a unit is not cut.
+struct ChunkCut { int per, keys, unit, whole; };
+constexpr int CT_UNIT_COST = 2, CT_WHOLE = 12;                                // tcgen05
+// fp32 rows, whose stages are half as many rows and take longer.  In us, (1, 4) / (2, 12), as the tcgen05 kernel has it / (1, 0) / (0, 0) / (3, 0): one prompt of 2000
+// tokens, 32 heads over 8 of 128, 829 / 871 / 824 / 909 / 903; 8 x 300 over 1000 567 / 651 / 567 / 579 / 621; documents 2 x 3001 789 / 890 / 788 / 881 / 900;
+// 3 x 777 with prefixes, 8 heads of 64, 90 / 99 / 90 / 96 / 105; 64 x 100 205 / 206 / 207 / 240 / 208.
+constexpr int CF_UNIT_COST = 1, CF_WHOLE = 4;
 
 struct __align__(16) ChunkTile {
     int seq, tile, from, stages;                   // 2 * tile of the sequence, + 1 the last; first stage, stages
@@ -90,8 +92,8 @@ struct ChunkWalk {
     }
 };
 
-// Host side.  per: tokens of a tile, keys: rows of a stage.
-int chunk_plan_launch(const TreeArgs& a, const ChunkPlan& plan, int sms, int per, int keys, cudaStream_t st);
+// Host side.
+int chunk_plan_launch(const TreeArgs& a, const ChunkPlan& plan, int sms, const ChunkCut& cut, cudaStream_t st);
 // The bytes up to the end of the plan in a workspace whose first `at` are taken.
 // wide_pages > 0: FP8 rows are turned into bf16.
 size_t chunk_plan_space(int64_t n_tokens, int per, int n_seqs, int ctas, long long wide_pages, size_t at, char* base, ChunkPlan* plan);

@@ -780,7 +780,7 @@ static int chunk_tc_launch_hd(const dynakv_row_cache* cache, const TreeArgs& a, 
 }
 
 int chunk_tc_launch(const dynakv_row_cache* cache, const TreeArgs& a, const ChunkPlan& plan, void* wide, bool always, int sms, cudaStream_t st) {
-    const int rc = chunk_plan_launch(a, plan, sms, tile_tokens(a.G), CT_KEYS, st);
+    const int rc = chunk_plan_launch(a, plan, sms, {tile_tokens(a.G), CT_KEYS, CT_UNIT_COST, CT_WHOLE}, st);
     if (rc != DYNAKV_OK) return rc;
     return cache->head_dim == 128 ? chunk_tc_launch_hd<128>(cache, a, plan, wide, always, sms, st) : chunk_tc_launch_hd<64>(cache, a, plan, wide, always, sms, st);
 }
