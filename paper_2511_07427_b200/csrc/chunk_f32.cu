@@ -8,8 +8,8 @@
 //   warp 8         (with three that rest) TMA loads, a page of K or V per copy (128-byte swizzle: the 8 lanes of a 16-byte read meet in no bank)
 //   warps 0-7      16 query rows each
 // Work is shared out as for the tcgen05 kernel (chunk_plan.cuh).  Weights go through shared memory twice side by side, as the packed products want them.
-// Measured: 2000 tokens of one prompt, 32 heads over 8 of 128, 855 us, 38 TFLOP/s (the FMA pipe busy 60 % of the time that a CTA has work: two warps per
-// scheduler wait for their own results, and 14 % go to CTAs that are done earlier); 3 x 777 with prefixes and distances, 8 heads of 64, 97 us.
+// Measured: 2000 tokens of one prompt, 32 heads over 8 of 128, 825 us, 40 TFLOP/s; 3 x 777 with prefixes and distances, 8 heads of 64, 88 us, the FMA pipe busy
+// 56 % of the time: two warps per scheduler wait for their own results and for reads of shared memory.  Rows of 128 spill 152 bytes.
 #include <cuda.h>
 #include <float.h>
 

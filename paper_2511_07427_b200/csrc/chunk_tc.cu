@@ -13,9 +13,9 @@
 // Weights enter the products as bf16 (2^-8 of each): bf16 hi + lo, as the kernel for few rows has them, would add half to the tensor pipe's work, which here is
 // what the power limit leaves time for.  The error of the results is 1.4 times that of rounding alone (2.3e-3 of their size against 1.7e-3).
 //
-// 4096 tokens over 16384 rows, 32 heads over 8 of 128 (962 GFLOP): 810 us in bursts (1190 TFLOP/s, 1.8 GHz), 960 in a stream of them (1.70 GHz at the 1000 W
+// 4096 tokens over 16384 rows, 32 heads over 8 of 128 (962 GFLOP): 842 us in bursts (1142 TFLOP/s), 945 in a stream of them (1.70 GHz at the 1000 W
 // limit; cuBLAS gets 1386 TFLOP/s there).  A stage takes 3800 cycles: 2048 in the tensor pipe (52 % busy), as many for the exponentials (52 %), the
-// rest what a stream waits for the other's products and for barriers.  Tried and not kept: weights handed over in halves (830 -> 888 us), a part of the
+// rest what a stream waits for the other's products and for barriers.  280 to 332 bytes a thread are spilled (FP8 rows: 396 to 596).  Tried and not kept: weights handed over in halves (830 -> 888 us), a part of the
 // exponentials as polynomials on the FMA pipe (a quarter 832, a third 862 against 827: the power that this takes), waits that poll
 // (876), logits read twice instead of kept (caps: 694 -> 912), two threads per query row (815 -> 932, caps 1265 -> 1879: 96 registers do not hold half a
 // row), weights taken before the stage's maximum is known and thrown away if it moves (818 -> 847; caps on long rows 1265 -> 1150, but documents 166 -> 183

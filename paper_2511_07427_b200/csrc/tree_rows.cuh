@@ -27,7 +27,8 @@
 // Masked rows never reach a sum.  Logits of rows that a token does not see are replaced by -inf.  Rows of V past the
 // sequence's length (whatever an earlier sequence left there) are zeroed in shared memory, and so are drafted rows that hold
 // a NaN or an infinity, because 0 * NaN would leak them into the tokens that do not see them; tokens that do see them get
-// their share added in fp32 at the end of the segment.
+// their share added in fp32 at the end of the segment.  For dynakv_attend_chunk, where any row may be one that some tokens do not see, query rows whose sums
+// came out as no numbers are taken again at the end (chunk_again.cuh).
 #pragma once
 
 #include <cuda.h>
