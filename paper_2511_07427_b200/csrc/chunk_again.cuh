@@ -3,7 +3,7 @@
 // The kernels multiply a tile's weights with all rows of V of a stage, so that 0 * NaN reaches the sums of query rows that do not see
 // the row of V in which the NaN lies.  (0 * infinity does too, and sums of large values may leave fp32 although the result fits it.)  While they walk over their
 // segments they only note that it happened.  A CTA that has a note goes over its segments once more when all of them are done and no copy, product or
-// wait is left: rows whose values are no numbers, in out or in a record, are taken again, a warp per row, from the rows that the query sees
+// wait is left: rows whose values are no numbers, in out or in a record, and need not be, are taken again, a warp per row, from the rows that the query sees
 // alone.  (Done between two units it kept the warps that load and multiply waiting beyond the limit of their waits, from some tens of thousands
 // of rows on.  Done by the launch that merges, whose registers it trebles, it cost calls without any such row 7 to 16 us.)
 // Rows whose sum of weights is no number (a NaN in the query, or in a key that it sees) are not taken again: their result is NaN.
@@ -175,22 +175,25 @@ __device__ __forceinline__ void chunk_row_again(const TreeArgs& a, const AgainSe
     }
 }
 
-// A segment, by WARPS warps (this one: `warp`) that all call it: rows in which a value is no number are taken again, unless every such value has its
-// reason in a NaN that the row sees, in which case it is right.  place_of(row): packed token * heads + query head, -1: there is none.
-// shared: 2 HD + 1 ints; sync: a barrier of those warps.
+// A segment, by WARPS warps (this one: `warp`) that all call it.  What a row of V that holds no number does to a column of a query row that sees it needs no sums: the column
+// is NaN, or infinite where all that it sees of this kind are infinities of one sign.  So the segment's rows of V are looked through once, for the first and the last NaN and
+// infinity of either sign in every column, and a query row is taken again only where a column's value has no such reason.  (A row of V between the first and the last leaves
+// it open, which counts as none.)
+// place_of(row): packed token * heads + query head, -1: there is none.  shared: AGAIN_SHARED HD + 1 ints; sync: a barrier of those warps.
+constexpr int AGAIN_SHARED = 6;
 template <int HD, int DT, int RT, bool COLS, int WARPS, typename PLACE, typename SYNC>
 __device__ __forceinline__ void chunk_segment_again(const TreeArgs& a, const AgainSeg& g, int warp, int* shared, PLACE place_of, SYNC sync) {
     constexpr int E = HD / 32;
     const int lane = threadIdx.x & 31;
-    for (int c = warp * 32 + lane; c <= 2 * HD; c += WARPS * 32) shared[c] = c < HD ? 0x7fffffff : c < 2 * HD ? -1 : 0;
+    int* any = shared + AGAIN_SHARED * HD;                     // a row of the segment has such a value
+    for (int c = warp * 32 + lane; c <= AGAIN_SHARED * HD; c += WARPS * 32) shared[c] = c == AGAIN_SHARED * HD ? 0 : c / HD % 2 == 0 ? 0x7fffffff : -1;
     sync();
     for (int r = warp; r < g.rows; r += WARPS) {
         const long long place = place_of(r);
-        if (place >= 0 && odd_values<HD, DT, RT, COLS>(a, g, place, r, lane)) shared[2 * HD] = 1;
+        if (place >= 0 && odd_values<HD, DT, RT, COLS>(a, g, place, r, lane)) *any = 1;
     }
     sync();
-    if (!shared[2 * HD]) { sync(); return; }
-    // the first and the last row of V with a NaN, for every column
+    if (!*any) { sync(); return; }
 #pragma unroll 1
     for (int column = g.k0 / PAGE; column * PAGE < g.k1; column++) {
         const int page = chunk_page(a, g.seq, column);
@@ -201,7 +204,10 @@ __device__ __forceinline__ void chunk_segment_again(const TreeArgs& a, const Aga
             const int pos = column * PAGE + j;
 #pragma unroll
             for (int e = 0; e < E; e++)
-                if (v[e] != v[e] && pos < g.k1) { atomicMin(&shared[lane * E + e], pos); atomicMax(&shared[HD + lane * E + e], pos); }
+                if (!is_number(v[e]) && pos < g.k1) {
+                    int* at = shared + (v[e] != v[e] ? 0 : v[e] > 0.f ? 2 : 4) * HD + lane * E + e;
+                    atomicMin(at, pos); atomicMax(at + HD, pos);
+                }
         }
     }
     sync();
@@ -213,15 +219,35 @@ __device__ __forceinline__ void chunk_segment_again(const TreeArgs& a, const Aga
         const int token = (int)(place / a.Hq);
         int lo, hi;
         chunk_sees(a, token, g.n - g.T + token - g.q0, g.n, lo, hi);
+        lo = max(lo, g.k0); hi = min(hi, g.k1);
+        const bool nothing = g.whole ? a.lse && a.lse[place] != a.lse[place] : !is_number(a.ml[g.slot * RT + r].y);
+        if (nothing) continue;                                 // the same in the whole warp
         bool need = false;
+        float value[E];                                        // 0: to be taken again
 #pragma unroll
         for (int e = 0; e < E; e++) {
-            const int first = shared[lane * E + e], last = shared[HD + lane * E + e];
-            const bool seen = (first >= lo && first < hi) || (last >= lo && last < hi);
-            need |= ((bits >> e) & 1u) && !seen;
+            bool sees[3], open[3];
+#pragma unroll
+            for (int k = 0; k < 3; k++) {
+                const int first = shared[2 * k * HD + lane * E + e], last = shared[(2 * k + 1) * HD + lane * E + e];
+                sees[k] = (first >= lo && first < hi) || (last >= lo && last < hi);
+                open[k] = !sees[k] && first < lo && last >= hi;
+            }
+            value[e] = 0.f;
+            if (sees[0]) value[e] = NAN;
+            else if (!open[0] && !open[1] && !open[2]) value[e] = sees[1] ? sees[2] ? NAN : INFINITY : sees[2] ? -INFINITY : 0.f;
+            if (!((bits >> e) & 1u)) value[e] = 0.f;
+            else need |= value[e] == 0.f;
         }
-        const bool nothing = g.whole ? a.lse && a.lse[place] != a.lse[place] : !is_number(a.ml[g.slot * RT + r].y);
-        if (__any_sync(0xffffffffu, need) && !nothing) chunk_row_again<HD, DT, RT, COLS>(a, g, token, (int)(place - (long long)token * a.Hq), r);
+        if (__any_sync(0xffffffffu, need)) chunk_row_again<HD, DT, RT, COLS>(a, g, token, (int)(place - (long long)token * a.Hq), r);
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            if (value[e] == 0.f) continue;
+            const size_t at = (size_t)place * HD + lane * E + e;
+            if (!g.whole) record_part<HD, RT, COLS>(a, g.slot, r, lane)[e] = value[e];
+            else if (DT == DYNAKV_F32) reinterpret_cast<float*>(a.out)[at] = value[e];
+            else reinterpret_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16(value[e]);
+        }
     }
     sync();
 }

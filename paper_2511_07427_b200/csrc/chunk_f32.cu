@@ -9,7 +9,7 @@
 //   warps 0-7      16 query rows each
 // Work is shared out as for the tcgen05 kernel (chunk_plan.cuh).  Weights go through shared memory twice side by side, as the packed products want them.
 // Measured: 2000 tokens of one prompt, 32 heads over 8 of 128, 825 us, 40 TFLOP/s; 3 x 777 with prefixes and distances, 8 heads of 64, 88 us, the FMA pipe busy
-// 56 % of the time: two warps per scheduler wait for their own results and for reads of shared memory.  Rows of 128 spill 152 bytes.
+// 56 % of the time: two warps per scheduler wait for their own results and for reads of shared memory.  Rows of 128 spill 134 bytes.
 #include <cuda.h>
 #include <float.h>
 

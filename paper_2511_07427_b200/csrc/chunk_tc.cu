@@ -40,7 +40,7 @@ namespace dkv {
 constexpr int CT_CONVERT = 128;                                // FP8: threads that turn rows into bf16
 constexpr float CT_LOG2E = 1.4426950408889634f, CT_LN2 = 0.6931471805599453f;
 // The softmax's reference moves when the maximum has outgrown it by 2^24, so that O is rescaled next to never: weights have the range of
-// fp32, and sums of 2^24 rows' weights times V stay below its end up to |V| = 2^79.
+// fp32, and sums of 2^24 rows' weights times V stay below its end up to |V| = 2^79 (what does not is taken again).
 constexpr float CT_LAZY = 24.f;
 
 // ---------------------------------------------------------------------------------- the kernel

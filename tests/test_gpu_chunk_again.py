@@ -203,3 +203,56 @@ def test_values_near_the_end_of_fp32(cache, d, lens, new):
     p.check(*p.run())
     p.check(*p.run(window=500), window=500)
     p.check(*p.run(softcap=3.0), softcap=3.0)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [3, 300])
+@pytest.mark.parametrize("kind", ["causal", "documents", "weights of nothing"])
+def test_which_of_them_a_token_sees(cache, new, kind):
+    """NaN and infinities of both signs in one column, at several rows: the column is what the token sees of them makes it.  Slopes of 30 and 1000 make
+    weights of e^-1000 and less, which are 0 in fp32, and 0 times infinity is NaN: there a column with an infinity may be either."""
+    p = Strict([2000], [new], 4, 2, 64, cache, seed=10)
+    if kind == "documents":
+        p.see(low=lambda b, place, n: place // 50 * 50, high=lambda b, place, n: (place // 50 * 50 + 50).clamp(max=n))
+    if kind == "weights of nothing":
+        p.slopes = torch.tensor([1.0, 4.0, 30.0, 1000.0], device="cuda")
+    marks = [(2000 - new + x * (new - 1) // 12, 11 + x % 3, v) for x, v in enumerate([math.inf, math.inf, math.inf, math.nan, -math.inf, math.inf, math.inf, -math.inf, math.nan, math.inf, math.inf, -math.inf, math.nan])]
+    marks += [(1000, 20, math.inf), (1500, 20, math.inf), (1100, 21, -math.inf), (900, 22, math.nan), (1600, 22, math.inf)]
+    undo = [spoil(p, 0, 1, at, v, [c]) for at, c, v in marks]
+    out, lse = p.run()
+    assert p.c.get_status() == 0
+    held = {}
+    for at, c, v in marks:                                        # the last one written is what a place holds
+        held[at, c] = v
+    want = torch.zeros(new, 64, dtype=torch.float64, device="cuda")
+    for (at, c), v in held.items():
+        want[:, c] += torch.where((p.low <= at) & (at < p.high), v, 0.0)
+    odd = want != 0                                               # NaN != 0 too
+    got = out[:, 2:].double()
+    for h in range(2):
+        x = got[:, h]
+        nothing = kind == "weights of nothing"
+        assert bool(((x == want) | (x.isnan() & (want.isnan() | nothing)))[odd].all()) and bool(torch.isfinite(x[~odd]).all())
+    for u in reversed(undo):
+        u()
+    clean, _ = p.run()
+    out[:, 2:] = torch.where(odd[:, None], clean[:, 2:], out[:, 2:])
+    p.check(out, lse)
+
+
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+def test_a_long_prompt_over_one_odd_row(what):
+    """32768 tokens that nearly all see one row with such a value, in a few of its columns: no query row but those around it is taken again."""
+    p = Strict([32768], [32768], 4, 1, 128, "bf16", seed=11)
+    clean, clean_lse = p.run()
+    spoil(p, 0, 0, 70, what, [5, 6])
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    out, lse = p.run()
+    end.record()
+    torch.cuda.synchronize()
+    assert p.c.get_status() == 0 and begin.elapsed_time(end) < 400
+    seen = out[70:, :, 5:7].float()
+    assert bool((seen.isnan() if math.isnan(what) else seen == what).all()) and torch.equal(lse, clean_lse)
+    out[70:, :, 5:7] = clean[70:, :, 5:7]
+    assert bool(((out.float() - clean.float()).abs() <= 2.0 ** -6 * clean.float().abs() + 2.0 ** -6).all())
